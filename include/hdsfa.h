@@ -47,8 +47,12 @@ typedef enum {
 /* Bits the kernels OR into *dev_status. */
 #define HD_DEVBIT_INDEX 1   /* a token id outside [0, V): hd_expand_embed zeroed its n output
                                rows; hd_expand_embed_bwd left it out of the sums.  A sequence
-                               length outside its range in sfa_decode / sfa_kv_append */
+                               length outside its range in sfa_decode / sfa_kv_append; a length,
+                               page, offset or sequence index outside its range in the paged
+                               and packed calls below */
 #define HD_DEVBIT_TIMEOUT 2 /* a bounded pipeline wait expired; outputs are invalid */
+#define HD_DEVBIT_PAGES 4   /* no page was free for a sequence of hd_pages_grow or a fork of
+                               hd_pages_fork: it was left as it was */
 
 /* Attention mask of one SFA layer (Sec. 2.2, Eq. 4 and Fig. 2). */
 typedef enum {
@@ -268,6 +272,106 @@ hd_status_t sfa_decode(const void* q, const void* k_cache, const void* v_cache, 
  */
 hd_status_t sfa_kv_append(const void* k_new, const void* v_new, void* k_cache, void* v_cache,
                           const int32_t* lens, int B, int Lcap, int n, int Hkv, int Dh,
+                          int32_t* dev_status, cudaStream_t stream);
+
+/*
+ * Paged cache.  K and V rows of many sequences share one pool each (one pair of pools a
+ * layer), cut into pages of P = page_tokens tokens, all n streams of a token together:
+ *   k_pages, v_pages : bf16 [num_pages][P*n][Hkv][Dh]
+ *   page_table       : int32 [B][max_pages], a sequence's pages in order
+ *   lens             : int32 [B], tokens of each sequence (0: an empty slot)
+ * Token t, stream s of sequence b is row (t mod P)*n + s of page page_table[b][t / P].  Any
+ * P >= 1 will do.  A contiguous cache [B][Lcap*n][Hkv][Dh] with P dividing Lcap is a pool
+ * with page_table[b][i] = b*Lcap/P + i.  Entries of a table behind the pages in use are never
+ * looked at, and neither are rows of a page behind its sequence's tokens.
+ * Limits: max_pages*P*n <= 2^30, num_pages*P*n < 2^31, B*max_pages < 2^31.
+ *
+ * sfa_kv_append_paged -- new tokens' K and V rows into the pages: sfa_kv_append for a paged
+ * cache, and for whole prompts.  lens counts the new tokens already.
+ *   offsets NULL: one new token a sequence: N = B, k_new, v_new bf16 [B][n][Hkv][Dh], to
+ *     token lens[b]-1.  A slot with lens[b] = 0 is left out.
+ *   offsets int32 [B+1]: packed rows k_new, v_new bf16 [N*n][Hkv][Dh]; sequence b's new
+ *     tokens are offsets[b] .. offsets[b+1]-1, its last ones: token i goes to token
+ *     lens[b] - offsets[b+1] + i.  Rows before offsets[0] and from offsets[B] on are not
+ *     read.  N = 0 is allowed.
+ * Bit copy.  The pages must be held by the sequence alone.  Rows whose page is not in the
+ * pool, and the rows of a sequence whose offsets descend, leave [0, N] or hold more tokens
+ * than lens[b], are not written and set HD_DEVBIT_INDEX (so does a length outside
+ * [0, max_pages*P]).
+ */
+hd_status_t sfa_kv_append_paged(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                                const int32_t* page_table, const int32_t* lens, const int32_t* offsets, int B, int N,
+                                int num_pages, int page_tokens, int max_pages, int n, int Hkv, int Dh,
+                                int32_t* dev_status, cudaStream_t stream);
+
+/*
+ * sfa_decode_paged -- sfa_decode over a paged cache: the same masks, outputs and limits (Dh,
+ * n*Hq), with the rows found through page_table.  B <= 65535; max_tokens <= max_pages*P.
+ *   An empty slot (lens[b] = 0) gets zero rows and LSE = -inf, and is no error.  A length
+ *   outside [0, max_tokens], or a page that is needed and not in the pool, gives the
+ *   sequence zero rows, LSE = -inf and HD_DEVBIT_INDEX; the others are not affected.
+ *   SFA_LOCAL needs only the pages that the window of the new token's positions touches.
+ *   What a mask hides has no effect, infinities and NaN in it included.
+ *   workspace: >= sfa_decode_paged_workspace_bytes(...) bytes, 16-byte aligned, not shared by
+ *   calls that may run at the same time.
+ */
+size_t sfa_decode_paged_workspace_bytes(int B, int max_tokens, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode,
+                                        int window); /* 0 for invalid sizes */
+hd_status_t sfa_decode_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table,
+                             const int32_t* lens, void* o, float* lse, int B, int max_tokens, int num_pages,
+                             int page_tokens, int max_pages, int n, int Hq, int Hkv, int Dh, float softmax_scale,
+                             sfa_mode_t mode, int window, void* workspace, size_t workspace_bytes,
+                             int32_t* dev_status, cudaStream_t stream);
+
+/*
+ * Who holds which page.  The state is page_table and lens as above and
+ *   refs : int32 [num_pages], the number of sequences that hold each page (0: free).
+ * Start with refs and lens zero.  A sequence of T tokens holds the first ceil(T / P) entries
+ * of its table; the calls keep it so.  Free pages are given out lowest id first, so results
+ * depend on the state alone.  One table serves every layer; the copies that fork and compact
+ * list are to be made in each layer's pools (hd_pages_copy) before the pages are written again.
+ * The calls of one state are to be ordered on one stream; the workspace (>=
+ * hd_pages_workspace_bytes(B, num_pages) bytes, 16-byte aligned) holds nothing between them.
+ * Shared pages are always full, as long as lens only changes through these calls.
+ *
+ * hd_pages_grow : lens[b] += add[b], with the pages for it: sequence b, in ascending order,
+ *   gets them if all that b and those before it ask for are free; else it and its length are
+ *   left as they were (HD_DEVBIT_PAGES).  add[b] < 0, or a length that leaves
+ *   [0, max_pages*P], is left out with HD_DEVBIT_INDEX.
+ * hd_pages_fork : for i < F, the empty slot dst[i] gets the first tokens[i] tokens of src[i]
+ *   (tokens NULL: all of them): floor(tokens/P) pages are shared, the rest of the prefix gets
+ *   a page of its own and copies[i] = (page of src, page of dst), else (-1, -1).  src may name
+ *   a slot many times.  A fork that finds no free page is left out (HD_DEVBIT_PAGES); with
+ *   HD_DEVBIT_INDEX one whose slots are out of range or the same, whose dst is not empty or
+ *   was named by an earlier fork, whose tokens exceed lens[src], or whose pages are not held.
+ *   (A slot that the same call forks to counts as empty as a source.)  F <= B.
+ * hd_pages_free : slots seqs[0 .. F-1] are emptied: lens 0, their table entries -1, one holder
+ *   less for their pages.  An empty slot, or a slot named before, is no error; an index or a
+ *   table entry out of range, or a page that nobody holds, sets HD_DEVBIT_INDEX.
+ * hd_pages_compact : the K pages in use get the ids 0 .. K-1: the j-th page in use with an id
+ *   >= K goes to the j-th free id below K, moves[j] = (old, new); the other moves are
+ *   (-1, -1).  new_refs and new_table (entries behind a sequence's pages -1) may be refs and
+ *   page_table themselves.  moves: int32 [num_pages/2][2].
+ * hd_pages_copy : for i < F, page copies[i][0] onto page copies[i][1] in both pools
+ *   (page_bytes a page, a multiple of 16), as listed above; pairs of negative ids are left
+ *   out, others outside the pool set HD_DEVBIT_INDEX.  No page may be written twice, or
+ *   written and read.
+ * F = 0 is allowed and does nothing.  refs is 16-byte, copies and moves 8-byte aligned.
+ */
+size_t hd_pages_workspace_bytes(int B, int num_pages); /* 0 for invalid sizes */
+hd_status_t hd_pages_grow(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* add, int B, int max_pages,
+                          int num_pages, int page_tokens, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                          cudaStream_t stream);
+hd_status_t hd_pages_fork(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* src, const int32_t* dst,
+                          const int32_t* tokens, int F, int32_t* copies, int B, int max_pages, int num_pages,
+                          int page_tokens, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                          cudaStream_t stream);
+hd_status_t hd_pages_free(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* seqs, int F, int B,
+                          int max_pages, int num_pages, int page_tokens, int32_t* dev_status, cudaStream_t stream);
+hd_status_t hd_pages_compact(const int32_t* refs, const int32_t* page_table, const int32_t* lens, int32_t* new_refs,
+                             int32_t* new_table, int32_t* moves, int B, int max_pages, int num_pages, int page_tokens,
+                             void* workspace, size_t workspace_bytes, int32_t* dev_status, cudaStream_t stream);
+hd_status_t hd_pages_copy(void* k_pages, void* v_pages, const int32_t* copies, int F, int num_pages, size_t page_bytes,
                           int32_t* dev_status, cudaStream_t stream);
 
 /*

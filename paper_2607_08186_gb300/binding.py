@@ -23,6 +23,7 @@ _lib = None
 HD_OK = 0
 HD_DEVBIT_INDEX = 1
 HD_DEVBIT_TIMEOUT = 2
+HD_DEVBIT_PAGES = 4
 
 
 class HdError(RuntimeError):
@@ -71,6 +72,24 @@ def lib():
             L.sfa_decode.argtypes = [P, P, P, P, P, P, I, I, I, I, I, I, I, F, I, I, P, Z, P, P]
             L.sfa_kv_append.restype = I
             L.sfa_kv_append.argtypes = [P, P, P, P, P, I, I, I, I, I, P, P]
+            L.sfa_decode_paged_workspace_bytes.restype = Z
+            L.sfa_decode_paged_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I]
+            L.sfa_decode_paged.restype = I
+            L.sfa_decode_paged.argtypes = [P, P, P, P, P, P, P, I, I, I, I, I, I, I, I, I, F, I, I, P, Z, P, P]
+            L.sfa_kv_append_paged.restype = I
+            L.sfa_kv_append_paged.argtypes = [P, P, P, P, P, P, P, I, I, I, I, I, I, I, I, P, P]
+            L.hd_pages_workspace_bytes.restype = Z
+            L.hd_pages_workspace_bytes.argtypes = [I, I]
+            L.hd_pages_grow.restype = I
+            L.hd_pages_grow.argtypes = [P, P, P, P, I, I, I, I, P, Z, P, P]
+            L.hd_pages_fork.restype = I
+            L.hd_pages_fork.argtypes = [P, P, P, P, P, P, I, P, I, I, I, I, P, Z, P, P]
+            L.hd_pages_free.restype = I
+            L.hd_pages_free.argtypes = [P, P, P, P, I, I, I, I, I, P, P]
+            L.hd_pages_compact.restype = I
+            L.hd_pages_compact.argtypes = [P, P, P, P, P, P, I, I, I, I, P, Z, P, P]
+            L.hd_pages_copy.restype = I
+            L.hd_pages_copy.argtypes = [P, P, P, I, I, Z, P, P]
             L.sfa_fwd.restype = I
             L.sfa_fwd.argtypes = [P, P, P, P, P, I, I, I, I, I, I, F, I, I, P, P]
             L.sfa_bwd_workspace_bytes.restype = Z
@@ -290,6 +309,158 @@ def sfa_kv_append(k_new, v_new, k_cache, v_cache, lens, n, dev_status=None, stre
     Lcap = k_cache.shape[1] // n
     _check(lib().sfa_kv_append(_p(k_new), _p(v_new), _p(k_cache), _p(v_cache), _p(lens), B, Lcap, n, Hkv, Dh,
                                _p(dev_status), _stream(stream)), "sfa_kv_append")
+
+
+# ---- paged cache, pages and packed prompts.  These calls check their tensors: a wrong type,
+# shape, layout or device raises ValueError before anything is enqueued.
+
+def _tensors(stream, *args):
+    """Each of args is (name, tensor, dtype, shape), or None for what the caller left out."""
+    args = [a for a in args if a is not None]
+    for name, t, dtype, shape in args:
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not {t.dtype} "
+                             f"{tuple(t.shape)}{'' if t.is_contiguous() else ' (not contiguous)'}")
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for name, t, _, _ in args:
+        if t.get_device() != dev or dev < 0:
+            raise ValueError(f"{name} is on {t.device}; it must be on the current CUDA device")
+    if stream is not None and stream.device_index != dev:
+        raise ValueError("stream belongs to another device than the current one")
+
+
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+def _opt(name, t, dtype, shape):
+    return None if t is None else (name, t, dtype, shape)
+
+
+def _workspace(ws):
+    if ws is None:
+        raise ValueError("workspace must be a uint8 CUDA tensor")
+    return "workspace", ws, torch.uint8, (ws.numel(),)
+
+
+def _dev_status(st):
+    return None if st is None else ("dev_status", st, _I32, (1,))
+
+
+def _pool_dims(k_pages, page_table, n):
+    """(num_pages, page_tokens, Hkv, Dh, B, max_pages) of a paged cache."""
+    if k_pages.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("k_pages must be [num_pages][page_tokens*n][Hkv][Dh] and page_table [B][max_pages]")
+    pages, rows, Hkv, Dh = k_pages.shape
+    if n < 1 or rows % n:
+        raise ValueError("k_pages.shape[1] must be page_tokens * n")
+    return pages, rows // n, Hkv, Dh, *page_table.shape
+
+
+def sfa_kv_append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, n, offsets=None, dev_status=None, stream=None):
+    """New tokens' K/V rows into a paged cache: pools [num_pages][page_tokens*n][Hkv][Dh] bf16, page_table
+    [B][max_pages] and lens [B] int32 (the new tokens counted).  Without offsets k_new, v_new [B][n][Hkv][Dh] hold one
+    token a sequence (a slot with lens 0 is left out); with offsets [B+1] int32, packed rows [N*n][Hkv][Dh], tokens
+    offsets[b] .. offsets[b+1]-1 are the last ones of sequence b."""
+    pages, P, Hkv, Dh, B, width = _pool_dims(k_pages, page_table, n)
+    if offsets is None:
+        N, shape = B, (B, n, Hkv, Dh)
+    else:
+        N, shape = k_new.shape[0] // n, (k_new.shape[0] // n * n, Hkv, Dh)
+    _tensors(stream, ("k_new", k_new, _BF16, shape), ("v_new", v_new, _BF16, shape),
+             ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
+             ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
+             _opt("offsets", offsets, _I32, (B + 1,)), _dev_status(dev_status))
+    _check(lib().sfa_kv_append_paged(_p(k_new), _p(v_new), _p(k_pages), _p(v_pages), _p(page_table), _p(lens),
+                                     _p(offsets), B, N, pages, P, width, n, Hkv, Dh, _p(dev_status), _stream(stream)),
+           "sfa_kv_append_paged")
+
+
+def sfa_decode_paged_workspace_bytes(B, max_tokens, n, Hq, Hkv, Dh, mode, window=0) -> int:
+    return int(lib().sfa_decode_paged_workspace_bytes(B, max_tokens, n, Hq, Hkv, Dh, int(mode), int(window)))
+
+
+def sfa_decode_paged(q, k_pages, v_pages, page_table, lens, o, n, mode, workspace, max_tokens=None, lse=None,
+                     softmax_scale=0.0, window=0, dev_status=None, stream=None):
+    """sfa_decode over a paged cache (pools, page_table and lens as in sfa_kv_append_paged): q, o [B][n][Hq][Dh] bf16,
+    lse [B][Hq][n] float32 or None.  An empty slot (lens 0) gives zero rows and LSE -inf.  max_tokens bounds every
+    lens[b] (default: what page_table has entries for)."""
+    pages, P, Hkv, Dh, B, width = _pool_dims(k_pages, page_table, n)
+    if q.dim() != 4:
+        raise ValueError("q must be [B][n][Hq][Dh]")
+    Hq = q.shape[2]
+    T = P * width if max_tokens is None else int(max_tokens)
+    _tensors(stream, ("q", q, _BF16, (B, n, Hq, Dh)), ("o", o, _BF16, (B, n, Hq, Dh)),
+             ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
+             ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
+             _opt("lse", lse, _F32, (B, Hq, n)), _workspace(workspace), _dev_status(dev_status))
+    _check(lib().sfa_decode_paged(_p(q), _p(k_pages), _p(v_pages), _p(page_table), _p(lens), _p(o), _p(lse), B, T, pages,
+                                  P, width, n, Hq, Hkv, Dh, float(softmax_scale), int(mode), int(window), _p(workspace),
+                                  _wsb(workspace), _p(dev_status), _stream(stream)), "sfa_decode_paged")
+    return o
+
+
+def hd_pages_workspace_bytes(B, num_pages) -> int:
+    return int(lib().hd_pages_workspace_bytes(B, num_pages))
+
+
+def _page_state(refs, page_table, lens):
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [B][max_pages]")
+    B, width = page_table.shape
+    return B, width, refs.numel(), (("refs", refs, _I32, (refs.numel(),)), ("page_table", page_table, _I32, (B, width)),
+                                    ("lens", lens, _I32, (B,)))
+
+
+def hd_pages_grow(refs, page_table, lens, add, page_tokens, workspace, dev_status=None, stream=None):
+    """lens[b] += add[b], with pages for the new tokens (lowest free ids first, sequences ascending).  refs [num_pages],
+    page_table [B][max_pages], lens, add [B] int32.  A sequence that finds no free page stays as it was and sets
+    HD_DEVBIT_PAGES."""
+    B, width, pages, state = _page_state(refs, page_table, lens)
+    _tensors(stream, *state, ("add", add, _I32, (B,)), _workspace(workspace), _dev_status(dev_status))
+    _check(lib().hd_pages_grow(_p(refs), _p(page_table), _p(lens), _p(add), B, width, pages, int(page_tokens),
+                               _p(workspace), _wsb(workspace), _p(dev_status), _stream(stream)), "hd_pages_grow")
+
+
+def hd_pages_fork(refs, page_table, lens, src, dst, tokens, copies, page_tokens, workspace, dev_status=None, stream=None):
+    """The empty slots dst get the first `tokens` tokens (None: all) of the slots src: full pages are shared, a partly
+    filled last one is new and listed in copies [F][2] (page of src, page of dst; else -1, -1) for hd_pages_copy."""
+    B, width, pages, state = _page_state(refs, page_table, lens)
+    F = src.numel()
+    _tensors(stream, *state, ("src", src, _I32, (F,)), ("dst", dst, _I32, (F,)), _opt("tokens", tokens, _I32, (F,)),
+             ("copies", copies, _I32, (F, 2)), _workspace(workspace), _dev_status(dev_status))
+    _check(lib().hd_pages_fork(_p(refs), _p(page_table), _p(lens), _p(src), _p(dst), _p(tokens), F, _p(copies), B, width,
+                               pages, int(page_tokens), _p(workspace), _wsb(workspace), _p(dev_status), _stream(stream)),
+           "hd_pages_fork")
+    return copies
+
+
+def hd_pages_free(refs, page_table, lens, seqs, page_tokens, dev_status=None, stream=None):
+    """The slots seqs are emptied: lens 0, their entries of page_table -1, their pages held by one sequence less."""
+    B, width, pages, state = _page_state(refs, page_table, lens)
+    _tensors(stream, *state, ("seqs", seqs, _I32, (seqs.numel(),)), _dev_status(dev_status))
+    _check(lib().hd_pages_free(_p(refs), _p(page_table), _p(lens), _p(seqs), seqs.numel(), B, width, pages,
+                               int(page_tokens), _p(dev_status), _stream(stream)), "hd_pages_free")
+
+
+def hd_pages_compact(refs, page_table, lens, new_refs, new_table, moves, page_tokens, workspace, dev_status=None,
+                     stream=None):
+    """The K pages in use get the ids 0 .. K-1 in new_refs and new_table (which may be refs and page_table); moves
+    [num_pages // 2][2] lists the pages to copy (old, new; then -1, -1) for hd_pages_copy."""
+    B, width, pages, state = _page_state(refs, page_table, lens)
+    _tensors(stream, *state, ("new_refs", new_refs, _I32, (pages,)), ("new_table", new_table, _I32, (B, width)),
+             ("moves", moves, _I32, (pages // 2, 2)), _workspace(workspace), _dev_status(dev_status))
+    _check(lib().hd_pages_compact(_p(refs), _p(page_table), _p(lens), _p(new_refs), _p(new_table), _p(moves), B, width,
+                                  pages, int(page_tokens), _p(workspace), _wsb(workspace), _p(dev_status),
+                                  _stream(stream)), "hd_pages_compact")
+    return new_refs, new_table, moves
+
+
+def hd_pages_copy(k_pages, v_pages, copies, dev_status=None, stream=None):
+    """Page copies[i][0] onto page copies[i][1] in both pools (one layer's); pairs of -1 are left out."""
+    _tensors(stream, ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
+             ("copies", copies, _I32, (copies.numel() // 2, 2)), _dev_status(dev_status))
+    _check(lib().hd_pages_copy(_p(k_pages), _p(v_pages), _p(copies), copies.shape[0], k_pages.shape[0],
+                               k_pages[0].numel() * 2, _p(dev_status), _stream(stream)), "hd_pages_copy")
 
 
 SFA_BWD_NOALLOC_MAX_BYTES = 64 << 20

@@ -24,6 +24,26 @@ cudaError_t launch_sfa_decode(const void* q, const void* kc, const void* vc, con
 cudaError_t launch_bounded_wait_selftest(int32_t* status, int32_t* result, cudaStream_t st);
 cudaError_t launch_kv_append(const void* kn, const void* vn, void* kc, void* vc, const int32_t* lens, int B,
                              int Lcap, int n, int Hkv, int Dh, int32_t* status, cudaStream_t st);
+cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* vp, const int32_t* table,
+                                    const int32_t* lens, void* o, float* lse, int B, int maxT, int num_pages, int P,
+                                    int max_pages, int n, int Hq, int Hkv, int Dh, float scale, int mode, int window,
+                                    void* ws, int32_t* status, cudaStream_t st);
+cudaError_t launch_kv_append_paged(const void* kn, const void* vn, void* kp, void* vp, const int32_t* table,
+                                   const int32_t* lens, const int32_t* offsets, int B, int N, int num_pages, int P,
+                                   int max_pages, int n, int Hkv, int Dh, int32_t* status, cudaStream_t st);
+size_t pages_ws_bytes(int B, int num_pages);
+cudaError_t launch_pages_grow(int32_t* refs, int32_t* table, int32_t* lens, const int32_t* add, int B, int max_pages,
+                              int num_pages, int P, void* ws, int32_t* status, cudaStream_t st);
+cudaError_t launch_pages_fork(int32_t* refs, int32_t* table, int32_t* lens, const int32_t* src, const int32_t* dst,
+                              const int32_t* tokens, int F, int32_t* copies, int B, int max_pages, int num_pages, int P,
+                              void* ws, int32_t* status, cudaStream_t st);
+cudaError_t launch_pages_free(int32_t* refs, int32_t* table, int32_t* lens, const int32_t* seqs, int F, int B,
+                              int max_pages, int num_pages, int P, int32_t* status, cudaStream_t st);
+cudaError_t launch_pages_compact(const int32_t* refs, const int32_t* table, const int32_t* lens, int32_t* new_refs,
+                                 int32_t* new_table, int32_t* moves, int B, int max_pages, int num_pages, int P,
+                                 void* ws, int32_t* status, cudaStream_t st);
+cudaError_t launch_pages_copy(void* kp, void* vp, const int32_t* copies, int F, int num_pages, int page16,
+                              int32_t* status, cudaStream_t st);
 cudaError_t launch_sfa_fwd_tc(const void* q, const void* k, const void* v, void* o, float* lse,
                               const SfaGeom& g, int Dh, float scale, int32_t* status, cudaStream_t st);
 cudaError_t launch_sfa_fwd_tc256(const void* q, const void* k, const void* v, void* o, float* lse,
@@ -423,6 +443,156 @@ hd_status_t sfa_kv_append(const void* k_new, const void* v_new, void* k_cache, v
   if ((long long)Lcap * n > (1LL << 30)) return HD_ERR_UNSUPPORTED;
   return cuda_status(hdsfa::launch_kv_append(k_new, v_new, k_cache, v_cache, lens, B, Lcap, n, Hkv, Dh,
                                              dev_status, stream));
+}
+
+// ---- paged cache ----
+static bool aligned_to(const void* p, uintptr_t a) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+static bool aligned_or_null(const void* p, uintptr_t a) { return p == nullptr || aligned_to(p, a); }
+
+// Sizes of a pool and its tables; n = 1 where rows do not matter.
+static hd_status_t page_sizes(int B, int max_pages, int num_pages, int P, int n) {
+  if (B <= 0 || max_pages <= 0 || num_pages <= 0 || P <= 0 || n <= 0) return HD_ERR_INVALID_ARG;
+  const long long prow = (long long)P * n;
+  if (prow > (1LL << 30) || max_pages * prow > (1LL << 30) || num_pages * prow >= (1LL << 31) ||
+      (long long)B * max_pages >= (1LL << 31))
+    return HD_ERR_UNSUPPORTED;
+  return HD_OK;
+}
+
+hd_status_t sfa_kv_append_paged(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                                const int32_t* page_table, const int32_t* lens, const int32_t* offsets, int B, int N,
+                                int num_pages, int page_tokens, int max_pages, int n, int Hkv, int Dh,
+                                int32_t* dev_status, cudaStream_t stream) {
+  HD_NVTX_RANGE("sfa_kv_append_paged");
+  if (!aligned16(k_pages) || !aligned16(v_pages)) return HD_ERR_INVALID_ARG;
+  if (!aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_or_null(offsets, 4) || !aligned_or_null(dev_status, 4))
+    return HD_ERR_INVALID_ARG;
+  if (N < 0 || Hkv <= 0 || Dh <= 0 || Dh % 8 != 0 || (offsets == nullptr && N != B)) return HD_ERR_INVALID_ARG;
+  hd_status_t st = page_sizes(B, max_pages, num_pages, page_tokens, n);
+  if (st != HD_OK) return st;
+  if ((long long)N * n >= (1LL << 31) || (long long)Hkv * Dh > (1LL << 24) || (long long)n * Hkv * Dh > (1LL << 24))
+    return HD_ERR_UNSUPPORTED;
+  if (N == 0) return HD_OK;
+  if (!aligned16(k_new) || !aligned16(v_new)) return HD_ERR_INVALID_ARG;
+  return cuda_status(hdsfa::launch_kv_append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, offsets, B, N,
+                                                   num_pages, page_tokens, max_pages, n, Hkv, Dh, dev_status, stream));
+}
+
+static hd_status_t decode_paged_sizes(int B, int maxT, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode, int window) {
+  hd_status_t st = decode_sizes(B, maxT, maxT, n, Hq, Hkv, Dh, mode, window);
+  if (st != HD_OK) return st;
+  const long long groups = ((long long)n * (Hq / Hkv) + 31) / 32;  // a grid's limits
+  return B > 65535 || Hkv * groups > 65535 ? HD_ERR_UNSUPPORTED : HD_OK;
+}
+
+// A window of every position sees them all: larger ones are cut to it, so that sums of a position
+// and the window stay in 32 bits.
+static int cut_window(sfa_mode_t mode, int window, long long positions) {
+  return mode != SFA_LOCAL ? 0 : window < positions ? window : (int)positions;
+}
+
+size_t sfa_decode_paged_workspace_bytes(int B, int max_tokens, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode,
+                                        int window) {
+  if (decode_paged_sizes(B, max_tokens, n, Hq, Hkv, Dh, mode, window) != HD_OK) return 0;
+  return hdsfa::decode_ws_bytes(hdsfa::decode_plan(B, max_tokens, n, Hq, Hkv, Dh, mode,
+                                                   cut_window(mode, window, (long long)max_tokens * n)));
+}
+
+hd_status_t sfa_decode_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table,
+                             const int32_t* lens, void* o, float* lse, int B, int max_tokens, int num_pages,
+                             int page_tokens, int max_pages, int n, int Hq, int Hkv, int Dh, float softmax_scale,
+                             sfa_mode_t mode, int window, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                             cudaStream_t stream) {
+  HD_NVTX_RANGE("sfa_decode_paged");
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o)) return HD_ERR_INVALID_ARG;
+  if (!aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_or_null(lse, 4) || !aligned_or_null(dev_status, 4))
+    return HD_ERR_INVALID_ARG;
+  hd_status_t st = decode_paged_sizes(B, max_tokens, n, Hq, Hkv, Dh, mode, window);
+  if (st != HD_OK || (st = page_sizes(B, max_pages, num_pages, page_tokens, n)) != HD_OK) return st;
+  if (max_tokens > max_pages * page_tokens) return HD_ERR_INVALID_ARG;
+  const size_t need = sfa_decode_paged_workspace_bytes(B, max_tokens, n, Hq, Hkv, Dh, mode, window);
+  if (!aligned16(workspace) || workspace_bytes < need) return HD_ERR_WORKSPACE;
+  return cuda_status(hdsfa::launch_sfa_decode_paged(
+      q, k_pages, v_pages, page_table, lens, o, lse, B, max_tokens, num_pages, page_tokens, max_pages, n, Hq, Hkv, Dh,
+      resolve_scale(softmax_scale, Dh), (int)mode, cut_window(mode, window, (long long)max_tokens * n), workspace,
+      dev_status, stream));
+}
+
+// ---- who holds which page ----
+static hd_status_t page_state_args(const int32_t* refs, const int32_t* table, const int32_t* lens, int B, int max_pages,
+                                   int num_pages, int P, const int32_t* dev_status) {
+  if (!aligned16(refs) || !aligned_to(table, 4) || !aligned_to(lens, 4) || !aligned_or_null(dev_status, 4))
+    return HD_ERR_INVALID_ARG;
+  return page_sizes(B, max_pages, num_pages, P, 1);
+}
+
+size_t hd_pages_workspace_bytes(int B, int num_pages) {
+  return B <= 0 || num_pages <= 0 ? 0 : hdsfa::pages_ws_bytes(B, num_pages);
+}
+
+hd_status_t hd_pages_grow(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* add, int B, int max_pages,
+                          int num_pages, int page_tokens, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                          cudaStream_t stream) {
+  HD_NVTX_RANGE("hd_pages_grow");
+  hd_status_t st = page_state_args(refs, page_table, lens, B, max_pages, num_pages, page_tokens, dev_status);
+  if (st != HD_OK) return st;
+  if (!aligned_to(add, 4)) return HD_ERR_INVALID_ARG;
+  if (!aligned16(workspace) || workspace_bytes < hd_pages_workspace_bytes(B, num_pages)) return HD_ERR_WORKSPACE;
+  return cuda_status(hdsfa::launch_pages_grow(refs, page_table, lens, add, B, max_pages, num_pages, page_tokens,
+                                              workspace, dev_status, stream));
+}
+
+hd_status_t hd_pages_fork(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* src, const int32_t* dst,
+                          const int32_t* tokens, int F, int32_t* copies, int B, int max_pages, int num_pages,
+                          int page_tokens, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                          cudaStream_t stream) {
+  HD_NVTX_RANGE("hd_pages_fork");
+  hd_status_t st = page_state_args(refs, page_table, lens, B, max_pages, num_pages, page_tokens, dev_status);
+  if (st != HD_OK) return st;
+  if (F < 0 || F > B) return HD_ERR_INVALID_ARG;
+  if (F == 0) return HD_OK;
+  if (!aligned_to(src, 4) || !aligned_to(dst, 4) || !aligned_or_null(tokens, 4) || !aligned_to(copies, 8))
+    return HD_ERR_INVALID_ARG;
+  if (!aligned16(workspace) || workspace_bytes < hd_pages_workspace_bytes(B, num_pages)) return HD_ERR_WORKSPACE;
+  return cuda_status(hdsfa::launch_pages_fork(refs, page_table, lens, src, dst, tokens, F, copies, B, max_pages,
+                                              num_pages, page_tokens, workspace, dev_status, stream));
+}
+
+hd_status_t hd_pages_free(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* seqs, int F, int B,
+                          int max_pages, int num_pages, int page_tokens, int32_t* dev_status, cudaStream_t stream) {
+  HD_NVTX_RANGE("hd_pages_free");
+  hd_status_t st = page_state_args(refs, page_table, lens, B, max_pages, num_pages, page_tokens, dev_status);
+  if (st != HD_OK) return st;
+  if (F < 0) return HD_ERR_INVALID_ARG;
+  if (F == 0) return HD_OK;
+  if (!aligned_to(seqs, 4)) return HD_ERR_INVALID_ARG;
+  return cuda_status(hdsfa::launch_pages_free(refs, page_table, lens, seqs, F, B, max_pages, num_pages, page_tokens,
+                                              dev_status, stream));
+}
+
+hd_status_t hd_pages_compact(const int32_t* refs, const int32_t* page_table, const int32_t* lens, int32_t* new_refs,
+                             int32_t* new_table, int32_t* moves, int B, int max_pages, int num_pages, int page_tokens,
+                             void* workspace, size_t workspace_bytes, int32_t* dev_status, cudaStream_t stream) {
+  HD_NVTX_RANGE("hd_pages_compact");
+  hd_status_t st = page_state_args(refs, page_table, lens, B, max_pages, num_pages, page_tokens, dev_status);
+  if (st != HD_OK) return st;
+  if (!aligned16(new_refs) || !aligned_to(new_table, 4) || !(num_pages < 2 ? true : aligned_to(moves, 8)))
+    return HD_ERR_INVALID_ARG;
+  if (!aligned16(workspace) || workspace_bytes < hd_pages_workspace_bytes(B, num_pages)) return HD_ERR_WORKSPACE;
+  return cuda_status(hdsfa::launch_pages_compact(refs, page_table, lens, new_refs, new_table, moves, B, max_pages,
+                                                 num_pages, page_tokens, workspace, dev_status, stream));
+}
+
+hd_status_t hd_pages_copy(void* k_pages, void* v_pages, const int32_t* copies, int F, int num_pages, size_t page_bytes,
+                          int32_t* dev_status, cudaStream_t stream) {
+  HD_NVTX_RANGE("hd_pages_copy");
+  if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned_or_null(dev_status, 4)) return HD_ERR_INVALID_ARG;
+  if (F < 0 || num_pages <= 0 || page_bytes == 0 || page_bytes % 16 != 0) return HD_ERR_INVALID_ARG;
+  if (page_bytes > (size_t)1 << 34) return HD_ERR_UNSUPPORTED;
+  if (F == 0) return HD_OK;
+  if (!aligned_to(copies, 8)) return HD_ERR_INVALID_ARG;
+  return cuda_status(hdsfa::launch_pages_copy(k_pages, v_pages, copies, F, num_pages, (int)(page_bytes / 16), dev_status,
+                                              stream));
 }
 
 // ---- final-stream problems (Eq. 2 rows; Sec. 3.1 final-stream-only layers) ----

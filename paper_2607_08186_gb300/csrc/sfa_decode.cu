@@ -27,9 +27,19 @@
 // intra-stream layer, the window); rows past the group's query count and positions
 // past the sequence are zero-filled and masked.  A sequence whose length is outside
 // [1, max_tokens] gets zero rows, LSE = -inf and HD_DEVBIT_INDEX.
+//
+// A paged cache (sfa_decode_paged) is read by the same kernels, instantiated with PAGED: a
+// position's row comes from the sequence's page table (page_row) instead of its index.  These
+// instantiations also keep a sequence that holds nothing apart from a bad length, mark a split
+// that meets a bad page, and settle exactly what a product of P and V cannot: a masked key has
+// P = 0, and 0 times an infinity or a NaN in its V row is NaN, so partial rows that come out
+// not finite are computed again from their visible keys alone (exact_row).
+#include <float.h>
+
 #include <algorithm>
 
 #include "decode_plan.cuh"
+#include "pages.cuh"
 #include "tc_common.cuh"
 
 namespace hdsfa {
@@ -67,7 +77,12 @@ struct DecodeArgs {
   int rg;               // query rows per row group (the partials' row pitch)
   float scale_log2;
   FastDiv d_nsplit;
+  const int32_t* table;  // paged: [B][pg.max_pages]; kc, vc are the pools
+  PageGeom pg;
 };
+
+// What a partial's (max, sum) says beyond that: the split met a page that is not in the pool.
+constexpr float kBadPage = -1.f;  // as its sum
 
 // Both kernels are launched early (launch_early's attribute): the decode kernel lets the
 // combine kernel start at once, so the combine's launch and start overlap its tail.
@@ -79,30 +94,73 @@ HD_DEVINLINE void seq_range(const DecodeArgs& a, int T, int& lo, int& hi) {
   lo = a.mode == SFA_LOCAL ? max(0, (T - 1) * a.n - a.window + 1) : 0;
 }
 
+// One row's partial over the visible positions of [k0, k1), by one warp on the fp32 units: lane
+// i holds DH/32 columns.  Only visible rows of K and V are read.
+template <int DH>
+__device__ __noinline__ void exact_row(const DecodeArgs& a, int b, int g, int r, int T, int k0, int k1, float* po,
+                                       float2* pml) {
+  constexpr int C = DH / 32;
+  const int lane = threadIdx.x & 31, s = r / a.G, h = g * a.G + r % a.G, pq = (T - 1) * a.n + s;
+  const bf16* q = a.q + (((long long)b * a.n + s) * a.Hq + h) * DH + lane * C;
+  int p = a.mode == SFA_LOCAL ? max(k0, pq - a.window + 1) : k0, step = 1;
+  if (a.mode == SFA_WITHIN) {
+    step = a.n;
+    p += (s + a.n - p % a.n) % a.n;
+  }
+  float m = -INFINITY, l = 0.f, o[C] = {};
+  for (; p < k1 && p <= pq; p += step) {
+    const int row = page_row(a.pg, a.table + (long long)b * a.pg.max_pages, p);
+    if (row < 0) continue;  // the split is marked bad already
+    const long long off = ((long long)row * a.Hkv + g) * DH + lane * C;
+    float x = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) x += __bfloat162float(q[c]) * __bfloat162float(a.kc[off + c]);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    x *= a.scale_log2;
+    const float mn = fmaxf(m, x), mu = mn == -INFINITY ? 0.f : mn, corr = exp2f(m - mu), w = exp2f(x - mu);
+    m = mn;
+    l = l * corr + w;
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = o[c] * corr + w * __bfloat162float(a.vc[off + c]);
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) po[lane * C + c] = o[c];
+  if (lane == 0) *pml = make_float2(l != l ? INFINITY : m, l);
+}
+
 // Positions [k0, k1) of split c of a sequence of T tokens, in whole tiles of `kt`
 // positions: the sequence's own range over all nsplit splits, not a share of max_tokens, so
 // that a batch of different lengths keeps every CTA busy (16 sequences of 8k to 32k tokens,
 // cross-stream: 815 -> 779 us).  Empty for lengths outside [1, max_tokens] and for splits
 // past the range.  (32-bit with a multiplication for the division: in 64 bits this cost a
 // 30 us step 3 us.)
+// Paged on the tensor cores, the first tile starts at a multiple of ALIGN (its positions before
+// the window are masked), so that no piece of a tile crosses a page.
+template <int ALIGN = 1>
 HD_DEVINLINE void split_range(const DecodeArgs& a, int T, int c, int kt, int& k0, int& k1) {
   k0 = k1 = 0;
   if (T < 1 || T > a.maxT) return;
   int lo, hi;
   seq_range(a, T, lo, hi);
+  lo -= lo % ALIGN;
   const int tiles = (hi - lo + kt - 1) / kt, per = fast_div(tiles + a.nsplit - 1, a.d_nsplit);
   if ((long long)c * per >= tiles) return;
   k0 = lo + c * per * kt;
   k1 = min(k0 + per * kt, hi);
 }
 
-template <int DH, int MT>
+template <int DH, int MT, bool PAGED>
 __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
   constexpr int DS = dsplit<DH>(), KT = ktile<DH>(), KW = 4 / DS, DC = DH / DS;  // DC: O columns per warp
   extern __shared__ __align__(128) uint8_t smem_raw[];
   bf16* sQ = reinterpret_cast<bf16*>(smem_raw);  // [MT*16][DH]
   bf16* sK = sQ + MT * 16 * DH;                   // [STAGES][KT][DH]
   bf16* sV = sK + STAGES * KT * DH;               // [STAGES][KT][DH]
+  // paged: the pool rows of four tiles (of which three are loaded or about to be), -1 for none
+  [[maybe_unused]] int* sRow = reinterpret_cast<int*>(sV + STAGES * KT * DH);
+  [[maybe_unused]] __shared__ int bad_page;
+  [[maybe_unused]] __shared__ unsigned not_finite;  // a bit per row of the merged partial
   constexpr int CPR = DH / 8;
   const int c = blockIdx.x, g = blockIdx.y / a.ngroups, rg = blockIdx.y % a.ngroups, b = blockIdx.z;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, t4 = lane & 3;
@@ -120,6 +178,21 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
     return;
   }
   const long long pbase = (long long)b * a.Lcap * a.n;  // cache row of position 0
+  // paged: pool row of this thread's position of tile `it` (-1 beyond the split)
+  [[maybe_unused]] auto row_of = [&](int it) {
+    const int p = k0 + it * KT + tid;
+    if (tid >= KT || p >= k1) return -1;
+    const int row = page_row(a.pg, a.table + (long long)b * a.pg.max_pages, p);
+    if (row < 0) bad_page = 1;
+    return row;
+  };
+  if constexpr (PAGED) {
+    if (tid == 0) bad_page = 0, not_finite = 0;
+    __syncthreads();
+    const int r0 = row_of(0), r1 = row_of(1), r2 = row_of(2);
+    if (tid < KT) sRow[tid] = r0, sRow[KT + tid] = r1, sRow[2 * KT + tid] = r2;
+    __syncthreads();
+  }
 
   // query rows of the group -> smem (rows past M zero-filled)
   for (int i = tid; i < MT * 16 * CPR; i += NT) {
@@ -129,21 +202,30 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
     cp_async_16(smem_u32(sQ + swz<DH>(rr, cc * 8)), a.q + (((long long)b * a.n + s) * a.Hq + h) * DH + cc * 8,
                 ok);
   }
-  auto load_stage = [&](int st, int kp0) {
+  auto load_stage = [&](int st, int it) {
+    const int kp0 = k0 + it * KT;
     bf16* dK = sK + st * KT * DH;
     bf16* dV = sV + st * KT * DH;
     for (int i = tid; i < KT * CPR; i += NT) {
       const int rr = i / CPR, cc = i % CPR, p = kp0 + rr;
-      const bool ok = p < k1;
-      const long long off = ((pbase + (ok ? p : k0)) * a.Hkv + g) * DH + cc * 8;
+      bool ok;
+      long long off;
+      if constexpr (PAGED) {
+        const int row = sRow[(it & 3) * KT + rr];
+        ok = row >= 0;
+        off = ((long long)(ok ? row : 0) * a.Hkv + g) * DH + cc * 8;
+      } else {
+        ok = p < k1;
+        off = ((pbase + (ok ? p : k0)) * a.Hkv + g) * DH + cc * 8;
+      }
       cp_async_16(smem_u32(dK + swz<DH>(rr, cc * 8)), a.kc + off, ok);
       cp_async_16(smem_u32(dV + swz<DH>(rr, cc * 8)), a.vc + off, ok);
     }
   };
   const int nsub = (k1 - k0 + KT - 1) / KT;
-  load_stage(0, k0);
+  load_stage(0, 0);
   cp_async_commit();
-  if (nsub > 1) load_stage(1, k0 + KT);
+  if (nsub > 1) load_stage(1, 1);
   cp_async_commit();
 
   // this thread's query rows: (mt, half) -> local row mt*16 + g4 + 8*half
@@ -176,8 +258,11 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
   for (int it = 0; it < nsub; ++it) {
     cp_async_wait<STAGES - 2>();  // stage `it` has landed
     __syncthreads();              // ... for every thread, and stage it-1 is no longer read
-    if (it + 2 < nsub) load_stage((it + 2) % STAGES, k0 + (it + 2) * KT);
+    if (it + 2 < nsub) load_stage((it + 2) % STAGES, it + 2);
     cp_async_commit();
+    // the rows that the next iteration loads by are looked up under this one's products
+    [[maybe_unused]] int next_row;
+    if constexpr (PAGED) next_row = row_of(it + 3);
     const bf16* cK = sK + (it % STAGES) * KT * DH;
     const bf16* cV = sV + (it % STAGES) * KT * DH;
 
@@ -273,6 +358,8 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
         mma_bf16_16816(oacc[mt][2 * dp + 1], pa[mt], b2, b3);
       }
     }
+    if constexpr (PAGED)
+      if (tid < KT) sRow[((it + 3) & 3) * KT + tid] = next_row;
   }
 
   // merge the 4 warps' partials in shared memory (the K/V ring is free now)
@@ -319,6 +406,10 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
       l += f * sL[w * MT * 16 + tid];
       sM[w * MT * 16 + tid] = f;
     }
+    if constexpr (PAGED) {
+      if (l != l) m = INFINITY;  // a visible score that is not finite: the combined row is NaN
+      if (bad_page) m = -INFINITY, l = kBadPage;
+    }
     pml[tid] = make_float2(m, l);
   }
   __syncthreads();
@@ -335,6 +426,19 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
       o.w += f * v.w;
     }
     *reinterpret_cast<float4*>(po + row * DH + c4 * 4) = o;
+    if constexpr (PAGED)
+      if (!(fmaxf(fmaxf(fabsf(o.x), fabsf(o.y)), fmaxf(fabsf(o.z), fabsf(o.w))) <= FLT_MAX) ||
+          o.x != o.x || o.y != o.y || o.z != o.z || o.w != o.w)
+        atomicOr(&not_finite, 1u << row);
+  }
+  if constexpr (PAGED) {
+    __syncthreads();
+    if (bad_page) return;  // uniform
+    for (unsigned rows = not_finite, i = 0; rows; rows &= rows - 1, ++i) {
+      const int row = __ffs(rows) - 1;
+      if ((int)(i & 3) == warp && rg * RG + row < a.M)
+        exact_row<DH>(a, b, g, rg * RG + row, T, k0, k1, po + row * DH, pml + row);
+    }
   }
 }
 
@@ -346,7 +450,7 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
 // LSE.  Partials of empty splits are not read into the sum.  (One warp per row and 8
 // columns, its lanes over the splits 1 KB and more apart, took 10.5 us for 19 splits of 384
 // rows of 256 columns and 6.5 us for 37 of 128 rows of 128; this 5.2 and 4.3.)
-template <int DH>
+template <int DH, bool PAGED>
 __global__ void __launch_bounds__(256) combine_kernel(DecodeArgs a) {
   constexpr int LW = DH / 4, SG = 256 / LW, NB = 8;  // column quads, split groups, loads in flight
   static_assert(kMaxSplit <= 256, "one thread per split");
@@ -362,7 +466,8 @@ __global__ void __launch_bounds__(256) combine_kernel(DecodeArgs a) {
   const int r = rg * a.rg + row;
   const int T = a.lens[b];
   const bool valid = T >= 1 && T <= a.maxT;
-  if (!valid && blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) set_status(a.status, HD_DEVBIT_INDEX);
+  if (!valid && !(PAGED && T == 0) && blockIdx.x == 0 && blockIdx.y == 0 && tid == 0)
+    set_status(a.status, HD_DEVBIT_INDEX);
   if (r >= a.M) return;  // the last row group may be short
   const float2 ml = tid < a.nsplit ? a.part_ml[(pidx0 + tid) * a.rg + row] : make_float2(-INFINITY, 0.f);
   float4 x[NB];
@@ -384,7 +489,13 @@ __global__ void __launch_bounds__(256) combine_kernel(DecodeArgs a) {
 #pragma unroll
   for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
   if (lane == 0) red[1][warp] = l;
-  __syncthreads();
+  [[maybe_unused]] int bad = 0;
+  if constexpr (PAGED) {
+    bad = __syncthreads_or(ml.y == kBadPage);
+    if (bad && tid == 0) set_status(a.status, HD_DEVBIT_INDEX);
+  } else {
+    __syncthreads();
+  }
   l = 0.f;
 #pragma unroll
   for (int w = 0; w < 8; ++w) l += red[1][w];
@@ -420,12 +531,13 @@ __global__ void __launch_bounds__(256) combine_kernel(DecodeArgs a) {
       acc.z += v.z;
       acc.w += v.w;
     }
-    const bool ok = valid && l > 0.f;
+    const bool ok = PAGED ? valid && !bad && l != 0.f : valid && l > 0.f;
     const float inv = ok ? 1.f / l : 0.f;
     const int s = r / a.G, h = g * a.G + r % a.G;
     uint2 out;
     out.x = pack_bf16(acc.x * inv, acc.y * inv);
     out.y = pack_bf16(acc.z * inv, acc.w * inv);
+    if (PAGED && !ok) out = make_uint2(0, 0);  // a bad page's other splits may hold anything
     *reinterpret_cast<uint2*>(a.o + (((long long)b * a.n + s) * a.Hq + h) * DH + tid * 4) = out;
     if (tid == 0 && a.lse != nullptr)
       a.lse[((long long)b * a.Hq + h) * a.n + s] = ok ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY;
@@ -500,12 +612,13 @@ struct Smem {
   bf16 ring[NSLOT][2][BN * 64];  // per slot: one K or V half, two [128][64] blocks
   uint64_t q_full, full[NSLOT], empty[NSLOT], s_full[2], p_full[2], pv_done, drain;
   uint32_t tmem_base;
-  int abort;
+  int abort, bad_page;
 };
 
 struct Params {
   CUtensorMap tm_q, tm_k, tm_v;
   dec::DecodeArgs a;
+  int piece;  // paged: rows of a K/V box, a power of two that divides a page's rows and a tile's
 };
 
 // Unit u of the ring sequence K(0), K(1), V(0), K(2), V(1), ..., V(nt-1), two halves per
@@ -528,6 +641,10 @@ HD_DEVINLINE void unit_of(int u, int nt, int& j, int& isv, int& half) {
   isv = 1;
 }
 
+// PAGED: a tile's rows come in pieces of P.piece rows, none of which crosses a page; the warp's
+// lanes look their pages up and issue their loads.  Pieces outside the sequence (or the window)
+// are loaded from behind the pool's last row, which fills them with zeros.
+template <bool PAGED>
 __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_constant__ Params P) {
   const dec::DecodeArgs& a = P.a;
   extern __shared__ uint8_t smem_raw[];
@@ -557,6 +674,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
     mbar_init(&sm.pv_done, 1);
     mbar_init(&sm.drain, 1);
     sm.abort = 0;
+    sm.bad_page = 0;
     fence_mbar_init();
   }
   if (warp == 0) {
@@ -567,7 +685,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
   grid_dep_launch();
   const int T = a.lens[b];
   int k0, k1;
-  dec::split_range(a, T, c, BN, k0, k1);
+  dec::split_range<PAGED ? BN : 1>(a, T, c, BN, k0, k1);
   const int nt = (k1 - k0 + BN - 1) / BN, nunits = 4 * nt;
   tc_fence_before();
   __syncthreads();
@@ -582,19 +700,64 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
-    if (lane == 0) {
+    if constexpr (PAGED) {
+      fence_async_global();  // rows that an earlier kernel stored, before the copies read them
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&sm.q_full, a.M * DH * 2);
+        for (int cb = 0; cb < DH / 64; ++cb) tma_load_4d(sm.q[cb], &P.tm_q, &sm.q_full, cb * 64, g * a.G, 0, b);
+      }
+      const int beyond = a.pg.num_pages * a.pg.prow;
+      const int seen = a.mode == SFA_LOCAL ? (T - 1) * a.n - a.window + 1 : 0;  // first position any row sees
+      int at[2][4];  // pool rows of this lane's pieces, of an even and an odd tile
+      auto look_up = [&](int j, int* x) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int p = (lane + 32 * i) * P.piece, pos = k0 + j * BN + p;
+          x[i] = beyond;
+          if (p >= BN || pos >= k1 || pos + P.piece <= seen) continue;
+          const int row = page_row(a.pg, a.table + (long long)b * a.pg.max_pages, pos);
+          if (row >= 0) x[i] = row;
+          else sm.bad_page = 1;
+        }
+      };
+      int issued = 0;
+      look_up(0, at[0]);
+      look_up(1, at[1]);  // nothing of it where the split has one tile
+      for (int u = 0; u < nunits; ++u, ++issued) {
+        const int slot = u % NSLOT;
+        if (u >= NSLOT &&
+            !__all_sync(0xffffffffu, mbar_wait(&sm.empty[slot], ((u / NSLOT) - 1) & 1, abort, a.status)))
+          break;
+        int j, isv, half;
+        unit_of(u, nt, j, isv, half);
+        const CUtensorMap* tm = isv ? &P.tm_v : &P.tm_k;
+        if (lane == 0) mbar_arrive_expect_tx(&sm.full[slot], BN * 128 * 2);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int p = (lane + 32 * i) * P.piece;
+          if (p >= BN) continue;
+          const int row = (j & 1) ? at[1][i] : at[0][i];
+          tma_load_5d(sm.ring[slot][0] + p * 64, tm, &sm.full[slot], half * 128, g, 0, row, 0);
+          tma_load_5d(sm.ring[slot][1] + p * 64, tm, &sm.full[slot], half * 128 + 64, g, 0, row, 0);
+        }
+        // the rows of tile j + 2, whose K comes after V(j), in the place of tile j's
+        if (isv && half == 1 && j + 2 < nt) {
+          if (j & 1) look_up(j + 2, at[1]);
+          else look_up(j + 2, at[0]);
+        }
+      }
+      if (lane == 0) {
+        mbar_drain(&sm.q_full, 0);
+        for (int u = max(0, issued - NSLOT); u < issued; ++u) mbar_drain(&sm.full[u % NSLOT], (u / NSLOT) & 1);
+      }
+      __syncwarp();
+    } else if (lane == 0) {
       tma_prefetch(&P.tm_q);
       tma_prefetch(&P.tm_k);
       tma_prefetch(&P.tm_v);
       mbar_arrive_expect_tx(&sm.q_full, a.M * DH * 2);
-      for (int cb = 0; cb < DH / 64; ++cb) {
-        asm volatile(
-            "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-            " [%0], [%1, {%3, %4, %5, %6}], [%2];\n" ::"r"(smem_u32(sm.q[cb])),
-            "l"(reinterpret_cast<uint64_t>(&P.tm_q)), "r"(smem_u32(&sm.q_full)), "r"(cb * 64), "r"(g * a.G),
-            "r"(0), "r"(b)
-            : "memory");
-      }
+      for (int cb = 0; cb < DH / 64; ++cb) tma_load_4d(sm.q[cb], &P.tm_q, &sm.q_full, cb * 64, g * a.G, 0, b);
       int issued = 0;
       for (int u = 0; u < nunits; ++u, ++issued) {
         const int slot = u % NSLOT;
@@ -807,11 +970,15 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
       // the partial rows leave through shared memory (the ring is no longer read), 32 columns
       // at a time: 16-byte units XOR-swizzled by the row, then 128 bytes of four rows per store
       uint8_t* stg = reinterpret_cast<uint8_t*>(sm.ring[0][0]) + q4 * 8192;
+      [[maybe_unused]] bool finite = true;
 #pragma unroll 2
       for (int cc = 0; cc < DH / 32; ++cc) {
         uint32_t o[32];
         tmem_ld32(tO + cc * 32, o);
         tmem_ld_wait();
+        if constexpr (PAGED)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) finite = finite && fabsf(__uint_as_float(o[e])) <= FLT_MAX;
         uint8_t* buf = stg + (cc & 1) * 4096;
 #pragma unroll
         for (int u = 0; u < 8; ++u)
@@ -826,7 +993,19 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
                 *reinterpret_cast<const uint4*>(buf + rr * 128 + ((u ^ (rr & 7)) << 4));
         }
       }
-      if (rv) pml[row] = make_float2(m_run * c2, l_run);
+      if constexpr (PAGED) {
+        const bool bad = *(volatile int*)&sm.bad_page != 0;
+        const float m = l_run != l_run ? INFINITY : m_run * c2;
+        if (rv) pml[row] = bad ? make_float2(-INFINITY, dec::kBadPage) : make_float2(m, l_run);
+        // the warp's own stores above come before those of exact_row
+        unsigned rows = __ballot_sync(0xffffffffu, rv && !finite && !bad);
+        for (; rows; rows &= rows - 1) {
+          const int r = q4 * 32 + __ffs(rows) - 1;
+          dec::exact_row<DH>(a, b, g, r, T, k0, k1, po + (size_t)r * DH, pml + r);
+        }
+      } else if (rv) {
+        pml[row] = make_float2(m_run * c2, l_run);
+      }
     }
   }
 
@@ -879,11 +1058,12 @@ DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode
 
 size_t decode_ws_bytes(const DecodePlan& p) { return ((p.part_o_bytes + 255) & ~size_t(255)) + p.part_ml_bytes; }
 
-template <int DH, int MT>
+template <int DH, int MT, bool PAGED>
 static cudaError_t launch_decode_t(const dec::DecodeArgs& a, cudaStream_t st) {
   using namespace dec;
-  const size_t smem = (size_t)(MT * 16 + 2 * STAGES * ktile<DH>()) * DH * sizeof(bf16);
-  cudaError_t e = cudaFuncSetAttribute(decode_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const size_t smem = (size_t)(MT * 16 + 2 * STAGES * ktile<DH>()) * DH * sizeof(bf16) +
+                      (PAGED ? 4 * ktile<DH>() * sizeof(int) : 0);
+  cudaError_t e = cudaFuncSetAttribute(decode_kernel<DH, MT, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute pdl[1];
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -895,14 +1075,15 @@ static cudaError_t launch_decode_t(const dec::DecodeArgs& a, cudaStream_t st) {
   cfg.stream = st;
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, decode_kernel<DH, MT>, a);
+  e = cudaLaunchKernelEx(&cfg, decode_kernel<DH, MT, PAGED>, a);
   if (e != cudaSuccess) return e;
   cfg.gridDim = dim3(std::min(a.rg, a.M), a.Hkv * a.ngroups, a.B);
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, combine_kernel<DH>, a);
+  return cudaLaunchKernelEx(&cfg, combine_kernel<DH, PAGED>, a);
 }
 
+template <bool PAGED>
 static cudaError_t launch_decode_tc(const dec::DecodeArgs& a, cudaStream_t st) {
   using namespace dectc;
   Params p;
@@ -916,11 +1097,17 @@ static cudaError_t launch_decode_tc(const dec::DecodeArgs& a, cudaStream_t st) {
   gk.Lv = a.Lcap * a.n;
   gk.ns = 1;
   gk.rs = 1;
-  if (!make_qgroup_tmap(&p.tm_q, a.q, a.B, a.n, a.Hq, DH, a.G) || !make_rows_tmap(&p.tm_k, a.kc, gk, a.Hkv, DH, BN) ||
-      !make_rows_tmap(&p.tm_v, a.vc, gk, a.Hkv, DH, BN))
+  p.piece = BN;
+  if (PAGED) {  // the pool as one problem of all its rows
+    gk.B = 1;
+    gk.nL = gk.Lv = a.pg.num_pages * a.pg.prow;
+    p.piece = std::min(BN, a.pg.prow & -a.pg.prow);
+  }
+  if (!make_qgroup_tmap(&p.tm_q, a.q, a.B, a.n, a.Hq, DH, a.G) ||
+      !make_rows_tmap(&p.tm_k, a.kc, gk, a.Hkv, DH, p.piece) || !make_rows_tmap(&p.tm_v, a.vc, gk, a.Hkv, DH, p.piece))
     return cudaErrorInvalidValue;
   const int smem = (int)sizeof(Smem) + 1024;
-  cudaError_t e = cudaFuncSetAttribute(decode_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(decode_tc_kernel<PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute pdl[1];
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -932,48 +1119,70 @@ static cudaError_t launch_decode_tc(const dec::DecodeArgs& a, cudaStream_t st) {
   cfg.stream = st;
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, decode_tc_kernel, p);
+  e = cudaLaunchKernelEx(&cfg, decode_tc_kernel<PAGED>, p);
   if (e != cudaSuccess) return e;
   cfg.gridDim = dim3(a.M, a.Hkv, a.B);
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, dec::combine_kernel<DH>, a);
+  return cudaLaunchKernelEx(&cfg, dec::combine_kernel<DH, PAGED>, a);
 }
 
-cudaError_t launch_sfa_decode(const void* q, const void* kc, const void* vc, const int32_t* lens, void* o,
-                              float* lse, int B, int maxT, int Lcap, int n, int Hq, int Hkv, int Dh, float scale,
-                              int mode, int window, void* ws, int32_t* status, cudaStream_t st) {
-  const DecodePlan p = decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window);
-  dec::DecodeArgs a;
+template <bool PAGED>
+static cudaError_t launch_decode(dec::DecodeArgs& a, int Dh, float scale, void* ws, cudaStream_t st) {
+  const DecodePlan p = decode_plan(a.B, a.maxT, a.n, a.Hq, a.Hkv, Dh, a.mode, a.window);
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + ((p.part_o_bytes + 255) & ~size_t(255)));
+  a.G = p.G;
+  a.M = p.M;
+  a.ngroups = p.ngroups;
+  a.nsplit = p.nsplit;
+  a.rg = p.rg;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.d_nsplit = make_fast_div((uint32_t)p.nsplit);
+  if (p.tc) return launch_decode_tc<PAGED>(a, st);
+  const bool two = p.M > 16;  // a row group of more than 16 rows takes two m16 tiles
+  if (Dh == 64) return two ? launch_decode_t<64, 2, PAGED>(a, st) : launch_decode_t<64, 1, PAGED>(a, st);
+  if (Dh == 256) return two ? launch_decode_t<256, 2, PAGED>(a, st) : launch_decode_t<256, 1, PAGED>(a, st);
+  return two ? launch_decode_t<128, 2, PAGED>(a, st) : launch_decode_t<128, 1, PAGED>(a, st);
+}
+
+static dec::DecodeArgs decode_args(const void* q, const void* kc, const void* vc, const int32_t* lens, void* o,
+                                   float* lse, int B, int maxT, int n, int Hq, int Hkv, int mode, int window,
+                                   int32_t* status) {
+  dec::DecodeArgs a = {};
   a.q = (const bf16*)q;
   a.kc = (const bf16*)kc;
   a.vc = (const bf16*)vc;
   a.lens = lens;
   a.o = (bf16*)o;
   a.lse = lse;
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + ((p.part_o_bytes + 255) & ~size_t(255)));
   a.status = status;
   a.B = B;
-  a.Lcap = Lcap;
   a.maxT = maxT;
   a.n = n;
   a.Hq = Hq;
   a.Hkv = Hkv;
-  a.G = p.G;
-  a.M = p.M;
-  a.ngroups = p.ngroups;
-  a.nsplit = p.nsplit;
-  a.rg = p.rg;
   a.mode = mode;
   a.window = window;
-  a.scale_log2 = scale * 1.4426950408889634f;
-  a.d_nsplit = make_fast_div((uint32_t)p.nsplit);
-  if (p.tc) return launch_decode_tc(a, st);
-  const bool two = p.M > 16;  // a row group of more than 16 rows takes two m16 tiles
-  if (Dh == 64) return two ? launch_decode_t<64, 2>(a, st) : launch_decode_t<64, 1>(a, st);
-  if (Dh == 256) return two ? launch_decode_t<256, 2>(a, st) : launch_decode_t<256, 1>(a, st);
-  return two ? launch_decode_t<128, 2>(a, st) : launch_decode_t<128, 1>(a, st);
+  return a;
+}
+
+cudaError_t launch_sfa_decode(const void* q, const void* kc, const void* vc, const int32_t* lens, void* o,
+                              float* lse, int B, int maxT, int Lcap, int n, int Hq, int Hkv, int Dh, float scale,
+                              int mode, int window, void* ws, int32_t* status, cudaStream_t st) {
+  dec::DecodeArgs a = decode_args(q, kc, vc, lens, o, lse, B, maxT, n, Hq, Hkv, mode, window, status);
+  a.Lcap = Lcap;
+  return launch_decode<false>(a, Dh, scale, ws, st);
+}
+
+cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* vp, const int32_t* table,
+                                    const int32_t* lens, void* o, float* lse, int B, int maxT, int num_pages, int P,
+                                    int max_pages, int n, int Hq, int Hkv, int Dh, float scale, int mode, int window,
+                                    void* ws, int32_t* status, cudaStream_t st) {
+  dec::DecodeArgs a = decode_args(q, kp, vp, lens, o, lse, B, maxT, n, Hq, Hkv, mode, window, status);
+  a.table = table;
+  a.pg = make_page_geom(num_pages, max_pages, P * n);
+  return launch_decode<true>(a, Dh, scale, ws, st);
 }
 
 cudaError_t launch_kv_append(const void* kn, const void* vn, void* kc, void* vc, const int32_t* lens, int B,

@@ -86,6 +86,14 @@ HD_DEVINLINE void tma_load_5d(void* dst, const CUtensorMap* m, uint64_t* bar, in
       : "memory");
 }
 
+HD_DEVINLINE void tma_load_4d(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1, int c2, int c3) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5, %6}], [%2];\n" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+
 // 1-D bulk copy global -> shared (16-byte aligned, size a multiple of 16).
 HD_DEVINLINE void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile(
@@ -109,6 +117,7 @@ HD_DEVINLINE void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
 }
 HD_DEVINLINE void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
 HD_DEVINLINE void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
+HD_DEVINLINE void fence_async_global() { asm volatile("fence.proxy.async.global;\n" ::: "memory"); }
 HD_DEVINLINE void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
 
 // D[tmem] (+)= A * B, bf16 inputs, fp32 accumulate; B from shared memory, A from shared
