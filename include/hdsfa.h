@@ -275,6 +275,25 @@ hd_status_t sfa_kv_append(const void* k_new, const void* v_new, void* k_cache, v
                           int32_t* dev_status, cudaStream_t stream);
 
 /*
+ * sfa_fwd_packed -- sfa_fwd over B whole prompts of different lengths, packed one behind
+ * another without padding: sequence b's tokens are offsets[b] .. offsets[b+1]-1 of N, its
+ * positions count from its own first token, and no query sees another sequence's keys.
+ *   q, o : bf16 [N*n][Hq][Dh]      k, v : bf16 [N*n][Hkv][Dh]      lse : float32 [Hq][N*n]
+ *   offsets : int32 device array [B+1], 0 <= offsets[0] <= ... <= offsets[B] <= N.
+ * Sequences of no tokens are allowed; rows of o and lse before offsets[0] and from offsets[B]
+ * on are left as they were, and q, k, v there may hold anything.  Offsets that descend or leave
+ * [0, N] write nothing and set HD_DEVBIT_INDEX.  What a mask hides has no effect, infinities and
+ * NaN in it included.  Masks, limits and head dims are those of sfa_fwd with B = 1 and L = N
+ * (no SFA_WITHIN_NAIVE); forward only.
+ * workspace: >= sfa_fwd_packed_workspace_bytes(...) bytes, 16-byte aligned (the list of query
+ * tiles, built by each call), not shared by calls that may run at the same time.
+ */
+size_t sfa_fwd_packed_workspace_bytes(int B, int N, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode); /* 0 for invalid sizes */
+hd_status_t sfa_fwd_packed(const void* q, const void* k, const void* v, void* o, float* lse, const int32_t* offsets,
+                           int B, int N, int n, int Hq, int Hkv, int Dh, float softmax_scale, sfa_mode_t mode, int window,
+                           void* workspace, size_t workspace_bytes, int32_t* dev_status, cudaStream_t stream);
+
+/*
  * Paged cache.  K and V rows of many sequences share one pool each (one pair of pools a
  * layer), cut into pages of P = page_tokens tokens, all n streams of a token together:
  *   k_pages, v_pages : bf16 [num_pages][P*n][Hkv][Dh]

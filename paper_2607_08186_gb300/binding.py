@@ -72,6 +72,10 @@ def lib():
             L.sfa_decode.argtypes = [P, P, P, P, P, P, I, I, I, I, I, I, I, F, I, I, P, Z, P, P]
             L.sfa_kv_append.restype = I
             L.sfa_kv_append.argtypes = [P, P, P, P, P, I, I, I, I, I, P, P]
+            L.sfa_fwd_packed_workspace_bytes.restype = Z
+            L.sfa_fwd_packed_workspace_bytes.argtypes = [I, I, I, I, I, I, I]
+            L.sfa_fwd_packed.restype = I
+            L.sfa_fwd_packed.argtypes = [P, P, P, P, P, P, I, I, I, I, I, I, F, I, I, P, Z, P, P]
             L.sfa_decode_paged_workspace_bytes.restype = Z
             L.sfa_decode_paged_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I]
             L.sfa_decode_paged.restype = I
@@ -344,6 +348,29 @@ def _workspace(ws):
 
 def _dev_status(st):
     return None if st is None else ("dev_status", st, _I32, (1,))
+
+
+def sfa_fwd_packed_workspace_bytes(B, N, n, Hq, Hkv, Dh, mode) -> int:
+    return int(lib().sfa_fwd_packed_workspace_bytes(B, N, n, Hq, Hkv, Dh, int(mode)))
+
+
+def sfa_fwd_packed(q, k, v, o, lse, offsets, n, mode, workspace, softmax_scale=0.0, window=0, dev_status=None, stream=None):
+    """sfa_fwd over whole prompts of different lengths, packed: q, o [N*n][Hq][Dh], k, v [N*n][Hkv][Dh] bf16, lse
+    [Hq][N*n] float32; sequence b holds tokens offsets[b] .. offsets[b+1]-1 (int32 [B+1], ascending, within [0, N]).
+    Rows outside [offsets[0], offsets[B]) are left as they were."""
+    if q.dim() != 3 or k.dim() != 3 or offsets.dim() != 1:
+        raise ValueError("q must be [N*n][Hq][Dh], k [N*n][Hkv][Dh] and offsets [B+1]")
+    rows, Hq, Dh = q.shape
+    Hkv, B = k.shape[1], offsets.shape[0] - 1
+    if n < 1 or rows % n:
+        raise ValueError("q.shape[0] must be N * n")
+    _tensors(stream, ("q", q, _BF16, (rows, Hq, Dh)), ("k", k, _BF16, (rows, Hkv, Dh)), ("v", v, _BF16, (rows, Hkv, Dh)),
+             ("o", o, _BF16, (rows, Hq, Dh)), ("lse", lse, _F32, (Hq, rows)), ("offsets", offsets, _I32, (B + 1,)),
+             _workspace(workspace), _dev_status(dev_status))
+    _check(lib().sfa_fwd_packed(_p(q), _p(k), _p(v), _p(o), _p(lse), _p(offsets), B, rows // n, n, Hq, Hkv, Dh,
+                                float(softmax_scale), int(mode), int(window), _p(workspace), _wsb(workspace),
+                                _p(dev_status), _stream(stream)), "sfa_fwd_packed")
+    return o, lse
 
 
 def _pool_dims(k_pages, page_table, n):

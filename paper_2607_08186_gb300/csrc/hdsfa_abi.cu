@@ -7,6 +7,7 @@
 #include "common.cuh"
 #include "decode_plan.cuh"
 #include "nvtx_range.h"
+#include "packed.cuh"
 
 namespace hdsfa {
 cudaError_t launch_expand_embed(const void* tables, const int32_t* ids, void* out, int B, int L,
@@ -48,6 +49,12 @@ cudaError_t launch_sfa_fwd_tc(const void* q, const void* k, const void* v, void*
                               const SfaGeom& g, int Dh, float scale, int32_t* status, cudaStream_t st);
 cudaError_t launch_sfa_fwd_tc256(const void* q, const void* k, const void* v, void* o, float* lse,
                                  const SfaGeom& g, float scale, int32_t* status, cudaStream_t st);
+cudaError_t launch_sfa_fwd_packed_tc(const void* q, const void* k, const void* v, void* o, float* lse, const SfaGeom& g,
+                                     int Dh, float scale, const PackedList& list, long long max_items, int32_t* status,
+                                     cudaStream_t st);
+cudaError_t launch_sfa_fwd_packed_tc256(const void* q, const void* k, const void* v, void* o, float* lse,
+                                        const SfaGeom& g, float scale, const PackedList& list, long long max_items,
+                                        int32_t* status, cudaStream_t st);
 cudaError_t launch_sfa_bwd_prep(const void* o, const void* dout, const float* lse, float* lse2_ws,
                                 float* delta_ws, float* dq_ws, const SfaGeom& g, int Dh,
                                 cudaStream_t st, bool zero = true);
@@ -67,6 +74,8 @@ cudaError_t launch_sfa_bwd_finalize(void* dq, const float* dq_ws, const SfaGeom&
 namespace {
 
 bool aligned16(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned_to(const void* p, uintptr_t a) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool aligned_or_null(const void* p, uintptr_t a) { return p == nullptr || aligned_to(p, a); }
 
 // Validates sizes shared by sfa_fwd / sfa_bwd and builds the virtual-problem geometry.
 
@@ -445,10 +454,54 @@ hd_status_t sfa_kv_append(const void* k_new, const void* v_new, void* k_cache, v
                                              dev_status, stream));
 }
 
-// ---- paged cache ----
-static bool aligned_to(const void* p, uintptr_t a) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-static bool aligned_or_null(const void* p, uintptr_t a) { return p == nullptr || aligned_to(p, a); }
+// ---- packed prompts ----
+// Geometry of N packed tokens (one sequence of them, of which the kernels take pieces), rows of a
+// CTA's query tile and the most tiles there can be.
+static hd_status_t packed_sizes(int B, int N, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode, int window, SfaGeom* g,
+                                int* tile_rows, long long* max_items) {
+  if (B <= 0) return HD_ERR_INVALID_ARG;
+  hd_status_t st = make_geom(1, N, n, Hq, Hkv, Dh, mode, window, g);
+  if (st != HD_OK) return st;
+  if (mode == SFA_WITHIN_NAIVE) return HD_ERR_UNSUPPORTED;
+  const bool pairs = (Hq / Hkv) % 2 == 0;  // two heads' tiles to a CTA (or pair), else two tiles of a head
+  *tile_rows = pairs ? 128 : 256;
+  *max_items = hdsfa::packed_max_items(B, N, n / g->ns, *tile_rows);
+  // a grid's limit, in CTAs (pairs at head dim 256)
+  if (*max_items * (pairs ? Hq / 2 : Hq) * g->ns >= (1LL << 30)) return HD_ERR_UNSUPPORTED;
+  return HD_OK;
+}
 
+size_t sfa_fwd_packed_workspace_bytes(int B, int N, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode) {
+  SfaGeom g;
+  int rows;
+  long long items;
+  if (packed_sizes(B, N, n, Hq, Hkv, Dh, mode, mode == SFA_LOCAL ? 1 : 0, &g, &rows, &items) != HD_OK) return 0;
+  return (size_t)(items + 1) * sizeof(hdsfa::PackedItem);
+}
+
+hd_status_t sfa_fwd_packed(const void* q, const void* k, const void* v, void* o, float* lse, const int32_t* offsets,
+                           int B, int N, int n, int Hq, int Hkv, int Dh, float softmax_scale, sfa_mode_t mode, int window,
+                           void* workspace, size_t workspace_bytes, int32_t* dev_status, cudaStream_t stream) {
+  HD_NVTX_RANGE("sfa_fwd_packed");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(lse)) return HD_ERR_INVALID_ARG;
+  if (!aligned_to(offsets, 4) || !aligned_or_null(dev_status, 4)) return HD_ERR_INVALID_ARG;
+  SfaGeom g;
+  int rows;
+  long long items;
+  hd_status_t st = packed_sizes(B, N, n, Hq, Hkv, Dh, mode, window, &g, &rows, &items);
+  if (st != HD_OK) return st;
+  if (!aligned16(workspace) || workspace_bytes < (size_t)(items + 1) * sizeof(hdsfa::PackedItem)) return HD_ERR_WORKSPACE;
+  int32_t* count = static_cast<int32_t*>(workspace);
+  hdsfa::PackedItem* list = static_cast<hdsfa::PackedItem*>(workspace) + 1;
+  cudaError_t e = hdsfa::launch_packed_plan(offsets, B, N, n / g.ns, rows, list, count, dev_status, stream);
+  if (e != cudaSuccess) return cuda_status(e);
+  const float scale = resolve_scale(softmax_scale, Dh);
+  const hdsfa::PackedList pl{list, count};
+  if (Dh == 256) return cuda_status(hdsfa::launch_sfa_fwd_packed_tc256(q, k, v, o, lse, g, scale, pl, items, dev_status, stream));
+  return cuda_status(hdsfa::launch_sfa_fwd_packed_tc(q, k, v, o, lse, g, Dh, scale, pl, items, dev_status, stream));
+}
+
+// ---- paged cache ----
 // Sizes of a pool and its tables; n = 1 where rows do not matter.
 static hd_status_t page_sizes(int B, int max_pages, int num_pages, int P, int n) {
   if (B <= 0 || max_pages <= 0 || num_pages <= 0 || P <= 0 || n <= 0) return HD_ERR_INVALID_ARG;

@@ -34,11 +34,10 @@
 // that meets a bad page, and settle exactly what a product of P and V cannot: a masked key has
 // P = 0, and 0 times an infinity or a NaN in its V row is NaN, so partial rows that come out
 // not finite are computed again from their visible keys alone (exact_row).
-#include <float.h>
-
 #include <algorithm>
 
 #include "decode_plan.cuh"
+#include "packed.cuh"
 #include "pages.cuh"
 #include "tc_common.cuh"
 
@@ -101,32 +100,19 @@ __device__ __noinline__ void exact_row(const DecodeArgs& a, int b, int g, int r,
                                        float2* pml) {
   constexpr int C = DH / 32;
   const int lane = threadIdx.x & 31, s = r / a.G, h = g * a.G + r % a.G, pq = (T - 1) * a.n + s;
-  const bf16* q = a.q + (((long long)b * a.n + s) * a.Hq + h) * DH + lane * C;
   int p = a.mode == SFA_LOCAL ? max(k0, pq - a.window + 1) : k0, step = 1;
   if (a.mode == SFA_WITHIN) {
     step = a.n;
     p += (s + a.n - p % a.n) % a.n;
   }
-  float m = -INFINITY, l = 0.f, o[C] = {};
-  for (; p < k1 && p <= pq; p += step) {
-    const int row = page_row(a.pg, a.table + (long long)b * a.pg.max_pages, p);
-    if (row < 0) continue;  // the split is marked bad already
-    const long long off = ((long long)row * a.Hkv + g) * DH + lane * C;
-    float x = 0.f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) x += __bfloat162float(q[c]) * __bfloat162float(a.kc[off + c]);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    x *= a.scale_log2;
-    const float mn = fmaxf(m, x), mu = mn == -INFINITY ? 0.f : mn, corr = exp2f(m - mu), w = exp2f(x - mu);
-    m = mn;
-    l = l * corr + w;
-#pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = o[c] * corr + w * __bfloat162float(a.vc[off + c]);
-  }
+  const int end = min(k1, pq + 1), keys = p < end ? (end - p + step - 1) / step : 0;
+  float o[C], m, l;
+  visible_row<DH>(a.q + (((long long)b * a.n + s) * a.Hq + h) * DH, a.kc + g * DH, a.vc + g * DH, (long long)a.Hkv * DH,
+                  keys, [&](int i) { return (long long)page_row(a.pg, a.table + (long long)b * a.pg.max_pages, p + i * step); },
+                  a.scale_log2, o, m, l);
 #pragma unroll
   for (int c = 0; c < C; ++c) po[lane * C + c] = o[c];
-  if (lane == 0) *pml = make_float2(l != l ? INFINITY : m, l);
+  if (lane == 0) *pml = make_float2(m, l);
 }
 
 // Positions [k0, k1) of split c of a sequence of T tokens, in whole tiles of `kt`

@@ -91,6 +91,22 @@ def test_page_calls_refusals(lib):
     assert [fork(F=0, src=z, copies=z, ws=z), free(F=0, seqs=z), copy(F=0, c=z)] == [0] * 3
 
 
+def _packed(lib, B=2, N=40, n=2, Hq=4, Hkv=2, Dh=64, mode=0, window=0, ptr=FAKE, off=FAKE, ws=FAKE, ws_bytes=1 << 40, status=0):
+    return lib.sfa_fwd_packed(P_(ptr), P_(ptr), P_(ptr), P_(ptr), P_(ptr), P_(off), B, N, n, Hq, Hkv, Dh, 0.0, mode, window,
+                              P_(ws), ws_bytes, P_(status), None)
+
+
+def test_packed_refusals(lib):
+    for bad in (dict(B=0), dict(N=0), dict(n=0), dict(Hq=5), dict(mode=7), dict(mode=2), dict(ptr=FAKE + 8), dict(ptr=0),
+                dict(off=0), dict(off=FAKE + 2), dict(status=FAKE + 1)):
+        assert _packed(lib, **bad) == 1, bad
+    for bad in (dict(Dh=96), dict(Dh=128, mode=3), dict(N=1 << 30), dict(N=1 << 27, Hq=64)):
+        assert _packed(lib, **bad) == 2, bad
+    need = binding.sfa_fwd_packed_workspace_bytes(2, 40, 2, 4, 2, 64, 0)
+    assert need > 0 and binding.sfa_fwd_packed_workspace_bytes(2, 0, 2, 4, 2, 64, 0) == 0
+    assert _packed(lib, ws=0) == 4 and _packed(lib, ws=FAKE + 8) == 4 and _packed(lib, ws_bytes=need - 1) == 4
+
+
 def _cpu_pool(pages=6, P=8, n=2, Hkv=2, Dh=64):
     return torch.zeros(pages, P * n, Hkv, Dh, dtype=torch.bfloat16)
 
@@ -128,6 +144,17 @@ def test_binding_refuses_wrong_tensors(lib):
     assert "k_new" in append(torch.zeros(3, 1, 2, 64, dtype=torch.bfloat16))
     assert "k_new" in append(torch.zeros(7, 2, 64, dtype=torch.bfloat16), offsets=torch.zeros(4, dtype=i32))
     assert "offsets" in append(torch.zeros(8, 2, 64, dtype=torch.bfloat16), offsets=torch.zeros(3, dtype=i32))
+    p = torch.zeros(8, 4, 64, dtype=torch.bfloat16)
+    off, lse = torch.zeros(3, dtype=i32), torch.zeros(4, 8)
+
+    def packed(q=p, k=p, v=p, o=p, lse=lse, off=off, n=2, ws=ws):
+        with pytest.raises(ValueError) as e:
+            binding.sfa_fwd_packed(q, k, v, o, lse, off, n, 0, ws)
+        return str(e.value)
+
+    assert "CUDA" in packed() and "lse" in packed(lse=lse.double()) and "offsets" in packed(off=off.long())
+    assert "v must" in packed(v=p[:4]) and "o must" in packed(o=p.float()) and "N * n" in packed(n=3)
+    assert "q must" in packed(q=p[0]) and "workspace" in packed(ws=None)
     refs = torch.zeros(6, dtype=i32)
     for call in (lambda: binding.hd_pages_grow(refs, table, lens, lens[:2], 8, ws),
                  lambda: binding.hd_pages_grow(refs, table, lens, lens, 8, ws),  # on the host
