@@ -320,17 +320,22 @@ def sfa_kv_append(k_new, v_new, k_cache, v_cache, lens, n, dev_status=None, stre
 
 def _tensors(stream, *args):
     """Each of args is (name, tensor, dtype, shape), or None for what the caller left out."""
-    args = [a for a in args if a is not None]
-    for name, t, dtype, shape in args:
-        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not {t.dtype} "
-                             f"{tuple(t.shape)}{'' if t.is_contiguous() else ' (not contiguous)'}")
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    for name, t, _, _ in args:
-        if t.get_device() != dev or dev < 0:
-            raise ValueError(f"{name} is on {t.device}; it must be on the current CUDA device")
+    dev = args[0][1].get_device()  # -1: not on a CUDA device
+    for a in args:
+        if a is not None and not (a[1].dtype is a[2] and a[1].shape == a[3] and a[1].is_contiguous()
+                                  and a[1].get_device() == dev):
+            _refuse(dev, *a)
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"{args[0][0]} is on {args[0][1].device}; it must be on the current CUDA device")
     if stream is not None and stream.device_index != dev:
         raise ValueError("stream belongs to another device than the current one")
+
+
+def _refuse(dev, name, t, dtype, shape):
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        raise ValueError(f"{name} is on {t.device}; all tensors must be on the current CUDA device")
+    raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not {t.dtype} "
+                     f"{tuple(t.shape)}{'' if t.is_contiguous() else ' (not contiguous)'}")
 
 
 _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32

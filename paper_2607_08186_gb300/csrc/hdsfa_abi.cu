@@ -455,19 +455,18 @@ hd_status_t sfa_kv_append(const void* k_new, const void* v_new, void* k_cache, v
 }
 
 // ---- packed prompts ----
-// Geometry of N packed tokens (one sequence of them, of which the kernels take pieces), rows of a
-// CTA's query tile and the most tiles there can be.
+// Geometry of N packed tokens (one sequence of them, of which the kernels take pieces), rows of an
+// entry of their list and the most entries there can be.
 static hd_status_t packed_sizes(int B, int N, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode, int window, SfaGeom* g,
                                 int* tile_rows, long long* max_items) {
   if (B <= 0) return HD_ERR_INVALID_ARG;
   hd_status_t st = make_geom(1, N, n, Hq, Hkv, Dh, mode, window, g);
   if (st != HD_OK) return st;
   if (mode == SFA_WITHIN_NAIVE) return HD_ERR_UNSUPPORTED;
-  const bool pairs = (Hq / Hkv) % 2 == 0;  // two heads' tiles to a CTA (or pair), else two tiles of a head
-  *tile_rows = pairs ? 128 : 256;
+  *tile_rows = (Hq / Hkv) % 2 == 0 ? 128 : 256;  // two query tiles: of two heads, or of one
   *max_items = hdsfa::packed_max_items(B, N, n / g->ns, *tile_rows);
-  // a grid's limit, in CTAs (pairs at head dim 256)
-  if (*max_items * (pairs ? Hq / 2 : Hq) * g->ns >= (1LL << 30)) return HD_ERR_UNSUPPORTED;
+  // the entries of every head and stream are counted in 32 bits
+  if (*max_items * Hq * g->ns >= (1LL << 30)) return HD_ERR_UNSUPPORTED;
   return HD_OK;
 }
 
@@ -493,7 +492,7 @@ hd_status_t sfa_fwd_packed(const void* q, const void* k, const void* v, void* o,
   if (!aligned16(workspace) || workspace_bytes < (size_t)(items + 1) * sizeof(hdsfa::PackedItem)) return HD_ERR_WORKSPACE;
   int32_t* count = static_cast<int32_t*>(workspace);
   hdsfa::PackedItem* list = static_cast<hdsfa::PackedItem*>(workspace) + 1;
-  cudaError_t e = hdsfa::launch_packed_plan(offsets, B, N, n / g.ns, rows, list, count, dev_status, stream);
+  cudaError_t e = hdsfa::launch_packed_plan(offsets, B, N, n / g.ns, rows, g.window, list, count, dev_status, stream);
   if (e != cudaSuccess) return cuda_status(e);
   const float scale = resolve_scale(softmax_scale, Dh);
   const hdsfa::PackedList pl{list, count};

@@ -1,20 +1,17 @@
-// The list of query tiles of packed prompts.  One CTA: it is a few KB of work that every layer of
-// a batch repeats, under the start of the attention kernel (about 4 us alone).
+// The list of query tiles of packed prompts.  One CTA: a few KB of work that starts while the kernel
+// before it ends, and under which the attention kernel starts (about 4 us alone).
 #include "packed.cuh"
 
 namespace hdsfa {
 namespace packed {
 constexpr int NT = 1024;
 
-// Sequences by number of tiles, most first: one class each up to 511 tiles, then one for 512.
-HD_DEVINLINE int size_class(int tiles) { return NT - 1 - (tiles < 512 ? tiles : min(NT - 1, 512 + (tiles >> 9))); }
-
-// items: every sequence's tiles, its last (the most keys) first; classes in order of size, so that
-// the longest work starts first and the shortest ends the launch.  Which sequence of a class comes
-// first depends on the atomics and changes no result.  Offsets that descend or leave [0, N] make no
-// items at all.
+// items: every sequence's tiles, by their number of key tiles, most first (a counting sort by the
+// tile's number, capped where the window or the number of classes ends the growth), so that the long
+// ones start first and the short ones fill the end.  The order within a class depends on the atomics
+// and changes no result.  Offsets that descend or leave [0, N] make no items at all.
 __global__ void __launch_bounds__(NT) packed_plan_kernel(const int32_t* offsets, int B, int N, int mult, FastDiv d_tile,
-                                                         int tile_rows, PackedItem* items, int32_t* count,
+                                                         int tile_rows, int top, PackedItem* items, int32_t* count,
                                                          int32_t* status) {
   __shared__ int place[NT], sums[32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -30,11 +27,23 @@ __global__ void __launch_bounds__(NT) packed_plan_kernel(const int32_t* offsets,
     }
     return;
   }
-  auto tiles_of = [&](int b) { return fast_div((offsets[b + 1] - offsets[b]) * mult + tile_rows - 1, d_tile); };
-  for (int b = tid; b < B; b += NT) {
-    const int t = tiles_of(b);
-    if (t > 0) atomicAdd(place + size_class(t), t);
-  }
+  // f(first row, rows, tile) for every tile: a thread takes its sequences' first tiles, its warp the rest
+  auto for_tiles = [&](auto f) {
+    constexpr int OWN = 8;
+    for (int b0 = 0; b0 < B; b0 += NT) {
+      const int b = b0 + tid;
+      const int first = b < B ? offsets[b] * mult : 0, rows = b < B ? offsets[b + 1] * mult - first : 0;
+      const int tiles = fast_div(rows + tile_rows - 1, d_tile);
+      for (int t = 0; t < min(tiles, OWN); ++t) f(first, rows, t);
+      for (unsigned more = __ballot_sync(0xffffffffu, tiles > OWN); more; more &= more - 1) {
+        const int l = __ffs(more) - 1, fl = __shfl_sync(0xffffffffu, first, l), rl = __shfl_sync(0xffffffffu, rows, l),
+                  tl = __shfl_sync(0xffffffffu, tiles, l);
+        for (int t = OWN + lane; t < tl; t += 32) f(fl, rl, t);
+      }
+    }
+  };
+  auto place_of = [&](int tile) { return place + NT - 1 - min(tile, top); };
+  for_tiles([&](int, int, int t) { atomicAdd(place_of(t), 1); });
   __syncthreads();
   const int mine = place[tid];  // exclusive prefix sum over the classes
   int x = mine;
@@ -50,21 +59,15 @@ __global__ void __launch_bounds__(NT) packed_plan_kernel(const int32_t* offsets,
   place[tid] = before + x - mine;
   if (tid == NT - 1) *count = before + x;
   __syncthreads();
-  for (int b = warp; b < B; b += NT / 32) {
-    const int t = tiles_of(b);
-    if (t == 0) continue;
-    int at = lane == 0 ? atomicAdd(place + size_class(t), t) : 0;
-    at = __shfl_sync(0xffffffffu, at, 0);
-    const int first = offsets[b] * mult, rows = (offsets[b + 1] - offsets[b]) * mult;
-    for (int i = lane; i < t; i += 32) items[at + i] = PackedItem{first, rows, t - 1 - i, 0};
-  }
+  for_tiles([&](int first, int rows, int t) { items[atomicAdd(place_of(t), 1)] = PackedItem{first, rows, t, 0}; });
 }
 }  // namespace packed
 
-cudaError_t launch_packed_plan(const int32_t* offsets, int B, int N, int mult, int tile_rows, PackedItem* items,
-                               int32_t* count, int32_t* status, cudaStream_t st) {
+cudaError_t launch_packed_plan(const int32_t* offsets, int B, int N, int mult, int tile_rows, int window,
+                               PackedItem* items, int32_t* count, int32_t* status, cudaStream_t st) {
+  const int top = window > 0 && window / tile_rows < packed::NT - 2 ? window / tile_rows + 1 : packed::NT - 1;
   return launch_early(packed::packed_plan_kernel, dim3(1), packed::NT, st, offsets, B, N, mult,
-                      make_fast_div((uint32_t)tile_rows), tile_rows, items, count, status);
+                      make_fast_div((uint32_t)tile_rows), tile_rows, top, items, count, status);
 }
 
 }  // namespace hdsfa

@@ -13,15 +13,77 @@ struct PackedItem {
   int first, rows, tile, unused;
 };
 struct PackedList {
-  const PackedItem* items;  // the longest sequences' tiles first, each sequence's last tile first
+  const PackedItem* items;  // those with the most key tiles first
   const int32_t* count;
 };
 // Items that `tokens` packed tokens of B sequences make at most: sum of ceil(rows / tile_rows).
 inline long long packed_max_items(int B, int tokens, int mult, int tile_rows) {
   return (long long)tokens * mult / tile_rows + (B < tokens ? B : tokens);
 }
-cudaError_t launch_packed_plan(const int32_t* offsets, int B, int N, int mult, int tile_rows, PackedItem* items,
-                               int32_t* count, int32_t* status, cudaStream_t st);
+cudaError_t launch_packed_plan(const int32_t* offsets, int B, int N, int mult, int tile_rows, int window,
+                               PackedItem* items, int32_t* count, int32_t* status, cudaStream_t st);
+
+// What the forward kernels over packed prompts are given besides their tensor maps.
+struct PackedArgs {
+  const __nv_bfloat16 *q, *k, *v;
+  __nv_bfloat16* o;
+  float* lse;
+  SfaGeom g;  // of all packed rows: B = 1, Lv = Lq = rows of a stream's problem
+  PackedList list;
+  float scale_log2;
+  int32_t* status;
+  int head_pairs;  // 1: an entry's two query tiles are the same rows of two heads of one K/V group,
+                   // 0: two tiles of a head
+  int o_wide;      // o is 32-byte aligned
+  int per;         // places of a list entry: head slots x streams
+  FastDiv d_per, d_ns, d_grp;  // by per, streams, query heads of a K/V head
+};
+inline PackedArgs make_packed_args(const void* q, const void* k, const void* v, void* o, float* lse, const SfaGeom& g,
+                                   float scale, const PackedList& list, int32_t* status) {
+  PackedArgs a;
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.k = static_cast<const __nv_bfloat16*>(k);
+  a.v = static_cast<const __nv_bfloat16*>(v);
+  a.o = static_cast<__nv_bfloat16*>(o);
+  a.lse = lse;
+  a.g = g;
+  a.list = list;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.status = status;
+  a.head_pairs = (g.Hq / g.Hkv) % 2 == 0;
+  a.o_wide = (reinterpret_cast<uintptr_t>(o) & 31) == 0;
+  a.per = (a.head_pairs ? g.Hq / 2 : g.Hq) * g.q_ns;
+  a.d_per = make_fast_div((uint32_t)a.per);
+  a.d_ns = make_fast_div((uint32_t)g.q_ns);
+  a.d_grp = make_fast_div((uint32_t)(g.Hq / g.Hkv));
+  return a;
+}
+
+// The work at place `pos` of the list (every entry stands for all head slots and streams).
+struct PackedEntry {
+  int first, rows;  // the sequence's first row and its rows
+  int m0, head, stream;
+  HD_DEVINLINE PackedEntry(const PackedArgs& a, int pos) {
+    const int i = fast_div(pos, a.d_per);
+    const PackedItem it = a.list.items[i];
+    const int hs = pos - i * a.per, hx = fast_div(hs, a.d_ns);
+    first = it.first;
+    rows = it.rows;
+    stream = hs - hx * a.g.q_ns;
+    head = a.head_pairs ? 2 * hx : hx;
+    m0 = it.tile * (a.head_pairs ? 128 : 256);
+  }
+  HD_DEVINLINE int head_of(const PackedArgs& a, int g) const { return a.head_pairs ? head + g : head; }
+  HD_DEVINLINE int row0(const PackedArgs& a, int g) const { return a.head_pairs ? m0 : m0 + g * 128; }
+};
+// Key tiles of 128 [lo, hi] of the query tile at row r0 (hi < lo: no rows).
+HD_DEVINLINE int packed_lo(const PackedArgs& a, int r0) { return a.g.window > 0 ? max(0, r0 - a.g.window + 1) / 128 : 0; }
+HD_DEVINLINE int packed_hi(int r0, int rows) { return r0 >= rows ? -1 : (min(r0 + 128, rows) - 1) / 128; }
+// The place of the k-th piece of work of one of `workers`: the list in rounds of one place each,
+// every second round backwards, which evens out the descending sizes.
+HD_DEVINLINE int packed_place(int k, int worker, int workers) {
+  return k * workers + ((k & 1) ? workers - 1 - worker : worker);
+}
 
 // One query row against its visible key rows alone, by one warp on the fp32 units: row(i) is the
 // tensor row of the i-th visible key, q, k and v start at the head; o: DH/32 columns a lane, not

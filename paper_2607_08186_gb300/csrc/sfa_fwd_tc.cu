@@ -47,17 +47,6 @@
 // Slower: one issuer per group (459 us: the groups' MMAs interleave and their softmaxes
 // meet on the SFU), the tile waits inside the S batch (440 us) or between the halves of P
 // (454 us), two single-tile CTAs per SM (463 us: K and V are loaded twice).
-//
-// Packed prompts (PACKED): the CTAs' query tiles come from a list (PackedItem) instead of the grid
-// alone; a tile's rows and keys are those of its own sequence, a run of rows of the packed tensors.
-// A key tile that reaches past its sequence holds rows of the next one, or memory behind the last:
-// their scores are masked like later keys, and their V rows, which 0 of P would not silence if they
-// held an infinity or a NaN, are zeroed in shared memory.  Later keys of the own sequence that are
-// not finite are rare; rows that come out not finite with such keys about are computed again
-// (visible_row).
-#include <type_traits>
-
-#include "packed.cuh"
 #include "tc_common.cuh"
 
 namespace hdsfa {
@@ -93,8 +82,6 @@ struct Params {
   int32_t* status;
   int head_pairs;  // 1: a CTA's two query tiles are the same rows of two heads of one K/V group
   FastDiv d_rank, d_hns, d_ns, d_grp;
-  PackedList list;        // packed prompts
-  const bf16 *q, *k, *v;  // their tensors, for rows that are computed again
 };
 
 // Key-tile range [lo, hi] of the query tile starting at row m0 (hi < lo: no rows).
@@ -113,7 +100,7 @@ HD_DEVINLINE void tile_range(const SfaGeom& G, int m0, int& lo, int& hi) {
 // NAIVE: the naive intra-stream schedule (G.smod > 1): every tile is masked, a pair
 // also needing key row = query row (mod smod); its own instantiation, so the other
 // modes' softmax carries none of that code.
-template <int DH, bool NAIVE, bool PACKED>
+template <int DH, bool NAIVE>
 __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant__ Params P) {
   constexpr int NSLOT = Smem<DH>::NSLOT;
   extern __shared__ uint8_t smem_raw[];
@@ -127,17 +114,8 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant_
     }
   }
   Smem<DH>& sm = *reinterpret_cast<Smem<DH>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  std::conditional_t<PACKED, SfaGeom, const SfaGeom&> G = P.g;
+  const SfaGeom& G = P.g;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  [[maybe_unused]] PackedItem item = {};
-  if constexpr (PACKED) {  // first: the grid may hold many more CTAs than there are items
-    if (gridDim.x <= kSmCount) grid_dep_launch();
-    grid_dep_wait();
-    const int i = fast_div((int)blockIdx.x, P.d_rank);
-    item = P.list.items[i];  // the list has room for every i of the grid
-    if (i >= *P.list.count) return;
-    G.Lv = G.Lq = item.rows;
-  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < NSLOT; ++i) {
       mbar_init(&sm.full[i], 1);
@@ -159,7 +137,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant_
     tmem_relinquish();
     tc_fence_before();
   }
-  if constexpr (!PACKED) attn_dep_wait(1);
+  attn_dep_wait(1);
   // A CTA's two query tiles: with head_pairs the same 128 rows of heads 2x and 2x+1
   // (one K/V group: both tiles see exactly the same key tiles and finish together),
   // else rows m0 and m0 + 128 of one head (the second tile sees one more key tile).
@@ -171,8 +149,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant_
   // visit) of every head, stream and batch launch first
   const int per_rank = nh * G.q_ns * G.B;
   const int rank = fast_div((int)blockIdx.x, P.d_rank);
-  const int mt = PACKED ? item.tile : ncta - 1 - rank, hsb = (int)blockIdx.x - rank * per_rank;
-  const int base = PACKED ? item.first : 0;  // row of the tensors at which the virtual rows start
+  const int mt = ncta - 1 - rank, hsb = (int)blockIdx.x - rank * per_rank;
   const int b = fast_div(hsb, P.d_hns), hs = hsb - b * nh * G.q_ns;
   const int hx = fast_div(hs, P.d_ns), s = hs - hx * G.q_ns;
   int qm[NG], hd[NG];  // first query row and head of each group's tile
@@ -221,7 +198,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant_
           return;
         }
         mbar_arrive_expect_tx(&sm.full[slot], BN * DH * 2);
-        const int row = base + (j > hi[0] ? j + gap : j) * BN;
+        const int row = (j > hi[0] ? j + gap : j) * BN;
         for (int c = 0; c < DH / 64; ++c)
           tma_load_5d(sm.ring[slot] + c * BN * 64, tm, &sm.full[slot], c * 64, kvh, sk, row, b);
         ++issued;
@@ -233,7 +210,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant_
       auto load_q = [&](int g) {
         mbar_arrive_expect_tx(&sm.q_full[g], BM * DH * 2);
         for (int c = 0; c < DH / 64; ++c)
-          tma_load_5d(sm.q[g] + c * BM * 64, &P.tm_q, &sm.q_full[g], c * 64, hd[g], s, base + qm[g], b);
+          tma_load_5d(sm.q[g] + c * BM * 64, &P.tm_q, &sm.q_full[g], c * 64, hd[g], s, qm[g], b);
       };
       load_q(0);
       if (n_lo <= n_hi) load_tile(&P.tm_k, n_lo);
@@ -396,20 +373,6 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant_
       const float m_use = rescale ? m_new : m_run;
       const float neg = (m_use == -INFINITY) ? 0.f : -m_use * c2;
       const uint64_t c2x2 = f2pack(c2, c2), neg2 = f2pack(neg, neg);
-      if constexpr (PACKED) {
-        if (kb + BN > G.Lv) {  // V rows behind the sequence (zeroed by both groups where both read them)
-          const int u = 2 * (j - n_lo) + 1, slot = u % NSLOT;
-          if (!__all_sync(0xffffffffu, mbar_wait(&sm.full[slot], (u / NSLOT) & 1, abort, P.status))) {
-            ok = false;
-            break;
-          }
-          for (int e = (G.Lv - kb) * 8 + row; e < BN * 8; e += 128)
-#pragma unroll
-            for (int c = 0; c < DH / 64; ++c)
-              reinterpret_cast<uint4*>(sm.ring[slot] + c * BN * 64)[e] = make_uint4(0, 0, 0, 0);
-          fence_async_smem();
-        }
-      }
       // P (bf16 pairs) over the first 64 columns of this group's S, published in halves
       uint64_t sum2[4] = {0, 0, 0, 0};
       const bool mine = rescale && m_run != -INFINITY && i > 0;
@@ -463,15 +426,11 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant_
       // DH = 128), instead of one 16-byte piece of 32 different rows.
       constexpr int UPR = DH * 2 / 16;  // 16-byte units per row
       uint8_t* stg = reinterpret_cast<uint8_t*>(sm.q[g]) + q4 * (32 * DH * 2);
-      [[maybe_unused]] bool finite = true;
 #pragma unroll
       for (int c = 0; c < DH / 32; ++c) {
         uint32_t o[32];
         tmem_ld32(tO + c * 32, o);
         tmem_ld_wait();
-        if constexpr (PACKED)
-#pragma unroll
-          for (int e = 0; e < 32; ++e) finite = finite && fabsf(__uint_as_float(o[e])) <= FLT_MAX;
 #pragma unroll
         for (int e = 0; e < 32; e += 8) {
           uint4 w;
@@ -486,7 +445,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant_
       __syncwarp();
       {
         const long long rstride = (long long)G.q_rs * G.Hq * DH;  // elements between query rows
-        bf16* obase = P.o + (((long long)b * G.q_nL + s) * G.Hq + hg) * DH + (long long)base * rstride;
+        bf16* obase = P.o + (((long long)b * G.q_nL + s) * G.Hq + hg) * DH;
         const int r0 = qm[g] + q4 * 32;  // this warp's first row
 #pragma unroll
         for (int i = 0; i < 32 * UPR / 32; ++i) {
@@ -496,18 +455,8 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant_
                 *reinterpret_cast<const uint4*>(stg + rr * (DH * 2) + ((u ^ (rr & 7)) << 4));
         }
       }
-      float* lse_row = P.lse + ((long long)b * G.Hq + hg) * G.q_nL + (long long)(base + r) * G.q_rs + s;
-      if (r < G.Lq) *lse_row = (m_run * c2 + log2f(l_run)) * kLn2;
-      if constexpr (PACKED) {
-        const unsigned again = __ballot_sync(0xffffffffu, r < G.Lq && !finite);
-        if (again) {
-          const long long kp = (long long)G.rs * G.Hkv * DH, first = ((long long)base * G.rs + s) * G.Hkv * DH + kvh * DH;
-          recompute_rows<DH>(P.q + ((long long)base * G.rs + s) * G.Hq * DH + hg * DH, P.k + first, P.v + first, kp,
-                             P.o + ((long long)base * G.rs + s) * G.Hq * DH + hg * DH, (long long)G.rs * G.Hq * DH,
-                             lse_row - (long long)lane * G.rs, G.rs, r - lane, again, lo[g] * BN, min((hi[g] + 1) * BN, G.Lv),
-                             G.window, c2);
-        }
-      }
+      if (r < G.Lq)
+        P.lse[((long long)b * G.Hq + hg) * G.q_nL + (long long)r * G.q_rs + s] = (m_run * c2 + log2f(l_run)) * kLn2;
     }
   }
 
@@ -522,27 +471,25 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_kernel(const __grid_constant_
 }  // namespace tcfwd
 
 // --------------------------------------------------------------------- host
-template <int DH, bool NAIVE, bool PACKED>
-static cudaError_t tc_fwd_impl(tcfwd::Params& p, cudaStream_t st, long long max_items = 0) {
+template <int DH, bool NAIVE>
+static cudaError_t tc_fwd_impl(tcfwd::Params& p, cudaStream_t st) {
   constexpr int smem = tcfwd::smem_bytes<DH>();
   cudaError_t e =
-      cudaFuncSetAttribute(tcfwd::fwd_kernel<DH, NAIVE, PACKED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      cudaFuncSetAttribute(tcfwd::fwd_kernel<DH, NAIVE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const int rows_per_cta = p.head_pairs ? tcfwd::BM : tcfwd::NG * tcfwd::BM;
   const int nh = p.head_pairs ? p.g.Hq / tcfwd::NG : p.g.Hq;
-  const unsigned ranks = PACKED ? (unsigned)max_items : (unsigned)((p.g.Lq + rows_per_cta - 1) / rows_per_cta);
-  const unsigned grid = ranks * (unsigned)(nh * p.g.q_ns * p.g.B);
-  if (PACKED)
-    return launch_kernel(true, tcfwd::fwd_kernel<DH, NAIVE, PACKED>, dim3(grid), tcfwd::NTHREADS, smem, st, p);
-  return launch_attn(tcfwd::fwd_kernel<DH, NAIVE, PACKED>, grid, tcfwd::NTHREADS, smem, st, p);
+  const unsigned grid = (unsigned)((p.g.Lq + rows_per_cta - 1) / rows_per_cta) * (unsigned)(nh * p.g.q_ns * p.g.B);
+  return launch_attn(tcfwd::fwd_kernel<DH, NAIVE>, grid, tcfwd::NTHREADS, smem, st, p);
 }
 
-static bool make_params(tcfwd::Params& p, const void* q, const void* k, const void* v, void* o, float* lse,
-                        const SfaGeom& g, int Dh, float scale, int32_t* status) {
+cudaError_t launch_sfa_fwd_tc(const void* q, const void* k, const void* v, void* o, float* lse,
+                              const SfaGeom& g, int Dh, float scale, int32_t* status, cudaStream_t st) {
+  tcfwd::Params p;
   if (!make_rows_tmap(&p.tm_q, q, query_geom(g), g.Hq, Dh, tcfwd::BM) ||
       !make_rows_tmap(&p.tm_k, k, g, g.Hkv, Dh, tcfwd::BN) ||
       !make_rows_tmap(&p.tm_v, v, g, g.Hkv, Dh, tcfwd::BN))
-    return false;
+    return cudaErrorInvalidValue;
   p.o = (bf16*)o;
   p.lse = lse;
   p.g = g;
@@ -554,27 +501,8 @@ static bool make_params(tcfwd::Params& p, const void* q, const void* k, const vo
   p.d_hns = make_fast_div((uint32_t)(nh * g.q_ns));
   p.d_ns = make_fast_div((uint32_t)g.q_ns);
   p.d_grp = make_fast_div((uint32_t)(g.Hq / g.Hkv));
-  return true;
-}
-
-cudaError_t launch_sfa_fwd_tc(const void* q, const void* k, const void* v, void* o, float* lse,
-                              const SfaGeom& g, int Dh, float scale, int32_t* status, cudaStream_t st) {
-  tcfwd::Params p = {};
-  if (!make_params(p, q, k, v, o, lse, g, Dh, scale, status)) return cudaErrorInvalidValue;
-  if (Dh == 64) return tc_fwd_impl<64, false, false>(p, st);
-  return g.smod > 1 ? tc_fwd_impl<128, true, false>(p, st) : tc_fwd_impl<128, false, false>(p, st);
-}
-
-cudaError_t launch_sfa_fwd_packed_tc(const void* q, const void* k, const void* v, void* o, float* lse, const SfaGeom& g,
-                                     int Dh, float scale, const PackedList& list, long long max_items, int32_t* status,
-                                     cudaStream_t st) {
-  tcfwd::Params p = {};
-  if (!make_params(p, q, k, v, o, lse, g, Dh, scale, status)) return cudaErrorInvalidValue;
-  p.list = list;
-  p.q = (const bf16*)q;
-  p.k = (const bf16*)k;
-  p.v = (const bf16*)v;
-  return Dh == 64 ? tc_fwd_impl<64, false, true>(p, st, max_items) : tc_fwd_impl<128, false, true>(p, st, max_items);
+  if (Dh == 64) return tc_fwd_impl<64, false>(p, st);
+  return g.smod > 1 ? tc_fwd_impl<128, true>(p, st) : tc_fwd_impl<128, false>(p, st);
 }
 
 }  // namespace hdsfa

@@ -30,13 +30,6 @@
 // streams: WITHIN 607 -> 499 us, final-stream CROSS 488 -> 411 us.
 // Every mbarrier wait is bounded; copies still in flight when a wait gives up were issued
 // a whole timeout (about a second) earlier.
-//
-// Packed prompts (PACKED): as in the forward of the smaller head dims, a pair's query tiles come
-// from a list, and the V rows of a sequence's last key tile that lie behind it are zeroed.  Each CTA
-// loads its half of that V tile on a barrier of its own (v_tail), since its own threads write it.
-#include <type_traits>
-
-#include "packed.cuh"
 #include "tc_common.cuh"
 
 namespace hdsfa {
@@ -59,7 +52,7 @@ struct Smem {
   // S(t) and PV(t) complete: by t mod 4, since the producer, which takes them as the release
   // of K(t) and V(t), may be up to two tiles late
   uint64_t s_full[4], pv_done[4];
-  uint64_t full[NSLOT], q_full[DH / 64], p_full[2][2], o_done, v_tail;
+  uint64_t full[NSLOT], q_full[DH / 64], p_full[2][2], o_done;
   uint32_t tmem_base;
   int abort;
 };
@@ -76,11 +69,8 @@ struct Params {
   int32_t* status;
   int head_pairs;  // 1: a pair's two query tiles are the same rows of two heads of one K/V group
   FastDiv d_rank, d_hns, d_ns, d_grp;
-  PackedList list;        // packed prompts
-  const bf16 *q, *k, *v;  // their tensors, for rows that are computed again
 };
 
-template <bool PACKED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_kernel(const __grid_constant__ Params P) {
   extern __shared__ uint8_t smem_raw[];
   {
@@ -93,18 +83,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
     }
   }
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  std::conditional_t<PACKED, SfaGeom, const SfaGeom&> G = P.g;
+  const SfaGeom& G = P.g;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)(blockIdx.x & 1);  // = %cluster_ctarank
-  [[maybe_unused]] PackedItem listed = {};
-  if constexpr (PACKED) {  // first: the grid may hold many more pairs than there are items
-    if (gridDim.x <= kSmCount) grid_dep_launch();
-    grid_dep_wait();
-    const int i = fast_div((int)(blockIdx.x >> 1), P.d_rank);
-    listed = P.list.items[i];  // the list has room for every i of the grid
-    if (i >= *P.list.count) return;  // both CTAs of the pair
-    G.Lv = G.Lq = listed.rows;
-  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < NSLOT; ++i) mbar_init(&sm.full[i], 1);
     for (int i = 0; i < 4; ++i) {
@@ -117,7 +98,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
       mbar_init(&sm.p_full[i][1], 16);
     }
     mbar_init(&sm.o_done, 1);
-    mbar_init(&sm.v_tail, 1);
     sm.abort = 0;
     fence_mbar_init();
   }
@@ -130,14 +110,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
     tmem_alloc_pair(&sm.tmem_base, 512);
     tc_fence_before();
   }
-  if constexpr (!PACKED) attn_dep_wait(1);
+  attn_dep_wait(1);
   // linear grid of pairs, query-tile rank slowest: the last query tiles (the most key tiles
   // to visit) of every head, stream and batch launch first
   const int hp = P.head_pairs, rows = hp ? BM : 2 * BM, nh = hp ? G.Hq / 2 : G.Hq;
   const int item = (int)(blockIdx.x >> 1), per_rank = nh * G.q_ns * G.B;
   const int tr = fast_div(item, P.d_rank);
-  const int m0 = (PACKED ? listed.tile : (G.Lq + rows - 1) / rows - 1 - tr) * rows;  // first query row of the pair
-  const int base = PACKED ? listed.first : 0;  // row of the tensors at which the virtual rows start
+  const int m0 = ((G.Lq + rows - 1) / rows - 1 - tr) * rows;  // first query row of the pair
   const int hsb = item - tr * per_rank;
   const int b = fast_div(hsb, P.d_hns), hs = hsb - b * nh * G.q_ns;
   const int hx = fast_div(hs, P.d_ns), s = hs - hx * G.q_ns;
@@ -173,13 +152,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
       };
       auto load_unit = [&](int t, bool is_v) {
         if (!ok || !(ok = take_slot())) return;
-        const int r0 = base + (lo + t) * BN;
-        if (PACKED && is_v && t == T - 1) {
-          mbar_arrive_expect_tx(&sm.v_tail, BN * PC * 2);
-          for (int c = 0; c < PC / 64; ++c)
-            tma_load_5d(sm.ring[slot] + c * BN * 64, &P.tm_v, &sm.v_tail, rank * PC + c * 64, kvh, sk, r0, b);
-          return;  // the last unit
-        }
+        const int r0 = (lo + t) * BN;
         if (rank == 0) mbar_arrive_expect_tx(&sm.full[slot], 2 * HB * DH * 2);
         const uint32_t lb = lead_addr(&sm.full[slot]);
         if (is_v) {
@@ -194,7 +167,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
       };
       auto load_q = [&](int c) {  // 64 columns: S(0) starts on the first
         if (rank == 0) mbar_arrive_expect_tx(&sm.q_full[c], 2 * BM * 64 * 2);
-        tma_load_pair(sm.q + c * BM * 64, &P.tm_q, lead_addr(&sm.q_full[c]), c * 64, h, s, base + row0, b);
+        tma_load_pair(sm.q + c * BM * 64, &P.tm_q, lead_addr(&sm.q_full[c]), c * 64, h, s, row0, b);
       };
       load_q(0);
       load_unit(0, false);
@@ -294,7 +267,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
       if (ok && rank == 0 && warp == 2 && lane == 0) {
         // V(t) and K(t+2) have landed, before this thread's arrival on p_full
         const int uv = t + 1 < T ? 2 * t + 2 : 2 * t + 1;
-        if (!PACKED || t + 1 < T) mbar_wait(&sm.full[uv % NSLOT], (uv / NSLOT) & 1, abort, P.status);
+        mbar_wait(&sm.full[uv % NSLOT], (uv / NSLOT) & 1, abort, P.status);
         if (t + 2 < T) mbar_wait(&sm.full[(2 * t + 3) % NSLOT], ((2 * t + 3) / NSLOT) & 1, abort, P.status);
       }
       __syncwarp();
@@ -331,18 +304,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
       }
       // the two warps of these 32 rows meet here on every tile, also after a wait gave up
       named_bar_sync(1 + q4, 64);
-      if constexpr (PACKED) {
-        if (ok && t == T - 1) {  // this CTA's half of the last V tile has landed
-          ok = __all_sync(0xffffffffu, mbar_wait(&sm.v_tail, 0, abort, P.status));
-          if (ok && (j + 1) * BN > G.Lv) {  // its rows behind the sequence
-            bf16* vt = sm.ring[(2 * T - 1) % NSLOT];
-            for (int e = (G.Lv - j * BN) * 8 + hc * BM + row; e < BN * 8; e += 2 * BM)
-#pragma unroll
-              for (int c = 0; c < PC / 64; ++c) reinterpret_cast<uint4*>(vt + c * BN * 64)[e] = make_uint4(0, 0, 0, 0);
-            fence_async_smem();
-          }
-        }
-      }
       if (!ok) continue;
       const float m_new = fmaxf(m_run, fmaxf(tmax, sm.part[t & 1][hc ^ 1][row]));
       const bool rescale = (m_run == -INFINITY) || ((m_new - m_run) * c2 > kRescaleThreshold);
@@ -397,8 +358,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
     sm.part[T & 1][hc][row] = l_run;  // last read two tiles before the end
     named_bar_sync(1 + q4, 64);
     l_run += sm.part[T & 1][hc ^ 1][row];
-    [[maybe_unused]] bool finite = true;
-    float* lse_row = P.lse + ((long long)b * G.Hq + h) * G.q_nL + (long long)(base + r) * G.q_rs + s;
     if (ok && __all_sync(0xffffffffu, mbar_wait(&sm.o_done, 0, abort, P.status))) {
       tc_fence_after();
       const float inv = 1.f / l_run;
@@ -412,9 +371,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
         uint32_t o[32];
         tmem_ld32(tO + c * 32, o);
         tmem_ld_wait();
-        if constexpr (PACKED)
-#pragma unroll
-          for (int e = 0; e < 32; ++e) finite = finite && fabsf(__uint_as_float(o[e])) <= FLT_MAX;
 #pragma unroll
         for (int e = 0; e < 32; e += 8) {
           uint4 w;
@@ -427,28 +383,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
         }
       }
       __syncwarp();
+      bf16* base = P.o + (((long long)b * G.q_nL + s) * G.Hq + h) * DH;
       const long long rstride = (long long)G.q_rs * G.Hq * DH;  // elements between query rows
-      bf16* obase = P.o + (((long long)b * G.q_nL + s) * G.Hq + h) * DH + (long long)base * rstride;
       const int r0 = row0 + q4 * 32, u = hc * (UPR / 2) + (lane & 15);
 #pragma unroll 8
       for (int i = lane >> 4; i < 32; i += 2)
         if (r0 + i < G.Lq)
-          *reinterpret_cast<uint4*>(obase + (long long)(r0 + i) * rstride + u * 8) =
+          *reinterpret_cast<uint4*>(base + (long long)(r0 + i) * rstride + u * 8) =
               *reinterpret_cast<const uint4*>(stg + i * (DH * 2) + ((u ^ (i & 7)) << 4));
-      if (hc == 0 && r < G.Lq) *lse_row = (m_run * c2 + log2f(l_run)) * kLn2;
-    }
-    if constexpr (PACKED) {  // either half of a row not finite: the first of its two warps computes it again
-      sm.part[(T + 1) & 1][hc][row] = finite ? 0.f : 1.f;
-      named_bar_sync(1 + q4, 64);  // both halves are stored, too
-      const bool mine = hc == 0 && r < G.Lq && sm.part[(T + 1) & 1][0][row] + sm.part[(T + 1) & 1][1][row] > 0.f;
-      const unsigned again = __ballot_sync(0xffffffffu, mine);
-      if (again) {
-        const long long qp = (long long)G.rs * G.Hq * DH, kp = (long long)G.rs * G.Hkv * DH;
-        const long long first = ((long long)base * G.rs + s) * G.Hkv * DH + kvh * DH;
-        const long long qfirst = ((long long)base * G.rs + s) * G.Hq * DH + h * DH;
-        recompute_rows<DH>(P.q + qfirst, P.k + first, P.v + first, kp, P.o + qfirst, qp, lse_row - (long long)lane * G.rs,
-                           G.rs, r - lane, again, lo * BN, min((lo + T) * BN, G.Lv), G.window, c2);
-      }
+      if (hc == 0 && r < G.Lq)
+        P.lse[((long long)b * G.Hq + h) * G.q_nL + (long long)r * G.q_rs + s] = (m_run * c2 + log2f(l_run)) * kLn2;
     }
   }
 
@@ -462,53 +406,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1) fwd256_
 }
 }  // namespace tcfwd256
 
-static bool make_params256(tcfwd256::Params& p, const void* q, const void* k, const void* v, void* o, float* lse,
-                           const SfaGeom& g, float scale, int32_t* status) {
+cudaError_t launch_sfa_fwd_tc256(const void* q, const void* k, const void* v, void* o, float* lse,
+                                 const SfaGeom& g, float scale, int32_t* status, cudaStream_t st) {
   using namespace tcfwd256;
+  Params p;
   if (!make_rows_tmap(&p.tm_q, q, query_geom(g), g.Hq, DH, BM) || !make_rows_tmap(&p.tm_k, k, g, g.Hkv, DH, HB) ||
       !make_rows_tmap(&p.tm_v, v, g, g.Hkv, DH, BN))
-    return false;
+    return cudaErrorInvalidValue;
   p.o = (bf16*)o;
   p.lse = lse;
   p.g = g;
   p.scale_log2 = scale * kLog2e;
   p.status = status;
   p.head_pairs = (g.Hq / g.Hkv) % 2 == 0;
-  const int nh = p.head_pairs ? g.Hq / 2 : g.Hq;
+  const int rows = p.head_pairs ? BM : 2 * BM, nh = p.head_pairs ? g.Hq / 2 : g.Hq;
   p.d_rank = make_fast_div((uint32_t)(nh * g.q_ns * g.B));
   p.d_hns = make_fast_div((uint32_t)(nh * g.q_ns));
   p.d_ns = make_fast_div((uint32_t)g.q_ns);
   p.d_grp = make_fast_div((uint32_t)(g.Hq / g.Hkv));
-  return true;
-}
-
-cudaError_t launch_sfa_fwd_tc256(const void* q, const void* k, const void* v, void* o, float* lse,
-                                 const SfaGeom& g, float scale, int32_t* status, cudaStream_t st) {
-  using namespace tcfwd256;
-  Params p = {};
-  if (!make_params256(p, q, k, v, o, lse, g, scale, status)) return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(fwd256_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  cudaError_t e = cudaFuncSetAttribute(fwd256_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   if (e != cudaSuccess) return e;
-  const int rows = p.head_pairs ? BM : 2 * BM, nh = p.head_pairs ? g.Hq / 2 : g.Hq;
   const unsigned grid = 2 * (unsigned)((g.Lq + rows - 1) / rows) * (unsigned)(nh * g.q_ns * g.B);
-  return launch_attn(fwd256_kernel<false>, grid, NTHREADS, kSmemBytes, st, p);
-}
-
-cudaError_t launch_sfa_fwd_packed_tc256(const void* q, const void* k, const void* v, void* o, float* lse,
-                                        const SfaGeom& g, float scale, const PackedList& list, long long max_items,
-                                        int32_t* status, cudaStream_t st) {
-  using namespace tcfwd256;
-  Params p = {};
-  if (!make_params256(p, q, k, v, o, lse, g, scale, status)) return cudaErrorInvalidValue;
-  p.list = list;
-  p.q = (const bf16*)q;
-  p.k = (const bf16*)k;
-  p.v = (const bf16*)v;
-  cudaError_t e = cudaFuncSetAttribute(fwd256_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-  if (e != cudaSuccess) return e;
-  const int nh = p.head_pairs ? g.Hq / 2 : g.Hq;
-  const unsigned grid = 2 * (unsigned)max_items * (unsigned)(nh * g.q_ns);
-  return launch_kernel(true, fwd256_kernel<true>, dim3(grid), NTHREADS, kSmemBytes, st, p);
+  return launch_attn(fwd256_kernel, grid, NTHREADS, kSmemBytes, st, p);
 }
 
 }  // namespace hdsfa

@@ -161,6 +161,13 @@ HD_DEVINLINE void red_add4(float* p, float a, float b, float c, float d) {
                : "memory");
 }
 
+// 32 bytes, a whole sector, in one store (p 32-byte aligned).
+HD_DEVINLINE void st_global_32(void* p, const uint32_t* r) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
 // Two fp32 -> packed bf16x2 (round to nearest even); `lo` lands in the low half.
 HD_DEVINLINE uint32_t cvt_bf16x2(float lo, float hi) {
   uint32_t r;
