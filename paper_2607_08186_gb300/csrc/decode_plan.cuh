@@ -9,7 +9,8 @@ struct DecodePlan {
   bool tc;  // head dim 256 with <= 128 query rows per K/V head: the tcgen05 kernel
   size_t part_o_bytes, part_ml_bytes;
 };
-DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window);
+DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, bool allow_tc = true);
+size_t decode_paged_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window);
 size_t decode_ws_bytes(const DecodePlan& p);
 
 }  // namespace hdsfa

@@ -546,8 +546,8 @@ static int cut_window(sfa_mode_t mode, int window, long long positions) {
 size_t sfa_decode_paged_workspace_bytes(int B, int max_tokens, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode,
                                         int window) {
   if (decode_paged_sizes(B, max_tokens, n, Hq, Hkv, Dh, mode, window) != HD_OK) return 0;
-  return hdsfa::decode_ws_bytes(hdsfa::decode_plan(B, max_tokens, n, Hq, Hkv, Dh, mode,
-                                                   cut_window(mode, window, (long long)max_tokens * n)));
+  return hdsfa::decode_paged_ws_bytes(B, max_tokens, n, Hq, Hkv, Dh, mode,
+                                      cut_window(mode, window, (long long)max_tokens * n));
 }
 
 hd_status_t sfa_decode_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table,

@@ -28,125 +28,29 @@
 // past the sequence are zero-filled and masked.  A sequence whose length is outside
 // [1, max_tokens] gets zero rows, LSE = -inf and HD_DEVBIT_INDEX.
 //
-// A paged cache (sfa_decode_paged) is read by the same kernels, instantiated with PAGED: a
-// position's row comes from the sequence's page table (page_row) instead of its index.  These
-// instantiations also keep a sequence that holds nothing apart from a bad length, mark a split
-// that meets a bad page, and settle exactly what a product of P and V cannot: a masked key has
-// P = 0, and 0 times an infinity or a NaN in its V row is NaN, so partial rows that come out
-// not finite are computed again from their visible keys alone (exact_row).
+// A paged cache (sfa_decode_paged) is read at head dim 256 by the tcgen05 kernel below and else by a
+// kernel of its own (sfa_decode_paged.cu); the combine kernel is shared.  With PAGED it keeps a
+// sequence that holds nothing apart from a bad length, and empties one that met a bad page.
 #include <algorithm>
 
+#include "decode.cuh"
 #include "decode_plan.cuh"
-#include "packed.cuh"
-#include "pages.cuh"
 #include "tc_common.cuh"
 
 namespace hdsfa {
-
-typedef __nv_bfloat16 bf16;
 
 // Defined in tmap.cu: the decoding step's queries [B][n][Hq][Dh] as {Dh, Hq, n, B}, box
 // 64 columns x G heads x n streams.
 bool make_qgroup_tmap(CUtensorMap* m, const void* base, int B, int n, int Hq, int Dh, int G);
 
 namespace dec {
-constexpr int NT = 128;      // 4 warps
-constexpr int STAGES = 3;
-// Head-dim split of the warps: at head dim 256 the four warps form two key groups x two
-// halves of the head dim (a warp's O accumulator would not fit its registers whole);
-// otherwise four key groups.  A stage holds 16 cached positions per key group.
-template <int DH>
-constexpr int dsplit() { return DH == 256 ? 2 : 1; }
-template <int DH>
-constexpr int ktile() { return 64 / dsplit<DH>(); }  // cached positions per pipeline stage
-constexpr int RG = 32;       // query rows per CTA at most (two m16 tiles)
-constexpr int kMaxSplit = 128;
-
-struct DecodeArgs {
-  const bf16* q;        // [B][n][Hq][Dh]
-  const bf16* kc;       // [B][Lcap*n][Hkv][Dh]
-  const bf16* vc;
-  const int32_t* lens;  // [B] tokens in the cache
-  bf16* o;              // [B][n][Hq][Dh]
-  float* lse;           // [B][Hq][n] or null
-  float* part_o;        // [B][Hkv][ngroups][nsplit][rg][Dh]
-  float2* part_ml;      // [B][Hkv][ngroups][nsplit][rg]: (max in log2 units, sum)
-  int32_t* status;
-  int B, Lcap, maxT, n, Hq, Hkv, G, M, ngroups, nsplit, mode, window;
-  int rg;               // query rows per row group (the partials' row pitch)
-  float scale_log2;
-  FastDiv d_nsplit;
-  const int32_t* table;  // paged: [B][pg.max_pages]; kc, vc are the pools
-  PageGeom pg;
-};
-
-// What a partial's (max, sum) says beyond that: the split met a page that is not in the pool.
-constexpr float kBadPage = -1.f;  // as its sum
-
-// Both kernels are launched early (launch_early's attribute): the decode kernel lets the
-// combine kernel start at once, so the combine's launch and start overlap its tail.
-
-// Visible position range [lo, hi) of a sequence of T tokens (the new token's rows
-// see nothing outside it; per-row conditions are applied per element).
-HD_DEVINLINE void seq_range(const DecodeArgs& a, int T, int& lo, int& hi) {
-  hi = T * a.n;
-  lo = a.mode == SFA_LOCAL ? max(0, (T - 1) * a.n - a.window + 1) : 0;
-}
-
-// One row's partial over the visible positions of [k0, k1), by one warp on the fp32 units: lane
-// i holds DH/32 columns.  Only visible rows of K and V are read.
-template <int DH>
-__device__ __noinline__ void exact_row(const DecodeArgs& a, int b, int g, int r, int T, int k0, int k1, float* po,
-                                       float2* pml) {
-  constexpr int C = DH / 32;
-  const int lane = threadIdx.x & 31, s = r / a.G, h = g * a.G + r % a.G, pq = (T - 1) * a.n + s;
-  int p = a.mode == SFA_LOCAL ? max(k0, pq - a.window + 1) : k0, step = 1;
-  if (a.mode == SFA_WITHIN) {
-    step = a.n;
-    p += (s + a.n - p % a.n) % a.n;
-  }
-  const int end = min(k1, pq + 1), keys = p < end ? (end - p + step - 1) / step : 0;
-  float o[C], m, l;
-  visible_row<DH>(a.q + (((long long)b * a.n + s) * a.Hq + h) * DH, a.kc + g * DH, a.vc + g * DH, (long long)a.Hkv * DH,
-                  keys, [&](int i) { return (long long)page_row(a.pg, a.table + (long long)b * a.pg.max_pages, p + i * step); },
-                  a.scale_log2, o, m, l);
-#pragma unroll
-  for (int c = 0; c < C; ++c) po[lane * C + c] = o[c];
-  if (lane == 0) *pml = make_float2(m, l);
-}
-
-// Positions [k0, k1) of split c of a sequence of T tokens, in whole tiles of `kt`
-// positions: the sequence's own range over all nsplit splits, not a share of max_tokens, so
-// that a batch of different lengths keeps every CTA busy (16 sequences of 8k to 32k tokens,
-// cross-stream: 815 -> 779 us).  Empty for lengths outside [1, max_tokens] and for splits
-// past the range.  (32-bit with a multiplication for the division: in 64 bits this cost a
-// 30 us step 3 us.)
-// Paged on the tensor cores, the first tile starts at a multiple of ALIGN (its positions before
-// the window are masked), so that no piece of a tile crosses a page.
-template <int ALIGN = 1>
-HD_DEVINLINE void split_range(const DecodeArgs& a, int T, int c, int kt, int& k0, int& k1) {
-  k0 = k1 = 0;
-  if (T < 1 || T > a.maxT) return;
-  int lo, hi;
-  seq_range(a, T, lo, hi);
-  lo -= lo % ALIGN;
-  const int tiles = (hi - lo + kt - 1) / kt, per = fast_div(tiles + a.nsplit - 1, a.d_nsplit);
-  if ((long long)c * per >= tiles) return;
-  k0 = lo + c * per * kt;
-  k1 = min(k0 + per * kt, hi);
-}
-
-template <int DH, int MT, bool PAGED>
+template <int DH, int MT>
 __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
   constexpr int DS = dsplit<DH>(), KT = ktile<DH>(), KW = 4 / DS, DC = DH / DS;  // DC: O columns per warp
   extern __shared__ __align__(128) uint8_t smem_raw[];
   bf16* sQ = reinterpret_cast<bf16*>(smem_raw);  // [MT*16][DH]
   bf16* sK = sQ + MT * 16 * DH;                   // [STAGES][KT][DH]
   bf16* sV = sK + STAGES * KT * DH;               // [STAGES][KT][DH]
-  // paged: the pool rows of four tiles (of which three are loaded or about to be), -1 for none
-  [[maybe_unused]] int* sRow = reinterpret_cast<int*>(sV + STAGES * KT * DH);
-  [[maybe_unused]] __shared__ int bad_page;
-  [[maybe_unused]] __shared__ unsigned not_finite;  // a bit per row of the merged partial
   constexpr int CPR = DH / 8;
   const int c = blockIdx.x, g = blockIdx.y / a.ngroups, rg = blockIdx.y % a.ngroups, b = blockIdx.z;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, t4 = lane & 3;
@@ -164,21 +68,6 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
     return;
   }
   const long long pbase = (long long)b * a.Lcap * a.n;  // cache row of position 0
-  // paged: pool row of this thread's position of tile `it` (-1 beyond the split)
-  [[maybe_unused]] auto row_of = [&](int it) {
-    const int p = k0 + it * KT + tid;
-    if (tid >= KT || p >= k1) return -1;
-    const int row = page_row(a.pg, a.table + (long long)b * a.pg.max_pages, p);
-    if (row < 0) bad_page = 1;
-    return row;
-  };
-  if constexpr (PAGED) {
-    if (tid == 0) bad_page = 0, not_finite = 0;
-    __syncthreads();
-    const int r0 = row_of(0), r1 = row_of(1), r2 = row_of(2);
-    if (tid < KT) sRow[tid] = r0, sRow[KT + tid] = r1, sRow[2 * KT + tid] = r2;
-    __syncthreads();
-  }
 
   // query rows of the group -> smem (rows past M zero-filled)
   for (int i = tid; i < MT * 16 * CPR; i += NT) {
@@ -188,30 +77,21 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
     cp_async_16(smem_u32(sQ + swz<DH>(rr, cc * 8)), a.q + (((long long)b * a.n + s) * a.Hq + h) * DH + cc * 8,
                 ok);
   }
-  auto load_stage = [&](int st, int it) {
-    const int kp0 = k0 + it * KT;
+  auto load_stage = [&](int st, int kp0) {
     bf16* dK = sK + st * KT * DH;
     bf16* dV = sV + st * KT * DH;
     for (int i = tid; i < KT * CPR; i += NT) {
       const int rr = i / CPR, cc = i % CPR, p = kp0 + rr;
-      bool ok;
-      long long off;
-      if constexpr (PAGED) {
-        const int row = sRow[(it & 3) * KT + rr];
-        ok = row >= 0;
-        off = ((long long)(ok ? row : 0) * a.Hkv + g) * DH + cc * 8;
-      } else {
-        ok = p < k1;
-        off = ((pbase + (ok ? p : k0)) * a.Hkv + g) * DH + cc * 8;
-      }
+      const bool ok = p < k1;
+      const long long off = ((pbase + (ok ? p : k0)) * a.Hkv + g) * DH + cc * 8;
       cp_async_16(smem_u32(dK + swz<DH>(rr, cc * 8)), a.kc + off, ok);
       cp_async_16(smem_u32(dV + swz<DH>(rr, cc * 8)), a.vc + off, ok);
     }
   };
   const int nsub = (k1 - k0 + KT - 1) / KT;
-  load_stage(0, 0);
+  load_stage(0, k0);
   cp_async_commit();
-  if (nsub > 1) load_stage(1, 1);
+  if (nsub > 1) load_stage(1, k0 + KT);
   cp_async_commit();
 
   // this thread's query rows: (mt, half) -> local row mt*16 + g4 + 8*half
@@ -244,11 +124,8 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
   for (int it = 0; it < nsub; ++it) {
     cp_async_wait<STAGES - 2>();  // stage `it` has landed
     __syncthreads();              // ... for every thread, and stage it-1 is no longer read
-    if (it + 2 < nsub) load_stage((it + 2) % STAGES, it + 2);
+    if (it + 2 < nsub) load_stage((it + 2) % STAGES, k0 + (it + 2) * KT);
     cp_async_commit();
-    // the rows that the next iteration loads by are looked up under this one's products
-    [[maybe_unused]] int next_row;
-    if constexpr (PAGED) next_row = row_of(it + 3);
     const bf16* cK = sK + (it % STAGES) * KT * DH;
     const bf16* cV = sV + (it % STAGES) * KT * DH;
 
@@ -344,8 +221,6 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
         mma_bf16_16816(oacc[mt][2 * dp + 1], pa[mt], b2, b3);
       }
     }
-    if constexpr (PAGED)
-      if (tid < KT) sRow[((it + 3) & 3) * KT + tid] = next_row;
   }
 
   // merge the 4 warps' partials in shared memory (the K/V ring is free now)
@@ -392,10 +267,6 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
       l += f * sL[w * MT * 16 + tid];
       sM[w * MT * 16 + tid] = f;
     }
-    if constexpr (PAGED) {
-      if (l != l) m = INFINITY;  // a visible score that is not finite: the combined row is NaN
-      if (bad_page) m = -INFINITY, l = kBadPage;
-    }
     pml[tid] = make_float2(m, l);
   }
   __syncthreads();
@@ -412,19 +283,6 @@ __global__ void __launch_bounds__(NT) decode_kernel(DecodeArgs a) {
       o.w += f * v.w;
     }
     *reinterpret_cast<float4*>(po + row * DH + c4 * 4) = o;
-    if constexpr (PAGED)
-      if (!(fmaxf(fmaxf(fabsf(o.x), fabsf(o.y)), fmaxf(fabsf(o.z), fabsf(o.w))) <= FLT_MAX) ||
-          o.x != o.x || o.y != o.y || o.z != o.z || o.w != o.w)
-        atomicOr(&not_finite, 1u << row);
-  }
-  if constexpr (PAGED) {
-    __syncthreads();
-    if (bad_page) return;  // uniform
-    for (unsigned rows = not_finite, i = 0; rows; rows &= rows - 1, ++i) {
-      const int row = __ffs(rows) - 1;
-      if ((int)(i & 3) == warp && rg * RG + row < a.M)
-        exact_row<DH>(a, b, g, rg * RG + row, T, k0, k1, po + row * DH, pml + row);
-    }
   }
 }
 
@@ -604,7 +462,6 @@ struct Smem {
 struct Params {
   CUtensorMap tm_q, tm_k, tm_v;
   dec::DecodeArgs a;
-  int piece;  // paged: rows of a K/V box, a power of two that divides a page's rows and a tile's
 };
 
 // Unit u of the ring sequence K(0), K(1), V(0), K(2), V(1), ..., V(nt-1), two halves per
@@ -627,9 +484,10 @@ HD_DEVINLINE void unit_of(int u, int nt, int& j, int& isv, int& half) {
   isv = 1;
 }
 
-// PAGED: a tile's rows come in pieces of P.piece rows, none of which crosses a page; the warp's
-// lanes look their pages up and issue their loads.  Pieces outside the sequence (or the window)
-// are loaded from behind the pool's last row, which fills them with zeros.
+// PAGED: a tile's rows come in pieces, none of which crosses a page (paged_tile); the warp's lanes
+// look their pages up and issue their loads.  Pieces outside the sequence (or the window) are loaded
+// from behind the pool's last row, which fills them with zeros.  A tile that pieces do not fill leaves
+// the slots' last rows as they are zeroed at the start.
 template <bool PAGED>
 __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_constant__ Params P) {
   const dec::DecodeArgs& a = P.a;
@@ -645,6 +503,11 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
   for (int i = threadIdx.x; i < (DH / 64) * (BM - a.M) * 8; i += NTHREADS) {
     const int blk = i / ((BM - a.M) * 8), rem = i % ((BM - a.M) * 8);
     reinterpret_cast<uint4*>(sm.q[blk] + (a.M + rem / 8) * 64)[rem % 8] = make_uint4(0, 0, 0, 0);
+  }
+  if (PAGED && a.tile < BN) {
+    const int per = (BN - a.tile) * 8;  // 16-byte units of a block's last rows
+    for (int i = threadIdx.x; i < NSLOT * 2 * per; i += NTHREADS)
+      reinterpret_cast<uint4*>(sm.ring[0][0] + (i / per) * (BN * 64) + a.tile * 64)[i % per] = make_uint4(0, 0, 0, 0);
   }
   fence_async_smem();
   if (threadIdx.x == 0) {
@@ -671,8 +534,9 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
   grid_dep_launch();
   const int T = a.lens[b];
   int k0, k1;
-  dec::split_range<PAGED ? BN : 1>(a, T, c, BN, k0, k1);
-  const int nt = (k1 - k0 + BN - 1) / BN, nunits = 4 * nt;
+  const int tile = PAGED ? a.tile : BN;  // positions of a key tile: columns beyond them are masked
+  dec::split_range<PAGED>(a, T, c, tile, k0, k1);
+  const int nt = (k1 - k0 + tile - 1) / tile, nunits = 4 * nt;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -687,51 +551,73 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     if constexpr (PAGED) {
-      fence_async_global();  // rows that an earlier kernel stored, before the copies read them
       if (lane == 0) {
+        tma_prefetch(&P.tm_k);
+        tma_prefetch(&P.tm_v);
         mbar_arrive_expect_tx(&sm.q_full, a.M * DH * 2);
         for (int cb = 0; cb < DH / 64; ++cb) tma_load_4d(sm.q[cb], &P.tm_q, &sm.q_full, cb * 64, g * a.G, 0, b);
       }
       const int beyond = a.pg.num_pages * a.pg.prow;
       const int seen = a.mode == SFA_LOCAL ? (T - 1) * a.n - a.window + 1 : 0;  // first position any row sees
-      int at[2][4];  // pool rows of this lane's pieces, of an even and an odd tile
-      auto look_up = [&](int j, int* x) {
+      // Rows of this lane's pieces of the tiles whose V (cur) and K (nxt) come next, and the page
+      // entries of the one after them, loaded a tile ahead: a look-up's two loads would otherwise hold
+      // the ring up on every tile.
+      int cur[4], nxt[4], entry[4];
+      const int32_t* table = a.table + (long long)b * a.pg.max_pages;
+      auto pos_of = [&](int j, int i) {  // first position of piece i of tile j, -1: none that a row sees
+        const int p = (lane + 32 * i) * a.piece, pos = k0 + j * tile + p;
+        return p >= tile || pos >= k1 || pos + a.piece <= seen ? -1 : pos;
+      };
+      auto fetch = [&](int j) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int p = (lane + 32 * i) * P.piece, pos = k0 + j * BN + p;
-          x[i] = beyond;
-          if (p >= BN || pos >= k1 || pos + P.piece <= seen) continue;
-          const int row = page_row(a.pg, a.table + (long long)b * a.pg.max_pages, pos);
-          if (row >= 0) x[i] = row;
-          else sm.bad_page = 1;
+          const int pos = pos_of(j, i);
+          if (pos >= 0) entry[i] = table[fast_div(pos, a.pg.d_prow)];
         }
       };
-      int issued = 0;
-      look_up(0, at[0]);
-      look_up(1, at[1]);  // nothing of it where the split has one tile
-      for (int u = 0; u < nunits; ++u, ++issued) {
-        const int slot = u % NSLOT;
-        if (u >= NSLOT &&
-            !__all_sync(0xffffffffu, mbar_wait(&sm.empty[slot], ((u / NSLOT) - 1) & 1, abort, a.status)))
-          break;
-        int j, isv, half;
-        unit_of(u, nt, j, isv, half);
-        const CUtensorMap* tm = isv ? &P.tm_v : &P.tm_k;
-        if (lane == 0) mbar_arrive_expect_tx(&sm.full[slot], BN * 128 * 2);
+      auto rows_of = [&](int j, int* x) {  // of the tile that was fetched
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int pos = pos_of(j, i);
+          x[i] = beyond;
+          if (pos < 0) continue;
+          if ((unsigned)entry[i] < (unsigned)a.pg.num_pages)
+            x[i] = entry[i] * a.pg.prow + pos - fast_div(pos, a.pg.d_prow) * a.pg.prow;
+          else
+            sm.bad_page = 1;
+        }
+      };
+      int issued = 0, slot = 0, lap = 0;
+      auto load_half = [&](const CUtensorMap* tm, const int* x, int half) -> bool {
+        if (lap > 0 && !__all_sync(0xffffffffu, mbar_wait(&sm.empty[slot], (lap - 1) & 1, abort, a.status))) return false;
+        if (lane == 0) mbar_arrive_expect_tx(&sm.full[slot], tile * 128 * 2);
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int p = (lane + 32 * i) * P.piece;
-          if (p >= BN) continue;
-          const int row = (j & 1) ? at[1][i] : at[0][i];
-          tma_load_5d(sm.ring[slot][0] + p * 64, tm, &sm.full[slot], half * 128, g, 0, row, 0);
-          tma_load_5d(sm.ring[slot][1] + p * 64, tm, &sm.full[slot], half * 128 + 64, g, 0, row, 0);
+          const int p = (lane + 32 * i) * a.piece;
+          if (p >= tile) break;
+          tma_load_5d(sm.ring[slot][0] + p * 64, tm, &sm.full[slot], half * 128, g, 0, x[i], 0);
+          tma_load_5d(sm.ring[slot][1] + p * 64, tm, &sm.full[slot], half * 128 + 64, g, 0, x[i], 0);
         }
-        // the rows of tile j + 2, whose K comes after V(j), in the place of tile j's
-        if (isv && half == 1 && j + 2 < nt) {
-          if (j & 1) look_up(j + 2, at[1]);
-          else look_up(j + 2, at[0]);
+        __syncwarp();
+        ++issued;
+        if (++slot == NSLOT) {
+          slot = 0;
+          ++lap;
         }
+        return true;
+      };
+      fetch(0);
+      rows_of(0, cur);
+      fetch(1);
+      bool go = load_half(&P.tm_k, cur, 0) && load_half(&P.tm_k, cur, 1);
+      for (int j = 0; go && j < nt; ++j) {  // K(j+1), then V(j)
+        rows_of(j + 1, nxt);
+        fetch(j + 2);
+        if (j + 1 < nt) go = load_half(&P.tm_k, nxt, 0) && load_half(&P.tm_k, nxt, 1);
+        go = go && load_half(&P.tm_v, cur, 0) && load_half(&P.tm_v, cur, 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) cur[i] = nxt[i];
       }
       if (lane == 0) {
         mbar_drain(&sm.q_full, 0);
@@ -853,11 +739,11 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
 #pragma unroll
       for (int cc = 0; cc < BN / 32; ++cc) tmem_ld32(tS + cc * 32, reinterpret_cast<uint32_t*>(x) + cc * 32);
       tmem_ld_wait();
-      const int base = k0 + i * BN;
+      const int base = k0 + i * tile;
       // the tile that reaches the new token's own positions or the split's end, and (LOCAL)
       // those at the rows' window edges
-      if (base + BN - 1 > own_lo || base + BN > k1 || base <= win_hi) {
-        const int e_hi = min(k1 - 1, pq) - base, e_lo = a.mode == SFA_LOCAL ? pq - a.window + 1 - base : 0;
+      if (base + tile - 1 > own_lo || base + tile > k1 || base <= win_hi || tile < BN) {
+        const int e_hi = min(min(k1 - 1, pq), base + tile - 1) - base, e_lo = a.mode == SFA_LOCAL ? pq - a.window + 1 - base : 0;
 #pragma unroll
         for (int e = 0; e < BN; ++e)
           if (e > e_hi || e < e_lo) x[e] = -INFINITY;
@@ -936,7 +822,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
       // The sequence's last tile holds cached rows past its length, which may never have been
       // written: their P is 0, and 0 times an infinity or a NaN is NaN, so their V rows are
       // zeroed before the PV (which waits for this thread's arrival).
-      if (base + BN > k1) {
+      if (base + tile > k1) {
 #pragma unroll
         for (int u = nunits - 2; u < nunits; ++u)  // the ring's last units: this tile's V halves
           ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.full[u % NSLOT], (u / NSLOT) & 1, abort, a.status));
@@ -1007,12 +893,12 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
 
 // ------------------------------------------------------------------ host side
 
-DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {
+DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, bool allow_tc) {
   using namespace dec;
   DecodePlan p;
   p.G = Hq / Hkv;
   p.M = n * p.G;
-  p.tc = Dh == 256 && p.M <= dectc::BM;
+  p.tc = allow_tc && Dh == 256 && p.M <= dectc::BM;
   p.rg = p.tc ? p.M : RG;
   p.ngroups = p.tc ? 1 : (p.M + RG - 1) / RG;
   const long long range = mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1)
@@ -1044,12 +930,11 @@ DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode
 
 size_t decode_ws_bytes(const DecodePlan& p) { return ((p.part_o_bytes + 255) & ~size_t(255)) + p.part_ml_bytes; }
 
-template <int DH, int MT, bool PAGED>
+template <int DH, int MT>
 static cudaError_t launch_decode_t(const dec::DecodeArgs& a, cudaStream_t st) {
   using namespace dec;
-  const size_t smem = (size_t)(MT * 16 + 2 * STAGES * ktile<DH>()) * DH * sizeof(bf16) +
-                      (PAGED ? 4 * ktile<DH>() * sizeof(int) : 0);
-  cudaError_t e = cudaFuncSetAttribute(decode_kernel<DH, MT, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const size_t smem = (size_t)(MT * 16 + 2 * STAGES * ktile<DH>()) * DH * sizeof(bf16);
+  cudaError_t e = cudaFuncSetAttribute(decode_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute pdl[1];
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1061,12 +946,12 @@ static cudaError_t launch_decode_t(const dec::DecodeArgs& a, cudaStream_t st) {
   cfg.stream = st;
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, decode_kernel<DH, MT, PAGED>, a);
+  e = cudaLaunchKernelEx(&cfg, decode_kernel<DH, MT>, a);
   if (e != cudaSuccess) return e;
   cfg.gridDim = dim3(std::min(a.rg, a.M), a.Hkv * a.ngroups, a.B);
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, combine_kernel<DH, PAGED>, a);
+  return cudaLaunchKernelEx(&cfg, combine_kernel<DH, false>, a);
 }
 
 template <bool PAGED>
@@ -1083,14 +968,13 @@ static cudaError_t launch_decode_tc(const dec::DecodeArgs& a, cudaStream_t st) {
   gk.Lv = a.Lcap * a.n;
   gk.ns = 1;
   gk.rs = 1;
-  p.piece = BN;
   if (PAGED) {  // the pool as one problem of all its rows
     gk.B = 1;
     gk.nL = gk.Lv = a.pg.num_pages * a.pg.prow;
-    p.piece = std::min(BN, a.pg.prow & -a.pg.prow);
   }
+  const int box = PAGED ? a.piece : BN;
   if (!make_qgroup_tmap(&p.tm_q, a.q, a.B, a.n, a.Hq, DH, a.G) ||
-      !make_rows_tmap(&p.tm_k, a.kc, gk, a.Hkv, DH, p.piece) || !make_rows_tmap(&p.tm_v, a.vc, gk, a.Hkv, DH, p.piece))
+      !make_rows_tmap(&p.tm_k, a.kc, gk, a.Hkv, DH, box) || !make_rows_tmap(&p.tm_v, a.vc, gk, a.Hkv, DH, box))
     return cudaErrorInvalidValue;
   const int smem = (int)sizeof(Smem) + 1024;
   cudaError_t e = cudaFuncSetAttribute(decode_tc_kernel<PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -1113,28 +997,19 @@ static cudaError_t launch_decode_tc(const dec::DecodeArgs& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, dec::combine_kernel<DH, PAGED>, a);
 }
 
-template <bool PAGED>
-static cudaError_t launch_decode(dec::DecodeArgs& a, int Dh, float scale, void* ws, cudaStream_t st) {
-  const DecodePlan p = decode_plan(a.B, a.maxT, a.n, a.Hq, a.Hkv, Dh, a.mode, a.window);
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + ((p.part_o_bytes + 255) & ~size_t(255)));
-  a.G = p.G;
-  a.M = p.M;
-  a.ngroups = p.ngroups;
-  a.nsplit = p.nsplit;
-  a.rg = p.rg;
-  a.scale_log2 = scale * 1.4426950408889634f;
-  a.d_nsplit = make_fast_div((uint32_t)p.nsplit);
-  if (p.tc) return launch_decode_tc<PAGED>(a, st);
-  const bool two = p.M > 16;  // a row group of more than 16 rows takes two m16 tiles
-  if (Dh == 64) return two ? launch_decode_t<64, 2, PAGED>(a, st) : launch_decode_t<64, 1, PAGED>(a, st);
-  if (Dh == 256) return two ? launch_decode_t<256, 2, PAGED>(a, st) : launch_decode_t<256, 1, PAGED>(a, st);
-  return two ? launch_decode_t<128, 2, PAGED>(a, st) : launch_decode_t<128, 1, PAGED>(a, st);
+cudaError_t launch_decode_paged_tc(const dec::DecodeArgs& a, cudaStream_t st) { return launch_decode_tc<true>(a, st); }
+
+cudaError_t launch_combine_paged(const dec::DecodeArgs& a, int Dh, cudaStream_t st) {
+  const dim3 grid(std::min(a.rg, a.M), a.Hkv * a.ngroups, a.B);
+  if (Dh == 64) return launch_early(dec::combine_kernel<64, true>, grid, 256, st, a);
+  if (Dh == 128) return launch_early(dec::combine_kernel<128, true>, grid, 256, st, a);
+  return launch_early(dec::combine_kernel<256, true>, grid, 256, st, a);
 }
 
-static dec::DecodeArgs decode_args(const void* q, const void* kc, const void* vc, const int32_t* lens, void* o,
-                                   float* lse, int B, int maxT, int n, int Hq, int Hkv, int mode, int window,
-                                   int32_t* status) {
+cudaError_t launch_sfa_decode(const void* q, const void* kc, const void* vc, const int32_t* lens, void* o,
+                              float* lse, int B, int maxT, int Lcap, int n, int Hq, int Hkv, int Dh, float scale,
+                              int mode, int window, void* ws, int32_t* status, cudaStream_t st) {
+  const DecodePlan p = decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window);
   dec::DecodeArgs a = {};
   a.q = (const bf16*)q;
   a.kc = (const bf16*)kc;
@@ -1142,33 +1017,29 @@ static dec::DecodeArgs decode_args(const void* q, const void* kc, const void* vc
   a.lens = lens;
   a.o = (bf16*)o;
   a.lse = lse;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + ((p.part_o_bytes + 255) & ~size_t(255)));
   a.status = status;
   a.B = B;
+  a.Lcap = Lcap;
   a.maxT = maxT;
   a.n = n;
   a.Hq = Hq;
   a.Hkv = Hkv;
+  a.G = p.G;
+  a.M = p.M;
+  a.ngroups = p.ngroups;
+  a.nsplit = p.nsplit;
+  a.rg = p.rg;
   a.mode = mode;
   a.window = window;
-  return a;
-}
-
-cudaError_t launch_sfa_decode(const void* q, const void* kc, const void* vc, const int32_t* lens, void* o,
-                              float* lse, int B, int maxT, int Lcap, int n, int Hq, int Hkv, int Dh, float scale,
-                              int mode, int window, void* ws, int32_t* status, cudaStream_t st) {
-  dec::DecodeArgs a = decode_args(q, kc, vc, lens, o, lse, B, maxT, n, Hq, Hkv, mode, window, status);
-  a.Lcap = Lcap;
-  return launch_decode<false>(a, Dh, scale, ws, st);
-}
-
-cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* vp, const int32_t* table,
-                                    const int32_t* lens, void* o, float* lse, int B, int maxT, int num_pages, int P,
-                                    int max_pages, int n, int Hq, int Hkv, int Dh, float scale, int mode, int window,
-                                    void* ws, int32_t* status, cudaStream_t st) {
-  dec::DecodeArgs a = decode_args(q, kp, vp, lens, o, lse, B, maxT, n, Hq, Hkv, mode, window, status);
-  a.table = table;
-  a.pg = make_page_geom(num_pages, max_pages, P * n);
-  return launch_decode<true>(a, Dh, scale, ws, st);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.d_nsplit = make_fast_div((uint32_t)p.nsplit);
+  if (p.tc) return launch_decode_tc<false>(a, st);
+  const bool two = p.M > 16;  // a row group of more than 16 rows takes two m16 tiles
+  if (Dh == 64) return two ? launch_decode_t<64, 2>(a, st) : launch_decode_t<64, 1>(a, st);
+  if (Dh == 256) return two ? launch_decode_t<256, 2>(a, st) : launch_decode_t<256, 1>(a, st);
+  return two ? launch_decode_t<128, 2>(a, st) : launch_decode_t<128, 1>(a, st);
 }
 
 cudaError_t launch_kv_append(const void* kn, const void* vn, void* kc, void* vc, const int32_t* lens, int B,

@@ -117,7 +117,6 @@ HD_DEVINLINE void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
 }
 HD_DEVINLINE void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
 HD_DEVINLINE void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
-HD_DEVINLINE void fence_async_global() { asm volatile("fence.proxy.async.global;\n" ::: "memory"); }
 HD_DEVINLINE void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
 
 // D[tmem] (+)= A * B, bf16 inputs, fp32 accumulate; B from shared memory, A from shared

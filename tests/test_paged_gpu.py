@@ -76,11 +76,12 @@ def _check(q, kc, vc, lens, n, mode, window, P, seed=0, max_tokens=None, width=N
 MASKS = [(WITHIN, 0), (CROSS, 0), (LOCAL, 1), (LOCAL, 100), (LOCAL, 2**31 - 1)]
 
 
-# rows per K/V head: 16 and 32 (one and two m16 tiles), 64 (two row groups), 9; one page of every size
-# against tiles of 64 rows: smaller, equal, larger, odd
+# rows per K/V head: 16 and 32 (one and two m16 tiles), 64 (two row groups), 9; pages of every
+# size against tiles of 64 rows: smaller, equal, larger, odd, prime, one token with more streams than a tile holds
 @pytest.mark.parametrize("mode,w", MASKS)
 @pytest.mark.parametrize("n,Hq,Hkv,Dh,P", [(4, 32, 8, 128, 16), (8, 32, 8, 128, 3), (8, 64, 8, 128, 1), (1, 8, 8, 128, 64),
-                                           (3, 6, 2, 128, 7), (2, 4, 4, 64, 8), (3, 16, 4, 64, 50), (4, 8, 2, 64, 5)])
+                                           (3, 6, 2, 128, 7), (2, 4, 4, 64, 8), (3, 16, 4, 64, 50), (4, 8, 2, 64, 5),
+                                           (1, 8, 2, 128, 131), (4, 32, 8, 128, 2), (70, 2, 1, 64, 1), (5, 10, 2, 64, 9)])
 def test_ragged(mode, w, n, Hq, Hkv, Dh, P):
     q, kc, vc = _case(4, 150, n, Hq, Hkv, Dh, n + Hq + P)
     _check(q, kc, vc, _i32([150, 1, 0, 129]), n, mode, w, P)
@@ -90,7 +91,7 @@ def test_ragged(mode, w, n, Hq, Hkv, Dh, P):
 # tiles), 256 rows on the other one
 @pytest.mark.parametrize("mode,w", MASKS)
 @pytest.mark.parametrize("n,Hq,Hkv,P", [(4, 24, 2, 16), (1, 4, 1, 3), (3, 6, 2, 5), (8, 32, 2, 4), (4, 24, 2, 32),
-                                        (4, 24, 2, 64), (2, 12, 2, 1), (8, 64, 2, 6)])
+                                        (4, 24, 2, 64), (2, 12, 2, 1), (8, 64, 2, 6), (8, 64, 2, 1), (3, 24, 2, 43), (1, 12, 1, 131), (1, 4, 1, 1)])
 def test_ragged_head_dim_256(mode, w, n, Hq, Hkv, P):
     q, kc, vc = _case(4, 150, n, Hq, Hkv, 256, 40 + n + Hq + P)
     _check(q, kc, vc, _i32([150, 1, 0, 129]), n, mode, w, P)
@@ -112,18 +113,17 @@ def test_max_tokens_and_wide_tables(Dh):
 
 
 @pytest.mark.parametrize("mode,w", [(WITHIN, 0), (CROSS, 0), (LOCAL, 70)])
-@pytest.mark.parametrize("Hq,Hkv,Dh", [(32, 8, 128), (4, 4, 64)])
-def test_identity_table_gives_the_contiguous_bits(mode, w, Hq, Hkv, Dh):
-    B, L, n, P = 3, 200, 4, 20
-    q, kc, vc = _case(B, L, n, Hq, Hkv, Dh, 3)
+@pytest.mark.parametrize("Hq,Hkv,Dh,P", [(32, 8, 128, 16), (4, 4, 64, 5), (24, 2, 256, 20)])
+def test_where_pages_lie_changes_no_bit(mode, w, Hq, Hkv, Dh, P):
+    n = 4
+    q, kc, vc = _case(3, 200, n, Hq, Hkv, Dh, 3)
     lens = _i32([200, 33, 121])
-    table = torch.arange(B * L // P, dtype=I32).view(B, L // P)
-    o, lse, st = _decode(q, kc.view(B * L // P, P * n, Hkv, Dh), vc.view(B * L // P, P * n, Hkv, Dh), table, lens, n, mode, w)
-    assert st == 0
-    o2, lse2 = torch.empty_like(q, device="cuda"), torch.empty(B, Hq, n, device="cuda")
-    ws = torch.empty(binding.sfa_decode_workspace_bytes(B, L, n, Hq, Hkv, Dh, mode, w), dtype=torch.uint8, device="cuda")
-    binding.sfa_decode(q.cuda(), kc.cuda(), vc.cuda(), lens.cuda(), o2, n, mode, ws, lse=lse2, window=w)
-    assert torch.equal(o.view(torch.int16), o2.cpu().view(torch.int16)) and torch.equal(lse, lse2.cpu())
+    runs = []
+    for seed in (1, 2):
+        kp, table = paging.to_pages(kc, lens, P, n, seed)
+        vp, _ = paging.to_pages(vc, lens, P, n, seed)
+        runs.append(_decode(q, kp, vp, table, lens, n, mode, w))
+    assert torch.equal(runs[0][0], runs[1][0]) and torch.equal(runs[0][1], runs[1][1]) and runs[0][2] == 0
 
 
 @pytest.mark.parametrize("Hq,Hkv,Dh", [(8, 2, 128), (24, 2, 256)])
