@@ -39,6 +39,7 @@ struct DecodeArgs {
   PageGeom pg;
   int tile, piece;       // paged: positions of a tile, in pieces of which none crosses a page
   int split_pages;       // paged: pages of a split of max_tokens tokens
+  FastDiv d_G, d_n;      // paged
 };
 
 // What a partial's (max, sum) says beyond that: the split met a page that is not in the pool.

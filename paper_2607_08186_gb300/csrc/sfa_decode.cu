@@ -722,9 +722,9 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
     const int own_lo = (T - 1) * a.n;                                             // first position of the new token
     const int win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;  // outside some row's window up to here
     // n divides 32: columns of the row's stream repeat from word to word and tile to tile
-    // (a split starts at a multiple of BN)
+    // (a split starts at a multiple of BN; paged, a tile is n's multiple or the pattern shifts)
     uint32_t stream_word = 0;
-    if (a.mode == SFA_WITHIN && 32 % a.n == 0)
+    if (a.mode == SFA_WITHIN && 32 % a.n == 0 && (!PAGED || tile % a.n == 0))
       for (int e = (s + a.n - k0 % a.n) % a.n; e < 32; e += a.n) stream_word |= 1u << e;
     float m_run = -INFINITY, l_run = 0.f;
     bool ok = true;
@@ -751,7 +751,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
       if (a.mode == SFA_WITHIN && a.n > 1) {
         // the stream condition as one bit per column
         uint32_t vis[4] = {stream_word, stream_word, stream_word, stream_word};
-        if (stream_word == 0) {  // n does not divide 32: the pattern shifts from tile to tile
+        if (stream_word == 0) {  // n does not divide 32 (or a tile): the pattern shifts from tile to tile
           int e = (base - s) % a.n;  // first column of the row's stream
           e = e <= 0 ? -e : a.n - e;
           for (; e < BN; e += a.n) {

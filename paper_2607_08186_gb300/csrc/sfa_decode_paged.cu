@@ -114,23 +114,47 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
       const int blkno = i / ((KT - tile) * 8), e = i % ((KT - tile) * 8);
       reinterpret_cast<uint4*>(sm.v[0] + (size_t)blkno * KT * 64 + tile * 64)[e] = make_uint4(0, 0, 0, 0);
     }
+  // What needs nothing from the kernels before this one.  This thread's query rows: (mt, half) -> local
+  // row mt*16 + g4 + 8*half, its stream (-1: padding row).  Where n divides a tile, which of this
+  // thread's keys are of a row's stream is the same in every tile.
+  int rs_[MT][2];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int r = rg * RG + mt * 16 + g4 + 8 * hf;
+      rs_[mt][hf] = r < a.M ? fast_div(r, a.d_G) : -1;
+    }
+  const bool streams = a.mode == SFA_WITHIN && a.n > 1;
+  const bool shifting = streams && tile - fast_div(tile, a.d_n) * a.n != 0;
+  uint32_t mine = 0;                            // bit mt*8 + hf*4 + j*2 + e: the row may see the key
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int key = kw * 16 + (i >> 1) * 8 + 2 * t4 + (i & 1);
+    const int ks = streams && !shifting ? key - fast_div(key, a.d_n) * a.n : -1;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+        if (rs_[mt][hf] >= 0 && key < tile && (ks < 0 || ks == rs_[mt][hf])) mine |= 1u << (mt * 8 + hf * 4 + i);
+  }
   grid_dep_wait();
   grid_dep_launch();
   const int T = a.lens[b];
   const int32_t* table = a.table + (long long)b * a.pg.max_pages;
-  // under that load: the page entries where the split starts if the sequence has max_tokens, and the
-  // query rows of the group (rows past M zero-filled)
+  // under that load: the page entries where the split starts if the sequence has max_tokens
   if (tid == 32) prefetch_l1(table + min(c * a.split_pages, a.pg.max_pages - 1));
-  for (int i = tid; i < MT * 16 * CPR; i += NT) {
-    const int rr = i / CPR, cc = i % CPR, r = rg * RG + rr;
-    const bool ok = r < a.M;
-    const int s = ok ? r / a.G : 0, h = g * a.G + (ok ? r % a.G : 0);
-    cp_async_16(smem_u32(sm.q + swz<DH>(rr, cc * 8)), a.q + (((long long)b * a.n + s) * a.Hq + h) * DH + cc * 8, ok);
-  }
+  auto load_q = [&] {  // query rows of the group (rows past M zero-filled)
+    for (int i = tid; i < MT * 16 * CPR; i += NT) {
+      const int rr = i / CPR, cc = i % CPR, r = rg * RG + rr;
+      const bool ok = r < a.M;
+      const int s = ok ? fast_div(r, a.d_G) : 0, h = g * a.G + (ok ? r - s * a.G : 0);
+      cp_async_16(smem_u32(sm.q + swz<DH>(rr, cc * 8)), a.q + (((long long)b * a.n + s) * a.Hq + h) * DH + cc * 8, ok);
+    }
+  };
   int k0, k1;
   split_range<true>(a, T, c, tile, k0, k1);
   if (k0 >= k1) {  // nothing of this sequence in this split: an empty partial, or an empty result
-    cp_async_wait<0>();
     if (a.nsplit > 1) {
       for (int i = tid; i < RG; i += NT) pml[i] = make_float2(-INFINITY, 0.f);
     } else {
@@ -199,40 +223,21 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
     const int t = (warp + 2) & 3;  // this warp's first tile
     fetch(t);
     if (t < min(2, nsub)) load_tile(t);
-    cp_async_wait<0>();  // the queries
+    load_q();
+    cp_async_commit();
+    cp_async_wait<0>();
     __syncthreads();
   } else {
     const int r0 = row_of(0), r1 = row_of(1), r2 = row_of(2);
     if (tid < tile) sm.row[0][tid] = r0, sm.row[1][tid] = r1, sm.row[2][tid] = r2;
     __syncthreads();
+    load_q();
     load_tile(0);
     cp_async_commit();
     if (nsub > 1) load_tile(1);
     cp_async_commit();
   }
 
-  // this thread's query rows: (mt, half) -> local row mt*16 + g4 + 8*half
-  int rs_[MT][2], rq[MT][2];  // stream of the row (-1: padding row) and its position
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const int r = rg * RG + mt * 16 + g4 + 8 * hf;
-      rs_[mt][hf] = r < a.M ? r / a.G : -1;
-      rq[mt][hf] = (T - 1) * a.n + (r < a.M ? r / a.G : 0);
-    }
-  // A tile starts at a multiple of n (streams fit a tile), so which of this thread's keys are of a
-  // row's stream is the same in every tile; rows past M see nothing.
-  const bool streams = a.mode == SFA_WITHIN && a.n > 1;
-  uint32_t mine = 0;  // bit mt*8 + hf*4 + j*2 + e
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int hf = i >> 2, key = kw * 16 + ((i >> 1) & 1) * 8 + 2 * t4 + (i & 1);
-      if (rs_[mt][hf] >= 0 && key < tile && (!streams || tile % a.n != 0 || key % a.n == rs_[mt][hf])) mine |= 1u << (mt * 8 + i);
-    }
-  const bool shifting = streams && tile % a.n != 0;  // more streams than a tile holds
   const int own_lo = (T - 1) * a.n, win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;
   float mx[MT][2], ls[MT][2], oacc[MT][DC / 8][4];
 #pragma unroll
@@ -300,9 +305,9 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int hf = i >> 2, p = kb + ((i >> 1) & 1) * 8 + (i & 1), pq = rq[mt][hf];
+          const int hf = i >> 2, p = kb + ((i >> 1) & 1) * 8 + (i & 1), pq = own_lo + rs_[mt][hf];
           const bool in = p < k1 && p <= pq && (a.mode != SFA_LOCAL || p > pq - a.window) &&
-                          (!shifting || p % a.n == rs_[mt][hf]);
+                          (!shifting || p - fast_div(p, a.d_n) * a.n == rs_[mt][hf]);
           if (!in) vis &= ~(1u << (mt * 8 + i));
         }
     }
@@ -550,6 +555,8 @@ cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* v
   a.d_nsplit = make_fast_div((uint32_t)plan.nsplit);
   a.table = table;
   a.pg = make_page_geom(num_pages, max_pages, P * n);
+  a.d_G = make_fast_div((uint32_t)plan.G);
+  a.d_n = make_fast_div((uint32_t)n);
   a.split_pages = (maxT + P - 1) / P / plan.nsplit;
   if (plan.tc) {
     paged_tile(a, 128);

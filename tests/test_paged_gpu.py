@@ -81,7 +81,7 @@ MASKS = [(WITHIN, 0), (CROSS, 0), (LOCAL, 1), (LOCAL, 100), (LOCAL, 2**31 - 1)]
 @pytest.mark.parametrize("mode,w", MASKS)
 @pytest.mark.parametrize("n,Hq,Hkv,Dh,P", [(4, 32, 8, 128, 16), (8, 32, 8, 128, 3), (8, 64, 8, 128, 1), (1, 8, 8, 128, 64),
                                            (3, 6, 2, 128, 7), (2, 4, 4, 64, 8), (3, 16, 4, 64, 50), (4, 8, 2, 64, 5),
-                                           (1, 8, 2, 128, 131), (4, 32, 8, 128, 2), (70, 2, 1, 64, 1), (5, 10, 2, 64, 9)])
+                                           (1, 8, 2, 128, 131), (4, 8, 2, 128, 43), (4, 32, 8, 128, 2), (70, 2, 1, 64, 1), (5, 10, 2, 64, 9)])
 def test_ragged(mode, w, n, Hq, Hkv, Dh, P):
     q, kc, vc = _case(4, 150, n, Hq, Hkv, Dh, n + Hq + P)
     _check(q, kc, vc, _i32([150, 1, 0, 129]), n, mode, w, P)
@@ -91,7 +91,7 @@ def test_ragged(mode, w, n, Hq, Hkv, Dh, P):
 # tiles), 256 rows on the other one
 @pytest.mark.parametrize("mode,w", MASKS)
 @pytest.mark.parametrize("n,Hq,Hkv,P", [(4, 24, 2, 16), (1, 4, 1, 3), (3, 6, 2, 5), (8, 32, 2, 4), (4, 24, 2, 32),
-                                        (4, 24, 2, 64), (2, 12, 2, 1), (8, 64, 2, 6), (8, 64, 2, 1), (3, 24, 2, 43), (1, 12, 1, 131), (1, 4, 1, 1)])
+                                        (4, 24, 2, 64), (2, 12, 2, 1), (8, 64, 2, 6), (8, 64, 2, 1), (3, 24, 2, 43), (4, 24, 2, 43), (1, 12, 1, 131), (1, 4, 1, 1)])
 def test_ragged_head_dim_256(mode, w, n, Hq, Hkv, P):
     q, kc, vc = _case(4, 150, n, Hq, Hkv, 256, 40 + n + Hq + P)
     _check(q, kc, vc, _i32([150, 1, 0, 129]), n, mode, w, P)
