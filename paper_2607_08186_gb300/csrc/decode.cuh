@@ -39,7 +39,7 @@ struct DecodeArgs {
   PageGeom pg;
   int tile, piece;       // paged: positions of a tile, in pieces of which none crosses a page
   int split_pages;       // paged: pages of a split of max_tokens tokens
-  FastDiv d_G, d_n;      // paged
+  FastDiv d_G, d_n, d_tile;  // paged
 };
 
 // What a partial's (max, sum) says beyond that: the split met a page that is not in the pool.
@@ -91,8 +91,8 @@ HD_DEVINLINE void split_range(const DecodeArgs& a, int T, int c, int kt, int& k0
   if (T < 1 || T > a.maxT) return;
   int lo, hi;
   seq_range(a, T, lo, hi);
-  if (PAGED) lo -= lo % kt;
-  const int tiles = (hi - lo + kt - 1) / kt, per = fast_div(tiles + a.nsplit - 1, a.d_nsplit);
+  if (PAGED) lo = fast_div(lo, a.d_tile) * kt;
+  const int tiles = PAGED ? fast_div(hi - lo + kt - 1, a.d_tile) : (hi - lo + kt - 1) / kt, per = fast_div(tiles + a.nsplit - 1, a.d_nsplit);
   if ((long long)c * per >= tiles) return;
   k0 = lo + c * per * kt;
   k1 = min(k0 + per * kt, hi);

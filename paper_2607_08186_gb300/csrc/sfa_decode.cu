@@ -533,10 +533,13 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
   grid_dep_wait();
   grid_dep_launch();
   const int T = a.lens[b];
+  // under that load: the page entries where the split starts if the sequence has max_tokens
+  if (PAGED && threadIdx.x == 32)
+    prefetch_l1(a.table + (long long)b * a.pg.max_pages + min(c * a.split_pages, a.pg.max_pages - 1));
   int k0, k1;
   const int tile = PAGED ? a.tile : BN;  // positions of a key tile: columns beyond them are masked
   dec::split_range<PAGED>(a, T, c, tile, k0, k1);
-  const int nt = (k1 - k0 + tile - 1) / tile, nunits = 4 * nt;
+  const int nt = PAGED ? fast_div(k1 - k0 + tile - 1, a.d_tile) : (k1 - k0 + BN - 1) / BN, nunits = 4 * nt;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();

@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
     }
     return;
   }
-  const int nsub = (k1 - k0 + tile - 1) / tile;
+  const int nsub = fast_div(k1 - k0 + tile - 1, a.d_tile);
   __syncthreads();  // the barriers and flags are set
 
   // ---- the tiles' loads
@@ -503,6 +503,7 @@ static void paged_tile(dec::DecodeArgs& a, int most) {
   while (a.pg.prow % d) --d;
   a.piece = d;
   a.tile = most / d * d;
+  a.d_tile = make_fast_div((uint32_t)a.tile);
 }
 
 template <int DH, int MT, bool TMA>
@@ -575,6 +576,7 @@ cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* v
       return cudaErrorInvalidValue;
   } else {
     a.tile = n <= KT ? KT / n * n : KT;  // any rows: whole tokens where a tile holds one
+    a.d_tile = make_fast_div((uint32_t)a.tile);
   }
   cudaError_t e;
   if (Dh == 64)
