@@ -319,16 +319,21 @@ def sfa_kv_append(k_new, v_new, k_cache, v_cache, lens, n, dev_status=None, stre
 # shape, layout or device raises ValueError before anything is enqueued.
 
 def _tensors(stream, *args):
-    """Each of args is (name, tensor, dtype, shape), or None for what the caller left out."""
+    """Check each of args, (name, tensor, dtype, shape) or None for what the caller left out; the stream's handle.
+    (A call's host time is what a short step takes: the checks are about 0.4 us a tensor.)"""
     dev = args[0][1].get_device()  # -1: not on a CUDA device
     for a in args:
-        if a is not None and not (a[1].dtype is a[2] and a[1].shape == a[3] and a[1].is_contiguous()
-                                  and a[1].get_device() == dev):
-            _refuse(dev, *a)
+        if a is not None:
+            name, t, dtype, shape = a
+            if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+                _refuse(dev, name, t, dtype, shape)
     if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError(f"{args[0][0]} is on {args[0][1].device}; it must be on the current CUDA device")
-    if stream is not None and stream.device_index != dev:
+    if stream is None:
+        return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+    if stream.device_index != dev:
         raise ValueError("stream belongs to another device than the current one")
+    return stream.cuda_stream
 
 
 def _refuse(dev, name, t, dtype, shape):
@@ -359,7 +364,8 @@ def sfa_fwd_packed_workspace_bytes(B, N, n, Hq, Hkv, Dh, mode) -> int:
     return int(lib().sfa_fwd_packed_workspace_bytes(B, N, n, Hq, Hkv, Dh, int(mode)))
 
 
-def sfa_fwd_packed(q, k, v, o, lse, offsets, n, mode, workspace, softmax_scale=0.0, window=0, dev_status=None, stream=None):
+def sfa_fwd_packed(q, k, v, o, lse, offsets, n, mode, workspace, softmax_scale=0.0, window=0, dev_status=None,
+                   stream=None):
     """sfa_fwd over whole prompts of different lengths, packed: q, o [N*n][Hq][Dh], k, v [N*n][Hkv][Dh] bf16, lse
     [Hq][N*n] float32; sequence b holds tokens offsets[b] .. offsets[b+1]-1 (int32 [B+1], ascending, within [0, N]).
     Rows outside [offsets[0], offsets[B]) are left as they were."""
@@ -369,12 +375,13 @@ def sfa_fwd_packed(q, k, v, o, lse, offsets, n, mode, workspace, softmax_scale=0
     Hkv, B = k.shape[1], offsets.shape[0] - 1
     if n < 1 or rows % n:
         raise ValueError("q.shape[0] must be N * n")
-    _tensors(stream, ("q", q, _BF16, (rows, Hq, Dh)), ("k", k, _BF16, (rows, Hkv, Dh)), ("v", v, _BF16, (rows, Hkv, Dh)),
-             ("o", o, _BF16, (rows, Hq, Dh)), ("lse", lse, _F32, (Hq, rows)), ("offsets", offsets, _I32, (B + 1,)),
-             _workspace(workspace), _dev_status(dev_status))
+    st = _tensors(stream, ("q", q, _BF16, (rows, Hq, Dh)), ("k", k, _BF16, (rows, Hkv, Dh)),
+                  ("v", v, _BF16, (rows, Hkv, Dh)), ("o", o, _BF16, (rows, Hq, Dh)), ("lse", lse, _F32, (Hq, rows)),
+                  ("offsets", offsets, _I32, (B + 1,)),
+                  _workspace(workspace), _dev_status(dev_status))
     _check(lib().sfa_fwd_packed(_p(q), _p(k), _p(v), _p(o), _p(lse), _p(offsets), B, rows // n, n, Hq, Hkv, Dh,
-                                float(softmax_scale), int(mode), int(window), _p(workspace), _wsb(workspace),
-                                _p(dev_status), _stream(stream)), "sfa_fwd_packed")
+                                float(softmax_scale), int(mode), int(window), _p(workspace), workspace.numel(),
+                                _p(dev_status), st), "sfa_fwd_packed")
     return o, lse
 
 
@@ -388,7 +395,8 @@ def _pool_dims(k_pages, page_table, n):
     return pages, rows // n, Hkv, Dh, *page_table.shape
 
 
-def sfa_kv_append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, n, offsets=None, dev_status=None, stream=None):
+def sfa_kv_append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, n, offsets=None, dev_status=None,
+                        stream=None):
     """New tokens' K/V rows into a paged cache: pools [num_pages][page_tokens*n][Hkv][Dh] bf16, page_table
     [B][max_pages] and lens [B] int32 (the new tokens counted).  Without offsets k_new, v_new [B][n][Hkv][Dh] hold one
     token a sequence (a slot with lens 0 is left out); with offsets [B+1] int32, packed rows [N*n][Hkv][Dh], tokens
@@ -398,12 +406,12 @@ def sfa_kv_append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, n, off
         N, shape = B, (B, n, Hkv, Dh)
     else:
         N, shape = k_new.shape[0] // n, (k_new.shape[0] // n * n, Hkv, Dh)
-    _tensors(stream, ("k_new", k_new, _BF16, shape), ("v_new", v_new, _BF16, shape),
-             ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
-             ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
-             _opt("offsets", offsets, _I32, (B + 1,)), _dev_status(dev_status))
+    st = _tensors(stream, ("k_new", k_new, _BF16, shape), ("v_new", v_new, _BF16, shape),
+                  ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
+                  ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
+                  _opt("offsets", offsets, _I32, (B + 1,)), _dev_status(dev_status))
     _check(lib().sfa_kv_append_paged(_p(k_new), _p(v_new), _p(k_pages), _p(v_pages), _p(page_table), _p(lens),
-                                     _p(offsets), B, N, pages, P, width, n, Hkv, Dh, _p(dev_status), _stream(stream)),
+                                     _p(offsets), B, N, pages, P, width, n, Hkv, Dh, _p(dev_status), st),
            "sfa_kv_append_paged")
 
 
@@ -421,13 +429,13 @@ def sfa_decode_paged(q, k_pages, v_pages, page_table, lens, o, n, mode, workspac
         raise ValueError("q must be [B][n][Hq][Dh]")
     Hq = q.shape[2]
     T = P * width if max_tokens is None else int(max_tokens)
-    _tensors(stream, ("q", q, _BF16, (B, n, Hq, Dh)), ("o", o, _BF16, (B, n, Hq, Dh)),
-             ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
-             ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
-             _opt("lse", lse, _F32, (B, Hq, n)), _workspace(workspace), _dev_status(dev_status))
+    st = _tensors(stream, ("q", q, _BF16, (B, n, Hq, Dh)), ("o", o, _BF16, (B, n, Hq, Dh)),
+                  ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
+                  ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
+                  _opt("lse", lse, _F32, (B, Hq, n)), _workspace(workspace), _dev_status(dev_status))
     _check(lib().sfa_decode_paged(_p(q), _p(k_pages), _p(v_pages), _p(page_table), _p(lens), _p(o), _p(lse), B, T, pages,
                                   P, width, n, Hq, Hkv, Dh, float(softmax_scale), int(mode), int(window), _p(workspace),
-                                  _wsb(workspace), _p(dev_status), _stream(stream)), "sfa_decode_paged")
+                                  workspace.numel(), _p(dev_status), st), "sfa_decode_paged")
     return o
 
 
@@ -448,20 +456,21 @@ def hd_pages_grow(refs, page_table, lens, add, page_tokens, workspace, dev_statu
     page_table [B][max_pages], lens, add [B] int32.  A sequence that finds no free page stays as it was and sets
     HD_DEVBIT_PAGES."""
     B, width, pages, state = _page_state(refs, page_table, lens)
-    _tensors(stream, *state, ("add", add, _I32, (B,)), _workspace(workspace), _dev_status(dev_status))
+    st = _tensors(stream, *state, ("add", add, _I32, (B,)), _workspace(workspace), _dev_status(dev_status))
     _check(lib().hd_pages_grow(_p(refs), _p(page_table), _p(lens), _p(add), B, width, pages, int(page_tokens),
-                               _p(workspace), _wsb(workspace), _p(dev_status), _stream(stream)), "hd_pages_grow")
+                               _p(workspace), workspace.numel(), _p(dev_status), st), "hd_pages_grow")
 
 
-def hd_pages_fork(refs, page_table, lens, src, dst, tokens, copies, page_tokens, workspace, dev_status=None, stream=None):
+def hd_pages_fork(refs, page_table, lens, src, dst, tokens, copies, page_tokens, workspace, dev_status=None,
+                  stream=None):
     """The empty slots dst get the first `tokens` tokens (None: all) of the slots src: full pages are shared, a partly
     filled last one is new and listed in copies [F][2] (page of src, page of dst; else -1, -1) for hd_pages_copy."""
     B, width, pages, state = _page_state(refs, page_table, lens)
     F = src.numel()
-    _tensors(stream, *state, ("src", src, _I32, (F,)), ("dst", dst, _I32, (F,)), _opt("tokens", tokens, _I32, (F,)),
-             ("copies", copies, _I32, (F, 2)), _workspace(workspace), _dev_status(dev_status))
+    st = _tensors(stream, *state, ("src", src, _I32, (F,)), ("dst", dst, _I32, (F,)), _opt("tokens", tokens, _I32, (F,)),
+                  ("copies", copies, _I32, (F, 2)), _workspace(workspace), _dev_status(dev_status))
     _check(lib().hd_pages_fork(_p(refs), _p(page_table), _p(lens), _p(src), _p(dst), _p(tokens), F, _p(copies), B, width,
-                               pages, int(page_tokens), _p(workspace), _wsb(workspace), _p(dev_status), _stream(stream)),
+                               pages, int(page_tokens), _p(workspace), workspace.numel(), _p(dev_status), st),
            "hd_pages_fork")
     return copies
 
@@ -469,9 +478,9 @@ def hd_pages_fork(refs, page_table, lens, src, dst, tokens, copies, page_tokens,
 def hd_pages_free(refs, page_table, lens, seqs, page_tokens, dev_status=None, stream=None):
     """The slots seqs are emptied: lens 0, their entries of page_table -1, their pages held by one sequence less."""
     B, width, pages, state = _page_state(refs, page_table, lens)
-    _tensors(stream, *state, ("seqs", seqs, _I32, (seqs.numel(),)), _dev_status(dev_status))
+    st = _tensors(stream, *state, ("seqs", seqs, _I32, (seqs.numel(),)), _dev_status(dev_status))
     _check(lib().hd_pages_free(_p(refs), _p(page_table), _p(lens), _p(seqs), seqs.numel(), B, width, pages,
-                               int(page_tokens), _p(dev_status), _stream(stream)), "hd_pages_free")
+                               int(page_tokens), _p(dev_status), st), "hd_pages_free")
 
 
 def hd_pages_compact(refs, page_table, lens, new_refs, new_table, moves, page_tokens, workspace, dev_status=None,
@@ -479,20 +488,20 @@ def hd_pages_compact(refs, page_table, lens, new_refs, new_table, moves, page_to
     """The K pages in use get the ids 0 .. K-1 in new_refs and new_table (which may be refs and page_table); moves
     [num_pages // 2][2] lists the pages to copy (old, new; then -1, -1) for hd_pages_copy."""
     B, width, pages, state = _page_state(refs, page_table, lens)
-    _tensors(stream, *state, ("new_refs", new_refs, _I32, (pages,)), ("new_table", new_table, _I32, (B, width)),
-             ("moves", moves, _I32, (pages // 2, 2)), _workspace(workspace), _dev_status(dev_status))
+    st = _tensors(stream, *state, ("new_refs", new_refs, _I32, (pages,)), ("new_table", new_table, _I32, (B, width)),
+                  ("moves", moves, _I32, (pages // 2, 2)), _workspace(workspace), _dev_status(dev_status))
     _check(lib().hd_pages_compact(_p(refs), _p(page_table), _p(lens), _p(new_refs), _p(new_table), _p(moves), B, width,
-                                  pages, int(page_tokens), _p(workspace), _wsb(workspace), _p(dev_status),
-                                  _stream(stream)), "hd_pages_compact")
+                                  pages, int(page_tokens), _p(workspace), workspace.numel(), _p(dev_status),
+                                  st), "hd_pages_compact")
     return new_refs, new_table, moves
 
 
 def hd_pages_copy(k_pages, v_pages, copies, dev_status=None, stream=None):
     """Page copies[i][0] onto page copies[i][1] in both pools (one layer's); pairs of -1 are left out."""
-    _tensors(stream, ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
-             ("copies", copies, _I32, (copies.numel() // 2, 2)), _dev_status(dev_status))
+    st = _tensors(stream, ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
+                  ("copies", copies, _I32, (copies.numel() // 2, 2)), _dev_status(dev_status))
     _check(lib().hd_pages_copy(_p(k_pages), _p(v_pages), _p(copies), copies.shape[0], k_pages.shape[0],
-                               k_pages[0].numel() * 2, _p(dev_status), _stream(stream)), "hd_pages_copy")
+                               k_pages[0].numel() * 2, _p(dev_status), st), "hd_pages_copy")
 
 
 SFA_BWD_NOALLOC_MAX_BYTES = 64 << 20
