@@ -57,20 +57,25 @@ HD_DEVINLINE int block_scan(int v, int* sh, int& total) {
   return before + x - v;
 }
 
+// Counts of pages id .. id + 3 (id a multiple of 4); `none` for those behind the pool.
+HD_DEVINLINE void load_refs(const int32_t* refs, int num_pages, int id, int none, int* r) {
+  if (id + 3 < num_pages) {
+    const int4 q = *reinterpret_cast<const int4*>(refs + id);
+    r[0] = q.x, r[1] = q.y, r[2] = q.z, r[3] = q.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = id + e < num_pages ? refs[id + e] : none;
+  }
+}
+
 // The free pages' ids, ascending, into list[0, want), as far as there are as many; returns how
 // many were written.
 HD_DEVINLINE int list_free(const State& s, int want, int32_t* list, int* sh) {
   int found = 0;
   for (int p0 = 0; p0 < s.num_pages && found < want; p0 += 4 * NT) {
     const int id = p0 + 4 * (int)threadIdx.x;
-    int r[4] = {1, 1, 1, 1};
-    if (id + 3 < s.num_pages) {
-      const int4 q = *reinterpret_cast<const int4*>(s.refs + id);
-      r[0] = q.x, r[1] = q.y, r[2] = q.z, r[3] = q.w;
-    } else {
-      for (int e = 0; e < 4; ++e)
-        if (id + e < s.num_pages) r[e] = s.refs[id + e];
-    }
+    int r[4];
+    load_refs(s.refs, s.num_pages, id, 1, r);
     int total;
     int at = found + block_scan((r[0] == 0) + (r[1] == 0) + (r[2] == 0) + (r[3] == 0), sh, total);
 #pragma unroll
@@ -237,19 +242,35 @@ __global__ void __launch_bounds__(NT) compact_plan_kernel(const int32_t* refs, i
   grid_dep_wait();
   grid_dep_launch();
   int live = 0;
-  for (int p = threadIdx.x; p < num_pages; p += NT) live += refs[p] > 0;
+  for (int p0 = 0; p0 < num_pages; p0 += 4 * NT) {
+    int r[4];
+    load_refs(refs, num_pages, p0 + 4 * (int)threadIdx.x, 0, r);
+    live += (r[0] > 0) + (r[1] > 0) + (r[2] > 0) + (r[3] > 0);
+  }
   int K;
   block_scan(live, sh, K);
   int nlow = 0, nhigh = 0;
-  for (int p0 = 0; p0 < num_pages; p0 += NT) {
-    const int p = p0 + (int)threadIdx.x;
-    const bool in = p < num_pages, on = in && refs[p] > 0;
-    const bool is_low = in && !on && p < K, is_high = on && p >= K;
-    int sum;  // a chunk's two counts in one scan, 16 bits each (at most NT of both)
-    const int at = block_scan((int)is_low | (int)is_high << 16, sh, sum);
-    if (is_low) low[nlow + (at & 0xffff)] = p;
-    if (is_high) high[nhigh + (at >> 16)] = p;
-    if (in && !is_high) map[p] = on ? p : -1;
+  for (int p0 = 0; p0 < num_pages; p0 += 4 * NT) {
+    const int p = p0 + 4 * (int)threadIdx.x;
+    int r[4], both = 0;
+    load_refs(refs, num_pages, p, 0, r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (p + e < num_pages) both += r[e] > 0 ? (int)(p + e >= K) << 16 : (int)(p + e < K);
+    int sum;  // a chunk's two counts in one scan, 16 bits each (at most 4 * NT of both)
+    const int at = block_scan(both, sh, sum);
+    int lo = nlow + (at & 0xffff), hi = nhigh + (at >> 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (p + e >= num_pages) continue;
+      const bool on = r[e] > 0;
+      if (on && p + e >= K) {
+        high[hi++] = p + e;
+      } else {
+        map[p + e] = on ? p + e : -1;
+        if (!on && p + e < K) low[lo++] = p + e;
+      }
+    }
     nlow += sum & 0xffff;
     nhigh += sum >> 16;
   }
