@@ -307,6 +307,18 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
           if (j < n_hi) mbar_wait(&sm.full[(u + 1) % NSLOT], ((u + 1) / NSLOT) & 1, abort, P.a.status);
         }
         __syncwarp();
+        if (kb + BN > rows) {  // V rows behind the sequence (every group that reads them zeroes them);
+                               // here, under the S of the tile
+          if (!__all_sync(0xffffffffu, mbar_wait(&sm.full[u % NSLOT], (u / NSLOT) & 1, abort, P.a.status))) {
+            ok = false;
+            break;
+          }
+          for (int e = (rows - kb) * 8 + row; e < BN * 8; e += 128)
+#pragma unroll
+            for (int c = 0; c < DH / 64; ++c)
+              reinterpret_cast<uint4*>(sm.ring[u % NSLOT] + c * BN * 64)[e] = make_uint4(0, 0, 0, 0);
+          fence_async_smem();
+        }
         // tcgen05.ld/st are warp-collective: every wait result is made warp-uniform
         if (!__all_sync(0xffffffffu, mbar_wait(&sm.s_full[g], tiles & 1, abort, P.a.status))) {
           ok = false;
@@ -332,29 +344,17 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
               if (e < e_lo) x[e] = -INFINITY;
           }
         }
-        float mx[8];
+        float mx[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) mx[e] = x[e];
+        for (int e = 0; e < 4; ++e) mx[e] = x[e];
 #pragma unroll
-        for (int e = 8; e < BN; ++e) mx[e & 7] = fmaxf(mx[e & 7], x[e]);
-        const float tmax = fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
-                                 fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
+        for (int e = 4; e < BN; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], x[e], x[e + 1]);
+        const float tmax = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]);
         const float m_new = fmaxf(m_run, tmax);
         const bool rescale = (m_run == -INFINITY) || ((m_new - m_run) * c2 > kRescaleThreshold);
         const float m_use = rescale ? m_new : m_run;
         const float neg = (m_use == -INFINITY) ? 0.f : -m_use * c2;
         const uint64_t neg2 = f2pack(neg, neg);
-        if (kb + BN > rows) {  // V rows behind the sequence (every group that reads them zeroes them)
-          if (!__all_sync(0xffffffffu, mbar_wait(&sm.full[u % NSLOT], (u / NSLOT) & 1, abort, P.a.status))) {
-            ok = false;
-            break;
-          }
-          for (int e = (rows - kb) * 8 + row; e < BN * 8; e += 128)
-#pragma unroll
-            for (int c = 0; c < DH / 64; ++c)
-              reinterpret_cast<uint4*>(sm.ring[u % NSLOT] + c * BN * 64)[e] = make_uint4(0, 0, 0, 0);
-          fence_async_smem();
-        }
         // P (bf16 pairs) over the first half of this group's S columns
         uint64_t sum2[4] = {0, 0, 0, 0};
         const bool mine = rescale && m_run != -INFINITY && j > lo;

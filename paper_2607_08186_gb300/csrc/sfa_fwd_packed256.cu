@@ -285,6 +285,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
           if (t + 2 < T) mbar_wait(&sm.full[uk % NSLOT], (uk / NSLOT) & 1, abort, A.status);
         }
         __syncwarp();
+        if (ok && t == T - 1) {  // under the S of the tile: this CTA's half of the last V has landed
+          ok = __all_sync(0xffffffffu, mbar_wait(&sm.v_tail[k & 3], (k >> 2) & 1, abort, A.status));
+          if (ok && (j + 1) * BN > w.rows) {  // its rows behind the sequence
+            bf16* vt = sm.ring[(units + 2 * T - 1) % NSLOT];
+            for (int e = (w.rows - j * BN) * 8 + hc * BM + row; e < BN * 8; e += 2 * BM)
+#pragma unroll
+              for (int c = 0; c < PC / 64; ++c) reinterpret_cast<uint4*>(vt + c * BN * 64)[e] = make_uint4(0, 0, 0, 0);
+            fence_async_smem();
+          }
+        }
         // tcgen05.ld/st are warp-collective: every wait result is made warp-uniform
         ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.s_full[tile & 3], (tile >> 2) & 1, abort, A.status));
         float x[HB], tmax = -INFINITY;
@@ -313,22 +323,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
 #pragma unroll
           for (int e = 0; e < 4; ++e) mx[e] = x[e];
 #pragma unroll
-          for (int e = 4; e < HB; ++e) mx[e & 3] = fmaxf(mx[e & 3], x[e]);
-          tmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          for (int e = 4; e < HB; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], x[e], x[e + 1]);
+          tmax = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]);
           sm.part[tile & 1][hc][row] = tmax;
         }
         // the two warps of these 32 rows meet here on every tile, also after a wait gave up
         named_bar_sync(1 + q4, 64);
-        if (ok && t == T - 1) {  // this CTA's half of the last V tile has landed
-          ok = __all_sync(0xffffffffu, mbar_wait(&sm.v_tail[k & 3], (k >> 2) & 1, abort, A.status));
-          if (ok && (j + 1) * BN > w.rows) {  // its rows behind the sequence
-            bf16* vt = sm.ring[(units + 2 * T - 1) % NSLOT];
-            for (int e = (w.rows - j * BN) * 8 + hc * BM + row; e < BN * 8; e += 2 * BM)
-#pragma unroll
-              for (int c = 0; c < PC / 64; ++c) reinterpret_cast<uint4*>(vt + c * BN * 64)[e] = make_uint4(0, 0, 0, 0);
-            fence_async_smem();
-          }
-        }
         if (!ok) continue;
         const float m_new = fmaxf(m_run, fmaxf(tmax, sm.part[tile & 1][hc ^ 1][row]));
         const bool rescale = (m_run == -INFINITY) || ((m_new - m_run) * c2 > kRescaleThreshold);

@@ -167,6 +167,13 @@ HD_DEVINLINE void st_global_32(void* p, const uint32_t* r) {
                : "memory");
 }
 
+// The largest of three (NaN operands are passed over, as by fmaxf).
+HD_DEVINLINE float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // Two fp32 -> packed bf16x2 (round to nearest even); `lo` lands in the low half.
 HD_DEVINLINE uint32_t cvt_bf16x2(float lo, float hi) {
   uint32_t r;
