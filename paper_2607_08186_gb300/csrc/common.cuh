@@ -104,7 +104,6 @@ HD_DEVINLINE void cp_async_16(uint32_t dst, const void* src, bool pred) {
   int sz = pred ? 16 : 0;  // src-size 0 zero-fills the 16 destination bytes
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(sz));
 }
-HD_DEVINLINE void prefetch_l1(const void* p) { asm volatile("prefetch.global.L1 [%0];\n" ::"l"(p)); }
 HD_DEVINLINE void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::); }
 template <int N>
 HD_DEVINLINE void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N)); }

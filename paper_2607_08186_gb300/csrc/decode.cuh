@@ -28,8 +28,8 @@ struct DecodeArgs {
   const int32_t* lens;  // [B] tokens in the cache
   bf16* o;              // [B][n][Hq][Dh]
   float* lse;           // [B][Hq][n] or null
-  float* part_o;        // [B][Hkv][ngroups][nsplit][rg][Dh]
-  float2* part_ml;      // [B][Hkv][ngroups][nsplit][rg]: (max in log2 units, sum)
+  float* part_o;        // [B][Hkv][ngroups][nsplit][rg][Dh]; paged: [B * nsplit][Hkv][ngroups][rg][Dh]
+  float2* part_ml;      // the same without [Dh]: (max in log2 units, sum)
   int32_t* status;
   int B, Lcap, maxT, n, Hq, Hkv, G, M, ngroups, nsplit, mode, window;
   int rg;               // query rows per row group (the partials' row pitch)
@@ -38,8 +38,13 @@ struct DecodeArgs {
   const int32_t* table;  // paged: [B][pg.max_pages]; kc, vc are the pools
   PageGeom pg;
   int tile, piece;       // paged: positions of a tile, in pieces of which none crosses a page
-  int split_pages;       // paged: pages of a split of max_tokens tokens
   FastDiv d_G, d_n, d_tile;  // paged
+  // paged: the grid is linear, a split's K/V heads (x row groups) together, since their rows are
+  FastDiv d_heads;
+  // paged: the B * nsplit splits are shared out by the sequences' lengths (PagedSplit); share [B]: the
+  // first split of each sequence and their number, for the combine kernel
+  int balanced;
+  int2* share;
 };
 
 // What a partial's (max, sum) says beyond that: the split met a page that is not in the pool.
@@ -97,6 +102,84 @@ HD_DEVINLINE void split_range(const DecodeArgs& a, int T, int c, int kt, int& k0
   k0 = lo + c * per * kt;
   k1 = min(k0 + per * kt, hi);
 }
+
+// Split x of the B * nsplit of a paged batch (tensor-core kernel): sequence, its tokens and the
+// positions [k0, k1), found by a whole warp.  In general split x is the (x mod nsplit)-th of sequence
+// x / nsplit.  Balanced (several sequences, long splits), a split is `per` tiles of whichever sequence,
+// with the least `per` (to 1/16) at which all splits suffice.
+constexpr int kBalancedSeqs = 128;
+struct PagedSplit {
+  int b, T, k0, k1;
+  HD_DEVINLINE PagedSplit(const DecodeArgs& a, int x, bool report) {
+    k0 = k1 = 0;
+    if (!a.balanced) {
+      b = fast_div(x, a.d_nsplit);
+      T = a.lens[b];
+      split_range<true>(a, T, x - b * a.nsplit, a.tile, k0, k1);
+      return;
+    }
+    constexpr int NI = kBalancedSeqs / 32;
+    const int lane = threadIdx.x & 31, nb = (a.B + 31) / 32, S = a.B * a.nsplit;
+    int len[NI], tiles[NI], total = 0, most = 0;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int q = i * 32 + lane;
+      len[i] = i < nb && q < a.B ? a.lens[q] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      tiles[i] = 0;
+      if (len[i] >= 1 && len[i] <= a.maxT) {
+        int lo, hi;
+        seq_range(a, len[i], lo, hi);
+        tiles[i] = fast_div(hi - fast_div(lo, a.d_tile) * a.tile + a.tile - 1, a.d_tile);
+      }
+      total += tiles[i];
+      most = max(most, tiles[i]);
+    }
+    total = __reduce_add_sync(0xffffffffu, total);
+    most = __reduce_max_sync(0xffffffffu, most);
+    // the least `per` is between these two: sum ceil(tiles / per) <= total / per + B
+    unsigned least = max(1u, max((total + (unsigned)S - 1) / S, (most + (unsigned)kMaxSplit - 1) / kMaxSplit));
+    unsigned per = max(least, (total + (unsigned)(S - a.B) - 1) / (S - a.B));
+    for (int step = 0; step < 4 && least < per; ++step) {
+      const unsigned mid = (least + per) / 2;
+      unsigned need = 0;
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        if (i < nb) need += (tiles[i] + mid - 1) / mid;
+      if (__reduce_add_sync(0xffffffffu, need) <= (unsigned)S) per = mid;
+      else least = mid + 1;
+    }
+    int before = 0;
+    b = T = 0;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      if (i >= nb) break;
+      const int n = (int)((tiles[i] + per - 1) / per);
+      int upto = n;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += y;
+      }
+      const int first = before + upto - n;
+      if (report && i * 32 + lane < a.B) a.share[i * 32 + lane] = make_int2(first, n);
+      const unsigned hit = __ballot_sync(0xffffffffu, first <= x && x < first + n);
+      if (hit) {
+        const int l = __ffs(hit) - 1;
+        b = i * 32 + l;
+        T = __shfl_sync(0xffffffffu, len[i], l);
+        int lo, hi;
+        seq_range(a, T, lo, hi);
+        const int step = (int)per * a.tile;
+        k0 = fast_div(lo, a.d_tile) * a.tile + (x - __shfl_sync(0xffffffffu, first, l)) * step;
+        k1 = hi - k0 < step ? hi : k0 + step;
+      }
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+  }
+};
 }  // namespace dec
 
 // The tcgen05 kernel over a paged cache (head dim 256), and the combine kernel after either.

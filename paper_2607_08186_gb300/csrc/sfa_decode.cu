@@ -303,22 +303,27 @@ __global__ void __launch_bounds__(256) combine_kernel(DecodeArgs a) {
   __shared__ float4 part[SG][LW];
   const int row = blockIdx.x, g = blockIdx.y / a.ngroups, rg = blockIdx.y % a.ngroups, b = blockIdx.z;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, l4 = tid % LW, sg = tid / LW;
-  const size_t pidx0 = (((size_t)b * a.Hkv + g) * a.ngroups + rg) * a.nsplit;
-  const float* po = a.part_o + (pidx0 * a.rg + row) * DH + l4 * 4;
-  const size_t pitch = (size_t)a.rg * DH;  // between a row's partials
   grid_dep_wait();  // every partial of the decode kernel is written
+  const int2 own = PAGED ? (a.balanced ? a.share[b] : make_int2(b * a.nsplit, a.nsplit)) : make_int2(0, a.nsplit);
+  const int nsplit = own.y;
+  // partials of a row: the first, and (in rows) how far they lie apart
+  const size_t pidx0 = PAGED ? ((size_t)own.x * a.Hkv + g) * a.ngroups + rg
+                             : (((size_t)b * a.Hkv + g) * a.ngroups + rg) * a.nsplit;
+  const size_t step = PAGED ? (size_t)a.Hkv * a.ngroups * a.rg : (size_t)a.rg;
+  const float* po = a.part_o + (pidx0 * a.rg + row) * DH + l4 * 4;
+  const size_t pitch = step * DH;
   const int r = rg * a.rg + row;
   const int T = a.lens[b];
   const bool valid = T >= 1 && T <= a.maxT;
   if (!valid && !(PAGED && T == 0) && blockIdx.x == 0 && blockIdx.y == 0 && tid == 0)
     set_status(a.status, HD_DEVBIT_INDEX);
   if (r >= a.M) return;  // the last row group may be short
-  const float2 ml = tid < a.nsplit ? a.part_ml[(pidx0 + tid) * a.rg + row] : make_float2(-INFINITY, 0.f);
+  const float2 ml = tid < nsplit ? a.part_ml[pidx0 * a.rg + tid * step + row] : make_float2(-INFINITY, 0.f);
   float4 x[NB];
 #pragma unroll
   for (int k = 0; k < NB; ++k) {
     const int c = sg + k * SG;
-    if (c < a.nsplit) x[k] = *reinterpret_cast<const float4*>(po + c * pitch);
+    if (c < nsplit) x[k] = *reinterpret_cast<const float4*>(po + c * pitch);
   }
   float m = ml.x;
 #pragma unroll
@@ -328,7 +333,7 @@ __global__ void __launch_bounds__(256) combine_kernel(DecodeArgs a) {
 #pragma unroll
   for (int w = 0; w < 8; ++w) m = fmaxf(m, red[0][w]);
   const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - m);
-  if (tid < a.nsplit) wgt[tid] = f;
+  if (tid < nsplit) wgt[tid] = f;
   float l = f * ml.y;
 #pragma unroll
   for (int off = 16; off; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
@@ -355,14 +360,14 @@ __global__ void __launch_bounds__(256) combine_kernel(DecodeArgs a) {
   };
 #pragma unroll
   for (int k = 0; k < NB; ++k)
-    if (sg + k * SG < a.nsplit) add(sg + k * SG, x[k]);
-  for (int c0 = sg + NB * SG; c0 < a.nsplit; c0 += NB * SG) {
+    if (sg + k * SG < nsplit) add(sg + k * SG, x[k]);
+  for (int c0 = sg + NB * SG; c0 < nsplit; c0 += NB * SG) {
 #pragma unroll
     for (int k = 0; k < NB; ++k)
-      if (c0 + k * SG < a.nsplit) x[k] = *reinterpret_cast<const float4*>(po + (c0 + k * SG) * pitch);
+      if (c0 + k * SG < nsplit) x[k] = *reinterpret_cast<const float4*>(po + (c0 + k * SG) * pitch);
 #pragma unroll
     for (int k = 0; k < NB; ++k)
-      if (c0 + k * SG < a.nsplit) add(c0 + k * SG, x[k]);
+      if (c0 + k * SG < nsplit) add(c0 + k * SG, x[k]);
   }
   part[sg][l4] = acc;
   __syncthreads();
@@ -493,9 +498,11 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
   const dec::DecodeArgs& a = P.a;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  const int c = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+  const int c = PAGED ? fast_div((int)blockIdx.x, a.d_heads) : blockIdx.x;
+  const int g = PAGED ? (int)blockIdx.x - c * a.Hkv : blockIdx.y;
+  int b = blockIdx.z;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const size_t pidx = ((size_t)b * a.Hkv + g) * a.nsplit + c;
+  const size_t pidx = PAGED ? blockIdx.x : ((size_t)b * a.Hkv + g) * a.nsplit + c;
   float* po = a.part_o + pidx * a.rg * DH;
   float2* pml = a.part_ml + pidx * a.rg;
   // Set-up first: it needs nothing from the kernels before this one.  Rows M..127 of the
@@ -532,13 +539,18 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
   }
   grid_dep_wait();
   grid_dep_launch();
-  const int T = a.lens[b];
-  // under that load: the page entries where the split starts if the sequence has max_tokens
-  if (PAGED && threadIdx.x == 32)
-    prefetch_l1(a.table + (long long)b * a.pg.max_pages + min(c * a.split_pages, a.pg.max_pages - 1));
-  int k0, k1;
+  int T, k0, k1;
   const int tile = PAGED ? a.tile : BN;  // positions of a key tile: columns beyond them are masked
-  dec::split_range<PAGED>(a, T, c, tile, k0, k1);
+  if constexpr (PAGED) {
+    const dec::PagedSplit sp(a, c, c == 0 && g == 0 && warp == 0);
+    b = sp.b;
+    T = sp.T;
+    k0 = sp.k0;
+    k1 = sp.k1;
+  } else {
+    T = a.lens[b];
+    dec::split_range(a, T, c, tile, k0, k1);
+  }
   const int nt = PAGED ? fast_div(k1 - k0 + tile - 1, a.d_tile) : (k1 - k0 + BN - 1) / BN, nunits = 4 * nt;
   tc_fence_before();
   __syncthreads();
@@ -986,7 +998,7 @@ static cudaError_t launch_decode_tc(const dec::DecodeArgs& a, cudaStream_t st) {
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   pdl[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.nsplit, a.Hkv, a.B);
+  cfg.gridDim = PAGED ? dim3((unsigned)a.nsplit * a.B * a.Hkv) : dim3(a.nsplit, a.Hkv, a.B);
   cfg.blockDim = dim3(NTHREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;

@@ -86,10 +86,11 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
     }
   }
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  const int c = blockIdx.x, g = blockIdx.y / a.ngroups, rg = blockIdx.y % a.ngroups, b = blockIdx.z;
+  const int split = fast_div((int)blockIdx.x, a.d_heads), head = (int)blockIdx.x - split * a.Hkv * a.ngroups;
+  const int g = a.ngroups == 1 ? head : head / a.ngroups, rg = a.ngroups == 1 ? 0 : head % a.ngroups;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, t4 = lane & 3;
   const int kw = warp / DS, dw = warp % DS;  // key group and head-dim part of this warp
-  const size_t pidx = (((size_t)b * a.Hkv + g) * a.ngroups + rg) * a.nsplit + c;
+  const size_t pidx = blockIdx.x;
   float* po = a.part_o + pidx * RG * DH;
   float2* pml = a.part_ml + pidx * RG;
   const int tile = a.tile;
@@ -140,10 +141,8 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
   }
   grid_dep_wait();
   grid_dep_launch();
-  const int T = a.lens[b];
+  const int b = fast_div(split, a.d_nsplit), T = a.lens[b];
   const int32_t* table = a.table + (long long)b * a.pg.max_pages;
-  // under that load: the page entries where the split starts if the sequence has max_tokens
-  if (tid == 32) prefetch_l1(table + min(c * a.split_pages, a.pg.max_pages - 1));
   auto load_q = [&] {  // query rows of the group (rows past M zero-filled)
     for (int i = tid; i < MT * 16 * CPR; i += NT) {
       const int rr = i / CPR, cc = i % CPR, r = rg * RG + rr;
@@ -153,7 +152,7 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
     }
   };
   int k0, k1;
-  split_range<true>(a, T, c, tile, k0, k1);
+  split_range<true>(a, T, split - b * a.nsplit, tile, k0, k1);
   if (k0 >= k1) {  // nothing of this sequence in this split: an empty partial, or an empty result
     if (a.nsplit > 1) {
       for (int i = tid; i < RG; i += NT) pml[i] = make_float2(-INFINITY, 0.f);
@@ -490,10 +489,13 @@ static DecodePlan paged_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, in
   return p;
 }
 
+// The sequences' shares of a balanced batch's splits, in front of the partials.
+constexpr size_t kShareBytes = dec::kBalancedSeqs * sizeof(int2);
+
 size_t decode_paged_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {
   // either kernel's, whatever the pages
   return std::max(decode_ws_bytes(decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, true)),
-                  decode_ws_bytes(decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, false)));
+                  decode_ws_bytes(decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, false))) + kShareBytes;
 }
 
 // A tile of at most `most` positions: whole pieces, the largest that no page boundary cuts (a page's
@@ -514,8 +516,8 @@ static cudaError_t launch_paged_t(const dec::PagedParams& p, cudaStream_t st) {
   const int smem = (int)sizeof(PagedSmem<DH, MT>) + (DH == 256 ? 0 : 1024);
   cudaError_t e = cudaFuncSetAttribute(decode_paged_kernel<DH, MT, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(true, decode_paged_kernel<DH, MT, TMA>, dim3(p.a.nsplit, p.a.Hkv * p.a.ngroups, p.a.B), NT, smem, st,
-                       p);
+  return launch_kernel(true, decode_paged_kernel<DH, MT, TMA>, dim3((unsigned)p.a.nsplit * p.a.B * p.a.Hkv * p.a.ngroups), NT,
+                       smem, st, p);
 }
 
 template <int DH, bool TMA>
@@ -537,8 +539,9 @@ cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* v
   a.lens = lens;
   a.o = (bf16*)o;
   a.lse = lse;
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + ((plan.part_o_bytes + 255) & ~size_t(255)));
+  a.share = static_cast<int2*>(ws);
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + kShareBytes);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + kShareBytes + ((plan.part_o_bytes + 255) & ~size_t(255)));
   a.status = status;
   a.B = B;
   a.maxT = maxT;
@@ -558,9 +561,17 @@ cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* v
   a.pg = make_page_geom(num_pages, max_pages, P * n);
   a.d_G = make_fast_div((uint32_t)plan.G);
   a.d_n = make_fast_div((uint32_t)n);
-  a.split_pages = (maxT + P - 1) / P / plan.nsplit;
+  a.d_heads = make_fast_div((uint32_t)(Hkv * plan.ngroups));
   if (plan.tc) {
     paged_tile(a, 128);
+    // Splits shared out by length, where they are of some tiles (finding one takes about 0.5 us).  This
+    // kernel has an SM to itself, so nobody takes up what a short sequence's split leaves: 7 sequences
+    // of a quarter to all of 8192 tokens, 24 over 2 heads, 68.2 -> 60.9 us.  The other kernel's two
+    // CTAs per SM do (4 and 16 such sequences 69.3 and 113 us, shared out 72.0 and 115).
+    const long long range = mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1)
+                                              : (long long)maxT * n;
+    a.balanced = B > 1 && B <= dec::kBalancedSeqs && plan.nsplit > 1 && range / plan.nsplit >= 4 * 64 &&
+                 B * (range / a.tile + 1) < (1LL << 30);  // the tiles of all sequences, counted in 32 bits
     return launch_decode_paged_tc(a, st);
   }
   const int KT = Dh == 256 ? dec::ktile<256>() : dec::ktile<128>();

@@ -105,6 +105,27 @@ def test_long(n, Hq, Hkv, Dh, mode, P):
     _check(q, kc, vc, _i32([8192, 3001]), n, mode, 0, P)
 
 
+@pytest.mark.parametrize("mode,w", [(WITHIN, 0), (CROSS, 0), (LOCAL, 2000)])
+@pytest.mark.parametrize("B,Hq,Hkv,Dh,P", [(3, 8, 2, 128, 16), (33, 4, 1, 128, 7), (70, 2, 2, 64, 16), (7, 24, 2, 256, 16),
+                                           (40, 2, 1, 256, 20)])
+def test_splits_shared_out_by_length(mode, w, B, Hq, Hkv, Dh, P):
+    # long splits of sequences of very different lengths, empty ones, one beyond max_tokens and one below
+    # zero among them (these three alone are empty); more sequences than a warp has lanes
+    n, L = 4, 1500
+    lens = [max(0, int(L * (0.618 * b % 1.0)) - 60) for b in range(B)]
+    lens[0] = L
+    if B > 10:
+        lens[5], lens[B - 1] = -7, L + 1
+    q, kc, vc = _case(B, L, n, Hq, Hkv, Dh, B)
+    held = [x if 0 <= x <= L else 0 for x in lens]
+    kp, table = paging.to_pages(kc, held, P, n, 1, width=-(-L // P))
+    vp, _ = paging.to_pages(vc, held, P, n, 1, width=-(-L // P))
+    o, lse, st = _decode(q, kp, vp, table, _i32(lens), n, mode, w, max_tokens=L)
+    assert st == (binding.HD_DEVBIT_INDEX if B > 10 else 0)
+    for b, T in enumerate(held):
+        _assert_empty(o, lse, b) if T == 0 else _assert_rows(o, lse, q, kc, vc, T, b, n, mode, w)
+
+
 @pytest.mark.parametrize("Dh", [64, 128, 256])
 def test_max_tokens_and_wide_tables(Dh):
     # a table with more entries than the longest sequence needs, and a bound above it
