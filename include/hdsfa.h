@@ -365,8 +365,8 @@ hd_status_t sfa_decode_paged(const void* q, const void* k_pages, const void* v_p
  *   was named by an earlier fork, whose tokens exceed lens[src], or whose pages are not held.
  *   (A slot that the same call forks to counts as empty as a source.)  F <= B.
  * hd_pages_free : slots seqs[0 .. F-1] are emptied: lens 0, their table entries -1, one holder
- *   less for their pages.  An empty slot, or a slot named before, is no error; an index or a
- *   table entry out of range, or a page that nobody holds, sets HD_DEVBIT_INDEX.
+ *   less for their pages.  An empty slot, or a slot named before, is no error; an index, a
+ *   length or a table entry out of range, or a page that nobody holds, sets HD_DEVBIT_INDEX.
  * hd_pages_compact : the K pages in use get the ids 0 .. K-1: the j-th page in use with an id
  *   >= K goes to the j-th free id below K, moves[j] = (old, new); the other moves are
  *   (-1, -1).  new_refs and new_table (entries behind a sequence's pages -1) may be refs and

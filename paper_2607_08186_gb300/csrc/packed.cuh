@@ -101,23 +101,43 @@ HD_DEVINLINE void visible_row(const __nv_bfloat16* q, const __nv_bfloat16* k, co
   }
   m = -INFINITY;
   l = 0.f;
-  for (int i = 0; i < keys; ++i) {
-    const long long r = row(i);
-    if (r < 0) continue;
-    const long long off = r * pitch + lane * C;
-    float x = 0.f;
+  for (int i0 = 0; i0 < keys; i0 += 4) {  // four keys' loads and sums in flight
+    long long off[4];
+    float x[4];
 #pragma unroll
-    for (int c = 0; c < C; ++c) x += qf[c] * __bfloat162float(k[off + c]);
+    for (int e = 0; e < 4; ++e) {
+      const long long r = i0 + e < keys ? row(i0 + e) : -1;
+      off[e] = r < 0 ? -1 : r * pitch + lane * C;
+      x[e] = 0.f;
+      if (off[e] >= 0)
 #pragma unroll
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    x *= scale_log2;
-    const float mn = fmaxf(m, x), mu = mn == -INFINITY ? 0.f : mn, corr = exp2f(m - mu), w = exp2f(x - mu);
-    m = mn;
-    l = l * corr + w;
+        for (int c = 0; c < C; ++c) x[e] += qf[c] * __bfloat162float(k[off[e] + c]);
+    }
 #pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = o[c] * corr + w * __bfloat162float(v[off + c]);
+    for (int d = 16; d; d >>= 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += __shfl_xor_sync(0xffffffffu, x[e], d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (off[e] < 0) continue;
+      x[e] *= scale_log2;
+      const float mn = fmaxf(m, x[e]), mu = mn == -INFINITY ? 0.f : mn, corr = exp2f(m - mu), w = exp2f(x[e] - mu);
+      m = mn;
+      l = l * corr + w;
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[c] = o[c] * corr + w * __bfloat162float(v[off[e] + c]);
+    }
   }
   if (l != l) m = INFINITY;
+}
+
+// Eight bf16 values, all of them finite: no exponent is all ones.
+HD_DEVINLINE bool finite8(const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) bad = bad || (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+  return !bad;
 }
 
 // A masked key has P = 0, and 0 times an infinity or a NaN of its V row is NaN: whether hidden key
@@ -127,38 +147,39 @@ template <int DH>
 HD_DEVINLINE bool hides_not_finite(const __nv_bfloat16* v, long long pitch, int k0, int k1) {
   const int lane = threadIdx.x & 31;
   bool bad = false;
-  for (int i = k0 * (DH / 8) + lane; i < k1 * (DH / 8); i += 32) {
-    const uint4 x = *reinterpret_cast<const uint4*>(v + (long long)(i / (DH / 8)) * pitch + i % (DH / 8) * 8);
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e)  // an exponent of all ones in either half
-      bad = bad || (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
-  }
+  for (int i = k0 * (DH / 8) + lane; i < k1 * (DH / 8); i += 32)
+    bad = bad || !finite8(*reinterpret_cast<const uint4*>(v + (long long)(i / (DH / 8)) * pitch + i % (DH / 8) * 8));
   return __any_sync(0xffffffffu, bad);
 }
 
-// The rows r0 + i (bits i of `rows`) of a query tile that came out not finite: computed again if keys
-// of the tile's range [klo, khi) that they do not see hold an infinity or a NaN.  q, k, v, o and lse
-// start at row 0 of the sequence (lse at row r0); rows lie qo_pitch, kv_pitch, lse_pitch apart.  One
-// warp, which has written the rows before.
+// The 32 query rows from row r0 of an entry's sequence, head and stream, whose results this warp and
+// others of its CTA have stored: those that came out not finite are computed again if keys of their
+// tile's range [klo, khi) that they do not see hold an infinity or a NaN.  By a warp, after the CTA's
+// other work, since nobody waits for it then (a row takes as long as its sequence is).
 template <int DH>
-__device__ __noinline__ void recompute_rows(const __nv_bfloat16* q, const __nv_bfloat16* k, const __nv_bfloat16* v,
-                                            long long kv_pitch, __nv_bfloat16* o, long long qo_pitch, float* lse,
-                                            long long lse_pitch, int r0, unsigned rows, int klo, int khi, int window,
-                                            float scale_log2) {
+__device__ __noinline__ void settle_rows(const PackedArgs& a, const PackedEntry& w, int head, int r0, int klo, int khi) {
   constexpr int C = DH / 32;
-  const int lane = threadIdx.x & 31;
-  __syncwarp();  // the rows' first results, stored by other lanes, come before these
-  for (; rows; rows &= rows - 1) {
-    const int i = __ffs(rows) - 1, r = r0 + i, first = window > 0 ? max(0, r - window + 1) : 0;
-    if (!hides_not_finite<DH>(v, kv_pitch, r + 1, khi) && !hides_not_finite<DH>(v, kv_pitch, klo, first)) continue;
+  const int lane = threadIdx.x & 31, window = a.g.window;
+  const long long qp = (long long)a.g.rs * a.g.Hq * DH, kp = (long long)a.g.rs * a.g.Hkv * DH;
+  const long long tensor_row = (long long)w.first * a.g.rs + w.stream;
+  const long long q0 = tensor_row * a.g.Hq * DH + (long long)head * DH;
+  const long long k0 = tensor_row * a.g.Hkv * DH + (long long)fast_div(head, a.d_grp) * DH;
+  float* lse = a.lse + (long long)head * a.g.q_nL + tensor_row;
+  bool odd = false;
+  if (r0 + lane < w.rows) {
+    const __nv_bfloat16* o = a.o + q0 + (r0 + lane) * qp;
+    for (int i = 0; i < DH; i += 8) odd = odd || !finite8(*reinterpret_cast<const uint4*>(o + i));
+  }
+  for (unsigned rows = __ballot_sync(0xffffffffu, odd); rows; rows &= rows - 1) {
+    const int r = r0 + __ffs(rows) - 1, first = window > 0 ? max(0, r - window + 1) : 0;
+    if (!hides_not_finite<DH>(a.v + k0, kp, r + 1, khi) && !hides_not_finite<DH>(a.v + k0, kp, klo, first)) continue;
     float acc[C], m, l;
-    visible_row<DH>(q + r * qo_pitch, k, v, kv_pitch, r + 1 - first, [&](int j) { return (long long)(first + j); },
-                    scale_log2, acc, m, l);
+    visible_row<DH>(a.q + q0 + r * qp, a.k + k0, a.v + k0, kp, r + 1 - first,
+                    [&](int j) { return (long long)(first + j); }, a.scale_log2, acc, m, l);
     const float inv = 1.f / l;
 #pragma unroll
-    for (int c = 0; c < C; ++c) o[r * qo_pitch + lane * C + c] = __float2bfloat16_rn(acc[c] * inv);
-    if (lane == 0) lse[i * lse_pitch] = (m + log2f(l)) * 0.6931471805599453f;
+    for (int c = 0; c < C; ++c) a.o[q0 + r * qp + lane * C + c] = __float2bfloat16_rn(acc[c] * inv);
+    if (lane == 0) lse[(long long)r * a.g.rs] = (m + log2f(l)) * 0.6931471805599453f;
   }
 }
 

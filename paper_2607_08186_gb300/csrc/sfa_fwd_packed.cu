@@ -19,7 +19,7 @@
 // their scores are masked like later keys, and their V rows, which P = 0 would not silence if they
 // held an infinity or a NaN, are zeroed in shared memory.  Later keys of the own sequence that are
 // not finite are rare; rows that come out not finite with such keys about are computed again
-// (recompute_rows).  Every mbarrier wait is bounded.
+// (settle_rows).  Every mbarrier wait is bounded.
 #include "packed.cuh"
 #include "tc_common.cuh"
 
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
     const bool lead = warp == 2 + 4 * g && lane == 0;
     uint32_t units = 0;
     int used = 0, tiles = 0;
-    bool ok = true;
+    bool ok = true, odd = false;  // odd: a row of this thread's came out not finite
     // of an entry only this is held over the key tiles, whose scores take the registers
     int rows = 0, m0 = 0, n_lo = 0, n_hi = 0;
     auto take = [&](const PackedEntry& w) {
@@ -450,17 +450,17 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
         }
       }
       tc_fence_before();  // ... before this thread's next arrival on p_full
-      float* lse = A.lse + (long long)hd * A.g.q_nL + (long long)(w.first + r) * A.g.q_rs + w.stream;
-      if (store) *lse = (m_run * c2 + log2f(l_run)) * kLn2;
+      if (store)
+        A.lse[(long long)hd * A.g.q_nL + (long long)(w.first + r) * A.g.q_rs + w.stream] = (m_run * c2 + log2f(l_run)) * kLn2;
       float z0, z1;
       f2unpack(zero2, z0, z1);
-      const unsigned again = __ballot_sync(0xffffffffu, store && !(z0 + z1 == 0.f));
-      if (again) {
-        const long long qp = (long long)A.g.rs * A.g.Hq * DH, kp = (long long)A.g.rs * A.g.Hkv * DH;
-        const long long q0 = ((long long)w.first * A.g.rs + w.stream) * A.g.Hq * DH + (long long)hd * DH;
-        const long long k0 = ((long long)w.first * A.g.rs + w.stream) * A.g.Hkv * DH + fast_div(hd, A.d_grp) * DH;
-        recompute_rows<DH>(A.q + q0, A.k + k0, A.v + k0, kp, A.o + q0, qp, lse - (long long)lane * A.g.q_rs, A.g.q_rs,
-                           r - lane, again, lo * BN, min((hi + 1) * BN, rows_now), A.g.window, c2);
+      odd = odd || (store && !(z0 + z1 == 0.f));
+    }
+    if (ok && __any_sync(0xffffffffu, odd)) {  // some row of some entry is not finite
+      for (int k = 0; (pos = place_of(k)) < total; ++k) {
+        const PackedEntry w(A, pos);
+        const int r0 = w.row0(A, g);
+        settle_rows<DH>(A, w, w.head_of(A, g), r0 + q4 * 32, packed_lo(A, r0) * BN, min((packed_hi(r0, w.rows) + 1) * BN, w.rows));
       }
     }
   }

@@ -35,8 +35,8 @@ constexpr float kRescaleThreshold = 8.0f;  // log2 units: P stays <= 256 between
 struct Smem {
   bf16 q[BM * DH];            // four [128 rows][64] swizzle blocks
   bf16 ring[NSLOT][HB * DH];  // K: four [64 keys][64] swizzle blocks; V: two [128 keys][64]
-  float part[2][2][BM];       // by tile parity and key half: a row's maximum (at an entry's end: its sum)
-  uint8_t odd[2][BM];         // whether a half row of O holds a value that is not finite
+  float part[2][2][BM];       // by tile parity and key half: a row's maximum, at an entry's end its sum
+  uint8_t odd[2][BM];         // at the end: whether a thread's half rows of O held a value that is not finite
   // S and PV of a tile complete: by tile mod 4, since the producer, which takes them as the release
   // of K and V, may be up to two tiles late; V(last) landed in this CTA, by entry mod 4 (the ring
   // holds the last V tiles of up to three entries)
@@ -266,7 +266,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
     const float c2 = A.scale_log2;
     const uint64_t c2x2 = f2pack(c2, c2);
     int units = 0, tile = 0;
-    bool ok = true;
+    bool ok = true, odd = false;  // odd: a row of this thread's came out not finite
     // (after a wait gave up, the warps go on through the entries: two of them meet on every tile)
     for (int k = 0, pos; (pos = place_of(k)) < total; ++k) {
       const PackedEntry w(A, pos);
@@ -381,10 +381,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
         m_run = m_use;
       }
       units += 2 * T;
-      sm.part[tile & 1][hc][row] = l_run;  // last read two tiles ago, written next behind the second barrier
-      named_bar_sync(1 + q4, 64);
-      l_run += sm.part[tile & 1][hc ^ 1][row];
       ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(tile - 1) & 3], ((tile - 1) >> 2) & 1, abort, A.status));
+      // over the last tile's maxima, which the other warp has read where its P is in that PV; written
+      // next behind the next tile's barrier
+      sm.part[(tile - 1) & 1][hc][row] = l_run;
+      named_bar_sync(1 + q4, 64);
+      l_run += sm.part[(tile - 1) & 1][hc ^ 1][row];
       const int h = w.head_of(A, rank);
       const bool store = ok && r < w.rows;
       uint64_t zero2 = 0;
@@ -421,21 +423,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
         }
         tc_fence_before();  // ... before this thread's next arrival on p_full
       }
+      if (hc == 0 && store)
+        A.lse[(long long)h * A.g.q_nL + (long long)(w.first + r) * A.g.q_rs + w.stream] = (m_run * c2 + log2f(l_run)) * kLn2;
       float z0, z1;
       f2unpack(zero2, z0, z1);
-      float* lse = A.lse + (long long)h * A.g.q_nL + (long long)(w.first + r) * A.g.q_rs + w.stream;
-      if (hc == 0 && store) *lse = (m_run * c2 + log2f(l_run)) * kLn2;
-      sm.odd[hc][row] = store && !(z0 + z1 == 0.f);
-      named_bar_sync(1 + q4, 64);  // both halves of the rows are stored, too
-      if (hc == 0) {  // rows of which either half is not finite
-        const unsigned again = __ballot_sync(0xffffffffu, sm.odd[0][row] | sm.odd[1][row]);
-        if (again) {
-          const long long qp = (long long)A.g.rs * A.g.Hq * DH, kp = (long long)A.g.rs * A.g.Hkv * DH;
-          const long long q0 = ((long long)w.first * A.g.rs + w.stream) * A.g.Hq * DH + (long long)h * DH;
-          const long long k0 = ((long long)w.first * A.g.rs + w.stream) * A.g.Hkv * DH + fast_div(h, A.d_grp) * DH;
-          recompute_rows<DH>(A.q + q0, A.k + k0, A.v + k0, kp, A.o + q0, qp, lse - (long long)lane * A.g.q_rs, A.g.q_rs,
-                             r - lane, again, lo * BN, min((lo + T) * BN, w.rows), A.g.window, c2);
-        }
+      odd = odd || (store && !(z0 + z1 == 0.f));
+    }
+    sm.odd[hc][row] = odd;
+    named_bar_sync(1 + q4, 64);  // both halves of the rows are stored, too
+    if (ok && hc == 0 && __any_sync(0xffffffffu, sm.odd[0][row] | sm.odd[1][row])) {  // some row is not finite
+      for (int k = 0, pos; (pos = place_of(k)) < total; ++k) {
+        const PackedEntry w(A, pos);
+        int lo, T;
+        key_tiles(A, w, lo, T);
+        settle_rows<DH>(A, w, w.head_of(A, rank), w.row0(A, rank) + q4 * 32, lo * BN, min((lo + T) * BN, w.rows));
       }
     }
   }
