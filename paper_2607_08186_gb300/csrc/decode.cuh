@@ -182,8 +182,9 @@ struct PagedSplit {
 };
 }  // namespace dec
 
-// The tcgen05 kernel over a paged cache (head dim 256), and the combine kernel after either.
-cudaError_t launch_decode_paged_tc(const dec::DecodeArgs& a, cudaStream_t st);
+// The tcgen05 kernel over a paged cache (head dims 128 and 256) with the combine kernel, and the
+// combine kernel alone.
+cudaError_t launch_decode_paged_tc(const dec::DecodeArgs& a, int Dh, cudaStream_t st);
 cudaError_t launch_combine_paged(const dec::DecodeArgs& a, int Dh, cudaStream_t st);
 
 }  // namespace hdsfa

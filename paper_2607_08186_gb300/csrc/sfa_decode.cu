@@ -452,13 +452,15 @@ __global__ void __launch_bounds__(256) append_kernel(const uint4* kn, const uint
 // each) took 4400 of a tile's 7000 cycles; its 128 KB take 5800 at the HBM rate with every
 // SM streaming.
 namespace dectc {
-constexpr int DH = 256, BM = 128, BN = 128, NSLOT = 5, NTHREADS = 192;
+constexpr int BM = 128, BN = 128, NTHREADS = 192;
 constexpr uint32_t COL_O = 256;
 constexpr float kRescaleThreshold = 8.0f;
 
+template <int DH>
 struct Smem {
-  bf16 q[DH / 64][BM * 64];      // the group's query rows: four [128][64] swizzle blocks
-  bf16 ring[NSLOT][2][BN * 64];  // per slot: one K or V half, two [128][64] blocks
+  static constexpr int NSLOT = DH == 256 ? 5 : 6;
+  bf16 q[DH / 64][BM * 64];      // the group's query rows: DH/64 [128][64] swizzle blocks
+  bf16 ring[NSLOT][2][BN * 64];  // per slot: 128 columns (at head dim 256 a half) of K or V, two [128][64] blocks
   uint64_t q_full, full[NSLOT], empty[NSLOT], s_full[2], p_full[2], pv_done, drain;
   uint32_t tmem_base;
   int abort, bad_page;
@@ -469,11 +471,12 @@ struct Params {
   dec::DecodeArgs a;
 };
 
-// Unit u of the ring sequence K(0), K(1), V(0), K(2), V(1), ..., V(nt-1), two halves per
+// Unit u of the ring sequence K(0), K(1), V(0), K(2), V(1), ..., V(nt-1), HV units of 128 columns per
 // tile: its tile, tensor (0 = K, 1 = V) and half.
+template <int HV>
 HD_DEVINLINE void unit_of(int u, int nt, int& j, int& isv, int& half) {
-  half = u & 1;
-  const int p = u >> 1;
+  half = u % HV;
+  const int p = u / HV;
   if (p == 0) {
     j = 0;
     isv = 0;
@@ -493,8 +496,10 @@ HD_DEVINLINE void unit_of(int u, int nt, int& j, int& isv, int& half) {
 // look their pages up and issue their loads.  Pieces outside the sequence (or the window) are loaded
 // from behind the pool's last row, which fills them with zeros.  A tile that pieces do not fill leaves
 // the slots' last rows as they are zeroed at the start.
-template <bool PAGED>
+template <int DH, bool PAGED>
 __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_constant__ Params P) {
+  using Smem = dectc::Smem<DH>;
+  constexpr int NSLOT = Smem::NSLOT, HV = DH / 128;  // HV: ring units of a K or V tile
   const dec::DecodeArgs& a = P.a;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -551,7 +556,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
     T = a.lens[b];
     dec::split_range(a, T, c, tile, k0, k1);
   }
-  const int nt = PAGED ? fast_div(k1 - k0 + tile - 1, a.d_tile) : (k1 - k0 + BN - 1) / BN, nunits = 4 * nt;
+  const int nt = PAGED ? fast_div(k1 - k0 + tile - 1, a.d_tile) : (k1 - k0 + BN - 1) / BN, nunits = 2 * HV * nt;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -625,12 +630,15 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
       fetch(0);
       rows_of(0, cur);
       fetch(1);
-      bool go = load_half(&P.tm_k, cur, 0) && load_half(&P.tm_k, cur, 1);
+      auto load_unit = [&](const CUtensorMap* tm, const int* x) {
+        return load_half(tm, x, 0) && (HV == 1 || load_half(tm, x, 1));
+      };
+      bool go = load_unit(&P.tm_k, cur);
       for (int j = 0; go && j < nt; ++j) {  // K(j+1), then V(j)
         rows_of(j + 1, nxt);
         fetch(j + 2);
-        if (j + 1 < nt) go = load_half(&P.tm_k, nxt, 0) && load_half(&P.tm_k, nxt, 1);
-        go = go && load_half(&P.tm_v, cur, 0) && load_half(&P.tm_v, cur, 1);
+        if (j + 1 < nt) go = load_unit(&P.tm_k, nxt);
+        go = go && load_unit(&P.tm_v, cur);
 #pragma unroll
         for (int i = 0; i < 4; ++i) cur[i] = nxt[i];
       }
@@ -650,7 +658,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
         const int slot = u % NSLOT;
         if (u >= NSLOT && !mbar_wait(&sm.empty[slot], ((u / NSLOT) - 1) & 1, abort, a.status)) break;
         int j, isv, half;
-        unit_of(u, nt, j, isv, half);
+        unit_of<HV>(u, nt, j, isv, half);
         const CUtensorMap* tm = isv ? &P.tm_v : &P.tm_k;
         mbar_arrive_expect_tx(&sm.full[slot], BN * 128 * 2);
         tma_load_5d(sm.ring[slot][0], tm, &sm.full[slot], half * 128, g, 0, k0 + j * BN, b);
@@ -676,7 +684,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
     const uint64_t rv = sdesc_sw128(smem_u32(sm.ring[0][0]), BN * 128, 1024);
     auto issue_s = [&](int sb) -> bool {
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
+      for (int hf = 0; hf < HV; ++hf) {
         if (!wait_unit(u + hf)) return false;
         const int slot = (u + hf) % NSLOT;
         const uint64_t kd = rd + (uint64_t)(slot * (32768 / 16));
@@ -689,13 +697,13 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
         }
         tc_commit_w(&sm.empty[slot]);
       }
-      u += 2;
+      u += HV;
       tc_commit_w(&sm.s_full[sb]);
       return true;
     };
     auto issue_pv = [&](int sb, bool acc0) -> bool {
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
+      for (int hf = 0; hf < HV; ++hf) {
         if (!wait_unit(u + hf)) return false;
         const int slot = (u + hf) % NSLOT;
         const uint64_t vd = rv + (uint64_t)(slot * (32768 / 16));
@@ -705,7 +713,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
                       (acc0 || kk > 0) ? 1u : 0u);
         tc_commit_w(&sm.empty[slot]);
       }
-      u += 2;
+      u += HV;
       tc_commit_w(&sm.pv_done);
       return true;
     };
@@ -839,13 +847,13 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
       // zeroed before the PV (which waits for this thread's arrival).
       if (base + tile > k1) {
 #pragma unroll
-        for (int u = nunits - 2; u < nunits; ++u)  // the ring's last units: this tile's V halves
+        for (int u = nunits - HV; u < nunits; ++u)  // the ring's last units: this tile's V
           ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.full[u % NSLOT], (u / NSLOT) & 1, abort, a.status));
         if (!ok) break;
         for (int r = k1 - base + row / 8; r < BN; r += 16)
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            reinterpret_cast<uint4*>(sm.ring[(nunits - 2 + (c >> 1)) % NSLOT][c & 1] + r * 64)[row % 8] =
+          for (int c = 0; c < 2 * HV; ++c)
+            reinterpret_cast<uint4*>(sm.ring[(nunits - HV + (c >> 1)) % NSLOT][c & 1] + r * 64)[row % 8] =
                 make_uint4(0, 0, 0, 0);
         fence_async_smem();
       }
@@ -908,12 +916,13 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
 
 // ------------------------------------------------------------------ host side
 
-DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, bool allow_tc) {
+DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, TcDims tc_dims) {
   using namespace dec;
   DecodePlan p;
   p.G = Hq / Hkv;
   p.M = n * p.G;
-  p.tc = allow_tc && Dh == 256 && p.M <= dectc::BM;
+  p.tc = p.M <= dectc::BM && ((Dh == 256 && tc_dims != TcDims::kNone) ||
+                              (Dh == 128 && tc_dims == TcDims::kWith128 && p.M > RG));
   p.rg = p.tc ? p.M : RG;
   p.ngroups = p.tc ? 1 : (p.M + RG - 1) / RG;
   const long long range = mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1)
@@ -969,7 +978,7 @@ static cudaError_t launch_decode_t(const dec::DecodeArgs& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, combine_kernel<DH, false>, a);
 }
 
-template <bool PAGED>
+template <int DH, bool PAGED>
 static cudaError_t launch_decode_tc(const dec::DecodeArgs& a, cudaStream_t st) {
   using namespace dectc;
   Params p;
@@ -991,8 +1000,8 @@ static cudaError_t launch_decode_tc(const dec::DecodeArgs& a, cudaStream_t st) {
   if (!make_qgroup_tmap(&p.tm_q, a.q, a.B, a.n, a.Hq, DH, a.G) ||
       !make_rows_tmap(&p.tm_k, a.kc, gk, a.Hkv, DH, box) || !make_rows_tmap(&p.tm_v, a.vc, gk, a.Hkv, DH, box))
     return cudaErrorInvalidValue;
-  const int smem = (int)sizeof(Smem) + 1024;
-  cudaError_t e = cudaFuncSetAttribute(decode_tc_kernel<PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const int smem = (int)sizeof(Smem<DH>) + 1024;
+  cudaError_t e = cudaFuncSetAttribute(decode_tc_kernel<DH, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute pdl[1];
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1004,7 +1013,7 @@ static cudaError_t launch_decode_tc(const dec::DecodeArgs& a, cudaStream_t st) {
   cfg.stream = st;
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, decode_tc_kernel<PAGED>, p);
+  e = cudaLaunchKernelEx(&cfg, decode_tc_kernel<DH, PAGED>, p);
   if (e != cudaSuccess) return e;
   cfg.gridDim = dim3(a.M, a.Hkv, a.B);
   cfg.blockDim = dim3(256);
@@ -1012,7 +1021,9 @@ static cudaError_t launch_decode_tc(const dec::DecodeArgs& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, dec::combine_kernel<DH, PAGED>, a);
 }
 
-cudaError_t launch_decode_paged_tc(const dec::DecodeArgs& a, cudaStream_t st) { return launch_decode_tc<true>(a, st); }
+cudaError_t launch_decode_paged_tc(const dec::DecodeArgs& a, int Dh, cudaStream_t st) {
+  return Dh == 256 ? launch_decode_tc<256, true>(a, st) : launch_decode_tc<128, true>(a, st);
+}
 
 cudaError_t launch_combine_paged(const dec::DecodeArgs& a, int Dh, cudaStream_t st) {
   const dim3 grid(std::min(a.rg, a.M), a.Hkv * a.ngroups, a.B);
@@ -1050,7 +1061,7 @@ cudaError_t launch_sfa_decode(const void* q, const void* kc, const void* vc, con
   a.window = window;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.d_nsplit = make_fast_div((uint32_t)p.nsplit);
-  if (p.tc) return launch_decode_tc<false>(a, st);
+  if (p.tc) return launch_decode_tc<256, false>(a, st);
   const bool two = p.M > 16;  // a row group of more than 16 rows takes two m16 tiles
   if (Dh == 64) return two ? launch_decode_t<64, 2>(a, st) : launch_decode_t<64, 1>(a, st);
   if (Dh == 256) return two ? launch_decode_t<256, 2>(a, st) : launch_decode_t<256, 1>(a, st);

@@ -1,4 +1,4 @@
-// Decoding over a paged cache (head dims 64 and 128, and 256 where the tcgen05 kernel does not fit):
+// Decoding over a paged cache (where the tcgen05 kernel of sfa_decode.cu is not taken, see paged_tc):
 // the decoding step's split over the cached positions and its warp-level products (mma.sync m16n8k16),
 // with the rows found through a page table.
 //
@@ -469,14 +469,19 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
 
 // ------------------------------------------------------------------ host side
 
-// Head dim 256: the tensor-core kernel reads by TMA alone, which pages of fewer than four rows make
-// slow; one row group (up to 32 query rows) goes to the other kernel then.
-static bool paged_tc(int n, int Hq, int Hkv, int prow) { return !(prow < 4 && n * (Hq / Hkv) <= dec::RG); }
+// The tensor-core kernel reads by TMA alone, which small pages make slow.  At head dim 256 it is taken
+// all the same from four rows a page on, or where the other kernel would read the cache once for each
+// 32 query rows; at 128, where that costs less, for more than 32 rows from pages of eight rows on.
+static TcDims paged_tc(int n, int Hq, int Hkv, int prow) {
+  const bool one_group = n * (Hq / Hkv) <= dec::RG;
+  return prow < 4 && one_group ? TcDims::kNone : prow < 8 ? TcDims::k256 : TcDims::kWith128;
+}
 
 // The contiguous cache's plan, with the combine kernel (about three tiles' time, nothing to do for one
 // split) in the cost: short sequences take one split, whose CTAs write the results.
-static DecodePlan paged_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, bool allow_tc) {
-  DecodePlan p = decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, allow_tc);
+static DecodePlan paged_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window,
+                             TcDims tc_dims) {
+  DecodePlan p = decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, tc_dims);
   if (p.tc || p.nsplit == 1) return p;
   const long long range = mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1)
                                             : (long long)maxT * n;
@@ -494,8 +499,8 @@ constexpr size_t kShareBytes = dec::kBalancedSeqs * sizeof(int2);
 
 size_t decode_paged_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {
   // either kernel's, whatever the pages
-  return std::max(decode_ws_bytes(decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, true)),
-                  decode_ws_bytes(decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, false))) + kShareBytes;
+  return std::max(decode_ws_bytes(decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, TcDims::kWith128)),
+                  decode_ws_bytes(decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, TcDims::kNone))) + kShareBytes;
 }
 
 // A tile of at most `most` positions: whole pieces, the largest that no page boundary cuts (a page's
@@ -572,7 +577,7 @@ cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* v
                                               : (long long)maxT * n;
     a.balanced = B > 1 && B <= dec::kBalancedSeqs && plan.nsplit > 1 && range / plan.nsplit >= 4 * 64 &&
                  B * (range / a.tile + 1) < (1LL << 30);  // the tiles of all sequences, counted in 32 bits
-    return launch_decode_paged_tc(a, st);
+    return launch_decode_paged_tc(a, Dh, st);
   }
   const int KT = Dh == 256 ? dec::ktile<256>() : dec::ktile<128>();
   paged_tile(a, KT);

@@ -76,12 +76,14 @@ def _check(q, kc, vc, lens, n, mode, window, P, seed=0, max_tokens=None, width=N
 MASKS = [(WITHIN, 0), (CROSS, 0), (LOCAL, 1), (LOCAL, 100), (LOCAL, 2**31 - 1)]
 
 
-# rows per K/V head: 16 and 32 (one and two m16 tiles), 64 (two row groups), 9; pages of every
+# rows per K/V head: 16 and 32 (one and two m16 tiles), 9, 48, 64 and 128 (on the tensor-core kernel from
+# pages of eight rows on, else two row groups); pages of every
 # size against tiles of 64 rows: smaller, equal, larger, odd, prime, one token with more streams than a tile holds
 @pytest.mark.parametrize("mode,w", MASKS)
 @pytest.mark.parametrize("n,Hq,Hkv,Dh,P", [(4, 32, 8, 128, 16), (8, 32, 8, 128, 3), (8, 64, 8, 128, 1), (1, 8, 8, 128, 64),
                                            (3, 6, 2, 128, 7), (2, 4, 4, 64, 8), (3, 16, 4, 64, 50), (4, 8, 2, 64, 5),
-                                           (1, 8, 2, 128, 131), (4, 8, 2, 128, 43), (4, 32, 8, 128, 2), (70, 2, 1, 64, 1), (5, 10, 2, 64, 9)])
+                                           (1, 8, 2, 128, 131), (4, 8, 2, 128, 43), (4, 32, 8, 128, 2), (70, 2, 1, 64, 1), (5, 10, 2, 64, 9),
+                                           (4, 96, 8, 128, 16), (8, 32, 2, 128, 3), (3, 96, 8, 128, 1), (4, 12, 1, 128, 43)])
 def test_ragged(mode, w, n, Hq, Hkv, Dh, P):
     q, kc, vc = _case(4, 150, n, Hq, Hkv, Dh, n + Hq + P)
     _check(q, kc, vc, _i32([150, 1, 0, 129]), n, mode, w, P)
@@ -107,7 +109,7 @@ def test_long(n, Hq, Hkv, Dh, mode, P):
 
 @pytest.mark.parametrize("mode,w", [(WITHIN, 0), (CROSS, 0), (LOCAL, 2000)])
 @pytest.mark.parametrize("B,Hq,Hkv,Dh,P", [(3, 8, 2, 128, 16), (33, 4, 1, 128, 7), (70, 2, 2, 64, 16), (7, 24, 2, 256, 16),
-                                           (40, 2, 1, 256, 20)])
+                                           (40, 2, 1, 256, 20), (9, 12, 1, 128, 16)])
 def test_splits_shared_out_by_length(mode, w, B, Hq, Hkv, Dh, P):
     # long splits of sequences of very different lengths, empty ones, one beyond max_tokens and one below
     # zero among them (these three alone are empty); more sequences than a warp has lanes
@@ -176,7 +178,7 @@ def test_bad_lengths_empty_the_sequence_alone():
     _assert_rows(o, lse, q, kc, vc, 48, 1, 2, CROSS, 0)
 
 
-@pytest.mark.parametrize("Hq,Hkv,Dh,P", [(8, 2, 128, 16), (24, 2, 256, 16), (24, 2, 256, 5), (4, 2, 64, 1)])
+@pytest.mark.parametrize("Hq,Hkv,Dh,P", [(8, 2, 128, 16), (24, 2, 128, 16), (24, 2, 256, 16), (24, 2, 256, 5), (4, 2, 64, 1)])
 def test_local_needs_only_the_windows_pages(Hq, Hkv, Dh, P):
     n, T, w = 4, 333, 150  # the window of the first row begins at position 1328 - 149 = 1179, token 294
     q, kc, vc = _case(1, T, n, Hq, Hkv, Dh, 21)
@@ -189,7 +191,7 @@ def test_local_needs_only_the_windows_pages(Hq, Hkv, Dh, P):
 
 
 @pytest.mark.parametrize("bad", [NAN, float("inf"), -float("inf"), 3.38e38])
-@pytest.mark.parametrize("Hq,Hkv,Dh", [(8, 2, 128), (24, 2, 256), (4, 2, 64)])
+@pytest.mark.parametrize("Hq,Hkv,Dh", [(8, 2, 128), (24, 2, 128), (24, 2, 256), (4, 2, 64)])
 @pytest.mark.parametrize("mode,w", [(WITHIN, 0), (CROSS, 0), (LOCAL, 90)])
 def test_what_the_mask_hides_has_no_effect(mode, w, Hq, Hkv, Dh, bad):
     # cached rows that stream 0's new position does not see hold infinities, NaN or huge values: those of
