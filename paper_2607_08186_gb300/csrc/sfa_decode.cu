@@ -28,8 +28,9 @@
 // past the sequence are zero-filled and masked.  A sequence whose length is outside
 // [1, max_tokens] gets zero rows, LSE = -inf and HD_DEVBIT_INDEX.
 //
-// A paged cache (sfa_decode_paged) is read at head dim 256 by the tcgen05 kernel below and else by a
-// kernel of its own (sfa_decode_paged.cu); the combine kernel is shared.  With PAGED it keeps a
+// A paged cache (sfa_decode_paged) is read by the tcgen05 kernel below, at head dim 128 too, where there are
+// query rows enough and pages not too small, and else by a kernel of its own (sfa_decode_paged.cu, which has
+// the rule: paged_tc); the combine kernel is shared.  With PAGED it keeps a
 // sequence that holds nothing apart from a bad length, and empties one that met a bad page.
 #include <algorithm>
 
@@ -451,6 +452,9 @@ __global__ void __launch_bounds__(256) append_kernel(const uint4* kn, const uint
 // and combine 74 -> 44 us.  Before, per-element masks (three compares and a modular step
 // each) took 4400 of a tile's 7000 cycles; its 128 KB take 5800 at the HBM rate with every
 // SM streaming.
+// Paged caches use it at head dim 128 too (S and O as above, O 128 columns wide; a ring unit is a whole
+// tile of K or V, six slots): 96 over 8 heads, 4 streams, 8 sequences of 2048 tokens in pages of 16 in
+// 56.6 us, 16 of 8192 in 358 us (the contiguous cache's mma.sync kernel 113 and 714 us).
 namespace dectc {
 constexpr int BM = 128, BN = 128, NTHREADS = 192;
 constexpr uint32_t COL_O = 256;

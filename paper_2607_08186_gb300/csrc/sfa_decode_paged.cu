@@ -9,7 +9,7 @@
 // (issuing one takes a warp up to 1000 cycles) and meet on the stages' barriers alone.  Pieces of fewer than
 // kTmaRows rows cost more to issue than to move (about 35 ns each), so such pages go through cp.async,
 // 16 bytes a thread, with each row's place looked up a tile ahead.
-// (By cp.async for all pages, 8 sequences of 8192 tokens, one stream, 32 over 8 heads: 57.7 us; so 45.)
+// (By cp.async for all pages, 8 sequences of 8192 tokens, one stream, 32 over 8 heads: 57.7 us; so 47.)
 //
 // In shared memory a K or V tile is DH/64 blocks of [KT][64] with the 128-byte swizzle that TMA
 // writes: conflict-free for ldmatrix as well.  Splits, partials and the combine kernel are those of
@@ -469,12 +469,22 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
 
 // ------------------------------------------------------------------ host side
 
-// The tensor-core kernel reads by TMA alone, which small pages make slow.  At head dim 256 it is taken
-// all the same from four rows a page on, or where the other kernel would read the cache once for each
-// 32 query rows; at 128, where that costs less, for more than 32 rows from pages of eight rows on.
+// Which kernel reads the pages, by query rows per K/V head and rows per page.  The tensor-core kernel reads
+// the cache once for up to 128 rows, but by TMA alone, which small pages make slow; the other one reads it
+// once for each 32 rows, by cp.async where pages are small.  Measured in us, tensor cores / the other (at head
+// dim 256 4 sequences of 8192 tokens, 2 K/V heads; at 128 8 of 2048, 8 K/V heads; n streams):
+//   <= 16 query rows   never    256: 16 rows a page 23.8 / 19.0 (n 1), 64: 51.6 / 48.6 (n 4), 128: 22.0 / 18.8 (n 1);
+//                               only lengths of a quarter to all 58.3 / 65.4 (7 sequences, n 4)
+//   <= 32, 256 only    from 12  8 rows a page 79 / 69, 9: 80 / 61, 10: 96 / 83, 12: 70.7 / 75.6, 16: 56.3 / 60.9
+//   <= 64              from 5   256: 3 rows a page 130 / 105, 4: 126 / 125, 5: 136 / 158, 6: 81 / 101
+//                               128: 3 rows a page 158 / 110, 4: 159 / 139, 5: 175 / 174, 6: 98 / 109, 8: 103 / 128, 64: 57 / 95
+//   <= 128             from 4   256: 2 rows a page 72 / 58 (n 1), 3: 65 / 57 (n 1), 4: 45 / 57 (n 1)
+//                               128: 3 rows a page 168 / 155 (n 3), 4: 55 / 69 (n 1), 164 / 191 (n 4)
 static TcDims paged_tc(int n, int Hq, int Hkv, int prow) {
-  const bool one_group = n * (Hq / Hkv) <= dec::RG;
-  return prow < 4 && one_group ? TcDims::kNone : prow < 8 ? TcDims::k256 : TcDims::kWith128;
+  const int M = n * (Hq / Hkv);
+  if (M <= 16) return TcDims::kNone;
+  if (M <= 32) return prow < 12 ? TcDims::kNone : TcDims::k256;
+  return prow < (M <= 64 ? 5 : 4) ? TcDims::kNone : TcDims::kWith128;
 }
 
 // The contiguous cache's plan, with the combine kernel (about three tiles' time, nothing to do for one

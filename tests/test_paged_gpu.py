@@ -89,11 +89,12 @@ def test_ragged(mode, w, n, Hq, Hkv, Dh, P):
     _check(q, kc, vc, _i32([150, 1, 0, 129]), n, mode, w, P)
 
 
-# head dim 256: 48, 4, 9 and 128 rows on the tensor-core kernel (pieces of 64, 1, 1, 32, 128 rows and whole
-# tiles), 256 rows on the other one
+# head dim 256: 24 to 128 query rows on the tensor-core kernel where pages are not too small, up to 16 and 256
+# of them on the other one, by TMA and by cp.async
 @pytest.mark.parametrize("mode,w", MASKS)
 @pytest.mark.parametrize("n,Hq,Hkv,P", [(4, 24, 2, 16), (1, 4, 1, 3), (3, 6, 2, 5), (8, 32, 2, 4), (4, 24, 2, 32),
-                                        (4, 24, 2, 64), (2, 12, 2, 1), (8, 64, 2, 6), (8, 64, 2, 1), (3, 24, 2, 43), (4, 24, 2, 43), (1, 12, 1, 131), (1, 4, 1, 1)])
+                                        (4, 24, 2, 64), (2, 12, 2, 1), (8, 64, 2, 6), (8, 64, 2, 1), (3, 24, 2, 43), (4, 24, 2, 43), (1, 12, 1, 131), (1, 4, 1, 1),
+                                        (4, 16, 2, 3), (3, 16, 2, 4), (4, 16, 2, 2), (1, 24, 1, 16), (4, 8, 2, 16), (3, 10, 2, 11)])
 def test_ragged_head_dim_256(mode, w, n, Hq, Hkv, P):
     q, kc, vc = _case(4, 150, n, Hq, Hkv, 256, 40 + n + Hq + P)
     _check(q, kc, vc, _i32([150, 1, 0, 129]), n, mode, w, P)
@@ -109,7 +110,7 @@ def test_long(n, Hq, Hkv, Dh, mode, P):
 
 @pytest.mark.parametrize("mode,w", [(WITHIN, 0), (CROSS, 0), (LOCAL, 2000)])
 @pytest.mark.parametrize("B,Hq,Hkv,Dh,P", [(3, 8, 2, 128, 16), (33, 4, 1, 128, 7), (70, 2, 2, 64, 16), (7, 24, 2, 256, 16),
-                                           (40, 2, 1, 256, 20), (9, 12, 1, 128, 16)])
+                                           (40, 2, 1, 256, 20), (40, 8, 1, 256, 20), (9, 12, 1, 128, 16)])
 def test_splits_shared_out_by_length(mode, w, B, Hq, Hkv, Dh, P):
     # long splits of sequences of very different lengths, empty ones, one beyond max_tokens and one below
     # zero among them (these three alone are empty); more sequences than a warp has lanes
@@ -149,7 +150,7 @@ def test_where_pages_lie_changes_no_bit(mode, w, Hq, Hkv, Dh, P):
     assert torch.equal(runs[0][0], runs[1][0]) and torch.equal(runs[0][1], runs[1][1]) and runs[0][2] == 0
 
 
-@pytest.mark.parametrize("Hq,Hkv,Dh", [(8, 2, 128), (24, 2, 256)])
+@pytest.mark.parametrize("Hq,Hkv,Dh", [(8, 2, 128), (24, 2, 256), (8, 2, 256)])
 @pytest.mark.parametrize("entry", [-1, -2**31, 2**31 - 1, None])  # None: one past the pool
 def test_bad_pages_empty_the_sequence_alone(Hq, Hkv, Dh, entry):
     n, P = 4, 16
@@ -178,7 +179,8 @@ def test_bad_lengths_empty_the_sequence_alone():
     _assert_rows(o, lse, q, kc, vc, 48, 1, 2, CROSS, 0)
 
 
-@pytest.mark.parametrize("Hq,Hkv,Dh,P", [(8, 2, 128, 16), (24, 2, 128, 16), (24, 2, 256, 16), (24, 2, 256, 5), (4, 2, 64, 1)])
+@pytest.mark.parametrize("Hq,Hkv,Dh,P", [(8, 2, 128, 16), (24, 2, 128, 16), (24, 2, 256, 16), (24, 2, 256, 5), (8, 2, 256, 16),
+                                           (4, 2, 64, 1)])
 def test_local_needs_only_the_windows_pages(Hq, Hkv, Dh, P):
     n, T, w = 4, 333, 150  # the window of the first row begins at position 1328 - 149 = 1179, token 294
     q, kc, vc = _case(1, T, n, Hq, Hkv, Dh, 21)
@@ -191,7 +193,7 @@ def test_local_needs_only_the_windows_pages(Hq, Hkv, Dh, P):
 
 
 @pytest.mark.parametrize("bad", [NAN, float("inf"), -float("inf"), 3.38e38])
-@pytest.mark.parametrize("Hq,Hkv,Dh", [(8, 2, 128), (24, 2, 128), (24, 2, 256), (4, 2, 64)])
+@pytest.mark.parametrize("Hq,Hkv,Dh", [(8, 2, 128), (24, 2, 128), (24, 2, 256), (8, 2, 256), (4, 2, 64)])
 @pytest.mark.parametrize("mode,w", [(WITHIN, 0), (CROSS, 0), (LOCAL, 90)])
 def test_what_the_mask_hides_has_no_effect(mode, w, Hq, Hkv, Dh, bad):
     # cached rows that stream 0's new position does not see hold infinities, NaN or huge values: those of
@@ -218,7 +220,7 @@ def test_what_the_mask_hides_has_no_effect(mode, w, Hq, Hkv, Dh, bad):
         assert not bool(torch.isfinite(o[0, 1, :, 5].float()).any())
 
 
-@pytest.mark.parametrize("Hq,Hkv,Dh", [(8, 2, 128), (24, 2, 256)])
+@pytest.mark.parametrize("Hq,Hkv,Dh", [(8, 2, 128), (24, 2, 256), (8, 2, 256)])
 def test_nan_query_is_its_own(Hq, Hkv, Dh):
     q, kc, vc = _case(1, 400, 4, Hq, Hkv, Dh, 33)
     qn = q.clone()
@@ -233,7 +235,7 @@ def test_nan_query_is_its_own(Hq, Hkv, Dh):
     assert torch.equal(o[0][keep], o2[0][keep]) and torch.equal(lse[0].t()[keep], lse2[0].t()[keep])
 
 
-@pytest.mark.parametrize("Hq,Hkv,Dh", [(16, 8, 128), (8, 4, 256)])
+@pytest.mark.parametrize("Hq,Hkv,Dh", [(16, 8, 128), (8, 4, 256), (24, 4, 256)])
 def test_pools_beyond_32_bits(Hq, Hkv, Dh):
     # pages whose rows start more than 2^32 elements into the pool (8.6 GB each)
     n, P, T = 4, 16, 100
