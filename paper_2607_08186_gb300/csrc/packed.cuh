@@ -147,8 +147,9 @@ template <int DH>
 HD_DEVINLINE bool hides_not_finite(const __nv_bfloat16* v, long long pitch, int k0, int k1) {
   const int lane = threadIdx.x & 31;
   bool bad = false;
-  for (int i = k0 * (DH / 8) + lane; i < k1 * (DH / 8); i += 32)
-    bad = bad || !finite8(*reinterpret_cast<const uint4*>(v + (long long)(i / (DH / 8)) * pitch + i % (DH / 8) * 8));
+  const __nv_bfloat16* row = v + k0 * pitch;  // from here, within a tile: a sequence's rows times DH/8 may pass 31 bits
+  for (int i = lane; i < (k1 - k0) * (DH / 8); i += 32)
+    bad = bad || !finite8(*reinterpret_cast<const uint4*>(row + (long long)(i / (DH / 8)) * pitch + i % (DH / 8) * 8));
   return __any_sync(0xffffffffu, bad);
 }
 
