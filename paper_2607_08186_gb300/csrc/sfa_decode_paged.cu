@@ -480,11 +480,24 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
 //                               128: 3 rows a page 158 / 110, 4: 159 / 139, 5: 175 / 174, 6: 98 / 109, 8: 103 / 128, 64: 57 / 95
 //   <= 128             from 4   256: 2 rows a page 72 / 58 (n 1), 3: 65 / 57 (n 1), 4: 45 / 57 (n 1)
 //                               128: 3 rows a page 168 / 155 (n 3), 4: 55 / 69 (n 1), 164 / 191 (n 4)
-static TcDims paged_tc(int n, int Hq, int Hkv, int prow) {
+// And it takes longer to start and end, one CTA per SM, so a range of few positions is the other one's (4
+// streams, pages of 64 rows; B sequences of so many tokens):
+//   128, > 32 rows   B 4: 50 tokens 13.7 / 11.6, 150: 14.5 / 16.3; B 16 (128 CTAs): 50: 27.6 / 14.8, 400: 41.6 /
+//                    39.0, 1000: 64 / 79; B 64: 12: 97 / 41, 150: 122 / 81, 400: 164 / 145, 1000: 275 / 357
+//   256, > 32 rows   B 4: 50: 13.1 / 10.6, 150: 13.2 / 12.9, 400: 13.8 / 15.5; B 33: 50: 22 / 20, 150: 28 / 34
+//   256, <= 32 rows  B 4: 50: 12.9 / 10.0, 400: 13.9 / 14.4; B 33: 50: 19.3 / 18.2, 400: 35.2 / 36.7
+static TcDims paged_tc(int B, int n, int Hq, int Hkv, int Dh, int prow, long long range) {
   const int M = n * (Hq / Hkv);
   if (M <= 16) return TcDims::kNone;
+  const int few = M <= 32 ? 1200 : Dh == 128 && (long long)B * Hkv > kSmCount / 4 ? 2000 : 400;
+  if (range < few) return TcDims::kNone;
   if (M <= 32) return prow < 12 ? TcDims::kNone : TcDims::k256;
   return prow < (M <= 64 ? 5 : 4) ? TcDims::kNone : TcDims::kWith128;
+}
+
+// Positions that a step of maxT tokens reads at most.
+static long long paged_range(int maxT, int n, int mode, int window) {
+  return mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1) : (long long)maxT * n;
 }
 
 // The contiguous cache's plan, with the combine kernel (about three tiles' time, nothing to do for one
@@ -493,8 +506,7 @@ static DecodePlan paged_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, in
                              TcDims tc_dims) {
   DecodePlan p = decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, tc_dims);
   if (p.tc || p.nsplit == 1) return p;
-  const long long range = mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1)
-                                            : (long long)maxT * n;
+  const long long range = paged_range(maxT, n, mode, window);
   const int KT = Dh == 256 ? dec::ktile<256>() : dec::ktile<128>();
   const long long tiles = (range + KT - 1) / KT, per = (tiles + p.nsplit - 1) / p.nsplit;
   const long long ctas = (long long)B * Hkv * p.ngroups, resident = 152LL * (Dh == 64 ? 4 : 2);
@@ -545,7 +557,8 @@ cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* v
                                     const int32_t* lens, void* o, float* lse, int B, int maxT, int num_pages, int P,
                                     int max_pages, int n, int Hq, int Hkv, int Dh, float scale, int mode, int window,
                                     void* ws, int32_t* status, cudaStream_t st) {
-  const DecodePlan plan = paged_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, paged_tc(n, Hq, Hkv, P * n));
+  const long long range = paged_range(maxT, n, mode, window);
+  const DecodePlan plan = paged_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, paged_tc(B, n, Hq, Hkv, Dh, P * n, range));
   dec::PagedParams p = {};
   dec::DecodeArgs& a = p.a;
   a.q = (const bf16*)q;
@@ -583,8 +596,6 @@ cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* v
     // kernel has an SM to itself, so nobody takes up what a short sequence's split leaves: 7 sequences
     // of a quarter to all of 8192 tokens, 24 over 2 heads, 68.2 -> 60.9 us.  The other kernel's two
     // CTAs per SM do (4 and 16 such sequences 69.3 and 113 us, shared out 72.0 and 115).
-    const long long range = mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1)
-                                              : (long long)maxT * n;
     a.balanced = B > 1 && B <= dec::kBalancedSeqs && plan.nsplit > 1 && range / plan.nsplit >= 4 * 64 &&
                  B * (range / a.tile + 1) < (1LL << 30);  // the tiles of all sequences, counted in 32 bits
     return launch_decode_paged_tc(a, Dh, st);
