@@ -284,7 +284,9 @@ hd_status_t sfa_kv_append(const void* k_new, const void* v_new, void* k_cache, v
  * on are left as they were, and q, k, v there may hold anything.  Offsets that descend or leave
  * [0, N] write nothing and set HD_DEVBIT_INDEX.  What a mask hides has no effect, infinities and
  * NaN in it included.  Masks, limits and head dims are those of sfa_fwd with B = 1 and L = N
- * (no SFA_WITHIN_NAIVE); forward only.
+ * (no SFA_WITHIN_NAIVE); forward only.  A sequence's results do not depend on what is packed around
+ * it, to the bit where it has more than 48 rows (n per token, or one in SFA_WITHIN); shorter ones share
+ * tiles, where their place may change the rounding.
  * workspace: >= sfa_fwd_packed_workspace_bytes(...) bytes, 16-byte aligned (the list of query
  * tiles, built by each call), not shared by calls that may run at the same time.
  */

@@ -50,11 +50,11 @@ cudaError_t launch_sfa_fwd_tc(const void* q, const void* k, const void* v, void*
 cudaError_t launch_sfa_fwd_tc256(const void* q, const void* k, const void* v, void* o, float* lse,
                                  const SfaGeom& g, float scale, int32_t* status, cudaStream_t st);
 cudaError_t launch_sfa_fwd_packed_tc(const void* q, const void* k, const void* v, void* o, float* lse, const SfaGeom& g,
-                                     int Dh, float scale, const PackedList& list, long long max_items, int32_t* status,
-                                     cudaStream_t st);
+                                     int Dh, float scale, const PackedList& list, const int32_t* offsets,
+                                     bool shared, long long max_items, int32_t* status, cudaStream_t st);
 cudaError_t launch_sfa_fwd_packed_tc256(const void* q, const void* k, const void* v, void* o, float* lse,
-                                        const SfaGeom& g, float scale, const PackedList& list, long long max_items,
-                                        int32_t* status, cudaStream_t st);
+                                        const SfaGeom& g, float scale, const PackedList& list, const int32_t* offsets,
+                                        long long max_items, int32_t* status, cudaStream_t st);
 cudaError_t launch_sfa_bwd_prep(const void* o, const void* dout, const float* lse, float* lse2_ws,
                                 float* delta_ws, float* dq_ws, const SfaGeom& g, int Dh,
                                 cudaStream_t st, bool zero = true);
@@ -492,12 +492,13 @@ hd_status_t sfa_fwd_packed(const void* q, const void* k, const void* v, void* o,
   if (!aligned16(workspace) || workspace_bytes < (size_t)(items + 1) * sizeof(hdsfa::PackedItem)) return HD_ERR_WORKSPACE;
   int32_t* count = static_cast<int32_t*>(workspace);
   hdsfa::PackedItem* list = static_cast<hdsfa::PackedItem*>(workspace) + 1;
-  cudaError_t e = hdsfa::launch_packed_plan(offsets, B, N, n / g.ns, rows, g.window, list, count, dev_status, stream);
+  const bool shared = hdsfa::packed_shared(Dh, B, N, n / g.ns);
+  cudaError_t e = hdsfa::launch_packed_plan(offsets, B, N, n / g.ns, rows, g.window, shared, list, count, dev_status, stream);
   if (e != cudaSuccess) return cuda_status(e);
   const float scale = resolve_scale(softmax_scale, Dh);
   const hdsfa::PackedList pl{list, count};
-  if (Dh == 256) return cuda_status(hdsfa::launch_sfa_fwd_packed_tc256(q, k, v, o, lse, g, scale, pl, items, dev_status, stream));
-  return cuda_status(hdsfa::launch_sfa_fwd_packed_tc(q, k, v, o, lse, g, Dh, scale, pl, items, dev_status, stream));
+  if (Dh == 256) return cuda_status(hdsfa::launch_sfa_fwd_packed_tc256(q, k, v, o, lse, g, scale, pl, offsets, items, dev_status, stream));
+  return cuda_status(hdsfa::launch_sfa_fwd_packed_tc(q, k, v, o, lse, g, Dh, scale, pl, offsets, shared, items, dev_status, stream));
 }
 
 // ---- paged cache ----

@@ -2,25 +2,39 @@
 // tiles that the forward kernels work through.
 #pragma once
 #include <float.h>
+#include <limits.h>
 
 #include "common.cuh"
 
 namespace hdsfa {
 
 // A query tile: `rows` virtual rows of a sequence (SfaGeom) that start at virtual row `first` of
-// the packed tensors, and the tile's number among the sequence's.
+// the packed tensors, and the tile's number among the sequence's.  Or a tile of short sequences (seqs
+// > 0): the rows of sequences seq .. seq + seqs - 1 one behind another, at most a tile of them, in which
+// a row's keys begin at its own sequence's first row.
 struct PackedItem {
-  int first, rows, tile, unused;
+  int first, rows;
+  int tile_or_seqs;  // the tile's number, or -seqs
+  int seq;
 };
+constexpr int kShortRows = 48;  // a sequence of at most so many rows shares a tile with its neighbours
 struct PackedList {
   const PackedItem* items;  // those with the most key tiles first
   const int32_t* count;
 };
+// Whether short neighbours share tiles.  It costs the softmax a register and a comparison a tile: at head
+// dims 128 and 256 no time (200 sequences, 32 over 8 heads of 128, 4 streams, intra-stream: of 7 rows 359 -> 53
+// us, 16: 97, 33: 177, 48: 244; 24 over 2 of 256: 357 -> 64, 118, 217, 295; 128 rows 381 / 394 and 558 / 561,
+// 512 rows, 50 of them, 670 / 655 and 705 / 710), but at head dim 64, whose tiles have half the MMAs, about 6 %
+// of every tile, so there it depends on an average sequence's rows (us apart / shared, 16 over 4 heads, 3
+// streams, rows uniform around the average: 16: 217 / 65, 32: 216 / 150, 64: 112 / 109, 96: 104 / 106, 128: 96 /
+// 103).  (The first row from shared memory instead of a register: 574 us for 200 of 128 rows at head dim 128.)
+inline bool packed_shared(int Dh, int B, int tokens, int mult) { return Dh > 64 || (long long)tokens * mult <= 64LL * B; }
 // Items that `tokens` packed tokens of B sequences make at most: sum of ceil(rows / tile_rows).
 inline long long packed_max_items(int B, int tokens, int mult, int tile_rows) {
   return (long long)tokens * mult / tile_rows + (B < tokens ? B : tokens);
 }
-cudaError_t launch_packed_plan(const int32_t* offsets, int B, int N, int mult, int tile_rows, int window,
+cudaError_t launch_packed_plan(const int32_t* offsets, int B, int N, int mult, int tile_rows, int window, bool shared,
                                PackedItem* items, int32_t* count, int32_t* status, cudaStream_t st);
 
 // What the forward kernels over packed prompts are given besides their tensor maps.
@@ -30,6 +44,8 @@ struct PackedArgs {
   float* lse;
   SfaGeom g;  // of all packed rows: B = 1, Lv = Lq = rows of a stream's problem
   PackedList list;
+  const int32_t* offsets;  // [B + 1], in tokens of `mult` rows
+  int mult;
   float scale_log2;
   int32_t* status;
   int head_pairs;  // 1: an entry's two query tiles are the same rows of two heads of one K/V group,
@@ -39,7 +55,7 @@ struct PackedArgs {
   FastDiv d_per, d_ns, d_grp;  // by per, streams, query heads of a K/V head
 };
 inline PackedArgs make_packed_args(const void* q, const void* k, const void* v, void* o, float* lse, const SfaGeom& g,
-                                   float scale, const PackedList& list, int32_t* status) {
+                                   float scale, const PackedList& list, const int32_t* offsets, int32_t* status) {
   PackedArgs a;
   a.q = static_cast<const __nv_bfloat16*>(q);
   a.k = static_cast<const __nv_bfloat16*>(k);
@@ -48,6 +64,8 @@ inline PackedArgs make_packed_args(const void* q, const void* k, const void* v, 
   a.lse = lse;
   a.g = g;
   a.list = list;
+  a.offsets = offsets;
+  a.mult = g.n / g.ns;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.status = status;
   a.head_pairs = (g.Hq / g.Hkv) % 2 == 0;
@@ -61,8 +79,9 @@ inline PackedArgs make_packed_args(const void* q, const void* k, const void* v, 
 
 // The work at place `pos` of the list (every entry stands for all head slots and streams).
 struct PackedEntry {
-  int first, rows;  // the sequence's first row and its rows
+  int first, rows;  // the sequence's first row and its rows, or the short sequences'
   int m0, head, stream;
+  int seq, seqs;  // short sequences of a shared tile (seqs = 0: one sequence)
   HD_DEVINLINE PackedEntry(const PackedArgs& a, int pos) {
     const int i = fast_div(pos, a.d_per);
     const PackedItem it = a.list.items[i];
@@ -71,7 +90,9 @@ struct PackedEntry {
     rows = it.rows;
     stream = hs - hx * a.g.q_ns;
     head = a.head_pairs ? 2 * hx : hx;
-    m0 = it.tile * (a.head_pairs ? 128 : 256);
+    m0 = max(it.tile_or_seqs, 0) * (a.head_pairs ? 128 : 256);
+    seq = it.seq;
+    seqs = max(-it.tile_or_seqs, 0);
   }
   HD_DEVINLINE int head_of(const PackedArgs& a, int g) const { return a.head_pairs ? head + g : head; }
   HD_DEVINLINE int row0(const PackedArgs& a, int g) const { return a.head_pairs ? m0 : m0 + g * 128; }
@@ -79,6 +100,18 @@ struct PackedEntry {
 // Key tiles of 128 [lo, hi] of the query tile at row r0 (hi < lo: no rows).
 HD_DEVINLINE int packed_lo(const PackedArgs& a, int r0) { return a.g.window > 0 ? max(0, r0 - a.g.window + 1) / 128 : 0; }
 HD_DEVINLINE int packed_hi(int r0, int rows) { return r0 >= rows ? -1 : (min(r0 + 128, rows) - 1) / 128; }
+// First row of the sequence that row r of an entry belongs to: 0, or one of up to 32 in a shared tile
+// (empty ones among them hold no row).  By a whole warp.
+HD_DEVINLINE int sequence_first(const PackedArgs& a, const PackedEntry& w, int r) {
+  if (w.seqs == 0) return 0;
+  const int lane = threadIdx.x & 31;
+  const int at = lane < w.seqs ? a.offsets[w.seq + lane] * a.mult - w.first : INT_MAX;
+  int s = 0;
+#pragma unroll
+  for (int d = 16; d; d >>= 1)
+    if (__shfl_sync(0xffffffffu, at, s + d) <= r) s += d;
+  return __shfl_sync(0xffffffffu, at, s);
+}
 // The place of the k-th piece of work of one of `workers`: the list in rounds of one place each,
 // every second round backwards, which evens out the descending sizes.
 HD_DEVINLINE int packed_place(int k, int worker, int workers) {
@@ -153,11 +186,11 @@ HD_DEVINLINE bool hides_not_finite(const __nv_bfloat16* v, long long pitch, int 
   return __any_sync(0xffffffffu, bad);
 }
 
-// The 32 query rows from row r0 of an entry's sequence, head and stream, whose results this warp and
+// The 32 query rows from row r0 of an entry's sequence or sequences, head and stream, whose results this warp and
 // others of its CTA have stored: those that came out not finite are computed again if keys of their
 // tile's range [klo, khi) that they do not see hold an infinity or a NaN.  By a warp, after the CTA's
 // other work, since nobody waits for it then (a row takes as long as its sequence is).
-template <int DH>
+template <int DH, bool SHARED>
 __device__ __noinline__ void settle_rows(const PackedArgs& a, const PackedEntry& w, int head, int r0, int klo, int khi) {
   constexpr int C = DH / 32;
   const int lane = threadIdx.x & 31, window = a.g.window;
@@ -166,21 +199,24 @@ __device__ __noinline__ void settle_rows(const PackedArgs& a, const PackedEntry&
   const long long q0 = tensor_row * a.g.Hq * DH + (long long)head * DH;
   const long long k0 = tensor_row * a.g.Hkv * DH + (long long)fast_div(head, a.d_grp) * DH;
   float* lse = a.lse + (long long)head * a.g.q_nL + tensor_row;
+  const int mine = SHARED ? sequence_first(a, w, r0 + lane) : 0;
   bool odd = false;
   if (r0 + lane < w.rows) {
     const __nv_bfloat16* o = a.o + q0 + (r0 + lane) * qp;
     for (int i = 0; i < DH; i += 8) odd = odd || !finite8(*reinterpret_cast<const uint4*>(o + i));
   }
   for (unsigned rows = __ballot_sync(0xffffffffu, odd); rows; rows &= rows - 1) {
-    const int r = r0 + __ffs(rows) - 1, first = window > 0 ? max(0, r - window + 1) : 0;
+    const int l = __ffs(rows) - 1, r = r0 + l;
+    const int own = SHARED ? __shfl_sync(0xffffffffu, mine, l) : 0;
+    const int first = max(own, window > 0 ? r - window + 1 : 0);
     if (!hides_not_finite<DH>(a.v + k0, kp, r + 1, khi) && !hides_not_finite<DH>(a.v + k0, kp, klo, first)) continue;
-    float acc[C], m, l;
+    float acc[C], m, sum;
     visible_row<DH>(a.q + q0 + r * qp, a.k + k0, a.v + k0, kp, r + 1 - first,
-                    [&](int j) { return (long long)(first + j); }, a.scale_log2, acc, m, l);
-    const float inv = 1.f / l;
+                    [&](int j) { return (long long)(first + j); }, a.scale_log2, acc, m, sum);
+    const float inv = 1.f / sum;
 #pragma unroll
     for (int c = 0; c < C; ++c) a.o[q0 + r * qp + lane * C + c] = __float2bfloat16_rn(acc[c] * inv);
-    if (lane == 0) lse[(long long)r * a.g.rs] = (m + log2f(l)) * 0.6931471805599453f;
+    if (lane == 0) lse[(long long)r * a.g.rs] = (m + log2f(sum)) * 0.6931471805599453f;
   }
 }
 

@@ -15,6 +15,10 @@
 // thread per row.  Per key tile and group: S = Q K^T into 128 TMEM columns, P (bf16) over their first
 // half, O += P V into DH columns.
 //
+// Short sequences (at most kShortRows rows) that lie together share a tile: to a row of one, its
+// neighbours' keys are masked, like those before a window, up to its own sequence's first row (SHARED;
+// packed_shared has what it costs and brings).
+//
 // A key tile that reaches past its sequence holds rows of the next one, or memory behind the last:
 // their scores are masked like later keys, and their V rows, which P = 0 would not silence if they
 // held an infinity or a NaN, are zeroed in shared memory.  Later keys of the own sequence that are
@@ -75,7 +79,8 @@ struct Tiles {
 };
 HD_DEVINLINE int place_of(int k) { return packed_place(k, (int)blockIdx.x, (int)gridDim.x); }
 
-template <int DH>
+// SHARED: the list may hold tiles of short sequences.
+template <int DH, bool SHARED>
 __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_constant__ Params P) {
   constexpr int NSLOT = Smem<DH>::NSLOT;
   extern __shared__ uint8_t smem_raw[];
@@ -291,11 +296,13 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
     bool ok = true, odd = false;  // odd: a row of this thread's came out not finite
     // of an entry only this is held over the key tiles, whose scores take the registers
     int rows = 0, m0 = 0, n_lo = 0, n_hi = 0;
+    int own = 0;  // SHARED: first row of the sequence of this thread's row
     auto take = [&](const PackedEntry& w) {
       rows = w.rows;
       m0 = w.row0(A, g);
       n_lo = packed_lo(A, w.m0);
       n_hi = max(packed_hi(w.m0, rows), packed_hi(w.row0(A, 1), rows));
+      if constexpr (SHARED) own = sequence_first(A, w, m0 + row);
     };
     int pos = place_of(0);
     if (pos < total) take(PackedEntry(A, pos));
@@ -336,14 +343,15 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
         for (int c = 0; c < BN / 32; ++c) tmem_ld32(tS + c * 32, reinterpret_cast<uint32_t*>(x) + c * 32);
         tmem_ld_wait();
         // tiles holding a key past the first query's key row (the diagonal band) or the sequence,
-        // and (LOCAL) a key at or below the last query's window edge
-        if (kb + BN - 1 > m0 || kb + BN > rows || (A.g.window > 0 && kb <= min(m0 + BM, rows) - 1 - A.g.window)) {
+        // and (LOCAL) a key at or below the last query's window edge, or one before the row's sequence
+        if (kb + BN - 1 > m0 || kb + BN > rows || (SHARED && own > kb) ||
+            (A.g.window > 0 && kb <= min(m0 + BM, rows) - 1 - A.g.window)) {
           const int e_hi = min(r, rows - 1) - kb;
 #pragma unroll
           for (int e = 0; e < BN; ++e)
             if (e > e_hi) x[e] = -INFINITY;
-          if (A.g.window > 0) {
-            const int e_lo = r - A.g.window + 1 - kb;
+          if (A.g.window > 0 || (SHARED && own > kb)) {
+            const int e_lo = (SHARED ? max(own, A.g.window > 0 ? r - A.g.window + 1 : 0) : r - A.g.window + 1) - kb;
 #pragma unroll
             for (int e = 0; e < BN; ++e)
               if (e < e_lo) x[e] = -INFINITY;
@@ -460,7 +468,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
       for (int k = 0; (pos = place_of(k)) < total; ++k) {
         const PackedEntry w(A, pos);
         const int r0 = w.row0(A, g);
-        settle_rows<DH>(A, w, w.head_of(A, g), r0 + q4 * 32, packed_lo(A, r0) * BN, min((packed_hi(r0, w.rows) + 1) * BN, w.rows));
+        settle_rows<DH, SHARED>(A, w, w.head_of(A, g), r0 + q4 * 32, packed_lo(A, r0) * BN, min((packed_hi(r0, w.rows) + 1) * BN, w.rows));
       }
     }
   }
@@ -474,27 +482,28 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
   }
 }
 
-template <int DH>
+template <int DH, bool SHARED>
 static cudaError_t launch(const Params& p, long long max_items, cudaStream_t st) {
   constexpr int smem = smem_bytes<DH>();
-  cudaError_t e = cudaFuncSetAttribute(fwd_packed_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(fwd_packed_kernel<DH, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const long long work = max_items * p.a.per;
-  return launch_kernel(true, fwd_packed_kernel<DH>, dim3((unsigned)(work < kSmCount ? work : kSmCount)), NTHREADS, smem,
+  return launch_kernel(true, fwd_packed_kernel<DH, SHARED>, dim3((unsigned)(work < kSmCount ? work : kSmCount)), NTHREADS, smem,
                        st, p);
 }
 }  // namespace packed
 
 cudaError_t launch_sfa_fwd_packed_tc(const void* q, const void* k, const void* v, void* o, float* lse, const SfaGeom& g,
-                                     int Dh, float scale, const PackedList& list, long long max_items, int32_t* status,
-                                     cudaStream_t st) {
+                                     int Dh, float scale, const PackedList& list, const int32_t* offsets,
+                                     bool shared, long long max_items, int32_t* status, cudaStream_t st) {
   using namespace packed;
   Params p;
   if (!make_rows_tmap(&p.tm_q, q, query_geom(g), g.Hq, Dh, BM) || !make_rows_tmap(&p.tm_k, k, g, g.Hkv, Dh, BN) ||
       !make_rows_tmap(&p.tm_v, v, g, g.Hkv, Dh, BN))
     return cudaErrorInvalidValue;
-  p.a = make_packed_args(q, k, v, o, lse, g, scale, list, status);
-  return Dh == 64 ? launch<64>(p, max_items, st) : launch<128>(p, max_items, st);
+  p.a = make_packed_args(q, k, v, o, lse, g, scale, list, offsets, status);
+  if (Dh == 128) return launch<128, true>(p, max_items, st);
+  return shared ? launch<64, true>(p, max_items, st) : launch<64, false>(p, max_items, st);
 }
 
 }  // namespace hdsfa

@@ -15,6 +15,7 @@
 // A full barrier lives in the first CTA and counts both CTAs' bytes; commits are multicast.  An
 // entry's last V tile is loaded on a barrier of each CTA's own (v_tail), since its threads zero the
 // rows behind the sequence (see the forward of the smaller head dims for why).
+// Short sequences that lie together share a tile, as there.
 // Before, as one pair per entry: 16000 cycles for an entry of one key tile, of which 2060 are MMAs.
 // Every mbarrier wait is bounded.
 #include "packed.cuh"
@@ -273,6 +274,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
       int lo, T;
       key_tiles(A, w, lo, T);
       const int row0 = w.row0(A, rank), r = row0 + row;  // first query row of the tile, the thread's
+      const int own = sequence_first(A, w, r);           // first row of the sequence of the thread's row
       float m_run = -INFINITY, l_run = 0.f;              // m_run in raw score units
       for (int t = 0; t < T; ++t, ++tile) {
         const int j = lo + t;
@@ -304,16 +306,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
           for (int c = 0; c < HB / 32; ++c) tmem_ld32(tS + c * 32, reinterpret_cast<uint32_t*>(x) + c * 32);
           tmem_ld_wait();
           // tiles holding a key past the first query's key row (the diagonal band) or the sequence,
-          // and (LOCAL) a key at or below the last query's window edge
-          if ((j + 1) * BN - 1 > row0 || (j + 1) * BN > w.rows ||
+          // and (LOCAL) a key at or below the last query's window edge, or before the row's sequence
+          if ((j + 1) * BN - 1 > row0 || (j + 1) * BN > w.rows || own > j * BN ||
               (A.g.window > 0 && j * BN <= min(row0 + BM, w.rows) - 1 - A.g.window)) {
             const int k0 = j * BN + HB * hc;
             const int e_hi = min(r, w.rows - 1) - k0;
 #pragma unroll
             for (int e = 0; e < HB; ++e)
               if (e > e_hi) x[e] = -INFINITY;
-            if (A.g.window > 0) {
-              const int e_lo = r - A.g.window + 1 - k0;
+            if (A.g.window > 0 || own > j * BN) {
+              const int e_lo = max(own, A.g.window > 0 ? r - A.g.window + 1 : 0) - k0;
 #pragma unroll
               for (int e = 0; e < HB; ++e)
                 if (e < e_lo) x[e] = -INFINITY;
@@ -436,7 +438,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
         const PackedEntry w(A, pos);
         int lo, T;
         key_tiles(A, w, lo, T);
-        settle_rows<DH>(A, w, w.head_of(A, rank), w.row0(A, rank) + q4 * 32, lo * BN, min((lo + T) * BN, w.rows));
+        settle_rows<DH, true>(A, w, w.head_of(A, rank), w.row0(A, rank) + q4 * 32, lo * BN, min((lo + T) * BN, w.rows));
       }
     }
   }
@@ -452,14 +454,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
 }  // namespace packed256
 
 cudaError_t launch_sfa_fwd_packed_tc256(const void* q, const void* k, const void* v, void* o, float* lse,
-                                        const SfaGeom& g, float scale, const PackedList& list, long long max_items,
-                                        int32_t* status, cudaStream_t st) {
+                                        const SfaGeom& g, float scale, const PackedList& list, const int32_t* offsets,
+                                        long long max_items, int32_t* status, cudaStream_t st) {
   using namespace packed256;
   Params p;
   if (!make_rows_tmap(&p.tm_q, q, query_geom(g), g.Hq, DH, BM) || !make_rows_tmap(&p.tm_k, k, g, g.Hkv, DH, HB) ||
       !make_rows_tmap(&p.tm_v, v, g, g.Hkv, DH, BN))
     return cudaErrorInvalidValue;
-  p.a = make_packed_args(q, k, v, o, lse, g, scale, list, status);
+  p.a = make_packed_args(q, k, v, o, lse, g, scale, list, offsets, status);
   cudaError_t e = cudaFuncSetAttribute(fwd_packed256_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
   if (e != cudaSuccess) return e;
   const long long work = max_items * p.a.per;

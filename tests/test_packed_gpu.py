@@ -93,6 +93,39 @@ def test_many_short_sequences(n, Hq, Hkv, Dh):
     _check(q, k, v, off, n, CROSS, 0)
 
 
+# Short neighbours share a tile: pairs of heads, and two tiles of a head; at most 32 sequences of a tile, empty ones
+# among them, lengths around the longest that shares one (48 rows), and others that interrupt
+SHORT = [(1, 4, 2, 64), (3, 3, 1, 64), (4, 8, 2, 128), (1, 3, 1, 128), (2, 4, 2, 256), (4, 3, 3, 256), (1, 1, 1, 256)]
+
+
+@pytest.mark.parametrize("mode,w", MASKS[:2] + [(LOCAL, 1), (LOCAL, 7), (LOCAL, 2**31 - 1)])
+@pytest.mark.parametrize("n,Hq,Hkv,Dh", SHORT)
+def test_short_neighbours(mode, w, n, Hq, Hkv, Dh):
+    lens = [3, 0, 0, 7, 12, 11, 24, 48, 1, 49, 5, 16, 0, 47, 47, 200, 2, 9] + [1] * 70 + [0] * 40 + [2, 30, 17, 0]
+    q, k, v, off = _case(lens, n, Hq, Hkv, Dh, 60 + n + Hq, before=1, behind=2)
+    _check(q, k, v, off, n, mode, w)
+
+
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+@pytest.mark.parametrize("mode,w", [(WITHIN, 0), (CROSS, 0), (LOCAL, 5)])
+@pytest.mark.parametrize("n,Hq,Hkv,Dh", SHORT)
+def test_short_neighbours_that_are_not_finite(mode, w, n, Hq, Hkv, Dh, bad):
+    # all of one sequence, behind and before the others, and the last token of another one's K and V
+    lens = [6, 9, 3, 11, 0, 8]
+    q, k, v, off = _case(lens, n, Hq, Hkv, Dh, 90 + n + Hq, behind=2)
+    kb, vb = k.clone(), v.clone()
+    r = slice(off[1] * n, off[2] * n)
+    kb[r], vb[r] = bad, bad
+    last = slice((off[4] - 1) * n, off[4] * n)
+    kb[last], vb[last] = bad, bad
+    o, lse, st = _run(q, kb, vb, off, n, mode, w)
+    assert st == 0
+    for i, rows in ((0, lens[0]), (2, lens[2]), (3, lens[3] - 1), (5, lens[5])):
+        r, keep = slice(off[i] * n, off[i + 1] * n), slice(0, rows * n)
+        o_r, A, lse_r = _reference(q, k, v, r, n, mode, w)
+        _near(o[r], o_r, A, lse[:, r], lse_r, keep)
+
+
 @pytest.mark.parametrize("B", [1, 3])
 @pytest.mark.parametrize("n,Hq,Hkv,Dh", [(2, 4, 2, 128), (2, 1, 1, 64), (4, 2, 1, 256)])
 def test_nothing_but_empty_sequences(B, n, Hq, Hkv, Dh):
