@@ -102,7 +102,8 @@ def test_ragged_head_dim_256(mode, w, n, Hq, Hkv, P):
 
 @pytest.mark.parametrize("n,Hq,Hkv,Dh,mode,P", [(4, 32, 8, 128, WITHIN, 16), (4, 32, 8, 128, CROSS, 37),
                                                 (4, 24, 2, 256, WITHIN, 16), (4, 24, 2, 256, CROSS, 24),
-                                                (4, 96, 8, 128, CROSS, 32)])
+                                                (4, 96, 8, 128, CROSS, 32), (4, 16, 2, 256, CROSS, 3),
+                                                (3, 16, 2, 256, WITHIN, 5), (4, 16, 2, 256, WITHIN, 2)])
 def test_long(n, Hq, Hkv, Dh, mode, P):
     q, kc, vc = _case(2, 8192, n, Hq, Hkv, Dh, 8)
     _check(q, kc, vc, _i32([8192, 3001]), n, mode, 0, P)
@@ -181,12 +182,14 @@ def test_bad_lengths_empty_the_sequence_alone():
 
 @pytest.mark.parametrize("Hq,Hkv,Dh,P", [(8, 2, 128, 16), (24, 2, 128, 16), (24, 2, 256, 16), (24, 2, 256, 5), (8, 2, 256, 16),
                                            (4, 2, 64, 1)])
-def test_local_needs_only_the_windows_pages(Hq, Hkv, Dh, P):
-    n, T, w = 4, 333, 150  # the window of the first row begins at position 1328 - 149 = 1179, token 294
+@pytest.mark.parametrize("w", [150, 500])  # a range for the mma.sync kernel, and for the tensor cores
+def test_local_needs_only_the_windows_pages(Hq, Hkv, Dh, P, w):
+    n, T = 4, 333
+    first = ((T - 1) * n - w + 1) // n  # the token at which the first row's window begins
     q, kc, vc = _case(1, T, n, Hq, Hkv, Dh, 21)
     kp, table = paging.to_pages(kc, _i32([T]), P, n, 3)
     vp, _ = paging.to_pages(vc, _i32([T]), P, n, 3)
-    table[0, :294 // P] = -1
+    table[0, :first // P] = -1
     o, lse, st = _decode(q, kp, vp, table, _i32([T]), n, LOCAL, w)
     assert st == 0
     _assert_rows(o, lse, q, kc, vc, T, 0, n, LOCAL, w)
@@ -194,7 +197,7 @@ def test_local_needs_only_the_windows_pages(Hq, Hkv, Dh, P):
 
 @pytest.mark.parametrize("bad", [NAN, float("inf"), -float("inf"), 3.38e38])
 @pytest.mark.parametrize("Hq,Hkv,Dh", [(8, 2, 128), (24, 2, 128), (24, 2, 256), (8, 2, 256), (4, 2, 64)])
-@pytest.mark.parametrize("mode,w", [(WITHIN, 0), (CROSS, 0), (LOCAL, 90)])
+@pytest.mark.parametrize("mode,w", [(WITHIN, 0), (CROSS, 0), (LOCAL, 90), (LOCAL, 600)])
 def test_what_the_mask_hides_has_no_effect(mode, w, Hq, Hkv, Dh, bad):
     # cached rows that stream 0's new position does not see hold infinities, NaN or huge values: those of
     # another stream (WITHIN), the new token's later positions (CROSS), what lies before the window (LOCAL)
