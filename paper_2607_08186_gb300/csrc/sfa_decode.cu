@@ -896,7 +896,9 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
         const bool bad = *(volatile int*)&sm.bad_page != 0;
         const float m = l_run != l_run ? INFINITY : m_run * c2;
         if (rv) pml[row] = bad ? make_float2(-INFINITY, dec::kBadPage) : make_float2(m, l_run);
-        // the warp's own stores above come before those of exact_row
+        // The rows that exact_row stores were stored above by other lanes of this warp, and a vote orders
+        // no memory.
+        __syncwarp();
         unsigned rows = __ballot_sync(0xffffffffu, rv && !finite && !bad);
         for (; rows; rows &= rows - 1) {
           const int r = q4 * 32 + __ffs(rows) - 1;
