@@ -201,10 +201,12 @@ __device__ __noinline__ void settle_rows(const PackedArgs& a, const PackedEntry&
   float* lse = a.lse + (long long)head * a.g.q_nL + tensor_row;
   const int mine = SHARED ? sequence_first(a, w, r0 + lane) : 0;
   bool odd = false;
+  __syncwarp();  // rows stored by single lanes, and by others below: votes and shuffles order no memory
   if (r0 + lane < w.rows) {
     const __nv_bfloat16* o = a.o + q0 + (r0 + lane) * qp;
     for (int i = 0; i < DH; i += 8) odd = odd || !finite8(*reinterpret_cast<const uint4*>(o + i));
   }
+  __syncwarp();
   for (unsigned rows = __ballot_sync(0xffffffffu, odd); rows; rows &= rows - 1) {
     const int l = __ffs(rows) - 1, r = r0 + l;
     const int own = SHARED ? __shfl_sync(0xffffffffu, mine, l) : 0;

@@ -17,3 +17,11 @@ def test_partial_rows_are_ordered_before_they_are_computed_again():
     again = src.index("exact_row<DH>(")
     stored = src.rindex("pml[row] =", 0, again)
     assert "__syncwarp();" in src[stored:again]
+
+
+def test_rows_are_ordered_before_they_are_settled():
+    # settle_rows: rows stored by a lane each (the LSE too) are read by these lanes, then stored by the whole warp
+    src = _source("packed.cuh")
+    body = src[src.index("void settle_rows("):]
+    read, vote, store = (body.index(x) for x in ("finite8(", "__ballot_sync(", "a.o[q0"))
+    assert "__syncwarp();" in body[:read] and "__syncwarp();" in body[read:vote] and vote < store
