@@ -891,6 +891,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
             *reinterpret_cast<uint4*>(po + (size_t)(q4 * 32 + rr) * DH + cc * 32 + u * 4) =
                 *reinterpret_cast<const uint4*>(buf + rr * 128 + ((u ^ (rr & 7)) << 4));
         }
+        __syncwarp();
       }
       if constexpr (PAGED) {
         const bool bad = *(volatile int*)&sm.bad_page != 0;

@@ -338,19 +338,22 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
         }
         tc_fence_after();
         if (lead && j == hi) mbar_arrive(&sm.q_empty[g]);  // the group's last S has read Q
+        __syncwarp();
         float x[BN];
 #pragma unroll
         for (int c = 0; c < BN / 32; ++c) tmem_ld32(tS + c * 32, reinterpret_cast<uint32_t*>(x) + c * 32);
         tmem_ld_wait();
         // tiles holding a key past the first query's key row (the diagonal band) or the sequence,
-        // and (LOCAL) a key at or below the last query's window edge, or one before the row's sequence
-        if (kb + BN - 1 > m0 || kb + BN > rows || (SHARED && own > kb) ||
+        // and (LOCAL) a key at or below the last query's window edge, or one before a row's sequence.  All
+        // conditions are the warp's: its lanes go on together to the tcgen05 instructions below.
+        const bool before = SHARED && __any_sync(0xffffffffu, own > kb);
+        if (kb + BN - 1 > m0 || kb + BN > rows || before ||
             (A.g.window > 0 && kb <= min(m0 + BM, rows) - 1 - A.g.window)) {
           const int e_hi = min(r, rows - 1) - kb;
 #pragma unroll
           for (int e = 0; e < BN; ++e)
             if (e > e_hi) x[e] = -INFINITY;
-          if (A.g.window > 0 || (SHARED && own > kb)) {
+          if (A.g.window > 0 || before) {
             const int e_lo = (SHARED ? max(own, A.g.window > 0 ? r - A.g.window + 1 : 0) : r - A.g.window + 1) - kb;
 #pragma unroll
             for (int e = 0; e < BN; ++e)
@@ -403,6 +406,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
             tc_fence_before();
             __syncwarp();
             if (lane == 0 && (parts<DH>() == 2 || c == 3)) mbar_arrive(&sm.p_full[g][parts<DH>() == 2 ? c >> 1 : 0]);
+            if (c < BN / 32 - 1) __syncwarp();
           }
         }
         float s0, s1, s2, s3;
@@ -456,6 +460,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
               reinterpret_cast<uint4*>(to)[e] = make_uint4(h[4 * e], h[4 * e + 1], h[4 * e + 2], h[4 * e + 3]);
           }
         }
+        __syncwarp();
       }
       tc_fence_before();  // ... before this thread's next arrival on p_full
       if (store)

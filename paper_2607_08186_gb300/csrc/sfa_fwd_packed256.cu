@@ -306,15 +306,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
           for (int c = 0; c < HB / 32; ++c) tmem_ld32(tS + c * 32, reinterpret_cast<uint32_t*>(x) + c * 32);
           tmem_ld_wait();
           // tiles holding a key past the first query's key row (the diagonal band) or the sequence,
-          // and (LOCAL) a key at or below the last query's window edge, or before the row's sequence
-          if ((j + 1) * BN - 1 > row0 || (j + 1) * BN > w.rows || own > j * BN ||
+          // and (LOCAL) a key at or below the last query's window edge, or before a row's sequence.  All
+          // conditions are the warp's: its lanes go on together to the tcgen05 instructions below.
+          const bool before = __any_sync(0xffffffffu, own > j * BN);
+          if ((j + 1) * BN - 1 > row0 || (j + 1) * BN > w.rows || before ||
               (A.g.window > 0 && j * BN <= min(row0 + BM, w.rows) - 1 - A.g.window)) {
             const int k0 = j * BN + HB * hc;
             const int e_hi = min(r, w.rows - 1) - k0;
 #pragma unroll
             for (int e = 0; e < HB; ++e)
               if (e > e_hi) x[e] = -INFINITY;
-            if (A.g.window > 0 || own > j * BN) {
+            if (A.g.window > 0 || before) {
               const int e_lo = max(own, A.g.window > 0 ? r - A.g.window + 1 : 0) - k0;
 #pragma unroll
               for (int e = 0; e < HB; ++e)
@@ -375,6 +377,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) arrive_lead(bar_p + 8 * c);
+          if (c < HB / 32 - 1) __syncwarp();
         }
         float s0, s1, s2, s3;
         f2unpack(fadd2(sum2[0], sum2[1]), s0, s1);
@@ -422,6 +425,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
                 reinterpret_cast<uint4*>(to + c * 32)[e] = make_uint4(b[4 * e], b[4 * e + 1], b[4 * e + 2], b[4 * e + 3]);
             }
           }
+          __syncwarp();
         }
         tc_fence_before();  // ... before this thread's next arrival on p_full
       }

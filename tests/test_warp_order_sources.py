@@ -25,3 +25,62 @@ def test_rows_are_ordered_before_they_are_settled():
     body = src[src.index("void settle_rows("):]
     read, vote, store = (body.index(x) for x in ("finite8(", "__ballot_sync(", "a.o[q0"))
     assert "__syncwarp();" in body[:read] and "__syncwarp();" in body[read:vote] and vote < store
+
+
+# The TMEM accesses (.sync.aligned) need the whole warp.  Behind a condition that single lanes decide, the lanes meet
+# at a warp barrier, vote or shuffle before the next one.
+LANE = re.compile(r"\bif \((?:lane == 0|lead|store|rv|q4 \* 32 \+ rr < a\.M)\b")
+MEET = r"__syncwarp|__any_sync|__all_sync|__ballot_sync|__shfl\w*_sync|named_bar_sync|__syncthreads"
+
+
+def _warp_level(body):
+    """For each lane-level condition, in the order of the source: the next thing of the whole warp."""
+    for m in LANE.finditer(body):
+        rest = body[m.end():]
+        yield body[m.start():m.start() + 60], re.search(r"\b(" + MEET + r"|tmem_(?:ld|st)\w*)\(", rest)
+
+
+def _softmax(name):
+    src = _source(name)
+    for kernel in ("fwd_packed_kernel(", "fwd_packed256_kernel(", "decode_tc_kernel("):
+        if kernel in src:
+            src = src[src.index(kernel):]
+            return src[src.index("const uint32_t tl ="):src.rindex("tmem_dealloc")]
+    raise AssertionError(name)
+
+
+def _closing(src, at):
+    depth = 0
+    for i in range(at, len(src)):
+        depth += (src[i] == "{") - (src[i] == "}")
+        if depth == 0:
+            return i
+    raise AssertionError("unbalanced source")
+
+
+def test_lanes_meet_before_tmem_accesses():
+    for name in ("sfa_fwd_packed.cu", "sfa_fwd_packed256.cu", "sfa_decode.cu"):
+        body = _softmax(name)
+        found = list(_warp_level(body))
+        assert len(found) >= 2, name
+        for where, m in found:
+            assert m is None or not m.group(1).startswith("tmem_"), (name, where)
+
+
+def test_store_loops_end_with_a_barrier():
+    # O leaves in a loop: load from TMEM, store what is a row's.  The next round's load is the whole warp's again
+    for name, loop in (("sfa_fwd_packed.cu", "for (int c = 0; c < DH / 32; ++c)"),
+                       ("sfa_fwd_packed256.cu", "for (int c = 0; c < PC / 32; ++c)"),
+                       ("sfa_decode.cu", "for (int cc = 0; cc < DH / 32; ++cc) {\n        uint32_t o[32];\n        tmem_ld32(tO + cc * 32, o);\n        tmem_ld_wait();\n        if")):
+        body = _softmax(name)
+        at = body.index(loop)
+        at = body.index("{", at)
+        assert body[at:_closing(body, at)].rstrip().endswith("__syncwarp();"), name
+
+
+def test_the_masks_of_shared_tiles_are_decided_by_the_warp():
+    # `own` differs from lane to lane: as a condition it is voted on
+    for name in ("sfa_fwd_packed.cu", "sfa_fwd_packed256.cu"):
+        body = _softmax(name)
+        uses = [m.start() for m in re.finditer(r"\bown >", body)]
+        assert len(uses) == 1 and body[:uses[0]].endswith("__any_sync(0xffffffffu, "), name
