@@ -296,13 +296,14 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
     bool ok = true, odd = false;  // odd: a row of this thread's came out not finite
     // of an entry only this is held over the key tiles, whose scores take the registers
     int rows = 0, m0 = 0, n_lo = 0, n_hi = 0;
-    int own = 0;  // SHARED: first row of the sequence of this thread's row
+    bool apart = false;  // SHARED: the entry holds several sequences
+    int own = 0;         // ... and the first row of that of this thread's row
     auto take = [&](const PackedEntry& w) {
       rows = w.rows;
       m0 = w.row0(A, g);
       n_lo = packed_lo(A, w.m0);
       n_hi = max(packed_hi(w.m0, rows), packed_hi(w.row0(A, 1), rows));
-      if constexpr (SHARED) own = sequence_first(A, w, m0 + row);
+      if constexpr (SHARED) own = sequence_first(A, w, m0 + row), apart = w.seqs > 0;
     };
     int pos = place_of(0);
     if (pos < total) take(PackedEntry(A, pos));
@@ -337,23 +338,22 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
           break;
         }
         tc_fence_after();
-        if (lead && j == hi) mbar_arrive(&sm.q_empty[g]);  // the group's last S has read Q
-        __syncwarp();
+        mbar_arrive_if(lead && j == hi, &sm.q_empty[g]);  // the group's last S has read Q
         float x[BN];
 #pragma unroll
         for (int c = 0; c < BN / 32; ++c) tmem_ld32(tS + c * 32, reinterpret_cast<uint32_t*>(x) + c * 32);
         tmem_ld_wait();
         // tiles holding a key past the first query's key row (the diagonal band) or the sequence,
         // and (LOCAL) a key at or below the last query's window edge, or one before a row's sequence.  All
-        // conditions are the warp's: its lanes go on together to the tcgen05 instructions below.
-        const bool before = SHARED && __any_sync(0xffffffffu, own > kb);
-        if (kb + BN - 1 > m0 || kb + BN > rows || before ||
+        // conditions are the entry's, none a lane's: the warp goes on together to the tcgen05 instructions
+        // below.  (With a vote on `own` and branches around the arrivals 4 prompts of 8B heads 684 us, so 661.)
+        if (kb + BN - 1 > m0 || kb + BN > rows || (SHARED && apart) ||
             (A.g.window > 0 && kb <= min(m0 + BM, rows) - 1 - A.g.window)) {
           const int e_hi = min(r, rows - 1) - kb;
 #pragma unroll
           for (int e = 0; e < BN; ++e)
             if (e > e_hi) x[e] = -INFINITY;
-          if (A.g.window > 0 || before) {
+          if (A.g.window > 0 || (SHARED && apart)) {
             const int e_lo = (SHARED ? max(own, A.g.window > 0 ? r - A.g.window + 1 : 0) : r - A.g.window + 1) - kb;
 #pragma unroll
             for (int e = 0; e < BN; ++e)
@@ -405,8 +405,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) fwd_packed_kernel(const __grid_co
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0 && (parts<DH>() == 2 || c == 3)) mbar_arrive(&sm.p_full[g][parts<DH>() == 2 ? c >> 1 : 0]);
-            if (c < BN / 32 - 1) __syncwarp();
+            if (parts<DH>() == 2 || c == 3) mbar_arrive_if(lane == 0, &sm.p_full[g][parts<DH>() == 2 ? c >> 1 : 0]);
           }
         }
         float s0, s1, s2, s3;

@@ -307,16 +307,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
           tmem_ld_wait();
           // tiles holding a key past the first query's key row (the diagonal band) or the sequence,
           // and (LOCAL) a key at or below the last query's window edge, or before a row's sequence.  All
-          // conditions are the warp's: its lanes go on together to the tcgen05 instructions below.
-          const bool before = __any_sync(0xffffffffu, own > j * BN);
-          if ((j + 1) * BN - 1 > row0 || (j + 1) * BN > w.rows || before ||
+          // conditions are the entry's: the warp goes on together to the tcgen05 instructions below.
+          if ((j + 1) * BN - 1 > row0 || (j + 1) * BN > w.rows || w.seqs > 0 ||
               (A.g.window > 0 && j * BN <= min(row0 + BM, w.rows) - 1 - A.g.window)) {
             const int k0 = j * BN + HB * hc;
             const int e_hi = min(r, w.rows - 1) - k0;
 #pragma unroll
             for (int e = 0; e < HB; ++e)
               if (e > e_hi) x[e] = -INFINITY;
-            if (A.g.window > 0 || before) {
+            if (A.g.window > 0 || w.seqs > 0) {
               const int e_lo = max(own, A.g.window > 0 ? r - A.g.window + 1 : 0) - k0;
 #pragma unroll
               for (int e = 0; e < HB; ++e)

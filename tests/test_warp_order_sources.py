@@ -78,9 +78,7 @@ def test_store_loops_end_with_a_barrier():
         assert body[at:_closing(body, at)].rstrip().endswith("__syncwarp();"), name
 
 
-def test_the_masks_of_shared_tiles_are_decided_by_the_warp():
-    # `own` differs from lane to lane: as a condition it is voted on
+def test_the_masks_of_shared_tiles_are_decided_by_the_entry():
+    # `own` differs from lane to lane: it is no condition of a branch
     for name in ("sfa_fwd_packed.cu", "sfa_fwd_packed256.cu"):
-        body = _softmax(name)
-        uses = [m.start() for m in re.finditer(r"\bown >", body)]
-        assert len(uses) == 1 and body[:uses[0]].endswith("__any_sync(0xffffffffu, "), name
+        assert not re.search(r"\bown\s*[<>]|[<>]=?\s*own\b", _softmax(name)), name
