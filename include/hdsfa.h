@@ -318,12 +318,23 @@ hd_status_t sfa_fwd_packed(const void* q, const void* k, const void* v, void* o,
  * Bit copy.  The pages must be held by the sequence alone.  Rows whose page is not in the
  * pool, and the rows of a sequence whose offsets descend, leave [0, N] or hold more tokens
  * than lens[b], are not written and set HD_DEVBIT_INDEX (so does a length outside
- * [0, max_pages*P]).
+ * [0, max_pages*P]).  With offsets that descend anywhere, rows of other sequences may be left out as
+ * well.
+ *
+ * sfa_kv_append_paged_served -- the same after a hd_pages_grow_served whose result nobody has looked at:
+ *   served int32 [B], its output.  A sequence that got fewer tokens than it brings (one, or
+ *   offsets[b+1] - offsets[b]) is left out, without a bit of its own.  (The plain call cannot tell: to it
+ *   lens[b]-1 is the new token, and where a grow was refused that is the token before, in a page that
+ *   others may share.)
  */
 hd_status_t sfa_kv_append_paged(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
                                 const int32_t* page_table, const int32_t* lens, const int32_t* offsets, int B, int N,
                                 int num_pages, int page_tokens, int max_pages, int n, int Hkv, int Dh,
                                 int32_t* dev_status, cudaStream_t stream);
+hd_status_t sfa_kv_append_paged_served(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                                       const int32_t* page_table, const int32_t* lens, const int32_t* offsets,
+                                       const int32_t* served, int B, int N, int num_pages, int page_tokens, int max_pages,
+                                       int n, int Hkv, int Dh, int32_t* dev_status, cudaStream_t stream);
 
 /*
  * sfa_decode_paged -- sfa_decode over a paged cache: the same masks, outputs and limits (Dh,
@@ -358,7 +369,11 @@ hd_status_t sfa_decode_paged(const void* q, const void* k_pages, const void* v_p
  * hd_pages_grow : lens[b] += add[b], with the pages for it: sequence b, in ascending order,
  *   gets them if all that b and those before it ask for are free; else it and its length are
  *   left as they were (HD_DEVBIT_PAGES).  add[b] < 0, or a length that leaves
- *   [0, max_pages*P], is left out with HD_DEVBIT_INDEX.
+ *   [0, max_pages*P], is left out with HD_DEVBIT_INDEX.  Nothing is to be appended to a sequence that was
+ *   left as it was: look at the status first, or use
+ * hd_pages_grow_served : the same, and served [B] is the tokens that each sequence got, add[b] or 0, for
+ *   sfa_kv_append_paged_served (and the caller: o of a decoding step that follows is no token's for a
+ *   sequence that got none).
  * hd_pages_fork : for i < F, the empty slot dst[i] gets the first tokens[i] tokens of src[i]
  *   (tokens NULL: all of them): floor(tokens/P) pages are shared, the rest of the prefix gets
  *   a page of its own and copies[i] = (page of src, page of dst), else (-1, -1).  src may name
@@ -383,6 +398,9 @@ size_t hd_pages_workspace_bytes(int B, int num_pages); /* 0 for invalid sizes */
 hd_status_t hd_pages_grow(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* add, int B, int max_pages,
                           int num_pages, int page_tokens, void* workspace, size_t workspace_bytes, int32_t* dev_status,
                           cudaStream_t stream);
+hd_status_t hd_pages_grow_served(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* add, int32_t* served,
+                                 int B, int max_pages, int num_pages, int page_tokens, void* workspace,
+                                 size_t workspace_bytes, int32_t* dev_status, cudaStream_t stream);
 hd_status_t hd_pages_fork(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* src, const int32_t* dst,
                           const int32_t* tokens, int F, int32_t* copies, int B, int max_pages, int num_pages,
                           int page_tokens, void* workspace, size_t workspace_bytes, int32_t* dev_status,

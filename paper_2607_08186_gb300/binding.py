@@ -82,10 +82,14 @@ def lib():
             L.sfa_decode_paged.argtypes = [P, P, P, P, P, P, P, I, I, I, I, I, I, I, I, I, F, I, I, P, Z, P, P]
             L.sfa_kv_append_paged.restype = I
             L.sfa_kv_append_paged.argtypes = [P, P, P, P, P, P, P, I, I, I, I, I, I, I, I, P, P]
+            L.sfa_kv_append_paged_served.restype = I
+            L.sfa_kv_append_paged_served.argtypes = [P, P, P, P, P, P, P, P, I, I, I, I, I, I, I, I, P, P]
             L.hd_pages_workspace_bytes.restype = Z
             L.hd_pages_workspace_bytes.argtypes = [I, I]
             L.hd_pages_grow.restype = I
             L.hd_pages_grow.argtypes = [P, P, P, P, I, I, I, I, P, Z, P, P]
+            L.hd_pages_grow_served.restype = I
+            L.hd_pages_grow_served.argtypes = [P, P, P, P, P, I, I, I, I, P, Z, P, P]
             L.hd_pages_fork.restype = I
             L.hd_pages_fork.argtypes = [P, P, P, P, P, P, I, P, I, I, I, I, P, Z, P, P]
             L.hd_pages_free.restype = I
@@ -396,11 +400,12 @@ def _pool_dims(k_pages, page_table, n):
 
 
 def sfa_kv_append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, n, offsets=None, dev_status=None,
-                        stream=None):
+                        stream=None, served=None):
     """New tokens' K/V rows into a paged cache: pools [num_pages][page_tokens*n][Hkv][Dh] bf16, page_table
     [B][max_pages] and lens [B] int32 (the new tokens counted).  Without offsets k_new, v_new [B][n][Hkv][Dh] hold one
     token a sequence (a slot with lens 0 is left out); with offsets [B+1] int32, packed rows [N*n][Hkv][Dh], tokens
-    offsets[b] .. offsets[b+1]-1 are the last ones of sequence b."""
+    offsets[b] .. offsets[b+1]-1 are the last ones of sequence b.  served [B] int32 (hd_pages_grow's): a sequence that
+    got fewer tokens than it brings is left out."""
     pages, P, Hkv, Dh, B, width = _pool_dims(k_pages, page_table, n)
     if offsets is None:
         N, shape = B, (B, n, Hkv, Dh)
@@ -409,7 +414,12 @@ def sfa_kv_append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, n, off
     st = _tensors(stream, ("k_new", k_new, _BF16, shape), ("v_new", v_new, _BF16, shape),
                   ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
                   ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
-                  _opt("offsets", offsets, _I32, (B + 1,)), _dev_status(dev_status))
+                  _opt("offsets", offsets, _I32, (B + 1,)), _opt("served", served, _I32, (B,)), _dev_status(dev_status))
+    if served is not None:
+        _check(lib().sfa_kv_append_paged_served(_p(k_new), _p(v_new), _p(k_pages), _p(v_pages), _p(page_table), _p(lens),
+                                                _p(offsets), _p(served), B, N, pages, P, width, n, Hkv, Dh,
+                                                _p(dev_status), st), "sfa_kv_append_paged_served")
+        return
     _check(lib().sfa_kv_append_paged(_p(k_new), _p(v_new), _p(k_pages), _p(v_pages), _p(page_table), _p(lens),
                                      _p(offsets), B, N, pages, P, width, n, Hkv, Dh, _p(dev_status), st),
            "sfa_kv_append_paged")
@@ -451,12 +461,19 @@ def _page_state(refs, page_table, lens):
                                     ("lens", lens, _I32, (B,)))
 
 
-def hd_pages_grow(refs, page_table, lens, add, page_tokens, workspace, dev_status=None, stream=None):
+def hd_pages_grow(refs, page_table, lens, add, page_tokens, workspace, dev_status=None, stream=None, served=None):
     """lens[b] += add[b], with pages for the new tokens (lowest free ids first, sequences ascending).  refs [num_pages],
     page_table [B][max_pages], lens, add [B] int32.  A sequence that finds no free page stays as it was and sets
-    HD_DEVBIT_PAGES."""
+    HD_DEVBIT_PAGES; nothing is to be appended to it.  served [B] int32 (written): the tokens each sequence got, add[b]
+    or 0, for sfa_kv_append_paged."""
     B, width, pages, state = _page_state(refs, page_table, lens)
-    st = _tensors(stream, *state, ("add", add, _I32, (B,)), _workspace(workspace), _dev_status(dev_status))
+    st = _tensors(stream, *state, ("add", add, _I32, (B,)), _opt("served", served, _I32, (B,)), _workspace(workspace),
+                  _dev_status(dev_status))
+    if served is not None:
+        _check(lib().hd_pages_grow_served(_p(refs), _p(page_table), _p(lens), _p(add), _p(served), B, width, pages,
+                                          int(page_tokens), _p(workspace), workspace.numel(), _p(dev_status), st),
+               "hd_pages_grow_served")
+        return
     _check(lib().hd_pages_grow(_p(refs), _p(page_table), _p(lens), _p(add), B, width, pages, int(page_tokens),
                                _p(workspace), workspace.numel(), _p(dev_status), st), "hd_pages_grow")
 

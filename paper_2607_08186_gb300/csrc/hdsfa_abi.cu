@@ -30,11 +30,12 @@ cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* v
                                     int max_pages, int n, int Hq, int Hkv, int Dh, float scale, int mode, int window,
                                     void* ws, int32_t* status, cudaStream_t st);
 cudaError_t launch_kv_append_paged(const void* kn, const void* vn, void* kp, void* vp, const int32_t* table,
-                                   const int32_t* lens, const int32_t* offsets, int B, int N, int num_pages, int P,
-                                   int max_pages, int n, int Hkv, int Dh, int32_t* status, cudaStream_t st);
+                                   const int32_t* lens, const int32_t* offsets, const int32_t* served, int B, int N,
+                                   int num_pages, int P, int max_pages, int n, int Hkv, int Dh, int32_t* status,
+                                   cudaStream_t st);
 size_t pages_ws_bytes(int B, int num_pages);
-cudaError_t launch_pages_grow(int32_t* refs, int32_t* table, int32_t* lens, const int32_t* add, int B, int max_pages,
-                              int num_pages, int P, void* ws, int32_t* status, cudaStream_t st);
+cudaError_t launch_pages_grow(int32_t* refs, int32_t* table, int32_t* lens, const int32_t* add, int32_t* served, int B,
+                              int max_pages, int num_pages, int P, void* ws, int32_t* status, cudaStream_t st);
 cudaError_t launch_pages_fork(int32_t* refs, int32_t* table, int32_t* lens, const int32_t* src, const int32_t* dst,
                               const int32_t* tokens, int F, int32_t* copies, int B, int max_pages, int num_pages, int P,
                               void* ws, int32_t* status, cudaStream_t st);
@@ -512,11 +513,10 @@ static hd_status_t page_sizes(int B, int max_pages, int num_pages, int P, int n)
   return HD_OK;
 }
 
-hd_status_t sfa_kv_append_paged(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
-                                const int32_t* page_table, const int32_t* lens, const int32_t* offsets, int B, int N,
-                                int num_pages, int page_tokens, int max_pages, int n, int Hkv, int Dh,
-                                int32_t* dev_status, cudaStream_t stream) {
-  HD_NVTX_RANGE("sfa_kv_append_paged");
+static hd_status_t append_paged(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                                const int32_t* page_table, const int32_t* lens, const int32_t* offsets,
+                                const int32_t* served, int B, int N, int num_pages, int page_tokens, int max_pages, int n,
+                                int Hkv, int Dh, int32_t* dev_status, cudaStream_t stream) {
   if (!aligned16(k_pages) || !aligned16(v_pages)) return HD_ERR_INVALID_ARG;
   if (!aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_or_null(offsets, 4) || !aligned_or_null(dev_status, 4))
     return HD_ERR_INVALID_ARG;
@@ -527,8 +527,27 @@ hd_status_t sfa_kv_append_paged(const void* k_new, const void* v_new, void* k_pa
     return HD_ERR_UNSUPPORTED;
   if (N == 0) return HD_OK;
   if (!aligned16(k_new) || !aligned16(v_new)) return HD_ERR_INVALID_ARG;
-  return cuda_status(hdsfa::launch_kv_append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, offsets, B, N,
-                                                   num_pages, page_tokens, max_pages, n, Hkv, Dh, dev_status, stream));
+  return cuda_status(hdsfa::launch_kv_append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, offsets, served, B,
+                                                   N, num_pages, page_tokens, max_pages, n, Hkv, Dh, dev_status, stream));
+}
+
+hd_status_t sfa_kv_append_paged(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                                const int32_t* page_table, const int32_t* lens, const int32_t* offsets, int B, int N,
+                                int num_pages, int page_tokens, int max_pages, int n, int Hkv, int Dh,
+                                int32_t* dev_status, cudaStream_t stream) {
+  HD_NVTX_RANGE("sfa_kv_append_paged");
+  return append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, offsets, nullptr, B, N, num_pages, page_tokens,
+                      max_pages, n, Hkv, Dh, dev_status, stream);
+}
+
+hd_status_t sfa_kv_append_paged_served(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                                       const int32_t* page_table, const int32_t* lens, const int32_t* offsets,
+                                       const int32_t* served, int B, int N, int num_pages, int page_tokens, int max_pages,
+                                       int n, int Hkv, int Dh, int32_t* dev_status, cudaStream_t stream) {
+  HD_NVTX_RANGE("sfa_kv_append_paged_served");
+  if (!aligned_to(served, 4)) return HD_ERR_INVALID_ARG;
+  return append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, offsets, served, B, N, num_pages, page_tokens,
+                      max_pages, n, Hkv, Dh, dev_status, stream);
 }
 
 static hd_status_t decode_paged_sizes(int B, int maxT, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode, int window) {
@@ -583,16 +602,32 @@ size_t hd_pages_workspace_bytes(int B, int num_pages) {
   return B <= 0 || num_pages <= 0 ? 0 : hdsfa::pages_ws_bytes(B, num_pages);
 }
 
-hd_status_t hd_pages_grow(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* add, int B, int max_pages,
-                          int num_pages, int page_tokens, void* workspace, size_t workspace_bytes, int32_t* dev_status,
-                          cudaStream_t stream) {
-  HD_NVTX_RANGE("hd_pages_grow");
+static hd_status_t pages_grow(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* add, int32_t* served,
+                              int B, int max_pages, int num_pages, int page_tokens, void* workspace,
+                              size_t workspace_bytes, int32_t* dev_status, cudaStream_t stream) {
   hd_status_t st = page_state_args(refs, page_table, lens, B, max_pages, num_pages, page_tokens, dev_status);
   if (st != HD_OK) return st;
   if (!aligned_to(add, 4)) return HD_ERR_INVALID_ARG;
   if (!aligned16(workspace) || workspace_bytes < hd_pages_workspace_bytes(B, num_pages)) return HD_ERR_WORKSPACE;
-  return cuda_status(hdsfa::launch_pages_grow(refs, page_table, lens, add, B, max_pages, num_pages, page_tokens,
+  return cuda_status(hdsfa::launch_pages_grow(refs, page_table, lens, add, served, B, max_pages, num_pages, page_tokens,
                                               workspace, dev_status, stream));
+}
+
+hd_status_t hd_pages_grow(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* add, int B, int max_pages,
+                          int num_pages, int page_tokens, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                          cudaStream_t stream) {
+  HD_NVTX_RANGE("hd_pages_grow");
+  return pages_grow(refs, page_table, lens, add, nullptr, B, max_pages, num_pages, page_tokens, workspace, workspace_bytes,
+                    dev_status, stream);
+}
+
+hd_status_t hd_pages_grow_served(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* add, int32_t* served,
+                                 int B, int max_pages, int num_pages, int page_tokens, void* workspace,
+                                 size_t workspace_bytes, int32_t* dev_status, cudaStream_t stream) {
+  HD_NVTX_RANGE("hd_pages_grow_served");
+  if (!aligned_to(served, 4)) return HD_ERR_INVALID_ARG;
+  return pages_grow(refs, page_table, lens, add, served, B, max_pages, num_pages, page_tokens, workspace, workspace_bytes,
+                    dev_status, stream);
 }
 
 hd_status_t hd_pages_fork(int32_t* refs, int32_t* page_table, int32_t* lens, const int32_t* src, const int32_t* dst,

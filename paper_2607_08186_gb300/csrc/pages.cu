@@ -90,8 +90,10 @@ HD_DEVINLINE int list_free(const State& s, int want, int32_t* list, int* sh) {
   return min(found, want);
 }
 
-// Pages for add[b] more tokens of each sequence: ids ascending, sequences ascending.
-__global__ void __launch_bounds__(NT) grow_kernel(State s, const int32_t* add, int32_t* base, int32_t* list) {
+// Pages for add[b] more tokens of each sequence: ids ascending, sequences ascending.  served (or null): the
+// tokens that each got.
+__global__ void __launch_bounds__(NT) grow_kernel(State s, const int32_t* add, int32_t* served, int32_t* base,
+                                                  int32_t* list) {
   __shared__ int sh[32];
   grid_dep_wait();
   grid_dep_launch();
@@ -112,8 +114,10 @@ __global__ void __launch_bounds__(NT) grow_kernel(State s, const int32_t* add, i
   const int avail = list_free(s, total, list, sh);  // its barrier also orders base
   for (int b = warp; b < s.B; b += NT / 32) {
     const int T = s.lens[b], x = add[b], need = need_of(T, x), at = base[b];
+    const bool none = need > 0 && at + need > avail;
+    if (lane == 0 && served != nullptr) served[b] = need < 0 || none ? 0 : x;
     if (need < 0 || x == 0) continue;
-    if (need > 0 && at + need > avail) {
+    if (none) {
       if (lane == 0) set_status(s.status, HD_DEVBIT_PAGES);
       continue;
     }
@@ -379,11 +383,13 @@ HD_DEVINLINE int find_sequence(const int32_t* offsets, int B, int w, int lane) {
 
 // New tokens' K and V rows (blockIdx.y: tensor, 4 KB piece) into pages: a warp per token, whose n
 // rows lie together on both sides.  Without offsets token b is sequence b's one new token; with
-// them sequence b's are the packed tokens offsets[b] .. offsets[b + 1].
+// them sequence b's are the packed tokens offsets[b] .. offsets[b + 1].  served (or null): the tokens that
+// grow gave each sequence; one that got fewer than it brings is left out, since its last tokens' rows are
+// others', in a page that it may share.
 __global__ void __launch_bounds__(256, 5) append_paged_kernel(const uint4* kn, const uint4* vn, uint4* kp, uint4* vp,
                                                               const int32_t* page_table, const int32_t* lens,
-                                                              const int32_t* offsets, int B, int N, int n, int cap,
-                                                              PageGeom g, int tok16, int chunks, int32_t* status) {
+                                                              const int32_t* offsets, const int32_t* served, int B,
+                                                              int N, int n, int cap, PageGeom g, int tok16, int chunks, int32_t* status) {
   const int lane = threadIdx.x & 31;
   const bool first = blockIdx.y == 0;  // reports errors
   const int piece = (int)blockIdx.y % chunks * 256;
@@ -394,7 +400,9 @@ __global__ void __launch_bounds__(256, 5) append_paged_kernel(const uint4* kn, c
   if (offsets != nullptr && blockIdx.x == 0 && first)
     for (int b = threadIdx.x; b < B; b += 256) {
       const int a = offsets[b], z = offsets[b + 1], T = lens[b];
-      if (a < 0 || z < a || z > N || T < 0 || T > cap || z - a > T) set_status(status, HD_DEVBIT_INDEX);
+      bool bad = a < 0 || z < a || z > N || T < 0 || T > cap;
+      if (!bad) bad = z - a > T && (served == nullptr || served[b] >= z - a);
+      if (bad) set_status(status, HD_DEVBIT_INDEX);
     }
   for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < N; w += (long long)gridDim.x * 8) {
     int b = (int)w, t;
@@ -403,6 +411,7 @@ __global__ void __launch_bounds__(256, 5) append_paged_kernel(const uint4* kn, c
       if (b < 0) continue;
       const int a = offsets[b], z = offsets[b + 1], T = lens[b];
       if (a < 0 || z <= w || z > N || T > cap || z - a > T) continue;
+      if (served != nullptr && served[b] < z - a) continue;
       t = T - z + (int)w;
     } else {
       const int T = lens[b];
@@ -411,7 +420,7 @@ __global__ void __launch_bounds__(256, 5) append_paged_kernel(const uint4* kn, c
         continue;
       }
       t = T - 1;
-      if (t < 0) continue;  // an idle slot
+      if (t < 0 || (served != nullptr && served[b] < 1)) continue;  // an idle slot, or one that grow refused
     }
     const int row = page_row(g, page_table + (long long)b * g.max_pages, t * n);
     if (row < 0) {
@@ -445,11 +454,11 @@ static pages::State page_state(int32_t* refs, int32_t* table, int32_t* lens, int
 // (free or low ids, high ids, the map), two counts.
 size_t pages_ws_bytes(int B, int num_pages) { return ((size_t)3 * B + (size_t)3 * num_pages + 2) * sizeof(int32_t); }
 
-cudaError_t launch_pages_grow(int32_t* refs, int32_t* table, int32_t* lens, const int32_t* add, int B, int max_pages,
-                              int num_pages, int P, void* ws, int32_t* status, cudaStream_t st) {
+cudaError_t launch_pages_grow(int32_t* refs, int32_t* table, int32_t* lens, const int32_t* add, int32_t* served, int B,
+                              int max_pages, int num_pages, int P, void* ws, int32_t* status, cudaStream_t st) {
   const pages::State s = page_state(refs, table, lens, B, max_pages, num_pages, P, status);
   int32_t* w = static_cast<int32_t*>(ws);
-  return launch_early(pages::grow_kernel, dim3(1), pages::NT, st, s, add, w, w + (size_t)3 * B);
+  return launch_early(pages::grow_kernel, dim3(1), pages::NT, st, s, add, served, w, w + (size_t)3 * B);
 }
 
 cudaError_t launch_pages_fork(int32_t* refs, int32_t* table, int32_t* lens, const int32_t* src, const int32_t* dst,
@@ -492,13 +501,14 @@ cudaError_t launch_pages_copy(void* kp, void* vp, const int32_t* copies, int F, 
 }
 
 cudaError_t launch_kv_append_paged(const void* kn, const void* vn, void* kp, void* vp, const int32_t* table,
-                                   const int32_t* lens, const int32_t* offsets, int B, int N, int num_pages, int P,
-                                   int max_pages, int n, int Hkv, int Dh, int32_t* status, cudaStream_t st) {
+                                   const int32_t* lens, const int32_t* offsets, const int32_t* served, int B, int N,
+                                   int num_pages, int P, int max_pages, int n, int Hkv, int Dh, int32_t* status,
+                                   cudaStream_t st) {
   const int tok16 = n * Hkv * Dh / 8, chunks = (tok16 + 255) / 256;
   const PageGeom g = make_page_geom(num_pages, max_pages, P * n);
   const unsigned grid = (unsigned)std::min<long long>(((long long)N + 7) / 8, 64 * kSmCount);
   return launch_early(pages::append_paged_kernel, dim3(grid, 2 * chunks), 256, st, (const uint4*)kn, (const uint4*)vn,
-                      (uint4*)kp, (uint4*)vp, table, lens, offsets, B, N, n, max_pages * P, g, tok16, chunks, status);
+                      (uint4*)kp, (uint4*)vp, table, lens, offsets, served, B, N, n, max_pages * P, g, tok16, chunks, status);
 }
 
 }  // namespace hdsfa
