@@ -345,7 +345,9 @@ hd_status_t sfa_kv_append_paged_served(const void* k_new, const void* v_new, voi
  *   SFA_LOCAL needs only the pages that the window of the new token's positions touches.
  *   What a mask hides has no effect, infinities and NaN in it included.
  *   workspace: >= sfa_decode_paged_workspace_bytes(...) bytes, 16-byte aligned, not shared by
- *   calls that may run at the same time.
+ *   calls that may run at the same time.  With the other sizes the same, the bytes for some
+ *   max_tokens and window are enough for every smaller max_tokens and window, any pages and any
+ *   table width; another B asks anew (fewer sequences are split more).
  */
 size_t sfa_decode_paged_workspace_bytes(int B, int max_tokens, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode,
                                         int window); /* 0 for invalid sizes */

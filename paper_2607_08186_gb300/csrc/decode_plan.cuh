@@ -13,6 +13,7 @@ struct DecodePlan {
   size_t part_o_bytes, part_ml_bytes;
 };
 DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, TcDims tc_dims = TcDims::k256);
+DecodePlan decode_plan_bound(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, TcDims tc_dims);
 size_t decode_paged_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window);
 size_t decode_ws_bytes(const DecodePlan& p);
 

@@ -28,7 +28,7 @@ cudaError_t launch_kv_append(const void* kn, const void* vn, void* kc, void* vc,
 cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* vp, const int32_t* table,
                                     const int32_t* lens, void* o, float* lse, int B, int maxT, int num_pages, int P,
                                     int max_pages, int n, int Hq, int Hkv, int Dh, float scale, int mode, int window,
-                                    void* ws, int32_t* status, cudaStream_t st);
+                                    void* ws, size_t ws_bytes, int32_t* status, cudaStream_t st);
 cudaError_t launch_kv_append_paged(const void* kn, const void* vn, void* kp, void* vp, const int32_t* table,
                                    const int32_t* lens, const int32_t* offsets, const int32_t* served, int B, int N,
                                    int num_pages, int P, int max_pages, int n, int Hkv, int Dh, int32_t* status,
@@ -587,7 +587,7 @@ hd_status_t sfa_decode_paged(const void* q, const void* k_pages, const void* v_p
   return cuda_status(hdsfa::launch_sfa_decode_paged(
       q, k_pages, v_pages, page_table, lens, o, lse, B, max_tokens, num_pages, page_tokens, max_pages, n, Hq, Hkv, Dh,
       resolve_scale(softmax_scale, Dh), (int)mode, cut_window(mode, window, (long long)max_tokens * n), workspace,
-      dev_status, stream));
+      workspace_bytes, dev_status, stream));
 }
 
 // ---- who holds which page ----

@@ -923,9 +923,16 @@ __global__ void __launch_bounds__(NTHREADS, 1) decode_tc_kernel(const __grid_con
 
 // ------------------------------------------------------------------ host side
 
-DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, TcDims tc_dims) {
+// What a step's plan follows from: the kernel and its row groups (of the plan), the tiles of a sequence of
+// maxT tokens, CTAs of a split and those that fit at a time.
+namespace {
+struct DecodeLoad {
+  long long tiles, ctas, resident;
+};
+}  // namespace
+static DecodeLoad decode_load(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, TcDims tc_dims,
+                              DecodePlan& p) {
   using namespace dec;
-  DecodePlan p;
   p.G = Hq / Hkv;
   p.M = n * p.G;
   p.tc = p.M <= dectc::BM && ((Dh == 256 && tc_dims != TcDims::kNone) ||
@@ -935,11 +942,22 @@ DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode
   const long long range = mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1)
                                             : (long long)maxT * n;
   const int KT = p.tc ? dectc::BN : Dh == 256 ? ktile<256>() : ktile<128>();
-  const long long tiles = (range + KT - 1) / KT;
-  const long long ctas = (long long)B * Hkv * p.ngroups;
   // resident decode CTAs: two per SM at head dim 128 (104 KB of shared memory) and 256
-  // (112 KB), four at 64
-  const long long resident = 152LL * (p.tc ? 1 : Dh == 64 ? 4 : 2);  // the tcgen05 kernel: one per SM
+  // (112 KB), four at 64; the tcgen05 kernel: one per SM
+  return DecodeLoad{(range + KT - 1) / KT, (long long)B * Hkv * p.ngroups, 152LL * (p.tc ? 1 : Dh == 64 ? 4 : 2)};
+}
+
+static void set_splits(DecodePlan& p, long long ctas, int Dh, int nsplit) {
+  p.nsplit = nsplit;
+  const size_t parts = (size_t)ctas * nsplit;
+  p.part_o_bytes = parts * p.rg * Dh * sizeof(float);
+  p.part_ml_bytes = parts * p.rg * sizeof(float2);
+}
+
+DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, TcDims tc_dims) {
+  using namespace dec;
+  DecodePlan p;
+  const auto [tiles, ctas, resident] = decode_load(B, maxT, n, Hq, Hkv, Dh, mode, window, tc_dims, p);
   // split count: least (waves x (tiles per CTA + a fixed cost of about two tiles))
   long long best = 1, best_cost = -1;
   for (long long ns = 1; ns <= std::min(tiles, (long long)kMaxSplit); ++ns) {
@@ -952,10 +970,28 @@ DecodePlan decode_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode
     }
   }
   const long long tiles_per = (tiles + best - 1) / best;
-  p.nsplit = (int)((tiles + tiles_per - 1) / tiles_per);
-  const size_t parts = (size_t)B * Hkv * p.ngroups * p.nsplit;
-  p.part_o_bytes = parts * p.rg * Dh * sizeof(float);
-  p.part_ml_bytes = parts * p.rg * sizeof(float2);
+  set_splits(p, ctas, Dh, (int)((tiles + tiles_per - 1) / tiles_per));
+  return p;
+}
+
+// A plan with at least the splits of decode_plan for every length up to maxT (and window up to `window`).
+// With w(s) = ceil(ctas s / resident) waves, t tiles take at most w(s) (t / s + 3) for any s, in decode_plan's
+// measure, and the splits s* that it takes at least w* (t / s* + 2) >= t ctas / resident + 2 w*.  So
+//   2 w* <= min over s of t (w(s) / s - ctas / resident) + 3 w(s),
+// which grows with t, and s* <= w* resident / ctas.  (Search itself is not monotonic: one sequence of 1216 tokens,
+// 4 streams, 32 over 8 heads of 128, takes 38 splits, one of 8192 takes 37.)
+DecodePlan decode_plan_bound(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, TcDims tc_dims) {
+  DecodePlan p;
+  const auto [tiles, ctas, resident] = decode_load(B, maxT, n, Hq, Hkv, Dh, mode, window, tc_dims, p);
+  long long waves = -1;
+  for (long long ns = 1; ns <= dec::kMaxSplit; ++ns) {
+    const long long w = (ctas * ns + resident - 1) / resident;
+    if (waves >= 0 && 3 * w / 2 >= waves) break;  // nor does any more splits' value lie below
+    const long long x = (tiles * (w * resident - ctas * ns) + 3 * w * ns * resident) / (2 * ns * resident);
+    if (waves < 0 || x < waves) waves = x;
+  }
+  const long long most = std::min(waves * resident / ctas, std::min(tiles, (long long)dec::kMaxSplit));
+  set_splits(p, ctas, Dh, (int)std::max(1LL, most));
   return p;
 }
 

@@ -520,9 +520,9 @@ static DecodePlan paged_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, in
 constexpr size_t kShareBytes = dec::kBalancedSeqs * sizeof(int2);
 
 size_t decode_paged_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {
-  // either kernel's, whatever the pages
-  return std::max(decode_ws_bytes(decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, TcDims::kWith128)),
-                  decode_ws_bytes(decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, TcDims::kNone))) + kShareBytes;
+  // either kernel's, whatever the pages, and enough for every smaller maxT and window
+  return std::max(decode_ws_bytes(decode_plan_bound(B, maxT, n, Hq, Hkv, Dh, mode, window, TcDims::kWith128)),
+                  decode_ws_bytes(decode_plan_bound(B, maxT, n, Hq, Hkv, Dh, mode, window, TcDims::kNone))) + kShareBytes;
 }
 
 // A tile of at most `most` positions: whole pieces, the largest that no page boundary cuts (a page's
@@ -556,9 +556,10 @@ static cudaError_t launch_paged_d(const dec::PagedParams& p, cudaStream_t st) {
 cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* vp, const int32_t* table,
                                     const int32_t* lens, void* o, float* lse, int B, int maxT, int num_pages, int P,
                                     int max_pages, int n, int Hq, int Hkv, int Dh, float scale, int mode, int window,
-                                    void* ws, int32_t* status, cudaStream_t st) {
+                                    void* ws, size_t ws_bytes, int32_t* status, cudaStream_t st) {
   const long long range = paged_range(maxT, n, mode, window);
   const DecodePlan plan = paged_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, paged_tc(B, n, Hq, Hkv, Dh, P * n, range));
+  if (kShareBytes + decode_ws_bytes(plan) > ws_bytes) return cudaErrorInvalidValue;  // the bound says that it is not
   dec::PagedParams p = {};
   dec::DecodeArgs& a = p.a;
   a.q = (const bf16*)q;
