@@ -469,32 +469,6 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
 
 // ------------------------------------------------------------------ host side
 
-// Which kernel reads the pages, by query rows per K/V head and rows per page.  The tensor-core kernel reads
-// the cache once for up to 128 rows, but by TMA alone, which small pages make slow; the other one reads it
-// once for each 32 rows, by cp.async where pages are small.  Measured in us, tensor cores / the other (at head
-// dim 256 4 sequences of 8192 tokens, 2 K/V heads; at 128 8 of 2048, 8 K/V heads; n streams):
-//   <= 16 query rows   never    256: 16 rows a page 23.8 / 19.0 (n 1), 64: 51.6 / 48.6 (n 4), 128: 22.0 / 18.8 (n 1);
-//                               only lengths of a quarter to all 58.3 / 65.4 (7 sequences, n 4)
-//   <= 32, 256 only    from 12  8 rows a page 79 / 69, 9: 80 / 61, 10: 96 / 83, 12: 70.7 / 75.6, 16: 56.3 / 60.9
-//   <= 64              from 5   256: 3 rows a page 130 / 105, 4: 126 / 125, 5: 136 / 158, 6: 81 / 101
-//                               128: 3 rows a page 158 / 110, 4: 159 / 139, 5: 175 / 174, 6: 98 / 109, 8: 103 / 128, 64: 57 / 95
-//   <= 128             from 4   256: 2 rows a page 72 / 58 (n 1), 3: 65 / 57 (n 1), 4: 45 / 57 (n 1)
-//                               128: 3 rows a page 168 / 155 (n 3), 4: 55 / 69 (n 1), 164 / 191 (n 4)
-// And it takes longer to start and end, one CTA per SM, so a range of few positions is the other one's (4
-// streams, pages of 64 rows; B sequences of so many tokens):
-//   128, > 32 rows   B 4: 50 tokens 13.7 / 11.6, 150: 14.5 / 16.3; B 16 (128 CTAs): 50: 27.6 / 14.8, 400: 41.6 /
-//                    39.0, 1000: 64 / 79; B 64: 12: 97 / 41, 150: 122 / 81, 400: 164 / 145, 1000: 275 / 357
-//   256, > 32 rows   B 4: 50: 13.1 / 10.6, 150: 13.2 / 12.9, 400: 13.8 / 15.5; B 33: 50: 22 / 20, 150: 28 / 34
-//   256, <= 32 rows  B 4: 50: 12.9 / 10.0, 400: 13.9 / 14.4; B 33: 50: 19.3 / 18.2, 400: 35.2 / 36.7
-static TcDims paged_tc(int B, int n, int Hq, int Hkv, int Dh, int prow, long long range) {
-  const int M = n * (Hq / Hkv);
-  if (M <= 16) return TcDims::kNone;
-  const int few = M <= 32 ? 1200 : Dh == 128 && (long long)B * Hkv > kSmCount / 4 ? 2000 : 400;
-  if (range < few) return TcDims::kNone;
-  if (M <= 32) return prow < 12 ? TcDims::kNone : TcDims::k256;
-  return prow < (M <= 64 ? 5 : 4) ? TcDims::kNone : TcDims::kWith128;
-}
-
 // Positions that a step of maxT tokens reads at most.
 static long long paged_range(int maxT, int n, int mode, int window) {
   return mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1) : (long long)maxT * n;
@@ -525,13 +499,10 @@ size_t decode_paged_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, in
                   decode_ws_bytes(decode_plan_bound(B, maxT, n, Hq, Hkv, Dh, mode, window, TcDims::kNone))) + kShareBytes;
 }
 
-// A tile of at most `most` positions: whole pieces, the largest that no page boundary cuts (a page's
-// rows, or their largest divisor that a tile holds).
+// A tile of at most `most` positions: whole pieces of pages.
 static void paged_tile(dec::DecodeArgs& a, int most) {
-  int d = std::min(a.pg.prow, most);
-  while (a.pg.prow % d) --d;
-  a.piece = d;
-  a.tile = most / d * d;
+  a.piece = paged_piece(a.pg.prow, most);
+  a.tile = most / a.piece * a.piece;
   a.d_tile = make_fast_div((uint32_t)a.tile);
 }
 
@@ -558,7 +529,7 @@ cudaError_t launch_sfa_decode_paged(const void* q, const void* kp, const void* v
                                     int max_pages, int n, int Hq, int Hkv, int Dh, float scale, int mode, int window,
                                     void* ws, size_t ws_bytes, int32_t* status, cudaStream_t st) {
   const long long range = paged_range(maxT, n, mode, window);
-  const DecodePlan plan = paged_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, paged_tc(B, n, Hq, Hkv, Dh, P * n, range));
+  const DecodePlan plan = paged_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, paged_tc(B, n, Hq, Hkv, Dh, paged_piece(P * n, 128), range));
   if (kShareBytes + decode_ws_bytes(plan) > ws_bytes) return cudaErrorInvalidValue;  // the bound says that it is not
   dec::PagedParams p = {};
   dec::DecodeArgs& a = p.a;
