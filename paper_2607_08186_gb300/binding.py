@@ -410,7 +410,8 @@ def sfa_kv_append_paged(k_new, v_new, k_pages, v_pages, page_table, lens, n, off
     if offsets is None:
         N, shape = B, (B, n, Hkv, Dh)
     else:
-        N, shape = k_new.shape[0] // n, (k_new.shape[0] // n * n, Hkv, Dh)
+        N = k_new.shape[0] // n if k_new.dim() == 3 else 0
+        shape = (N * n, Hkv, Dh)
     st = _tensors(stream, ("k_new", k_new, _BF16, shape), ("v_new", v_new, _BF16, shape),
                   ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
                   ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
@@ -515,10 +516,12 @@ def hd_pages_compact(refs, page_table, lens, new_refs, new_table, moves, page_to
 
 def hd_pages_copy(k_pages, v_pages, copies, dev_status=None, stream=None):
     """Page copies[i][0] onto page copies[i][1] in both pools (one layer's); pairs of -1 are left out."""
+    if k_pages.dim() < 1 or k_pages.shape[0] < 1:
+        raise ValueError("k_pages must have a page: [num_pages][page_tokens*n][Hkv][Dh]")
     st = _tensors(stream, ("k_pages", k_pages, _BF16, k_pages.shape), ("v_pages", v_pages, _BF16, k_pages.shape),
                   ("copies", copies, _I32, (copies.numel() // 2, 2)), _dev_status(dev_status))
     _check(lib().hd_pages_copy(_p(k_pages), _p(v_pages), _p(copies), copies.shape[0], k_pages.shape[0],
-                               k_pages[0].numel() * 2, _p(dev_status), st), "hd_pages_copy")
+                               k_pages.numel() // k_pages.shape[0] * 2, _p(dev_status), st), "hd_pages_copy")
 
 
 SFA_BWD_NOALLOC_MAX_BYTES = 64 << 20

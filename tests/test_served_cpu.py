@@ -42,3 +42,15 @@ def test_binding_refuses_wrong_tensors(lib):
             binding.hd_pages_grow(refs, table, lens, lens, 8, ws, served=served)
         with pytest.raises(ValueError, match=word):
             binding.sfa_kv_append_paged(kn, kn, k, k, table, lens, 2, served=served)
+
+
+def test_tensors_without_the_expected_dimensions_are_value_errors(lib):
+    i32, bf16 = torch.int32, torch.bfloat16
+    table, lens, off = torch.zeros(3, 4, dtype=i32), torch.zeros(3, dtype=i32), torch.zeros(4, dtype=i32)
+    k = torch.zeros(6, 16, 2, 64, dtype=bf16)
+    for pool in (torch.zeros(0, 16, 2, 64, dtype=bf16), torch.zeros((), dtype=bf16)):
+        with pytest.raises(ValueError):
+            binding.hd_pages_copy(pool, pool, torch.zeros(0, 2, dtype=i32))
+    for new in (torch.zeros((), dtype=bf16), torch.zeros(4, dtype=bf16)):
+        with pytest.raises(ValueError, match="k_new"):
+            binding.sfa_kv_append_paged(new, new, k, k, table, lens, 2, offsets=off)
