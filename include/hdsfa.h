@@ -287,6 +287,7 @@ hd_status_t sfa_kv_append(const void* k_new, const void* v_new, void* k_cache, v
  * (no SFA_WITHIN_NAIVE); forward only.  A sequence's results do not depend on what is packed around
  * it, to the bit where it has more than 48 rows (n per token, or one in SFA_WITHIN); shorter ones share
  * tiles, where their place may change the rounding.
+ * o and lse overlap no input (rows are read again where values are not finite).
  * workspace: >= sfa_fwd_packed_workspace_bytes(...) bytes, 16-byte aligned (the list of query
  * tiles, built by each call), not shared by calls that may run at the same time.
  */
@@ -373,7 +374,7 @@ hd_status_t sfa_decode_paged(const void* q, const void* k_pages, const void* v_p
  *   left as they were (HD_DEVBIT_PAGES).  add[b] < 0, or a length that leaves
  *   [0, max_pages*P], is left out with HD_DEVBIT_INDEX.  Nothing is to be appended to a sequence that was
  *   left as it was: look at the status first, or use
- * hd_pages_grow_served : the same, and served [B] is the tokens that each sequence got, add[b] or 0, for
+ * hd_pages_grow_served : the same, and served [B] (a buffer of its own) is the tokens that each sequence got, add[b] or 0, for
  *   sfa_kv_append_paged_served (and the caller: o of a decoding step that follows is no token's for a
  *   sequence that got none).
  * hd_pages_fork : for i < F, the empty slot dst[i] gets the first tokens[i] tokens of src[i]

@@ -3,7 +3,8 @@
 // State, all int32 in device memory of the caller: refs [num_pages] counts the sequences that
 // hold a page (0: free), page_table [B][max_pages] lists a sequence's pages in order, lens [B]
 // its tokens; a sequence of T tokens holds ceil(T / P) pages.  A page that two sequences share
-// is full (hd_pages_fork copies the partly filled one), so nobody appends to a shared page.
+// is full (hd_pages_fork copies the partly filled one), so a sequence that grow gave its pages appends to
+// none that is shared.
 // There is no list of free pages to keep: the lowest free ids are found by a scan of refs,
 // which makes every result a function of the state alone.
 //

@@ -13,7 +13,9 @@
 //
 // In shared memory a K or V tile is DH/64 blocks of [KT][64] with the 128-byte swizzle that TMA
 // writes: conflict-free for ldmatrix as well.  Splits, partials and the combine kernel are those of
-// the contiguous cache; a masked key's V row that is not finite is settled by exact_row.
+// the contiguous cache; a masked key's V row that is not finite is settled by exact_row.  P is rounded to
+// bf16 for its product, whose operands have one type (at most 2^-8 of each term, as O's own rounding);
+// maxima, sums, partials and LSE are fp32.
 #include <float.h>
 
 #include <algorithm>
@@ -475,7 +477,9 @@ static long long paged_range(int maxT, int n, int mode, int window) {
 }
 
 // The contiguous cache's plan, with the combine kernel (about three tiles' time, nothing to do for one
-// split) in the cost: short sequences take one split, whose CTAs write the results.
+// split) in the cost: short sequences take one split, whose CTAs write the results.  (Four resident CTAs at
+// head dim 64 are the contiguous kernel's and this one's for up to 16 query rows; with more rows its 158 to
+// 160 registers leave room for three.)
 static DecodePlan paged_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window,
                              TcDims tc_dims) {
   DecodePlan p = decode_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, tc_dims);

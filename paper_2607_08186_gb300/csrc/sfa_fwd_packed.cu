@@ -13,7 +13,8 @@
 // two heads of a K/V head where there is an even number of them, else 256 rows of one head.  Roles:
 // warp 0 loads (TMA), warp 1 issues MMAs and owns TMEM, four warps per group do the online softmax, a
 // thread per row.  Per key tile and group: S = Q K^T into 128 TMEM columns, P (bf16) over their first
-// half, O += P V into DH columns.
+// half, O += P V into DH columns.  P is rounded to bf16 because V is bf16 and an MMA's operands have one type:
+// at most 2^-8 of each term, as O's own rounding; maxima, sums, O and LSE are fp32.
 //
 // Short sequences (at most kShortRows rows) that lie together share a tile: to a row of one, its
 // neighbours' keys are masked, like those before a window, up to its own sequence's first row (SHARED;
