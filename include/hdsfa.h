@@ -374,9 +374,9 @@ hd_status_t sfa_decode_paged(const void* q, const void* k_pages, const void* v_p
  *   left as they were (HD_DEVBIT_PAGES).  add[b] < 0, or a length that leaves
  *   [0, max_pages*P], is left out with HD_DEVBIT_INDEX.  Nothing is to be appended to a sequence that was
  *   left as it was: look at the status first, or use
- * hd_pages_grow_served : the same, and served [B] (a buffer of its own) is the tokens that each sequence got, add[b] or 0, for
- *   sfa_kv_append_paged_served (and the caller: o of a decoding step that follows is no token's for a
- *   sequence that got none).
+ * hd_pages_grow_served : the same, and served [B] (a buffer of its own) is the tokens that each
+ *   sequence got, add[b] or 0, for sfa_kv_append_paged_served (and the caller: o of a decoding step that
+ *   follows is no token's for a sequence that got none).
  * hd_pages_fork : for i < F, the empty slot dst[i] gets the first tokens[i] tokens of src[i]
  *   (tokens NULL: all of them): floor(tokens/P) pages are shared, the rest of the prefix gets
  *   a page of its own and copies[i] = (page of src, page of dst), else (-1, -1).  src may name
