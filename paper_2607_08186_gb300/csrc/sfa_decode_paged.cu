@@ -189,9 +189,11 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
     if (row < 0) sm.bad_page = 1;
     return row;
   };
+  [[maybe_unused]] int brought = -1;  // TMA: the last tile that this warp brought
   auto load_tile = [&](int it) {
     const int st = it % STAGES;
     if constexpr (TMA) {
+      brought = it;
       if (lane == 0) mbar_arrive_expect_tx(&sm.full[st], tile * DH * 2 * 2);
       __syncwarp();
       if (lane * a.piece < tile) {
@@ -380,8 +382,12 @@ __global__ void __launch_bounds__(NT, DH == 64 ? (MT == 1 ? 4 : 3) : 2)
       sm.row[(it + 3) & 3][tid] = next_row;
     }
   }
-  // a wait gave up (about a second after every copy in flight was issued): the results are invalid
-  if (TMA && __syncthreads_or(!alive)) return;
+  if constexpr (TMA) {
+    // a wait gave up: the results are invalid.  A warp that goes on has seen every tile land; one that does not
+    // waits (again with a limit) for the last that it brought, whose stage no earlier one can still be filling.
+    if (!alive && brought >= 0 && lane == 0) mbar_drain(&sm.full[brought % STAGES], (brought / STAGES) & 1);
+    if (__syncthreads_or(!alive)) return;
+  }
 
   // merge the 4 warps' partials in shared memory (the K/V ring is free now)
   if (!TMA) {

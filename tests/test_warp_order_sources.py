@@ -82,3 +82,10 @@ def test_the_masks_of_shared_tiles_are_decided_by_the_entry():
     # `own` differs from lane to lane: it is no condition of a branch
     for name in ("sfa_fwd_packed.cu", "sfa_fwd_packed256.cu"):
         assert not re.search(r"\bown\s*[<>]|[<>]=?\s*own\b", _softmax(name)), name
+
+
+def test_copies_land_before_a_cta_that_gave_up_exits():
+    # a bounded wait that runs out ends the kernel's work, not its copies in flight
+    src = _source("sfa_decode_paged.cu")
+    leave = src.index("if (__syncthreads_or(!alive)) return;")
+    assert "mbar_drain(&sm.full[brought % STAGES], (brought / STAGES) & 1);" in src[leave - 300:leave]
