@@ -122,6 +122,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
       // Units in the ring, entry after entry: K(0), then K(t+1), V(t) for each tile.  A slot is free
       // once the MMAs that read what it holds have completed.
       int units = 0, slot = 0, tiles = 0;  // ... and tiles of the entries before
+      int queries = 0, tails = 0;          // entries whose Q, and whose last V, have been asked for
       bool ok = true;
       for (int k = 0, pos; ok && (pos = place_of(k)) < total; ++k) {
         const PackedEntry w(A, pos);
@@ -140,6 +141,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
             if (rank == 0) mbar_arrive(&sm.full[slot]);  // nobody waits for this phase; the slot's go on
             uint64_t* bar = &sm.v_tail[k & 3];
             mbar_arrive_expect_tx(bar, BN * PC * 2);
+            ++tails;
             for (int c = 0; c < PC / 64; ++c)
               tma_load_5d(sm.ring[slot] + c * BN * 64, &P.tm_v, bar, rank * PC + c * 64, kvh, w.stream, r0, 0);
           } else {
@@ -160,6 +162,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
         // the last S of the entry before has read Q
         if (ok && k > 0) ok = mbar_wait(&sm.s_full[(tiles - 1) & 3], ((tiles - 1) >> 2) & 1, abort, A.status);
         if (!ok) break;
+        ++queries;
         for (int c = 0; c < DH / 64; ++c) {
           if (rank == 0) mbar_arrive_expect_tx(&sm.q_full[c], 2 * BM * 64 * 2);
           tma_load_pair(sm.q + c * BM * 64, &P.tm_q, lead_addr(&sm.q_full[c]), c * 64, w.head_of(A, rank), w.stream,
@@ -171,6 +174,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
         }
         tiles += T;
       }
+      // Every copy that this thread started lands before the pair exits, also after a wait gave up (one limit for
+      // all).  On the first CTA's barriers are both CTAs' bytes.
+      const long long t0 = clock64();
+      auto land = [&](uint64_t* bar, int par) {
+        while (!mbar_try_wait(bar, par & 1) && clock64() - t0 < kWaitTimeoutCycles) {
+        }
+      };
+      if (rank == 0) {
+        for (int u = max(0, units - NSLOT); u < units; ++u) land(&sm.full[u % NSLOT], u / NSLOT);
+        for (int c = 0; queries > 0 && c < DH / 64; ++c) land(&sm.q_full[c], queries - 1);
+      }
+      for (int k = max(0, tails - 4); k < tails; ++k) land(&sm.v_tail[k & 3], k >> 2);
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (first CTA)

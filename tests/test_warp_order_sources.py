@@ -89,3 +89,7 @@ def test_copies_land_before_a_cta_that_gave_up_exits():
     src = _source("sfa_decode_paged.cu")
     leave = src.index("if (__syncthreads_or(!alive)) return;")
     assert "mbar_drain(&sm.full[brought % STAGES], (brought / STAGES) & 1);" in src[leave - 300:leave]
+    src = _source("sfa_fwd_packed256.cu")
+    producer = src[src.index("if (warp == 0) {"):src.index("} else if (warp == 1) {")]
+    for bar in ("land(&sm.full[u % NSLOT], u / NSLOT);", "land(&sm.q_full[c], queries - 1);", "land(&sm.v_tail[k & 3], k >> 2);"):
+        assert bar in producer[producer.rindex("tiles += T;"):], bar
