@@ -417,6 +417,58 @@ hd_status_t hd_pages_copy(void* k_pages, void* v_pages, const int32_t* copies, i
                           int32_t* dev_status, cudaStream_t stream);
 
 /*
+ * Paged cache in 8 bits.  The same tables, lengths and page calls as above; the pools of a layer hold
+ *   k_pages, v_pages   : e4m3 codes, 1 byte each, [num_pages][Hkv][P*n][Dh]: a page's rows of one head together
+ *   k_scales, v_scales : uint8 [num_pages][Hkv][P/block_tokens], a scale for each block of block_tokens tokens (which
+ *                        divides P; all n streams of a token together) and head: a power of two 2^e as the byte e + 127
+ * A code c of a block stands for c * 2^e, which is exact in bf16.  e lies in [-64, 50] (bytes 63 ... 177; others
+ * are read as the nearest of these): values below 2^-74 become 0, values above 448 * 2^50 saturate.
+ * Limits beside those above: Dh a multiple of 16, n*Hkv*Dh <= 2^24, block_tokens*n*Dh <= 2^30, Hkv <= 32767,
+ * num_pages*P*n*Hkv < 2^32.
+ *
+ * sfa_kv_append_paged_q8 -- sfa_kv_append_paged into such a cache: the same arguments, rows and refusals; served
+ *   (nullable) as in sfa_kv_append_paged_served.  Of a block, the call brings some last tokens.  If no token before
+ *   them is in the block, its e is the smallest with 448 * 2^e no smaller than their largest finite magnitude
+ *   (within [-64, 50]); else the larger of that and the e that it has, and where that is larger than it was the codes
+ *   of the tokens before them are rounded again (exactly, but for values that become subnormal in e4m3).  Values are
+ *   rounded to the nearest code, ties to even; infinities and NaN become NaN.  Rows of the block behind the
+ *   sequence's tokens are left as they were.  So the same tokens in the same calls give the same bits, and in other
+ *   calls differ by one rounding more at most for each growth.
+ *
+ * sfa_kv_read_paged_q8 -- the way back: packed rows k, v bf16 [N*n][Hkv][Dh] of the last tokens of each sequence,
+ *   sequence b's to offsets[b] .. offsets[b+1]-1 (token lens[b] - offsets[b+1] + i to packed token i; lens may be less
+ *   than the sequence holds).  Exact.  Rows before offsets[0] and from offsets[B] on are left as they were, and so
+ *   are, with HD_DEVBIT_INDEX, the rows of what sfa_kv_append_paged would refuse.
+ *
+ * sfa_decode_paged_q8 -- sfa_decode_paged over such a cache: the same masks, outputs, errors and workspace rules (with
+ *   its own workspace size).  The result is that of the values that the codes stand for.  Dh 64, 128 or 256.
+ *
+ * hd_pages_copy_q8 -- hd_pages_copy for codes (page_bytes = Hkv*P*n*Dh, a multiple of 16) and scales (page_scales =
+ *   Hkv*P/block_tokens bytes a page).
+ */
+hd_status_t sfa_kv_append_paged_q8(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                                   uint8_t* k_scales, uint8_t* v_scales, const int32_t* page_table, const int32_t* lens,
+                                   const int32_t* offsets, const int32_t* served, int B, int N, int num_pages,
+                                   int page_tokens, int max_pages, int n, int Hkv, int Dh, int block_tokens,
+                                   int32_t* dev_status, cudaStream_t stream);
+hd_status_t sfa_kv_read_paged_q8(const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+                                 const uint8_t* v_scales, const int32_t* page_table, const int32_t* lens,
+                                 const int32_t* offsets, void* k, void* v, int B, int N, int num_pages, int page_tokens,
+                                 int max_pages, int n, int Hkv, int Dh, int block_tokens, int32_t* dev_status,
+                                 cudaStream_t stream);
+size_t sfa_decode_paged_q8_workspace_bytes(int B, int max_tokens, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode,
+                                           int window); /* 0 for invalid sizes */
+hd_status_t sfa_decode_paged_q8(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+                                const uint8_t* v_scales, const int32_t* page_table, const int32_t* lens, void* o,
+                                float* lse, int B, int max_tokens, int num_pages, int page_tokens, int max_pages, int n,
+                                int Hq, int Hkv, int Dh, int block_tokens, float softmax_scale, sfa_mode_t mode,
+                                int window, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                                cudaStream_t stream);
+hd_status_t hd_pages_copy_q8(void* k_pages, void* v_pages, uint8_t* k_scales, uint8_t* v_scales, const int32_t* copies,
+                             int F, int num_pages, size_t page_bytes, size_t page_scales, int32_t* dev_status,
+                             cudaStream_t stream);
+
+/*
  * sfa_bwd_noalloc -- sfa_bwd without a caller-supplied workspace.  The paper has no
  * counterpart: this is an interface for callers that cannot hand the library device
  * memory of their own (a runtime that commits its whole device-memory budget at

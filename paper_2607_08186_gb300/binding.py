@@ -98,6 +98,16 @@ def lib():
             L.hd_pages_compact.argtypes = [P, P, P, P, P, P, I, I, I, I, P, Z, P, P]
             L.hd_pages_copy.restype = I
             L.hd_pages_copy.argtypes = [P, P, P, I, I, Z, P, P]
+            L.sfa_kv_append_paged_q8.restype = I
+            L.sfa_kv_append_paged_q8.argtypes = [P] * 10 + [I] * 9 + [P, P]
+            L.sfa_kv_read_paged_q8.restype = I
+            L.sfa_kv_read_paged_q8.argtypes = [P] * 9 + [I] * 9 + [P, P]
+            L.sfa_decode_paged_q8_workspace_bytes.restype = Z
+            L.sfa_decode_paged_q8_workspace_bytes.argtypes = [I] * 8
+            L.sfa_decode_paged_q8.restype = I
+            L.sfa_decode_paged_q8.argtypes = [P] * 9 + [I] * 10 + [F, I, I, P, Z, P, P]
+            L.hd_pages_copy_q8.restype = I
+            L.hd_pages_copy_q8.argtypes = [P] * 5 + [I, I, Z, Z, P, P]
             L.sfa_fwd.restype = I
             L.sfa_fwd.argtypes = [P, P, P, P, P, I, I, I, I, I, I, F, I, I, P, P]
             L.sfa_bwd_workspace_bytes.restype = Z
@@ -347,7 +357,7 @@ def _refuse(dev, name, t, dtype, shape):
                      f"{tuple(t.shape)}{'' if t.is_contiguous() else ' (not contiguous)'}")
 
 
-_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+_BF16, _F32, _I32, _F8 = torch.bfloat16, torch.float32, torch.int32, torch.float8_e4m3fn
 
 
 def _opt(name, t, dtype, shape):
@@ -522,6 +532,99 @@ def hd_pages_copy(k_pages, v_pages, copies, dev_status=None, stream=None):
                   ("copies", copies, _I32, (copies.numel() // 2, 2)), _dev_status(dev_status))
     _check(lib().hd_pages_copy(_p(k_pages), _p(v_pages), _p(copies), copies.shape[0], k_pages.shape[0],
                                k_pages.numel() // k_pages.shape[0] * 2, _p(dev_status), st), "hd_pages_copy")
+
+
+# ---- paged cache in 8 bits: the pools hold e4m3 codes [num_pages][Hkv][page_tokens*n][Dh] (torch.float8_e4m3fn), with a
+# scale for each block of block_tokens tokens and head, [num_pages][Hkv][page_tokens/block_tokens] (torch.uint8): the
+# power of two 2^(byte - 127).
+
+def _q8_pools(k_pages, v_pages, k_scales, v_scales, page_table, n):
+    """(num_pages, page_tokens, Hkv, Dh, block_tokens, B, max_pages) and the pools' tensors to check."""
+    if k_pages.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("k_pages must be [num_pages][Hkv][page_tokens*n][Dh] and page_table [B][max_pages]")
+    pages, Hkv, rows, Dh = k_pages.shape
+    if n < 1 or rows % n:
+        raise ValueError("k_pages.shape[2] must be page_tokens * n")
+    P, blocks = rows // n, k_scales.shape[2] if k_scales.dim() == 3 else 0
+    if blocks < 1 or P % blocks:
+        raise ValueError("k_scales must be [num_pages][Hkv][page_tokens/block_tokens]")
+    scales = (pages, Hkv, blocks)
+    return (pages, P, Hkv, Dh, P // blocks, *page_table.shape), (
+        ("k_pages", k_pages, _F8, k_pages.shape), ("v_pages", v_pages, _F8, k_pages.shape),
+        ("k_scales", k_scales, torch.uint8, scales), ("v_scales", v_scales, torch.uint8, scales))
+
+
+def sfa_kv_append_paged_q8(k_new, v_new, k_pages, v_pages, k_scales, v_scales, page_table, lens, n, offsets=None,
+                           dev_status=None, stream=None, served=None):
+    """sfa_kv_append_paged into an 8-bit cache: k_new, v_new bf16 [B][n][Hkv][Dh], or with offsets packed rows
+    [N*n][Hkv][Dh].  A block's scale is the smallest power of two that holds its new tokens, and at least the one that
+    it had if it held tokens before (whose codes are rounded again where it grows)."""
+    (pages, P, Hkv, Dh, T, B, width), pools = _q8_pools(k_pages, v_pages, k_scales, v_scales, page_table, n)
+    if offsets is None:
+        N, shape = B, (B, n, Hkv, Dh)
+    else:
+        N = k_new.shape[0] // n if k_new.dim() == 3 else 0
+        shape = (N * n, Hkv, Dh)
+    st = _tensors(stream, ("k_new", k_new, _BF16, shape), ("v_new", v_new, _BF16, shape), *pools,
+                  ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
+                  _opt("offsets", offsets, _I32, (B + 1,)), _opt("served", served, _I32, (B,)), _dev_status(dev_status))
+    _check(lib().sfa_kv_append_paged_q8(_p(k_new), _p(v_new), _p(k_pages), _p(v_pages), _p(k_scales), _p(v_scales),
+                                        _p(page_table), _p(lens), _p(offsets), _p(served), B, N, pages, P, width, n, Hkv,
+                                        Dh, T, _p(dev_status), st), "sfa_kv_append_paged_q8")
+
+
+def sfa_kv_read_paged_q8(k_pages, v_pages, k_scales, v_scales, page_table, lens, offsets, k, v, n, dev_status=None,
+                         stream=None):
+    """The values of an 8-bit cache back as packed bf16 rows k, v [N*n][Hkv][Dh] (written, exact): the last
+    offsets[b+1] - offsets[b] of the first lens[b] tokens of each sequence.  Rows outside [offsets[0], offsets[B]) are
+    left as they were."""
+    (pages, P, Hkv, Dh, T, B, width), pools = _q8_pools(k_pages, v_pages, k_scales, v_scales, page_table, n)
+    N = k.shape[0] // n if k.dim() == 3 else 0
+    shape = (N * n, Hkv, Dh)
+    st = _tensors(stream, *pools, ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
+                  ("offsets", offsets, _I32, (B + 1,)), ("k", k, _BF16, shape), ("v", v, _BF16, shape),
+                  _dev_status(dev_status))
+    _check(lib().sfa_kv_read_paged_q8(_p(k_pages), _p(v_pages), _p(k_scales), _p(v_scales), _p(page_table), _p(lens),
+                                      _p(offsets), _p(k), _p(v), B, N, pages, P, width, n, Hkv, Dh, T, _p(dev_status), st),
+           "sfa_kv_read_paged_q8")
+    return k, v
+
+
+def sfa_decode_paged_q8_workspace_bytes(B, max_tokens, n, Hq, Hkv, Dh, mode, window=0) -> int:
+    return int(lib().sfa_decode_paged_q8_workspace_bytes(B, max_tokens, n, Hq, Hkv, Dh, int(mode), int(window)))
+
+
+def sfa_decode_paged_q8(q, k_pages, v_pages, k_scales, v_scales, page_table, lens, o, n, mode, workspace,
+                        max_tokens=None, lse=None, softmax_scale=0.0, window=0, dev_status=None, stream=None):
+    """sfa_decode_paged over an 8-bit cache: q, o [B][n][Hq][Dh] bf16, lse [B][Hq][n] float32 or None; the result is that
+    of the values that the codes stand for."""
+    (pages, P, Hkv, Dh, T, B, width), pools = _q8_pools(k_pages, v_pages, k_scales, v_scales, page_table, n)
+    if q.dim() != 4:
+        raise ValueError("q must be [B][n][Hq][Dh]")
+    Hq = q.shape[2]
+    most = P * width if max_tokens is None else int(max_tokens)
+    st = _tensors(stream, ("q", q, _BF16, (B, n, Hq, Dh)), ("o", o, _BF16, (B, n, Hq, Dh)), *pools,
+                  ("page_table", page_table, _I32, (B, width)), ("lens", lens, _I32, (B,)),
+                  _opt("lse", lse, _F32, (B, Hq, n)), _workspace(workspace), _dev_status(dev_status))
+    _check(lib().sfa_decode_paged_q8(_p(q), _p(k_pages), _p(v_pages), _p(k_scales), _p(v_scales), _p(page_table), _p(lens),
+                                     _p(o), _p(lse), B, most, pages, P, width, n, Hq, Hkv, Dh, T, float(softmax_scale),
+                                     int(mode), int(window), _p(workspace), workspace.numel(), _p(dev_status), st),
+           "sfa_decode_paged_q8")
+    return o
+
+
+def hd_pages_copy_q8(k_pages, v_pages, k_scales, v_scales, copies, dev_status=None, stream=None):
+    """hd_pages_copy for an 8-bit cache: codes and scales of page copies[i][0] onto page copies[i][1] in both pools."""
+    if k_pages.dim() != 4 or k_scales.dim() != 3 or k_pages.shape[0] < 1:
+        raise ValueError("k_pages must be [num_pages][Hkv][page_tokens*n][Dh] and k_scales [num_pages][Hkv][blocks]")
+    pages, Hkv = k_pages.shape[:2]
+    scales = (pages, Hkv, k_scales.shape[2])
+    st = _tensors(stream, ("k_pages", k_pages, _F8, k_pages.shape), ("v_pages", v_pages, _F8, k_pages.shape),
+                  ("k_scales", k_scales, torch.uint8, scales), ("v_scales", v_scales, torch.uint8, scales),
+                  ("copies", copies, _I32, (copies.numel() // 2, 2)), _dev_status(dev_status))
+    _check(lib().hd_pages_copy_q8(_p(k_pages), _p(v_pages), _p(k_scales), _p(v_scales), _p(copies), copies.shape[0], pages,
+                                  k_pages.numel() // pages, Hkv * k_scales.shape[2], _p(dev_status), st),
+           "hd_pages_copy_q8")
 
 
 SFA_BWD_NOALLOC_MAX_BYTES = 64 << 20

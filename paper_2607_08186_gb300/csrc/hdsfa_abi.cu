@@ -33,6 +33,22 @@ cudaError_t launch_kv_append_paged(const void* kn, const void* vn, void* kp, voi
                                    const int32_t* lens, const int32_t* offsets, const int32_t* served, int B, int N,
                                    int num_pages, int P, int max_pages, int n, int Hkv, int Dh, int32_t* status,
                                    cudaStream_t st);
+cudaError_t launch_kv_append_paged_q8(const void* kn, const void* vn, void* kc, void* vc, uint8_t* ks, uint8_t* vs,
+                                      const int32_t* table, const int32_t* lens, const int32_t* offsets,
+                                      const int32_t* served, int B, int N, int num_pages, int P, int max_pages, int n,
+                                      int Hkv, int Dh, int T, int32_t* status, cudaStream_t st);
+cudaError_t launch_kv_read_paged_q8(const void* kc, const void* vc, const uint8_t* ks, const uint8_t* vs,
+                                    const int32_t* table, const int32_t* lens, const int32_t* offsets, void* k, void* v,
+                                    int B, int N, int num_pages, int P, int max_pages, int n, int Hkv, int Dh, int T,
+                                    int32_t* status, cudaStream_t st);
+size_t decode_paged_q8_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window);
+cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void* vc, const uint8_t* ks, const uint8_t* vs,
+                                       const int32_t* table, const int32_t* lens, void* o, float* lse, int B, int maxT,
+                                       int num_pages, int P, int max_pages, int n, int Hq, int Hkv, int Dh, int T,
+                                       float scale, int mode, int window, void* ws, size_t ws_bytes, int32_t* status,
+                                       cudaStream_t st);
+cudaError_t launch_pages_copy_q8(void* kc, void* vc, uint8_t* ks, uint8_t* vs, const int32_t* copies, int F,
+                                 int num_pages, size_t page_bytes, int page_scales, int32_t* status, cudaStream_t st);
 size_t pages_ws_bytes(int B, int num_pages);
 cudaError_t launch_pages_grow(int32_t* refs, int32_t* table, int32_t* lens, const int32_t* add, int32_t* served, int B,
                               int max_pages, int num_pages, int P, void* ws, int32_t* status, cudaStream_t st);
@@ -588,6 +604,112 @@ hd_status_t sfa_decode_paged(const void* q, const void* k_pages, const void* v_p
       q, k_pages, v_pages, page_table, lens, o, lse, B, max_tokens, num_pages, page_tokens, max_pages, n, Hq, Hkv, Dh,
       resolve_scale(softmax_scale, Dh), (int)mode, cut_window(mode, window, (long long)max_tokens * n), workspace,
       workspace_bytes, dev_status, stream));
+}
+
+// ---- paged cache in 8 bits ----
+static hd_status_t q8_sizes(int B, int max_pages, int num_pages, int P, int n, int Hkv, int Dh, int T) {
+  if (Hkv <= 0 || Dh <= 0 || Dh % 16 != 0 || T <= 0) return HD_ERR_INVALID_ARG;
+  hd_status_t st = page_sizes(B, max_pages, num_pages, P, n);
+  if (st != HD_OK) return st;
+  if (P % T != 0) return HD_ERR_INVALID_ARG;
+  if ((long long)Hkv * Dh > (1LL << 24) || (long long)n * Hkv * Dh > (1LL << 24) || (long long)T * n * Dh > (1LL << 30) ||
+      Hkv > 32767 || (long long)num_pages * P * n >= (1LL << 32) / Hkv)
+    return HD_ERR_UNSUPPORTED;
+  return HD_OK;
+}
+
+hd_status_t sfa_kv_append_paged_q8(const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                                   uint8_t* k_scales, uint8_t* v_scales, const int32_t* page_table, const int32_t* lens,
+                                   const int32_t* offsets, const int32_t* served, int B, int N, int num_pages,
+                                   int page_tokens, int max_pages, int n, int Hkv, int Dh, int block_tokens,
+                                   int32_t* dev_status, cudaStream_t stream) {
+  HD_NVTX_RANGE("sfa_kv_append_paged_q8");
+  if (!aligned16(k_pages) || !aligned16(v_pages) || k_scales == nullptr || v_scales == nullptr) return HD_ERR_INVALID_ARG;
+  if (!aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_or_null(offsets, 4) || !aligned_or_null(served, 4) ||
+      !aligned_or_null(dev_status, 4))
+    return HD_ERR_INVALID_ARG;
+  if (N < 0 || (offsets == nullptr && N != B)) return HD_ERR_INVALID_ARG;
+  hd_status_t st = q8_sizes(B, max_pages, num_pages, page_tokens, n, Hkv, Dh, block_tokens);
+  if (st != HD_OK) return st;
+  if ((long long)N * n >= (1LL << 31)) return HD_ERR_UNSUPPORTED;
+  if (N == 0) return HD_OK;
+  if (!aligned16(k_new) || !aligned16(v_new)) return HD_ERR_INVALID_ARG;
+  return cuda_status(hdsfa::launch_kv_append_paged_q8(k_new, v_new, k_pages, v_pages, k_scales, v_scales, page_table, lens,
+                                                      offsets, served, B, N, num_pages, page_tokens, max_pages, n, Hkv, Dh,
+                                                      block_tokens, dev_status, stream));
+}
+
+hd_status_t sfa_kv_read_paged_q8(const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+                                 const uint8_t* v_scales, const int32_t* page_table, const int32_t* lens,
+                                 const int32_t* offsets, void* k, void* v, int B, int N, int num_pages, int page_tokens,
+                                 int max_pages, int n, int Hkv, int Dh, int block_tokens, int32_t* dev_status,
+                                 cudaStream_t stream) {
+  HD_NVTX_RANGE("sfa_kv_read_paged_q8");
+  if (!aligned16(k_pages) || !aligned16(v_pages) || k_scales == nullptr || v_scales == nullptr) return HD_ERR_INVALID_ARG;
+  if (!aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_to(offsets, 4) || !aligned_or_null(dev_status, 4))
+    return HD_ERR_INVALID_ARG;
+  if (N < 0) return HD_ERR_INVALID_ARG;
+  hd_status_t st = q8_sizes(B, max_pages, num_pages, page_tokens, n, Hkv, Dh, block_tokens);
+  if (st != HD_OK) return st;
+  if ((long long)N * n >= (1LL << 31)) return HD_ERR_UNSUPPORTED;
+  if (N == 0) return HD_OK;
+  if (!aligned16(k) || !aligned16(v)) return HD_ERR_INVALID_ARG;
+  return cuda_status(hdsfa::launch_kv_read_paged_q8(k_pages, v_pages, k_scales, v_scales, page_table, lens, offsets, k, v, B,
+                                                    N, num_pages, page_tokens, max_pages, n, Hkv, Dh, block_tokens,
+                                                    dev_status, stream));
+}
+
+static hd_status_t decode_q8_sizes(int B, int maxT, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode, int window) {
+  hd_status_t st = decode_paged_sizes(B, maxT, n, Hq, Hkv, Dh, mode, window);
+  if (st != HD_OK) return st;
+  const long long groups = ((long long)n * (Hq / Hkv) + 63) / 64;
+  return B * Hkv * groups > (1LL << 30) ? HD_ERR_UNSUPPORTED : HD_OK;  // CTAs of one split
+}
+
+size_t sfa_decode_paged_q8_workspace_bytes(int B, int max_tokens, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode,
+                                           int window) {
+  if (decode_q8_sizes(B, max_tokens, n, Hq, Hkv, Dh, mode, window) != HD_OK) return 0;
+  return hdsfa::decode_paged_q8_ws_bytes(B, max_tokens, n, Hq, Hkv, Dh, mode,
+                                         cut_window(mode, window, (long long)max_tokens * n));
+}
+
+hd_status_t sfa_decode_paged_q8(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scales,
+                                const uint8_t* v_scales, const int32_t* page_table, const int32_t* lens, void* o,
+                                float* lse, int B, int max_tokens, int num_pages, int page_tokens, int max_pages, int n,
+                                int Hq, int Hkv, int Dh, int block_tokens, float softmax_scale, sfa_mode_t mode,
+                                int window, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                                cudaStream_t stream) {
+  HD_NVTX_RANGE("sfa_decode_paged_q8");
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o) || k_scales == nullptr ||
+      v_scales == nullptr)
+    return HD_ERR_INVALID_ARG;
+  if (!aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_or_null(lse, 4) || !aligned_or_null(dev_status, 4))
+    return HD_ERR_INVALID_ARG;
+  hd_status_t st = decode_q8_sizes(B, max_tokens, n, Hq, Hkv, Dh, mode, window);
+  if (st != HD_OK || (st = q8_sizes(B, max_pages, num_pages, page_tokens, n, Hkv, Dh, block_tokens)) != HD_OK) return st;
+  if (max_tokens > max_pages * page_tokens) return HD_ERR_INVALID_ARG;
+  const int w = cut_window(mode, window, (long long)max_tokens * n);
+  const size_t need = hdsfa::decode_paged_q8_ws_bytes(B, max_tokens, n, Hq, Hkv, Dh, mode, w);
+  if (!aligned16(workspace) || workspace_bytes < need) return HD_ERR_WORKSPACE;
+  return cuda_status(hdsfa::launch_sfa_decode_paged_q8(
+      q, k_pages, v_pages, k_scales, v_scales, page_table, lens, o, lse, B, max_tokens, num_pages, page_tokens, max_pages, n,
+      Hq, Hkv, Dh, block_tokens, resolve_scale(softmax_scale, Dh), (int)mode, w, workspace, workspace_bytes, dev_status,
+      stream));
+}
+
+hd_status_t hd_pages_copy_q8(void* k_pages, void* v_pages, uint8_t* k_scales, uint8_t* v_scales, const int32_t* copies,
+                             int F, int num_pages, size_t page_bytes, size_t page_scales, int32_t* dev_status,
+                             cudaStream_t stream) {
+  HD_NVTX_RANGE("hd_pages_copy_q8");
+  if (!aligned16(k_pages) || !aligned16(v_pages) || k_scales == nullptr || v_scales == nullptr ||
+      !aligned_or_null(dev_status, 4))
+    return HD_ERR_INVALID_ARG;
+  if (F < 0 || num_pages <= 0 || page_bytes == 0 || page_bytes % 16 != 0 || page_scales == 0) return HD_ERR_INVALID_ARG;
+  if (page_bytes > (size_t)1 << 34 || page_scales > (size_t)1 << 30) return HD_ERR_UNSUPPORTED;
+  if (F == 0) return HD_OK;
+  if (!aligned_to(copies, 8)) return HD_ERR_INVALID_ARG;
+  return cuda_status(hdsfa::launch_pages_copy_q8(k_pages, v_pages, k_scales, v_scales, copies, F, num_pages, page_bytes,
+                                                 (int)page_scales, dev_status, stream));
 }
 
 // ---- who holds which page ----

@@ -1,0 +1,757 @@
+// Decoding over the 8-bit paged cache: softmax(q k^T) v over e4m3 codes with a power of two for each block of tokens
+// and head (q8.cuh).
+//
+// The mathematics.  With K = 2^ek ck and V = 2^ev cv per position, a row's result is
+//   o = sum_p 2^(s_p) 2^(ev_p) cv_p / sum_p 2^(s_p),   s_p = c (q . ck_p) 2^(ek_p)   (c: scale * log2 e).
+// The codes go into the products as they are (e4m3 -> f16 is exact), ek multiplies a score, and ev is added to its
+// exponent: with x_p = s_p + ev_p and m the running maximum of x (not of s), P_p = 2^(x_p - m + 15) is at most 2^15, f16
+// holds it to 2^-12 down to 2^-29 of the largest contribution (2^-40 as a subnormal), and
+//   o = sum P_p cv_p / sum P_p 2^(-ev_p):
+// the sum's terms are one fused multiply-add each.  As e lies in [-64, 50], no term that counts leaves fp32's range.  The
+// queries are scaled by a power of two for each row, so that f16 holds them as bf16 did (a row's largest to 2^15; values
+// 2^-39 below it lose bits).
+//
+// Bound by memory: half the bytes of the bf16 step, so each byte brings twice the products.  A warp takes 16 query
+// rows and 32 of a tile's positions; the warps of the row tiles share the tile in shared memory, so up to 64 rows of a
+// K/V head's group read the cache once.  Tiles stream through a ring: by TMA, in pieces that lie within a page, the
+// warps taking turns at bringing them; pieces of fewer than kTmaRows rows by cp.async.  mma.sync m16n8k16 (f16): a
+// thread's four bytes of an ldmatrix row are k = 2t, 2t + 1, 2t + 8, 2t + 9 of the product, so q lies in that order; V's
+// transposed loads bring pairs of head-dim columns for two keys, so even and odd columns are products of their own.
+#include <float.h>
+
+#include <algorithm>
+
+#include "decode.cuh"
+#include "decode_plan.cuh"
+#include "q8.cuh"
+#include "tc_common.cuh"
+
+namespace hdsfa {
+namespace decq8 {
+using dec::DecodeArgs;
+using dec::kBadPage;
+
+constexpr int kTmaRows = 8;
+constexpr int kWarpKeys = 32;        // positions of a tile that a warp takes
+constexpr float kShift = 15.f;       // P's largest exponent
+constexpr int kMaxRows = 64;         // query rows of a CTA at most (four row tiles)
+constexpr uint32_t kNoRow = 0xffffffffu;
+
+template <int DH>
+constexpr int dsplit() { return DH == 256 ? 2 : 1; }  // head-dim parts: a warp's O must fit its registers
+template <int DH>
+constexpr int key_warps() { return 4 / dsplit<DH>(); }
+template <int DH>
+constexpr int ktile() { return kWarpKeys * key_warps<DH>(); }
+
+struct Args : DecodeArgs {
+  const uint8_t *kcodes, *vcodes, *kscale, *vscale;
+  int blocks;       // blocks of a page
+  FastDiv d_brow;   // rows of a block
+  int mt;           // row tiles of a CTA
+};
+struct Params {
+  CUtensorMap tm_k, tm_v;
+  Args a;
+};
+
+// Two CTAs an SM while their queries leave room for three stages each: up to two row tiles, one at head dim 256.  WIDE:
+// more row tiles, one CTA an SM.
+template <int DH, bool WIDE>
+struct Cfg {
+  static constexpr int KT = ktile<DH>(), MT = WIDE ? 4 : DH == 256 ? 1 : 2, STAGES = !WIDE ? 3 : DH == 256 ? 5 : 6;
+  static constexpr int kThreads = MT * 4 * 32;
+};
+
+template <int DH, bool WIDE, bool TMA>
+struct Smem {
+  using C = Cfg<DH, WIDE>;
+  uint8_t k[C::STAGES][C::KT * DH];
+  uint8_t v[C::STAGES][C::KT * DH];
+  __half q[C::MT * 16 * DH];
+  float4 scale[C::MT * 4][kWarpKeys];   // a warp's keys: 2^ek, ev, 2^-ev
+  float qscale[C::MT * 16];
+  uint32_t row[TMA ? 1 : 4][C::KT];     // cp.async: rows of the pool (kNoRow: none) of four tiles
+  uint64_t full[C::STAGES], empty[C::STAGES];
+  unsigned not_finite[2];               // a bit for each row of the merged partial
+  int bad_page, abort;
+};
+
+// Byte offset of 16-byte chunk `c` of a row of a tile: blocks of [KT][128 bytes] with the 128-byte swizzle that TMA
+// writes, at head dim 64 [KT][64] with the 64-byte one; conflict-free for ldmatrix.
+template <int DH, int KT>
+HD_DEVINLINE int chunk_at(int row, int c) {
+  if (DH == 64) return row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+  return (c >> 3) * (KT * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+}
+
+HD_DEVINLINE void mma_f16_16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+HD_DEVINLINE uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Row of position p >= 0 of K/V head g in the pools (of Dh codes each; below 2^32, checked on the host), kNoRow where
+// the table names no page; and its block's scale.
+HD_DEVINLINE uint32_t row_at(const Args& a, const int32_t* table, int g, int p, size_t* scale) {
+  const int i = fast_div(p, a.pg.d_prow);
+  if (i >= a.pg.max_pages) return kNoRow;
+  const int id = table[i];
+  if ((unsigned)id >= (unsigned)a.pg.num_pages) return kNoRow;
+  const int off = p - i * a.pg.prow;
+  const size_t ph = (size_t)id * a.Hkv + g;
+  if (scale != nullptr) *scale = ph * a.blocks + fast_div(off, a.d_brow);
+  return (uint32_t)(ph * a.pg.prow + off);
+}
+
+// A row's partial over the visible positions of [k0, k1), by one warp on the fp32 units: lane i holds DH/32 columns.
+// Only visible rows are read: what a hidden NaN has made of the products' row is not.
+template <int DH>
+__device__ __noinline__ void exact_row(const Args& a, int b, int g, int r, int T, int k0, int k1, float* po, float2* pml) {
+  constexpr int C = DH / 32;
+  const int lane = threadIdx.x & 31, s = r / a.G, h = g * a.G + r % a.G, pq = (T - 1) * a.n + s;
+  const int32_t* table = a.table + (long long)b * a.pg.max_pages;
+  int p = a.mode == SFA_LOCAL ? max(k0, pq - a.window + 1) : k0, step = 1;
+  if (a.mode == SFA_WITHIN) {
+    step = a.n;
+    p += (s + a.n - p % a.n) % a.n;
+  }
+  const int end = min(k1, pq + 1);
+  const bf16* q = a.q + (((long long)b * a.n + s) * a.Hq + h) * DH + lane * C;
+  float qf[C], o[C], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) qf[c] = __bfloat162float(q[c]), o[c] = 0.f;
+  for (; p < end; p += step) {
+    size_t sc = 0;
+    const uint32_t row = row_at(a, table, g, p, &sc);
+    if (row == kNoRow) continue;
+    const size_t at = (size_t)row * DH;
+    float x = 0.f, v[C];
+#pragma unroll
+    for (int c = 0; c < C; c += 2) {
+      const float2 kv = q8::values2(*reinterpret_cast<const uint16_t*>(a.kcodes + at + lane * C + c));
+      const float2 vv = q8::values2(*reinterpret_cast<const uint16_t*>(a.vcodes + at + lane * C + c));
+      x += qf[c] * kv.x + qf[c + 1] * kv.y;
+      v[c] = vv.x, v[c + 1] = vv.y;
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    x *= a.scale_log2 * q8::scale_of(q8::clamp_byte(a.kscale[sc]));
+    const float fv = q8::scale_of(q8::clamp_byte(a.vscale[sc]));
+    const float mn = fmaxf(m, x), mu = mn == -INFINITY ? 0.f : mn, corr = exp2f(m - mu), w = exp2f(x - mu);
+    m = mn;
+    l = l * corr + w;
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = o[c] * corr + w * (v[c] * fv);
+  }
+  if (l != l) m = INFINITY;
+#pragma unroll
+  for (int c = 0; c < C; ++c) po[lane * C + c] = o[c];
+  if (lane == 0) *pml = make_float2(m, l);
+}
+
+// A finished row by one warp: o / l and its LSE, or an empty row (l = 0).
+template <int DH>
+HD_DEVINLINE void store_row(const Args& a, int b, int g, int r, const float* o, float m, float l) {
+  const int lane = threadIdx.x & 31, s = fast_div(r, a.d_G), h = g * a.G + r - s * a.G;
+  const bool some = l != 0.f;
+  const float inv = some ? 1.f / l : 0.f;
+  bf16* to = a.o + (((long long)b * a.n + s) * a.Hq + h) * DH;
+  for (int i = lane; i < DH / 4; i += 32) {
+    uint2 w = make_uint2(0, 0);
+    if (some) {
+      const float4 x = *reinterpret_cast<const float4*>(o + i * 4);
+      w = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
+    }
+    *reinterpret_cast<uint2*>(to + i * 4) = w;
+  }
+  if (lane == 0 && a.lse != nullptr)
+    a.lse[((long long)b * a.Hq + h) * a.n + s] = some ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+template <int DH, bool WIDE, bool TMA>
+__global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_q8_kernel(const __grid_constant__ Params P) {
+  using C = Cfg<DH, WIDE>;
+  using Sm = Smem<DH, WIDE, TMA>;
+  constexpr int KT = C::KT, STAGES = C::STAGES, AHEAD = STAGES - 1;
+  constexpr int KW = key_warps<DH>(), DC = DH / dsplit<DH>(), CPR = DH / 16;  // DC: O columns of a warp
+  constexpr int RB = DH < 128 ? DH : 128;                                     // bytes of a row in a block of the tile
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const Args& a = P.a;
+  {
+    uint32_t dyn;
+    asm("mov.u32 %0, %%dynamic_smem_size;\n" : "=r"(dyn));
+    const uint32_t pad = (1024 - (smem_u32(smem_raw) & 1023)) & 1023;
+    if (pad + sizeof(Sm) > dyn) {  // uniform: nothing touched yet
+      if (threadIdx.x == 0) set_status(a.status, HD_DEVBIT_TIMEOUT);
+      return;
+    }
+  }
+  Sm& sm = *reinterpret_cast<Sm*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int split = fast_div((int)blockIdx.x, a.d_heads), head = (int)blockIdx.x - split * a.Hkv * a.ngroups;
+  const int g = a.ngroups == 1 ? head : head / a.ngroups, rg = a.ngroups == 1 ? 0 : head % a.ngroups;
+  const int tid = threadIdx.x, nt = blockDim.x, W = nt >> 5, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, t4 = lane & 3;
+  // this warp's row tile, key group and head-dim part
+  const int mt = warp >> 2, kw = (warp & 3) % KW, dw = (warp & 3) / KW;
+  const int R = a.rg;  // rows of the CTA
+  const size_t pidx = blockIdx.x;
+  float* po = a.part_o + pidx * R * DH;
+  float2* pml = a.part_ml + pidx * R;
+  const int tile = a.tile;
+  if (TMA && tid == 32) {
+    tma_prefetch(&P.tm_k);
+    tma_prefetch(&P.tm_v);
+  }
+  if (tid == 0) {
+    sm.bad_page = sm.abort = 0;
+    sm.not_finite[0] = sm.not_finite[1] = 0;
+    if (TMA) {
+      for (int i = 0; i < STAGES; ++i) {
+        mbar_init(&sm.full[i], 1);
+        mbar_init(&sm.empty[i], W);  // one arrival per warp
+      }
+      fence_mbar_init();
+    }
+  }
+  // rows that no piece fills: their P is zero, and their V must not be NaN
+  if (TMA && tile < KT)
+    for (int i = tid; i < STAGES * (KT - tile) * CPR; i += nt) {
+      const int st = i / ((KT - tile) * CPR), e = i % ((KT - tile) * CPR);
+      *reinterpret_cast<uint4*>(sm.v[st] + chunk_at<DH, KT>(tile + e / CPR, e % CPR)) = make_uint4(0, 0, 0, 0);
+    }
+  // this thread's query rows g4 and g4 + 8 of the row tile: their streams (-1: padding).  Where n divides a tile, which
+  // of this thread's keys are of a row's stream is the same in every tile.
+  int rs_[2];
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf) {
+    const int r = rg * R + mt * 16 + g4 + 8 * hf;
+    rs_[hf] = r < a.M ? fast_div(r, a.d_G) : -1;
+  }
+  const bool streams = a.mode == SFA_WITHIN && a.n > 1;
+  const bool shifting = streams && tile - fast_div(tile, a.d_n) * a.n != 0;
+  uint32_t mine = 0;  // bit hf*8 + j*2 + e: the row may see key j*8 + 2*t4 + e
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int key = kw * kWarpKeys + (i >> 1) * 8 + 2 * t4 + (i & 1);
+    const int ks = streams && !shifting ? key - fast_div(key, a.d_n) * a.n : -1;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+      if (rs_[hf] >= 0 && key < tile && (ks < 0 || ks == rs_[hf])) mine |= 1u << (hf * 8 + i);
+  }
+  grid_dep_wait();
+  grid_dep_launch();
+  const int b = fast_div(split, a.d_nsplit), T = a.lens[b];
+  const int32_t* table = a.table + (long long)b * a.pg.max_pages;
+  int k0, k1;
+  dec::split_range<true>(a, T, split - b * a.nsplit, tile, k0, k1);
+  if (k0 >= k1) {  // nothing of this sequence in this split: an empty partial, or an empty result
+    if (a.nsplit > 1) {
+      for (int i = tid; i < R; i += nt) pml[i] = make_float2(-INFINITY, 0.f);
+    } else {
+      if (T != 0 && g == 0 && rg == 0 && tid == 0) set_status(a.status, HD_DEVBIT_INDEX);
+      for (int row = warp; row < min(R, a.M - rg * R); row += W) store_row<DH>(a, b, g, rg * R + row, nullptr, -INFINITY, 0.f);
+    }
+    return;
+  }
+  const int nsub = fast_div(k1 - k0 + tile - 1, a.d_tile);
+  __syncthreads();  // the barriers and flags are set
+
+  // ---- the tiles' loads
+  const int seen = a.mode == SFA_LOCAL ? (T - 1) * a.n - a.window + 1 : 0;  // first position any row sees
+  // TMA: tile t is brought by warp (t - AHEAD) mod W; lane i brings piece i, whose page entry it has looked up when the
+  // warp brought its last tile
+  auto pos_of = [&](int t) {  // first position of this lane's piece of a tile, -1: none that a row sees
+    const int p = lane * a.piece, pos = k0 + t * tile + p;
+    return p >= tile || pos >= k1 || pos + a.piece <= seen ? -1 : pos;
+  };
+  int entry = 0;
+  auto fetch = [&](int t) {
+    const int pos = t < nsub ? pos_of(t) : -1;
+    if (pos >= 0) {
+      const int i = fast_div(pos, a.pg.d_prow);
+      entry = i < a.pg.max_pages ? table[i] : -1;
+    }
+  };
+  // cp.async: the pools' row of this thread's position of a tile
+  auto row_of = [&](int it) {
+    const int p = k0 + it * tile + tid;
+    if (tid >= tile || p >= k1 || p < seen) return kNoRow;
+    const uint32_t row = row_at(a, table, g, p, nullptr);
+    if (row == kNoRow) sm.bad_page = 1;
+    return row;
+  };
+  [[maybe_unused]] int brought = -1;  // TMA: the last tile that this warp brought
+  auto load_tile = [&](int it) {
+    const int st = it % STAGES;
+    if constexpr (TMA) {
+      brought = it;
+      if (lane == 0) mbar_arrive_expect_tx(&sm.full[st], tile * DH * 2);
+      __syncwarp();
+      if (lane * a.piece < tile) {
+        const int pos = pos_of(it);
+        int page = a.pg.num_pages, off = 0;  // behind the pool: zeros
+        if (pos >= 0) {
+          if ((unsigned)entry < (unsigned)a.pg.num_pages) {
+            page = entry;
+            off = pos - fast_div(pos, a.pg.d_prow) * a.pg.prow;
+          } else {
+            sm.bad_page = 1;
+          }
+        }
+#pragma unroll
+        for (int cb = 0; cb < DH / RB; ++cb) {
+          const int at = cb * KT * RB + lane * a.piece * RB;
+          tma_load_4d(sm.k[st] + at, &P.tm_k, &sm.full[st], cb * RB, off, g, page);
+          tma_load_4d(sm.v[st] + at, &P.tm_v, &sm.full[st], cb * RB, off, g, page);
+        }
+      }
+      __syncwarp();
+      fetch(it + W);
+    } else {
+      for (int i = tid; i < KT * CPR; i += nt) {
+        const int rr = i / CPR, cc = i % CPR;
+        const uint32_t row = rr < tile ? sm.row[it & 3][rr] : kNoRow;
+        const size_t off = (row == kNoRow ? 0 : (size_t)row * DH) + cc * 16;
+        cp_async_16(smem_u32(sm.k[st] + chunk_at<DH, KT>(rr, cc)), a.kcodes + off, row != kNoRow);
+        cp_async_16(smem_u32(sm.v[st] + chunk_at<DH, KT>(rr, cc)), a.vcodes + off, row != kNoRow);
+      }
+    }
+  };
+  // The scales of this warp's keys, a lane's key each: the page entry two tiles ahead, the bytes one tile ahead.
+  const int my_key = kw * kWarpKeys + lane;
+  auto scale_pos = [&](int it) {
+    const int p = k0 + it * tile + my_key;
+    return it < nsub && my_key < tile && p < k1 && p >= seen ? p : -1;
+  };
+  auto scale_entry = [&](int it) {
+    const int p = scale_pos(it);
+    if (p < 0) return -1;
+    const int i = fast_div(p, a.pg.d_prow);
+    return i < a.pg.max_pages ? table[i] : -1;
+  };
+  auto scale_bytes = [&](int it, int id, int& kb, int& vb) {
+    kb = vb = 127;
+    const int p = scale_pos(it);
+    if (p < 0 || (unsigned)id >= (unsigned)a.pg.num_pages) return;
+    const int off = p - fast_div(p, a.pg.d_prow) * a.pg.prow;
+    const size_t at = ((size_t)id * a.Hkv + g) * a.blocks + fast_div(off, a.d_brow);
+    kb = a.kscale[at];
+    vb = a.vscale[at];
+  };
+  if constexpr (TMA) {
+    const int t = (warp + AHEAD) % W;  // this warp's first tile
+    fetch(t);
+    if (t < min(AHEAD, nsub)) load_tile(t);
+  } else {
+    const uint32_t r0 = row_of(0), r1 = row_of(1), r2 = row_of(2);
+    if (tid < tile) sm.row[0][tid] = r0, sm.row[1][tid] = r1, sm.row[2][tid] = r2;
+    __syncthreads();
+    load_tile(0);
+    cp_async_commit();
+    if (nsub > 1) load_tile(1);
+    cp_async_commit();
+  }
+  int kb, vb, next_entry;
+  scale_bytes(0, scale_entry(0), kb, vb);
+  next_entry = scale_entry(1);
+  // The queries: a warp per row scales its row by a power of two, rounds it to f16 and lays it out in the products'
+  // order: value 16i + 4t + j at column 16i + 2t + j (j < 2) or 16i + 6 + 2t + j.
+  for (int rr = warp; rr < R; rr += W) {
+    constexpr int NP = DH / 64;  // pairs of a lane
+    const int r = rg * R + rr;
+    uint32_t w[NP];
+    uint32_t most = 0;
+    if (r < a.M) {
+      const int s = fast_div(r, a.d_G), h = g * a.G + r - s * a.G;
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (((long long)b * a.n + s) * a.Hq + h) * DH) + lane * NP;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) w[i] = src[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) w[i] = 0;
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) most = max(most, max(w[i] << 16 & 0x7fff0000u, w[i] & 0x7fff0000u));
+    most = __reduce_max_sync(0xffffffffu, most);
+    // the exponent field of the largest magnitude, kept where both powers are normal
+    const int e = min(max((int)(most >> 23), 20), 254);
+    const float to = __int_as_float(min(127 + 14 + 127 - e, 254) << 23);  // 2^(14 - (e - 127)), at most 2^127
+    const float back = __int_as_float(max(e - 14, 1) << 23);              // 2^(e - 127 - 14)
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int p = lane * NP + i, kk = p >> 3, t = (p >> 1) & 3, hi = p & 1;
+      *reinterpret_cast<uint32_t*>(sm.q + swz<DH>(rr, kk * 16 + hi * 8 + 2 * t)) =
+          pack_f16(__uint_as_float(w[i] << 16) * to, __uint_as_float(w[i] & 0xffff0000u) * to);
+    }
+    if (lane == 0) sm.qscale[rr] = back * a.scale_log2;
+  }
+  __syncthreads();
+
+  const float rowf[2] = {sm.qscale[mt * 16 + g4], sm.qscale[mt * 16 + g4 + 8]};
+  const int own_lo = (T - 1) * a.n, win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;
+  float mx[2] = {-INFINITY, -INFINITY}, ls[2] = {0.f, 0.f}, oacc[DC / 8][4];
+#pragma unroll
+  for (int i = 0; i < DC / 8; ++i) oacc[i][0] = oacc[i][1] = oacc[i][2] = oacc[i][3] = 0.f;
+
+  bool alive = true;
+  for (int it = 0; it < nsub; ++it) {
+    const int st = it % STAGES, base = k0 + it * tile;
+    [[maybe_unused]] uint32_t next_row = kNoRow;
+    // this tile's scales into shared memory, the next ones' loads on their way
+    {
+      kb = q8::clamp_byte(kb);
+      vb = q8::clamp_byte(vb);
+      sm.scale[warp][lane] = make_float4(q8::scale_of(kb), (float)(vb - 127), q8::inverse_of(vb), 0.f);
+      const int id = next_entry;
+      next_entry = scale_entry(it + 2);
+      scale_bytes(it + 1, id, kb, vb);
+    }
+    if constexpr (TMA) {
+      // the warps meet on the stages' barriers alone: one that loads does not hold up the others
+      if (it % W == warp && it + AHEAD < nsub) {
+        const int t = it + AHEAD;
+        if (t >= STAGES)
+          alive = __all_sync(0xffffffffu, mbar_wait(&sm.empty[t % STAGES], (t / STAGES - 1) & 1, &sm.abort, a.status));
+        if (alive) load_tile(t);
+      }
+      alive = alive && __all_sync(0xffffffffu, mbar_wait(&sm.full[st], (it / STAGES) & 1, &sm.abort, a.status));
+      if (!alive) break;
+      if (base + tile > k1) {  // cached rows behind the sequence's length may never have been written
+        const int r0 = max(kw * kWarpKeys, k1 - base), r1 = min((kw + 1) * kWarpKeys, tile);
+        for (int i = r0 * CPR + lane; i < r1 * CPR; i += 32)
+          *reinterpret_cast<uint4*>(sm.v[st] + chunk_at<DH, KT>(i / CPR, i % CPR)) = make_uint4(0, 0, 0, 0);
+      }
+      __syncwarp();
+    } else {
+      cp_async_wait<1>();  // stage `it` has landed
+      __syncthreads();     // ... for every thread, and stage it-1 is no longer read
+      if (it + 2 < nsub) load_tile(it + 2);
+      cp_async_commit();
+      next_row = row_of(it + 3);  // the rows that the next iteration loads by
+    }
+    const uint8_t *cK = sm.k[st], *cV = sm.v[st];
+
+    // S = q ck^T: key tile j of 8 keys
+    float sacc[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sacc[j][0] = sacc[j][1] = sacc[j][2] = sacc[j][3] = 0.f;
+#pragma unroll
+    for (int kq = 0; kq < DH / 64; ++kq) {
+      uint32_t qa[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        ldsm_x4(smem_u32(sm.q + swz<DH>(mt * 16 + (lane & 15), (kq * 4 + i) * 16 + (lane >> 4) * 8)), qa[i][0], qa[i][1],
+                qa[i][2], qa[i][3]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t c[4];
+        ldsm_x4(smem_u32(cK + chunk_at<DH, KT>(kw * kWarpKeys + j * 8 + (lane & 7), kq * 4 + (lane >> 3))), c[0], c[1], c[2],
+                c[3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          mma_f16_16816(sacc[j], qa[i], q8::f16x2_of((uint16_t)c[i]), q8::f16x2_of((uint16_t)(c[i] >> 16)));
+      }
+    }
+    // x = s + ev, the mask, and the online softmax in log2 units
+    uint32_t vis = mine;
+    const int kp = base + kw * kWarpKeys + 2 * t4;
+    if (base + tile - 1 > own_lo || base + tile > k1 || base <= win_hi || shifting) {
+      // positions at the sequence's end, at the rows' windows, or streams that shift from tile to tile
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int hf = i >> 3, p = kp + ((i >> 1) & 3) * 8 + (i & 1), pq = own_lo + rs_[hf];
+        const bool in = p < k1 && p <= pq && (a.mode != SFA_LOCAL || p > pq - a.window) &&
+                        (!shifting || p - fast_div(p, a.d_n) * a.n == rs_[hf]);
+        if (!in) vis &= ~(1u << i);
+      }
+    }
+    float tmax[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float4 sc = sm.scale[warp][j * 8 + 2 * t4 + e];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const float x = fmaf(sacc[j][hf * 2 + e] * rowf[hf], sc.x, sc.y);
+          sacc[j][hf * 2 + e] = (vis >> (hf * 8 + j * 2 + e)) & 1u ? x : -INFINITY;
+          tmax[hf] = fmaxf(tmax[hf], sacc[j][hf * 2 + e]);
+        }
+      }
+    float corr[2], msub[2];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      tmax[hf] = fmaxf(tmax[hf], __shfl_xor_sync(0xffffffffu, tmax[hf], 1));
+      tmax[hf] = fmaxf(tmax[hf], __shfl_xor_sync(0xffffffffu, tmax[hf], 2));
+      const float mnew = fmaxf(mx[hf], tmax[hf]), mu = mnew == -INFINITY ? 0.f : mnew;
+      corr[hf] = ex2_approx(mx[hf] - mu);
+      msub[hf] = mu - kShift;
+      mx[hf] = mnew;
+      ls[hf] *= corr[hf];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float inv = sm.scale[warp][j * 8 + 2 * t4 + e].z;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const float p = ex2_approx(sacc[j][hf * 2 + e] - msub[hf]);
+          sacc[j][hf * 2 + e] = p;
+          ls[hf] = fmaf(p, inv, ls[hf]);
+        }
+      }
+    if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+      for (int i = 0; i < DC / 8; ++i) {
+        oacc[i][0] *= corr[0];
+        oacc[i][1] *= corr[0];
+        oacc[i][2] *= corr[1];
+        oacc[i][3] *= corr[1];
+      }
+    }
+    // O += P cv over this warp's 32 keys, 16 at a time
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t pa[4] = {pack_f16(sacc[2 * u][0], sacc[2 * u][1]), pack_f16(sacc[2 * u][2], sacc[2 * u][3]),
+                              pack_f16(sacc[2 * u + 1][0], sacc[2 * u + 1][1]), pack_f16(sacc[2 * u + 1][2], sacc[2 * u + 1][3])};
+#pragma unroll
+      for (int c2 = 0; c2 < DC / 32; ++c2) {
+        uint32_t r[4];
+        ldsm_x4_t(smem_u32(cV + chunk_at<DH, KT>(kw * kWarpKeys + u * 16 + (lane & 15), dw * (DC / 16) + c2 * 2 + (lane >> 4))),
+                  r[0], r[1], r[2], r[3]);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const uint32_t lo = __byte_perm(r[2 * c], 0, 0x3120), hi = __byte_perm(r[2 * c + 1], 0, 0x3120);
+          float(*acc)[4] = &oacc[(c2 * 2 + c) * 2];
+          mma_f16_16816(acc[0], pa, q8::f16x2_of((uint16_t)lo), q8::f16x2_of((uint16_t)hi));
+          mma_f16_16816(acc[1], pa, q8::f16x2_of((uint16_t)(lo >> 16)), q8::f16x2_of((uint16_t)(hi >> 16)));
+        }
+      }
+    }
+    if constexpr (TMA) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.empty[st]);
+    } else {
+      __syncwarp();  // this tile's scales are read
+      if (tid < tile) sm.row[(it + 3) & 3][tid] = next_row;
+    }
+  }
+  if constexpr (TMA) {
+    // a wait gave up: the results are invalid.  A warp that goes on has seen every tile land; one that does not
+    // waits (again with a limit) for the last that it brought, whose stage no earlier one can still be filling.
+    if (!alive && brought >= 0 && lane == 0) mbar_drain(&sm.full[brought % STAGES], (brought / STAGES) & 1);
+    if (__syncthreads_or(!alive)) return;
+  } else {
+    cp_async_wait<0>();
+    __syncthreads();
+  }
+
+  // merge the key groups' partials in shared memory (the ring is free now): [KW][R][DH], then the running maxima (in
+  // the partials' units, where P is at most 2^15) and sums
+  static_assert((KW * C::MT * 16 * DH + 2 * KW * C::MT * 16) * 4 <= 2 * STAGES * KT * DH, "merge fits the ring");
+  static_assert(kMaxRows <= 128, "one thread per row");
+  float* sO = reinterpret_cast<float*>(sm.k[0]);
+  float* sM = sO + KW * R * DH;  // [KW][R]
+  float* sL = sM + KW * R;       // [KW][R]
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf) {
+    ls[hf] += __shfl_xor_sync(0xffffffffu, ls[hf], 1);
+    ls[hf] += __shfl_xor_sync(0xffffffffu, ls[hf], 2);
+    const int row = kw * R + mt * 16 + g4 + 8 * hf;
+    if (t4 == 0 && dw == 0) {
+      sM[row] = mx[hf] - kShift;
+      sL[row] = ls[hf];
+    }
+#pragma unroll
+    for (int c = 0; c < DC / 16; ++c)
+      *reinterpret_cast<float4*>(sO + row * DH + dw * DC + c * 16 + 4 * t4) =
+          make_float4(oacc[2 * c][2 * hf], oacc[2 * c + 1][2 * hf], oacc[2 * c][2 * hf + 1], oacc[2 * c + 1][2 * hf + 1]);
+  }
+  __syncthreads();
+  const bool bad = sm.bad_page != 0;
+  if (tid < R) {  // one thread per row: its maximum and sum over the key groups, whose weights replace their maxima
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < KW; ++w) m = fmaxf(m, sM[w * R + tid]);
+    const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      const float f = exp2f(sM[w * R + tid] - mu);
+      l += f * sL[w * R + tid];
+      sM[w * R + tid] = f;
+    }
+    if (l != l) m = INFINITY;  // a visible score that is not finite: the combined row is NaN
+    if (bad) m = -INFINITY, l = kBadPage;
+    pml[tid] = make_float2(m, l);
+    if (a.nsplit == 1 && bad && tid == 0) set_status(a.status, HD_DEVBIT_INDEX);
+  }
+  __syncthreads();
+  for (int idx = tid; idx < R * (DH / 4); idx += nt) {
+    const int row = idx / (DH / 4), c4 = idx % (DH / 4);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      const float f = sM[w * R + row];
+      const float4 v = *reinterpret_cast<const float4*>(sO + (w * R + row) * DH + c4 * 4);
+      o.x += f * v.x;
+      o.y += f * v.y;
+      o.z += f * v.z;
+      o.w += f * v.w;
+    }
+    *reinterpret_cast<float4*>(po + row * DH + c4 * 4) = o;
+    if (!(fabsf(o.x) + fabsf(o.y) + fabsf(o.z) + fabsf(o.w) <= FLT_MAX)) atomicOr(&sm.not_finite[row >> 5], 1u << (row & 31));
+  }
+  __syncthreads();
+  if (!bad)
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+      for (unsigned rows = sm.not_finite[half]; rows; rows &= rows - 1) {
+        const int row = half * 32 + __ffs(rows) - 1;
+        if (row % W == warp && rg * R + row < a.M)
+          exact_row<DH>(a, b, g, rg * R + row, T, k0, k1, po + row * DH, pml + row);
+      }
+  if (a.nsplit > 1) return;
+  // the only split: its rows are the results
+  __syncthreads();
+  for (int row = warp; row < min(R, a.M - rg * R); row += W) {
+    const float2 ml = pml[row];
+    store_row<DH>(a, b, g, rg * R + row, po + row * DH, ml.x, bad ? 0.f : ml.y);
+  }
+}
+}  // namespace decq8
+
+// ------------------------------------------------------------------ host side
+
+namespace {
+struct Q8Plan {
+  int G, M, ngroups, rg, nsplit;
+  size_t part_o_bytes, part_ml_bytes;
+  size_t bytes() const { return ((part_o_bytes + 255) & ~size_t(255)) + part_ml_bytes; }
+};
+}  // namespace
+
+// Positions that a step of maxT tokens reads at most.
+static long long q8_range(int maxT, int n, int mode, int window) {
+  return mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1) : (long long)maxT * n;
+}
+
+// Splits of a step: the fewest waves times (tiles of a CTA + about two tiles' time to start and end it), a combine
+// kernel of about three tiles' time beside more than one split.  At most four waves of CTAs, which bounds the
+// workspace: `bound` gives the most that any smaller maxT or window takes.
+static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, bool bound) {
+  Q8Plan p = {};
+  p.G = Hq / Hkv;
+  p.M = n * p.G;
+  p.ngroups = (p.M + decq8::kMaxRows - 1) / decq8::kMaxRows;
+  const int rows = (p.M + p.ngroups - 1) / p.ngroups;
+  p.rg = (rows + 15) / 16 * 16;
+  const int KT = Dh == 256 ? decq8::ktile<256>() : decq8::ktile<128>();
+  const long long tiles = (q8_range(maxT, n, mode, window) + KT - 1) / KT, ctas = (long long)B * Hkv * p.ngroups;
+  const long long resident = (long long)kSmCount * (p.rg > (Dh == 256 ? 16 : 32) ? 1 : Dh == 64 && p.rg == 16 ? 4 : 2);
+  const long long most = std::min({tiles, (long long)dec::kMaxSplit, std::max(1LL, 4 * resident / ctas)});
+  long long best = 1, best_cost = -1;
+  if (bound) {
+    best = most;
+  } else {
+    for (long long ns = 1; ns <= most; ++ns) {
+      const long long per = (tiles + ns - 1) / ns, used = (tiles + per - 1) / per;
+      if (used != ns) continue;  // another ns gives the same chunks
+      const long long cost = ((ctas * ns + resident - 1) / resident) * (per + 2) + (ns > 1 ? 3 : 0);
+      if (best_cost < 0 || cost < best_cost) {
+        best = ns;
+        best_cost = cost;
+      }
+    }
+  }
+  p.nsplit = (int)best;
+  const size_t parts = (size_t)ctas * best;
+  p.part_o_bytes = parts * p.rg * Dh * sizeof(float);
+  p.part_ml_bytes = parts * p.rg * sizeof(float2);
+  return p;
+}
+
+size_t decode_paged_q8_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {
+  return q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, true).bytes();
+}
+
+template <int DH, bool WIDE, bool TMA>
+static cudaError_t launch_q8_t(const decq8::Params& p, cudaStream_t st) {
+  using namespace decq8;
+  const int smem = (int)sizeof(Smem<DH, WIDE, TMA>) + 1024;
+  static_assert(sizeof(Smem<DH, WIDE, TMA>) + 1024 <= (WIDE ? 227 : 113) * 1024, "an SM's CTAs fit");
+  cudaError_t e = cudaFuncSetAttribute(decode_q8_kernel<DH, WIDE, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(true, decode_q8_kernel<DH, WIDE, TMA>, dim3((unsigned)p.a.nsplit * p.a.B * p.a.Hkv * p.a.ngroups),
+                       (unsigned)p.a.mt * 128, smem, st, p);
+}
+template <int DH>
+static cudaError_t launch_q8_d(const decq8::Params& p, bool tma, cudaStream_t st) {
+  if (p.a.mt > decq8::Cfg<DH, false>::MT) return tma ? launch_q8_t<DH, true, true>(p, st) : launch_q8_t<DH, true, false>(p, st);
+  return tma ? launch_q8_t<DH, false, true>(p, st) : launch_q8_t<DH, false, false>(p, st);
+}
+
+cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void* vc, const uint8_t* ks, const uint8_t* vs,
+                                       const int32_t* table, const int32_t* lens, void* o, float* lse, int B, int maxT,
+                                       int num_pages, int P, int max_pages, int n, int Hq, int Hkv, int Dh, int T,
+                                       float scale, int mode, int window, void* ws, size_t ws_bytes, int32_t* status,
+                                       cudaStream_t st) {
+  const Q8Plan plan = q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, false);
+  if (plan.bytes() > ws_bytes) return cudaErrorInvalidValue;  // the bound says that it is not
+  decq8::Params p = {};
+  decq8::Args& a = p.a;
+  a.q = (const bf16*)q;
+  a.kcodes = (const uint8_t*)kc;
+  a.vcodes = (const uint8_t*)vc;
+  a.kscale = ks;
+  a.vscale = vs;
+  a.blocks = P / T;
+  a.d_brow = make_fast_div((uint32_t)(T * n));
+  a.mt = plan.rg / 16;
+  a.lens = lens;
+  a.o = (bf16*)o;
+  a.lse = lse;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + ((plan.part_o_bytes + 255) & ~size_t(255)));
+  a.status = status;
+  a.B = B;
+  a.maxT = maxT;
+  a.n = n;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = plan.G;
+  a.M = plan.M;
+  a.ngroups = plan.ngroups;
+  a.nsplit = plan.nsplit;
+  a.rg = plan.rg;
+  a.mode = mode;
+  a.window = window;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.d_nsplit = make_fast_div((uint32_t)plan.nsplit);
+  a.table = table;
+  a.pg = make_page_geom(num_pages, max_pages, P * n);
+  a.d_G = make_fast_div((uint32_t)plan.G);
+  a.d_n = make_fast_div((uint32_t)n);
+  a.d_heads = make_fast_div((uint32_t)(Hkv * plan.ngroups));
+  const int KT = Dh == 256 ? decq8::ktile<256>() : decq8::ktile<128>();
+  a.piece = paged_piece(a.pg.prow, KT);
+  // a piece's rows start on 128 bytes of shared memory
+  const bool tma = a.piece >= decq8::kTmaRows && (Dh >= 128 || a.piece % 2 == 0);
+  a.tile = tma ? KT / a.piece * a.piece : n <= KT ? KT / n * n : KT;  // cp.async: whole tokens where a tile holds one
+  a.d_tile = make_fast_div((uint32_t)a.tile);
+  if (tma && (!make_q8_tmap(&p.tm_k, kc, num_pages, Hkv, a.pg.prow, Dh, a.piece) ||
+              !make_q8_tmap(&p.tm_v, vc, num_pages, Hkv, a.pg.prow, Dh, a.piece)))
+    return cudaErrorInvalidValue;
+  const cudaError_t e = Dh == 64    ? launch_q8_d<64>(p, tma, st)
+                        : Dh == 128 ? launch_q8_d<128>(p, tma, st)
+                                    : launch_q8_d<256>(p, tma, st);
+  return e != cudaSuccess || a.nsplit == 1 ? e : launch_combine_paged(a, Dh, st);
+}
+
+}  // namespace hdsfa

@@ -287,6 +287,9 @@ HD_DEVINLINE void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;\
 // {Dh, H, ns, Lv, B} (innermost first): virtual row r of stream s is position
 // r*rs + s.  Box = 64 columns x box_rows rows, 128-byte swizzle.  Defined in tmap.cu.
 bool make_rows_tmap(CUtensorMap* m, const void* base, const SfaGeom& g, int H, int Dh, int box_rows);
+// The pools of an 8-bit paged cache, codes [num_pages][Hkv][prow][Dh]; box = up to 128 codes x `rows` rows of one head
+// and page (see tmap.cu).
+bool make_q8_tmap(CUtensorMap* m, const void* base, int num_pages, int Hkv, int prow, int Dh, int rows);
 
 // ---------------------------------------------------------------- CTA pairs (cta_group::2)
 HD_DEVINLINE void tmem_alloc_pair(uint32_t* dst, uint32_t ncols) {

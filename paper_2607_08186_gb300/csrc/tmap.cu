@@ -50,4 +50,20 @@ bool make_qgroup_tmap(CUtensorMap* m, const void* base, int B, int n, int Hq, in
   return r == CUDA_SUCCESS;
 }
 
+// Tensor map over a pool of e4m3 codes [num_pages][Hkv][prow][Dh] seen as {Dh, prow, Hkv, num_pages}; box = up to 128
+// columns x `rows` rows, whose tile in shared memory is swizzled by 128 bytes, at head dim 64 by 64.
+bool make_q8_tmap(CUtensorMap* m, const void* base, int num_pages, int Hkv, int prow, int Dh, int rows) {
+  auto enc = tmap_encoder();
+  if (enc == nullptr) return false;
+  const cuuint64_t head = (cuuint64_t)prow * Dh;
+  cuuint64_t dims[4] = {(cuuint64_t)Dh, (cuuint64_t)prow, (cuuint64_t)Hkv, (cuuint64_t)num_pages};
+  cuuint64_t strides[3] = {(cuuint64_t)Dh, head, head * Hkv};
+  cuuint32_t box[4] = {(cuuint32_t)(Dh < 128 ? Dh : 128), (cuuint32_t)rows, 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, Dh < 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
 }  // namespace hdsfa
