@@ -58,6 +58,12 @@ HD_DEVINLINE uint32_t f16x2_of(uint16_t codes) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(r) : "h"(codes));
   return r;
 }
+// ... of the four codes of a word.  (One asm statement: the conversions take the word's halves as they lie.)
+HD_DEVINLINE void f16x4_of(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}\n"
+      : "=r"(lo), "=r"(hi)
+      : "r"(codes));
+}
 HD_DEVINLINE float2 values2(uint16_t codes) {
   const uint32_t r = f16x2_of(codes);
   return __half22float2(*reinterpret_cast<const __half2*>(&r));

@@ -21,21 +21,15 @@
 
 #include <algorithm>
 
-#include "decode.cuh"
 #include "decode_plan.cuh"
-#include "q8.cuh"
-#include "tc_common.cuh"
+#include "decode_q8.cuh"
 
 namespace hdsfa {
 namespace decq8 {
-using dec::DecodeArgs;
-using dec::kBadPage;
-
 constexpr int kTmaRows = 8;
 constexpr int kWarpKeys = 32;        // positions of a tile that a warp takes
 constexpr float kShift = 15.f;       // P's largest exponent
 constexpr int kMaxRows = 64;         // query rows of a CTA at most (four row tiles)
-constexpr uint32_t kNoRow = 0xffffffffu;
 
 template <int DH>
 constexpr int dsplit() { return DH == 256 ? 2 : 1; }  // head-dim parts: a warp's O must fit its registers
@@ -44,23 +38,15 @@ constexpr int key_warps() { return 4 / dsplit<DH>(); }
 template <int DH>
 constexpr int ktile() { return kWarpKeys * key_warps<DH>(); }
 
-struct Args : DecodeArgs {
-  const uint8_t *kcodes, *vcodes, *kscale, *vscale;
-  int blocks;       // blocks of a page
-  FastDiv d_brow;   // rows of a block
-  int mt;           // row tiles of a CTA
-};
-struct Params {
-  CUtensorMap tm_k, tm_v;
-  Args a;
-};
 
 // Two CTAs an SM while their queries leave room for three stages each: up to two row tiles, one at head dim 256.  WIDE:
-// more row tiles, one CTA an SM.
+// more row tiles, one CTA an SM.  Sixteen warps an SM hide the products' latency, so where the row tiles are few there
+// are two sets of warps, which take alternate tiles.
 template <int DH, bool WIDE>
 struct Cfg {
   static constexpr int KT = ktile<DH>(), MT = WIDE ? 4 : DH == 256 ? 1 : 2, STAGES = !WIDE ? 3 : DH == 256 ? 5 : 6;
-  static constexpr int kThreads = MT * 4 * 32;
+  static constexpr int kWarps = WIDE ? 16 : 8, kThreads = kWarps * 32;
+  static constexpr int kMergeRows = WIDE ? 64 : 32;  // row tiles x sets, in rows, at most
 };
 
 template <int DH, bool WIDE, bool TMA>
@@ -69,10 +55,10 @@ struct Smem {
   uint8_t k[C::STAGES][C::KT * DH];
   uint8_t v[C::STAGES][C::KT * DH];
   __half q[C::MT * 16 * DH];
-  float4 scale[C::MT * 4][kWarpKeys];   // a warp's keys: 2^ek, ev, 2^-ev
+  float4 scale[C::kWarps][kWarpKeys];   // a warp's keys: 2^ek, ev, 2^-ev
   float qscale[C::MT * 16];
   uint32_t row[TMA ? 1 : 4][C::KT];     // cp.async: rows of the pool (kNoRow: none) of four tiles
-  uint64_t full[C::STAGES], empty[C::STAGES];
+  uint64_t full[2 * C::STAGES], empty[2 * C::STAGES];  // of a stage and set
   unsigned not_finite[2];               // a bit for each row of the merged partial
   int bad_page, abort;
 };
@@ -97,89 +83,11 @@ HD_DEVINLINE uint32_t pack_f16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// Row of position p >= 0 of K/V head g in the pools (of Dh codes each; below 2^32, checked on the host), kNoRow where
-// the table names no page; and its block's scale.
-HD_DEVINLINE uint32_t row_at(const Args& a, const int32_t* table, int g, int p, size_t* scale) {
-  const int i = fast_div(p, a.pg.d_prow);
-  if (i >= a.pg.max_pages) return kNoRow;
-  const int id = table[i];
-  if ((unsigned)id >= (unsigned)a.pg.num_pages) return kNoRow;
-  const int off = p - i * a.pg.prow;
-  const size_t ph = (size_t)id * a.Hkv + g;
-  if (scale != nullptr) *scale = ph * a.blocks + fast_div(off, a.d_brow);
-  return (uint32_t)(ph * a.pg.prow + off);
-}
-
-// A row's partial over the visible positions of [k0, k1), by one warp on the fp32 units: lane i holds DH/32 columns.
-// Only visible rows are read: what a hidden NaN has made of the products' row is not.
-template <int DH>
-__device__ __noinline__ void exact_row(const Args& a, int b, int g, int r, int T, int k0, int k1, float* po, float2* pml) {
-  constexpr int C = DH / 32;
-  const int lane = threadIdx.x & 31, s = r / a.G, h = g * a.G + r % a.G, pq = (T - 1) * a.n + s;
-  const int32_t* table = a.table + (long long)b * a.pg.max_pages;
-  int p = a.mode == SFA_LOCAL ? max(k0, pq - a.window + 1) : k0, step = 1;
-  if (a.mode == SFA_WITHIN) {
-    step = a.n;
-    p += (s + a.n - p % a.n) % a.n;
-  }
-  const int end = min(k1, pq + 1);
-  const bf16* q = a.q + (((long long)b * a.n + s) * a.Hq + h) * DH + lane * C;
-  float qf[C], o[C], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int c = 0; c < C; ++c) qf[c] = __bfloat162float(q[c]), o[c] = 0.f;
-  for (; p < end; p += step) {
-    size_t sc = 0;
-    const uint32_t row = row_at(a, table, g, p, &sc);
-    if (row == kNoRow) continue;
-    const size_t at = (size_t)row * DH;
-    float x = 0.f, v[C];
-#pragma unroll
-    for (int c = 0; c < C; c += 2) {
-      const float2 kv = q8::values2(*reinterpret_cast<const uint16_t*>(a.kcodes + at + lane * C + c));
-      const float2 vv = q8::values2(*reinterpret_cast<const uint16_t*>(a.vcodes + at + lane * C + c));
-      x += qf[c] * kv.x + qf[c + 1] * kv.y;
-      v[c] = vv.x, v[c + 1] = vv.y;
-    }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    x *= a.scale_log2 * q8::scale_of(q8::clamp_byte(a.kscale[sc]));
-    const float fv = q8::scale_of(q8::clamp_byte(a.vscale[sc]));
-    const float mn = fmaxf(m, x), mu = mn == -INFINITY ? 0.f : mn, corr = exp2f(m - mu), w = exp2f(x - mu);
-    m = mn;
-    l = l * corr + w;
-#pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = o[c] * corr + w * (v[c] * fv);
-  }
-  if (l != l) m = INFINITY;
-#pragma unroll
-  for (int c = 0; c < C; ++c) po[lane * C + c] = o[c];
-  if (lane == 0) *pml = make_float2(m, l);
-}
-
-// A finished row by one warp: o / l and its LSE, or an empty row (l = 0).
-template <int DH>
-HD_DEVINLINE void store_row(const Args& a, int b, int g, int r, const float* o, float m, float l) {
-  const int lane = threadIdx.x & 31, s = fast_div(r, a.d_G), h = g * a.G + r - s * a.G;
-  const bool some = l != 0.f;
-  const float inv = some ? 1.f / l : 0.f;
-  bf16* to = a.o + (((long long)b * a.n + s) * a.Hq + h) * DH;
-  for (int i = lane; i < DH / 4; i += 32) {
-    uint2 w = make_uint2(0, 0);
-    if (some) {
-      const float4 x = *reinterpret_cast<const float4*>(o + i * 4);
-      w = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
-    }
-    *reinterpret_cast<uint2*>(to + i * 4) = w;
-  }
-  if (lane == 0 && a.lse != nullptr)
-    a.lse[((long long)b * a.Hq + h) * a.n + s] = some ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY;
-}
-
 template <int DH, bool WIDE, bool TMA>
 __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_q8_kernel(const __grid_constant__ Params P) {
   using C = Cfg<DH, WIDE>;
   using Sm = Smem<DH, WIDE, TMA>;
-  constexpr int KT = C::KT, STAGES = C::STAGES, AHEAD = STAGES - 1;
+  constexpr int KT = C::KT, STAGES = C::STAGES;
   constexpr int KW = key_warps<DH>(), DC = DH / dsplit<DH>(), CPR = DH / 16;  // DC: O columns of a warp
   constexpr int RB = DH < 128 ? DH : 128;                                     // bytes of a row in a block of the tile
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -197,8 +105,9 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
   const int split = fast_div((int)blockIdx.x, a.d_heads), head = (int)blockIdx.x - split * a.Hkv * a.ngroups;
   const int g = a.ngroups == 1 ? head : head / a.ngroups, rg = a.ngroups == 1 ? 0 : head % a.ngroups;
   const int tid = threadIdx.x, nt = blockDim.x, W = nt >> 5, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, t4 = lane & 3;
-  // this warp's row tile, key group and head-dim part
-  const int mt = warp >> 2, kw = (warp & 3) % KW, dw = (warp & 3) / KW;
+  // this warp's set and its number there; row tile, key group and head-dim part
+  const int sets = TMA ? a.sets : 1, WS = 4 * a.mt, set = TMA && warp >= WS ? 1 : 0, ws = warp - set * WS;
+  const int mt = ws >> 2, kw = (ws & 3) % KW, dw = (ws & 3) / KW;
   const int R = a.rg;  // rows of the CTA
   const size_t pidx = blockIdx.x;
   float* po = a.part_o + pidx * R * DH;
@@ -212,9 +121,9 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     sm.bad_page = sm.abort = 0;
     sm.not_finite[0] = sm.not_finite[1] = 0;
     if (TMA) {
-      for (int i = 0; i < STAGES; ++i) {
+      for (int i = 0; i < 2 * STAGES; ++i) {
         mbar_init(&sm.full[i], 1);
-        mbar_init(&sm.empty[i], W);  // one arrival per warp
+        mbar_init(&sm.empty[i], WS);  // one arrival per warp of a set
       }
       fence_mbar_init();
     }
@@ -264,8 +173,9 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
 
   // ---- the tiles' loads
   const int seen = a.mode == SFA_LOCAL ? (T - 1) * a.n - a.window + 1 : 0;  // first position any row sees
-  // TMA: tile t is brought by warp (t - AHEAD) mod W; lane i brings piece i, whose page entry it has looked up when the
-  // warp brought its last tile
+  // TMA: the first tiles are brought by a warp each; after that a set that goes on to tile `it` brings tile
+  // it - sets + STAGES into the stage that it has left, its warps in turn.  Lane i brings piece i, whose page entry it has
+  // looked up when the warp brought its last tile
   auto pos_of = [&](int t) {  // first position of this lane's piece of a tile, -1: none that a row sees
     const int p = lane * a.piece, pos = k0 + t * tile + p;
     return p >= tile || pos >= k1 || pos + a.piece <= seen ? -1 : pos;
@@ -287,11 +197,15 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     return row;
   };
   [[maybe_unused]] int brought = -1;  // TMA: the last tile that this warp brought
-  auto load_tile = [&](int it) {
-    const int st = it % STAGES;
+  // A wait cannot tell a phase of a barrier from the one after the next, so who waits for a phase must have seen the one
+  // before: a stage that serves two sets in turn (STAGES is odd there) has barriers for each, at [set * STAGES + stage].
+  // A set's i-th tile is its barriers' phase i / STAGES.
+  static_assert(WIDE || STAGES % 2 == 1, "two sets share a stage");
+  auto load_tile = [&](int it, int st, int whose) {  // tile `it` of set `whose` into stage st
     if constexpr (TMA) {
       brought = it;
-      if (lane == 0) mbar_arrive_expect_tx(&sm.full[st], tile * DH * 2);
+      uint64_t* full = &sm.full[whose * STAGES + st];
+      if (lane == 0) mbar_arrive_expect_tx(full, tile * DH * 2);
       __syncwarp();
       if (lane * a.piece < tile) {
         const int pos = pos_of(it);
@@ -307,12 +221,11 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
 #pragma unroll
         for (int cb = 0; cb < DH / RB; ++cb) {
           const int at = cb * KT * RB + lane * a.piece * RB;
-          tma_load_4d(sm.k[st] + at, &P.tm_k, &sm.full[st], cb * RB, off, g, page);
-          tma_load_4d(sm.v[st] + at, &P.tm_v, &sm.full[st], cb * RB, off, g, page);
+          tma_load_4d(sm.k[st] + at, &P.tm_k, full, cb * RB, off, g, page);
+          tma_load_4d(sm.v[st] + at, &P.tm_v, full, cb * RB, off, g, page);
         }
       }
       __syncwarp();
-      fetch(it + W);
     } else {
       for (int i = tid; i < KT * CPR; i += nt) {
         const int rr = i / CPR, cc = i % CPR;
@@ -323,43 +236,47 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
       }
     }
   };
-  // The scales of this warp's keys, a lane's key each: the page entry two tiles ahead, the bytes one tile ahead.
-  const int my_key = kw * kWarpKeys + lane;
-  auto scale_pos = [&](int it) {
-    const int p = k0 + it * tile + my_key;
-    return it < nsub && my_key < tile && p < k1 && p >= seen ? p : -1;
+  // The scales of this warp's keys, a lane's key each: the page entry two of the set's tiles ahead, the bytes one ahead.
+  // The key's page and row there go on by the set's step, without divisions.
+  const int my_key = kw * kWarpKeys + lane, step = tile * sets;
+  const int step_pages = fast_div(step, a.pg.d_prow), step_rows = step - step_pages * a.pg.prow;
+  int at_pos = k0 + set * tile + my_key, at_page = fast_div(at_pos, a.pg.d_prow), at_row = at_pos - at_page * a.pg.prow;
+  int next_entry = -1, next_row_in = 0;
+  auto scale_entry = [&] {  // entry and row of the key in the set's next tile, whose number goes up by one
+    next_entry = -1;
+    next_row_in = at_row;
+    if (my_key < tile && at_pos < k1 && at_pos >= seen && at_page < a.pg.max_pages) next_entry = table[at_page];
+    at_pos += step;
+    at_page += step_pages;
+    at_row += step_rows;
+    if (at_row >= a.pg.prow) at_row -= a.pg.prow, ++at_page;
   };
-  auto scale_entry = [&](int it) {
-    const int p = scale_pos(it);
-    if (p < 0) return -1;
-    const int i = fast_div(p, a.pg.d_prow);
-    return i < a.pg.max_pages ? table[i] : -1;
-  };
-  auto scale_bytes = [&](int it, int id, int& kb, int& vb) {
-    kb = vb = 127;
-    const int p = scale_pos(it);
-    if (p < 0 || (unsigned)id >= (unsigned)a.pg.num_pages) return;
-    const int off = p - fast_div(p, a.pg.d_prow) * a.pg.prow;
-    const size_t at = ((size_t)id * a.Hkv + g) * a.blocks + fast_div(off, a.d_brow);
-    kb = a.kscale[at];
-    vb = a.vscale[at];
+  int kb = 127, vb = 127;
+  auto scale_bytes = [&] {
+    if ((unsigned)next_entry < (unsigned)a.pg.num_pages) {
+      const size_t at = ((size_t)next_entry * a.Hkv + g) * a.blocks + fast_div(next_row_in, a.d_brow);
+      kb = a.kscale[at];
+      vb = a.vscale[at];
+    }
   };
   if constexpr (TMA) {
-    const int t = (warp + AHEAD) % W;  // this warp's first tile
-    fetch(t);
-    if (t < min(AHEAD, nsub)) load_tile(t);
+    if (warp < min(STAGES, nsub)) {
+      fetch(warp);
+      load_tile(warp, warp, sets == 2 ? warp & 1 : 0);
+    }
+    fetch(set + sets * (ws == 0 ? WS - 1 : ws - 1) + STAGES);  // this warp's next one
   } else {
     const uint32_t r0 = row_of(0), r1 = row_of(1), r2 = row_of(2);
     if (tid < tile) sm.row[0][tid] = r0, sm.row[1][tid] = r1, sm.row[2][tid] = r2;
     __syncthreads();
-    load_tile(0);
+    load_tile(0, 0, 0);
     cp_async_commit();
-    if (nsub > 1) load_tile(1);
+    if (nsub > 1) load_tile(1, 1, 0);
     cp_async_commit();
   }
-  int kb, vb, next_entry;
-  scale_bytes(0, scale_entry(0), kb, vb);
-  next_entry = scale_entry(1);
+  scale_entry();
+  scale_bytes();
+  scale_entry();
   // The queries: a warp per row scales its row by a power of two, rounds it to f16 and lays it out in the products'
   // order: value 16i + 4t + j at column 16i + 2t + j (j < 2) or 16i + 6 + 2t + j.
   for (int rr = warp; rr < R; rr += W) {
@@ -400,27 +317,31 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
   for (int i = 0; i < DC / 8; ++i) oacc[i][0] = oacc[i][1] = oacc[i][2] = oacc[i][3] = 0.f;
 
   bool alive = true;
-  for (int it = 0; it < nsub; ++it) {
-    const int st = it % STAGES, base = k0 + it * tile;
+  int turn = 0;  // the warp of this set that brings a tile
+  int st = set, phase = 0, round = 0, left_st = 0, left_phase = 0;  // stage and phase of this tile and of the set's last
+  for (int it = set; it < nsub; it += sets) {
+    const int base = k0 + it * tile;
     [[maybe_unused]] uint32_t next_row = kNoRow;
     // this tile's scales into shared memory, the next ones' loads on their way
     {
       kb = q8::clamp_byte(kb);
       vb = q8::clamp_byte(vb);
       sm.scale[warp][lane] = make_float4(q8::scale_of(kb), (float)(vb - 127), q8::inverse_of(vb), 0.f);
-      const int id = next_entry;
-      next_entry = scale_entry(it + 2);
-      scale_bytes(it + 1, id, kb, vb);
+      scale_bytes();
+      scale_entry();
     }
     if constexpr (TMA) {
       // the warps meet on the stages' barriers alone: one that loads does not hold up the others
-      if (it % W == warp && it + AHEAD < nsub) {
-        const int t = it + AHEAD;
-        if (t >= STAGES)
-          alive = __all_sync(0xffffffffu, mbar_wait(&sm.empty[t % STAGES], (t / STAGES - 1) & 1, &sm.abort, a.status));
-        if (alive) load_tile(t);
+      const int left = it - sets, t = left + STAGES;
+      if (turn == ws && left >= 0 && t < nsub) {
+        alive = __all_sync(0xffffffffu, mbar_wait(&sm.empty[set * STAGES + left_st], left_phase, &sm.abort, a.status));
+        if (alive) {
+          load_tile(t, left_st, sets - 1 - set);
+          fetch(t + sets * WS);
+        }
       }
-      alive = alive && __all_sync(0xffffffffu, mbar_wait(&sm.full[st], (it / STAGES) & 1, &sm.abort, a.status));
+      if (++turn == WS) turn = 0;
+      alive = alive && __all_sync(0xffffffffu, mbar_wait(&sm.full[set * STAGES + st], phase, &sm.abort, a.status));
       if (!alive) break;
       if (base + tile > k1) {  // cached rows behind the sequence's length may never have been written
         const int r0 = max(kw * kWarpKeys, k1 - base), r1 = min((kw + 1) * kWarpKeys, tile);
@@ -431,7 +352,7 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     } else {
       cp_async_wait<1>();  // stage `it` has landed
       __syncthreads();     // ... for every thread, and stage it-1 is no longer read
-      if (it + 2 < nsub) load_tile(it + 2);
+      if (it + 2 < nsub) load_tile(it + 2, (it + 2) % STAGES, 0);
       cp_async_commit();
       next_row = row_of(it + 3);  // the rows that the next iteration loads by
     }
@@ -454,8 +375,11 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
         ldsm_x4(smem_u32(cK + chunk_at<DH, KT>(kw * kWarpKeys + j * 8 + (lane & 7), kq * 4 + (lane >> 3))), c[0], c[1], c[2],
                 c[3]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          mma_f16_16816(sacc[j], qa[i], q8::f16x2_of((uint16_t)c[i]), q8::f16x2_of((uint16_t)(c[i] >> 16)));
+        for (int i = 0; i < 4; ++i) {
+          uint32_t b0, b1;
+          q8::f16x4_of(c[i], b0, b1);
+          mma_f16_16816(sacc[j], qa[i], b0, b1);
+        }
       }
     }
     // x = s + ev, the mask, and the online softmax in log2 units
@@ -528,43 +452,51 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
                   r[0], r[1], r[2], r[3]);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const uint32_t lo = __byte_perm(r[2 * c], 0, 0x3120), hi = __byte_perm(r[2 * c + 1], 0, 0x3120);
+          uint32_t b0, b1, b2, b3;  // even columns of keys 2t, 2t+1 and 2t+8, 2t+9; odd columns
+          q8::f16x4_of(__byte_perm(r[2 * c], 0, 0x3120), b0, b2);
+          q8::f16x4_of(__byte_perm(r[2 * c + 1], 0, 0x3120), b1, b3);
           float(*acc)[4] = &oacc[(c2 * 2 + c) * 2];
-          mma_f16_16816(acc[0], pa, q8::f16x2_of((uint16_t)lo), q8::f16x2_of((uint16_t)hi));
-          mma_f16_16816(acc[1], pa, q8::f16x2_of((uint16_t)(lo >> 16)), q8::f16x2_of((uint16_t)(hi >> 16)));
+          mma_f16_16816(acc[0], pa, b0, b1);
+          mma_f16_16816(acc[1], pa, b2, b3);
         }
       }
     }
     if constexpr (TMA) {
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.empty[st]);
+      if (lane == 0) mbar_arrive(&sm.empty[set * STAGES + st]);
     } else {
       __syncwarp();  // this tile's scales are read
       if (tid < tile) sm.row[(it + 3) & 3][tid] = next_row;
     }
+    left_st = st;
+    left_phase = phase;
+    st = st + sets >= STAGES ? st + sets - STAGES : st + sets;
+    if (++round == STAGES) round = 0, phase ^= 1;
   }
   if constexpr (TMA) {
     // a wait gave up: the results are invalid.  A warp that goes on has seen every tile land; one that does not
-    // waits (again with a limit) for the last that it brought, whose stage no earlier one can still be filling.
-    if (!alive && brought >= 0 && lane == 0) mbar_drain(&sm.full[brought % STAGES], (brought / STAGES) & 1);
+    // waits (again with a limit) for the last that it brought, and those before it were read before its set went on.
+    if (!alive && brought >= 0 && lane == 0)
+      mbar_drain(&sm.full[(sets == 2 ? brought & 1 : 0) * STAGES + brought % STAGES], brought / (STAGES * sets) & 1);
     if (__syncthreads_or(!alive)) return;
   } else {
     cp_async_wait<0>();
     __syncthreads();
   }
 
-  // merge the key groups' partials in shared memory (the ring is free now): [KW][R][DH], then the running maxima (in
+  // merge the key groups' partials in shared memory (the ring is free now): [KP][R][DH], then the running maxima (in
   // the partials' units, where P is at most 2^15) and sums
-  static_assert((KW * C::MT * 16 * DH + 2 * KW * C::MT * 16) * 4 <= 2 * STAGES * KT * DH, "merge fits the ring");
+  static_assert((KW * C::kMergeRows * DH + 2 * KW * C::kMergeRows) * 4 <= 2 * STAGES * KT * DH, "merge fits the ring");
   static_assert(kMaxRows <= 128, "one thread per row");
+  const int KP = KW * sets;
   float* sO = reinterpret_cast<float*>(sm.k[0]);
-  float* sM = sO + KW * R * DH;  // [KW][R]
-  float* sL = sM + KW * R;       // [KW][R]
+  float* sM = sO + KP * R * DH;  // [KP][R]
+  float* sL = sM + KP * R;       // [KP][R]
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf) {
     ls[hf] += __shfl_xor_sync(0xffffffffu, ls[hf], 1);
     ls[hf] += __shfl_xor_sync(0xffffffffu, ls[hf], 2);
-    const int row = kw * R + mt * 16 + g4 + 8 * hf;
+    const int row = (set * KW + kw) * R + mt * 16 + g4 + 8 * hf;
     if (t4 == 0 && dw == 0) {
       sM[row] = mx[hf] - kShift;
       sL[row] = ls[hf];
@@ -578,11 +510,9 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
   const bool bad = sm.bad_page != 0;
   if (tid < R) {  // one thread per row: its maximum and sum over the key groups, whose weights replace their maxima
     float m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int w = 0; w < KW; ++w) m = fmaxf(m, sM[w * R + tid]);
+    for (int w = 0; w < KP; ++w) m = fmaxf(m, sM[w * R + tid]);
     const float mu = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int w = 0; w < KW; ++w) {
+    for (int w = 0; w < KP; ++w) {
       const float f = exp2f(sM[w * R + tid] - mu);
       l += f * sL[w * R + tid];
       sM[w * R + tid] = f;
@@ -596,8 +526,8 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
   for (int idx = tid; idx < R * (DH / 4); idx += nt) {
     const int row = idx / (DH / 4), c4 = idx % (DH / 4);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < KW; ++w) {
+#pragma unroll 2
+    for (int w = 0; w < KP; ++w) {
       const float f = sM[w * R + row];
       const float4 v = *reinterpret_cast<const float4*>(sO + (w * R + row) * DH + c4 * 4);
       o.x += f * v.x;
@@ -642,19 +572,19 @@ static long long q8_range(int maxT, int n, int mode, int window) {
   return mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1) : (long long)maxT * n;
 }
 
-// Splits of a step: the fewest waves times (tiles of a CTA + about two tiles' time to start and end it), a combine
-// kernel of about three tiles' time beside more than one split.  At most four waves of CTAs, which bounds the
-// workspace: `bound` gives the most that any smaller maxT or window takes.
-static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, bool bound) {
+// Splits of a step on the tensor cores (`tc`) or not: the fewest waves times (tiles of a CTA + about two tiles' time to
+// start and end it), a combine kernel of about three tiles' time beside more than one split.  At most four waves of
+// CTAs, which bounds the workspace: `bound` gives the most that any smaller maxT or window takes.
+static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window, bool tc, bool bound) {
   Q8Plan p = {};
   p.G = Hq / Hkv;
   p.M = n * p.G;
   p.ngroups = (p.M + decq8::kMaxRows - 1) / decq8::kMaxRows;
-  const int rows = (p.M + p.ngroups - 1) / p.ngroups;
-  p.rg = (rows + 15) / 16 * 16;
-  const int KT = Dh == 256 ? decq8::ktile<256>() : decq8::ktile<128>();
+  p.rg = ((p.M + p.ngroups - 1) / p.ngroups + 15) / 16 * 16;
+  const int KT = !tc && Dh == 256 ? decq8::ktile<256>() : decq8::ktile<128>();
   const long long tiles = (q8_range(maxT, n, mode, window) + KT - 1) / KT, ctas = (long long)B * Hkv * p.ngroups;
-  const long long resident = (long long)kSmCount * (p.rg > (Dh == 256 ? 16 : 32) ? 1 : Dh == 64 && p.rg == 16 ? 4 : 2);
+  const long long resident =
+      (long long)kSmCount * (tc ? decode_q8_tc_per_sm(p.rg, Dh) : p.rg > (Dh == 256 ? 16 : 32) ? 1 : Dh == 64 && p.rg == 16 ? 4 : 2);
   const long long most = std::min({tiles, (long long)dec::kMaxSplit, std::max(1LL, 4 * resident / ctas)});
   long long best = 1, best_cost = -1;
   if (bound) {
@@ -677,8 +607,13 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
   return p;
 }
 
+// Whether the tcgen05 kernel takes a step: it reads tiles by TMA alone.
+static bool q8_tc(int Dh, int prow) { return Dh >= 128 && paged_piece(prow, 128) >= decq8::kTmaRows; }
+
 size_t decode_paged_q8_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {
-  return q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, true).bytes();
+  // either kernel's, whatever the pages
+  const size_t x = q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, false, true).bytes();
+  return Dh == 64 ? x : std::max(x, q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, true, true).bytes());
 }
 
 template <int DH, bool WIDE, bool TMA>
@@ -689,11 +624,15 @@ static cudaError_t launch_q8_t(const decq8::Params& p, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(decode_q8_kernel<DH, WIDE, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   return launch_kernel(true, decode_q8_kernel<DH, WIDE, TMA>, dim3((unsigned)p.a.nsplit * p.a.B * p.a.Hkv * p.a.ngroups),
-                       (unsigned)p.a.mt * 128, smem, st, p);
+                       (unsigned)(p.a.mt * p.a.sets) * 128, smem, st, p);
 }
 template <int DH>
-static cudaError_t launch_q8_d(const decq8::Params& p, bool tma, cudaStream_t st) {
-  if (p.a.mt > decq8::Cfg<DH, false>::MT) return tma ? launch_q8_t<DH, true, true>(p, st) : launch_q8_t<DH, true, false>(p, st);
+static cudaError_t launch_q8_d(decq8::Params& p, bool tma, cudaStream_t st) {
+  // two sets only where the stages' number is odd (a stage serves both)
+  static_assert(decq8::Cfg<256, true>::STAGES % 2 == 1, "");
+  const bool wide = p.a.mt > decq8::Cfg<DH, false>::MT;
+  p.a.sets = !tma ? 1 : DH == 64 && p.a.mt == 1 ? 1 : p.a.mt == (wide ? 2 : 1) ? 2 : 1;
+  if (wide) return tma ? launch_q8_t<DH, true, true>(p, st) : launch_q8_t<DH, true, false>(p, st);
   return tma ? launch_q8_t<DH, false, true>(p, st) : launch_q8_t<DH, false, false>(p, st);
 }
 
@@ -702,7 +641,8 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
                                        int num_pages, int P, int max_pages, int n, int Hq, int Hkv, int Dh, int T,
                                        float scale, int mode, int window, void* ws, size_t ws_bytes, int32_t* status,
                                        cudaStream_t st) {
-  const Q8Plan plan = q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, false);
+  const bool tc = q8_tc(Dh, P * n);
+  const Q8Plan plan = q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, tc, false);
   if (plan.bytes() > ws_bytes) return cudaErrorInvalidValue;  // the bound says that it is not
   decq8::Params p = {};
   decq8::Args& a = p.a;
@@ -739,7 +679,7 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   a.d_G = make_fast_div((uint32_t)plan.G);
   a.d_n = make_fast_div((uint32_t)n);
   a.d_heads = make_fast_div((uint32_t)(Hkv * plan.ngroups));
-  const int KT = Dh == 256 ? decq8::ktile<256>() : decq8::ktile<128>();
+  const int KT = !tc && Dh == 256 ? decq8::ktile<256>() : decq8::ktile<128>();
   a.piece = paged_piece(a.pg.prow, KT);
   // a piece's rows start on 128 bytes of shared memory
   const bool tma = a.piece >= decq8::kTmaRows && (Dh >= 128 || a.piece % 2 == 0);
@@ -748,7 +688,8 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   if (tma && (!make_q8_tmap(&p.tm_k, kc, num_pages, Hkv, a.pg.prow, Dh, a.piece) ||
               !make_q8_tmap(&p.tm_v, vc, num_pages, Hkv, a.pg.prow, Dh, a.piece)))
     return cudaErrorInvalidValue;
-  const cudaError_t e = Dh == 64    ? launch_q8_d<64>(p, tma, st)
+  const cudaError_t e = tc          ? launch_decode_q8_tc(p, Dh, st)
+                        : Dh == 64  ? launch_q8_d<64>(p, tma, st)
                         : Dh == 128 ? launch_q8_d<128>(p, tma, st)
                                     : launch_q8_d<256>(p, tma, st);
   return e != cudaSuccess || a.nsplit == 1 ? e : launch_combine_paged(a, Dh, st);

@@ -1,0 +1,626 @@
+// Decoding over the 8-bit paged cache on the 5th-generation tensor cores (head dims 128 and 256; the mathematics of x, m
+// and the scales: sfa_decode_q8.cu).
+//
+// K and V go from TMA to the products as the codes that they are; only scores pass through registers.  Both products
+// have the cached positions or the head dim as their 128 rows, and the few query rows as columns, so that no row of a
+// tile is empty and a thread has one position:
+//   S^T [128 positions x 2 R] = K (e4m3) * [q_hi | q_lo]^T (e4m3): a row's bf16 values, scaled by a power of two to [2^7,
+//     2^8), are hi + lo / 16 in two codes, exact for values down to 2^-14 of the row's largest and to 2^-22 of it below;
+//   O^T [Dh x R] += V^T (e4m3) * P^T (e5m2), three times: P is hi + mid + lo in three codes of three bits, so rounded to nine
+//     bits (of its f16 form), down to steps of 2^-16; it is at most 2^15, and 2^11 or more at the row's largest score.
+// A thread of a softmax warp takes its position's scores for the warp group's RW rows: scales by 2^ek, adds ev, masks
+// (what a position is visible to is a range of rows), and subtracts the row's reference.  References are the whole
+// CTA's, in shared memory, and go up only when some P would pass 2^15 (a vote for each tile): then the rows' maxima are
+// reduced over the warps, O in tensor memory is rescaled, and the scores' references follow.
+//
+// Warp 0 brings tiles (TMA, pieces of pages), warp 1 issues the products, the others are WG groups of four softmax warps
+// with RW rows each.  S and P have two buffers, so S of the next tile is computed under this one's softmax and its P V
+// under the next one's.  Two CTAs an SM where shared and tensor memory hold them.
+#include <float.h>
+
+#include <algorithm>
+
+#include "decode_q8.cuh"
+
+namespace hdsfa {
+namespace decq8tc {
+using decq8::Args;
+using decq8::Params;
+
+constexpr int KT = 128;            // positions of a tile
+constexpr int kUnit = KT * 128;    // bytes of a ring slot: 128 columns of a K or V tile
+constexpr float kTop = 15.f;       // P's largest exponent
+constexpr float kSet = 11.f;       // the exponent of a row's largest P when its reference is set
+constexpr float kLo = 16.f;        // scale of a query's second codes
+
+// HV: 128-column units of a tile (Dh / 128)
+template <int HV, int RW, int WG>
+struct Cfg {
+  static constexpr int R = RW * WG, kThreads = 64 + WG * 128;
+  static constexpr int kCols = 4 * R + HV * R;  // tensor memory: two S, O
+  static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+  static constexpr int kFixed = 2 * R * HV * 128 + 6 * R * KT + 2048;  // queries, P, the rest
+  static constexpr int kPerSm = kAlloc <= 256 && kFixed + 3 * kUnit <= 112 * 1024 ? 2 : 1;
+  static constexpr int kRoom = ((kPerSm == 2 ? 112 : 225) * 1024 - kFixed) / kUnit;
+  static constexpr int NSLOT = kRoom < 10 ? kRoom : 10;
+};
+
+template <int HV, int RW, int WG>
+struct Smem {
+  using C = Cfg<HV, RW, WG>;
+  uint8_t ring[C::NSLOT][kUnit];             // [128 positions][128 bytes], 128-byte swizzle
+  uint8_t q[HV][2 * C::R * 128];             // [R rows of hi, R of lo][128 bytes], 128-byte swizzle
+  uint8_t p[2][3][C::R * KT];                // a buffer's hi, mid, lo: blocks of 16 rows, [128 positions][16 bytes]
+  float rowf[C::R], ref[C::R];               // a row's factor of q; its reference
+  float most[4][C::R];                       // a warp's maxima, or sums
+  uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], drain;
+  uint32_t tmem_base;
+  unsigned not_finite[2];
+  int abort, bad_page;
+};
+
+// kind::f8f6f4, fp32 D: operand types 0 e4m3, 1 e5m2.
+__host__ __device__ constexpr uint32_t idesc_f8(int M, int N, int a_type, int b_type, int a_mn, int b_mn) {
+  return (1u << 4) | ((uint32_t)a_type << 7) | ((uint32_t)b_type << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// Matrix descriptor without a swizzle, MN-major: 16 bytes of rows x 8 k lie together (128 bytes); the next 8 k are `kstep`
+// bytes on, the next 16 rows `mstep`.
+HD_DEVINLINE uint64_t sdesc_plain_mn(uint32_t saddr, uint32_t kstep, uint32_t mstep) {
+  uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)((kstep >> 4) & 0x3FFFu) << 16;
+  d |= (uint64_t)((mstep >> 4) & 0x3FFFu) << 32;
+  d |= 1ull << 46;  // descriptor version for tcgen05
+  return d;
+}
+HD_DEVINLINE void mma_f8_ss_w(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n elect.sync _|e, 0xffffffff;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accum));
+}
+HD_DEVINLINE void tmem_ld8(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+// Whether `v` holds for a thread of the 128 on hardware barrier `id`.
+HD_DEVINLINE bool group_any(int id, bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.or.pred q, %2, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+      : "=r"(r)
+      : "r"((uint32_t)v), "r"(id)
+      : "memory");
+  return r != 0;
+}
+// Floats as integers of the same order, and back.
+HD_DEVINLINE int ordered(float x) {
+  const int i = __float_as_int(x);
+  return i ^ ((i >> 31) & 0x7fffffff);
+}
+HD_DEVINLINE float from_ordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
+HD_DEVINLINE uint32_t hsub2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// Bits [lo, hi) of 32, the range cut to them.
+HD_DEVINLINE uint32_t bits(int lo, int hi) {
+  lo = min(max(lo, 0), 32);
+  hi = min(max(hi, 0), 32);
+  return hi <= lo ? 0u : (uint32_t)((1ull << hi) - (1ull << lo));
+}
+
+template <int HV, int RW, int WG>
+__global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kPerSm)
+    decode_q8_tc_kernel(const __grid_constant__ Params P) {
+  using C = Cfg<HV, RW, WG>;
+  using Sm = Smem<HV, RW, WG>;
+  constexpr int R = C::R, NSLOT = C::NSLOT, NT = C::kThreads, DH = HV * 128;
+  const Args& a = P.a;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  Sm& sm = *reinterpret_cast<Sm*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int split = fast_div((int)blockIdx.x, a.d_heads), head = (int)blockIdx.x - split * a.Hkv * a.ngroups;
+  const int g = a.ngroups == 1 ? head : head / a.ngroups, rg = a.ngroups == 1 ? 0 : head % a.ngroups;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const size_t pidx = blockIdx.x;
+  float* po = a.part_o + pidx * R * DH;
+  float2* pml = a.part_ml + pidx * R;
+  const int tile = a.tile, row0 = rg * R, rows = min(R, a.M - row0);
+  // positions of a tile that no piece fills: their V must not be NaN
+  for (int i = tid; i < NSLOT * (KT - tile) * 8; i += NT) {
+    const int per = (KT - tile) * 8;
+    reinterpret_cast<uint4*>(sm.ring[i / per] + tile * 128)[i % per] = make_uint4(0, 0, 0, 0);
+  }
+  if (tid == 0) {
+    for (int i = 0; i < NSLOT; ++i) {
+      mbar_init(&sm.full[i], 1);
+      mbar_init(&sm.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.s_full[i], 1);
+      mbar_init(&sm.s_free[i], 4 * WG);
+      mbar_init(&sm.p_full[i], 4 * WG);
+      mbar_init(&sm.pv_done[i], 1);
+    }
+    mbar_init(&sm.drain, 1);
+    sm.abort = sm.bad_page = 0;
+    sm.not_finite[0] = sm.not_finite[1] = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0) {
+    tmem_alloc(&sm.tmem_base, C::kAlloc);
+    tmem_relinquish();
+    if (lane == 0) {
+      tma_prefetch(&P.tm_k);
+      tma_prefetch(&P.tm_v);
+    }
+  }
+  grid_dep_wait();
+  grid_dep_launch();
+  const int b = fast_div(split, a.d_nsplit), T = a.lens[b];
+  const int32_t* table = a.table + (long long)b * a.pg.max_pages;
+  int k0, k1;
+  dec::split_range<true>(a, T, split - b * a.nsplit, tile, k0, k1);
+  const int nt = k0 < k1 ? fast_div(k1 - k0 + tile - 1, a.d_tile) : 0;
+  // the queries: a warp per row
+  if (nt > 0)
+    for (int rr = warp; rr < R; rr += NT / 32) {
+      constexpr int NP = DH / 64;  // pairs of a lane
+      uint32_t w[NP], most = 0;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) w[i] = 0;
+      if (rr < rows) {
+        const int r = row0 + rr, s = fast_div(r, a.d_G), h = g * a.G + r - s * a.G;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (((long long)b * a.n + s) * a.Hq + h) * DH) + lane * NP;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) w[i] = src[i];
+      }
+#pragma unroll
+      for (int i = 0; i < NP; ++i) most = max(most, max(w[i] << 16 & 0x7fff0000u, w[i] & 0x7fff0000u));
+      most = __reduce_max_sync(0xffffffffu, most);
+      // the exponent field of the largest magnitude, kept where both powers are normal
+      const int e = min(max((int)(most >> 23), 20), 254);
+      const float to = __int_as_float(min(127 + 7 + 127 - e, 254) << 23);  // 2^(7 - (e - 127)), at most 2^127
+      const float back = __int_as_float(max(e - 7, 1) << 23);              // 2^(e - 127 - 7)
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const float x0 = __uint_as_float(w[i] << 16) * to, x1 = __uint_as_float(w[i] & 0xffff0000u) * to;
+        const uint32_t hi = q8::code2(x0, x1);
+        const float2 y = q8::values2((uint16_t)hi);
+        const uint32_t lo = q8::code2((x0 - y.x) * kLo, (x1 - y.y) * kLo);
+        const int c = (lane * NP + i) * 2, at = (c & 127) >> 4, off = c & 15;  // column; its 16-byte chunk
+        uint8_t* blk = sm.q[c >> 7];
+        *reinterpret_cast<uint16_t*>(blk + rr * 128 + ((at ^ (rr & 7)) << 4) + off) = (uint16_t)hi;
+        *reinterpret_cast<uint16_t*>(blk + (R + rr) * 128 + ((at ^ (rr & 7)) << 4) + off) = (uint16_t)lo;
+      }
+      if (lane == 0) {
+        sm.rowf[rr] = back * a.scale_log2;
+        sm.ref[rr] = 0.f;
+      }
+    }
+  fence_async_smem();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem_base;
+  volatile int* abort = &sm.abort;
+  if (nt == 0) {  // nothing of this sequence in this split: an empty partial, or an empty result
+    if (a.nsplit > 1) {
+      for (int i = tid; i < R; i += NT) pml[i] = make_float2(-INFINITY, 0.f);
+    } else {
+      if (T != 0 && g == 0 && rg == 0 && tid == 0) set_status(a.status, HD_DEVBIT_INDEX);
+      for (int row = warp; row < rows; row += NT / 32) decq8::store_row<DH>(a, b, g, row0 + row, nullptr, -INFINITY, 0.f);
+    }
+  } else if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer: K(0), then K(j + 1), V(j)
+    const int seen = a.mode == SFA_LOCAL ? (T - 1) * a.n - a.window + 1 : 0;  // first position any row sees
+    // page and row there of this lane's piece of the tiles whose V (cur) and K (nxt) come next; the page entry of the
+    // one after them is loaded a tile ahead
+    auto pos_of = [&](int j) {  // first position of the piece, -1: none that a row sees
+      const int p = lane * a.piece, pos = k0 + j * tile + p;
+      return p >= tile || pos >= k1 || pos + a.piece <= seen ? -1 : pos;
+    };
+    int entry = 0;
+    auto fetch = [&](int j) {
+      const int pos = pos_of(j);
+      if (pos >= 0) {
+        const int i = fast_div(pos, a.pg.d_prow);
+        entry = i < a.pg.max_pages ? table[i] : -1;
+      }
+    };
+    auto place = [&](int j) {  // of the tile that was fetched: (page, row), behind the pool (zeros) where there is none
+      const int pos = pos_of(j);
+      int2 x = make_int2(a.pg.num_pages, 0);
+      if (pos >= 0) {
+        if ((unsigned)entry < (unsigned)a.pg.num_pages) x = make_int2(entry, pos - fast_div(pos, a.pg.d_prow) * a.pg.prow);
+        else sm.bad_page = 1;
+      }
+      return x;
+    };
+    int issued = 0, slot = 0, lap = 0;
+    auto load = [&](const CUtensorMap* tm, int2 x) -> bool {
+#pragma unroll
+      for (int hf = 0; hf < HV; ++hf) {
+        if (lap > 0 && !__all_sync(0xffffffffu, mbar_wait(&sm.empty[slot], (lap - 1) & 1, abort, a.status))) return false;
+        if (lane == 0) mbar_arrive_expect_tx(&sm.full[slot], tile * 128);
+        __syncwarp();
+        if (lane * a.piece < tile)
+          tma_load_4d(sm.ring[slot] + lane * a.piece * 128, tm, &sm.full[slot], hf * 128, x.y, g, x.x);
+        __syncwarp();
+        ++issued;
+        if (++slot == NSLOT) slot = 0, ++lap;
+      }
+      return true;
+    };
+    fetch(0);
+    int2 cur = place(0), nxt;
+    fetch(1);
+    bool go = load(&P.tm_k, cur);
+    for (int j = 0; go && j < nt; ++j) {
+      nxt = place(j + 1);
+      fetch(j + 2);
+      if (j + 1 < nt) go = load(&P.tm_k, nxt);
+      go = go && load(&P.tm_v, cur);
+      cur = nxt;
+    }
+    // (a wait that gave up ends the kernel's work, not its copies in flight)
+    if (lane == 0)
+      for (int u = max(0, issued - NSLOT); u < issued; ++u) mbar_drain(&sm.full[u % NSLOT], (u / NSLOT) & 1);
+    __syncwarp();
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ the products
+    constexpr uint32_t idS = idesc_f8(128, 2 * R, 0, 0, 0, 0), idO = idesc_f8(128, R, 0, 1, 1, 1);
+    const uint64_t kd = sdesc_sw128(smem_u32(sm.ring[0]), 16, 1024), qd = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024);
+    const uint64_t pd = sdesc_plain_mn(smem_u32(sm.p[0][0]), 128, KT * 16);
+    int slot = 0, lap = 0;
+    bool ok = true;
+    auto wait_unit = [&]() -> bool {
+      if (!__all_sync(0xffffffffu, mbar_wait(&sm.full[slot], lap & 1, abort, a.status))) return false;
+      tc_fence_after();
+      return true;
+    };
+    auto done_unit = [&] {
+      tc_commit_w(&sm.empty[slot]);
+      if (++slot == NSLOT) slot = 0, ++lap;
+    };
+    auto issue_s = [&](int j) -> bool {
+      const int sb = j & 1;
+      if (j >= 2) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&sm.s_free[sb], ((j >> 1) - 1) & 1, abort, a.status))) return false;
+        tc_fence_after();
+      }
+#pragma unroll
+      for (int hf = 0; hf < HV; ++hf) {
+        if (!wait_unit()) return false;
+        const uint64_t kk = kd + (uint64_t)(slot * (kUnit / 16)), qq = qd + (uint64_t)(hf * (2 * R * 128 / 16));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma_f8_ss_w(tmem + sb * 2 * R, kk + i * 2, qq + i * 2, idS, hf + i > 0 ? 1u : 0u);
+        done_unit();
+      }
+      tc_commit_w(&sm.s_full[sb]);
+      return true;
+    };
+    auto issue_pv = [&](int j) -> bool {
+      const int pb = j & 1;
+      if (!__all_sync(0xffffffffu, mbar_wait(&sm.p_full[pb], (j >> 1) & 1, abort, a.status))) return false;
+      tc_fence_after();
+#pragma unroll
+      for (int hf = 0; hf < HV; ++hf) {
+        if (!wait_unit()) return false;
+        const uint64_t vv = kd + (uint64_t)(slot * (kUnit / 16)), pp = pd + (uint64_t)(pb * (3 * R * KT / 16));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int term = 0; term < 3; ++term)
+            mma_f8_ss_w(tmem + 4 * R + hf * R, vv + i * 256, pp + term * (R * KT / 16) + i * 32, idO,
+                        j > 0 || i + term > 0 ? 1u : 0u);
+        done_unit();
+      }
+      tc_commit_w(&sm.pv_done[pb]);
+      return true;
+    };
+    ok = issue_s(0);
+    for (int j = 0; ok && j < nt; ++j) {
+      if (j + 1 < nt) ok = issue_s(j + 1);
+      ok = ok && issue_pv(j);
+    }
+    tc_commit_w(&sm.drain);
+    mbar_drain(&sm.drain, 0);
+  } else {
+    // ------------------------------------------------------------ softmax: a thread per position
+    const int wg = (warp - 2) >> 2, q4 = warp & 3, key = q4 * 32 + lane, r0 = wg * RW, bar = 1 + wg;
+    const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
+    const int own_lo = (T - 1) * a.n, win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;
+    const int seen = a.mode == SFA_LOCAL ? own_lo - a.window + 1 : 0;
+    const uint32_t real = bits(0, rows - r0) & (RW == 32 ? 0xffffffffu : (1u << (RW & 31)) - 1);
+    // this key's page and row there, going on by a tile; its page entry two tiles ahead, its scales' bytes one
+    const int step_pages = fast_div(tile, a.pg.d_prow), step_rows = tile - step_pages * a.pg.prow;
+    int at_pos = k0 + key, at_page = fast_div(at_pos, a.pg.d_prow), at_row = at_pos - at_page * a.pg.prow;
+    int next_entry = -1, next_row = 0, kb = 127, vb = 127;
+    auto scale_entry = [&] {
+      next_entry = -1;
+      next_row = at_row;
+      if (key < tile && at_pos < k1 && at_pos >= seen && at_page < a.pg.max_pages) next_entry = table[at_page];
+      at_pos += tile;
+      at_page += step_pages;
+      at_row += step_rows;
+      if (at_row >= a.pg.prow) at_row -= a.pg.prow, ++at_page;
+    };
+    auto scale_bytes = [&] {
+      if ((unsigned)next_entry < (unsigned)a.pg.num_pages) {
+        const size_t at = ((size_t)next_entry * a.Hkv + g) * a.blocks + fast_div(next_row, a.d_brow);
+        kb = a.kscale[at];
+        vb = a.vscale[at];
+      }
+    };
+    scale_entry();
+    scale_bytes();
+    scale_entry();
+    float l[RW];
+#pragma unroll
+    for (int r = 0; r < RW; ++r) l[r] = 0.f;
+    uint32_t set = 0;  // rows whose reference is set
+    bool ok = true;
+    for (int j = 0; j < nt; ++j) {
+      const int sb = j & 1, base = k0 + j * tile, p = base + key;
+      kb = q8::clamp_byte(kb);
+      vb = q8::clamp_byte(vb);
+      const float kf = q8::scale_of(kb), ev = (float)(vb - 127), inv = q8::inverse_of(vb);
+      scale_bytes();
+      scale_entry();
+      // the rows that see this position: a range
+      uint32_t vis = real;
+      if (a.mode == SFA_WITHIN && a.n > 1) {
+        const int s = p - fast_div(p, a.d_n) * a.n;
+        vis &= bits(s * a.G - row0 - r0, (s + 1) * a.G - row0 - r0);
+      }
+      if (base + tile - 1 >= own_lo || base + tile > k1 || base <= win_hi || tile < KT) {
+        const int first = (p - own_lo) * a.G - row0 - r0;  // rows of the streams from p's own on, where p is the new token's
+        const int last = a.mode == SFA_LOCAL ? (int)min((long long)(p - own_lo + a.window) * a.G - row0 - r0, 64ll) : 64;
+        vis = key < tile && p < k1 ? vis & bits(p < own_lo ? 0 : first, last) : 0u;
+      }
+      // (A wait that gave up: the warp goes on to the group's next vote, since the others may wait for it there, and all
+      // leave after it.)
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.s_full[sb], (j >> 1) & 1, abort, a.status));
+      tc_fence_after();
+      float y[RW];
+      float top = ok ? -INFINITY : INFINITY;
+#pragma unroll
+      for (int c = 0; c < RW; c += 8) {
+        uint32_t hi[8], lo[8];
+        tmem_ld8(tl + sb * 2 * R + r0 + c, hi);
+        tmem_ld8(tl + sb * 2 * R + R + r0 + c, lo);
+        tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(sm.rowf + r0 + c + e);
+          const float4 rf = *reinterpret_cast<const float4*>(sm.ref + r0 + c + e);
+          const float ff[4] = {f.x, f.y, f.z, f.w}, rr[4] = {rf.x, rf.y, rf.z, rf.w};
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            const uint64_t h2 = f2pack(__uint_as_float(hi[e + i]), __uint_as_float(hi[e + i + 1]));
+            const uint64_t l2 = f2pack(__uint_as_float(lo[e + i]), __uint_as_float(lo[e + i + 1]));
+            const uint64_t s2 = fmul2(ffma2(l2, f2pack(1.f / kLo, 1.f / kLo), h2), f2pack(ff[i], ff[i + 1]));
+            f2unpack(ffma2(s2, f2pack(kf, kf), f2pack(ev - rr[i], ev - rr[i + 1])), y[c + e + i], y[c + e + i + 1]);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (!((vis >> (c + e)) & 1u)) y[c + e] = -INFINITY;
+          top = fmaxf(top, y[c + e]);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.s_free[sb]);
+      if (group_any(bar, top > kTop || (vis & ~set) != 0)) {
+        if (group_any(bar, !ok)) {
+          ok = false;
+          break;
+        }
+        // new references: each row's largest P to 2^kSet where it is above that, or the row's first
+        int last_set = 0;
+#pragma unroll
+        for (int r = 0; r < RW; ++r) {
+          const int m = __reduce_max_sync(0xffffffffu, ordered(y[r]));
+          if (lane == r % 32) sm.most[q4][r0 + r] = from_ordered(m);
+        }
+        named_bar_sync(bar, 128);
+        float fac[RW];
+        bool scale_o = false;
+#pragma unroll
+        for (int r = 0; r < RW; ++r) {
+          const float m = fmaxf(fmaxf(sm.most[0][r0 + r], sm.most[1][r0 + r]), fmaxf(sm.most[2][r0 + r], sm.most[3][r0 + r]));
+          const bool first = !((set >> r) & 1u);
+          const float up = m > -INFINITY && (first || m > kSet) ? m - kSet : 0.f;
+          if (m > -INFINITY) set |= 1u << r;
+          fac[r] = first ? 1.f : ex2_approx(-up);
+          scale_o = scale_o || fac[r] != 1.f;
+          y[r] -= up;
+          l[r] *= fac[r];
+          if (key == r) last_set = __float_as_int(up);
+        }
+        named_bar_sync(bar, 128);  // the maxima and the references are read
+        if (key < RW) sm.ref[r0 + key] += __int_as_float(last_set);
+        if (scale_o && j > 0) {
+          if (!__all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort, a.status))) ok = false;
+          if (ok) {
+            tc_fence_after();
+#pragma unroll
+            for (int hf = 0; hf < HV; ++hf)
+#pragma unroll
+              for (int c = 0; c < RW; c += 8) {
+                uint32_t o[8];
+                tmem_ld8(tl + 4 * R + hf * R + r0 + c, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fac[c + e]);
+                tmem_st8(tl + 4 * R + hf * R + r0 + c, o);
+              }
+            tmem_st_wait();
+          }
+        }
+        named_bar_sync(bar, 128);  // the new references are written
+      }
+      // this buffer of P is free once the products of the tile before the last are done
+      ok = ok && (j < 2 || __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[sb], ((j >> 1) - 1) & 1, abort, a.status)));
+      if (!ok) continue;
+#pragma unroll
+      for (int c = 0; c < RW; c += 8) {
+        uint2 t[3];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t hi[2], mid[2], lo[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int r = c + h * 4 + i * 2;
+            const float p0 = ex2_approx(y[r]), p1 = ex2_approx(y[r + 1]);
+            l[r] = fmaf(p0, inv, l[r]);
+            l[r + 1] = fmaf(p1, inv, l[r + 1]);
+            const __half2 u2 = __floats2half2_rn(p0, p1);
+            const uint32_t u = *reinterpret_cast<const uint32_t*>(&u2);
+            // e5m2 is the upper byte of f16: three bits, three of what is left, and the rest to the nearest
+            hi[i] = u & 0xff00ff00u;
+            const uint32_t v = hsub2(u, hi[i]);
+            mid[i] = v & 0xff00ff00u;
+            lo[i] = hsub2(v, mid[i]) + 0x00800080u;
+          }
+          (&t[0].x)[h] = __byte_perm(hi[0], hi[1], 0x7531);
+          (&t[1].x)[h] = __byte_perm(mid[0], mid[1], 0x7531);
+          (&t[2].x)[h] = __byte_perm(lo[0], lo[1], 0x7531);
+        }
+        const int rr = r0 + c, at = (rr >> 4) * (KT * 16) + key * 16 + (rr & 15);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>(sm.p[sb][i] + at) = t[i];
+      }
+      // The sequence's last tile holds positions behind its length, which may never have been written: their P is 0, and
+      // 0 times a NaN is NaN, so their V is zeroed before the product (which waits for this thread's arrival).
+      if (base + tile > k1 && wg == 0) {
+        // The ring's last units are this tile's V.  (A wait tells only a phase from the next: that every unit but V of this
+        // tile and the one before has landed is known here, and the slot's last unit is none of these.)
+        static_assert(NSLOT >= 2 * HV, "");
+#pragma unroll
+        for (int h = 0; h < HV; ++h) {
+          const int u = 2 * HV * nt - HV + h;
+          if (!__all_sync(0xffffffffu, mbar_wait(&sm.full[u % NSLOT], (u / NSLOT) & 1, abort, a.status))) ok = false;
+          if (ok && p >= k1)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) reinterpret_cast<uint4*>(sm.ring[u % NSLOT] + key * 128)[c] = make_uint4(0, 0, 0, 0);
+        }
+        __syncwarp();
+        if (!ok) continue;
+      }
+      fence_async_smem();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.p_full[sb]);
+    }
+    ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(nt - 1) & 1], ((nt - 1) >> 1) & 1, abort, a.status));
+    if (group_any(bar, !ok)) ok = false;  // (also: every thread has read the last references)
+    if (ok) {
+      tc_fence_after();
+      const bool bad = *(volatile int*)&sm.bad_page != 0;
+#pragma unroll
+      for (int hf = 0; hf < HV; ++hf)
+#pragma unroll
+        for (int c = 0; c < RW; c += 8) {
+          uint32_t o[8];
+          tmem_ld8(tl + 4 * R + hf * R + r0 + c, o);
+          tmem_ld_wait();
+          uint32_t wrong = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float x = __uint_as_float(o[e]);
+            po[(size_t)(r0 + c + e) * DH + hf * 128 + key] = x;
+            if (!(fabsf(x) <= FLT_MAX)) wrong |= 1u << e;
+          }
+          wrong = __reduce_or_sync(0xffffffffu, wrong);
+          if (wrong != 0 && lane == 0) {
+            const int at = r0 + c;
+            atomicOr(&sm.not_finite[at >> 5], wrong << (at & 31));
+          }
+        }
+      // sums over the positions: a warp's, then the four warps'
+#pragma unroll
+      for (int r = 0; r < RW; ++r) {
+        float x = l[r];
+#pragma unroll
+        for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        if (lane == r % 32) sm.most[q4][r0 + r] = x;
+      }
+      named_bar_sync(bar, 128);
+      if (key < RW) {
+        const int r = r0 + key;
+        float sum = (sm.most[0][r] + sm.most[1][r]) + (sm.most[2][r] + sm.most[3][r]);
+        float m = (set >> key) & 1u ? sm.ref[r] : -INFINITY;
+        if (sum != sum) m = INFINITY;  // a visible score that is not finite: the combined row is NaN
+        if (bad) m = -INFINITY, sum = decq8::kBadPage;
+        pml[r] = make_float2(m, sum);
+        if (a.nsplit == 1 && bad && key == 0) set_status(a.status, HD_DEVBIT_INDEX);
+      }
+      named_bar_sync(bar, 128);
+      if (!bad)
+#pragma unroll 1
+        for (int r = q4; r < RW; r += 4) {
+          const int row = r0 + r;
+          if (row < rows && (sm.not_finite[row >> 5] >> (row & 31)) & 1u)
+            decq8::exact_row<DH>(a, b, g, row0 + row, T, k0, k1, po + (size_t)row * DH, pml + row);
+        }
+      if (a.nsplit == 1) {  // the only split: its rows are the results
+        __syncwarp();
+        for (int r = q4; r < RW; r += 4) {
+          const int row = r0 + r;
+          if (row >= rows) break;
+          const float2 ml = pml[row];
+          decq8::store_row<DH>(a, b, g, row0 + row, po + (size_t)row * DH, ml.x, bad ? 0.f : ml.y);
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, C::kAlloc);
+  }
+}
+}  // namespace decq8tc
+
+// ------------------------------------------------------------------ host side
+
+
+template <int HV, int RW, int WG>
+static cudaError_t launch_t(const decq8::Params& p, cudaStream_t st) {
+  using namespace decq8tc;
+  using C = Cfg<HV, RW, WG>;
+  const int smem = (int)sizeof(Smem<HV, RW, WG>) + 1024;
+  static_assert(sizeof(Smem<HV, RW, WG>) + 1024 <= (C::kPerSm == 2 ? 113 : 227) * 1024 && C::NSLOT >= 3 && C::kCols <= C::kAlloc,
+                "an SM's CTAs fit");
+  cudaError_t e = cudaFuncSetAttribute(decode_q8_tc_kernel<HV, RW, WG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(true, decode_q8_tc_kernel<HV, RW, WG>, dim3((unsigned)p.a.nsplit * p.a.B * p.a.Hkv * p.a.ngroups),
+                       (unsigned)C::kThreads, smem, st, p);
+}
+
+int decode_q8_tc_per_sm(int rows, int Dh) {
+  using namespace decq8tc;
+  if (Dh == 128) return rows <= 16 ? Cfg<1, 16, 1>::kPerSm : rows <= 32 ? Cfg<1, 16, 2>::kPerSm : rows <= 48 ? Cfg<1, 24, 2>::kPerSm : Cfg<1, 16, 4>::kPerSm;
+  return rows <= 16 ? Cfg<2, 16, 1>::kPerSm : rows <= 32 ? Cfg<2, 16, 2>::kPerSm : rows <= 48 ? Cfg<2, 24, 2>::kPerSm : Cfg<2, 16, 4>::kPerSm;
+}
+
+template <int HV>
+static cudaError_t launch_h(const decq8::Params& p, cudaStream_t st) {
+  if (p.a.rg == 16) return launch_t<HV, 16, 1>(p, st);
+  if (p.a.rg == 32) return launch_t<HV, 16, 2>(p, st);
+  if (p.a.rg == 48) return launch_t<HV, 24, 2>(p, st);
+  return launch_t<HV, 16, 4>(p, st);
+}
+
+cudaError_t launch_decode_q8_tc(decq8::Params& p, int Dh, cudaStream_t st) {
+  return Dh == 128 ? launch_h<1>(p, st) : launch_h<2>(p, st);
+}
+
+}  // namespace hdsfa
