@@ -30,7 +30,8 @@ using decq8::Params;
 constexpr int KT = 128;            // positions of a tile
 constexpr int kUnit = KT * 128;    // bytes of a ring slot: 128 columns of a K or V tile
 constexpr float kTop = 15.f;       // P's largest exponent
-constexpr float kSet = 11.f;       // the exponent of a row's largest P when its reference is set
+constexpr float kSet = 7.f;        // the exponent of a row's largest P when its reference is set
+constexpr uint32_t kGaveUp = 1u << 31;  // beside the rows' bits
 constexpr float kLo = 16.f;        // scale of a query's second codes
 
 // HV: 128-column units of a tile (Dh / 128)
@@ -39,7 +40,7 @@ struct Cfg {
   static constexpr int R = RW * WG, kThreads = 64 + WG * 128;
   static constexpr int kCols = 4 * R + HV * R;  // tensor memory: two S, O
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr int kFixed = 2 * R * HV * 128 + 6 * R * KT + 2048;  // queries, P, the rest
+  static constexpr int kFixed = 2 * R * HV * 128 + 6 * R * KT + 3072;  // queries, P, the rest
   static constexpr int kPerSm = kAlloc <= 256 && kFixed + 3 * kUnit <= 112 * 1024 ? 2 : 1;
   static constexpr int kRoom = ((kPerSm == 2 ? 112 : 225) * 1024 - kFixed) / kUnit;
   static constexpr int NSLOT = kRoom < 10 ? kRoom : 10;
@@ -51,11 +52,12 @@ struct Smem {
   uint8_t ring[C::NSLOT][kUnit];             // [128 positions][128 bytes], 128-byte swizzle
   uint8_t q[HV][2 * C::R * 128];             // [R rows of hi, R of lo][128 bytes], 128-byte swizzle
   uint8_t p[2][3][C::R * KT];                // a buffer's hi, mid, lo: blocks of 16 rows, [128 positions][16 bytes]
-  float rowf[C::R], ref[C::R];               // a row's factor of q; its reference
+  float rowf[C::R], nref[C::R];              // a row's factor of q; its reference, negated
+  float up[C::R], fac[C::R];                 // what the reference goes up by, negated; 2^ that
   float most[4][C::R];                       // a warp's maxima, or sums
   uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], drain;
   uint32_t tmem_base;
-  unsigned not_finite[2];
+  unsigned not_finite[2], raise[WG];
   int abort, bad_page;
 };
 
@@ -84,6 +86,14 @@ HD_DEVINLINE void tmem_ld8(uint32_t taddr, uint32_t* r) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr));
 }
+// This warp's 32 lanes of a column of tensor memory, times f.
+HD_DEVINLINE void tmem_scale1(uint32_t taddr, float f) {
+  float x;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n" : "=f"(x) : "r"(taddr));
+  tmem_ld_wait();
+  x *= f;
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};\n" ::"r"(taddr), "f"(x) : "memory");
+}
 // Whether `v` holds for a thread of the 128 on hardware barrier `id`.
 HD_DEVINLINE bool group_any(int id, bool v) {
   uint32_t r;
@@ -100,6 +110,7 @@ HD_DEVINLINE int ordered(float x) {
   return i ^ ((i >> 31) & 0x7fffffff);
 }
 HD_DEVINLINE float from_ordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
+HD_DEVINLINE void l2_prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p)); }
 HD_DEVINLINE uint32_t hsub2(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(d) : "r"(a), "r"(b));
@@ -147,6 +158,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     mbar_init(&sm.drain, 1);
     sm.abort = sm.bad_page = 0;
     sm.not_finite[0] = sm.not_finite[1] = 0;
+    for (int i = 0; i < WG; ++i) sm.raise[i] = 0;
     fence_mbar_init();
   }
   if (warp == 0) {
@@ -197,7 +209,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       }
       if (lane == 0) {
         sm.rowf[rr] = back * a.scale_log2;
-        sm.ref[rr] = 0.f;
+        sm.nref[rr] = 0.f;
       }
     }
   fence_async_smem();
@@ -254,6 +266,18 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       }
       return true;
     };
+    // The tile's scales are a few bytes that the softmax warps load a tile ahead of their use, which is not early behind a
+    // saturated memory's queue: they are asked for into L2 with the tile.
+    auto prefetch_scales = [&](int j, int2 x) {
+      if (pos_of(j) < 0 || x.x >= a.pg.num_pages) return;
+      const size_t at = ((size_t)x.x * a.Hkv + g) * a.blocks;
+      const int first = fast_div(x.y, a.d_brow), last = fast_div(x.y + a.piece - 1, a.d_brow);
+      for (int i = first;; i = min(i + 32, last)) {
+        l2_prefetch(a.kscale + at + i);
+        l2_prefetch(a.vscale + at + i);
+        if (i == last) break;
+      }
+    };
     fetch(0);
     int2 cur = place(0), nxt;
     fetch(1);
@@ -261,7 +285,10 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     for (int j = 0; go && j < nt; ++j) {
       nxt = place(j + 1);
       fetch(j + 2);
-      if (j + 1 < nt) go = load(&P.tm_k, nxt);
+      if (j + 1 < nt) {
+        prefetch_scales(j + 1, nxt);
+        go = load(&P.tm_k, nxt);
+      }
       go = go && load(&P.tm_v, cur);
       cur = nxt;
     }
@@ -333,8 +360,8 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     const int wg = (warp - 2) >> 2, q4 = warp & 3, key = q4 * 32 + lane, r0 = wg * RW, bar = 1 + wg;
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
     const int own_lo = (T - 1) * a.n, win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;
-    const int seen = a.mode == SFA_LOCAL ? own_lo - a.window + 1 : 0;
     const uint32_t real = bits(0, rows - r0) & (RW == 32 ? 0xffffffffu : (1u << (RW & 31)) - 1);
+    const int seen = a.mode == SFA_LOCAL ? own_lo - a.window + 1 : 0;
     // this key's page and row there, going on by a tile; its page entry two tiles ahead, its scales' bytes one
     const int step_pages = fast_div(tile, a.pg.d_prow), step_rows = tile - step_pages * a.pg.prow;
     int at_pos = k0 + key, at_page = fast_div(at_pos, a.pg.d_prow), at_row = at_pos - at_page * a.pg.prow;
@@ -358,18 +385,14 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     scale_entry();
     scale_bytes();
     scale_entry();
-    float l[RW];
+    uint64_t l[RW / 2];  // pairs of rows' sums over this thread's positions
 #pragma unroll
-    for (int r = 0; r < RW; ++r) l[r] = 0.f;
+    for (int r = 0; r < RW / 2; ++r) l[r] = 0;
     uint32_t set = 0;  // rows whose reference is set
     bool ok = true;
     for (int j = 0; j < nt; ++j) {
       const int sb = j & 1, base = k0 + j * tile, p = base + key;
-      kb = q8::clamp_byte(kb);
-      vb = q8::clamp_byte(vb);
-      const float kf = q8::scale_of(kb), ev = (float)(vb - 127), inv = q8::inverse_of(vb);
-      scale_bytes();
-      scale_entry();
+      const uint32_t tS = tl + sb * 2 * R + r0;
       // the rows that see this position: a range
       uint32_t vis = real;
       if (a.mode == SFA_WITHIN && a.n > 1) {
@@ -385,88 +408,100 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       // leave after it.)
       ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.s_full[sb], (j >> 1) & 1, abort, a.status));
       tc_fence_after();
+      kb = q8::clamp_byte(kb);
+      vb = q8::clamp_byte(vb);
+      const float kf = q8::scale_of(kb), ev = (float)(vb - 127), inv = q8::inverse_of(vb);
+      scale_bytes();
+      scale_entry();
+      const uint64_t kf2 = f2pack(kf, kf), ev2 = f2pack(ev, ev), lo2 = f2pack(1.f / kLo, 1.f / kLo);
       float y[RW];
-      float top = ok ? -INFINITY : INFINITY;
+      {
+        uint32_t hi[RW], lo[RW];
 #pragma unroll
-      for (int c = 0; c < RW; c += 8) {
-        uint32_t hi[8], lo[8];
-        tmem_ld8(tl + sb * 2 * R + r0 + c, hi);
-        tmem_ld8(tl + sb * 2 * R + R + r0 + c, lo);
+        for (int c = 0; c < RW; c += 8) {
+          tmem_ld8(tS + c, hi + c);
+          tmem_ld8(tS + R + c, lo + c);
+        }
         tmem_ld_wait();
 #pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(sm.rowf + r0 + c + e);
-          const float4 rf = *reinterpret_cast<const float4*>(sm.ref + r0 + c + e);
-          const float ff[4] = {f.x, f.y, f.z, f.w}, rr[4] = {rf.x, rf.y, rf.z, rf.w};
+        for (int c = 0; c < RW; c += 4) {
+          const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(sm.rowf + r0 + c);
+          const ulonglong2 rf = *reinterpret_cast<const ulonglong2*>(sm.nref + r0 + c);
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
-            const uint64_t h2 = f2pack(__uint_as_float(hi[e + i]), __uint_as_float(hi[e + i + 1]));
-            const uint64_t l2 = f2pack(__uint_as_float(lo[e + i]), __uint_as_float(lo[e + i + 1]));
-            const uint64_t s2 = fmul2(ffma2(l2, f2pack(1.f / kLo, 1.f / kLo), h2), f2pack(ff[i], ff[i + 1]));
-            f2unpack(ffma2(s2, f2pack(kf, kf), f2pack(ev - rr[i], ev - rr[i + 1])), y[c + e + i], y[c + e + i + 1]);
+            const uint64_t h2 = f2pack(__uint_as_float(hi[c + i]), __uint_as_float(hi[c + i + 1]));
+            const uint64_t l2 = f2pack(__uint_as_float(lo[c + i]), __uint_as_float(lo[c + i + 1]));
+            const uint64_t s2 = fmul2(ffma2(l2, lo2, h2), i == 0 ? f.x : f.y);
+            f2unpack(ffma2(s2, kf2, fadd2(ev2, i == 0 ? rf.x : rf.y)), y[c + i], y[c + i + 1]);
           }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (!((vis >> (c + e)) & 1u)) y[c + e] = -INFINITY;
-          top = fmaxf(top, y[c + e]);
         }
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.s_free[sb]);
-      if (group_any(bar, top > kTop || (vis & ~set) != 0)) {
-        if (group_any(bar, !ok)) {
+      if (__any_sync(0xffffffffu, vis != real))
+#pragma unroll
+        for (int r = 0; r < RW; ++r)
+          if (!((vis >> r) & 1u)) y[r] = -INFINITY;
+      float top = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < RW; r += 2) top = max3(top, y[r], y[r + 1]);
+      if (group_any(bar, !ok || top > kTop || (vis & ~set) != 0)) {
+        // New references for the rows (of the whole group) of which some P would pass 2^kTop, or which have none yet:
+        // their largest P to 2^kSet.
+        uint32_t mask = ok ? vis & ~set : kGaveUp;
+#pragma unroll
+        for (int r = 0; r < RW; ++r)
+          if (y[r] > kTop) mask |= 1u << r;
+        mask = __reduce_or_sync(0xffffffffu, mask);
+        if (lane == 0 && mask != 0) atomicOr(&sm.raise[wg], mask);
+        named_bar_sync(bar, 128);
+        mask = *(volatile uint32_t*)&sm.raise[wg];
+        if (mask & kGaveUp) {
           ok = false;
           break;
         }
-        // new references: each row's largest P to 2^kSet where it is above that, or the row's first
-        int last_set = 0;
 #pragma unroll
-        for (int r = 0; r < RW; ++r) {
-          const int m = __reduce_max_sync(0xffffffffu, ordered(y[r]));
-          if (lane == r % 32) sm.most[q4][r0 + r] = from_ordered(m);
+        for (int r = 0; r < RW; ++r)
+          if ((mask >> r) & 1u) {
+            const int m = __reduce_max_sync(0xffffffffu, ordered(y[r] == y[r] ? y[r] : -INFINITY));
+            if (lane == 0) sm.most[q4][r0 + r] = from_ordered(m);
+          }
+        const bool scale_o = (mask & set) != 0 && j > 0;
+        if (scale_o) {  // (the products of the tile before the last are done, see below: so the wait is for the right phase)
+          ok = __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort, a.status));
+          tc_fence_after();
         }
         named_bar_sync(bar, 128);
-        float fac[RW];
-        bool scale_o = false;
-#pragma unroll
-        for (int r = 0; r < RW; ++r) {
-          const float m = fmaxf(fmaxf(sm.most[0][r0 + r], sm.most[1][r0 + r]), fmaxf(sm.most[2][r0 + r], sm.most[3][r0 + r]));
-          const bool first = !((set >> r) & 1u);
-          const float up = m > -INFINITY && (first || m > kSet) ? m - kSet : 0.f;
-          if (m > -INFINITY) set |= 1u << r;
-          fac[r] = first ? 1.f : ex2_approx(-up);
-          scale_o = scale_o || fac[r] != 1.f;
-          y[r] -= up;
-          l[r] *= fac[r];
-          if (key == r) last_set = __float_as_int(up);
+        if (key == 0) sm.raise[wg] = 0;
+        if (key < RW) {
+          const int r = r0 + key;
+          float down = 0.f;
+          if ((mask >> key) & 1u)
+            down = kSet - fmaxf(fmaxf(sm.most[0][r], sm.most[1][r]), fmaxf(sm.most[2][r], sm.most[3][r]));
+          sm.nref[r] += down;
+          sm.up[r] = down;
+          sm.fac[r] = (set >> key) & 1u ? ex2_approx(down) : 1.f;
         }
-        named_bar_sync(bar, 128);  // the maxima and the references are read
-        if (key < RW) sm.ref[r0 + key] += __int_as_float(last_set);
-        if (scale_o && j > 0) {
-          if (!__all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort, a.status))) ok = false;
-          if (ok) {
-            tc_fence_after();
+        named_bar_sync(bar, 128);
 #pragma unroll
-            for (int hf = 0; hf < HV; ++hf)
+        for (int r = 0; r < RW; r += 2) {
+          l[r / 2] = fmul2(l[r / 2], *reinterpret_cast<const uint64_t*>(sm.fac + r0 + r));
+          f2unpack(fadd2(f2pack(y[r], y[r + 1]), *reinterpret_cast<const uint64_t*>(sm.up + r0 + r)), y[r], y[r + 1]);
+        }
+        if (scale_o) {
+          for (uint32_t left = mask & set; left; left &= left - 1) {
+            const int r = __ffs(left) - 1;
 #pragma unroll
-              for (int c = 0; c < RW; c += 8) {
-                uint32_t o[8];
-                tmem_ld8(tl + 4 * R + hf * R + r0 + c, o);
-                tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fac[c + e]);
-                tmem_st8(tl + 4 * R + hf * R + r0 + c, o);
-              }
-            tmem_st_wait();
+            for (int hf = 0; hf < HV; ++hf) tmem_scale1(tl + 4 * R + hf * R + r0 + r, sm.fac[r0 + r]);
           }
+          tmem_st_wait();
         }
-        named_bar_sync(bar, 128);  // the new references are written
+        set |= mask;
       }
-      // this buffer of P is free once the products of the tile before the last are done
-      ok = ok && (j < 2 || __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[sb], ((j >> 1) - 1) & 1, abort, a.status)));
       if (!ok) continue;
+      // S of this tile was issued behind the products of the tile before the last, so these are done: P's buffer is free
+      const uint64_t inv2 = f2pack(inv, inv);
 #pragma unroll
       for (int c = 0; c < RW; c += 8) {
         uint2 t[3];
@@ -477,8 +512,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
           for (int i = 0; i < 2; ++i) {
             const int r = c + h * 4 + i * 2;
             const float p0 = ex2_approx(y[r]), p1 = ex2_approx(y[r + 1]);
-            l[r] = fmaf(p0, inv, l[r]);
-            l[r + 1] = fmaf(p1, inv, l[r + 1]);
+            l[r / 2] = ffma2(f2pack(p0, p1), inv2, l[r / 2]);
             const __half2 u2 = __floats2half2_rn(p0, p1);
             const uint32_t u = *reinterpret_cast<const uint32_t*>(&u2);
             // e5m2 is the upper byte of f16: three bits, three of what is left, and the rest to the nearest
@@ -545,7 +579,9 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       // sums over the positions: a warp's, then the four warps'
 #pragma unroll
       for (int r = 0; r < RW; ++r) {
-        float x = l[r];
+        float x, other;
+        if (r & 1) f2unpack(l[r / 2], other, x);
+        else f2unpack(l[r / 2], x, other);
 #pragma unroll
         for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
         if (lane == r % 32) sm.most[q4][r0 + r] = x;
@@ -554,7 +590,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       if (key < RW) {
         const int r = r0 + key;
         float sum = (sm.most[0][r] + sm.most[1][r]) + (sm.most[2][r] + sm.most[3][r]);
-        float m = (set >> key) & 1u ? sm.ref[r] : -INFINITY;
+        float m = (set >> key) & 1u ? -sm.nref[r] : -INFINITY;
         if (sum != sum) m = INFINITY;  // a visible score that is not finite: the combined row is NaN
         if (bad) m = -INFINITY, sum = decq8::kBadPage;
         pml[r] = make_float2(m, sum);
