@@ -624,7 +624,7 @@ hd_status_t sfa_kv_append_paged_q8(const void* k_new, const void* v_new, void* k
                                    int page_tokens, int max_pages, int n, int Hkv, int Dh, int block_tokens,
                                    int32_t* dev_status, cudaStream_t stream) {
   HD_NVTX_RANGE("sfa_kv_append_paged_q8");
-  if (!aligned16(k_pages) || !aligned16(v_pages) || k_scales == nullptr || v_scales == nullptr) return HD_ERR_INVALID_ARG;
+  if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_scales) || !aligned16(v_scales)) return HD_ERR_INVALID_ARG;
   if (!aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_or_null(offsets, 4) || !aligned_or_null(served, 4) ||
       !aligned_or_null(dev_status, 4))
     return HD_ERR_INVALID_ARG;
@@ -645,7 +645,7 @@ hd_status_t sfa_kv_read_paged_q8(const void* k_pages, const void* v_pages, const
                                  int max_pages, int n, int Hkv, int Dh, int block_tokens, int32_t* dev_status,
                                  cudaStream_t stream) {
   HD_NVTX_RANGE("sfa_kv_read_paged_q8");
-  if (!aligned16(k_pages) || !aligned16(v_pages) || k_scales == nullptr || v_scales == nullptr) return HD_ERR_INVALID_ARG;
+  if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_scales) || !aligned16(v_scales)) return HD_ERR_INVALID_ARG;
   if (!aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_to(offsets, 4) || !aligned_or_null(dev_status, 4))
     return HD_ERR_INVALID_ARG;
   if (N < 0) return HD_ERR_INVALID_ARG;
@@ -680,8 +680,8 @@ hd_status_t sfa_decode_paged_q8(const void* q, const void* k_pages, const void* 
                                 int window, void* workspace, size_t workspace_bytes, int32_t* dev_status,
                                 cudaStream_t stream) {
   HD_NVTX_RANGE("sfa_decode_paged_q8");
-  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o) || k_scales == nullptr ||
-      v_scales == nullptr)
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o) || !aligned16(k_scales) ||
+      !aligned16(v_scales))
     return HD_ERR_INVALID_ARG;
   if (!aligned_to(page_table, 4) || !aligned_to(lens, 4) || !aligned_or_null(lse, 4) || !aligned_or_null(dev_status, 4))
     return HD_ERR_INVALID_ARG;
@@ -701,7 +701,7 @@ hd_status_t hd_pages_copy_q8(void* k_pages, void* v_pages, uint8_t* k_scales, ui
                              int F, int num_pages, size_t page_bytes, size_t page_scales, int32_t* dev_status,
                              cudaStream_t stream) {
   HD_NVTX_RANGE("hd_pages_copy_q8");
-  if (!aligned16(k_pages) || !aligned16(v_pages) || k_scales == nullptr || v_scales == nullptr ||
+  if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_scales) || !aligned16(v_scales) ||
       !aligned_or_null(dev_status, 4))
     return HD_ERR_INVALID_ARG;
   if (F < 0 || num_pages <= 0 || page_bytes == 0 || page_bytes % 16 != 0 || page_scales == 0) return HD_ERR_INVALID_ARG;

@@ -560,10 +560,12 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
 // ------------------------------------------------------------------ host side
 
 namespace {
+// The sequences' shares of a balanced batch's splits, in front of the partials.
+constexpr size_t kShareBytes = dec::kBalancedSeqs * sizeof(int2);
 struct Q8Plan {
   int G, M, ngroups, rg, nsplit;
   size_t part_o_bytes, part_ml_bytes;
-  size_t bytes() const { return ((part_o_bytes + 255) & ~size_t(255)) + part_ml_bytes; }
+  size_t bytes() const { return kShareBytes + ((part_o_bytes + 255) & ~size_t(255)) + part_ml_bytes; }
 };
 }  // namespace
 
@@ -657,8 +659,9 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   a.lens = lens;
   a.o = (bf16*)o;
   a.lse = lse;
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + ((plan.part_o_bytes + 255) & ~size_t(255)));
+  a.share = static_cast<int2*>(ws);
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + kShareBytes);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + kShareBytes + ((plan.part_o_bytes + 255) & ~size_t(255)));
   a.status = status;
   a.B = B;
   a.maxT = maxT;
@@ -685,6 +688,9 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   const bool tma = a.piece >= decq8::kTmaRows && (Dh >= 128 || a.piece % 2 == 0);
   a.tile = tma ? KT / a.piece * a.piece : n <= KT ? KT / n * n : KT;  // cp.async: whole tokens where a tile holds one
   a.d_tile = make_fast_div((uint32_t)a.tile);
+  const long long range = q8_range(maxT, n, mode, window);
+  a.balanced = tc && B > 1 && B <= dec::kBalancedSeqs && plan.nsplit > 1 && range / plan.nsplit >= 4 * 64 &&
+               B * (range / a.tile + 1) < (1LL << 30);  // the tiles of all sequences, counted in 32 bits
   if (tma && (!make_q8_tmap(&p.tm_k, kc, num_pages, Hkv, a.pg.prow, Dh, a.piece) ||
               !make_q8_tmap(&p.tm_v, vc, num_pages, Hkv, a.pg.prow, Dh, a.piece)))
     return cudaErrorInvalidValue;

@@ -30,19 +30,20 @@ using decq8::Params;
 constexpr int KT = 128;            // positions of a tile
 constexpr int kUnit = KT * 128;    // bytes of a ring slot: 128 columns of a K or V tile
 constexpr float kTop = 15.f;       // P's largest exponent
-constexpr float kSet = 7.f;        // the exponent of a row's largest P when its reference is set
-constexpr uint32_t kGaveUp = 1u << 31;  // beside the rows' bits
-constexpr float kLo = 16.f;        // scale of a query's second codes
+constexpr float kSet = 5.f;        // the exponent of a row's largest P when its reference is set
+constexpr float kLow = 64.f;       // P's third codes hold so many times what they stand for
 
 // HV: 128-column units of a tile (Dh / 128)
 template <int HV, int RW, int WG>
 struct Cfg {
   static constexpr int R = RW * WG, kThreads = 64 + WG * 128;
-  static constexpr int kCols = 4 * R + HV * R;  // tensor memory: two S, O
+  static constexpr int kCols = 2 * R + 3 * HV * R;  // tensor memory: two S, three O
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr int kFixed = 2 * R * HV * 128 + 6 * R * KT + 3072;  // queries, P, the rest
-  static constexpr int kPerSm = kAlloc <= 256 && kFixed + 3 * kUnit <= 112 * 1024 ? 2 : 1;
-  static constexpr int kRoom = ((kPerSm == 2 ? 112 : 225) * 1024 - kFixed) / kUnit;
+  static constexpr int kFixed = 3 * R * HV * 128 + 6 * R * KT + 4 * KT * 14 + 4 * 8 * R + 1024;  // all but the ring
+  static constexpr int kPerSm = kAlloc <= 128 && kFixed + 3 * kUnit <= 74 * 1024    ? 3
+                                : kAlloc <= 256 && kFixed + 3 * kUnit <= 112 * 1024 ? 2
+                                                                                    : 1;
+  static constexpr int kRoom = ((kPerSm == 3 ? 74 : kPerSm == 2 ? 112 : 226) * 1024 - kFixed) / kUnit;
   static constexpr int NSLOT = kRoom < 10 ? kRoom : 10;
 };
 
@@ -50,15 +51,19 @@ template <int HV, int RW, int WG>
 struct Smem {
   using C = Cfg<HV, RW, WG>;
   uint8_t ring[C::NSLOT][kUnit];             // [128 positions][128 bytes], 128-byte swizzle
-  uint8_t q[HV][2 * C::R * 128];             // [R rows of hi, R of lo][128 bytes], 128-byte swizzle
+  uint8_t q[HV][3][C::R * 128];              // hi, mid, lo: [R rows][128 bytes], 128-byte swizzle
   uint8_t p[2][3][C::R * KT];                // a buffer's hi, mid, lo: blocks of 16 rows, [128 positions][16 bytes]
+  uint2 words[4][KT];                        // of tiles: the words of K's and V's scales that hold a position's byte
+  int entry[4][KT];                          // its page entry
+  uint16_t scale[4][KT];                     // its scale bytes, K's and V's above it
   float rowf[C::R], nref[C::R];              // a row's factor of q; its reference, negated
   float up[C::R], fac[C::R];                 // what the reference goes up by, negated; 2^ that
   float most[4][C::R];                       // a warp's maxima, or sums
-  uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], drain;
+  uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], sc_full[4], drain;
+  unsigned long long raise[WG];              // rows whose references go up
   uint32_t tmem_base;
-  unsigned not_finite[2], raise[WG];
-  int abort, bad_page;
+  unsigned not_finite[2];
+  int abort, bad_page, gave_up[WG];
 };
 
 // kind::f8f6f4, fp32 D: operand types 0 e4m3, 1 e5m2.
@@ -81,18 +86,17 @@ HD_DEVINLINE void mma_f8_ss_w(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, u
       " @e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accum));
 }
-HD_DEVINLINE void tmem_ld8(uint32_t taddr, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-               : "r"(taddr));
-}
-// This warp's 32 lanes of a column of tensor memory, times f.
-HD_DEVINLINE void tmem_scale1(uint32_t taddr, float f) {
-  float x;
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n" : "=f"(x) : "r"(taddr));
+// This warp's 32 lanes of N columns of tensor memory, STEP apart, times f.
+template <int N, int STEP>
+HD_DEVINLINE void tmem_scale(uint32_t taddr, float f) {
+  float x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n" : "=f"(x[i]) : "r"(taddr + i * STEP));
   tmem_ld_wait();
-  x *= f;
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};\n" ::"r"(taddr), "f"(x) : "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};\n" ::"r"(taddr + i * STEP), "f"(x[i] * f) : "memory");
 }
 // Whether `v` holds for a thread of the 128 on hardware barrier `id`.
 HD_DEVINLINE bool group_any(int id, bool v) {
@@ -110,17 +114,50 @@ HD_DEVINLINE int ordered(float x) {
   return i ^ ((i >> 31) & 0x7fffffff);
 }
 HD_DEVINLINE float from_ordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
-HD_DEVINLINE void l2_prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];\n" ::"l"(p)); }
 HD_DEVINLINE uint32_t hsub2(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
-// Bits [lo, hi) of 32, the range cut to them.
-HD_DEVINLINE uint32_t bits(int lo, int hi) {
-  lo = min(max(lo, 0), 32);
-  hi = min(max(hi, 0), 32);
-  return hi <= lo ? 0u : (uint32_t)((1ull << hi) - (1ull << lo));
+// A bit for each row of a warp group.
+template <int RW>
+struct Rows {
+  typedef uint32_t Mask;
+};
+template <>
+struct Rows<48> {
+  typedef uint64_t Mask;
+};
+// Bits [lo, hi) of RW, the range cut to them.
+template <int RW>
+HD_DEVINLINE typename Rows<RW>::Mask bits(int lo, int hi) {
+  lo = min(max(lo, 0), RW);
+  hi = min(max(hi, 0), RW);
+  return hi <= lo ? 0 : (typename Rows<RW>::Mask)((1ull << hi) - (1ull << lo));
+}
+HD_DEVINLINE uint32_t warp_or(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
+HD_DEVINLINE uint64_t warp_or(uint64_t x) {
+  return (uint64_t)__reduce_or_sync(0xffffffffu, (uint32_t)(x >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)x);
+}
+HD_DEVINLINE int first_bit(uint32_t x) { return __ffs(x) - 1; }
+HD_DEVINLINE int first_bit(uint64_t x) { return __ffsll((long long)x) - 1; }
+// `bytes` of four bytes, the others zero.
+HD_DEVINLINE void cp_async_4(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(bytes));
+}
+// Three e5m2 codes of each of two f16: e5m2 is the upper byte of f16, so three bits, three of what is left, and the rest
+// (times `f`, a power of two) to the nearest; each in the upper bytes of the halves.
+template <bool SCALE>
+HD_DEVINLINE void split3(uint32_t u, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  hi = u & 0xff00ff00u;
+  const uint32_t v = hsub2(u, hi);
+  mid = v & 0xff00ff00u;
+  lo = hsub2(v, mid);
+  if (SCALE) {
+    const __half2 f = __float2half2_rn(kLow);
+    asm("mul.rn.f16x2 %0, %0, %1;\n" : "+r"(lo) : "r"(*reinterpret_cast<const uint32_t*>(&f)));
+  }
+  lo += 0x00800080u;
 }
 
 template <int HV, int RW, int WG>
@@ -155,10 +192,11 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       mbar_init(&sm.p_full[i], 4 * WG);
       mbar_init(&sm.pv_done[i], 1);
     }
+    for (int i = 0; i < 4; ++i) mbar_init(&sm.sc_full[i], 4);
     mbar_init(&sm.drain, 1);
     sm.abort = sm.bad_page = 0;
     sm.not_finite[0] = sm.not_finite[1] = 0;
-    for (int i = 0; i < WG; ++i) sm.raise[i] = 0;
+    for (int i = 0; i < WG; ++i) sm.raise[i] = 0, sm.gave_up[i] = 0;
     fence_mbar_init();
   }
   if (warp == 0) {
@@ -171,10 +209,9 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
   }
   grid_dep_wait();
   grid_dep_launch();
-  const int b = fast_div(split, a.d_nsplit), T = a.lens[b];
+  const dec::PagedSplit share(a, split, blockIdx.x == 0 && warp == 0);
+  const int b = share.b, T = share.T, k0 = share.k0, k1 = share.k1;
   const int32_t* table = a.table + (long long)b * a.pg.max_pages;
-  int k0, k1;
-  dec::split_range<true>(a, T, split - b * a.nsplit, tile, k0, k1);
   const int nt = k0 < k1 ? fast_div(k1 - k0 + tile - 1, a.d_tile) : 0;
   // the queries: a warp per row
   if (nt > 0)
@@ -194,18 +231,18 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       most = __reduce_max_sync(0xffffffffu, most);
       // the exponent field of the largest magnitude, kept where both powers are normal
       const int e = min(max((int)(most >> 23), 20), 254);
-      const float to = __int_as_float(min(127 + 7 + 127 - e, 254) << 23);  // 2^(7 - (e - 127)), at most 2^127
-      const float back = __int_as_float(max(e - 7, 1) << 23);              // 2^(e - 127 - 7)
+      const float to = __int_as_float(min(127 + 14 + 127 - e, 254) << 23);  // 2^(14 - (e - 127)), at most 2^127
+      const float back = __int_as_float(max(e - 14, 1) << 23);              // 2^(e - 127 - 14)
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        const float x0 = __uint_as_float(w[i] << 16) * to, x1 = __uint_as_float(w[i] & 0xffff0000u) * to;
-        const uint32_t hi = q8::code2(x0, x1);
-        const float2 y = q8::values2((uint16_t)hi);
-        const uint32_t lo = q8::code2((x0 - y.x) * kLo, (x1 - y.y) * kLo);
+        const __half2 u = __floats2half2_rn(__uint_as_float(w[i] << 16) * to, __uint_as_float(w[i] & 0xffff0000u) * to);
+        uint32_t t[3];
+        split3<false>(*reinterpret_cast<const uint32_t*>(&u), t[0], t[1], t[2]);
         const int c = (lane * NP + i) * 2, at = (c & 127) >> 4, off = c & 15;  // column; its 16-byte chunk
-        uint8_t* blk = sm.q[c >> 7];
-        *reinterpret_cast<uint16_t*>(blk + rr * 128 + ((at ^ (rr & 7)) << 4) + off) = (uint16_t)hi;
-        *reinterpret_cast<uint16_t*>(blk + (R + rr) * 128 + ((at ^ (rr & 7)) << 4) + off) = (uint16_t)lo;
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+          *reinterpret_cast<uint16_t*>(sm.q[c >> 7][x] + rr * 128 + ((at ^ (rr & 7)) << 4) + off) =
+              (uint16_t)__byte_perm(t[x], 0, 0x31);
       }
       if (lane == 0) {
         sm.rowf[rr] = back * a.scale_log2;
@@ -266,18 +303,6 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       }
       return true;
     };
-    // The tile's scales are a few bytes that the softmax warps load a tile ahead of their use, which is not early behind a
-    // saturated memory's queue: they are asked for into L2 with the tile.
-    auto prefetch_scales = [&](int j, int2 x) {
-      if (pos_of(j) < 0 || x.x >= a.pg.num_pages) return;
-      const size_t at = ((size_t)x.x * a.Hkv + g) * a.blocks;
-      const int first = fast_div(x.y, a.d_brow), last = fast_div(x.y + a.piece - 1, a.d_brow);
-      for (int i = first;; i = min(i + 32, last)) {
-        l2_prefetch(a.kscale + at + i);
-        l2_prefetch(a.vscale + at + i);
-        if (i == last) break;
-      }
-    };
     fetch(0);
     int2 cur = place(0), nxt;
     fetch(1);
@@ -286,7 +311,6 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       nxt = place(j + 1);
       fetch(j + 2);
       if (j + 1 < nt) {
-        prefetch_scales(j + 1, nxt);
         go = load(&P.tm_k, nxt);
       }
       go = go && load(&P.tm_v, cur);
@@ -298,8 +322,8 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ the products
-    constexpr uint32_t idS = idesc_f8(128, 2 * R, 0, 0, 0, 0), idO = idesc_f8(128, R, 0, 1, 1, 1);
-    const uint64_t kd = sdesc_sw128(smem_u32(sm.ring[0]), 16, 1024), qd = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024);
+    constexpr uint32_t idS = idesc_f8(128, R, 0, 1, 0, 0), idO = idesc_f8(128, 3 * R, 0, 1, 1, 1);
+    const uint64_t kd = sdesc_sw128(smem_u32(sm.ring[0]), 16, 1024), qd = sdesc_sw128(smem_u32(sm.q[0][0]), 16, 1024);
     const uint64_t pd = sdesc_plain_mn(smem_u32(sm.p[0][0]), 128, KT * 16);
     int slot = 0, lap = 0;
     bool ok = true;
@@ -321,9 +345,12 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
 #pragma unroll
       for (int hf = 0; hf < HV; ++hf) {
         if (!wait_unit()) return false;
-        const uint64_t kk = kd + (uint64_t)(slot * (kUnit / 16)), qq = qd + (uint64_t)(hf * (2 * R * 128 / 16));
+        const uint64_t kk = kd + (uint64_t)(slot * (kUnit / 16)), qq = qd + (uint64_t)(hf * (3 * R * 128 / 16));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mma_f8_ss_w(tmem + sb * 2 * R, kk + i * 2, qq + i * 2, idS, hf + i > 0 ? 1u : 0u);
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int term = 0; term < 3; ++term)
+            mma_f8_ss_w(tmem + sb * R, kk + i * 2, qq + term * (R * 128 / 16) + i * 2, idS, hf + i + term > 0 ? 1u : 0u);
         done_unit();
       }
       tc_commit_w(&sm.s_full[sb]);
@@ -339,10 +366,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
         const uint64_t vv = kd + (uint64_t)(slot * (kUnit / 16)), pp = pd + (uint64_t)(pb * (3 * R * KT / 16));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int term = 0; term < 3; ++term)
-            mma_f8_ss_w(tmem + 4 * R + hf * R, vv + i * 256, pp + term * (R * KT / 16) + i * 32, idO,
-                        j > 0 || i + term > 0 ? 1u : 0u);
+          mma_f8_ss_w(tmem + 2 * R + hf * 3 * R, vv + i * 256, pp + i * 32, idO, j > 0 || i > 0 ? 1u : 0u);
         done_unit();
       }
       tc_commit_w(&sm.pv_done[pb]);
@@ -357,88 +381,109 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     mbar_drain(&sm.drain, 0);
   } else {
     // ------------------------------------------------------------ softmax: a thread per position
+    typedef typename Rows<RW>::Mask Mask;
     const int wg = (warp - 2) >> 2, q4 = warp & 3, key = q4 * 32 + lane, r0 = wg * RW, bar = 1 + wg;
-    const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
+    const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16), tO = tl + 2 * R + r0;
     const int own_lo = (T - 1) * a.n, win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;
-    const uint32_t real = bits(0, rows - r0) & (RW == 32 ? 0xffffffffu : (1u << (RW & 31)) - 1);
     const int seen = a.mode == SFA_LOCAL ? own_lo - a.window + 1 : 0;
-    // this key's page and row there, going on by a tile; its page entry two tiles ahead, its scales' bytes one
+    const Mask real = bits<RW>(0, rows - r0);
+    // The first group brings the keys' scales, by cp.async: behind a saturated memory's queue a load takes thousands of
+    // cycles.  At tile j a thread asks for the words that hold the bytes of tile j + 4 (cut to the scales' array; the bytes'
+    // place is kept) and for the page entry of tile j + 7, and hands on the bytes of tile j + 1.  The key's page and row go
+    // on by a tile.
     const int step_pages = fast_div(tile, a.pg.d_prow), step_rows = tile - step_pages * a.pg.prow;
     int at_pos = k0 + key, at_page = fast_div(at_pos, a.pg.d_prow), at_row = at_pos - at_page * a.pg.prow;
-    int next_entry = -1, next_row = 0, kb = 127, vb = 127;
-    auto scale_entry = [&] {
-      next_entry = -1;
-      next_row = at_row;
-      if (key < tile && at_pos < k1 && at_pos >= seen && at_page < a.pg.max_pages) next_entry = table[at_page];
+    uint32_t places = 0;
+    const size_t scales = (size_t)a.pg.num_pages * a.Hkv * a.blocks;
+    auto use = [&](int pos, int page) { return key < tile && pos < k1 && pos >= seen && page < a.pg.max_pages; };
+    auto scale_copy = [&](int j, int entry) {  // tile j's, whose position at_pos is
+      if (use(at_pos, at_page) && (unsigned)entry < (unsigned)a.pg.num_pages) {
+        const size_t at = ((size_t)entry * a.Hkv + g) * a.blocks + fast_div(at_row, a.d_brow), word = at & ~(size_t)3;
+        const int bytes = (int)min(scales - word, (size_t)4), sh = (j & 3) * 2;
+        const uint32_t to = smem_u32(&sm.words[j & 3][key]);
+        cp_async_4(to, a.kscale + word, bytes);
+        cp_async_4(to + 4, a.vscale + word, bytes);
+        places = (places & ~(3u << sh)) | (uint32_t)(at & 3) << sh;
+      }
       at_pos += tile;
       at_page += step_pages;
       at_row += step_rows;
       if (at_row >= a.pg.prow) at_row -= a.pg.prow, ++at_page;
     };
-    auto scale_bytes = [&] {
-      if ((unsigned)next_entry < (unsigned)a.pg.num_pages) {
-        const size_t at = ((size_t)next_entry * a.Hkv + g) * a.blocks + fast_div(next_row, a.d_brow);
-        kb = a.kscale[at];
-        vb = a.vscale[at];
-      }
+    auto entry_copy = [&](int j) {
+      const int pos = k0 + j * tile + key, page = fast_div(pos, a.pg.d_prow);
+      if (use(pos, page)) cp_async_4(smem_u32(&sm.entry[j & 3][key]), table + page, 4);
+      cp_async_commit();
     };
-    scale_entry();
-    scale_bytes();
-    scale_entry();
+    auto hand_on = [&](int j) {  // tile j's bytes, from its words
+      const uint2 x = sm.words[j & 3][key];
+      const int sh = (places >> (j & 3) * 2 & 3) * 8;
+      sm.scale[j & 3][key] = (uint16_t)(q8::clamp_byte(x.x >> sh & 255) | q8::clamp_byte(x.y >> sh & 255) << 8);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.sc_full[j & 3]);
+    };
+    if (wg == 0) {
+      int first[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int pos = k0 + j * tile + key, page = fast_div(pos, a.pg.d_prow);
+        first[j] = use(pos, page) ? table[page] : -1;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        scale_copy(j, first[j]);
+        if (j > 0) entry_copy(j + 3);
+        else cp_async_commit();
+      }
+      cp_async_wait<3>();
+      hand_on(0);
+    }
     uint64_t l[RW / 2];  // pairs of rows' sums over this thread's positions
 #pragma unroll
     for (int r = 0; r < RW / 2; ++r) l[r] = 0;
-    uint32_t set = 0;  // rows whose reference is set
+    Mask set = 0;  // rows whose reference is set
     bool ok = true;
     for (int j = 0; j < nt; ++j) {
       const int sb = j & 1, base = k0 + j * tile, p = base + key;
-      const uint32_t tS = tl + sb * 2 * R + r0;
+      if (wg == 0) {
+        cp_async_wait<2>();  // what was asked for at tile j - 3
+        hand_on(j + 1);
+        scale_copy(j + 4, sm.entry[(j + 4) & 3][key]);
+        entry_copy(j + 7);
+      }
       // the rows that see this position: a range
-      uint32_t vis = real;
+      Mask vis = real;
       if (a.mode == SFA_WITHIN && a.n > 1) {
         const int s = p - fast_div(p, a.d_n) * a.n;
-        vis &= bits(s * a.G - row0 - r0, (s + 1) * a.G - row0 - r0);
+        vis &= bits<RW>(s * a.G - row0 - r0, (s + 1) * a.G - row0 - r0);
       }
-      if (base + tile - 1 >= own_lo || base + tile > k1 || base <= win_hi || tile < KT) {
+      if (base + tile - 1 > own_lo || base + tile > k1 || base <= win_hi || tile < KT) {
         const int first = (p - own_lo) * a.G - row0 - r0;  // rows of the streams from p's own on, where p is the new token's
         const int last = a.mode == SFA_LOCAL ? (int)min((long long)(p - own_lo + a.window) * a.G - row0 - r0, 64ll) : 64;
-        vis = key < tile && p < k1 ? vis & bits(p < own_lo ? 0 : first, last) : 0u;
+        vis = key < tile && p < k1 ? vis & bits<RW>(p < own_lo ? 0 : first, last) : (Mask)0;
       }
       // (A wait that gave up: the warp goes on to the group's next vote, since the others may wait for it there, and all
       // leave after it.)
       ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.s_full[sb], (j >> 1) & 1, abort, a.status));
       tc_fence_after();
-      kb = q8::clamp_byte(kb);
-      vb = q8::clamp_byte(vb);
+      if (wg > 0) ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.sc_full[j & 3], (j >> 2) & 1, abort, a.status));
+      const int sc = sm.scale[j & 3][key], kb = sc & 255, vb = sc >> 8;
       const float kf = q8::scale_of(kb), ev = (float)(vb - 127), inv = q8::inverse_of(vb);
-      scale_bytes();
-      scale_entry();
-      const uint64_t kf2 = f2pack(kf, kf), ev2 = f2pack(ev, ev), lo2 = f2pack(1.f / kLo, 1.f / kLo);
+      const uint64_t kf2 = f2pack(kf, kf), ev2 = f2pack(ev, ev);
       float y[RW];
-      {
-        uint32_t hi[RW], lo[RW];
 #pragma unroll
-        for (int c = 0; c < RW; c += 8) {
-          tmem_ld8(tS + c, hi + c);
-          tmem_ld8(tS + R + c, lo + c);
-        }
-        tmem_ld_wait();
-#pragma unroll
-        for (int c = 0; c < RW; c += 4) {
-          const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(sm.rowf + r0 + c);
-          const ulonglong2 rf = *reinterpret_cast<const ulonglong2*>(sm.nref + r0 + c);
-#pragma unroll
-          for (int i = 0; i < 4; i += 2) {
-            const uint64_t h2 = f2pack(__uint_as_float(hi[c + i]), __uint_as_float(hi[c + i + 1]));
-            const uint64_t l2 = f2pack(__uint_as_float(lo[c + i]), __uint_as_float(lo[c + i + 1]));
-            const uint64_t s2 = fmul2(ffma2(l2, lo2, h2), i == 0 ? f.x : f.y);
-            f2unpack(ffma2(s2, kf2, fadd2(ev2, i == 0 ? rf.x : rf.y)), y[c + i], y[c + i + 1]);
-          }
-        }
-      }
+      for (int c = 0; c < RW; c += 16) tmem_ld16(tl + sb * R + r0 + c, reinterpret_cast<uint32_t*>(y) + c);
+      tmem_ld_wait();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.s_free[sb]);
+#pragma unroll
+      for (int c = 0; c < RW; c += 4) {
+        const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(sm.rowf + r0 + c);
+        const ulonglong2 rf = *reinterpret_cast<const ulonglong2*>(sm.nref + r0 + c);
+        f2unpack(ffma2(fmul2(f2pack(y[c], y[c + 1]), f.x), kf2, fadd2(ev2, rf.x)), y[c], y[c + 1]);
+        f2unpack(ffma2(fmul2(f2pack(y[c + 2], y[c + 3]), f.y), kf2, fadd2(ev2, rf.y)), y[c + 2], y[c + 3]);
+      }
       if (__any_sync(0xffffffffu, vis != real))
 #pragma unroll
         for (int r = 0; r < RW; ++r)
@@ -449,15 +494,18 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       if (group_any(bar, !ok || top > kTop || (vis & ~set) != 0)) {
         // New references for the rows (of the whole group) of which some P would pass 2^kTop, or which have none yet:
         // their largest P to 2^kSet.
-        uint32_t mask = ok ? vis & ~set : kGaveUp;
+        Mask mask = vis & ~set;
 #pragma unroll
         for (int r = 0; r < RW; ++r)
-          if (y[r] > kTop) mask |= 1u << r;
-        mask = __reduce_or_sync(0xffffffffu, mask);
-        if (lane == 0 && mask != 0) atomicOr(&sm.raise[wg], mask);
+          if (y[r] > kTop) mask |= (Mask)1 << r;
+        mask = warp_or(mask);
+        if (lane == 0) {
+          if (mask != 0) atomicOr(&sm.raise[wg], (unsigned long long)mask);
+          if (!ok) sm.gave_up[wg] = 1;
+        }
         named_bar_sync(bar, 128);
-        mask = *(volatile uint32_t*)&sm.raise[wg];
-        if (mask & kGaveUp) {
+        mask = (Mask)*(volatile unsigned long long*)&sm.raise[wg];
+        if (*(volatile int*)&sm.gave_up[wg]) {
           ok = false;
           break;
         }
@@ -490,10 +538,9 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
           f2unpack(fadd2(f2pack(y[r], y[r + 1]), *reinterpret_cast<const uint64_t*>(sm.up + r0 + r)), y[r], y[r + 1]);
         }
         if (scale_o) {
-          for (uint32_t left = mask & set; left; left &= left - 1) {
-            const int r = __ffs(left) - 1;
-#pragma unroll
-            for (int hf = 0; hf < HV; ++hf) tmem_scale1(tl + 4 * R + hf * R + r0 + r, sm.fac[r0 + r]);
+          for (Mask left = mask & set; left; left &= left - 1) {
+            const int r = first_bit(left);
+            tmem_scale<3 * HV, R>(tO + r, sm.fac[r0 + r]);
           }
           tmem_st_wait();
         }
@@ -503,42 +550,38 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       // S of this tile was issued behind the products of the tile before the last, so these are done: P's buffer is free
       const uint64_t inv2 = f2pack(inv, inv);
 #pragma unroll
-      for (int c = 0; c < RW; c += 8) {
-        uint2 t[3];
+      for (int c = 0; c < RW; c += 16) {
+        uint4 t[3];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 4; ++h) {
           uint32_t hi[2], mid[2], lo[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int r = c + h * 4 + i * 2;
             const float p0 = ex2_approx(y[r]), p1 = ex2_approx(y[r + 1]);
             l[r / 2] = ffma2(f2pack(p0, p1), inv2, l[r / 2]);
-            const __half2 u2 = __floats2half2_rn(p0, p1);
-            const uint32_t u = *reinterpret_cast<const uint32_t*>(&u2);
-            // e5m2 is the upper byte of f16: three bits, three of what is left, and the rest to the nearest
-            hi[i] = u & 0xff00ff00u;
-            const uint32_t v = hsub2(u, hi[i]);
-            mid[i] = v & 0xff00ff00u;
-            lo[i] = hsub2(v, mid[i]) + 0x00800080u;
+            const __half2 u = __floats2half2_rn(p0, p1);
+            split3<true>(*reinterpret_cast<const uint32_t*>(&u), hi[i], mid[i], lo[i]);
           }
           (&t[0].x)[h] = __byte_perm(hi[0], hi[1], 0x7531);
           (&t[1].x)[h] = __byte_perm(mid[0], mid[1], 0x7531);
           (&t[2].x)[h] = __byte_perm(lo[0], lo[1], 0x7531);
         }
-        const int rr = r0 + c, at = (rr >> 4) * (KT * 16) + key * 16 + (rr & 15);
+        const int at = ((r0 + c) >> 4) * (KT * 16) + key * 16;
 #pragma unroll
-        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>(sm.p[sb][i] + at) = t[i];
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4*>(sm.p[sb][i] + at) = t[i];
       }
       // The sequence's last tile holds positions behind its length, which may never have been written: their P is 0, and
       // 0 times a NaN is NaN, so their V is zeroed before the product (which waits for this thread's arrival).
       if (base + tile > k1 && wg == 0) {
-        // The ring's last units are this tile's V.  (A wait tells only a phase from the next: that every unit but V of this
-        // tile and the one before has landed is known here, and the slot's last unit is none of these.)
-        static_assert(NSLOT >= 2 * HV, "");
+        // The ring's last units are this tile's V.  (A wait tells only a phase from the next: with the products of the
+        // tile before done, all units but these have landed.)
+        if (nt >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[nt & 1], ((nt - 2) >> 1) & 1, abort, a.status));
+        static_assert(NSLOT >= HV, "");
 #pragma unroll
         for (int h = 0; h < HV; ++h) {
           const int u = 2 * HV * nt - HV + h;
-          if (!__all_sync(0xffffffffu, mbar_wait(&sm.full[u % NSLOT], (u / NSLOT) & 1, abort, a.status))) ok = false;
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.full[u % NSLOT], (u / NSLOT) & 1, abort, a.status));
           if (ok && p >= k1)
 #pragma unroll
             for (int c = 0; c < 8; ++c) reinterpret_cast<uint4*>(sm.ring[u % NSLOT] + key * 128)[c] = make_uint4(0, 0, 0, 0);
@@ -551,6 +594,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.p_full[sb]);
     }
+    cp_async_wait<0>();
     ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(nt - 1) & 1], ((nt - 1) >> 1) & 1, abort, a.status));
     if (group_any(bar, !ok)) ok = false;  // (also: every thread has read the last references)
     if (ok) {
@@ -559,14 +603,15 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
 #pragma unroll
       for (int hf = 0; hf < HV; ++hf)
 #pragma unroll
-        for (int c = 0; c < RW; c += 8) {
-          uint32_t o[8];
-          tmem_ld8(tl + 4 * R + hf * R + r0 + c, o);
+        for (int c = 0; c < RW; c += 16) {
+          uint32_t o[3][16];
+#pragma unroll
+          for (int i = 0; i < 3; ++i) tmem_ld16(tO + (hf * 3 + i) * R + c, o[i]);
           tmem_ld_wait();
           uint32_t wrong = 0;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float x = __uint_as_float(o[e]);
+          for (int e = 0; e < 16; ++e) {
+            const float x = fmaf(__uint_as_float(o[2][e]), 1.f / kLow, __uint_as_float(o[0][e]) + __uint_as_float(o[1][e]));
             po[(size_t)(r0 + c + e) * DH + hf * 128 + key] = x;
             if (!(fabsf(x) <= FLT_MAX)) wrong |= 1u << e;
           }
@@ -633,7 +678,8 @@ static cudaError_t launch_t(const decq8::Params& p, cudaStream_t st) {
   using namespace decq8tc;
   using C = Cfg<HV, RW, WG>;
   const int smem = (int)sizeof(Smem<HV, RW, WG>) + 1024;
-  static_assert(sizeof(Smem<HV, RW, WG>) + 1024 <= (C::kPerSm == 2 ? 113 : 227) * 1024 && C::NSLOT >= 3 && C::kCols <= C::kAlloc,
+  static_assert(sizeof(Smem<HV, RW, WG>) + 1024 <= (C::kPerSm == 3 ? 75 : C::kPerSm == 2 ? 113 : 227) * 1024 && C::NSLOT >= 3 &&
+                    C::kCols <= C::kAlloc && C::kPerSm * C::kAlloc <= 512,
                 "an SM's CTAs fit");
   cudaError_t e = cudaFuncSetAttribute(decode_q8_tc_kernel<HV, RW, WG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
@@ -643,15 +689,15 @@ static cudaError_t launch_t(const decq8::Params& p, cudaStream_t st) {
 
 int decode_q8_tc_per_sm(int rows, int Dh) {
   using namespace decq8tc;
-  if (Dh == 128) return rows <= 16 ? Cfg<1, 16, 1>::kPerSm : rows <= 32 ? Cfg<1, 16, 2>::kPerSm : rows <= 48 ? Cfg<1, 24, 2>::kPerSm : Cfg<1, 16, 4>::kPerSm;
-  return rows <= 16 ? Cfg<2, 16, 1>::kPerSm : rows <= 32 ? Cfg<2, 16, 2>::kPerSm : rows <= 48 ? Cfg<2, 24, 2>::kPerSm : Cfg<2, 16, 4>::kPerSm;
+  if (Dh == 128) return rows <= 16 ? Cfg<1, 16, 1>::kPerSm : rows <= 32 ? Cfg<1, 16, 2>::kPerSm : rows <= 48 ? Cfg<1, 16, 3>::kPerSm : Cfg<1, 16, 4>::kPerSm;
+  return rows <= 16 ? Cfg<2, 16, 1>::kPerSm : rows <= 32 ? Cfg<2, 16, 2>::kPerSm : rows <= 48 ? Cfg<2, 16, 3>::kPerSm : Cfg<2, 16, 4>::kPerSm;
 }
 
 template <int HV>
 static cudaError_t launch_h(const decq8::Params& p, cudaStream_t st) {
   if (p.a.rg == 16) return launch_t<HV, 16, 1>(p, st);
   if (p.a.rg == 32) return launch_t<HV, 16, 2>(p, st);
-  if (p.a.rg == 48) return launch_t<HV, 24, 2>(p, st);
+  if (p.a.rg == 48) return launch_t<HV, 16, 3>(p, st);
   return launch_t<HV, 16, 4>(p, st);
 }
 
