@@ -14,7 +14,7 @@ constexpr uint32_t kNoRow = 0xffffffffu;
 struct Args : DecodeArgs {
   const uint8_t *kcodes, *vcodes, *kscale, *vscale;
   int blocks;       // blocks of a page
-  FastDiv d_brow;   // rows of a block
+  FastDiv d_brow, d_blocks;  // rows of a block; blocks of a page
   int mt, sets;     // row tiles of a CTA; sets of 4 mt warps
 };
 struct Params {

@@ -655,6 +655,7 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   a.vscale = vs;
   a.blocks = P / T;
   a.d_brow = make_fast_div((uint32_t)(T * n));
+  a.d_blocks = make_fast_div((uint32_t)a.blocks);
   a.mt = plan.rg / 16;
   a.lens = lens;
   a.o = (bf16*)o;

@@ -39,7 +39,7 @@ struct Cfg {
   static constexpr int R = RW * WG, kThreads = 64 + WG * 128;
   static constexpr int kCols = 2 * R + 3 * HV * R;  // tensor memory: two S, three O
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr int kFixed = 3 * R * HV * 128 + 6 * R * KT + 4 * KT * 14 + 4 * 8 * R + 1024;  // all but the ring
+  static constexpr int kFixed = 3 * R * HV * 128 + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 8 * R + 512;  // all but the ring
   static constexpr int kPerSm = kAlloc <= 128 && kFixed + 3 * kUnit <= 74 * 1024    ? 3
                                 : kAlloc <= 256 && kFixed + 3 * kUnit <= 112 * 1024 ? 2
                                                                                     : 1;
@@ -53,13 +53,13 @@ struct Smem {
   uint8_t ring[C::NSLOT][kUnit];             // [128 positions][128 bytes], 128-byte swizzle
   uint8_t q[HV][3][C::R * 128];              // hi, mid, lo: [R rows][128 bytes], 128-byte swizzle
   uint8_t p[2][3][C::R * KT];                // a buffer's hi, mid, lo: blocks of 16 rows, [128 positions][16 bytes]
-  uint2 words[4][KT];                        // of tiles: the words of K's and V's scales that hold a position's byte
-  int entry[4][KT];                          // its page entry
-  uint16_t scale[4][KT];                     // its scale bytes, K's and V's above it
+  uint2 words[4][128];                       // of chunks: the words of K's and V's scales that hold a block's byte
+  int entry[4][128];                         // its page entry
+  uint16_t scale[8 * 128];                   // blocks' scale bytes, K's and V's above it
   float rowf[C::R], nref[C::R];              // a row's factor of q; its reference, negated
   float up[C::R], fac[C::R];                 // what the reference goes up by, negated; 2^ that
   float most[4][C::R];                       // a warp's maxima, or sums
-  uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], sc_full[4], drain;
+  uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], sc_full[8], drain;
   unsigned long long raise[WG];              // rows whose references go up
   uint32_t tmem_base;
   unsigned not_finite[2];
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       mbar_init(&sm.p_full[i], 4 * WG);
       mbar_init(&sm.pv_done[i], 1);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(&sm.sc_full[i], 4);
+    for (int i = 0; i < 8; ++i) mbar_init(&sm.sc_full[i], 4);
     mbar_init(&sm.drain, 1);
     sm.abort = sm.bad_page = 0;
     sm.not_finite[0] = sm.not_finite[1] = 0;
@@ -387,70 +387,76 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     const int own_lo = (T - 1) * a.n, win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;
     const int seen = a.mode == SFA_LOCAL ? own_lo - a.window + 1 : 0;
     const Mask real = bits<RW>(0, rows - r0);
-    // The first group brings the keys' scales, by cp.async: behind a saturated memory's queue a load takes thousands of
-    // cycles.  At tile j a thread asks for the words that hold the bytes of tile j + 4 (cut to the scales' array; the bytes'
-    // place is kept) and for the page entry of tile j + 7, and hands on the bytes of tile j + 1.  The key's page and row go
-    // on by a tile.
-    const int step_pages = fast_div(tile, a.pg.d_prow), step_rows = tile - step_pages * a.pg.prow;
-    int at_pos = k0 + key, at_page = fast_div(at_pos, a.pg.d_prow), at_row = at_pos - at_page * a.pg.prow;
+    // The first group brings the scales, 128 blocks (a chunk) at a time, a thread each, by cp.async: behind a saturated
+    // memory's queue a load takes thousands of cycles.  Blocks are counted from the split's first.  As chunk c is handed on,
+    // the words that hold the bytes of chunk c + 3 are asked for (cut to the scales' array; a byte's place is kept), and
+    // the page entries of chunk c + 6.
+    const int b0 = fast_div(k0, a.d_brow), nblocks = fast_div(k1 - 1, a.d_brow) - b0 + 1;
+    const int b_seen = seen <= 0 ? 0 : fast_div(seen, a.d_brow) - b0;  // the first that a row sees
     uint32_t places = 0;
-    const size_t scales = (size_t)a.pg.num_pages * a.Hkv * a.blocks;
-    auto use = [&](int pos, int page) { return key < tile && pos < k1 && pos >= seen && page < a.pg.max_pages; };
-    auto scale_copy = [&](int j, int entry) {  // tile j's, whose position at_pos is
-      if (use(at_pos, at_page) && (unsigned)entry < (unsigned)a.pg.num_pages) {
-        const size_t at = ((size_t)entry * a.Hkv + g) * a.blocks + fast_div(at_row, a.d_brow), word = at & ~(size_t)3;
-        const int bytes = (int)min(scales - word, (size_t)4), sh = (j & 3) * 2;
-        const uint32_t to = smem_u32(&sm.words[j & 3][key]);
+    int handed = 0;
+    auto page_of = [&](int x, int& in) {  // of block x; -1: none that is needed
+      if (x >= nblocks || x < b_seen) return -1;
+      const int pg = fast_div(b0 + x, a.d_blocks);
+      in = b0 + x - pg * a.blocks;
+      return pg < a.pg.max_pages ? pg : -1;
+    };
+    auto chunk_words = [&](int c, int entry) {
+      int in = 0;
+      if (page_of(c * 128 + key, in) >= 0 && (unsigned)entry < (unsigned)a.pg.num_pages) {
+        const size_t at = ((size_t)entry * a.Hkv + g) * a.blocks + in, word = at & ~(size_t)3;
+        const int bytes = (int)min((size_t)a.pg.num_pages * a.Hkv * a.blocks - word, (size_t)4), sh = (c & 3) * 2;
+        const uint32_t to = smem_u32(&sm.words[c & 3][key]);
         cp_async_4(to, a.kscale + word, bytes);
         cp_async_4(to + 4, a.vscale + word, bytes);
         places = (places & ~(3u << sh)) | (uint32_t)(at & 3) << sh;
       }
-      at_pos += tile;
-      at_page += step_pages;
-      at_row += step_rows;
-      if (at_row >= a.pg.prow) at_row -= a.pg.prow, ++at_page;
     };
-    auto entry_copy = [&](int j) {
-      const int pos = k0 + j * tile + key, page = fast_div(pos, a.pg.d_prow);
-      if (use(pos, page)) cp_async_4(smem_u32(&sm.entry[j & 3][key]), table + page, 4);
+    auto chunk_entries = [&](int c) {
+      int in = 0;
+      const int pg = page_of(c * 128 + key, in);
+      if (pg >= 0) cp_async_4(smem_u32(&sm.entry[c & 3][key]), table + pg, 4);
+    };
+    auto hand_on = [&] {  // the next chunk's bytes
+      cp_async_wait<2>();
+      const int c = handed++;
+      const uint2 x = sm.words[c & 3][key];
+      const int sh = (places >> (c & 3) * 2 & 3) * 8;
+      sm.scale[(c & 7) * 128 + key] = (uint16_t)(q8::clamp_byte(x.x >> sh & 255) | q8::clamp_byte(x.y >> sh & 255) << 8);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.sc_full[c & 7]);
+      chunk_words(c + 3, sm.entry[(c + 3) & 3][key]);
+      chunk_entries(c + 6);
       cp_async_commit();
     };
-    auto hand_on = [&](int j) {  // tile j's bytes, from its words
-      const uint2 x = sm.words[j & 3][key];
-      const int sh = (places >> (j & 3) * 2 & 3) * 8;
-      sm.scale[j & 3][key] = (uint16_t)(q8::clamp_byte(x.x >> sh & 255) | q8::clamp_byte(x.y >> sh & 255) << 8);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.sc_full[j & 3]);
-    };
     if (wg == 0) {
-      int first[4];
+      int first[3], in = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int pos = k0 + j * tile + key, page = fast_div(pos, a.pg.d_prow);
-        first[j] = use(pos, page) ? table[page] : -1;
+      for (int c = 0; c < 3; ++c) {
+        const int pg = page_of(c * 128 + key, in);
+        first[c] = pg >= 0 ? table[pg] : -1;
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        scale_copy(j, first[j]);
-        if (j > 0) entry_copy(j + 3);
-        else cp_async_commit();
+      for (int c = 0; c < 3; ++c) {
+        chunk_words(c, first[c]);
+        chunk_entries(c + 3);
+        cp_async_commit();
       }
-      cp_async_wait<3>();
-      hand_on(0);
     }
     uint64_t l[RW / 2];  // pairs of rows' sums over this thread's positions
 #pragma unroll
     for (int r = 0; r < RW / 2; ++r) l[r] = 0;
     Mask set = 0;  // rows whose reference is set
     bool ok = true;
+    int waited = 0;  // chunks that this warp has waited for
     for (int j = 0; j < nt; ++j) {
       const int sb = j & 1, base = k0 + j * tile, p = base + key;
-      if (wg == 0) {
-        cp_async_wait<2>();  // what was asked for at tile j - 3
-        hand_on(j + 1);
-        scale_copy(j + 4, sm.entry[(j + 4) & 3][key]);
-        entry_copy(j + 7);
-      }
+      // the chunks of this tile's blocks: handed on by the first group, and waited for
+      const int need = fast_div(min(base + tile, k1) - 1, a.d_brow) - b0 >> 7;
+      if (wg == 0)
+        while (handed <= need) hand_on();
+      for (; waited <= need; ++waited)
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.sc_full[waited & 7], waited >> 3 & 1, abort, a.status));
       // the rows that see this position: a range
       Mask vis = real;
       if (a.mode == SFA_WITHIN && a.n > 1) {
@@ -466,8 +472,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       // leave after it.)
       ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.s_full[sb], (j >> 1) & 1, abort, a.status));
       tc_fence_after();
-      if (wg > 0) ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.sc_full[j & 3], (j >> 2) & 1, abort, a.status));
-      const int sc = sm.scale[j & 3][key], kb = sc & 255, vb = sc >> 8;
+      const int sc = sm.scale[fast_div(min(p, k1 - 1), a.d_brow) - b0 & 1023], kb = sc & 255, vb = sc >> 8;
       const float kf = q8::scale_of(kb), ev = (float)(vb - 127), inv = q8::inverse_of(vb);
       const uint64_t kf2 = f2pack(kf, kf), ev2 = f2pack(ev, ev);
       float y[RW];
