@@ -32,16 +32,21 @@ constexpr int kUnit = KT * 128;    // bytes of a ring slot: 128 columns of a K o
 constexpr float kTop = 15.f;       // P's largest exponent
 constexpr float kSet = 5.f;        // the exponent of a row's largest P when its reference is set
 constexpr float kLow = 64.f;       // P's third codes hold so many times what they stand for
+constexpr float kLo = 16.f;        // a query's second e4m3 codes too
 
 // HV: 128-column units of a tile (Dh / 128)
 template <int HV, int RW, int WG>
 struct Cfg {
   static constexpr int R = RW * WG, kThreads = 64 + WG * 128;
-  static constexpr int kCols = 2 * R + 3 * HV * R;  // tensor memory: two S, three O
+  // Queries in two e4m3 codes side by side (kPair: K is read once, S has two columns a row), or in three e5m2 codes one
+  // after another (K is read three times) where tensor memory has no room for that.
+  static constexpr bool kPair = 4 * R + 3 * HV * R <= (HV == 2 && R == 32 ? 256 : 512);
+  static constexpr int SC = kPair ? 2 * R : R, QT = kPair ? 2 : 3;  // columns of S; codes of a query's value
+  static constexpr int kCols = 2 * SC + 3 * HV * R;  // tensor memory: two S, three O
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr int kFixed = 3 * R * HV * 128 + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 8 * R + 512;  // all but the ring
+  static constexpr int kFixed = QT * R * HV * 128 + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 8 * R + 512;  // all but the ring
   static constexpr int kPerSm = kAlloc <= 128 && kFixed + 3 * kUnit <= 74 * 1024    ? 3
-                                : kAlloc <= 256 && kFixed + 3 * kUnit <= 112 * 1024 ? 2
+                                : kAlloc <= 256 && R <= 32 && kFixed + 3 * kUnit <= 112 * 1024 ? 2
                                                                                     : 1;
   static constexpr int kRoom = ((kPerSm == 3 ? 74 : kPerSm == 2 ? 112 : 226) * 1024 - kFixed) / kUnit;
   static constexpr int NSLOT = kRoom < 10 ? kRoom : 10;
@@ -51,7 +56,7 @@ template <int HV, int RW, int WG>
 struct Smem {
   using C = Cfg<HV, RW, WG>;
   uint8_t ring[C::NSLOT][kUnit];             // [128 positions][128 bytes], 128-byte swizzle
-  uint8_t q[HV][3][C::R * 128];              // hi, mid, lo: [R rows][128 bytes], 128-byte swizzle
+  uint8_t q[HV][C::QT][C::R * 128];          // codes: [R rows][128 bytes], 128-byte swizzle
   uint8_t p[2][3][C::R * KT];                // a buffer's hi, mid, lo: blocks of 16 rows, [128 positions][16 bytes]
   uint2 words[4][128];                       // of chunks: the words of K's and V's scales that hold a block's byte
   int entry[4][128];                         // its page entry
@@ -231,18 +236,27 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       most = __reduce_max_sync(0xffffffffu, most);
       // the exponent field of the largest magnitude, kept where both powers are normal
       const int e = min(max((int)(most >> 23), 20), 254);
-      const float to = __int_as_float(min(127 + 14 + 127 - e, 254) << 23);  // 2^(14 - (e - 127)), at most 2^127
-      const float back = __int_as_float(max(e - 14, 1) << 23);              // 2^(e - 127 - 14)
+      constexpr int kUp = C::kPair ? 7 : 14;  // the largest to [2^kUp, 2^(kUp + 1))
+      const float to = __int_as_float(min(127 + kUp + 127 - e, 254) << 23);  // 2^(kUp - (e - 127)), at most 2^127
+      const float back = __int_as_float(max(e - kUp, 1) << 23);              // 2^(e - 127 - kUp)
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        const __half2 u = __floats2half2_rn(__uint_as_float(w[i] << 16) * to, __uint_as_float(w[i] & 0xffff0000u) * to);
+        const float x0 = __uint_as_float(w[i] << 16) * to, x1 = __uint_as_float(w[i] & 0xffff0000u) * to;
         uint32_t t[3];
-        split3<false>(*reinterpret_cast<const uint32_t*>(&u), t[0], t[1], t[2]);
+        if (C::kPair) {
+          t[0] = q8::code2(x0, x1);
+          const float2 y = q8::values2((uint16_t)t[0]);
+          t[1] = q8::code2((x0 - y.x) * kLo, (x1 - y.y) * kLo);
+        } else {
+          const __half2 u = __floats2half2_rn(x0, x1);
+          split3<false>(*reinterpret_cast<const uint32_t*>(&u), t[0], t[1], t[2]);
+#pragma unroll
+          for (int x = 0; x < 3; ++x) t[x] = __byte_perm(t[x], 0, 0x31);
+        }
         const int c = (lane * NP + i) * 2, at = (c & 127) >> 4, off = c & 15;  // column; its 16-byte chunk
 #pragma unroll
-        for (int x = 0; x < 3; ++x)
-          *reinterpret_cast<uint16_t*>(sm.q[c >> 7][x] + rr * 128 + ((at ^ (rr & 7)) << 4) + off) =
-              (uint16_t)__byte_perm(t[x], 0, 0x31);
+        for (int x = 0; x < C::QT; ++x)
+          *reinterpret_cast<uint16_t*>(sm.q[c >> 7][x] + rr * 128 + ((at ^ (rr & 7)) << 4) + off) = (uint16_t)t[x];
       }
       if (lane == 0) {
         sm.rowf[rr] = back * a.scale_log2;
@@ -322,7 +336,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ the products
-    constexpr uint32_t idS = idesc_f8(128, R, 0, 1, 0, 0), idO = idesc_f8(128, 3 * R, 0, 1, 1, 1);
+    constexpr uint32_t idS = C::kPair ? idesc_f8(128, 2 * R, 0, 0, 0, 0) : idesc_f8(128, R, 0, 1, 0, 0), idO = idesc_f8(128, 3 * R, 0, 1, 1, 1);
     const uint64_t kd = sdesc_sw128(smem_u32(sm.ring[0]), 16, 1024), qd = sdesc_sw128(smem_u32(sm.q[0][0]), 16, 1024);
     const uint64_t pd = sdesc_plain_mn(smem_u32(sm.p[0][0]), 128, KT * 16);
     int slot = 0, lap = 0;
@@ -345,12 +359,12 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
 #pragma unroll
       for (int hf = 0; hf < HV; ++hf) {
         if (!wait_unit()) return false;
-        const uint64_t kk = kd + (uint64_t)(slot * (kUnit / 16)), qq = qd + (uint64_t)(hf * (3 * R * 128 / 16));
+        const uint64_t kk = kd + (uint64_t)(slot * (kUnit / 16)), qq = qd + (uint64_t)(hf * (C::QT * R * 128 / 16));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int term = 0; term < 3; ++term)
-            mma_f8_ss_w(tmem + sb * R, kk + i * 2, qq + term * (R * 128 / 16) + i * 2, idS, hf + i + term > 0 ? 1u : 0u);
+          for (int term = 0; term < (C::kPair ? 1 : 3); ++term)
+            mma_f8_ss_w(tmem + sb * C::SC, kk + i * 2, qq + term * (R * 128 / 16) + i * 2, idS, hf + i + term > 0 ? 1u : 0u);
         done_unit();
       }
       tc_commit_w(&sm.s_full[sb]);
@@ -366,7 +380,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
         const uint64_t vv = kd + (uint64_t)(slot * (kUnit / 16)), pp = pd + (uint64_t)(pb * (3 * R * KT / 16));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          mma_f8_ss_w(tmem + 2 * R + hf * 3 * R, vv + i * 256, pp + i * 32, idO, j > 0 || i > 0 ? 1u : 0u);
+          mma_f8_ss_w(tmem + 2 * C::SC + hf * 3 * R, vv + i * 256, pp + i * 32, idO, j > 0 || i > 0 ? 1u : 0u);
         done_unit();
       }
       tc_commit_w(&sm.pv_done[pb]);
@@ -383,7 +397,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     // ------------------------------------------------------------ softmax: a thread per position
     typedef typename Rows<RW>::Mask Mask;
     const int wg = (warp - 2) >> 2, q4 = warp & 3, key = q4 * 32 + lane, r0 = wg * RW, bar = 1 + wg;
-    const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16), tO = tl + 2 * R + r0;
+    const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16), tO = tl + 2 * C::SC + r0;
     const int own_lo = (T - 1) * a.n, win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;
     const int seen = a.mode == SFA_LOCAL ? own_lo - a.window + 1 : 0;
     const Mask real = bits<RW>(0, rows - r0);
@@ -476,9 +490,19 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       const float kf = q8::scale_of(kb), ev = (float)(vb - 127), inv = q8::inverse_of(vb);
       const uint64_t kf2 = f2pack(kf, kf), ev2 = f2pack(ev, ev);
       float y[RW];
+      {
+        float low[RW];
 #pragma unroll
-      for (int c = 0; c < RW; c += 16) tmem_ld16(tl + sb * R + r0 + c, reinterpret_cast<uint32_t*>(y) + c);
-      tmem_ld_wait();
+        for (int c = 0; c < RW; c += 16) {
+          tmem_ld16(tl + sb * C::SC + r0 + c, reinterpret_cast<uint32_t*>(y) + c);
+          if (C::kPair) tmem_ld16(tl + sb * C::SC + R + r0 + c, reinterpret_cast<uint32_t*>(low) + c);
+        }
+        tmem_ld_wait();
+        if (C::kPair)
+#pragma unroll
+          for (int r = 0; r < RW; r += 2)
+            f2unpack(ffma2(f2pack(low[r], low[r + 1]), f2pack(1.f / kLo, 1.f / kLo), f2pack(y[r], y[r + 1])), y[r], y[r + 1]);
+      }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.s_free[sb]);
