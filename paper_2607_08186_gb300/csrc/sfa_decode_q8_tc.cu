@@ -462,22 +462,29 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     for (int r = 0; r < RW / 2; ++r) l[r] = 0;
     Mask set = 0;  // rows whose reference is set
     bool ok = true;
-    int waited = 0;  // chunks that this warp has waited for
+    const int brow = a.pg.prow / a.blocks;
+    int waited = 0;                               // chunks that this warp has waited for
+    long long scales_end = (long long)b0 * brow;  // the first position behind them
+    // this key's block, from the split's first, and its row there; both go on by a tile
+    const int step_blocks = fast_div(tile, a.d_brow), step_rows = tile - step_blocks * brow;
+    int block = fast_div(k0 + key, a.d_brow) - b0, in_block = k0 + key - (block + b0) * brow;
+    const int edge = tile < KT ? 0 : min(own_lo + 1, k1);  // tiles that end at or before it have no mask but WITHIN's
     for (int j = 0; j < nt; ++j) {
       const int sb = j & 1, base = k0 + j * tile, p = base + key;
       // the chunks of this tile's blocks: handed on by the first group, and waited for
-      const int need = fast_div(min(base + tile, k1) - 1, a.d_brow) - b0 >> 7;
-      if (wg == 0)
-        while (handed <= need) hand_on();
-      for (; waited <= need; ++waited)
+      while (min(base + tile, k1) > scales_end) {
+        if (wg == 0) hand_on();
         ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.sc_full[waited & 7], waited >> 3 & 1, abort, a.status));
+        ++waited;
+        scales_end += 128ll * brow;
+      }
       // the rows that see this position: a range
       Mask vis = real;
       if (a.mode == SFA_WITHIN && a.n > 1) {
         const int s = p - fast_div(p, a.d_n) * a.n;
         vis &= bits<RW>(s * a.G - row0 - r0, (s + 1) * a.G - row0 - r0);
       }
-      if (base + tile - 1 > own_lo || base + tile > k1 || base <= win_hi || tile < KT) {
+      if (base + tile > edge || base <= win_hi) {
         const int first = (p - own_lo) * a.G - row0 - r0;  // rows of the streams from p's own on, where p is the new token's
         const int last = a.mode == SFA_LOCAL ? (int)min((long long)(p - own_lo + a.window) * a.G - row0 - r0, 64ll) : 64;
         vis = key < tile && p < k1 ? vis & bits<RW>(p < own_lo ? 0 : first, last) : (Mask)0;
@@ -486,7 +493,10 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
       // leave after it.)
       ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.s_full[sb], (j >> 1) & 1, abort, a.status));
       tc_fence_after();
-      const int sc = sm.scale[fast_div(min(p, k1 - 1), a.d_brow) - b0 & 1023], kb = sc & 255, vb = sc >> 8;
+      const int sc = sm.scale[min(block, nblocks - 1) & 1023], kb = sc & 255, vb = sc >> 8;
+      block += step_blocks;
+      in_block += step_rows;
+      if (in_block >= brow) in_block -= brow, ++block;
       const float kf = q8::scale_of(kb), ev = (float)(vb - 127), inv = q8::inverse_of(vb);
       const uint64_t kf2 = f2pack(kf, kf), ev2 = f2pack(ev, ev);
       float y[RW];
