@@ -610,12 +610,15 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
 }
 
 // Whether the tcgen05 kernel takes a step: it reads tiles by TMA alone.
-static bool q8_tc(int Dh, int prow) { return Dh >= 128 && paged_piece(prow, 128) >= decq8::kTmaRows; }
+static bool q8_tc(int Dh, int prow) {
+  const int piece = paged_piece(prow, 128);
+  return piece >= decq8::kTmaRows && (Dh >= 128 || piece % 2 == 0);  // a piece's rows start on 128 bytes of shared memory
+}
 
 size_t decode_paged_q8_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {
   // either kernel's, whatever the pages
   const size_t x = q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, false, true).bytes();
-  return Dh == 64 ? x : std::max(x, q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, true, true).bytes());
+  return std::max(x, q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, true, true).bytes());
 }
 
 template <int DH, bool WIDE, bool TMA>

@@ -28,23 +28,23 @@ using decq8::Args;
 using decq8::Params;
 
 constexpr int KT = 128;            // positions of a tile
-constexpr int kUnit = KT * 128;    // bytes of a ring slot: 128 columns of a K or V tile
 constexpr float kTop = 15.f;       // P's largest exponent
 constexpr float kSet = 5.f;        // the exponent of a row's largest P when its reference is set
 constexpr float kLow = 64.f;       // P's third codes hold so many times what they stand for
 constexpr float kLo = 16.f;        // a query's second e4m3 codes too
 
-// HV: 128-column units of a tile (Dh / 128)
-template <int HV, int RW, int WG>
+// HV units of a K or V tile, of RB columns (128, or 64 at head dim 64) each: a ring slot.  R query rows: WG warp groups of RW.
+template <int DH, int RW, int WG>
 struct Cfg {
   static constexpr int R = RW * WG, kThreads = 64 + WG * 128;
+  static constexpr int RB = DH < 128 ? DH : 128, HV = DH / RB, kUnit = KT * RB;
   // Queries in two e4m3 codes side by side (kPair: K is read once, S has two columns a row), or in three e5m2 codes one
   // after another (K is read three times) where tensor memory has no room for that.
   static constexpr bool kPair = 4 * R + 3 * HV * R <= (HV == 2 && R == 32 ? 256 : 512);
   static constexpr int SC = kPair ? 2 * R : R, QT = kPair ? 2 : 3;  // columns of S; codes of a query's value
   static constexpr int kCols = 2 * SC + 3 * HV * R;  // tensor memory: two S, three O
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr int kFixed = QT * R * HV * 128 + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 8 * R + 512;  // all but the ring
+  static constexpr int kFixed = QT * R * DH + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 8 * R + 512;  // all but the ring
   static constexpr int kPerSm = kAlloc <= 128 && kFixed + 3 * kUnit <= 74 * 1024    ? 3
                                 : kAlloc <= 256 && R <= 32 && kFixed + 3 * kUnit <= 112 * 1024 ? 2
                                                                                     : 1;
@@ -52,11 +52,11 @@ struct Cfg {
   static constexpr int NSLOT = kRoom < 10 ? kRoom : 10;
 };
 
-template <int HV, int RW, int WG>
+template <int DH, int RW, int WG>
 struct Smem {
-  using C = Cfg<HV, RW, WG>;
-  uint8_t ring[C::NSLOT][kUnit];             // [128 positions][128 bytes], 128-byte swizzle
-  uint8_t q[HV][C::QT][C::R * 128];          // codes: [R rows][128 bytes], 128-byte swizzle
+  using C = Cfg<DH, RW, WG>;
+  uint8_t ring[C::NSLOT][C::kUnit];          // [128 positions][RB bytes], swizzled by 128 bytes (64)
+  uint8_t q[C::HV][C::QT][C::R * C::RB];     // codes: [R rows][RB bytes], swizzled so too
   uint8_t p[2][3][C::R * KT];                // a buffer's hi, mid, lo: blocks of 16 rows, [128 positions][16 bytes]
   uint2 words[4][128];                       // of chunks: the words of K's and V's scales that hold a block's byte
   int entry[4][128];                         // its page entry
@@ -75,6 +75,18 @@ struct Smem {
 __host__ __device__ constexpr uint32_t idesc_f8(int M, int N, int a_type, int b_type, int a_mn, int b_mn) {
   return (1u << 4) | ((uint32_t)a_type << 7) | ((uint32_t)b_type << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
          ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// Matrix descriptor of rows of RB bytes, swizzled by as many: eight rows lie together.  K-major with a row to an index, or
+// MN-major with a k to a row and RB indices in it.
+template <int RB>
+HD_DEVINLINE uint64_t sdesc_rows(uint32_t saddr) {
+  if (RB == 128) return sdesc_sw128(saddr, 16, 1024);
+  uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= 1ull << 16;
+  d |= (uint64_t)(512 >> 4) << 32;
+  d |= 1ull << 46;  // descriptor version for tcgen05
+  d |= 4ull << 61;  // SWIZZLE_64B
+  return d;
 }
 // Matrix descriptor without a swizzle, MN-major: 16 bytes of rows x 8 k lie together (128 bytes); the next 8 k are `kstep`
 // bytes on, the next 16 rows `mstep`.
@@ -165,12 +177,12 @@ HD_DEVINLINE void split3(uint32_t u, uint32_t& hi, uint32_t& mid, uint32_t& lo) 
   lo += 0x00800080u;
 }
 
-template <int HV, int RW, int WG>
-__global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kPerSm)
+template <int DH, int RW, int WG>
+__global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kPerSm)
     decode_q8_tc_kernel(const __grid_constant__ Params P) {
-  using C = Cfg<HV, RW, WG>;
-  using Sm = Smem<HV, RW, WG>;
-  constexpr int R = C::R, NSLOT = C::NSLOT, NT = C::kThreads, DH = HV * 128;
+  using C = Cfg<DH, RW, WG>;
+  using Sm = Smem<DH, RW, WG>;
+  constexpr int R = C::R, NSLOT = C::NSLOT, NT = C::kThreads, HV = C::HV, RB = C::RB, kUnit = C::kUnit;
   const Args& a = P.a;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   Sm& sm = *reinterpret_cast<Sm*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -182,9 +194,9 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
   float2* pml = a.part_ml + pidx * R;
   const int tile = a.tile, row0 = rg * R, rows = min(R, a.M - row0);
   // positions of a tile that no piece fills: their V must not be NaN
-  for (int i = tid; i < NSLOT * (KT - tile) * 8; i += NT) {
-    const int per = (KT - tile) * 8;
-    reinterpret_cast<uint4*>(sm.ring[i / per] + tile * 128)[i % per] = make_uint4(0, 0, 0, 0);
+  for (int i = tid; i < NSLOT * (KT - tile) * (RB / 16); i += NT) {
+    const int per = (KT - tile) * (RB / 16);
+    reinterpret_cast<uint4*>(sm.ring[i / per] + tile * RB)[i % per] = make_uint4(0, 0, 0, 0);
   }
   if (tid == 0) {
     for (int i = 0; i < NSLOT; ++i) {
@@ -253,10 +265,11 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
 #pragma unroll
           for (int x = 0; x < 3; ++x) t[x] = __byte_perm(t[x], 0, 0x31);
         }
-        const int c = (lane * NP + i) * 2, at = (c & 127) >> 4, off = c & 15;  // column; its 16-byte chunk
+        const int c = (lane * NP + i) * 2, at = (c % RB) >> 4, off = c & 15;  // column; its 16-byte chunk
+        const int swizzled = RB == 64 ? at ^ (rr >> 1 & 3) : at ^ (rr & 7);
 #pragma unroll
         for (int x = 0; x < C::QT; ++x)
-          *reinterpret_cast<uint16_t*>(sm.q[c >> 7][x] + rr * 128 + ((at ^ (rr & 7)) << 4) + off) = (uint16_t)t[x];
+          *reinterpret_cast<uint16_t*>(sm.q[c / RB][x] + rr * RB + swizzled * 16 + off) = (uint16_t)t[x];
       }
       if (lane == 0) {
         sm.rowf[rr] = back * a.scale_log2;
@@ -307,10 +320,10 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
 #pragma unroll
       for (int hf = 0; hf < HV; ++hf) {
         if (lap > 0 && !__all_sync(0xffffffffu, mbar_wait(&sm.empty[slot], (lap - 1) & 1, abort, a.status))) return false;
-        if (lane == 0) mbar_arrive_expect_tx(&sm.full[slot], tile * 128);
+        if (lane == 0) mbar_arrive_expect_tx(&sm.full[slot], tile * RB);
         __syncwarp();
         if (lane * a.piece < tile)
-          tma_load_4d(sm.ring[slot] + lane * a.piece * 128, tm, &sm.full[slot], hf * 128, x.y, g, x.x);
+          tma_load_4d(sm.ring[slot] + lane * a.piece * RB, tm, &sm.full[slot], hf * RB, x.y, g, x.x);
         __syncwarp();
         ++issued;
         if (++slot == NSLOT) slot = 0, ++lap;
@@ -336,8 +349,8 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ the products
-    constexpr uint32_t idS = C::kPair ? idesc_f8(128, 2 * R, 0, 0, 0, 0) : idesc_f8(128, R, 0, 1, 0, 0), idO = idesc_f8(128, 3 * R, 0, 1, 1, 1);
-    const uint64_t kd = sdesc_sw128(smem_u32(sm.ring[0]), 16, 1024), qd = sdesc_sw128(smem_u32(sm.q[0][0]), 16, 1024);
+    constexpr uint32_t idS = C::kPair ? idesc_f8(128, 2 * R, 0, 0, 0, 0) : idesc_f8(128, R, 0, 1, 0, 0), idO = idesc_f8(RB, 3 * R, 0, 1, 1, 1);
+    const uint64_t kd = sdesc_rows<RB>(smem_u32(sm.ring[0])), qd = sdesc_rows<RB>(smem_u32(sm.q[0][0]));
     const uint64_t pd = sdesc_plain_mn(smem_u32(sm.p[0][0]), 128, KT * 16);
     int slot = 0, lap = 0;
     bool ok = true;
@@ -359,12 +372,12 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
 #pragma unroll
       for (int hf = 0; hf < HV; ++hf) {
         if (!wait_unit()) return false;
-        const uint64_t kk = kd + (uint64_t)(slot * (kUnit / 16)), qq = qd + (uint64_t)(hf * (C::QT * R * 128 / 16));
+        const uint64_t kk = kd + (uint64_t)(slot * (kUnit / 16)), qq = qd + (uint64_t)(hf * (C::QT * R * RB / 16));
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < RB / 32; ++i)
 #pragma unroll
           for (int term = 0; term < (C::kPair ? 1 : 3); ++term)
-            mma_f8_ss_w(tmem + sb * C::SC, kk + i * 2, qq + term * (R * 128 / 16) + i * 2, idS, hf + i + term > 0 ? 1u : 0u);
+            mma_f8_ss_w(tmem + sb * C::SC, kk + i * 2, qq + term * (R * RB / 16) + i * 2, idS, hf + i + term > 0 ? 1u : 0u);
         done_unit();
       }
       tc_commit_w(&sm.s_full[sb]);
@@ -380,7 +393,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
         const uint64_t vv = kd + (uint64_t)(slot * (kUnit / 16)), pp = pd + (uint64_t)(pb * (3 * R * KT / 16));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          mma_f8_ss_w(tmem + 2 * C::SC + hf * 3 * R, vv + i * 256, pp + i * 32, idO, j > 0 || i > 0 ? 1u : 0u);
+          mma_f8_ss_w(tmem + 2 * C::SC + hf * 3 * R, vv + i * (32 * RB / 16), pp + i * 32, idO, j > 0 || i > 0 ? 1u : 0u);
         done_unit();
       }
       tc_commit_w(&sm.pv_done[pb]);
@@ -623,7 +636,7 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
           ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.full[u % NSLOT], (u / NSLOT) & 1, abort, a.status));
           if (ok && p >= k1)
 #pragma unroll
-            for (int c = 0; c < 8; ++c) reinterpret_cast<uint4*>(sm.ring[u % NSLOT] + key * 128)[c] = make_uint4(0, 0, 0, 0);
+            for (int c = 0; c < RB / 16; ++c) reinterpret_cast<uint4*>(sm.ring[u % NSLOT] + key * RB)[c] = make_uint4(0, 0, 0, 0);
         }
         __syncwarp();
         if (!ok) continue;
@@ -639,6 +652,8 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
     if (ok) {
       tc_fence_after();
       const bool bad = *(volatile int*)&sm.bad_page != 0;
+      // this lane's row of O^T: all 128, or (a product of 64 rows) 16 of each 32
+      const int column = RB == 128 ? key : lane < 16 ? q4 * 16 + lane : -1;
 #pragma unroll
       for (int hf = 0; hf < HV; ++hf)
 #pragma unroll
@@ -651,7 +666,8 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float x = fmaf(__uint_as_float(o[2][e]), 1.f / kLow, __uint_as_float(o[0][e]) + __uint_as_float(o[1][e]));
-            po[(size_t)(r0 + c + e) * DH + hf * 128 + key] = x;
+            if (column < 0) continue;
+            po[(size_t)(r0 + c + e) * DH + hf * RB + column] = x;
             if (!(fabsf(x) <= FLT_MAX)) wrong |= 1u << e;
           }
           wrong = __reduce_or_sync(0xffffffffu, wrong);
@@ -712,36 +728,37 @@ __global__ void __launch_bounds__(Cfg<HV, RW, WG>::kThreads, Cfg<HV, RW, WG>::kP
 // ------------------------------------------------------------------ host side
 
 
-template <int HV, int RW, int WG>
+template <int DH, int RW, int WG>
 static cudaError_t launch_t(const decq8::Params& p, cudaStream_t st) {
   using namespace decq8tc;
-  using C = Cfg<HV, RW, WG>;
-  const int smem = (int)sizeof(Smem<HV, RW, WG>) + 1024;
-  static_assert(sizeof(Smem<HV, RW, WG>) + 1024 <= (C::kPerSm == 3 ? 75 : C::kPerSm == 2 ? 113 : 227) * 1024 && C::NSLOT >= 3 &&
+  using C = Cfg<DH, RW, WG>;
+  const int smem = (int)sizeof(Smem<DH, RW, WG>) + 1024;
+  static_assert(sizeof(Smem<DH, RW, WG>) + 1024 <= (C::kPerSm == 3 ? 75 : C::kPerSm == 2 ? 113 : 227) * 1024 && C::NSLOT >= 3 &&
                     C::kCols <= C::kAlloc && C::kPerSm * C::kAlloc <= 512,
                 "an SM's CTAs fit");
-  cudaError_t e = cudaFuncSetAttribute(decode_q8_tc_kernel<HV, RW, WG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(decode_q8_tc_kernel<DH, RW, WG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(true, decode_q8_tc_kernel<HV, RW, WG>, dim3((unsigned)p.a.nsplit * p.a.B * p.a.Hkv * p.a.ngroups),
+  return launch_kernel(true, decode_q8_tc_kernel<DH, RW, WG>, dim3((unsigned)p.a.nsplit * p.a.B * p.a.Hkv * p.a.ngroups),
                        (unsigned)C::kThreads, smem, st, p);
 }
 
-int decode_q8_tc_per_sm(int rows, int Dh) {
+template <int DH>
+static int per_sm(int rows) {
   using namespace decq8tc;
-  if (Dh == 128) return rows <= 16 ? Cfg<1, 16, 1>::kPerSm : rows <= 32 ? Cfg<1, 16, 2>::kPerSm : rows <= 48 ? Cfg<1, 16, 3>::kPerSm : Cfg<1, 16, 4>::kPerSm;
-  return rows <= 16 ? Cfg<2, 16, 1>::kPerSm : rows <= 32 ? Cfg<2, 16, 2>::kPerSm : rows <= 48 ? Cfg<2, 16, 3>::kPerSm : Cfg<2, 16, 4>::kPerSm;
+  return rows <= 16 ? Cfg<DH, 16, 1>::kPerSm : rows <= 32 ? Cfg<DH, 16, 2>::kPerSm : rows <= 48 ? Cfg<DH, 16, 3>::kPerSm : Cfg<DH, 16, 4>::kPerSm;
 }
+int decode_q8_tc_per_sm(int rows, int Dh) { return Dh == 64 ? per_sm<64>(rows) : Dh == 128 ? per_sm<128>(rows) : per_sm<256>(rows); }
 
-template <int HV>
-static cudaError_t launch_h(const decq8::Params& p, cudaStream_t st) {
-  if (p.a.rg == 16) return launch_t<HV, 16, 1>(p, st);
-  if (p.a.rg == 32) return launch_t<HV, 16, 2>(p, st);
-  if (p.a.rg == 48) return launch_t<HV, 16, 3>(p, st);
-  return launch_t<HV, 16, 4>(p, st);
+template <int DH>
+static cudaError_t launch_d(const decq8::Params& p, cudaStream_t st) {
+  if (p.a.rg == 16) return launch_t<DH, 16, 1>(p, st);
+  if (p.a.rg == 32) return launch_t<DH, 16, 2>(p, st);
+  if (p.a.rg == 48) return launch_t<DH, 16, 3>(p, st);
+  return launch_t<DH, 16, 4>(p, st);
 }
 
 cudaError_t launch_decode_q8_tc(decq8::Params& p, int Dh, cudaStream_t st) {
-  return Dh == 128 ? launch_h<1>(p, st) : launch_h<2>(p, st);
+  return Dh == 64 ? launch_d<64>(p, st) : Dh == 128 ? launch_d<128>(p, st) : launch_d<256>(p, st);
 }
 
 }  // namespace hdsfa
