@@ -18,12 +18,27 @@ struct AppendArgs {
   int32_t* status;
 };
 
+// 32 bytes, a whole sector, in one load (p 32-byte aligned); two of 16 bytes take a sector twice (6 prompts of up to 4000
+// tokens, 4 streams, 8 heads of 128, a scale a page, the CTA's teams: 42.7 -> 40.6 us; the warps' spill with it: a scale a
+// token 42.5 -> 49.9).
+HD_DEVINLINE void ld_global_32(const void* p, uint32_t* r) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "l"(p)
+               : "memory");
+}
+
 // Sixteen values of a row as 8 words of bf16 pairs.
 struct Chunk {
   uint32_t w[8];
 };
+template <bool WHOLE>
 HD_DEVINLINE Chunk load_chunk(const uint16_t* p) {
   Chunk c;
+  if (WHOLE && (reinterpret_cast<uintptr_t>(p) & 31) == 0) {  // (a base need only be aligned to 16 bytes)
+    ld_global_32(p, c.w);
+    return c;
+  }
   const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
   c.w[0] = a.x, c.w[1] = a.y, c.w[2] = a.z, c.w[3] = a.w;
   c.w[4] = b.x, c.w[5] = b.y, c.w[6] = b.z, c.w[7] = b.w;
@@ -77,22 +92,20 @@ HD_DEVINLINE int last_not_above(int B, long long u, int lane, Key key) {
 
 constexpr int kHeld = 4;  // chunks that a thread holds from the maximum to the codes
 
-// A unit is what a call appends to one block, for one head and tensor, by a team: its new rows' largest magnitude gives
-// the scale, then the rows are coded; the rows are read once where they fit kHeld chunks a thread.  A block that held
-// tokens before keeps at least its scale, and where that grows the older rows are coded again.
+// A unit is what a call appends to one block of tokens.  For each head and tensor (a pair, of which there are 2 Hkv) a team
+// of threads finds the new rows' largest magnitude, which gives the scale, and codes the rows; they are read once where
+// they fit kHeld chunks a thread.  A block that held tokens before keeps at least its scale, and where that grows the older
+// rows are coded again.  A team is the CTA (a unit and pair each), or as many lanes of a warp as the rows need: then a warp
+// takes a unit and finds its place once for all its pairs, or for one in gridDim.y of them where units are few.  (A warp
+// for each unit and pair: 24 prompts of up to 701 tokens, 3 streams, 4 heads of 64, a scale a token 35.7 us.)
 // With offsets, sequence b's units have the numbers from offsets[b] / T + 2 b on: x tokens touch at most x / T + 2
 // blocks, and those numbers are at least as far apart.
 template <int TEAM>
-__global__ void __launch_bounds__(128) append_q8_kernel(AppendArgs a) {
-  static_assert(TEAM == 32 || TEAM == 128, "a warp or the CTA");
+__global__ void __launch_bounds__(128, 6) append_q8_kernel(AppendArgs a) {
+  static_assert(TEAM == 8 || TEAM == 16 || TEAM == 32 || TEAM == 128, "lanes of a warp, or the CTA");
   __shared__ uint32_t warp_most[4];
   const int lane = threadIdx.x & 31, tid = threadIdx.x % TEAM;
-  const bool tensor = blockIdx.y & 1;
-  const int h = blockIdx.y >> 1;
-  const bool report = blockIdx.y == 0 && tid == 0;
-  const uint16_t* src = tensor ? a.vn : a.kn;
-  uint8_t* pool = tensor ? a.vc : a.kc;
-  uint8_t* scales = tensor ? a.vs : a.ks;
+  const bool report = blockIdx.y == 0 && (TEAM == 128 ? threadIdx.x : lane) == 0;
   const Geom& g = a.g;
   const int n = g.n, Dh = g.Dh;
   grid_dep_wait();
@@ -104,8 +117,10 @@ __global__ void __launch_bounds__(128) append_q8_kernel(AppendArgs a) {
       if (!bad) bad = z - x > L && (a.served == nullptr || a.served[b] >= z - x);
       if (bad) set_status(a.status, HD_DEVBIT_INDEX);
     }
-  for (long long u = (long long)blockIdx.x * (128 / TEAM) + threadIdx.x / TEAM; u < a.units;
-       u += (long long)gridDim.x * (128 / TEAM)) {
+  constexpr int kUnits = TEAM == 128 ? 1 : 4;        // of a CTA at a time
+  constexpr int kTeams = TEAM == 128 ? 1 : 32 / TEAM;  // of a unit at a time
+  for (long long u = (long long)blockIdx.x * kUnits + (TEAM == 128 ? 0 : threadIdx.x >> 5); u < a.units;
+       u += (long long)gridDim.x * kUnits) {
     // the block's new tokens [t0, t1) of sequence b, t0's packed token i0, and the block's first token tb
     int b, t0, t1, tb;
     long long i0;
@@ -140,50 +155,61 @@ __global__ void __launch_bounds__(128) append_q8_kernel(AppendArgs a) {
       if (report) set_status(a.status, HD_DEVBIT_INDEX);
       continue;
     }
-    const int page = fast_div(row, g.pg.d_prow), off = row - page * g.pg.prow;
-    uint8_t* codes = pool + (((size_t)page * g.Hkv + h) * g.pg.prow + off) * Dh;  // the block's rows
-    uint8_t* scale = scales + scale_at(g, page, h, fast_div(off, g.d_brow));
+    const int page = fast_div(row, g.pg.d_prow), off = row - page * g.pg.prow, block = fast_div(off, g.d_brow);
     const int cpr = Dh >> 4, chunks = (t1 - t0) * n * cpr;
     const size_t pitch = (size_t)g.Hkv * Dh;
-    const uint16_t* rows = src + (size_t)i0 * n * pitch + (size_t)h * Dh;
-    auto at = [&](int c) {
-      const int r = fast_div(c, a.d_cpr);
-      return rows + r * pitch + (c - r * cpr) * 16;
-    };
-    const int had = t0 > tb ? clamp_byte(*scale) : 0;
-    Chunk held[kHeld];
+    // (the same number of rounds for every team of a warp, whose lanes stay together)
+    for (int first = (int)blockIdx.y * kTeams; first < 2 * g.Hkv; first += (int)gridDim.y * kTeams) {
+      const int pair = first + (TEAM == 128 ? 0 : lane / TEAM);
+      const bool mine = pair < 2 * g.Hkv, tensor = pair >= g.Hkv;
+      const int h = mine ? pair - (tensor ? g.Hkv : 0) : 0, count = mine ? chunks : 0;
+      uint8_t* codes = (tensor ? a.vc : a.kc) + (((size_t)page * g.Hkv + h) * g.pg.prow + off) * Dh;  // the block's rows
+      uint8_t* scale = (tensor ? a.vs : a.ks) + scale_at(g, page, h, block);
+      const uint16_t* rows = (tensor ? a.vn : a.kn) + (size_t)i0 * n * pitch + (size_t)h * Dh;
+      auto at = [&](int c) {
+        const int r = fast_div(c, a.d_cpr);
+        return rows + r * pitch + (c - r * cpr) * 16;
+      };
+      const int had = mine && t0 > tb ? clamp_byte(*scale) : 0;
+      Chunk held[kHeld];
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      if (tid + k * TEAM < chunks) held[k] = load_chunk(at(tid + k * TEAM));
-    uint32_t most = 0;
+      for (int k = 0; k < kHeld; ++k)
+        if (tid + k * TEAM < count) held[k] = load_chunk<TEAM == 128>(at(tid + k * TEAM));
+      uint32_t most = 0;
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      if (tid + k * TEAM < chunks) most = max(most, most_of(held[k]));
-    for (int c = tid + kHeld * TEAM; c < chunks; c += TEAM) most = max(most, most_of(load_chunk(at(c))));
-    most = __reduce_max_sync(0xffffffffu, most);
-    if (TEAM > 32) {
-      if (lane == 0) warp_most[threadIdx.x >> 5] = most;
-      __syncthreads();
-      most = max(max(warp_most[0], warp_most[1]), max(warp_most[2], warp_most[3]));
-      __syncthreads();  // (also: every thread has read the block's old scale)
-    }
-    const int byte = max(scale_byte(most), had);
-    const float inv = inverse_of(byte);
-    uint4* to = reinterpret_cast<uint4*>(codes + (size_t)(t0 - tb) * n * Dh);
+      for (int k = 0; k < kHeld; ++k)
+        if (tid + k * TEAM < count) most = max(most, most_of(held[k]));
+      for (int c = tid + kHeld * TEAM; c < count; c += TEAM) most = max(most, most_of(load_chunk<TEAM == 128>(at(c))));
+      if (TEAM >= 32) {
+        most = __reduce_max_sync(0xffffffffu, most);
+      } else {
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      if (tid + k * TEAM < chunks) to[tid + k * TEAM] = codes_of(held[k], inv);
-    for (int c = tid + kHeld * TEAM; c < chunks; c += TEAM) to[c] = codes_of(load_chunk(at(c)), inv);
-    if (t0 > tb && byte > had) {
-      const float f = scale_of(had - byte + 127);
-      uint4* older = reinterpret_cast<uint4*>(codes);
-      for (int c = tid; c < (t0 - tb) * n * cpr; c += TEAM) {
-        const uint4 x = older[c];
-        older[c] = make_uint4(recode4(x.x, f), recode4(x.y, f), recode4(x.z, f), recode4(x.w, f));
+        for (int d = TEAM / 2; d; d >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
       }
+      if (TEAM == 128) {
+        if (lane == 0) warp_most[threadIdx.x >> 5] = most;
+        __syncthreads();
+        most = max(max(warp_most[0], warp_most[1]), max(warp_most[2], warp_most[3]));
+        __syncthreads();  // (also: every thread has read the block's old scale)
+      }
+      const int byte = max(scale_byte(most), had);
+      const float inv = inverse_of(byte);
+      uint4* to = reinterpret_cast<uint4*>(codes + (size_t)(t0 - tb) * n * Dh);
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k)
+        if (tid + k * TEAM < count) to[tid + k * TEAM] = codes_of(held[k], inv);
+      for (int c = tid + kHeld * TEAM; c < count; c += TEAM) to[c] = codes_of(load_chunk<TEAM == 128>(at(c)), inv);
+      if (mine && t0 > tb && byte > had) {
+        const float f = scale_of(had - byte + 127);
+        uint4* older = reinterpret_cast<uint4*>(codes);
+        for (int c = tid; c < (t0 - tb) * n * cpr; c += TEAM) {
+          const uint4 x = older[c];
+          older[c] = make_uint4(recode4(x.x, f), recode4(x.y, f), recode4(x.z, f), recode4(x.w, f));
+        }
+      }
+      if (TEAM < 128) __syncwarp();  // every lane has read the old scale
+      if (mine && tid == 0) *scale = (uint8_t)byte;
     }
-    if (TEAM == 32) __syncwarp();  // every lane has read the old scale
-    if (tid == 0) *scale = (uint8_t)byte;
   }
 }
 
@@ -198,16 +224,19 @@ struct ReadArgs {
 };
 constexpr int kPiece = 128;
 
-// Packed tokens out of the cache: a warp per (token, piece of its n * Hkv * Dh values, tensor), a lane's four loads
-// of 16 codes ahead of its stores.
+// Packed tokens out of the cache: a warp per token and piece (of its n * Hkv * Dh values, K's and V's), a lane's loads of 16
+// codes ahead of its stores.  Bound by the bytes, two thirds of them written (6 prompts of up to 4000 tokens, 4 streams, 8
+// heads of 128: 47.5 us, 5.2 TB/s; a warp that takes all of a token's pieces 53, pieces twice as large 57, stores of 32
+// bytes 50).
 __global__ void __launch_bounds__(256) read_q8_kernel(ReadArgs a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const bool tensor = (int)blockIdx.y >= a.pieces, report = blockIdx.y == 0;
-  const int first = (tensor ? (int)blockIdx.y - a.pieces : (int)blockIdx.y) * kPiece;
-  const uint8_t* pool = tensor ? a.vc : a.kc;
-  const uint8_t* scales = tensor ? a.vs : a.ks;
-  uint4* out = tensor ? a.vr : a.kr;
+  const bool report = blockIdx.y == 0;
   const Geom& g = a.g;
+  const int cpr = g.Dh >> 4;
+  const bool tensor = (int)blockIdx.y >= a.pieces;
+  const int first = (tensor ? (int)blockIdx.y - a.pieces : (int)blockIdx.y) * kPiece;
+  const uint4* pool = reinterpret_cast<const uint4*>(tensor ? a.vc : a.kc);
+  const uint8_t* scales = tensor ? a.vs : a.ks;
   grid_dep_wait();
   grid_dep_launch();
   if (report && blockIdx.x == 0)
@@ -227,7 +256,6 @@ __global__ void __launch_bounds__(256) read_q8_kernel(ReadArgs a) {
       continue;
     }
     const int page = fast_div(row, g.pg.d_prow), off = row - page * g.pg.prow, block = fast_div(off, g.d_brow);
-    const int cpr = g.Dh >> 4;
     uint4 code[kPiece / 32];
     int byte[kPiece / 32];
 #pragma unroll
@@ -235,11 +263,11 @@ __global__ void __launch_bounds__(256) read_q8_kernel(ReadArgs a) {
       const int c = first + lane + k * 32;
       if (c < a.chunks) {
         const int sh = fast_div(c, a.d_cpr), s = fast_div(sh, a.d_Hkv), h = sh - s * g.Hkv;
-        code[k] = reinterpret_cast<const uint4*>(pool)[(((size_t)page * g.Hkv + h) * g.pg.prow + off + s) * cpr + c - sh * cpr];
+        code[k] = pool[(((size_t)page * g.Hkv + h) * g.pg.prow + off + s) * cpr + c - sh * cpr];
         byte[k] = scales[scale_at(g, page, h, block)];
       }
     }
-    uint4* to = out + (size_t)w * a.chunks * 2;
+    uint4* to = (tensor ? a.vr : a.kr) + (size_t)w * a.chunks * 2;
 #pragma unroll
     for (int k = 0; k < kPiece / 32; ++k) {
       const int c = first + lane + k * 32;
@@ -325,11 +353,18 @@ cudaError_t launch_kv_append_paged_q8(const void* kn, const void* vn, void* kc, 
   a.d_cpr = make_fast_div((uint32_t)(Dh / 16));
   a.status = status;
   a.units = offsets != nullptr ? (long long)N / T + 2ll * B : B;
-  const long long values = (long long)(offsets != nullptr ? T : 1) * n * Dh;  // of a unit, at most
-  const bool warps = values <= 32 * 16 * q8::kHeld;
-  const long long ctas = warps ? (a.units + 3) / 4 : a.units;
-  const dim3 grid((unsigned)std::min<long long>(ctas, 1 << 20), 2 * Hkv);
-  return warps ? launch_early(q8::append_q8_kernel<32>, grid, 128, st, a) : launch_early(q8::append_q8_kernel<128>, grid, 128, st, a);
+  const long long values = (long long)(offsets != nullptr ? T : 1) * n * Dh;  // of a unit and pair, at most
+  const int lanes = values <= 8 * 16 * q8::kHeld ? 8 : values <= 16 * 16 * q8::kHeld ? 16 : values <= 32 * 16 * q8::kHeld ? 32 : 128;
+  // few units: their pairs are shared out, so that teams are a few for each place on the SMs (for CTAs 8 an SM take 62 us
+  // where 24 take 42.7 and 96 take 41.5)
+  const int rounds = lanes == 128 ? 2 * Hkv : (2 * Hkv * lanes + 31) / 32;
+  const long long share = std::max(1LL, std::min<long long>(rounds, 24LL * kSmCount / a.units));
+  if (lanes == 128)
+    return launch_early(q8::append_q8_kernel<128>, dim3((unsigned)std::min<long long>(a.units, 1 << 20), (unsigned)share), 128, st, a);
+  const dim3 grid((unsigned)std::min<long long>((a.units + 3) / 4, 1 << 20), (unsigned)share);
+  return lanes == 8    ? launch_early(q8::append_q8_kernel<8>, grid, 128, st, a)
+         : lanes == 16 ? launch_early(q8::append_q8_kernel<16>, grid, 128, st, a)
+                       : launch_early(q8::append_q8_kernel<32>, grid, 128, st, a);
 }
 
 cudaError_t launch_kv_read_paged_q8(const void* kc, const void* vc, const uint8_t* ks, const uint8_t* vs,
