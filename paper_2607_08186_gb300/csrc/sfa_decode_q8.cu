@@ -585,8 +585,11 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
   p.rg = ((p.M + p.ngroups - 1) / p.ngroups + 15) / 16 * 16;
   const int KT = !tc && Dh == 256 ? decq8::ktile<256>() : decq8::ktile<128>();
   const long long tiles = (q8_range(maxT, n, mode, window) + KT - 1) / KT, ctas = (long long)B * Hkv * p.ngroups;
-  const long long resident =
-      (long long)kSmCount * (tc ? decode_q8_tc_per_sm(p.rg, Dh) : p.rg > (Dh == 256 ? 16 : 32) ? 1 : Dh == 64 && p.rg == 16 ? 4 : 2);
+  int per_sm = tc ? decode_q8_tc_per_sm(p.rg, Dh) : p.rg > (Dh == 256 ? 16 : 32) ? 1 : Dh == 64 && p.rg == 16 ? 4 : 2;
+  // few tiles: fewer splits, which the combine kernel merges faster (1 x 8192 tokens, 4 streams, 32 over 8 heads of 128, 13
+  // tiles an SM: two CTAs an SM 21.2 us, three 23.1; 8 x 2048, 27 tiles: 29.1 and 28.0)
+  if (tc && ctas * tiles < 20 * kSmCount) per_sm = std::min(per_sm, 2);
+  const long long resident = (long long)kSmCount * per_sm;
   const long long most = std::min({tiles, (long long)dec::kMaxSplit, std::max(1LL, 4 * resident / ctas)});
   long long best = 1, best_cost = -1;
   if (bound) {
@@ -609,10 +612,17 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
   return p;
 }
 
-// Whether the tcgen05 kernel takes a step: it reads tiles by TMA alone.
-static bool q8_tc(int Dh, int prow) {
+// Whether the tcgen05 kernel takes a step.  It reads tiles by TMA alone, in pieces of at least kTmaRows rows of a page that
+// start on 128 bytes of shared memory, and takes longer to start and end, so up to 16 query rows leave it short ranges.
+// Measured (replayed from a graph, us, tcgen05 / mma.sync, 4 streams but where said):
+//   32 over 8 heads of 128   33 x 12 tokens 12.2 / 11.0, 4 x 50 10.3 / 9.2, 4 x 150 11.8 / 11.8, 4 x 1000 15.8 / 17.4, 16 x 1000
+//                            31.8 / 41.0; one stream, 7 of up to 20000 40.2 / 67.2
+//   16 over 4 of 64          3 streams, 4 x 400 11.7 / 9.7, 4 x 3000 16.8 / 18.2
+//   24 over 2 of 256         4 x 50 14.8 / 23.8;  96 over 8 of 128: 16 x 50 13.7 / 15.1, 16 x 400 26.6 / 46.9
+static bool q8_tc(int Dh, int prow, int rows, long long range) {
   const int piece = paged_piece(prow, 128);
-  return piece >= decq8::kTmaRows && (Dh >= 128 || piece % 2 == 0);  // a piece's rows start on 128 bytes of shared memory
+  if (piece < decq8::kTmaRows || (Dh == 64 && piece % 2 != 0)) return false;
+  return rows > 16 || range > (Dh == 64 ? 2048 : Dh == 128 ? 256 : 0);
 }
 
 size_t decode_paged_q8_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {
@@ -646,7 +656,8 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
                                        int num_pages, int P, int max_pages, int n, int Hq, int Hkv, int Dh, int T,
                                        float scale, int mode, int window, void* ws, size_t ws_bytes, int32_t* status,
                                        cudaStream_t st) {
-  const bool tc = q8_tc(Dh, P * n);
+  const long long range = q8_range(maxT, n, mode, window);
+  const bool tc = q8_tc(Dh, P * n, n * (Hq / Hkv), range);
   const Q8Plan plan = q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, tc, false);
   if (plan.bytes() > ws_bytes) return cudaErrorInvalidValue;  // the bound says that it is not
   decq8::Params p = {};
@@ -692,7 +703,6 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   const bool tma = a.piece >= decq8::kTmaRows && (Dh >= 128 || a.piece % 2 == 0);
   a.tile = tma ? KT / a.piece * a.piece : n <= KT ? KT / n * n : KT;  // cp.async: whole tokens where a tile holds one
   a.d_tile = make_fast_div((uint32_t)a.tile);
-  const long long range = q8_range(maxT, n, mode, window);
   a.balanced = tc && B > 1 && B <= dec::kBalancedSeqs && plan.nsplit > 1 && range / plan.nsplit >= 4 * 64 &&
                B * (range / a.tile + 1) < (1LL << 30);  // the tiles of all sequences, counted in 32 bits
   if (tma && (!make_q8_tmap(&p.tm_k, kc, num_pages, Hkv, a.pg.prow, Dh, a.piece) ||

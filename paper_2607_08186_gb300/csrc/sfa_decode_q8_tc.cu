@@ -498,7 +498,7 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
         vis &= bits<RW>(s * a.G - row0 - r0, (s + 1) * a.G - row0 - r0);
       }
       if (base + tile > edge || base <= win_hi) {
-        const int first = (p - own_lo) * a.G - row0 - r0;  // rows of the streams from p's own on, where p is the new token's
+        const int first = max(p - own_lo, 0) * a.G - row0 - r0;  // rows of the streams from p's own on, where p is the new token's
         const int last = a.mode == SFA_LOCAL ? (int)min((long long)(p - own_lo + a.window) * a.G - row0 - r0, 64ll) : 64;
         vis = key < tile && p < k1 ? vis & bits<RW>(p < own_lo ? 0 : first, last) : (Mask)0;
       }

@@ -32,7 +32,8 @@ def _append(lib, B=2, N=2, pages=20, P=8, width=8, n=2, Hkv=2, Dh=64, T=4, new=F
 def test_append_refusals(lib):
     for bad in (dict(B=0), dict(N=3), dict(N=-1, offsets=FAKE), dict(P=0), dict(n=0), dict(Dh=8), dict(Dh=72), dict(Hkv=0),
                 dict(T=0), dict(T=3), dict(T=16), dict(new=0), dict(new=FAKE + 8), dict(pool=FAKE + 8), dict(pool=0),
-                dict(scales=0), dict(offsets=FAKE + 2), dict(lens=0), dict(served=FAKE + 1), dict(status=FAKE + 2)):
+                dict(scales=0), dict(scales=FAKE + 8), dict(offsets=FAKE + 2), dict(lens=0), dict(served=FAKE + 1),
+                dict(status=FAKE + 2)):
         assert _append(lib, **bad) == 1, bad
     for bad in (dict(pages=1 << 28), dict(width=1 << 28), dict(Hkv=1 << 20), dict(N=1 << 30, offsets=FAKE),
                 dict(Hkv=40000, Dh=16), dict(pages=1 << 26, Hkv=8), dict(P=1 << 24, T=1 << 24, width=1, pages=1)):
@@ -48,7 +49,7 @@ def _read(lib, B=2, N=6, pages=20, P=8, width=8, n=2, Hkv=2, Dh=64, T=4, out=FAK
 
 def test_read_refusals(lib):
     for bad in (dict(B=0), dict(N=-1), dict(P=0), dict(n=0), dict(Dh=24), dict(T=5), dict(out=0), dict(out=FAKE + 8),
-                dict(pool=0), dict(scales=0), dict(offsets=0), dict(offsets=FAKE + 2), dict(lens=FAKE + 1)):
+                dict(pool=0), dict(scales=0), dict(scales=FAKE + 4), dict(offsets=0), dict(offsets=FAKE + 2), dict(lens=FAKE + 1)):
         assert _read(lib, **bad) == 1, bad
     for bad in (dict(pages=1 << 28), dict(N=1 << 30)):
         assert _read(lib, **bad) == 2, bad
@@ -64,7 +65,7 @@ def _decode(lib, B=2, T=64, pages=20, P=8, width=8, n=2, Hq=4, Hkv=2, Dh=64, blo
 
 def test_decode_refusals(lib):
     for bad in (dict(B=0), dict(T=0), dict(pages=0), dict(P=0), dict(width=0), dict(n=0), dict(Hq=5), dict(Hkv=0),
-                dict(mode=3), dict(mode=2, window=0), dict(ptr=FAKE + 8), dict(ptr=0), dict(scales=0), dict(table=FAKE + 2),
+                dict(mode=3), dict(mode=2, window=0), dict(ptr=FAKE + 8), dict(ptr=0), dict(scales=0), dict(scales=FAKE + 1), dict(table=FAKE + 2),
                 dict(table=0), dict(T=65), dict(lse=FAKE + 2), dict(status=FAKE + 2), dict(block=0), dict(block=3)):
         assert _decode(lib, **bad) == 1, bad
     for bad in (dict(Dh=96), dict(B=65536), dict(pages=1 << 27, P=8), dict(P=1 << 29, width=2, T=8, block=1),
@@ -95,8 +96,8 @@ def test_copy_refusals(lib):
     def copy(k=FAKE, s=FAKE, c=FAKE, F=2, pages=10, nbytes=64, ns=3):
         return lib.hd_pages_copy_q8(P_(k), P_(FAKE), P_(s), P_(FAKE), P_(c), F, pages, nbytes, ns, None, None)
 
-    assert [copy(k=0), copy(k=FAKE + 4), copy(s=0), copy(c=0), copy(c=FAKE + 4), copy(F=-1), copy(nbytes=0), copy(nbytes=24),
-            copy(ns=0), copy(pages=0)] == [1] * 10
+    assert [copy(k=0), copy(k=FAKE + 4), copy(s=0), copy(s=FAKE + 2), copy(c=0), copy(c=FAKE + 4), copy(F=-1), copy(nbytes=0),
+            copy(nbytes=24), copy(ns=0), copy(pages=0)] == [1] * 11
     assert copy(nbytes=1 << 35) == 2 and copy(ns=1 << 31) == 2 and copy(F=0, c=0) == 0
 
 
