@@ -15,7 +15,6 @@ struct Args : DecodeArgs {
   const uint8_t *kcodes, *vcodes, *kscale, *vscale;
   int blocks;       // blocks of a page
   FastDiv d_brow, d_blocks;  // rows of a block; blocks of a page
-  int mt, sets;     // row tiles of a CTA; sets of 4 mt warps
 };
 struct Params {
   CUtensorMap tm_k, tm_v;
@@ -101,7 +100,7 @@ HD_DEVINLINE void store_row(const Args& a, int b, int g, int r, const float* o, 
 }
 }  // namespace decq8
 
-// The tcgen05 kernel (head dims 128 and 256, pages whose pieces TMA can bring): CTAs of so many query rows that an SM
+// The tcgen05 kernel (pages whose pieces TMA can bring): CTAs of so many query rows that an SM
 // holds, and the launch without the combine kernel.
 int decode_q8_tc_per_sm(int rows, int Dh);
 cudaError_t launch_decode_q8_tc(decq8::Params& p, int Dh, cudaStream_t st);

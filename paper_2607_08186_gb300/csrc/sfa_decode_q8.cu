@@ -11,12 +11,18 @@
 // queries are scaled by a power of two for each row, so that f16 holds them as bf16 did (a row's largest to 2^15; values
 // 2^-39 below it lose bits).
 //
-// Bound by memory: half the bytes of the bf16 step, so each byte brings twice the products.  A warp takes 16 query
-// rows and 32 of a tile's positions; the warps of the row tiles share the tile in shared memory, so up to 64 rows of a
-// K/V head's group read the cache once.  Tiles stream through a ring: by TMA, in pieces that lie within a page, the
-// warps taking turns at bringing them; pieces of fewer than kTmaRows rows by cp.async.  mma.sync m16n8k16 (f16): a
+// This kernel takes what the tcgen05 kernel (sfa_decode_q8_tc.cu) does not: pages too small for TMA, and short ranges of few
+// query rows, where it starts and ends sooner.  A warp takes 16 query rows and 32 of a tile's positions; the warps of the
+// row tiles share the tile in shared memory, so up to 64 rows of a K/V head's group read the cache once.  Tiles stream
+// through a ring by 16-byte cp.async, whose rows the threads look up three tiles ahead.  mma.sync m16n8k16 (f16): a
 // thread's four bytes of an ldmatrix row are k = 2t, 2t + 1, 2t + 8, 2t + 9 of the product, so q lies in that order; V's
 // transposed loads bring pairs of head-dim columns for two keys, so even and odd columns are products of their own.
+//
+// Bound by the latency of a tile's chain (table entry, rows, scales, products, softmax) and by the instructions that
+// turn codes into f16: 32 over 8 heads of 128, 4 streams, 4 sequences of 4000 tokens on pages of 2 tokens take 28.1 us, 14.7
+// of them the bytes at the copy rate; pages of one token with a scale each 48.  Bringing larger pieces by TMA here with two
+// sets of warps on alternate tiles gains nothing where this kernel runs (4 x 50 tokens 9.3 us and 10.1 without, 33 x 12
+// 10.9 and 10.0, two sequences of 64 over heads of 64 6.5 and 6.1).
 #include <float.h>
 
 #include <algorithm>
@@ -26,7 +32,6 @@
 
 namespace hdsfa {
 namespace decq8 {
-constexpr int kTmaRows = 8;
 constexpr int kWarpKeys = 32;        // positions of a tile that a warp takes
 constexpr float kShift = 15.f;       // P's largest exponent
 constexpr int kMaxRows = 64;         // query rows of a CTA at most (four row tiles)
@@ -38,18 +43,16 @@ constexpr int key_warps() { return 4 / dsplit<DH>(); }
 template <int DH>
 constexpr int ktile() { return kWarpKeys * key_warps<DH>(); }
 
-
-// Two CTAs an SM while their queries leave room for three stages each: up to two row tiles, one at head dim 256.  WIDE:
-// more row tiles, one CTA an SM.  Sixteen warps an SM hide the products' latency, so where the row tiles are few there
-// are two sets of warps, which take alternate tiles.
+// Two CTAs an SM (more at head dim 64) while their queries leave room for three stages each: up to two row tiles, one at
+// head dim 256.  WIDE: more row tiles, one CTA an SM.
 template <int DH, bool WIDE>
 struct Cfg {
   static constexpr int KT = ktile<DH>(), MT = WIDE ? 4 : DH == 256 ? 1 : 2, STAGES = !WIDE ? 3 : DH == 256 ? 5 : 6;
-  static constexpr int kWarps = WIDE ? 16 : 8, kThreads = kWarps * 32;
-  static constexpr int kMergeRows = WIDE ? 64 : 32;  // row tiles x sets, in rows, at most
+  static constexpr int kWarps = 4 * MT, kThreads = kWarps * 32;
+  static constexpr int kMergeRows = 16 * MT;  // rows of the partials at most
 };
 
-template <int DH, bool WIDE, bool TMA>
+template <int DH, bool WIDE>
 struct Smem {
   using C = Cfg<DH, WIDE>;
   uint8_t k[C::STAGES][C::KT * DH];
@@ -57,14 +60,13 @@ struct Smem {
   __half q[C::MT * 16 * DH];
   float4 scale[C::kWarps][kWarpKeys];   // a warp's keys: 2^ek, ev, 2^-ev
   float qscale[C::MT * 16];
-  uint32_t row[TMA ? 1 : 4][C::KT];     // cp.async: rows of the pool (kNoRow: none) of four tiles
-  uint64_t full[2 * C::STAGES], empty[2 * C::STAGES];  // of a stage and set
+  uint32_t row[4][C::KT];               // rows of the pool (kNoRow: none) of four tiles
   unsigned not_finite[2];               // a bit for each row of the merged partial
-  int bad_page, abort;
+  int bad_page;
 };
 
-// Byte offset of 16-byte chunk `c` of a row of a tile: blocks of [KT][128 bytes] with the 128-byte swizzle that TMA
-// writes, at head dim 64 [KT][64] with the 64-byte one; conflict-free for ldmatrix.
+// Byte offset of 16-byte chunk `c` of a row of a tile: blocks of [KT][128 bytes], at head dim 64 [KT][64], whose
+// chunks are XORed with the row's number; conflict-free for ldmatrix.
 template <int DH, int KT>
 HD_DEVINLINE int chunk_at(int row, int c) {
   if (DH == 64) return row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
@@ -83,15 +85,13 @@ HD_DEVINLINE uint32_t pack_f16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-template <int DH, bool WIDE, bool TMA>
-__global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_q8_kernel(const __grid_constant__ Params P) {
+template <int DH, bool WIDE>
+__global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_q8_kernel(const __grid_constant__ Args a) {
   using C = Cfg<DH, WIDE>;
-  using Sm = Smem<DH, WIDE, TMA>;
+  using Sm = Smem<DH, WIDE>;
   constexpr int KT = C::KT, STAGES = C::STAGES;
   constexpr int KW = key_warps<DH>(), DC = DH / dsplit<DH>(), CPR = DH / 16;  // DC: O columns of a warp
-  constexpr int RB = DH < 128 ? DH : 128;                                     // bytes of a row in a block of the tile
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  const Args& a = P.a;
   {
     uint32_t dyn;
     asm("mov.u32 %0, %%dynamic_smem_size;\n" : "=r"(dyn));
@@ -105,35 +105,16 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
   const int split = fast_div((int)blockIdx.x, a.d_heads), head = (int)blockIdx.x - split * a.Hkv * a.ngroups;
   const int g = a.ngroups == 1 ? head : head / a.ngroups, rg = a.ngroups == 1 ? 0 : head % a.ngroups;
   const int tid = threadIdx.x, nt = blockDim.x, W = nt >> 5, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, t4 = lane & 3;
-  // this warp's set and its number there; row tile, key group and head-dim part
-  const int sets = TMA ? a.sets : 1, WS = 4 * a.mt, set = TMA && warp >= WS ? 1 : 0, ws = warp - set * WS;
-  const int mt = ws >> 2, kw = (ws & 3) % KW, dw = (ws & 3) / KW;
+  const int mt = warp >> 2, kw = (warp & 3) % KW, dw = (warp & 3) / KW;  // row tile, key group and head-dim part
   const int R = a.rg;  // rows of the CTA
   const size_t pidx = blockIdx.x;
   float* po = a.part_o + pidx * R * DH;
   float2* pml = a.part_ml + pidx * R;
   const int tile = a.tile;
-  if (TMA && tid == 32) {
-    tma_prefetch(&P.tm_k);
-    tma_prefetch(&P.tm_v);
-  }
   if (tid == 0) {
-    sm.bad_page = sm.abort = 0;
+    sm.bad_page = 0;
     sm.not_finite[0] = sm.not_finite[1] = 0;
-    if (TMA) {
-      for (int i = 0; i < 2 * STAGES; ++i) {
-        mbar_init(&sm.full[i], 1);
-        mbar_init(&sm.empty[i], WS);  // one arrival per warp of a set
-      }
-      fence_mbar_init();
-    }
   }
-  // rows that no piece fills: their P is zero, and their V must not be NaN
-  if (TMA && tile < KT)
-    for (int i = tid; i < STAGES * (KT - tile) * CPR; i += nt) {
-      const int st = i / ((KT - tile) * CPR), e = i % ((KT - tile) * CPR);
-      *reinterpret_cast<uint4*>(sm.v[st] + chunk_at<DH, KT>(tile + e / CPR, e % CPR)) = make_uint4(0, 0, 0, 0);
-    }
   // this thread's query rows g4 and g4 + 8 of the row tile: their streams (-1: padding).  Where n divides a tile, which
   // of this thread's keys are of a row's stream is the same in every tile.
   int rs_[2];
@@ -169,26 +150,10 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     return;
   }
   const int nsub = fast_div(k1 - k0 + tile - 1, a.d_tile);
-  __syncthreads();  // the barriers and flags are set
 
   // ---- the tiles' loads
   const int seen = a.mode == SFA_LOCAL ? (T - 1) * a.n - a.window + 1 : 0;  // first position any row sees
-  // TMA: the first tiles are brought by a warp each; after that a set that goes on to tile `it` brings tile
-  // it - sets + STAGES into the stage that it has left, its warps in turn.  Lane i brings piece i, whose page entry it has
-  // looked up when the warp brought its last tile
-  auto pos_of = [&](int t) {  // first position of this lane's piece of a tile, -1: none that a row sees
-    const int p = lane * a.piece, pos = k0 + t * tile + p;
-    return p >= tile || pos >= k1 || pos + a.piece <= seen ? -1 : pos;
-  };
-  int entry = 0;
-  auto fetch = [&](int t) {
-    const int pos = t < nsub ? pos_of(t) : -1;
-    if (pos >= 0) {
-      const int i = fast_div(pos, a.pg.d_prow);
-      entry = i < a.pg.max_pages ? table[i] : -1;
-    }
-  };
-  // cp.async: the pools' row of this thread's position of a tile
+  // the pools' row of this thread's position of a tile
   auto row_of = [&](int it) {
     const int p = k0 + it * tile + tid;
     if (tid >= tile || p >= k1 || p < seen) return kNoRow;
@@ -196,57 +161,26 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     if (row == kNoRow) sm.bad_page = 1;
     return row;
   };
-  [[maybe_unused]] int brought = -1;  // TMA: the last tile that this warp brought
-  // A wait cannot tell a phase of a barrier from the one after the next, so who waits for a phase must have seen the one
-  // before: a stage that serves two sets in turn (STAGES is odd there) has barriers for each, at [set * STAGES + stage].
-  // A set's i-th tile is its barriers' phase i / STAGES.
-  static_assert(WIDE || STAGES % 2 == 1, "two sets share a stage");
-  auto load_tile = [&](int it, int st, int whose) {  // tile `it` of set `whose` into stage st
-    if constexpr (TMA) {
-      brought = it;
-      uint64_t* full = &sm.full[whose * STAGES + st];
-      if (lane == 0) mbar_arrive_expect_tx(full, tile * DH * 2);
-      __syncwarp();
-      if (lane * a.piece < tile) {
-        const int pos = pos_of(it);
-        int page = a.pg.num_pages, off = 0;  // behind the pool: zeros
-        if (pos >= 0) {
-          if ((unsigned)entry < (unsigned)a.pg.num_pages) {
-            page = entry;
-            off = pos - fast_div(pos, a.pg.d_prow) * a.pg.prow;
-          } else {
-            sm.bad_page = 1;
-          }
-        }
-#pragma unroll
-        for (int cb = 0; cb < DH / RB; ++cb) {
-          const int at = cb * KT * RB + lane * a.piece * RB;
-          tma_load_4d(sm.k[st] + at, &P.tm_k, full, cb * RB, off, g, page);
-          tma_load_4d(sm.v[st] + at, &P.tm_v, full, cb * RB, off, g, page);
-        }
-      }
-      __syncwarp();
-    } else {
-      for (int i = tid; i < KT * CPR; i += nt) {
-        const int rr = i / CPR, cc = i % CPR;
-        const uint32_t row = rr < tile ? sm.row[it & 3][rr] : kNoRow;
-        const size_t off = (row == kNoRow ? 0 : (size_t)row * DH) + cc * 16;
-        cp_async_16(smem_u32(sm.k[st] + chunk_at<DH, KT>(rr, cc)), a.kcodes + off, row != kNoRow);
-        cp_async_16(smem_u32(sm.v[st] + chunk_at<DH, KT>(rr, cc)), a.vcodes + off, row != kNoRow);
-      }
+  auto load_tile = [&](int it, int st) {  // tile `it` into stage st
+    for (int i = tid; i < KT * CPR; i += nt) {
+      const int rr = i / CPR, cc = i % CPR;
+      const uint32_t row = rr < tile ? sm.row[it & 3][rr] : kNoRow;
+      const size_t off = (row == kNoRow ? 0 : (size_t)row * DH) + cc * 16;
+      cp_async_16(smem_u32(sm.k[st] + chunk_at<DH, KT>(rr, cc)), a.kcodes + off, row != kNoRow);
+      cp_async_16(smem_u32(sm.v[st] + chunk_at<DH, KT>(rr, cc)), a.vcodes + off, row != kNoRow);
     }
   };
-  // The scales of this warp's keys, a lane's key each: the page entry two of the set's tiles ahead, the bytes one ahead.
-  // The key's page and row there go on by the set's step, without divisions.
-  const int my_key = kw * kWarpKeys + lane, step = tile * sets;
-  const int step_pages = fast_div(step, a.pg.d_prow), step_rows = step - step_pages * a.pg.prow;
-  int at_pos = k0 + set * tile + my_key, at_page = fast_div(at_pos, a.pg.d_prow), at_row = at_pos - at_page * a.pg.prow;
+  // The scales of this warp's keys, a lane's key each: the page entry two tiles ahead, the bytes one ahead.  The
+  // key's page and row there go on by a tile, without divisions.
+  const int my_key = kw * kWarpKeys + lane;
+  const int step_pages = fast_div(tile, a.pg.d_prow), step_rows = tile - step_pages * a.pg.prow;
+  int at_pos = k0 + my_key, at_page = fast_div(at_pos, a.pg.d_prow), at_row = at_pos - at_page * a.pg.prow;
   int next_entry = -1, next_row_in = 0;
-  auto scale_entry = [&] {  // entry and row of the key in the set's next tile, whose number goes up by one
+  auto scale_entry = [&] {  // entry and row of the key in the next tile, whose number goes up by one
     next_entry = -1;
     next_row_in = at_row;
     if (my_key < tile && at_pos < k1 && at_pos >= seen && at_page < a.pg.max_pages) next_entry = table[at_page];
-    at_pos += step;
+    at_pos += tile;
     at_page += step_pages;
     at_row += step_rows;
     if (at_row >= a.pg.prow) at_row -= a.pg.prow, ++at_page;
@@ -259,21 +193,15 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
       vb = a.vscale[at];
     }
   };
-  if constexpr (TMA) {
-    if (warp < min(STAGES, nsub)) {
-      fetch(warp);
-      load_tile(warp, warp, sets == 2 ? warp & 1 : 0);
-    }
-    fetch(set + sets * (ws == 0 ? WS - 1 : ws - 1) + STAGES);  // this warp's next one
-  } else {
+  {
     const uint32_t r0 = row_of(0), r1 = row_of(1), r2 = row_of(2);
     if (tid < tile) sm.row[0][tid] = r0, sm.row[1][tid] = r1, sm.row[2][tid] = r2;
-    __syncthreads();
-    load_tile(0, 0, 0);
-    cp_async_commit();
-    if (nsub > 1) load_tile(1, 1, 0);
-    cp_async_commit();
   }
+  __syncthreads();  // ... and the flags are set
+  load_tile(0, 0);
+  cp_async_commit();
+  if (nsub > 1) load_tile(1, 1);
+  cp_async_commit();
   scale_entry();
   scale_bytes();
   scale_entry();
@@ -316,12 +244,8 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
 #pragma unroll
   for (int i = 0; i < DC / 8; ++i) oacc[i][0] = oacc[i][1] = oacc[i][2] = oacc[i][3] = 0.f;
 
-  bool alive = true;
-  int turn = 0;  // the warp of this set that brings a tile
-  int st = set, phase = 0, round = 0, left_st = 0, left_phase = 0;  // stage and phase of this tile and of the set's last
-  for (int it = set; it < nsub; it += sets) {
+  for (int it = 0, st = 0; it < nsub; ++it) {
     const int base = k0 + it * tile;
-    [[maybe_unused]] uint32_t next_row = kNoRow;
     // this tile's scales into shared memory, the next ones' loads on their way
     {
       kb = q8::clamp_byte(kb);
@@ -330,32 +254,11 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
       scale_bytes();
       scale_entry();
     }
-    if constexpr (TMA) {
-      // the warps meet on the stages' barriers alone: one that loads does not hold up the others
-      const int left = it - sets, t = left + STAGES;
-      if (turn == ws && left >= 0 && t < nsub) {
-        alive = __all_sync(0xffffffffu, mbar_wait(&sm.empty[set * STAGES + left_st], left_phase, &sm.abort, a.status));
-        if (alive) {
-          load_tile(t, left_st, sets - 1 - set);
-          fetch(t + sets * WS);
-        }
-      }
-      if (++turn == WS) turn = 0;
-      alive = alive && __all_sync(0xffffffffu, mbar_wait(&sm.full[set * STAGES + st], phase, &sm.abort, a.status));
-      if (!alive) break;
-      if (base + tile > k1) {  // cached rows behind the sequence's length may never have been written
-        const int r0 = max(kw * kWarpKeys, k1 - base), r1 = min((kw + 1) * kWarpKeys, tile);
-        for (int i = r0 * CPR + lane; i < r1 * CPR; i += 32)
-          *reinterpret_cast<uint4*>(sm.v[st] + chunk_at<DH, KT>(i / CPR, i % CPR)) = make_uint4(0, 0, 0, 0);
-      }
-      __syncwarp();
-    } else {
-      cp_async_wait<1>();  // stage `it` has landed
-      __syncthreads();     // ... for every thread, and stage it-1 is no longer read
-      if (it + 2 < nsub) load_tile(it + 2, (it + 2) % STAGES, 0);
-      cp_async_commit();
-      next_row = row_of(it + 3);  // the rows that the next iteration loads by
-    }
+    cp_async_wait<1>();  // stage `it` has landed
+    __syncthreads();     // ... for every thread, and stage it - 1 is no longer read
+    if (it + 2 < nsub) load_tile(it + 2, (it + 2) % STAGES);
+    cp_async_commit();
+    const uint32_t next_row = row_of(it + 3);  // the rows that the next iteration loads by
     const uint8_t *cK = sm.k[st], *cV = sm.v[st];
 
     // S = q ck^T: key tile j of 8 keys
@@ -461,42 +364,25 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
         }
       }
     }
-    if constexpr (TMA) {
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.empty[set * STAGES + st]);
-    } else {
-      __syncwarp();  // this tile's scales are read
-      if (tid < tile) sm.row[(it + 3) & 3][tid] = next_row;
-    }
-    left_st = st;
-    left_phase = phase;
-    st = st + sets >= STAGES ? st + sets - STAGES : st + sets;
-    if (++round == STAGES) round = 0, phase ^= 1;
+    __syncwarp();  // this tile's scales are read
+    if (tid < tile) sm.row[(it + 3) & 3][tid] = next_row;
+    if (++st == STAGES) st = 0;
   }
-  if constexpr (TMA) {
-    // a wait gave up: the results are invalid.  A warp that goes on has seen every tile land; one that does not
-    // waits (again with a limit) for the last that it brought, and those before it were read before its set went on.
-    if (!alive && brought >= 0 && lane == 0)
-      mbar_drain(&sm.full[(sets == 2 ? brought & 1 : 0) * STAGES + brought % STAGES], brought / (STAGES * sets) & 1);
-    if (__syncthreads_or(!alive)) return;
-  } else {
-    cp_async_wait<0>();
-    __syncthreads();
-  }
+  cp_async_wait<0>();
+  __syncthreads();
 
-  // merge the key groups' partials in shared memory (the ring is free now): [KP][R][DH], then the running maxima (in
+  // merge the key groups' partials in shared memory (the ring is free now): [KW][R][DH], then the running maxima (in
   // the partials' units, where P is at most 2^15) and sums
   static_assert((KW * C::kMergeRows * DH + 2 * KW * C::kMergeRows) * 4 <= 2 * STAGES * KT * DH, "merge fits the ring");
   static_assert(kMaxRows <= 128, "one thread per row");
-  const int KP = KW * sets;
   float* sO = reinterpret_cast<float*>(sm.k[0]);
-  float* sM = sO + KP * R * DH;  // [KP][R]
-  float* sL = sM + KP * R;       // [KP][R]
+  float* sM = sO + KW * R * DH;  // [KW][R]
+  float* sL = sM + KW * R;       // [KW][R]
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf) {
     ls[hf] += __shfl_xor_sync(0xffffffffu, ls[hf], 1);
     ls[hf] += __shfl_xor_sync(0xffffffffu, ls[hf], 2);
-    const int row = (set * KW + kw) * R + mt * 16 + g4 + 8 * hf;
+    const int row = kw * R + mt * 16 + g4 + 8 * hf;
     if (t4 == 0 && dw == 0) {
       sM[row] = mx[hf] - kShift;
       sL[row] = ls[hf];
@@ -510,9 +396,9 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
   const bool bad = sm.bad_page != 0;
   if (tid < R) {  // one thread per row: its maximum and sum over the key groups, whose weights replace their maxima
     float m = -INFINITY, l = 0.f;
-    for (int w = 0; w < KP; ++w) m = fmaxf(m, sM[w * R + tid]);
+    for (int w = 0; w < KW; ++w) m = fmaxf(m, sM[w * R + tid]);
     const float mu = m == -INFINITY ? 0.f : m;
-    for (int w = 0; w < KP; ++w) {
+    for (int w = 0; w < KW; ++w) {
       const float f = exp2f(sM[w * R + tid] - mu);
       l += f * sL[w * R + tid];
       sM[w * R + tid] = f;
@@ -527,7 +413,7 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     const int row = idx / (DH / 4), c4 = idx % (DH / 4);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
-    for (int w = 0; w < KP; ++w) {
+    for (int w = 0; w < KW; ++w) {
       const float f = sM[w * R + row];
       const float4 v = *reinterpret_cast<const float4*>(sO + (w * R + row) * DH + c4 * 4);
       o.x += f * v.x;
@@ -615,13 +501,14 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
 // Whether the tcgen05 kernel takes a step.  It reads tiles by TMA alone, in pieces of at least kTmaRows rows of a page that
 // start on 128 bytes of shared memory, and takes longer to start and end, so up to 16 query rows leave it short ranges.
 // Measured (replayed from a graph, us, tcgen05 / mma.sync, 4 streams but where said):
-//   32 over 8 heads of 128   33 x 12 tokens 12.2 / 11.0, 4 x 50 10.3 / 9.2, 4 x 150 11.8 / 11.8, 4 x 1000 15.8 / 17.4, 16 x 1000
+//   32 over 8 heads of 128   33 x 12 tokens 12.2 / 10.0, 4 x 50 10.3 / 10.1, 4 x 150 11.8 / 11.8, 4 x 1000 15.8 / 17.4, 16 x 1000
 //                            31.8 / 41.0; one stream, 7 of up to 20000 40.2 / 67.2
-//   16 over 4 of 64          3 streams, 4 x 400 11.7 / 9.7, 4 x 3000 16.8 / 18.2
+//   16 over 4 of 64          3 streams, 4 x 400 11.7 / 9.1, 4 x 3000 16.8 / 18.2
 //   24 over 2 of 256         4 x 50 14.8 / 23.8;  96 over 8 of 128: 16 x 50 13.7 / 15.1, 16 x 400 26.6 / 46.9
+constexpr int kTmaRows = 8;
 static bool q8_tc(int Dh, int prow, int rows, long long range) {
   const int piece = paged_piece(prow, 128);
-  if (piece < decq8::kTmaRows || (Dh == 64 && piece % 2 != 0)) return false;
+  if (piece < kTmaRows || (Dh == 64 && piece % 2 != 0)) return false;
   return rows > 16 || range > (Dh == 64 ? 2048 : Dh == 128 ? 256 : 0);
 }
 
@@ -631,24 +518,19 @@ size_t decode_paged_q8_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh,
   return std::max(x, q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, true, true).bytes());
 }
 
-template <int DH, bool WIDE, bool TMA>
-static cudaError_t launch_q8_t(const decq8::Params& p, cudaStream_t st) {
+template <int DH, bool WIDE>
+static cudaError_t launch_q8_t(const decq8::Args& a, cudaStream_t st) {
   using namespace decq8;
-  const int smem = (int)sizeof(Smem<DH, WIDE, TMA>) + 1024;
-  static_assert(sizeof(Smem<DH, WIDE, TMA>) + 1024 <= (WIDE ? 227 : 113) * 1024, "an SM's CTAs fit");
-  cudaError_t e = cudaFuncSetAttribute(decode_q8_kernel<DH, WIDE, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const int smem = (int)sizeof(Smem<DH, WIDE>) + 1024;
+  static_assert(sizeof(Smem<DH, WIDE>) + 1024 <= (WIDE ? 227 : 113) * 1024, "an SM's CTAs fit");
+  cudaError_t e = cudaFuncSetAttribute(decode_q8_kernel<DH, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(true, decode_q8_kernel<DH, WIDE, TMA>, dim3((unsigned)p.a.nsplit * p.a.B * p.a.Hkv * p.a.ngroups),
-                       (unsigned)(p.a.mt * p.a.sets) * 128, smem, st, p);
+  return launch_kernel(true, decode_q8_kernel<DH, WIDE>, dim3((unsigned)a.nsplit * a.B * a.Hkv * a.ngroups),
+                       (unsigned)a.rg / 16 * 128, smem, st, a);
 }
 template <int DH>
-static cudaError_t launch_q8_d(decq8::Params& p, bool tma, cudaStream_t st) {
-  // two sets only where the stages' number is odd (a stage serves both)
-  static_assert(decq8::Cfg<256, true>::STAGES % 2 == 1, "");
-  const bool wide = p.a.mt > decq8::Cfg<DH, false>::MT;
-  p.a.sets = !tma ? 1 : DH == 64 && p.a.mt == 1 ? 1 : p.a.mt == (wide ? 2 : 1) ? 2 : 1;
-  if (wide) return tma ? launch_q8_t<DH, true, true>(p, st) : launch_q8_t<DH, true, false>(p, st);
-  return tma ? launch_q8_t<DH, false, true>(p, st) : launch_q8_t<DH, false, false>(p, st);
+static cudaError_t launch_q8_d(const decq8::Args& a, cudaStream_t st) {
+  return a.rg > 16 * decq8::Cfg<DH, false>::MT ? launch_q8_t<DH, true>(a, st) : launch_q8_t<DH, false>(a, st);
 }
 
 cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void* vc, const uint8_t* ks, const uint8_t* vs,
@@ -670,7 +552,6 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   a.blocks = P / T;
   a.d_brow = make_fast_div((uint32_t)(T * n));
   a.d_blocks = make_fast_div((uint32_t)a.blocks);
-  a.mt = plan.rg / 16;
   a.lens = lens;
   a.o = (bf16*)o;
   a.lse = lse;
@@ -699,19 +580,17 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   a.d_heads = make_fast_div((uint32_t)(Hkv * plan.ngroups));
   const int KT = !tc && Dh == 256 ? decq8::ktile<256>() : decq8::ktile<128>();
   a.piece = paged_piece(a.pg.prow, KT);
-  // a piece's rows start on 128 bytes of shared memory
-  const bool tma = a.piece >= decq8::kTmaRows && (Dh >= 128 || a.piece % 2 == 0);
-  a.tile = tma ? KT / a.piece * a.piece : n <= KT ? KT / n * n : KT;  // cp.async: whole tokens where a tile holds one
+  a.tile = tc ? KT / a.piece * a.piece : n <= KT ? KT / n * n : KT;  // whole pieces; whole tokens where a tile holds one
   a.d_tile = make_fast_div((uint32_t)a.tile);
   a.balanced = tc && B > 1 && B <= dec::kBalancedSeqs && plan.nsplit > 1 && range / plan.nsplit >= 4 * 64 &&
                B * (range / a.tile + 1) < (1LL << 30);  // the tiles of all sequences, counted in 32 bits
-  if (tma && (!make_q8_tmap(&p.tm_k, kc, num_pages, Hkv, a.pg.prow, Dh, a.piece) ||
-              !make_q8_tmap(&p.tm_v, vc, num_pages, Hkv, a.pg.prow, Dh, a.piece)))
+  if (tc && (!make_q8_tmap(&p.tm_k, kc, num_pages, Hkv, a.pg.prow, Dh, a.piece) ||
+             !make_q8_tmap(&p.tm_v, vc, num_pages, Hkv, a.pg.prow, Dh, a.piece)))
     return cudaErrorInvalidValue;
   const cudaError_t e = tc          ? launch_decode_q8_tc(p, Dh, st)
-                        : Dh == 64  ? launch_q8_d<64>(p, tma, st)
-                        : Dh == 128 ? launch_q8_d<128>(p, tma, st)
-                                    : launch_q8_d<256>(p, tma, st);
+                        : Dh == 64  ? launch_q8_d<64>(a, st)
+                        : Dh == 128 ? launch_q8_d<128>(a, st)
+                                    : launch_q8_d<256>(a, st);
   return e != cudaSuccess || a.nsplit == 1 ? e : launch_combine_paged(a, Dh, st);
 }
 
