@@ -1,21 +1,36 @@
-// Decoding over the 8-bit paged cache on the 5th-generation tensor cores (head dims 128 and 256; the mathematics of x, m
-// and the scales: sfa_decode_q8.cu).
+// Decoding over the 8-bit paged cache on the 5th-generation tensor cores (the mathematics of x, m and the scales:
+// sfa_decode_q8.cu).
 //
 // K and V go from TMA to the products as the codes that they are; only scores pass through registers.  Both products
-// have the cached positions or the head dim as their 128 rows, and the few query rows as columns, so that no row of a
+// have the cached positions or the head dim as their rows, and the few query rows as columns, so that no row of a
 // tile is empty and a thread has one position:
 //   S^T [128 positions x 2 R] = K (e4m3) * [q_hi | q_lo]^T (e4m3): a row's bf16 values, scaled by a power of two to [2^7,
-//     2^8), are hi + lo / 16 in two codes, exact for values down to 2^-14 of the row's largest and to 2^-22 of it below;
-//   O^T [Dh x R] += V^T (e4m3) * P^T (e5m2), three times: P is hi + mid + lo in three codes of three bits, so rounded to nine
-//     bits (of its f16 form), down to steps of 2^-16; it is at most 2^15, and 2^11 or more at the row's largest score.
-// A thread of a softmax warp takes its position's scores for the warp group's RW rows: scales by 2^ek, adds ev, masks
-// (what a position is visible to is a range of rows), and subtracts the row's reference.  References are the whole
-// CTA's, in shared memory, and go up only when some P would pass 2^15 (a vote for each tile): then the rows' maxima are
-// reduced over the warps, O in tensor memory is rescaled, and the scores' references follow.
+//     2^8), are hi + lo / 16 in two codes, exact for values down to 2^-14 of the row's largest and to 2^-22 of it below.  K is
+//     read from shared memory once.  Where tensor memory has no room for two columns a row (R = 32 and 64 at head dim
+//     256), three e5m2 codes of the query's f16 form one after another instead, which read K three times.
+//   O^T [Dh x 3 R] += V^T (e4m3) * [P_hi | P_mid | P_lo] (e5m2): three codes of three bits, so P is rounded to nine bits (of
+//     its f16 form), half a step 2^-9 of it.  A row's largest P is 2^5 when its reference is set, and at most 2^15 before
+//     it goes up; the third codes hold 64 times what they stand for, so steps end at 2^-22, 2^-27 of the row's largest.
+//     The three columns are added at the end.
+// A thread of a softmax warp takes its position's scores for its group's 16 rows: scales by 2^ek, adds ev, masks (what
+// a position is visible to is a range of rows), and subtracts the row's reference.  References are the group's, in
+// shared memory, and go up only when some P would pass 2^15 (a vote for each tile; every tile after the first few has
+// none): then the rows' maxima are reduced over the four warps, and sums and O in tensor memory are rescaled.
 //
-// Warp 0 brings tiles (TMA, pieces of pages), warp 1 issues the products, the others are WG groups of four softmax warps
-// with RW rows each.  S and P have two buffers, so S of the next tile is computed under this one's softmax and its P V
-// under the next one's.  Two CTAs an SM where shared and tensor memory hold them.
+// Warp 0 brings tiles (TMA, pieces of pages) into a ring of units of 128 columns, warp 1 issues the products, the
+// others are R / 16 groups of four softmax warps.  S and P have two buffers, so S of the next tile is computed under this
+// one's softmax and its P V under the next one's.  The first group brings the scales 384 blocks ahead, since a load
+// behind a saturated memory's queue takes thousands of cycles, and a batch's splits are shared out by the sequences'
+// lengths, as for the bf16 cache (8 sequences of up to 16384 tokens, 4 streams: 32 over 8 heads of 128 139 us without the two
+// and 133 with them, 24 over 2 heads of 256 140 and 88).
+//
+// Bound by memory at 16 query rows, of 8 heads of 128: 16 sequences of 32768 tokens, 32 over 8 heads, 395 us (6.87
+// TB/s of codes and scales; floor 400 at the copy rate), 16384 tokens of 8 114.  With more rows the softmax warps' issue and
+// latency pass it, about 420 instructions for 16 rows of a warp's 32 positions: 32 rows reach 0.74 of the copy rate, 48
+// 0.56, 64 0.46 (equal lengths), more than 64 read the cache once for each group of 64 (96 rows: 0.31); 24 rows of heads
+// of 256 0.72.  Three CTAs an SM at 16 rows (up to head dim 128) hide a tile's chain of barriers: 133 us with two, 114 with
+// three.  Tried and dropped: warps of 24 to 48 rows (registers: fewer warps to hide the latency), two tiles in turn with
+// an O each, queries in three codes everywhere (K's reads three times: bound by shared memory at 16 rows).
 #include <float.h>
 
 #include <algorithm>
@@ -28,13 +43,14 @@ using decq8::Args;
 using decq8::Params;
 
 constexpr int KT = 128;            // positions of a tile
+constexpr int RW = 16;             // query rows of a warp group
 constexpr float kTop = 15.f;       // P's largest exponent
 constexpr float kSet = 5.f;        // the exponent of a row's largest P when its reference is set
 constexpr float kLow = 64.f;       // P's third codes hold so many times what they stand for
 constexpr float kLo = 16.f;        // a query's second e4m3 codes too
 
 // HV units of a K or V tile, of RB columns (128, or 64 at head dim 64) each: a ring slot.  R query rows: WG warp groups of RW.
-template <int DH, int RW, int WG>
+template <int DH, int WG>
 struct Cfg {
   static constexpr int R = RW * WG, kThreads = 64 + WG * 128;
   static constexpr int RB = DH < 128 ? DH : 128, HV = DH / RB, kUnit = KT * RB;
@@ -52,9 +68,9 @@ struct Cfg {
   static constexpr int NSLOT = kRoom < 10 ? kRoom : 10;
 };
 
-template <int DH, int RW, int WG>
+template <int DH, int WG>
 struct Smem {
-  using C = Cfg<DH, RW, WG>;
+  using C = Cfg<DH, WG>;
   uint8_t ring[C::NSLOT][C::kUnit];          // [128 positions][RB bytes], swizzled by 128 bytes (64)
   uint8_t q[C::HV][C::QT][C::R * C::RB];     // codes: [R rows][RB bytes], swizzled so too
   uint8_t p[2][3][C::R * KT];                // a buffer's hi, mid, lo: blocks of 16 rows, [128 positions][16 bytes]
@@ -65,7 +81,7 @@ struct Smem {
   float up[C::R], fac[C::R];                 // what the reference goes up by, negated; 2^ that
   float most[4][C::R];                       // a warp's maxima, or sums
   uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], sc_full[8], drain;
-  unsigned long long raise[WG];              // rows whose references go up
+  unsigned raise[WG];                        // rows whose references go up
   uint32_t tmem_base;
   unsigned not_finite[2];
   int abort, bad_page, gave_up[WG];
@@ -136,28 +152,12 @@ HD_DEVINLINE uint32_t hsub2(uint32_t a, uint32_t b) {
   asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
-// A bit for each row of a warp group.
-template <int RW>
-struct Rows {
-  typedef uint32_t Mask;
-};
-template <>
-struct Rows<48> {
-  typedef uint64_t Mask;
-};
 // Bits [lo, hi) of RW, the range cut to them.
-template <int RW>
-HD_DEVINLINE typename Rows<RW>::Mask bits(int lo, int hi) {
+HD_DEVINLINE uint32_t bits(int lo, int hi) {
   lo = min(max(lo, 0), RW);
   hi = min(max(hi, 0), RW);
-  return hi <= lo ? 0 : (typename Rows<RW>::Mask)((1ull << hi) - (1ull << lo));
+  return hi <= lo ? 0u : (1u << hi) - (1u << lo);
 }
-HD_DEVINLINE uint32_t warp_or(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
-HD_DEVINLINE uint64_t warp_or(uint64_t x) {
-  return (uint64_t)__reduce_or_sync(0xffffffffu, (uint32_t)(x >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (uint32_t)x);
-}
-HD_DEVINLINE int first_bit(uint32_t x) { return __ffs(x) - 1; }
-HD_DEVINLINE int first_bit(uint64_t x) { return __ffsll((long long)x) - 1; }
 // `bytes` of four bytes, the others zero.
 HD_DEVINLINE void cp_async_4(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(bytes));
@@ -177,11 +177,11 @@ HD_DEVINLINE void split3(uint32_t u, uint32_t& hi, uint32_t& mid, uint32_t& lo) 
   lo += 0x00800080u;
 }
 
-template <int DH, int RW, int WG>
-__global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kPerSm)
+template <int DH, int WG>
+__global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
     decode_q8_tc_kernel(const __grid_constant__ Params P) {
-  using C = Cfg<DH, RW, WG>;
-  using Sm = Smem<DH, RW, WG>;
+  using C = Cfg<DH, WG>;
+  using Sm = Smem<DH, WG>;
   constexpr int R = C::R, NSLOT = C::NSLOT, NT = C::kThreads, HV = C::HV, RB = C::RB, kUnit = C::kUnit;
   const Args& a = P.a;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -193,11 +193,12 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
   float* po = a.part_o + pidx * R * DH;
   float2* pml = a.part_ml + pidx * R;
   const int tile = a.tile, row0 = rg * R, rows = min(R, a.M - row0);
-  // positions of a tile that no piece fills: their V must not be NaN
+  // positions of a tile that no piece fills: their V must not be NaN, nor may their scales, which may not have come yet
   for (int i = tid; i < NSLOT * (KT - tile) * (RB / 16); i += NT) {
     const int per = (KT - tile) * (RB / 16);
     reinterpret_cast<uint4*>(sm.ring[i / per] + tile * RB)[i % per] = make_uint4(0, 0, 0, 0);
   }
+  for (int i = tid; i < 512; i += NT) reinterpret_cast<uint32_t*>(sm.scale)[i] = 0;
   if (tid == 0) {
     for (int i = 0; i < NSLOT; ++i) {
       mbar_init(&sm.full[i], 1);
@@ -337,9 +338,7 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
     for (int j = 0; go && j < nt; ++j) {
       nxt = place(j + 1);
       fetch(j + 2);
-      if (j + 1 < nt) {
-        go = load(&P.tm_k, nxt);
-      }
+      if (j + 1 < nt) go = load(&P.tm_k, nxt);
       go = go && load(&P.tm_v, cur);
       cur = nxt;
     }
@@ -408,12 +407,11 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
     mbar_drain(&sm.drain, 0);
   } else {
     // ------------------------------------------------------------ softmax: a thread per position
-    typedef typename Rows<RW>::Mask Mask;
     const int wg = (warp - 2) >> 2, q4 = warp & 3, key = q4 * 32 + lane, r0 = wg * RW, bar = 1 + wg;
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16), tO = tl + 2 * C::SC + r0;
     const int own_lo = (T - 1) * a.n, win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;
     const int seen = a.mode == SFA_LOCAL ? own_lo - a.window + 1 : 0;
-    const Mask real = bits<RW>(0, rows - r0);
+    const uint32_t real = bits(0, rows - r0);
     // The first group brings the scales, 128 blocks (a chunk) at a time, a thread each, by cp.async: behind a saturated
     // memory's queue a load takes thousands of cycles.  Blocks are counted from the split's first.  As chunk c is handed on,
     // the words that hold the bytes of chunk c + 3 are asked for (cut to the scales' array; a byte's place is kept), and
@@ -473,7 +471,7 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
     uint64_t l[RW / 2];  // pairs of rows' sums over this thread's positions
 #pragma unroll
     for (int r = 0; r < RW / 2; ++r) l[r] = 0;
-    Mask set = 0;  // rows whose reference is set
+    uint32_t set = 0;  // rows whose reference is set
     bool ok = true;
     const int brow = a.pg.prow / a.blocks;
     int waited = 0;                               // chunks that this warp has waited for
@@ -492,15 +490,16 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
         scales_end += 128ll * brow;
       }
       // the rows that see this position: a range
-      Mask vis = real;
+      uint32_t vis = real;
       if (a.mode == SFA_WITHIN && a.n > 1) {
         const int s = p - fast_div(p, a.d_n) * a.n;
-        vis &= bits<RW>(s * a.G - row0 - r0, (s + 1) * a.G - row0 - r0);
+        vis &= bits(s * a.G - row0 - r0, (s + 1) * a.G - row0 - r0);
       }
       if (base + tile > edge || base <= win_hi) {
-        const int first = max(p - own_lo, 0) * a.G - row0 - r0;  // rows of the streams from p's own on, where p is the new token's
-        const int last = a.mode == SFA_LOCAL ? (int)min((long long)(p - own_lo + a.window) * a.G - row0 - r0, 64ll) : 64;
-        vis = key < tile && p < k1 ? vis & bits<RW>(p < own_lo ? 0 : first, last) : (Mask)0;
+        // rows of the streams from p's own on, where p is the new token's
+        const int first = max(p - own_lo, 0) * a.G - row0 - r0;
+        const int last = a.mode == SFA_LOCAL ? (int)min(((long long)p - own_lo + a.window) * a.G - row0 - r0, (long long)RW) : RW;
+        vis = key < tile && p < k1 ? vis & bits(p < own_lo ? 0 : first, last) : (uint32_t)0;
       }
       // (A wait that gave up: the warp goes on to the group's next vote, since the others may wait for it there, and all
       // leave after it.)
@@ -515,11 +514,8 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
       float y[RW];
       {
         float low[RW];
-#pragma unroll
-        for (int c = 0; c < RW; c += 16) {
-          tmem_ld16(tl + sb * C::SC + r0 + c, reinterpret_cast<uint32_t*>(y) + c);
-          if (C::kPair) tmem_ld16(tl + sb * C::SC + R + r0 + c, reinterpret_cast<uint32_t*>(low) + c);
-        }
+        tmem_ld16(tl + sb * C::SC + r0, reinterpret_cast<uint32_t*>(y));
+        if (C::kPair) tmem_ld16(tl + sb * C::SC + R + r0, reinterpret_cast<uint32_t*>(low));
         tmem_ld_wait();
         if (C::kPair)
 #pragma unroll
@@ -546,17 +542,17 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
       if (group_any(bar, !ok || top > kTop || (vis & ~set) != 0)) {
         // New references for the rows (of the whole group) of which some P would pass 2^kTop, or which have none yet:
         // their largest P to 2^kSet.
-        Mask mask = vis & ~set;
+        uint32_t mask = vis & ~set;
 #pragma unroll
         for (int r = 0; r < RW; ++r)
-          if (y[r] > kTop) mask |= (Mask)1 << r;
-        mask = warp_or(mask);
+          if (y[r] > kTop) mask |= (uint32_t)1 << r;
+        mask = __reduce_or_sync(0xffffffffu, mask);
         if (lane == 0) {
-          if (mask != 0) atomicOr(&sm.raise[wg], (unsigned long long)mask);
+          if (mask != 0) atomicOr(&sm.raise[wg], mask);
           if (!ok) sm.gave_up[wg] = 1;
         }
         named_bar_sync(bar, 128);
-        mask = (Mask)*(volatile unsigned long long*)&sm.raise[wg];
+        mask = *(volatile unsigned*)&sm.raise[wg];
         if (*(volatile int*)&sm.gave_up[wg]) {
           ok = false;
           break;
@@ -590,8 +586,8 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
           f2unpack(fadd2(f2pack(y[r], y[r + 1]), *reinterpret_cast<const uint64_t*>(sm.up + r0 + r)), y[r], y[r + 1]);
         }
         if (scale_o) {
-          for (Mask left = mask & set; left; left &= left - 1) {
-            const int r = first_bit(left);
+          for (uint32_t left = mask & set; left; left &= left - 1) {
+            const int r = __ffs(left) - 1;
             tmem_scale<3 * HV, R>(tO + r, sm.fac[r0 + r]);
           }
           tmem_st_wait();
@@ -601,15 +597,14 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
       if (!ok) continue;
       // S of this tile was issued behind the products of the tile before the last, so these are done: P's buffer is free
       const uint64_t inv2 = f2pack(inv, inv);
-#pragma unroll
-      for (int c = 0; c < RW; c += 16) {
+      {
         uint4 t[3];
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
           uint32_t hi[2], mid[2], lo[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const int r = c + h * 4 + i * 2;
+            const int r = h * 4 + i * 2;
             const float p0 = ex2_approx(y[r]), p1 = ex2_approx(y[r + 1]);
             l[r / 2] = ffma2(f2pack(p0, p1), inv2, l[r / 2]);
             const __half2 u = __floats2half2_rn(p0, p1);
@@ -619,7 +614,7 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
           (&t[1].x)[h] = __byte_perm(mid[0], mid[1], 0x7531);
           (&t[2].x)[h] = __byte_perm(lo[0], lo[1], 0x7531);
         }
-        const int at = ((r0 + c) >> 4) * (KT * 16) + key * 16;
+        const int at = wg * (KT * 16) + key * 16;
 #pragma unroll
         for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4*>(sm.p[sb][i] + at) = t[i];
       }
@@ -656,25 +651,21 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
       const int column = RB == 128 ? key : lane < 16 ? q4 * 16 + lane : -1;
 #pragma unroll
       for (int hf = 0; hf < HV; ++hf)
-#pragma unroll
-        for (int c = 0; c < RW; c += 16) {
+        {
           uint32_t o[3][16];
 #pragma unroll
-          for (int i = 0; i < 3; ++i) tmem_ld16(tO + (hf * 3 + i) * R + c, o[i]);
+          for (int i = 0; i < 3; ++i) tmem_ld16(tO + (hf * 3 + i) * R, o[i]);
           tmem_ld_wait();
           uint32_t wrong = 0;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float x = fmaf(__uint_as_float(o[2][e]), 1.f / kLow, __uint_as_float(o[0][e]) + __uint_as_float(o[1][e]));
             if (column < 0) continue;
-            po[(size_t)(r0 + c + e) * DH + hf * RB + column] = x;
+            po[(size_t)(r0 + e) * DH + hf * RB + column] = x;
             if (!(fabsf(x) <= FLT_MAX)) wrong |= 1u << e;
           }
           wrong = __reduce_or_sync(0xffffffffu, wrong);
-          if (wrong != 0 && lane == 0) {
-            const int at = r0 + c;
-            atomicOr(&sm.not_finite[at >> 5], wrong << (at & 31));
-          }
+          if (wrong != 0 && lane == 0) atomicOr(&sm.not_finite[r0 >> 5], wrong << (r0 & 31));
         }
       // sums over the positions: a warp's, then the four warps'
 #pragma unroll
@@ -727,34 +718,36 @@ __global__ void __launch_bounds__(Cfg<DH, RW, WG>::kThreads, Cfg<DH, RW, WG>::kP
 
 // ------------------------------------------------------------------ host side
 
-
-template <int DH, int RW, int WG>
+template <int DH, int WG>
 static cudaError_t launch_t(const decq8::Params& p, cudaStream_t st) {
   using namespace decq8tc;
-  using C = Cfg<DH, RW, WG>;
-  const int smem = (int)sizeof(Smem<DH, RW, WG>) + 1024;
-  static_assert(sizeof(Smem<DH, RW, WG>) + 1024 <= (C::kPerSm == 3 ? 75 : C::kPerSm == 2 ? 113 : 227) * 1024 && C::NSLOT >= 3 &&
+  using C = Cfg<DH, WG>;
+  const int smem = (int)sizeof(Smem<DH, WG>) + 1024;
+  static_assert(sizeof(Smem<DH, WG>) + 1024 <= (C::kPerSm == 3 ? 75 : C::kPerSm == 2 ? 113 : 227) * 1024 && C::NSLOT >= 3 &&
                     C::kCols <= C::kAlloc && C::kPerSm * C::kAlloc <= 512,
                 "an SM's CTAs fit");
-  cudaError_t e = cudaFuncSetAttribute(decode_q8_tc_kernel<DH, RW, WG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(decode_q8_tc_kernel<DH, WG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(true, decode_q8_tc_kernel<DH, RW, WG>, dim3((unsigned)p.a.nsplit * p.a.B * p.a.Hkv * p.a.ngroups),
+  return launch_kernel(true, decode_q8_tc_kernel<DH, WG>, dim3((unsigned)p.a.nsplit * p.a.B * p.a.Hkv * p.a.ngroups),
                        (unsigned)C::kThreads, smem, st, p);
 }
 
 template <int DH>
 static int per_sm(int rows) {
   using namespace decq8tc;
-  return rows <= 16 ? Cfg<DH, 16, 1>::kPerSm : rows <= 32 ? Cfg<DH, 16, 2>::kPerSm : rows <= 48 ? Cfg<DH, 16, 3>::kPerSm : Cfg<DH, 16, 4>::kPerSm;
+  return rows <= 16   ? Cfg<DH, 1>::kPerSm
+         : rows <= 32 ? Cfg<DH, 2>::kPerSm
+         : rows <= 48 ? Cfg<DH, 3>::kPerSm
+                      : Cfg<DH, 4>::kPerSm;
 }
 int decode_q8_tc_per_sm(int rows, int Dh) { return Dh == 64 ? per_sm<64>(rows) : Dh == 128 ? per_sm<128>(rows) : per_sm<256>(rows); }
 
 template <int DH>
 static cudaError_t launch_d(const decq8::Params& p, cudaStream_t st) {
-  if (p.a.rg == 16) return launch_t<DH, 16, 1>(p, st);
-  if (p.a.rg == 32) return launch_t<DH, 16, 2>(p, st);
-  if (p.a.rg == 48) return launch_t<DH, 16, 3>(p, st);
-  return launch_t<DH, 16, 4>(p, st);
+  if (p.a.rg == 16) return launch_t<DH, 1>(p, st);
+  if (p.a.rg == 32) return launch_t<DH, 2>(p, st);
+  if (p.a.rg == 48) return launch_t<DH, 3>(p, st);
+  return launch_t<DH, 4>(p, st);
 }
 
 cudaError_t launch_decode_q8_tc(decq8::Params& p, int Dh, cudaStream_t st) {

@@ -49,7 +49,7 @@ def _decode(q, kc, vc, ks, vs, table, lens, n, mode, window=0, max_tokens=None, 
     return o.cpu(), lse.cpu() if with_lse else None, int(st.item())
 
 
-def _assert_rows(o, lse, q, kv, vv, T, b, n, mode, window, scale=0.0, lse_tol=1e-3):
+def _assert_rows(o, lse, q, kv, vv, T, b, n, mode, window, scale=0.0):
     """Sequence b's rows against the oracle on the values."""
     a = (q[b:b + 1], kv[b:b + 1], vv[b:b + 1], _i32([T]), n, mode)
     o_r, lse_r, bad = oracle.decode(*a, window=window, scale=scale)
@@ -59,7 +59,7 @@ def _assert_rows(o, lse, q, kv, vv, T, b, n, mode, window, scale=0.0, lse_tol=1e
     lim = 2.0**-8 * o_r[0].abs() + (2.0**-9 + 2.0**-11 + 1e-3) * A[0] + 1e-3 * o_r[0].abs()
     assert bool((err <= lim).all()), float((err / lim).max())
     if lse is not None:
-        assert float((lse[b].double() - lse_r[0]).abs().max()) <= lse_tol
+        assert float((lse[b].double() - lse_r[0]).abs().max()) <= 1e-3
 
 
 def _assert_empty(o, lse, b):
@@ -138,7 +138,32 @@ def test_scores_that_change(shape, B, n, Hq, Hkv, Dh, P, T, L):
         o, lse, st = _decode(q, kq, vq, ks, vs, table, _i32(lens), n, mode, w)
         assert st == 0
         for b in few:
-            _assert_rows(o, lse, q, kv, vv, lens[b], b, n, mode, w, lse_tol=1e-3)
+            _assert_rows(o, lse, q, kv, vv, lens[b], b, n, mode, w)
+
+
+# sequences whose tables name the same few pages, so that long ones in numbers stay small here: splits of one CTA and of many
+# tiles, shared out by length or not; blocks of one token, whose scales a split's first positions share with nobody, over
+# and over; pieces that leave positions of a tile over; scales whose bytes end inside a word
+@pytest.mark.parametrize("B,n,Hq,Hkv,Dh,P,T", [(132, 1, 8, 4, 64, 48, 1), (132, 1, 8, 4, 64, 16, 16), (100, 4, 12, 3, 128, 12, 1),
+                                               (60, 1, 9, 9, 128, 24, 1), (12, 4, 32, 8, 128, 16, 16), (24, 2, 48, 8, 128, 15, 1),
+                                               (128, 1, 12, 3, 256, 9, 9), (20, 4, 48, 1, 256, 10, 5), (9, 8, 72, 3, 128, 11, 11)])
+def test_long_sequences_in_numbers(B, n, Hq, Hkv, Dh, P, T):
+    L = 1500
+    q, kc, vc = _case(2, L, n, Hq, Hkv, Dh, B + P)
+    kq, ks, table, kv = q8.quantised(kc, [L, L], P, T, n, 3)
+    vq, vs, _, vv = q8.quantised(vc, [L, L], P, T, n, 3)
+    which = [b % 2 for b in range(B)]
+    lens = [1 + (b * 977) % L for b in range(B)]
+    lens[0], lens[1], lens[2], lens[3], lens[-1] = L, 0, -5, L + 1, L
+    q = torch.cat([q, inputs.normal_bf16((B - 2, n, Hq, Dh), 77)])
+    for mode, w in ((CROSS, 0), (WITHIN, 0), (LOCAL, 700 * n + 1)):
+        o, lse, st = _decode(q, kq, vq, ks, vs, table[which], _i32(lens), n, mode, w, max_tokens=L)
+        assert st == binding.HD_DEVBIT_INDEX
+        for b in (1, 2, 3):
+            _assert_empty(o, lse, b)
+        for b in (0, 4, 5, B // 2, B - 1):
+            i = which[b]
+            _assert_rows(o[b:b + 1], lse[b:b + 1], q[b:b + 1], kv[i:i + 1], vv[i:i + 1], lens[b], 0, n, mode, w)
 
 
 @pytest.mark.parametrize("Dh,P", [(64, 16), (128, 16), (256, 16), (128, 3)])
