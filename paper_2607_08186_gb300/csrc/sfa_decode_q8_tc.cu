@@ -48,6 +48,7 @@ constexpr float kTop = 15.f;       // P's largest exponent
 constexpr float kSet = 5.f;        // the exponent of a row's largest P when its reference is set
 constexpr float kLow = 64.f;       // P's third codes hold so many times what they stand for
 constexpr float kLo = 16.f;        // a query's second e4m3 codes too
+constexpr uint32_t kGaveUp = 1u << 31;
 
 // HV units of a K or V tile, of RB columns (128, or 64 at head dim 64) each: a ring slot.  R query rows: WG warp groups of RW.
 template <int DH, int WG>
@@ -60,7 +61,7 @@ struct Cfg {
   static constexpr int SC = kPair ? 2 * R : R, QT = kPair ? 2 : 3;  // columns of S; codes of a query's value
   static constexpr int kCols = 2 * SC + 3 * HV * R;  // tensor memory: two S, three O
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr int kFixed = QT * R * DH + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 8 * R + 512;  // all but the ring
+  static constexpr int kFixed = QT * R * DH + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 9 * R + 512;  // all but the ring
   static constexpr int kPerSm = kAlloc <= 128 && kFixed + 3 * kUnit <= 74 * 1024    ? 3
                                 : kAlloc <= 256 && R <= 32 && kFixed + 3 * kUnit <= 112 * 1024 ? 2
                                                                                     : 1;
@@ -77,14 +78,14 @@ struct Smem {
   uint2 words[4][128];                       // of chunks: the words of K's and V's scales that hold a block's byte
   int entry[4][128];                         // its page entry
   uint16_t scale[8 * 128];                   // blocks' scale bytes, K's and V's above it
-  float rowf[C::R], nref[C::R];              // a row's factor of q; its reference, negated
-  float up[C::R], fac[C::R];                 // what the reference goes up by, negated; 2^ that
+  float rowf[C::R];                          // a row's factor of q
+  float nref[4][C::R];                       // its reference, negated: a copy for each warp of the group
   float most[4][C::R];                       // a warp's maxima, or sums
-  uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], sc_full[8], drain;
-  unsigned raise[WG];                        // rows whose references go up
+  uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], sc_full[8], q_full, drain;
+  unsigned raise[4 * WG];                    // a warp's rows whose references go up; kGaveUp
   uint32_t tmem_base;
   unsigned not_finite[2];
-  int abort, bad_page, gave_up[WG];
+  int abort, bad_page;
 };
 
 // kind::f8f6f4, fp32 D: operand types 0 e4m3, 1 e5m2.
@@ -211,10 +212,10 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
       mbar_init(&sm.pv_done[i], 1);
     }
     for (int i = 0; i < 8; ++i) mbar_init(&sm.sc_full[i], 4);
+    mbar_init(&sm.q_full, 4 * WG);
     mbar_init(&sm.drain, 1);
     sm.abort = sm.bad_page = 0;
     sm.not_finite[0] = sm.not_finite[1] = 0;
-    for (int i = 0; i < WG; ++i) sm.raise[i] = 0, sm.gave_up[i] = 0;
     fence_mbar_init();
   }
   if (warp == 0) {
@@ -225,64 +226,18 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
       tma_prefetch(&P.tm_v);
     }
   }
-  grid_dep_wait();
-  grid_dep_launch();
-  const dec::PagedSplit share(a, split, blockIdx.x == 0 && warp == 0);
-  const int b = share.b, T = share.T, k0 = share.k0, k1 = share.k1;
-  const int32_t* table = a.table + (long long)b * a.pg.max_pages;
-  const int nt = k0 < k1 ? fast_div(k1 - k0 + tile - 1, a.d_tile) : 0;
-  // the queries: a warp per row
-  if (nt > 0)
-    for (int rr = warp; rr < R; rr += NT / 32) {
-      constexpr int NP = DH / 64;  // pairs of a lane
-      uint32_t w[NP], most = 0;
-#pragma unroll
-      for (int i = 0; i < NP; ++i) w[i] = 0;
-      if (rr < rows) {
-        const int r = row0 + rr, s = fast_div(r, a.d_G), h = g * a.G + r - s * a.G;
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (((long long)b * a.n + s) * a.Hq + h) * DH) + lane * NP;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) w[i] = src[i];
-      }
-#pragma unroll
-      for (int i = 0; i < NP; ++i) most = max(most, max(w[i] << 16 & 0x7fff0000u, w[i] & 0x7fff0000u));
-      most = __reduce_max_sync(0xffffffffu, most);
-      // the exponent field of the largest magnitude, kept where both powers are normal
-      const int e = min(max((int)(most >> 23), 20), 254);
-      constexpr int kUp = C::kPair ? 7 : 14;  // the largest to [2^kUp, 2^(kUp + 1))
-      const float to = __int_as_float(min(127 + kUp + 127 - e, 254) << 23);  // 2^(kUp - (e - 127)), at most 2^127
-      const float back = __int_as_float(max(e - kUp, 1) << 23);              // 2^(e - 127 - kUp)
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const float x0 = __uint_as_float(w[i] << 16) * to, x1 = __uint_as_float(w[i] & 0xffff0000u) * to;
-        uint32_t t[3];
-        if (C::kPair) {
-          t[0] = q8::code2(x0, x1);
-          const float2 y = q8::values2((uint16_t)t[0]);
-          t[1] = q8::code2((x0 - y.x) * kLo, (x1 - y.y) * kLo);
-        } else {
-          const __half2 u = __floats2half2_rn(x0, x1);
-          split3<false>(*reinterpret_cast<const uint32_t*>(&u), t[0], t[1], t[2]);
-#pragma unroll
-          for (int x = 0; x < 3; ++x) t[x] = __byte_perm(t[x], 0, 0x31);
-        }
-        const int c = (lane * NP + i) * 2, at = (c % RB) >> 4, off = c & 15;  // column; its 16-byte chunk
-        const int swizzled = RB == 64 ? at ^ (rr >> 1 & 3) : at ^ (rr & 7);
-#pragma unroll
-        for (int x = 0; x < C::QT; ++x)
-          *reinterpret_cast<uint16_t*>(sm.q[c / RB][x] + rr * RB + swizzled * 16 + off) = (uint16_t)t[x];
-      }
-      if (lane == 0) {
-        sm.rowf[rr] = back * a.scale_log2;
-        sm.nref[rr] = 0.f;
-      }
-    }
   fence_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm.tmem_base;
   volatile int* abort = &sm.abort;
+  grid_dep_wait();
+  grid_dep_launch();
+  const dec::PagedSplit share(a, split, blockIdx.x == 0 && warp == 0);
+  const int b = share.b, T = share.T, k0 = share.k0, k1 = share.k1;
+  const int32_t* table = a.table + (long long)b * a.pg.max_pages;
+  const int nt = k0 < k1 ? fast_div(k1 - k0 + tile - 1, a.d_tile) : 0;
   if (nt == 0) {  // nothing of this sequence in this split: an empty partial, or an empty result
     if (a.nsplit > 1) {
       for (int i = tid; i < R; i += NT) pml[i] = make_float2(-INFINITY, 0.f);
@@ -398,7 +353,8 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
       tc_commit_w(&sm.pv_done[pb]);
       return true;
     };
-    ok = issue_s(0);
+    ok = __all_sync(0xffffffffu, mbar_wait(&sm.q_full, 0, abort, a.status));
+    ok = ok && issue_s(0);
     for (int j = 0; ok && j < nt; ++j) {
       if (j + 1 < nt) ok = issue_s(j + 1);
       ok = ok && issue_pv(j);
@@ -454,19 +410,77 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
       chunk_entries(c + 6);
       cp_async_commit();
     };
+    int first[3] = {-1, -1, -1};
     if (wg == 0) {
-      int first[3], in = 0;
+      int in = 0;
 #pragma unroll
       for (int c = 0; c < 3; ++c) {
         const int pg = page_of(c * 128 + key, in);
-        first[c] = pg >= 0 ? table[pg] : -1;
+        if (pg >= 0) first[c] = table[pg];
+      }
+    }
+    {  // the queries: four rows a warp
+      constexpr int NP = DH / 64;  // pairs of a lane
+      uint32_t w[4][NP];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int rr = r0 + q4 * 4 + x;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) w[x][i] = 0;
+        if (rr < rows) {
+          const int r = row0 + rr, s = fast_div(r, a.d_G), h = g * a.G + r - s * a.G;
+          const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (((long long)b * a.n + s) * a.Hq + h) * DH) + lane * NP;
+#pragma unroll
+          for (int i = 0; i < NP; ++i) w[x][i] = src[i];
+        }
+      }
+      if (wg == 0) {
+#pragma unroll
+        for (int c = 0; c < 3; ++c) {
+          chunk_words(c, first[c]);
+          chunk_entries(c + 3);
+          cp_async_commit();
+        }
       }
 #pragma unroll
-      for (int c = 0; c < 3; ++c) {
-        chunk_words(c, first[c]);
-        chunk_entries(c + 3);
-        cp_async_commit();
+      for (int x = 0; x < 4; ++x) {
+        const int rr = r0 + q4 * 4 + x;
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) most = max(most, max(w[x][i] << 16 & 0x7fff0000u, w[x][i] & 0x7fff0000u));
+        most = __reduce_max_sync(0xffffffffu, most);
+        // the exponent field of the largest magnitude, kept where both powers are normal
+        const int e = min(max((int)(most >> 23), 20), 254);
+        constexpr int kUp = C::kPair ? 7 : 14;  // the largest to [2^kUp, 2^(kUp + 1))
+        const float to = __int_as_float(min(127 + kUp + 127 - e, 254) << 23);  // 2^(kUp - (e - 127)), at most 2^127
+        const float back = __int_as_float(max(e - kUp, 1) << 23);              // 2^(e - 127 - kUp)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const float x0 = __uint_as_float(w[x][i] << 16) * to, x1 = __uint_as_float(w[x][i] & 0xffff0000u) * to;
+          uint32_t t[3];
+          if (C::kPair) {
+            t[0] = q8::code2(x0, x1);
+            const float2 y = q8::values2((uint16_t)t[0]);
+            t[1] = q8::code2((x0 - y.x) * kLo, (x1 - y.y) * kLo);
+          } else {
+            const __half2 u = __floats2half2_rn(x0, x1);
+            split3<false>(*reinterpret_cast<const uint32_t*>(&u), t[0], t[1], t[2]);
+#pragma unroll
+            for (int y = 0; y < 3; ++y) t[y] = __byte_perm(t[y], 0, 0x31);
+          }
+          const int c = (lane * NP + i) * 2, at = (c % RB) >> 4, off = c & 15;  // column; its 16-byte chunk
+          const int swizzled = RB == 64 ? at ^ (rr >> 1 & 3) : at ^ (rr & 7);
+#pragma unroll
+          for (int y = 0; y < C::QT; ++y)
+            *reinterpret_cast<uint16_t*>(sm.q[c / RB][y] + rr * RB + swizzled * 16 + off) = (uint16_t)t[y];
+        }
+        if (lane == 0) sm.rowf[rr] = back * a.scale_log2;
       }
+      if (lane < RW) sm.nref[q4][r0 + lane] = 0.f;
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.q_full);
+      named_bar_sync(bar, 128);  // the group's rows
     }
     uint64_t l[RW / 2];  // pairs of rows' sums over this thread's positions
 #pragma unroll
@@ -528,7 +542,7 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
 #pragma unroll
       for (int c = 0; c < RW; c += 4) {
         const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(sm.rowf + r0 + c);
-        const ulonglong2 rf = *reinterpret_cast<const ulonglong2*>(sm.nref + r0 + c);
+        const ulonglong2 rf = *reinterpret_cast<const ulonglong2*>(sm.nref[q4] + r0 + c);
         f2unpack(ffma2(fmul2(f2pack(y[c], y[c + 1]), f.x), kf2, fadd2(ev2, rf.x)), y[c], y[c + 1]);
         f2unpack(ffma2(fmul2(f2pack(y[c + 2], y[c + 3]), f.y), kf2, fadd2(ev2, rf.y)), y[c + 2], y[c + 3]);
       }
@@ -543,52 +557,43 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
         // New references for the rows (of the whole group) of which some P would pass 2^kTop, or which have none yet:
         // their largest P to 2^kSet.
         uint32_t mask = vis & ~set;
+        float m = 0.f;  // lane r: row r's
 #pragma unroll
-        for (int r = 0; r < RW; ++r)
-          if (y[r] > kTop) mask |= (uint32_t)1 << r;
-        mask = __reduce_or_sync(0xffffffffu, mask);
-        if (lane == 0) {
-          if (mask != 0) atomicOr(&sm.raise[wg], mask);
-          if (!ok) sm.gave_up[wg] = 1;
+        for (int r = 0; r < RW; ++r) {
+          if (y[r] > kTop) mask |= 1u << r;
+          const int x = __reduce_max_sync(0xffffffffu, ordered(y[r] == y[r] ? y[r] : -INFINITY));
+          if (lane == r) m = from_ordered(x);
         }
-        named_bar_sync(bar, 128);
-        mask = *(volatile unsigned*)&sm.raise[wg];
-        if (*(volatile int*)&sm.gave_up[wg]) {
+        mask = __reduce_or_sync(0xffffffffu, mask | (ok ? 0 : kGaveUp));
+        if (lane < RW) sm.most[q4][r0 + lane] = m;
+        if (lane == 0) sm.raise[wg * 4 + q4] = mask;
+        named_bar_sync(bar, 128);  // (the next vote lies before these are written again)
+        mask = (sm.raise[wg * 4] | sm.raise[wg * 4 + 1]) | (sm.raise[wg * 4 + 2] | sm.raise[wg * 4 + 3]);
+        if (mask & kGaveUp) {
           ok = false;
           break;
         }
-#pragma unroll
-        for (int r = 0; r < RW; ++r)
-          if ((mask >> r) & 1u) {
-            const int m = __reduce_max_sync(0xffffffffu, ordered(y[r] == y[r] ? y[r] : -INFINITY));
-            if (lane == 0) sm.most[q4][r0 + r] = from_ordered(m);
-          }
-        const bool scale_o = (mask & set) != 0 && j > 0;
-        if (scale_o) {  // (the products of the tile before the last are done, see below: so the wait is for the right phase)
-          ok = __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort, a.status));
-          tc_fence_after();
+        float down = 0.f, fac = 1.f;  // lane r: what row r's reference goes up by, negated; 2^ that
+        if (lane < RW && (mask >> lane & 1u)) {
+          const int r = r0 + lane;
+          down = kSet - fmaxf(fmaxf(sm.most[0][r], sm.most[1][r]), fmaxf(sm.most[2][r], sm.most[3][r]));
+          sm.nref[q4][r] += down;
+          if (set >> lane & 1u) fac = ex2_approx(down);
         }
-        named_bar_sync(bar, 128);
-        if (key == 0) sm.raise[wg] = 0;
-        if (key < RW) {
-          const int r = r0 + key;
-          float down = 0.f;
-          if ((mask >> key) & 1u)
-            down = kSet - fmaxf(fmaxf(sm.most[0][r], sm.most[1][r]), fmaxf(sm.most[2][r], sm.most[3][r]));
-          sm.nref[r] += down;
-          sm.up[r] = down;
-          sm.fac[r] = (set >> key) & 1u ? ex2_approx(down) : 1.f;
-        }
-        named_bar_sync(bar, 128);
+        __syncwarp();
 #pragma unroll
         for (int r = 0; r < RW; r += 2) {
-          l[r / 2] = fmul2(l[r / 2], *reinterpret_cast<const uint64_t*>(sm.fac + r0 + r));
-          f2unpack(fadd2(f2pack(y[r], y[r + 1]), *reinterpret_cast<const uint64_t*>(sm.up + r0 + r)), y[r], y[r + 1]);
+          l[r / 2] = fmul2(l[r / 2], f2pack(__shfl_sync(0xffffffffu, fac, r), __shfl_sync(0xffffffffu, fac, r + 1)));
+          y[r] += __shfl_sync(0xffffffffu, down, r);
+          y[r + 1] += __shfl_sync(0xffffffffu, down, r + 1);
         }
-        if (scale_o) {
+        if ((mask & set) != 0 && j > 0) {
+          // (the products of the tile before the last are done, see below: so the wait is for the right phase)
+          ok = __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort, a.status));
+          tc_fence_after();
           for (uint32_t left = mask & set; left; left &= left - 1) {
             const int r = __ffs(left) - 1;
-            tmem_scale<3 * HV, R>(tO + r, sm.fac[r0 + r]);
+            tmem_scale<3 * HV, R>(tO + r, __shfl_sync(0xffffffffu, fac, r));
           }
           tmem_st_wait();
         }
@@ -642,9 +647,20 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
       if (lane == 0) mbar_arrive(&sm.p_full[sb]);
     }
     cp_async_wait<0>();
+    float sum = 0.f;  // lane r: row r's over this warp's positions
+#pragma unroll
+    for (int r = 0; r < RW; ++r) {
+      float x, other;
+      if (r & 1) f2unpack(l[r / 2], other, x);
+      else f2unpack(l[r / 2], x, other);
+#pragma unroll
+      for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+      if (lane == r) sum = x;
+    }
     ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(nt - 1) & 1], ((nt - 1) >> 1) & 1, abort, a.status));
-    if (group_any(bar, !ok)) ok = false;  // (also: every thread has read the last references)
+    if (group_any(bar, !ok)) ok = false;  // (also: every warp has read the last maxima)
     if (ok) {
+      if (lane < RW) sm.most[q4][r0 + lane] = sum;
       tc_fence_after();
       const bool bad = *(volatile int*)&sm.bad_page != 0;
       // this lane's row of O^T: all 128, or (a product of 64 rows) 16 of each 32
@@ -667,21 +683,11 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
           wrong = __reduce_or_sync(0xffffffffu, wrong);
           if (wrong != 0 && lane == 0) atomicOr(&sm.not_finite[r0 >> 5], wrong << (r0 & 31));
         }
-      // sums over the positions: a warp's, then the four warps'
-#pragma unroll
-      for (int r = 0; r < RW; ++r) {
-        float x, other;
-        if (r & 1) f2unpack(l[r / 2], other, x);
-        else f2unpack(l[r / 2], x, other);
-#pragma unroll
-        for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-        if (lane == r % 32) sm.most[q4][r0 + r] = x;
-      }
       named_bar_sync(bar, 128);
       if (key < RW) {
         const int r = r0 + key;
-        float sum = (sm.most[0][r] + sm.most[1][r]) + (sm.most[2][r] + sm.most[3][r]);
-        float m = (set >> key) & 1u ? -sm.nref[r] : -INFINITY;
+        sum = (sm.most[0][r] + sm.most[1][r]) + (sm.most[2][r] + sm.most[3][r]);
+        float m = (set >> key) & 1u ? -sm.nref[0][r] : -INFINITY;
         if (sum != sum) m = INFINITY;  // a visible score that is not finite: the combined row is NaN
         if (bad) m = -INFINITY, sum = decq8::kBadPage;
         pml[r] = make_float2(m, sum);
