@@ -15,6 +15,7 @@ struct Args : DecodeArgs {
   const uint8_t *kcodes, *vcodes, *kscale, *vscale;
   int blocks;       // blocks of a page
   FastDiv d_brow, d_blocks;  // rows of a block; blocks of a page
+  int total;        // balanced: CTAs of a K/V head and row group
 };
 struct Params {
   CUtensorMap tm_k, tm_v;

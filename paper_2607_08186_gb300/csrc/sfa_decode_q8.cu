@@ -449,7 +449,7 @@ namespace {
 // The sequences' shares of a balanced batch's splits, in front of the partials.
 constexpr size_t kShareBytes = dec::kBalancedSeqs * sizeof(int2);
 struct Q8Plan {
-  int G, M, ngroups, rg, nsplit;
+  int G, M, ngroups, rg, nsplit, total;  // total: CTAs of a K/V head and row group where the batch is balanced, or 0
   size_t part_o_bytes, part_ml_bytes;
   size_t bytes() const { return kShareBytes + ((part_o_bytes + 255) & ~size_t(255)) + part_ml_bytes; }
 };
@@ -492,7 +492,11 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
     }
   }
   p.nsplit = (int)best;
-  const size_t parts = (size_t)ctas * best;
+  // Several sequences, long splits: a wave of CTAs shares their tiles equally, whatever the lengths.
+  const long long heads = (long long)Hkv * p.ngroups, range = q8_range(maxT, n, mode, window);
+  if (tc && B > 1 && B <= dec::kBalancedSeqs && (bound || (best > 1 && range / best >= 4 * 64)))
+    p.total = (int)std::max(1LL, resident / heads);
+  const size_t parts = std::max((size_t)ctas * best, p.total > 0 ? (size_t)(p.total + B) * heads : 0);
   p.part_o_bytes = parts * p.rg * Dh * sizeof(float);
   p.part_ml_bytes = parts * p.rg * sizeof(float2);
   return p;
@@ -582,8 +586,8 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   a.piece = paged_piece(a.pg.prow, KT);
   a.tile = tc ? KT / a.piece * a.piece : n <= KT ? KT / n * n : KT;  // whole pieces; whole tokens where a tile holds one
   a.d_tile = make_fast_div((uint32_t)a.tile);
-  a.balanced = tc && B > 1 && B <= dec::kBalancedSeqs && plan.nsplit > 1 && range / plan.nsplit >= 4 * 64 &&
-               B * (range / a.tile + 1) < (1LL << 30);  // the tiles of all sequences, counted in 32 bits
+  a.balanced = plan.total > 0;
+  a.total = plan.total;
   if (tc && (!make_q8_tmap(&p.tm_k, kc, num_pages, Hkv, a.pg.prow, Dh, a.piece) ||
              !make_q8_tmap(&p.tm_v, vc, num_pages, Hkv, a.pg.prow, Dh, a.piece)))
     return cudaErrorInvalidValue;

@@ -49,6 +49,7 @@ constexpr float kSet = 5.f;        // the exponent of a row's largest P when its
 constexpr float kLow = 64.f;       // P's third codes hold so many times what they stand for
 constexpr float kLo = 16.f;        // a query's second e4m3 codes too
 constexpr uint32_t kGaveUp = 1u << 31;
+constexpr float kRedo = -2.f;      // as a partial's sum: the row is to be computed again (exact_row)
 
 // HV units of a K or V tile, of RB columns (128, or 64 at head dim 64) each: a ring slot.  R query rows: WG warp groups of RW.
 template <int DH, int WG>
@@ -84,8 +85,9 @@ struct Smem {
   uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], sc_full[8], q_full, drain;
   unsigned raise[4 * WG];                    // a warp's rows whose references go up; kGaveUp
   uint32_t tmem_base;
-  unsigned not_finite[2];
-  int abort, bad_page;
+  unsigned not_finite[2];                    // rows of O; whether a row is kRedo
+  int redo;
+  int abort, bad_page[16];                   // of the sequence with this number, mod 16 (the ring holds fewer)
 };
 
 // kind::f8f6f4, fp32 D: operand types 0 e4m3, 1 e5m2.
@@ -178,7 +180,119 @@ HD_DEVINLINE void split3(uint32_t u, uint32_t& hi, uint32_t& mid, uint32_t& lo) 
   lo += 0x00800080u;
 }
 
-template <int DH, int WG>
+// What CTA x of a K/V head and row group works through: the x-th of nsplit parts of one sequence, or (SHARED) the x-th
+// of `total` equal parts of the tiles of all sequences, one behind another, which may lie in several: then a partial is
+// a CTA's of one sequence, with the number x + b (each differs from the one before in x or in b).  A sequence counts
+// kStart tiles more in front of its own, for what a CTA takes to end one and start the next.  Found by a whole warp.
+template <bool SHARED>
+struct Work {
+  static constexpr int kStart = 6;
+  int x, b, T, k0, k1, slot, left;  // sequence, its tokens, positions [k0, k1), the partial's number; tiles after those
+  // (Loops that are not unrolled: what runs once is bound by the fetch of its instructions.  A batch of 4: 2000 cycles less
+  // than unrolled over 128 sequences.)
+  HD_DEVINLINE Work(const Args& a, int x_) : x(x_), b(0), T(0), k0(0), k1(0), slot(x_), left(0) {
+    if constexpr (!SHARED) {
+      b = fast_div(x, a.d_nsplit);
+      T = a.lens[b];
+      dec::split_range<true>(a, T, x - b * a.nsplit, a.tile, k0, k1);
+    } else {
+      const uint2 whole = parts(a);
+      const unsigned all = whole.x, S = whole.y, per = all / S, rest = all - per * S;
+      // part x begins at x * all / S; S and x are hundreds at most
+      const unsigned u0 = x * per + x * rest / S, u1 = (x + 1) * per + (x + 1) * rest / S;
+      if (x >= (int)S || u0 >= u1) return;
+      each(a, [&](int q, int len, unsigned first, unsigned size) {
+        const unsigned hit = __ballot_sync(0xffffffffu, first <= u0 && u0 < first + size);
+        if (hit == 0) return false;
+        const int l = __ffs(hit) - 1;
+        b = __shfl_sync(0xffffffffu, q, l);
+        T = __shfl_sync(0xffffffffu, len, l);
+        take(a, (int)(u0 - __shfl_sync(0xffffffffu, first, l)) - kStart, (int)(u1 - u0));
+        return true;
+      });
+    }
+  }
+  // On to the next sequence; whether there is one.
+  HD_DEVINLINE bool next(const Args& a) {
+    if constexpr (SHARED) {
+      if (left <= kStart) return false;
+      do {
+        if (++b >= a.B) return false;
+        T = a.lens[b];
+      } while (T < 1 || T > a.maxT);
+      take(a, -kStart, left);
+    }
+    return SHARED;
+  }
+  // For the combine kernel, by one warp: each sequence's first partial, and their number.
+  static HD_DEVINLINE void report(const Args& a) {
+    const uint2 whole = parts(a);
+    each(a, [&](int q, int, unsigned first, unsigned size) {
+      auto part_of = [&](unsigned u) { return (int)((((unsigned long long)u + 1) * whole.y - 1) / whole.x); };  // that holds tile u
+      if (q < a.B) {
+        const int x0 = size > 0 ? part_of(first + kStart) : 0;
+        a.share[q] = size > 0 ? make_int2(x0 + q, part_of(first + size - 1) - x0 + 1) : make_int2(0, 0);
+      }
+      return false;
+    });
+  }
+
+ private:
+  static HD_DEVINLINE int tiles_of(const Args& a, int T) {
+    int lo, hi;
+    dec::seq_range(a, T, lo, hi);
+    return fast_div(hi - fast_div(lo, a.d_tile) * a.tile + a.tile - 1, a.d_tile);
+  }
+  static HD_DEVINLINE unsigned size_of(const Args& a, int len) { return len >= 1 && len <= a.maxT ? tiles_of(a, len) + kStart : 0; }
+  // All sequences' tiles, starts among them, and the number of parts: none empty, and no sequence in more than kMaxSplit.
+  static HD_DEVINLINE uint2 parts(const Args& a) {
+    unsigned all = 0, most = 0;
+#pragma unroll 1
+    for (int q = threadIdx.x & 31; q < a.B; q += 32) {
+      const unsigned size = size_of(a, a.lens[q]);
+      all += size;
+      most = max(most, size);
+    }
+    __syncwarp();
+    all = __reduce_add_sync(0xffffffffu, all);
+    most = __reduce_max_sync(0xffffffffu, most);
+    unsigned S = max(1u, min((unsigned)a.total, all));
+    if ((unsigned long long)most * S > (dec::kMaxSplit - 2ull) * all) S = (unsigned)((dec::kMaxSplit - 2ull) * all / most);
+    return make_uint2(all, S);
+  }
+  // f(sequence, its tokens, the tiles before its start, its own and its start's) for each lane's, until one returns true.
+  template <class F>
+  static HD_DEVINLINE void each(const Args& a, F f) {
+    unsigned before = 0;
+#pragma unroll 1
+    for (int q0 = 0; q0 < a.B; q0 += 32) {
+      const int lane = threadIdx.x & 31, q = q0 + lane, len = q < a.B ? a.lens[q] : 0;
+      const unsigned size = size_of(a, len);
+      unsigned upto = size;
+#pragma unroll 1
+      for (int d = 1; d < 32; d <<= 1) {
+        const unsigned y = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += y;
+      }
+      if (f(q, len, before + upto - size, size)) return;
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+  }
+  // Sequence b's tiles from `skip` on, `want` of them at most, its start's among them (which have numbers below 0).
+  HD_DEVINLINE void take(const Args& a, int skip, int want) {
+    want += min(skip, 0);
+    skip = max(skip, 0);
+    int lo, hi;
+    dec::seq_range(a, T, lo, hi);
+    const int n = min(want, tiles_of(a, T) - skip);  // (none, if that is the start alone)
+    k0 = (fast_div(lo, a.d_tile) + skip) * a.tile;
+    k1 = n > 0 ? min(hi, k0 + n * a.tile) : k0;
+    slot = x + b;
+    left = want - n;
+  }
+};
+
+template <int DH, int WG, bool SHARED>
 __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
     decode_q8_tc_kernel(const __grid_constant__ Params P) {
   using C = Cfg<DH, WG>;
@@ -190,9 +304,6 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
   const int split = fast_div((int)blockIdx.x, a.d_heads), head = (int)blockIdx.x - split * a.Hkv * a.ngroups;
   const int g = a.ngroups == 1 ? head : head / a.ngroups, rg = a.ngroups == 1 ? 0 : head % a.ngroups;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const size_t pidx = blockIdx.x;
-  float* po = a.part_o + pidx * R * DH;
-  float2* pml = a.part_ml + pidx * R;
   const int tile = a.tile, row0 = rg * R, rows = min(R, a.M - row0);
   // positions of a tile that no piece fills: their V must not be NaN, nor may their scales, which may not have come yet
   for (int i = tid; i < NSLOT * (KT - tile) * (RB / 16); i += NT) {
@@ -214,8 +325,8 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
     for (int i = 0; i < 8; ++i) mbar_init(&sm.sc_full[i], 4);
     mbar_init(&sm.q_full, 4 * WG);
     mbar_init(&sm.drain, 1);
-    sm.abort = sm.bad_page = 0;
-    sm.not_finite[0] = sm.not_finite[1] = 0;
+    sm.abort = 0;
+    sm.not_finite[0] = sm.not_finite[1] = sm.redo = 0;
     fence_mbar_init();
   }
   if (warp == 0) {
@@ -234,44 +345,22 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
   volatile int* abort = &sm.abort;
   grid_dep_wait();
   grid_dep_launch();
-  const dec::PagedSplit share(a, split, blockIdx.x == 0 && warp == 0);
-  const int b = share.b, T = share.T, k0 = share.k0, k1 = share.k1;
-  const int32_t* table = a.table + (long long)b * a.pg.max_pages;
-  const int nt = k0 < k1 ? fast_div(k1 - k0 + tile - 1, a.d_tile) : 0;
-  if (nt == 0) {  // nothing of this sequence in this split: an empty partial, or an empty result
-    if (a.nsplit > 1) {
-      for (int i = tid; i < R; i += NT) pml[i] = make_float2(-INFINITY, 0.f);
-    } else {
-      if (T != 0 && g == 0 && rg == 0 && tid == 0) set_status(a.status, HD_DEVBIT_INDEX);
-      for (int row = warp; row < rows; row += NT / 32) decq8::store_row<DH>(a, b, g, row0 + row, nullptr, -INFINITY, 0.f);
+  Work<SHARED> work(a, split);
+  auto tiles_here = [&] { return work.k0 < work.k1 ? fast_div(work.k1 - work.k0 + tile - 1, a.d_tile) : 0; };
+  auto partial = [&] { return ((size_t)work.slot * a.Hkv * a.ngroups + head) * R; };  // its first row
+  if (work.k0 >= work.k1) {  // nothing of this sequence in this split: an empty partial, or an empty result
+    if (!SHARED) {
+      if (a.nsplit > 1) {
+        for (int i = tid; i < R; i += NT) a.part_ml[partial() + i] = make_float2(-INFINITY, 0.f);
+      } else {
+        if (work.T != 0 && g == 0 && rg == 0 && tid == 0) set_status(a.status, HD_DEVBIT_INDEX);
+        for (int row = warp; row < rows; row += NT / 32)
+          decq8::store_row<DH>(a, work.b, g, row0 + row, nullptr, -INFINITY, 0.f);
+      }
     }
   } else if (warp == 0) {
-    // ------------------------------------------------------------ TMA producer: K(0), then K(j + 1), V(j)
-    const int seen = a.mode == SFA_LOCAL ? (T - 1) * a.n - a.window + 1 : 0;  // first position any row sees
-    // page and row there of this lane's piece of the tiles whose V (cur) and K (nxt) come next; the page entry of the
-    // one after them is loaded a tile ahead
-    auto pos_of = [&](int j) {  // first position of the piece, -1: none that a row sees
-      const int p = lane * a.piece, pos = k0 + j * tile + p;
-      return p >= tile || pos >= k1 || pos + a.piece <= seen ? -1 : pos;
-    };
-    int entry = 0;
-    auto fetch = [&](int j) {
-      const int pos = pos_of(j);
-      if (pos >= 0) {
-        const int i = fast_div(pos, a.pg.d_prow);
-        entry = i < a.pg.max_pages ? table[i] : -1;
-      }
-    };
-    auto place = [&](int j) {  // of the tile that was fetched: (page, row), behind the pool (zeros) where there is none
-      const int pos = pos_of(j);
-      int2 x = make_int2(a.pg.num_pages, 0);
-      if (pos >= 0) {
-        if ((unsigned)entry < (unsigned)a.pg.num_pages) x = make_int2(entry, pos - fast_div(pos, a.pg.d_prow) * a.pg.prow);
-        else sm.bad_page = 1;
-      }
-      return x;
-    };
-    int issued = 0, slot = 0, lap = 0;
+    // ------------------------------------------------------------ TMA producer: K(0), then K(j + 1), V(j), of each sequence
+    int issued = 0, slot = 0, lap = 0, seq = 0;
     auto load = [&](const CUtensorMap* tm, int2 x) -> bool {
 #pragma unroll
       for (int hf = 0; hf < HV; ++hf) {
@@ -286,17 +375,49 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
       }
       return true;
     };
-    fetch(0);
-    int2 cur = place(0), nxt;
-    fetch(1);
-    bool go = load(&P.tm_k, cur);
-    for (int j = 0; go && j < nt; ++j) {
-      nxt = place(j + 1);
-      fetch(j + 2);
-      if (j + 1 < nt) go = load(&P.tm_k, nxt);
-      go = go && load(&P.tm_v, cur);
-      cur = nxt;
-    }
+    bool go = true;
+    do {
+      if (lane == 0) sm.bad_page[seq & 15] = 0;
+      __syncwarp();
+      const int b = work.b, T = work.T, k0 = work.k0, k1 = work.k1, nt = tiles_here();
+      const int32_t* table = a.table + (long long)b * a.pg.max_pages;
+      const int seen = a.mode == SFA_LOCAL ? (T - 1) * a.n - a.window + 1 : 0;  // first position any row sees
+      // page and row there of this lane's piece of the tiles whose V (cur) and K (nxt) come next; the page entry of the
+      // one after them is loaded a tile ahead
+      auto pos_of = [&](int j) {  // first position of the piece, -1: none that a row sees
+        const int p = lane * a.piece, pos = k0 + j * tile + p;
+        return p >= tile || pos >= k1 || pos + a.piece <= seen ? -1 : pos;
+      };
+      int entry = 0;
+      auto fetch = [&](int j) {
+        const int pos = pos_of(j);
+        if (pos >= 0) {
+          const int i = fast_div(pos, a.pg.d_prow);
+          entry = i < a.pg.max_pages ? table[i] : -1;
+        }
+      };
+      auto place = [&](int j) {  // of the tile that was fetched: (page, row), behind the pool (zeros) where there is none
+        const int pos = pos_of(j);
+        int2 x = make_int2(a.pg.num_pages, 0);
+        if (pos >= 0) {
+          if ((unsigned)entry < (unsigned)a.pg.num_pages) x = make_int2(entry, pos - fast_div(pos, a.pg.d_prow) * a.pg.prow);
+          else sm.bad_page[seq & 15] = 1;
+        }
+        return x;
+      };
+      fetch(0);
+      int2 cur = place(0), nxt;
+      fetch(1);
+      go = load(&P.tm_k, cur);
+      for (int j = 0; go && j < nt; ++j) {
+        nxt = place(j + 1);
+        fetch(j + 2);
+        if (j + 1 < nt) go = load(&P.tm_k, nxt);
+        go = go && load(&P.tm_v, cur);
+        cur = nxt;
+      }
+      ++seq;
+    } while (go && work.next(a));
     // (a wait that gave up ends the kernel's work, not its copies in flight)
     if (lane == 0)
       for (int u = max(0, issued - NSLOT); u < issued; ++u) mbar_drain(&sm.full[u % NSLOT], (u / NSLOT) & 1);
@@ -306,7 +427,7 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
     constexpr uint32_t idS = C::kPair ? idesc_f8(128, 2 * R, 0, 0, 0, 0) : idesc_f8(128, R, 0, 1, 0, 0), idO = idesc_f8(RB, 3 * R, 0, 1, 1, 1);
     const uint64_t kd = sdesc_rows<RB>(smem_u32(sm.ring[0])), qd = sdesc_rows<RB>(smem_u32(sm.q[0][0]));
     const uint64_t pd = sdesc_plain_mn(smem_u32(sm.p[0][0]), 128, KT * 16);
-    int slot = 0, lap = 0;
+    int slot = 0, lap = 0, done = 0, seq = 0;  // done: tiles of the sequences before
     bool ok = true;
     auto wait_unit = [&]() -> bool {
       if (!__all_sync(0xffffffffu, mbar_wait(&sm.full[slot], lap & 1, abort, a.status))) return false;
@@ -318,9 +439,9 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
       if (++slot == NSLOT) slot = 0, ++lap;
     };
     auto issue_s = [&](int j) -> bool {
-      const int sb = j & 1;
-      if (j >= 2) {
-        if (!__all_sync(0xffffffffu, mbar_wait(&sm.s_free[sb], ((j >> 1) - 1) & 1, abort, a.status))) return false;
+      const int at = done + j, sb = at & 1;
+      if (at >= 2) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&sm.s_free[sb], ((at >> 1) - 1) & 1, abort, a.status))) return false;
         tc_fence_after();
       }
 #pragma unroll
@@ -338,8 +459,8 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
       return true;
     };
     auto issue_pv = [&](int j) -> bool {
-      const int pb = j & 1;
-      if (!__all_sync(0xffffffffu, mbar_wait(&sm.p_full[pb], (j >> 1) & 1, abort, a.status))) return false;
+      const int at = done + j, pb = at & 1;
+      if (!__all_sync(0xffffffffu, mbar_wait(&sm.p_full[pb], (at >> 1) & 1, abort, a.status))) return false;
       tc_fence_after();
 #pragma unroll
       for (int hf = 0; hf < HV; ++hf) {
@@ -353,321 +474,332 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
       tc_commit_w(&sm.pv_done[pb]);
       return true;
     };
-    ok = __all_sync(0xffffffffu, mbar_wait(&sm.q_full, 0, abort, a.status));
-    ok = ok && issue_s(0);
-    for (int j = 0; ok && j < nt; ++j) {
-      if (j + 1 < nt) ok = issue_s(j + 1);
-      ok = ok && issue_pv(j);
-    }
+    do {
+      const int nt = tiles_here();
+      ok = __all_sync(0xffffffffu, mbar_wait(&sm.q_full, seq++ & 1, abort, a.status));  // (and O of the one before is read)
+      tc_fence_after();
+      ok = ok && issue_s(0);
+      for (int j = 0; ok && j < nt; ++j) {
+        if (j + 1 < nt) ok = issue_s(j + 1);
+        ok = ok && issue_pv(j);
+      }
+      done += nt;
+    } while (ok && work.next(a));
     tc_commit_w(&sm.drain);
     mbar_drain(&sm.drain, 0);
   } else {
     // ------------------------------------------------------------ softmax: a thread per position
     const int wg = (warp - 2) >> 2, q4 = warp & 3, key = q4 * 32 + lane, r0 = wg * RW, bar = 1 + wg;
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16), tO = tl + 2 * C::SC + r0;
-    const int own_lo = (T - 1) * a.n, win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;
-    const int seen = a.mode == SFA_LOCAL ? own_lo - a.window + 1 : 0;
     const uint32_t real = bits(0, rows - r0);
-    // The first group brings the scales, 128 blocks (a chunk) at a time, a thread each, by cp.async: behind a saturated
-    // memory's queue a load takes thousands of cycles.  Blocks are counted from the split's first.  As chunk c is handed on,
-    // the words that hold the bytes of chunk c + 3 are asked for (cut to the scales' array; a byte's place is kept), and
-    // the page entries of chunk c + 6.
-    const int b0 = fast_div(k0, a.d_brow), nblocks = fast_div(k1 - 1, a.d_brow) - b0 + 1;
-    const int b_seen = seen <= 0 ? 0 : fast_div(seen, a.d_brow) - b0;  // the first that a row sees
-    uint32_t places = 0;
-    int handed = 0;
-    auto page_of = [&](int x, int& in) {  // of block x; -1: none that is needed
-      if (x >= nblocks || x < b_seen) return -1;
-      const int pg = fast_div(b0 + x, a.d_blocks);
-      in = b0 + x - pg * a.blocks;
-      return pg < a.pg.max_pages ? pg : -1;
-    };
-    auto chunk_words = [&](int c, int entry) {
-      int in = 0;
-      if (page_of(c * 128 + key, in) >= 0 && (unsigned)entry < (unsigned)a.pg.num_pages) {
-        const size_t at = ((size_t)entry * a.Hkv + g) * a.blocks + in, word = at & ~(size_t)3;
-        const int bytes = (int)min((size_t)a.pg.num_pages * a.Hkv * a.blocks - word, (size_t)4), sh = (c & 3) * 2;
-        const uint32_t to = smem_u32(&sm.words[c & 3][key]);
-        cp_async_4(to, a.kscale + word, bytes);
-        cp_async_4(to + 4, a.vscale + word, bytes);
-        places = (places & ~(3u << sh)) | (uint32_t)(at & 3) << sh;
-      }
-    };
-    auto chunk_entries = [&](int c) {
-      int in = 0;
-      const int pg = page_of(c * 128 + key, in);
-      if (pg >= 0) cp_async_4(smem_u32(&sm.entry[c & 3][key]), table + pg, 4);
-    };
-    auto hand_on = [&] {  // the next chunk's bytes
-      cp_async_wait<2>();
-      const int c = handed++;
-      const uint2 x = sm.words[c & 3][key];
-      const int sh = (places >> (c & 3) * 2 & 3) * 8;
-      sm.scale[(c & 7) * 128 + key] = (uint16_t)(q8::clamp_byte(x.x >> sh & 255) | q8::clamp_byte(x.y >> sh & 255) << 8);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.sc_full[c & 7]);
-      chunk_words(c + 3, sm.entry[(c + 3) & 3][key]);
-      chunk_entries(c + 6);
-      cp_async_commit();
-    };
-    int first[3] = {-1, -1, -1};
-    if (wg == 0) {
-      int in = 0;
-#pragma unroll
-      for (int c = 0; c < 3; ++c) {
-        const int pg = page_of(c * 128 + key, in);
-        if (pg >= 0) first[c] = table[pg];
-      }
-    }
-    {  // the queries: four rows a warp
-      constexpr int NP = DH / 64;  // pairs of a lane
-      uint32_t w[4][NP];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int rr = r0 + q4 * 4 + x;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) w[x][i] = 0;
-        if (rr < rows) {
-          const int r = row0 + rr, s = fast_div(r, a.d_G), h = g * a.G + r - s * a.G;
-          const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (((long long)b * a.n + s) * a.Hq + h) * DH) + lane * NP;
-#pragma unroll
-          for (int i = 0; i < NP; ++i) w[x][i] = src[i];
+    bool ok = true;
+    int done = 0, chunks = 0, seq = 0;  // tiles and chunks of the sequences before; their number
+    do {
+      const int b = work.b, T = work.T, k0 = work.k0, k1 = work.k1, nt = tiles_here();
+      const int32_t* table = a.table + (long long)b * a.pg.max_pages;
+      float* po = a.part_o + partial() * DH;
+      float2* pml = a.part_ml + partial();
+      const int own_lo = (T - 1) * a.n, win_hi = a.mode == SFA_LOCAL ? T * a.n - 1 - a.window : -1;
+      const int seen = a.mode == SFA_LOCAL ? own_lo - a.window + 1 : 0;
+      // The first group brings the scales, 128 blocks (a chunk) at a time, a thread each, by cp.async: behind a saturated
+      // memory's queue a load takes thousands of cycles.  Blocks are counted from the split's first.  As chunk c is handed on,
+      // the words that hold the bytes of chunk c + 3 are asked for (cut to the scales' array; a byte's place is kept), and
+      // the page entries of chunk c + 6.
+      const int b0 = fast_div(k0, a.d_brow), nblocks = fast_div(k1 - 1, a.d_brow) - b0 + 1;
+      const int b_seen = seen <= 0 ? 0 : fast_div(seen, a.d_brow) - b0;  // the first that a row sees
+      uint32_t places = 0;
+      int handed = 0;  // chunks, from this sequence's first
+      auto page_of = [&](int x, int& in) {  // of block x; -1: none that is needed
+        if (x >= nblocks || x < b_seen) return -1;
+        const int pg = fast_div(b0 + x, a.d_blocks);
+        in = b0 + x - pg * a.blocks;
+        return pg < a.pg.max_pages ? pg : -1;
+      };
+      auto chunk_words = [&](int c, int entry) {
+        int in = 0;
+        if (page_of(c * 128 + key, in) >= 0 && (unsigned)entry < (unsigned)a.pg.num_pages) {
+          const size_t at = ((size_t)entry * a.Hkv + g) * a.blocks + in, word = at & ~(size_t)3;
+          const int bytes = (int)min((size_t)a.pg.num_pages * a.Hkv * a.blocks - word, (size_t)4), sh = (c & 3) * 2;
+          const uint32_t to = smem_u32(&sm.words[c & 3][key]);
+          cp_async_4(to, a.kscale + word, bytes);
+          cp_async_4(to + 4, a.vscale + word, bytes);
+          places = (places & ~(3u << sh)) | (uint32_t)(at & 3) << sh;
         }
-      }
+      };
+      auto chunk_entries = [&](int c) {
+        int in = 0;
+        const int pg = page_of(c * 128 + key, in);
+        if (pg >= 0) cp_async_4(smem_u32(&sm.entry[c & 3][key]), table + pg, 4);
+      };
+      auto hand_on = [&] {  // the next chunk's bytes
+        cp_async_wait<2>();
+        const int c = handed++;
+        const uint2 x = sm.words[c & 3][key];
+        const int sh = (places >> (c & 3) * 2 & 3) * 8;
+        sm.scale[((chunks + c) & 7) * 128 + key] = (uint16_t)(q8::clamp_byte(x.x >> sh & 255) | q8::clamp_byte(x.y >> sh & 255) << 8);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.sc_full[(chunks + c) & 7]);
+        chunk_words(c + 3, sm.entry[(c + 3) & 3][key]);
+        chunk_entries(c + 6);
+        cp_async_commit();
+      };
+      int first[3] = {-1, -1, -1};
       if (wg == 0) {
+        int in = 0;
 #pragma unroll
         for (int c = 0; c < 3; ++c) {
-          chunk_words(c, first[c]);
-          chunk_entries(c + 3);
-          cp_async_commit();
+          const int pg = page_of(c * 128 + key, in);
+          if (pg >= 0) first[c] = table[pg];
         }
       }
+      {  // the queries: four rows a warp
+        constexpr int NP = DH / 64;  // pairs of a lane
+        uint32_t w[4][NP];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int rr = r0 + q4 * 4 + x;
-        uint32_t most = 0;
+        for (int x = 0; x < 4; ++x) {
+          const int rr = r0 + q4 * 4 + x;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) most = max(most, max(w[x][i] << 16 & 0x7fff0000u, w[x][i] & 0x7fff0000u));
-        most = __reduce_max_sync(0xffffffffu, most);
-        // the exponent field of the largest magnitude, kept where both powers are normal
-        const int e = min(max((int)(most >> 23), 20), 254);
-        constexpr int kUp = C::kPair ? 7 : 14;  // the largest to [2^kUp, 2^(kUp + 1))
-        const float to = __int_as_float(min(127 + kUp + 127 - e, 254) << 23);  // 2^(kUp - (e - 127)), at most 2^127
-        const float back = __int_as_float(max(e - kUp, 1) << 23);              // 2^(e - 127 - kUp)
+          for (int i = 0; i < NP; ++i) w[x][i] = 0;
+          if (rr < rows) {
+            const int r = row0 + rr, s = fast_div(r, a.d_G), h = g * a.G + r - s * a.G;
+            const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (((long long)b * a.n + s) * a.Hq + h) * DH) + lane * NP;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const float x0 = __uint_as_float(w[x][i] << 16) * to, x1 = __uint_as_float(w[x][i] & 0xffff0000u) * to;
-          uint32_t t[3];
-          if (C::kPair) {
-            t[0] = q8::code2(x0, x1);
-            const float2 y = q8::values2((uint16_t)t[0]);
-            t[1] = q8::code2((x0 - y.x) * kLo, (x1 - y.y) * kLo);
-          } else {
-            const __half2 u = __floats2half2_rn(x0, x1);
-            split3<false>(*reinterpret_cast<const uint32_t*>(&u), t[0], t[1], t[2]);
-#pragma unroll
-            for (int y = 0; y < 3; ++y) t[y] = __byte_perm(t[y], 0, 0x31);
+            for (int i = 0; i < NP; ++i) w[x][i] = src[i];
           }
-          const int c = (lane * NP + i) * 2, at = (c % RB) >> 4, off = c & 15;  // column; its 16-byte chunk
-          const int swizzled = RB == 64 ? at ^ (rr >> 1 & 3) : at ^ (rr & 7);
-#pragma unroll
-          for (int y = 0; y < C::QT; ++y)
-            *reinterpret_cast<uint16_t*>(sm.q[c / RB][y] + rr * RB + swizzled * 16 + off) = (uint16_t)t[y];
         }
-        if (lane == 0) sm.rowf[rr] = back * a.scale_log2;
-      }
-      if (lane < RW) sm.nref[q4][r0 + lane] = 0.f;
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.q_full);
-      named_bar_sync(bar, 128);  // the group's rows
-    }
-    uint64_t l[RW / 2];  // pairs of rows' sums over this thread's positions
+        if (wg == 0) {
 #pragma unroll
-    for (int r = 0; r < RW / 2; ++r) l[r] = 0;
-    uint32_t set = 0;  // rows whose reference is set
-    bool ok = true;
-    const int brow = a.pg.prow / a.blocks;
-    int waited = 0;                               // chunks that this warp has waited for
-    long long scales_end = (long long)b0 * brow;  // the first position behind them
-    // this key's block, from the split's first, and its row there; both go on by a tile
-    const int step_blocks = fast_div(tile, a.d_brow), step_rows = tile - step_blocks * brow;
-    int block = fast_div(k0 + key, a.d_brow) - b0, in_block = k0 + key - (block + b0) * brow;
-    const int edge = tile < KT ? 0 : min(own_lo + 1, k1);  // tiles that end at or before it have no mask but WITHIN's
-    for (int j = 0; j < nt; ++j) {
-      const int sb = j & 1, base = k0 + j * tile, p = base + key;
-      // the chunks of this tile's blocks: handed on by the first group, and waited for
-      while (min(base + tile, k1) > scales_end) {
-        if (wg == 0) hand_on();
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.sc_full[waited & 7], waited >> 3 & 1, abort, a.status));
-        ++waited;
-        scales_end += 128ll * brow;
-      }
-      // the rows that see this position: a range
-      uint32_t vis = real;
-      if (a.mode == SFA_WITHIN && a.n > 1) {
-        const int s = p - fast_div(p, a.d_n) * a.n;
-        vis &= bits(s * a.G - row0 - r0, (s + 1) * a.G - row0 - r0);
-      }
-      if (base + tile > edge || base <= win_hi) {
-        // rows of the streams from p's own on, where p is the new token's
-        const int first = max(p - own_lo, 0) * a.G - row0 - r0;
-        const int last = a.mode == SFA_LOCAL ? (int)min(((long long)p - own_lo + a.window) * a.G - row0 - r0, (long long)RW) : RW;
-        vis = key < tile && p < k1 ? vis & bits(p < own_lo ? 0 : first, last) : (uint32_t)0;
-      }
-      // (A wait that gave up: the warp goes on to the group's next vote, since the others may wait for it there, and all
-      // leave after it.)
-      ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.s_full[sb], (j >> 1) & 1, abort, a.status));
-      tc_fence_after();
-      const int sc = sm.scale[min(block, nblocks - 1) & 1023], kb = sc & 255, vb = sc >> 8;
-      block += step_blocks;
-      in_block += step_rows;
-      if (in_block >= brow) in_block -= brow, ++block;
-      const float kf = q8::scale_of(kb), ev = (float)(vb - 127), inv = q8::inverse_of(vb);
-      const uint64_t kf2 = f2pack(kf, kf), ev2 = f2pack(ev, ev);
-      float y[RW];
-      {
-        float low[RW];
-        tmem_ld16(tl + sb * C::SC + r0, reinterpret_cast<uint32_t*>(y));
-        if (C::kPair) tmem_ld16(tl + sb * C::SC + R + r0, reinterpret_cast<uint32_t*>(low));
-        tmem_ld_wait();
-        if (C::kPair)
-#pragma unroll
-          for (int r = 0; r < RW; r += 2)
-            f2unpack(ffma2(f2pack(low[r], low[r + 1]), f2pack(1.f / kLo, 1.f / kLo), f2pack(y[r], y[r + 1])), y[r], y[r + 1]);
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.s_free[sb]);
-#pragma unroll
-      for (int c = 0; c < RW; c += 4) {
-        const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(sm.rowf + r0 + c);
-        const ulonglong2 rf = *reinterpret_cast<const ulonglong2*>(sm.nref[q4] + r0 + c);
-        f2unpack(ffma2(fmul2(f2pack(y[c], y[c + 1]), f.x), kf2, fadd2(ev2, rf.x)), y[c], y[c + 1]);
-        f2unpack(ffma2(fmul2(f2pack(y[c + 2], y[c + 3]), f.y), kf2, fadd2(ev2, rf.y)), y[c + 2], y[c + 3]);
-      }
-      if (__any_sync(0xffffffffu, vis != real))
-#pragma unroll
-        for (int r = 0; r < RW; ++r)
-          if (!((vis >> r) & 1u)) y[r] = -INFINITY;
-      float top = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < RW; r += 2) top = max3(top, y[r], y[r + 1]);
-      if (group_any(bar, !ok || top > kTop || (vis & ~set) != 0)) {
-        // New references for the rows (of the whole group) of which some P would pass 2^kTop, or which have none yet:
-        // their largest P to 2^kSet.
-        uint32_t mask = vis & ~set;
-        float m = 0.f;  // lane r: row r's
-#pragma unroll
-        for (int r = 0; r < RW; ++r) {
-          if (y[r] > kTop) mask |= 1u << r;
-          const int x = __reduce_max_sync(0xffffffffu, ordered(y[r] == y[r] ? y[r] : -INFINITY));
-          if (lane == r) m = from_ordered(x);
+          for (int c = 0; c < 3; ++c) {
+            chunk_words(c, first[c]);
+            chunk_entries(c + 3);
+            cp_async_commit();
+          }
         }
-        mask = __reduce_or_sync(0xffffffffu, mask | (ok ? 0 : kGaveUp));
-        if (lane < RW) sm.most[q4][r0 + lane] = m;
-        if (lane == 0) sm.raise[wg * 4 + q4] = mask;
-        named_bar_sync(bar, 128);  // (the next vote lies before these are written again)
-        mask = (sm.raise[wg * 4] | sm.raise[wg * 4 + 1]) | (sm.raise[wg * 4 + 2] | sm.raise[wg * 4 + 3]);
-        if (mask & kGaveUp) {
-          ok = false;
-          break;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int rr = r0 + q4 * 4 + x;
+          uint32_t most = 0;
+#pragma unroll
+          for (int i = 0; i < NP; ++i) most = max(most, max(w[x][i] << 16 & 0x7fff0000u, w[x][i] & 0x7fff0000u));
+          most = __reduce_max_sync(0xffffffffu, most);
+          // the exponent field of the largest magnitude, kept where both powers are normal
+          const int e = min(max((int)(most >> 23), 20), 254);
+          constexpr int kUp = C::kPair ? 7 : 14;  // the largest to [2^kUp, 2^(kUp + 1))
+          const float to = __int_as_float(min(127 + kUp + 127 - e, 254) << 23);  // 2^(kUp - (e - 127)), at most 2^127
+          const float back = __int_as_float(max(e - kUp, 1) << 23);              // 2^(e - 127 - kUp)
+#pragma unroll
+          for (int i = 0; i < NP; ++i) {
+            const float x0 = __uint_as_float(w[x][i] << 16) * to, x1 = __uint_as_float(w[x][i] & 0xffff0000u) * to;
+            uint32_t t[3];
+            if (C::kPair) {
+              t[0] = q8::code2(x0, x1);
+              const float2 y = q8::values2((uint16_t)t[0]);
+              t[1] = q8::code2((x0 - y.x) * kLo, (x1 - y.y) * kLo);
+            } else {
+              const __half2 u = __floats2half2_rn(x0, x1);
+              split3<false>(*reinterpret_cast<const uint32_t*>(&u), t[0], t[1], t[2]);
+#pragma unroll
+              for (int y = 0; y < 3; ++y) t[y] = __byte_perm(t[y], 0, 0x31);
+            }
+            const int c = (lane * NP + i) * 2, at = (c % RB) >> 4, off = c & 15;  // column; its 16-byte chunk
+            const int swizzled = RB == 64 ? at ^ (rr >> 1 & 3) : at ^ (rr & 7);
+#pragma unroll
+            for (int y = 0; y < C::QT; ++y)
+              *reinterpret_cast<uint16_t*>(sm.q[c / RB][y] + rr * RB + swizzled * 16 + off) = (uint16_t)t[y];
+          }
+          if (lane == 0) sm.rowf[rr] = back * a.scale_log2;
         }
-        float down = 0.f, fac = 1.f;  // lane r: what row r's reference goes up by, negated; 2^ that
-        if (lane < RW && (mask >> lane & 1u)) {
-          const int r = r0 + lane;
-          down = kSet - fmaxf(fmaxf(sm.most[0][r], sm.most[1][r]), fmaxf(sm.most[2][r], sm.most[3][r]));
-          sm.nref[q4][r] += down;
-          if (set >> lane & 1u) fac = ex2_approx(down);
-        }
+        if (lane < RW) sm.nref[q4][r0 + lane] = 0.f;
+        fence_async_smem();
+        tc_fence_before();
         __syncwarp();
-#pragma unroll
-        for (int r = 0; r < RW; r += 2) {
-          l[r / 2] = fmul2(l[r / 2], f2pack(__shfl_sync(0xffffffffu, fac, r), __shfl_sync(0xffffffffu, fac, r + 1)));
-          y[r] += __shfl_sync(0xffffffffu, down, r);
-          y[r + 1] += __shfl_sync(0xffffffffu, down, r + 1);
-        }
-        if ((mask & set) != 0 && j > 0) {
-          // (the products of the tile before the last are done, see below: so the wait is for the right phase)
-          ok = __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1, abort, a.status));
-          tc_fence_after();
-          for (uint32_t left = mask & set; left; left &= left - 1) {
-            const int r = __ffs(left) - 1;
-            tmem_scale<3 * HV, R>(tO + r, __shfl_sync(0xffffffffu, fac, r));
-          }
-          tmem_st_wait();
-        }
-        set |= mask;
+        if (lane == 0) mbar_arrive(&sm.q_full);
+        named_bar_sync(bar, 128);  // the group's rows
       }
-      if (!ok) continue;
-      // S of this tile was issued behind the products of the tile before the last, so these are done: P's buffer is free
-      const uint64_t inv2 = f2pack(inv, inv);
-      {
-        uint4 t[3];
+      uint64_t l[RW / 2];  // pairs of rows' sums over this thread's positions
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          uint32_t hi[2], mid[2], lo[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int r = h * 4 + i * 2;
-            const float p0 = ex2_approx(y[r]), p1 = ex2_approx(y[r + 1]);
-            l[r / 2] = ffma2(f2pack(p0, p1), inv2, l[r / 2]);
-            const __half2 u = __floats2half2_rn(p0, p1);
-            split3<true>(*reinterpret_cast<const uint32_t*>(&u), hi[i], mid[i], lo[i]);
-          }
-          (&t[0].x)[h] = __byte_perm(hi[0], hi[1], 0x7531);
-          (&t[1].x)[h] = __byte_perm(mid[0], mid[1], 0x7531);
-          (&t[2].x)[h] = __byte_perm(lo[0], lo[1], 0x7531);
+      for (int r = 0; r < RW / 2; ++r) l[r] = 0;
+      uint32_t set = 0;  // rows whose reference is set
+      const int brow = a.pg.prow / a.blocks;
+      int waited = 0;                               // chunks that this warp has waited for
+      long long scales_end = (long long)b0 * brow;  // the first position behind them
+      // this key's block, from the split's first, and its row there; both go on by a tile
+      const int step_blocks = fast_div(tile, a.d_brow), step_rows = tile - step_blocks * brow;
+      int block = fast_div(k0 + key, a.d_brow) - b0, in_block = k0 + key - (block + b0) * brow;
+      const int edge = tile < KT ? 0 : min(own_lo + 1, k1);  // tiles that end at or before it have no mask but WITHIN's
+      for (int j = 0; j < nt; ++j) {
+        const int at = done + j, sb = at & 1, base = k0 + j * tile, p = base + key;
+        // the chunks of this tile's blocks: handed on by the first group, and waited for
+        while (min(base + tile, k1) > scales_end) {
+          if (wg == 0) hand_on();
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.sc_full[(chunks + waited) & 7], (chunks + waited) >> 3 & 1, abort, a.status));
+          ++waited;
+          scales_end += 128ll * brow;
         }
-        const int at = wg * (KT * 16) + key * 16;
-#pragma unroll
-        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4*>(sm.p[sb][i] + at) = t[i];
-      }
-      // The sequence's last tile holds positions behind its length, which may never have been written: their P is 0, and
-      // 0 times a NaN is NaN, so their V is zeroed before the product (which waits for this thread's arrival).
-      if (base + tile > k1 && wg == 0) {
-        // The ring's last units are this tile's V.  (A wait tells only a phase from the next: with the products of the
-        // tile before done, all units but these have landed.)
-        if (nt >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[nt & 1], ((nt - 2) >> 1) & 1, abort, a.status));
-        static_assert(NSLOT >= HV, "");
-#pragma unroll
-        for (int h = 0; h < HV; ++h) {
-          const int u = 2 * HV * nt - HV + h;
-          ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.full[u % NSLOT], (u / NSLOT) & 1, abort, a.status));
-          if (ok && p >= k1)
-#pragma unroll
-            for (int c = 0; c < RB / 16; ++c) reinterpret_cast<uint4*>(sm.ring[u % NSLOT] + key * RB)[c] = make_uint4(0, 0, 0, 0);
+        // the rows that see this position: a range
+        uint32_t vis = real;
+        if (a.mode == SFA_WITHIN && a.n > 1) {
+          const int s = p - fast_div(p, a.d_n) * a.n;
+          vis &= bits(s * a.G - row0 - r0, (s + 1) * a.G - row0 - r0);
         }
-        __syncwarp();
-        if (!ok) continue;
-      }
-      fence_async_smem();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.p_full[sb]);
-    }
-    cp_async_wait<0>();
-    float sum = 0.f;  // lane r: row r's over this warp's positions
-#pragma unroll
-    for (int r = 0; r < RW; ++r) {
-      float x, other;
-      if (r & 1) f2unpack(l[r / 2], other, x);
-      else f2unpack(l[r / 2], x, other);
-#pragma unroll
-      for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-      if (lane == r) sum = x;
-    }
-    ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(nt - 1) & 1], ((nt - 1) >> 1) & 1, abort, a.status));
-    if (group_any(bar, !ok)) ok = false;  // (also: every warp has read the last maxima)
-    if (ok) {
-      if (lane < RW) sm.most[q4][r0 + lane] = sum;
-      tc_fence_after();
-      const bool bad = *(volatile int*)&sm.bad_page != 0;
-      // this lane's row of O^T: all 128, or (a product of 64 rows) 16 of each 32
-      const int column = RB == 128 ? key : lane < 16 ? q4 * 16 + lane : -1;
-#pragma unroll
-      for (int hf = 0; hf < HV; ++hf)
+        if (base + tile > edge || base <= win_hi) {
+          // rows of the streams from p's own on, where p is the new token's
+          const int first = max(p - own_lo, 0) * a.G - row0 - r0;
+          const int last = a.mode == SFA_LOCAL ? (int)min(((long long)p - own_lo + a.window) * a.G - row0 - r0, (long long)RW) : RW;
+          vis = key < tile && p < k1 ? vis & bits(p < own_lo ? 0 : first, last) : (uint32_t)0;
+        }
+        // (A wait that gave up: the warp goes on to the group's next vote, since the others may wait for it there, and all
+        // leave after it.)
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.s_full[sb], (at >> 1) & 1, abort, a.status));
+        tc_fence_after();
+        const int sc = sm.scale[(chunks * 128 + min(block, nblocks - 1)) & 1023], kb = sc & 255, vb = sc >> 8;
+        block += step_blocks;
+        in_block += step_rows;
+        if (in_block >= brow) in_block -= brow, ++block;
+        const float kf = q8::scale_of(kb), ev = (float)(vb - 127), inv = q8::inverse_of(vb);
+        const uint64_t kf2 = f2pack(kf, kf), ev2 = f2pack(ev, ev);
+        float y[RW];
         {
+          float low[RW];
+          tmem_ld16(tl + sb * C::SC + r0, reinterpret_cast<uint32_t*>(y));
+          if (C::kPair) tmem_ld16(tl + sb * C::SC + R + r0, reinterpret_cast<uint32_t*>(low));
+          tmem_ld_wait();
+          if (C::kPair)
+#pragma unroll
+            for (int r = 0; r < RW; r += 2)
+              f2unpack(ffma2(f2pack(low[r], low[r + 1]), f2pack(1.f / kLo, 1.f / kLo), f2pack(y[r], y[r + 1])), y[r], y[r + 1]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.s_free[sb]);
+#pragma unroll
+        for (int c = 0; c < RW; c += 4) {
+          const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(sm.rowf + r0 + c);
+          const ulonglong2 rf = *reinterpret_cast<const ulonglong2*>(sm.nref[q4] + r0 + c);
+          f2unpack(ffma2(fmul2(f2pack(y[c], y[c + 1]), f.x), kf2, fadd2(ev2, rf.x)), y[c], y[c + 1]);
+          f2unpack(ffma2(fmul2(f2pack(y[c + 2], y[c + 3]), f.y), kf2, fadd2(ev2, rf.y)), y[c + 2], y[c + 3]);
+        }
+        if (__any_sync(0xffffffffu, vis != real))
+#pragma unroll
+          for (int r = 0; r < RW; ++r)
+            if (!((vis >> r) & 1u)) y[r] = -INFINITY;
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < RW; r += 2) top = max3(top, y[r], y[r + 1]);
+        if (group_any(bar, !ok || top > kTop || (vis & ~set) != 0)) {
+          // New references for the rows (of the whole group) of which some P would pass 2^kTop, or which have none yet:
+          // their largest P to 2^kSet.
+          uint32_t mask = vis & ~set;
+          float m = 0.f;  // lane r: row r's
+#pragma unroll
+          for (int r = 0; r < RW; ++r) {
+            if (y[r] > kTop) mask |= 1u << r;
+            const int x = __reduce_max_sync(0xffffffffu, ordered(y[r] == y[r] ? y[r] : -INFINITY));
+            if (lane == r) m = from_ordered(x);
+          }
+          mask = __reduce_or_sync(0xffffffffu, mask | (ok ? 0 : kGaveUp));
+          if (lane < RW) sm.most[q4][r0 + lane] = m;
+          if (lane == 0) sm.raise[wg * 4 + q4] = mask;
+          named_bar_sync(bar, 128);  // (the next vote lies before these are written again)
+          mask = (sm.raise[wg * 4] | sm.raise[wg * 4 + 1]) | (sm.raise[wg * 4 + 2] | sm.raise[wg * 4 + 3]);
+          if (mask & kGaveUp) {
+            ok = false;
+            break;
+          }
+          float down = 0.f, fac = 1.f;  // lane r: what row r's reference goes up by, negated; 2^ that
+          if (lane < RW && (mask >> lane & 1u)) {
+            const int r = r0 + lane;
+            down = kSet - fmaxf(fmaxf(sm.most[0][r], sm.most[1][r]), fmaxf(sm.most[2][r], sm.most[3][r]));
+            sm.nref[q4][r] += down;
+            if (set >> lane & 1u) fac = ex2_approx(down);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int r = 0; r < RW; r += 2) {
+            l[r / 2] = fmul2(l[r / 2], f2pack(__shfl_sync(0xffffffffu, fac, r), __shfl_sync(0xffffffffu, fac, r + 1)));
+            y[r] += __shfl_sync(0xffffffffu, down, r);
+            y[r + 1] += __shfl_sync(0xffffffffu, down, r + 1);
+          }
+          if ((mask & set) != 0 && j > 0) {
+            // (the products of the tile before the last are done, see below: so the wait is for the right phase)
+            ok = __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(at - 1) & 1], ((at - 1) >> 1) & 1, abort, a.status));
+            tc_fence_after();
+            for (uint32_t left = mask & set; left; left &= left - 1) {
+              const int r = __ffs(left) - 1;
+              tmem_scale<3 * HV, R>(tO + r, __shfl_sync(0xffffffffu, fac, r));
+            }
+            tmem_st_wait();
+          }
+          set |= mask;
+        }
+        if (!ok) continue;
+        // S of this tile was issued behind the products of the tile before the last, so these are done: P's buffer is free
+        const uint64_t inv2 = f2pack(inv, inv);
+        {
+          uint4 t[3];
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            uint32_t hi[2], mid[2], lo[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int r = h * 4 + i * 2;
+              const float p0 = ex2_approx(y[r]), p1 = ex2_approx(y[r + 1]);
+              l[r / 2] = ffma2(f2pack(p0, p1), inv2, l[r / 2]);
+              const __half2 u = __floats2half2_rn(p0, p1);
+              split3<true>(*reinterpret_cast<const uint32_t*>(&u), hi[i], mid[i], lo[i]);
+            }
+            (&t[0].x)[h] = __byte_perm(hi[0], hi[1], 0x7531);
+            (&t[1].x)[h] = __byte_perm(mid[0], mid[1], 0x7531);
+            (&t[2].x)[h] = __byte_perm(lo[0], lo[1], 0x7531);
+          }
+          const int to = wg * (KT * 16) + key * 16;
+#pragma unroll
+          for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4*>(sm.p[sb][i] + to) = t[i];
+        }
+        // The sequence's last tile holds positions behind its length, which may never have been written: their P is 0, and
+        // 0 times a NaN is NaN, so their V is zeroed before the product (which waits for this thread's arrival).
+        if (base + tile > k1 && wg == 0) {
+          // The ring's last units are this tile's V.  (A wait tells only a phase from the next: with the products of the
+          // tile before done, all units but these have landed.)
+          if (at >= 1) ok = __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(at - 1) & 1], ((at - 1) >> 1) & 1, abort, a.status));
+          static_assert(NSLOT >= HV, "");
+#pragma unroll
+          for (int h = 0; h < HV; ++h) {
+            const int u = 2 * HV * (at + 1) - HV + h;
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.full[u % NSLOT], (u / NSLOT) & 1, abort, a.status));
+            if (ok && p >= k1)
+#pragma unroll
+              for (int c = 0; c < RB / 16; ++c) reinterpret_cast<uint4*>(sm.ring[u % NSLOT] + key * RB)[c] = make_uint4(0, 0, 0, 0);
+          }
+          __syncwarp();
+          if (!ok) continue;
+        }
+        fence_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.p_full[sb]);
+      }
+      cp_async_wait<0>();
+      float sum = 0.f;  // lane r: row r's over this warp's positions
+#pragma unroll
+      for (int r = 0; r < RW; ++r) {
+        float x, other;
+        if (r & 1) f2unpack(l[r / 2], other, x);
+        else f2unpack(l[r / 2], x, other);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        if (lane == r) sum = x;
+      }
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(done + nt - 1) & 1], ((done + nt - 1) >> 1) & 1, abort, a.status));
+      if (group_any(bar, !ok)) ok = false;  // (also: every warp has read the last maxima)
+      if (ok) {
+        if (lane < RW) sm.most[q4][r0 + lane] = sum;
+        tc_fence_after();
+        const bool bad = *(volatile int*)&sm.bad_page[seq & 15] != 0;
+        // this lane's row of O^T: all 128, or (a product of 64 rows) 16 of each 32
+        const int column = RB == 128 ? key : lane < 16 ? q4 * 16 + lane : -1;
+#pragma unroll
+        for (int hf = 0; hf < HV; ++hf) {
           uint32_t o[3][16];
 #pragma unroll
           for (int i = 0; i < 3; ++i) tmem_ld16(tO + (hf * 3 + i) * R, o[i]);
@@ -683,35 +815,50 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
           wrong = __reduce_or_sync(0xffffffffu, wrong);
           if (wrong != 0 && lane == 0) atomicOr(&sm.not_finite[r0 >> 5], wrong << (r0 & 31));
         }
-      named_bar_sync(bar, 128);
-      if (key < RW) {
-        const int r = r0 + key;
-        sum = (sm.most[0][r] + sm.most[1][r]) + (sm.most[2][r] + sm.most[3][r]);
-        float m = (set >> key) & 1u ? -sm.nref[0][r] : -INFINITY;
-        if (sum != sum) m = INFINITY;  // a visible score that is not finite: the combined row is NaN
-        if (bad) m = -INFINITY, sum = decq8::kBadPage;
-        pml[r] = make_float2(m, sum);
-        if (a.nsplit == 1 && bad && key == 0) set_status(a.status, HD_DEVBIT_INDEX);
+        named_bar_sync(bar, 128);
+        if (key < RW) {
+          const int r = r0 + key;
+          sum = (sm.most[0][r] + sm.most[1][r]) + (sm.most[2][r] + sm.most[3][r]);
+          float m = (set >> key) & 1u ? -sm.nref[0][r] : -INFINITY;
+          if (sum != sum) m = INFINITY;  // a visible score that is not finite: the combined row is NaN
+          if (bad) {
+            m = -INFINITY, sum = decq8::kBadPage;
+          } else if (r < rows && sm.not_finite[r >> 5] >> (r & 31) & 1u) {
+            sum = kRedo;
+            sm.redo = 1;
+          }
+          pml[r] = make_float2(m, sum);
+          if (!SHARED && a.nsplit == 1 && bad && key == 0) set_status(a.status, HD_DEVBIT_INDEX);
+        }
+        named_bar_sync(bar, 128);
+        if (key == 0) atomicAnd(&sm.not_finite[r0 >> 5], ~(0xffffu << (r0 & 31)));
       }
-      named_bar_sync(bar, 128);
-      if (!bad)
+      done += nt;
+      chunks += waited;
+      ++seq;
+    } while (ok && work.next(a));
+    // Rows that came out not finite, by their visible keys alone: last, so that no other warp's bounded wait runs meanwhile.
+    if (ok && *(volatile int*)&sm.redo) {
+      if (SHARED) work = Work<SHARED>(a, split);
+      do {
 #pragma unroll 1
         for (int r = q4; r < RW; r += 4) {
-          const int row = r0 + r;
-          if (row < rows && (sm.not_finite[row >> 5] >> (row & 31)) & 1u)
-            decq8::exact_row<DH>(a, b, g, row0 + row, T, k0, k1, po + (size_t)row * DH, pml + row);
+          const size_t at = partial() + r0 + r;
+          if (r0 + r < rows && a.part_ml[at].y == kRedo)
+            decq8::exact_row<DH>(a, work.b, g, row0 + r0 + r, work.T, work.k0, work.k1, a.part_o + at * DH, a.part_ml + at);
         }
-      if (a.nsplit == 1) {  // the only split: its rows are the results
-        __syncwarp();
-        for (int r = q4; r < RW; r += 4) {
-          const int row = r0 + r;
-          if (row >= rows) break;
-          const float2 ml = pml[row];
-          decq8::store_row<DH>(a, b, g, row0 + row, po + (size_t)row * DH, ml.x, bad ? 0.f : ml.y);
-        }
+      } while (work.next(a));
+    }
+    if (!SHARED && ok && a.nsplit == 1) {  // the only split: its rows are the results
+      __syncwarp();
+      for (int r = r0 + q4; r < min(r0 + RW, rows); r += 4) {
+        const size_t at = partial() + r;
+        const float2 ml = a.part_ml[at];
+        decq8::store_row<DH>(a, work.b, g, row0 + r, a.part_o + at * DH, ml.x, ml.y == decq8::kBadPage ? 0.f : ml.y);
       }
     }
   }
+  if (SHARED && blockIdx.x == 0 && warp == 1) Work<SHARED>::report(a);
   tc_fence_before();
   __syncthreads();
   if (warp == 0) {
@@ -724,18 +871,22 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
 
 // ------------------------------------------------------------------ host side
 
-template <int DH, int WG>
-static cudaError_t launch_t(const decq8::Params& p, cudaStream_t st) {
+template <int DH, int WG, bool SHARED>
+static cudaError_t launch_s(const decq8::Params& p, unsigned parts, cudaStream_t st) {
   using namespace decq8tc;
   using C = Cfg<DH, WG>;
   const int smem = (int)sizeof(Smem<DH, WG>) + 1024;
   static_assert(sizeof(Smem<DH, WG>) + 1024 <= (C::kPerSm == 3 ? 75 : C::kPerSm == 2 ? 113 : 227) * 1024 && C::NSLOT >= 3 &&
                     C::kCols <= C::kAlloc && C::kPerSm * C::kAlloc <= 512,
                 "an SM's CTAs fit");
-  cudaError_t e = cudaFuncSetAttribute(decode_q8_tc_kernel<DH, WG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const auto kernel = decode_q8_tc_kernel<DH, WG, SHARED>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(true, decode_q8_tc_kernel<DH, WG>, dim3((unsigned)p.a.nsplit * p.a.B * p.a.Hkv * p.a.ngroups),
-                       (unsigned)C::kThreads, smem, st, p);
+  return launch_kernel(true, kernel, dim3(parts * p.a.Hkv * p.a.ngroups), (unsigned)C::kThreads, smem, st, p);
+}
+template <int DH, int WG>
+static cudaError_t launch_t(const decq8::Params& p, cudaStream_t st) {
+  return p.a.balanced ? launch_s<DH, WG, true>(p, p.a.total, st) : launch_s<DH, WG, false>(p, p.a.nsplit * p.a.B, st);
 }
 
 template <int DH>
