@@ -441,6 +441,88 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     store_row<DH>(a, b, g, rg * R + row, po + row * DH, ml.x, bad ? 0.f : ml.y);
   }
 }
+
+// The splits' partials of a query row together, a warp a row, where rows are many: a lane has DH / 32 columns of it, and the
+// maximum and sum of each 32nd split; the splits' columns are asked for ahead of their weights.  Bound by latency.  The
+// bf16 cache's combine kernel takes a CTA for a row, so fewer rounds over many splits but waves of CTAs over many rows:
+// a step of 4 streams, CTA a row / warp a row, in us
+//   128 rows   1 x 8192 tokens, 32 over 8 heads of 128 19.0 / 28.0;  384   4 x 8192, 24 over 2 of 256 30.2 / 40.3
+//   512        4 x 4000, 32 over 8 28.9 / 33.3;  1024   8 x 16384 113.6 / 114.5;  2048   16 x 400 22.9 / 19.8
+//   2560       20 x 2000 49.7 / 45.3;  3072   8 x 8192, 96 over 8 101.5 / 96.0;  7680   20 x 2000, 96 over 8 87.0 / 73.1
+template <int DH>
+__global__ void __launch_bounds__(256) combine_rows_kernel(Args a) {
+  constexpr int C = DH / 32, NB = DH == 256 ? 4 : 8, NW = dec::kMaxSplit / 32;  // columns, splits in flight, weights of a lane
+  const int lane = threadIdx.x & 31, rows = min(a.rg, a.M);
+  const int x = (int)blockIdx.x * 8 + (threadIdx.x >> 5), unit = x / rows, row = x - unit * rows;  // (b, g, row group), row
+  const int heads = a.Hkv * a.ngroups, b = unit / heads, head = unit - b * heads, g = head / a.ngroups, rg = head - g * a.ngroups;
+  const int r = rg * a.rg + row;
+  grid_dep_wait();  // every partial of the decoding kernel is written
+  if (b >= a.B) return;
+  const int T = a.lens[b];
+  const bool valid = T >= 1 && T <= a.maxT;
+  if (!valid && T != 0 && head == 0 && row == 0 && lane == 0) set_status(a.status, HD_DEVBIT_INDEX);
+  if (r >= a.M) return;  // the last row group may be short
+  const int2 own = a.balanced ? a.share[b] : make_int2(b * a.nsplit, a.nsplit);
+  const int n = valid ? own.y : 0;
+  const size_t first = ((size_t)own.x * heads + head) * a.rg + row, step = (size_t)heads * a.rg;
+  const float* po = a.part_o + first * DH + lane * C;
+  auto load = [&](int i, float* v) {
+#pragma unroll
+    for (int c = 0; c < C; c += 2) {
+      const float2 t = *reinterpret_cast<const float2*>(po + i * step * DH + c);
+      v[c] = t.x, v[c + 1] = t.y;
+    }
+  };
+  float v[NB][C];
+#pragma unroll
+  for (int k = 0; k < NB; ++k)
+    if (k < n) load(k, v[k]);
+  float2 ml[NW];
+  float m = -INFINITY;
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < NW; ++k) {
+    ml[k] = lane + 32 * k < n ? a.part_ml[first + (lane + 32 * k) * step] : make_float2(-INFINITY, 0.f);
+    m = fmaxf(m, ml[k].x);
+    bad |= ml[k].y == kBadPage;
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  bad = __any_sync(0xffffffffu, bad);
+  if (bad && lane == 0) set_status(a.status, HD_DEVBIT_INDEX);
+  float w[NW], l = 0.f;
+#pragma unroll
+  for (int k = 0; k < NW; ++k) {
+    w[k] = ml[k].x == -INFINITY ? 0.f : exp2f(ml[k].x - m);
+    l += w[k] * ml[k].y;
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+  float o[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) o[c] = 0.f;
+#pragma unroll
+  for (int k = 0; k < NW; ++k)
+#pragma unroll 1
+    for (int i0 = 32 * k; i0 < min(n, 32 * (k + 1)); i0 += NB) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const float f = __shfl_sync(0xffffffffu, w[k], i0 + j & 31);
+        if (i0 + j < n && f != 0.f)
+#pragma unroll
+          for (int c = 0; c < C; ++c) o[c] += f * v[j][c];
+        if (i0 + j + NB < n) load(i0 + j + NB, v[j]);
+      }
+    }
+  const bool ok = valid && !bad && l != 0.f;
+  const float inv = ok ? 1.f / l : 0.f;
+  const int s = fast_div(r, a.d_G), h = g * a.G + r - s * a.G;
+  uint32_t* to = reinterpret_cast<uint32_t*>(a.o + (((long long)b * a.n + s) * a.Hq + h) * DH + lane * C);
+#pragma unroll
+  for (int c = 0; c < C; c += 2) to[c / 2] = ok ? pack_bf16(o[c] * inv, o[c + 1] * inv) : 0;
+  if (lane == 0 && a.lse != nullptr)
+    a.lse[((long long)b * a.Hq + h) * a.n + s] = ok ? (m + __log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
 }  // namespace decq8
 
 // ------------------------------------------------------------------ host side
@@ -537,6 +619,15 @@ static cudaError_t launch_q8_d(const decq8::Args& a, cudaStream_t st) {
   return a.rg > 16 * decq8::Cfg<DH, false>::MT ? launch_q8_t<DH, true>(a, st) : launch_q8_t<DH, false>(a, st);
 }
 
+static cudaError_t launch_combine_q8(const decq8::Args& a, int Dh, cudaStream_t st) {
+  const long long rows = (long long)std::min(a.rg, a.M) * a.B * a.Hkv * a.ngroups;
+  if (rows <= 8 * kSmCount) return launch_combine_paged(a, Dh, st);  // one wave of a CTA each
+  const dim3 grid((unsigned)((rows + 7) / 8));
+  if (Dh == 64) return launch_early(decq8::combine_rows_kernel<64>, grid, 256, st, a);
+  if (Dh == 128) return launch_early(decq8::combine_rows_kernel<128>, grid, 256, st, a);
+  return launch_early(decq8::combine_rows_kernel<256>, grid, 256, st, a);
+}
+
 cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void* vc, const uint8_t* ks, const uint8_t* vs,
                                        const int32_t* table, const int32_t* lens, void* o, float* lse, int B, int maxT,
                                        int num_pages, int P, int max_pages, int n, int Hq, int Hkv, int Dh, int T,
@@ -595,7 +686,7 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
                         : Dh == 64  ? launch_q8_d<64>(a, st)
                         : Dh == 128 ? launch_q8_d<128>(a, st)
                                     : launch_q8_d<256>(a, st);
-  return e != cudaSuccess || a.nsplit == 1 ? e : launch_combine_paged(a, Dh, st);
+  return e != cudaSuccess || a.nsplit == 1 ? e : launch_combine_q8(a, Dh, st);
 }
 
 }  // namespace hdsfa
