@@ -423,8 +423,8 @@ hd_status_t hd_pages_copy(void* k_pages, void* v_pages, const int32_t* copies, i
  *                        divides P; all n streams of a token together) and head: a power of two 2^e as the byte e + 127
  * A code c of a block stands for c * 2^e, which is exact in bf16.  e lies in [-64, 50] (bytes 63 ... 177; others
  * are read as the nearest of these): values below 2^-74 become 0, values above 448 * 2^50 saturate.
- * Pools and scales are 16-byte aligned.  Limits beside those above: Dh a multiple of 16, n*Hkv*Dh <= 2^24, block_tokens*n*Dh <= 2^30, Hkv <= 32767,
- * num_pages*P*n*Hkv < 2^32.
+ * Pools and scales are 16-byte aligned.  Limits beside those above: Dh a multiple of 16, n*Hkv*Dh <= 2^24,
+ * block_tokens*n*Dh <= 2^30, Hkv <= 32767, num_pages*P*n*Hkv < 2^32.
  *
  * sfa_kv_append_paged_q8 -- sfa_kv_append_paged into such a cache: the same arguments, rows and refusals; served
  *   (nullable) as in sfa_kv_append_paged_served.  Of a block, the call brings some last tokens.  If no token before

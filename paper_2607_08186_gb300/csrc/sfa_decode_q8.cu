@@ -555,7 +555,7 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
   const long long tiles = (q8_range(maxT, n, mode, window) + KT - 1) / KT, ctas = (long long)B * Hkv * p.ngroups;
   int per_sm = tc ? decode_q8_tc_per_sm(p.rg, Dh) : p.rg > (Dh == 256 ? 16 : 32) ? 1 : Dh == 64 && p.rg == 16 ? 4 : 2;
   // few tiles: fewer splits, which the combine kernel merges faster (1 x 8192 tokens, 4 streams, 32 over 8 heads of 128, 13
-  // tiles an SM: two CTAs an SM 21.2 us, three 23.1; 8 x 2048, 27 tiles: 29.1 and 28.0)
+  // tiles an SM: two CTAs an SM 21.2 us, three 23.1; 8 x 2048, 27 tiles: 29.1 and 28.0; both before starts were shortened)
   if (tc && ctas * tiles < 20 * kSmCount) per_sm = std::min(per_sm, 2);
   const long long resident = (long long)kSmCount * per_sm;
   const long long most = std::min({tiles, (long long)dec::kMaxSplit, std::max(1LL, 4 * resident / ctas)});
@@ -574,10 +574,14 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
     }
   }
   p.nsplit = (int)best;
-  // Several sequences, long splits: a wave of CTAs shares their tiles equally, whatever the lengths.
+  // Several sequences, long splits: a wave of CTAs shares their tiles equally, whatever the lengths; also where a CTA for
+  // each head and sequence would be one wave of long ones, but not several waves, which even lengths out by themselves
+  // and write results and not partials.  (One / the other, 4 streams and sequences of lengths from a quarter on, us: 96 over 8
+  // heads of 128, 8 x 8192, 8 streams 494 / 340; 3 streams, 16 over 4 of 64, 100 x 2000 76 / 70.5; 96 over 8, 120 x 2000, seven
+  // waves, 350 / 361; 60 x 400 68 / 78; 16 x 400, one wave of 13 tiles, 23.4 / 29.1.)
   const long long heads = (long long)Hkv * p.ngroups, range = q8_range(maxT, n, mode, window);
-  if (tc && B > 1 && B <= dec::kBalancedSeqs && (bound || (best > 1 && range / best >= 4 * 64)))
-    p.total = (int)std::max(1LL, resident / heads);
+  const bool shared = best > 1 ? range / best >= 4 * 64 : ctas <= resident && tiles >= 32;
+  if (tc && B > 1 && B <= dec::kBalancedSeqs && (bound || shared)) p.total = (int)std::max(1LL, resident / heads);
   const size_t parts = std::max((size_t)ctas * best, p.total > 0 ? (size_t)(p.total + B) * heads : 0);
   p.part_o_bytes = parts * p.rg * Dh * sizeof(float);
   p.part_ml_bytes = parts * p.rg * sizeof(float2);
@@ -587,10 +591,10 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
 // Whether the tcgen05 kernel takes a step.  It reads tiles by TMA alone, in pieces of at least kTmaRows rows of a page that
 // start on 128 bytes of shared memory, and takes longer to start and end, so up to 16 query rows leave it short ranges.
 // Measured (replayed from a graph, us, tcgen05 / mma.sync, 4 streams but where said):
-//   32 over 8 heads of 128   33 x 12 tokens 12.2 / 10.0, 4 x 50 10.3 / 10.1, 4 x 150 11.8 / 11.8, 4 x 1000 15.8 / 17.4, 16 x 1000
-//                            31.8 / 41.0; one stream, 7 of up to 20000 40.2 / 67.2
-//   16 over 4 of 64          3 streams, 4 x 400 11.7 / 9.1, 4 x 3000 16.8 / 18.2
-//   24 over 2 of 256         4 x 50 14.8 / 23.8;  96 over 8 of 128: 16 x 50 13.7 / 15.1, 16 x 400 26.6 / 46.9
+//   32 over 8 heads of 128   33 x 12 tokens 12.2 / 10.0, 4 x 50 10.3 / 10.1, 4 x 150 10.6 / 11.8, 4 x 1000 16.3 / 17.4, 16 x 1000
+//                            26.7 / 41.0; one stream, 7 of up to 20000 40.4 / 67.2
+//   16 over 4 of 64          3 streams, 4 x 400 11.7 / 9.1, 4 x 3000 17.0 / 18.2
+//   24 over 2 of 256         4 x 50 12.9 / 23.8;  96 over 8 of 128: 16 x 50 11.8 / 15.1, 16 x 400 23.3 / 46.9
 constexpr int kTmaRows = 8;
 static bool q8_tc(int Dh, int prow, int rows, long long range) {
   const int piece = paged_piece(prow, 128);
@@ -686,7 +690,7 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
                         : Dh == 64  ? launch_q8_d<64>(a, st)
                         : Dh == 128 ? launch_q8_d<128>(a, st)
                                     : launch_q8_d<256>(a, st);
-  return e != cudaSuccess || a.nsplit == 1 ? e : launch_combine_q8(a, Dh, st);
+  return e != cudaSuccess || (a.nsplit == 1 && !a.balanced) ? e : launch_combine_q8(a, Dh, st);
 }
 
 }  // namespace hdsfa

@@ -13,24 +13,29 @@
 //     it goes up; the third codes hold 64 times what they stand for, so steps end at 2^-22, 2^-27 of the row's largest.
 //     The three columns are added at the end.
 // A thread of a softmax warp takes its position's scores for its group's 16 rows: scales by 2^ek, adds ev, masks (what
-// a position is visible to is a range of rows), and subtracts the row's reference.  References are the group's, in
-// shared memory, and go up only when some P would pass 2^15 (a vote for each tile; every tile after the first few has
-// none): then the rows' maxima are reduced over the four warps, and sums and O in tensor memory are rescaled.
+// a position is visible to is a range of rows), and subtracts the row's reference.  References are the group's (a copy
+// for each warp), and go up only when some P would pass 2^15 (a vote for each tile; every tile after the first few has
+// none): then the rows' maxima are reduced over the four warps, and sums and O in tensor memory are rescaled.  (The vote as
+// an arrival and a wait, with the exponentials between them, was slower: 96 rows of 8 heads 99 us for 96.)
 //
 // Warp 0 brings tiles (TMA, pieces of pages) into a ring of units of 128 columns, warp 1 issues the products, the
-// others are R / 16 groups of four softmax warps.  S and P have two buffers, so S of the next tile is computed under this
-// one's softmax and its P V under the next one's.  The first group brings the scales 384 blocks ahead, since a load
-// behind a saturated memory's queue takes thousands of cycles, and a batch's splits are shared out by the sequences'
-// lengths, as for the bf16 cache (8 sequences of up to 16384 tokens, 4 streams: 32 over 8 heads of 128 139 us without the two
-// and 133 with them, 24 over 2 heads of 256 140 and 88).
+// others are R / 16 groups of four softmax warps, which first code the queries, four rows a warp.  S and P have two
+// buffers, so S of the next tile is computed under this one's softmax and its P V under the next one's.  The first group
+// brings the scales 384 blocks ahead, since a load behind a saturated memory's queue takes thousands of cycles.
 //
-// Bound by memory at 16 query rows, of 8 heads of 128: 16 sequences of 32768 tokens, 32 over 8 heads, 395 us (6.87
-// TB/s of codes and scales; floor 400 at the copy rate), 16384 tokens of 8 114.  With more rows the softmax warps' issue and
-// latency pass it, about 420 instructions for 16 rows of a warp's 32 positions: 32 rows reach 0.74 of the copy rate, 48
-// 0.56, 64 0.46 (equal lengths), more than 64 read the cache once for each group of 64 (96 rows: 0.31); 24 rows of heads
-// of 256 0.72.  Three CTAs an SM at 16 rows (up to head dim 128) hide a tile's chain of barriers: 133 us with two, 114 with
-// three.  Tried and dropped: warps of 24 to 48 rows (registers: fewer warps to hide the latency), two tiles in turn with
-// an O each, queries in three codes everywhere (K's reads three times: bound by shared memory at 16 rows).
+// A batch of long sequences is one wave of CTAs, each with an equal share of all tiles (Work), because a CTA takes about
+// 12000 cycles to start and 4000 to end, six tiles' time: 8 x 8192 tokens, 96 over 8 heads of 128, 122 us with three waves
+// of splits and 101 so.
+//
+// Bound by memory at 16 query rows, of 8 heads of 128: 16 sequences of 32768 tokens, 32 over 8 heads, 390 to 397 us (6.9
+// TB/s of codes and scales; 400 at the copy rate), 8 of up to 16384 112 for 103.  With more rows by the softmax warps'
+// chain, about 350 instructions for 16 rows of a warp's 32 positions, 2000 cycles a tile for each group at once (clock64,
+// 48 rows: masks and scales 450, waiting for S 240, scores 430, vote 340, codes of P 380, fence 130): these
+// lengths reach 0.88 of the copy rate at 32 rows (117 us), 0.61 at 48, 0.49 at 64; 48 of heads of 256 0.78 (66 for 52); more
+// than 64 rows read the cache once for each group of 64 (8 x 8192, 96 rows, 340 for 104).  Three
+// CTAs an SM at 16 rows (up to head dim 128) hide a tile's chain of barriers: 133 us with two, 114 with three.  Tried and
+// dropped: warps of 24 to 48 rows (registers: fewer warps to hide the latency), two tiles in turn with an O each, queries in
+// three codes everywhere (K's reads three times: bound by shared memory at 16 rows).
 #include <float.h>
 
 #include <algorithm>
