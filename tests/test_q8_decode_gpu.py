@@ -166,6 +166,79 @@ def test_long_sequences_in_numbers(B, n, Hq, Hkv, Dh, P, T):
             _assert_rows(o[b:b + 1], lse[b:b + 1], q[b:b + 1], kv[i:i + 1], vv[i:i + 1], lens[b], 0, n, mode, w)
 
 
+# batches whose tiles one wave of CTAs shares, with lengths from nothing to everything: a sequence in more parts than are
+# merged, in one, in none; parts of many sequences; the lengths of a captured call replaced between its replays
+@pytest.mark.parametrize("B,n,Hq,Hkv,Dh,P,T,L", [(2, 4, 4, 1, 64, 32, 8, 16000), (2, 4, 4, 1, 128, 16, 16, 16000), (6, 4, 48, 4, 128, 16, 16, 2500),
+                                                 (128, 2, 16, 2, 256, 20, 5, 1200), (128, 4, 48, 2, 64, 16, 1, 900), (33, 4, 24, 1, 128, 9, 3, 1000)])
+def test_a_wave_shared_by_uneven_sequences(B, n, Hq, Hkv, Dh, P, T, L):
+    q, kc, vc = _case(1, L, n, Hq, Hkv, Dh, B + P)
+    kq, ks, table, kv = q8.quantised(kc, [L], P, T, n, 3)
+    vq, vs, _, vv = q8.quantised(vc, [L], P, T, n, 3)
+    q = inputs.normal_bf16((B, n, Hq, Dh), 78)
+    many = [b * 37 % 90 for b in range(B)]
+    batches = [[L] + [0] * (B - 1), [0] * (B - 1) + [L], [1] * B, [0] * B, many[:-1] + [L], [L - b % 7 for b in range(B)]]
+    dev = [x.cuda() for x in (q, kq, vq, ks, vs, table.expand(B, -1).contiguous())]
+    lens = torch.zeros(B, dtype=I32, device="cuda")
+    ws = guards.empty((binding.sfa_decode_paged_q8_workspace_bytes(B, L, n, Hq, Hkv, Dh, CROSS),), torch.uint8, 0xFF, what="workspace")
+    o, lse = guards.empty(q.shape, BF, 7.0), guards.empty((B, Hq, n), torch.float32, 7.0)
+    st = torch.zeros(1, dtype=I32, device="cuda")
+    call = lambda: binding.sfa_decode_paged_q8(*dev, lens, o, n, CROSS, ws, max_tokens=L, lse=lse, dev_status=st)
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for batch in batches:
+        lens.copy_(_i32(batch))
+        g.replay()
+        torch.cuda.synchronize()
+        assert int(st.item()) == 0
+        oc, lc = o.cpu(), lse.cpu()
+        for b in {0, 1, B // 2, B - 1}:
+            if batch[b]:
+                _assert_rows(oc[b:b + 1], lc[b:b + 1], q[b:b + 1], kv, vv, batch[b], 0, n, CROSS, 0)
+            else:
+                _assert_empty(oc, lc, b)
+        ob = o.clone()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(o.view(torch.int16), ob.view(torch.int16))
+
+
+@pytest.mark.parametrize("B,n,Hq,Hkv,Dh,P,L", [(40, 2, 8, 2, 128, 16, 900), (70, 2, 48, 2, 64, 32, 1000), (40, 3, 36, 2, 256, 12, 700)])
+def test_a_shared_wave_keeps_bad_pages_and_hidden_nan_to_their_sequences(B, n, Hq, Hkv, Dh, P, L):
+    q, kc, vc = _case(2, L, n, Hq, Hkv, Dh, 21)
+    vc[1, (L - 300) * n, 0, 3] = float("nan")  # of stream 0: hidden from the other streams' rows
+    kq, ks, table, kv = q8.quantised(kc, [L, L], P, P, n, 3)
+    vq, vs, _, vv = q8.quantised(vc, [L, L], P, P, n, 3)
+    q = inputs.normal_bf16((B, n, Hq, Dh), 79)
+    which = [1 if b % 5 == 2 else 0 for b in range(B)]
+    tables = table[which].clone()
+    wrong = {3: kq.shape[0], 4: -1, B // 2: 2**31 - 1, B - 1: -5}
+    for b, page in wrong.items():
+        tables[b, (b * 7) % (L // P)] = page
+    lens = [L - 2 * (b % 9) for b in range(B)]
+    vv[1, (L - 300) * n, 0, 3] = 0.0
+    o, lse, st = _decode(q, kq, vq, ks, vs, tables, _i32(lens), n, WITHIN, max_tokens=L)
+    assert st == binding.HD_DEVBIT_INDEX
+    for b in range(B):
+        if b in wrong:
+            _assert_empty(o, lse, b)
+        elif which[b] == 0:
+            if b % 3 == 0 or b < 9:
+                _assert_rows(o[b:b + 1], lse[b:b + 1], q[b:b + 1], kv[:1], vv[:1], lens[b], 0, n, WITHIN, 0)
+        else:  # stream 0's rows of the first K/V head are NaN in that column, and nothing else is
+            assert bool(torch.isnan(o[b, 0, :Hq // Hkv, 3]).all()) and int(torch.isnan(o[b]).sum()) == Hq // Hkv
+            ob = o[b:b + 1].clone()
+            keep = torch.ones(n, Hq, Dh, dtype=torch.bool)
+            keep[0, :Hq // Hkv, 3] = False
+            o_r, lse_r, _ = oracle.decode(q[b:b + 1], kv[1:], vv[1:], _i32([lens[b]]), n, WITHIN)
+            A, _, _ = oracle.decode(q[b:b + 1], kv[1:], vv[1:].abs(), _i32([lens[b]]), n, WITHIN)
+            lim = 2.0**-8 * o_r.abs() + (2.0**-9 + 2.0**-11 + 1e-3) * A + 1e-3 * o_r.abs()
+            assert bool(((ob.double() - o_r).abs() <= lim)[0][keep].all())
+            assert float((lse[b].double() - lse_r[0]).abs().max()) <= 1e-3
+
+
 @pytest.mark.parametrize("Dh,P", [(64, 16), (128, 16), (256, 16), (128, 3)])
 def test_wrong_lengths_and_pages_empty_their_sequence_alone(Dh, P):
     n, Hq, Hkv, L = 2, 8, 2, 90
