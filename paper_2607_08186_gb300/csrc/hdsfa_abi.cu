@@ -663,7 +663,7 @@ static hd_status_t decode_q8_sizes(int B, int maxT, int n, int Hq, int Hkv, int 
   hd_status_t st = decode_paged_sizes(B, maxT, n, Hq, Hkv, Dh, mode, window);
   if (st != HD_OK) return st;
   const long long groups = ((long long)n * (Hq / Hkv) + 63) / 64;
-  return B * Hkv * groups > (1LL << 30) ? HD_ERR_UNSUPPORTED : HD_OK;  // CTAs of one split
+  return (long long)B * Hkv * groups > (1LL << 30) ? HD_ERR_UNSUPPORTED : HD_OK;  // CTAs of one split
 }
 
 size_t sfa_decode_paged_q8_workspace_bytes(int B, int max_tokens, int n, int Hq, int Hkv, int Dh, sfa_mode_t mode,

@@ -80,6 +80,11 @@ def test_decode_refusals(lib):
         binding.sfa_decode_paged_q8_workspace_bytes(2, 64, 2, 4, 2, 64, 2, 128)
 
 
+def test_counts_beyond_32_bits_are_refused(lib):
+    for B, Hkv in ((65535, 131072), (65535, 65536), (65535, 1 << 20)):  # CTAs of one split: 2^33, 2^32 and 2^36
+        assert binding.sfa_decode_paged_q8_workspace_bytes(B, 16, 1, Hkv, Hkv, 64, 1) == 0
+
+
 def test_workspace_serves_every_shorter_step(lib):
     r = random.Random(3)
     for _ in range(400):
@@ -178,3 +183,41 @@ def test_units_of_packed_prompts(T):
             assert blocks <= (off[b + 1] // T + 2 * b + 2) - start
             seen += [start + j for j in range(blocks)]
         assert len(set(seen)) == len(seen) and max(seen, default=0) <= N // T + 2 * B - 1
+
+
+def test_parts_of_a_shared_wave():
+    """Part x of S has the units floor(x all / S) ... of the sequences' tiles, each with 6 units of its start in front: every
+    tile is in one part, no two partials have the number x + b, and a sequence's have successive ones, 128 at most."""
+    r = random.Random(5)
+    start = 6
+    for _ in range(400):
+        B, total, kind = r.randint(2, 128), r.choice([1, 2, 9, 19, 76, 152, 228, 456]), r.random()
+        tiles = [0 if r.random() < 0.2 else r.randint(1, 5 if kind < 0.4 else 3000) if r.random() < 0.95 else 8000000 for _ in range(B)]
+        size = [t + start if t else 0 for t in tiles]
+        every, most = sum(size), max(size)
+        S = max(1, min(total, every))
+        if most * S > 126 * every:
+            S = 126 * every // most
+        per, rest = every // S, every % S
+        parts, numbers = {}, set()
+        for x in range(S):
+            u0, u1 = x * per + x * rest // S, (x + 1) * per + (x + 1) * rest // S
+            assert (u0, u1) == (x * every // S, (x + 1) * every // S) and (u0 < u1 or not every)
+            before = 0
+            for b in range(B):
+                lo, hi = max(u0, before + start), min(u1, before + size[b])
+                if size[b] and lo < hi:
+                    assert x + b not in numbers and x + b < total + B
+                    numbers.add(x + b)
+                    parts.setdefault(b, []).append((x + b, lo - before - start, hi - before - start))
+                before += size[b]
+        before = 0
+        for b in range(B):
+            if tiles[b]:
+                of = lambda u: ((u + 1) * S - 1) // every
+                x0 = of(before + start)
+                n = of(before + size[b] - 1) - x0 + 1
+                mine = parts[b]
+                assert n <= 128 and [p[0] for p in mine] == list(range(x0 + b, x0 + b + n))
+                assert mine[0][1] == 0 and mine[-1][2] == tiles[b] and all(p[2] == q[1] for p, q in zip(mine, mine[1:]))
+            before += size[b]
