@@ -34,8 +34,9 @@
 // lengths reach 0.88 of the copy rate at 32 rows (117 us), 0.61 at 48, 0.49 at 64; 48 of heads of 256 0.78 (66 for 52); more
 // than 64 rows read the cache once for each group of 64 (8 x 8192, 96 rows, 340 for 104).  Three
 // CTAs an SM at 16 rows (up to head dim 128) hide a tile's chain of barriers: 133 us with two, 114 with three.  Tried and
-// dropped: warps of 24 to 48 rows (registers: fewer warps to hide the latency), two tiles in turn with an O each, queries in
-// three codes everywhere (K's reads three times: bound by shared memory at 16 rows).
+// dropped: warps of 24 to 48 rows (registers: fewer warps to hide the latency), two tiles in turn with an O each, two tiles for
+// each vote (48 rows: 102 us for 96), queries in three codes everywhere (K's reads three times: bound by shared memory at
+// 16 rows).
 #include <float.h>
 
 #include <algorithm>
