@@ -442,3 +442,37 @@ def test_two_calls_at_once_and_the_same_bits():
         torch.cuda.synchronize()
         for (t, o, _, _), w in zip(runs, want):
             assert torch.equal(o, w)
+
+
+@pytest.mark.parametrize("Hq,Hkv,Dh,P,T", [(32, 8, 128, 16, 16), (16, 4, 64, 3, 1), (24, 2, 256, 20, 5)])
+def test_pools_beyond_32_bits(Hq, Hkv, Dh, P, T):
+    """Pages whose codes lie more than 2^32 bytes into the pool: prompt, token, read, copy and step give the bits that they
+    give in a small pool."""
+    n, L = 4, 100
+    far = 2**32 // (P * n * Hkv * Dh) + 2
+    held = -(-L // P)
+    q, kn, vn = (inputs.normal_bf16((1, n, h, Dh), 1 + i).cuda() for i, h in enumerate((Hq, Hkv, Hkv)))
+    kr, vr = (inputs.normal_bf16(((L - 1) * n, Hkv, Dh), 5 + i).cuda() for i in range(2))
+    runs = []
+    for base in (0, far):
+        pages = base + held + 1
+        kc, vc = (torch.empty(pages, Hkv, P * n, Dh, dtype=F8, device="cuda") for _ in range(2))
+        ks, vs = (torch.empty(pages, Hkv, P // T, dtype=torch.uint8, device="cuda") for _ in range(2))
+        table = (base + 1 + torch.arange(held, dtype=I32)).flip(0).view(1, held).cuda()
+        lens, st = _i32([L - 1]).cuda(), torch.zeros(1, dtype=I32, device="cuda")
+        binding.sfa_kv_append_paged_q8(kr, vr, kc, vc, ks, vs, table, lens, n, offsets=_i32([0, L - 1]).cuda(), dev_status=st)
+        lens += 1
+        binding.sfa_kv_append_paged_q8(kn, vn, kc, vc, ks, vs, table, lens, n, dev_status=st)
+        binding.hd_pages_copy_q8(kc, vc, ks, vs, torch.stack([table[0, -1:], table[0, -1:] - 1], 1).contiguous(), dev_status=st)
+        table[0, -1] -= 1  # the copy
+        k, v = (torch.empty(L * n, Hkv, Dh, dtype=BF, device="cuda") for _ in range(2))
+        binding.sfa_kv_read_paged_q8(kc, vc, ks, vs, table, lens, _i32([0, L]).cuda(), k, v, n, dev_status=st)
+        ws = torch.empty(binding.sfa_decode_paged_q8_workspace_bytes(1, held * P, n, Hq, Hkv, Dh, CROSS), dtype=torch.uint8,
+                         device="cuda")
+        o, lse = torch.empty_like(q), torch.empty(1, Hq, n, device="cuda")
+        binding.sfa_decode_paged_q8(q, kc, vc, ks, vs, table, lens, o, n, CROSS, ws, lse=lse, dev_status=st)
+        assert int(st.item()) == 0
+        runs.append([x.cpu() for x in (k, v, o, lse)])
+    for a, b in zip(*runs):
+        assert torch.equal(a.view(torch.int16 if a.dtype == BF else I32), b.view(torch.int16 if b.dtype == BF else I32))
+    _assert_rows(runs[1][2], runs[1][3], q.cpu(), runs[1][0][None], runs[1][1][None], L, 0, n, CROSS, 0)
