@@ -43,14 +43,15 @@ HD_DEVINLINE size_t scale_at(const Geom& g, int page, int h, int block) {
   return ((size_t)page * g.Hkv + h) * g.blocks + block;
 }
 
-// Two codes (lo, hi) of two values, to the nearest, ties to even.  What is not finite becomes NaN (e4m3 has no
-// infinities); finite values beyond 448 saturate.
-HD_DEVINLINE uint32_t code2(float lo, float hi) {
-  lo = fabsf(lo) <= 3.4e38f ? lo : NAN;
-  hi = fabsf(hi) <= 3.4e38f ? hi : NAN;
+// Two codes (lo, hi) of two values, to the nearest, ties to even; beyond 448 they saturate, NaN stays NaN.
+HD_DEVINLINE uint32_t code2_sat(float lo, float hi) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
+}
+// ... where infinities become NaN too (e4m3 has none).
+HD_DEVINLINE uint32_t code2(float lo, float hi) {
+  return code2_sat(fabsf(lo) <= 3.4e38f ? lo : NAN, fabsf(hi) <= 3.4e38f ? hi : NAN);
 }
 // The values of two codes, exactly.
 HD_DEVINLINE uint32_t f16x2_of(uint16_t codes) {
