@@ -19,10 +19,10 @@
 // transposed loads bring pairs of head-dim columns for two keys, so even and odd columns are products of their own.
 //
 // Bound by the latency of a tile's chain (table entry, rows, scales, products, softmax) and by the instructions that
-// turn codes into f16: 32 over 8 heads of 128, 4 streams, 4 sequences of 4000 tokens on pages of 2 tokens take 28.1 us, 14.7
-// of them the bytes at the copy rate; pages of one token with a scale each 48.  Bringing larger pieces by TMA here with two
-// sets of warps on alternate tiles gains nothing where this kernel runs (4 x 50 tokens 9.3 us and 10.1 without, 33 x 12
-// 10.9 and 10.0, two sequences of 64 over heads of 64 6.5 and 6.1).
+// turn codes into f16: 32 over 8 heads of 128, 4 streams, 4 sequences of 4000 tokens on pages of one token with a scale each
+// take 41.3 us, 14.7 of them the bytes at the copy rate (64 over 8 58, 96 over 8 92).  Bringing larger pieces by TMA here with
+// two sets of warps on alternate tiles gained nothing where this kernel runs (4 x 50 tokens 9.3 us and 10.1 without, 33 x
+// 12 10.9 and 10.0, two sequences of 64 over heads of 64 6.5 and 6.1).
 #include <float.h>
 
 #include <algorithm>
@@ -32,33 +32,31 @@
 
 namespace hdsfa {
 namespace decq8 {
-constexpr int kWarpKeys = 32;        // positions of a tile that a warp takes
 constexpr float kShift = 15.f;       // P's largest exponent
 constexpr int kMaxRows = 64;         // query rows of a CTA at most (four row tiles)
 
-template <int DH>
-constexpr int dsplit() { return DH == 256 ? 2 : 1; }  // head-dim parts: a warp's O must fit its registers
-template <int DH>
-constexpr int key_warps() { return 4 / dsplit<DH>(); }
-template <int DH>
-constexpr int ktile() { return kWarpKeys * key_warps<DH>(); }
-
-// Two CTAs an SM (more at head dim 64) while their queries leave room for three stages each: up to two row tiles, one at
-// head dim 256.  WIDE: more row tiles, one CTA an SM.
-template <int DH, bool WIDE>
+// Up to MT row tiles of 16 query rows; at head dim 256 a warp has half of the head dim, since O must fit its registers.  Two
+// CTAs an SM while the queries leave room for three stages each: up to two row tiles, one at head dim 256; with four row
+// tiles one.  At head dim 128 a single row tile leaves eight warps an SM so, so its warps take 16 positions of a tile and not
+// 32, and four CTAs fit (pages of one token, 4 x 4000 tokens, 32 over 8 heads: 48.6 us
+// for 41.3); at 64 four fit as it is.
+template <int DH, int MT_>
 struct Cfg {
-  static constexpr int KT = ktile<DH>(), MT = WIDE ? 4 : DH == 256 ? 1 : 2, STAGES = !WIDE ? 3 : DH == 256 ? 5 : 6;
+  static constexpr int MT = MT_, WK = DH == 128 && MT == 1 ? 16 : 32;             // positions of a tile that a warp takes
+  static constexpr int DS = DH == 256 ? 2 : 1, KW = 4 / DS, KT = WK * KW;         // head-dim parts, key groups, a tile
+  static constexpr bool kWide = MT == 4;
+  static constexpr int STAGES = !kWide ? 3 : DH == 256 ? 5 : 6;
+  static constexpr int kPerSm = kWide ? 1 : WK == 16 ? 4 : 2;
   static constexpr int kWarps = 4 * MT, kThreads = kWarps * 32;
   static constexpr int kMergeRows = 16 * MT;  // rows of the partials at most
 };
-
-template <int DH, bool WIDE>
+template <int DH, int MT>
 struct Smem {
-  using C = Cfg<DH, WIDE>;
+  using C = Cfg<DH, MT>;
   uint8_t k[C::STAGES][C::KT * DH];
   uint8_t v[C::STAGES][C::KT * DH];
   __half q[C::MT * 16 * DH];
-  float4 scale[C::kWarps][kWarpKeys];   // a warp's keys: 2^ek, ev, 2^-ev
+  float4 scale[C::kWarps][C::WK];   // a warp's keys: 2^ek, ev, 2^-ev
   float qscale[C::MT * 16];
   uint32_t row[4][C::KT];               // rows of the pool (kNoRow: none) of four tiles
   unsigned not_finite[2];               // a bit for each row of the merged partial
@@ -85,12 +83,12 @@ HD_DEVINLINE uint32_t pack_f16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-template <int DH, bool WIDE>
-__global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_q8_kernel(const __grid_constant__ Args a) {
-  using C = Cfg<DH, WIDE>;
-  using Sm = Smem<DH, WIDE>;
-  constexpr int KT = C::KT, STAGES = C::STAGES;
-  constexpr int KW = key_warps<DH>(), DC = DH / dsplit<DH>(), CPR = DH / 16;  // DC: O columns of a warp
+template <int DH, int MT>
+__global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) decode_q8_kernel(const __grid_constant__ Args a) {
+  using C = Cfg<DH, MT>;
+  using Sm = Smem<DH, MT>;
+  constexpr int KT = C::KT, STAGES = C::STAGES, WK = C::WK, NJ = WK / 8;  // NJ: tiles of 8 positions of a warp
+  constexpr int KW = C::KW, DC = DH / C::DS, CPR = DH / 16;  // DC: O columns of a warp
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   {
     uint32_t dyn;
@@ -125,14 +123,14 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
   }
   const bool streams = a.mode == SFA_WITHIN && a.n > 1;
   const bool shifting = streams && tile - fast_div(tile, a.d_n) * a.n != 0;
-  uint32_t mine = 0;  // bit hf*8 + j*2 + e: the row may see key j*8 + 2*t4 + e
+  uint32_t mine = 0;  // bit hf*2*NJ + j*2 + e: the row may see key j*8 + 2*t4 + e
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int key = kw * kWarpKeys + (i >> 1) * 8 + 2 * t4 + (i & 1);
+  for (int i = 0; i < 2 * NJ; ++i) {
+    const int key = kw * WK + (i >> 1) * 8 + 2 * t4 + (i & 1);
     const int ks = streams && !shifting ? key - fast_div(key, a.d_n) * a.n : -1;
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf)
-      if (rs_[hf] >= 0 && key < tile && (ks < 0 || ks == rs_[hf])) mine |= 1u << (hf * 8 + i);
+      if (rs_[hf] >= 0 && key < tile && (ks < 0 || ks == rs_[hf])) mine |= 1u << (hf * 2 * NJ + i);
   }
   grid_dep_wait();
   grid_dep_launch();
@@ -172,7 +170,7 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
   };
   // The scales of this warp's keys, a lane's key each: the page entry two tiles ahead, the bytes one ahead.  The
   // key's page and row there go on by a tile, without divisions.
-  const int my_key = kw * kWarpKeys + lane;
+  const int my_key = lane < WK ? kw * WK + lane : KT;
   const int step_pages = fast_div(tile, a.pg.d_prow), step_rows = tile - step_pages * a.pg.prow;
   int at_pos = k0 + my_key, at_page = fast_div(at_pos, a.pg.d_prow), at_row = at_pos - at_page * a.pg.prow;
   int next_entry = -1, next_row_in = 0;
@@ -250,7 +248,7 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     {
       kb = q8::clamp_byte(kb);
       vb = q8::clamp_byte(vb);
-      sm.scale[warp][lane] = make_float4(q8::scale_of(kb), (float)(vb - 127), q8::inverse_of(vb), 0.f);
+      if (lane < WK) sm.scale[warp][lane] = make_float4(q8::scale_of(kb), (float)(vb - 127), q8::inverse_of(vb), 0.f);
       scale_bytes();
       scale_entry();
     }
@@ -262,9 +260,9 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     const uint8_t *cK = sm.k[st], *cV = sm.v[st];
 
     // S = q ck^T: key tile j of 8 keys
-    float sacc[4][4];
+    float sacc[NJ][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sacc[j][0] = sacc[j][1] = sacc[j][2] = sacc[j][3] = 0.f;
+    for (int j = 0; j < NJ; ++j) sacc[j][0] = sacc[j][1] = sacc[j][2] = sacc[j][3] = 0.f;
 #pragma unroll
     for (int kq = 0; kq < DH / 64; ++kq) {
       uint32_t qa[4][4];
@@ -273,9 +271,9 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
         ldsm_x4(smem_u32(sm.q + swz<DH>(mt * 16 + (lane & 15), (kq * 4 + i) * 16 + (lane >> 4) * 8)), qa[i][0], qa[i][1],
                 qa[i][2], qa[i][3]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < NJ; ++j) {
         uint32_t c[4];
-        ldsm_x4(smem_u32(cK + chunk_at<DH, KT>(kw * kWarpKeys + j * 8 + (lane & 7), kq * 4 + (lane >> 3))), c[0], c[1], c[2],
+        ldsm_x4(smem_u32(cK + chunk_at<DH, KT>(kw * WK + j * 8 + (lane & 7), kq * 4 + (lane >> 3))), c[0], c[1], c[2],
                 c[3]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -287,12 +285,12 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     }
     // x = s + ev, the mask, and the online softmax in log2 units
     uint32_t vis = mine;
-    const int kp = base + kw * kWarpKeys + 2 * t4;
+    const int kp = base + kw * WK + 2 * t4;
     if (base + tile - 1 > own_lo || base + tile > k1 || base <= win_hi || shifting) {
       // positions at the sequence's end, at the rows' windows, or streams that shift from tile to tile
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int hf = i >> 3, p = kp + ((i >> 1) & 3) * 8 + (i & 1), pq = own_lo + rs_[hf];
+      for (int i = 0; i < 4 * NJ; ++i) {
+        const int hf = i / (2 * NJ), p = kp + ((i >> 1) % NJ) * 8 + (i & 1), pq = own_lo + rs_[hf];
         const bool in = p < k1 && p <= pq && (a.mode != SFA_LOCAL || p > pq - a.window) &&
                         (!shifting || p - fast_div(p, a.d_n) * a.n == rs_[hf]);
         if (!in) vis &= ~(1u << i);
@@ -300,14 +298,14 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
     }
     float tmax[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float4 sc = sm.scale[warp][j * 8 + 2 * t4 + e];
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
           const float x = fmaf(sacc[j][hf * 2 + e] * rowf[hf], sc.x, sc.y);
-          sacc[j][hf * 2 + e] = (vis >> (hf * 8 + j * 2 + e)) & 1u ? x : -INFINITY;
+          sacc[j][hf * 2 + e] = (vis >> (hf * 2 * NJ + j * 2 + e)) & 1u ? x : -INFINITY;
           tmax[hf] = fmaxf(tmax[hf], sacc[j][hf * 2 + e]);
         }
       }
@@ -323,7 +321,7 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
       ls[hf] *= corr[hf];
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float inv = sm.scale[warp][j * 8 + 2 * t4 + e].z;
@@ -343,15 +341,15 @@ __global__ void __launch_bounds__(Cfg<DH, WIDE>::kThreads, WIDE ? 1 : 2) decode_
         oacc[i][3] *= corr[1];
       }
     }
-    // O += P cv over this warp's 32 keys, 16 at a time
+    // O += P cv over this warp's keys, 16 at a time
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < NJ / 2; ++u) {
       const uint32_t pa[4] = {pack_f16(sacc[2 * u][0], sacc[2 * u][1]), pack_f16(sacc[2 * u][2], sacc[2 * u][3]),
                               pack_f16(sacc[2 * u + 1][0], sacc[2 * u + 1][1]), pack_f16(sacc[2 * u + 1][2], sacc[2 * u + 1][3])};
 #pragma unroll
       for (int c2 = 0; c2 < DC / 32; ++c2) {
         uint32_t r[4];
-        ldsm_x4_t(smem_u32(cV + chunk_at<DH, KT>(kw * kWarpKeys + u * 16 + (lane & 15), dw * (DC / 16) + c2 * 2 + (lane >> 4))),
+        ldsm_x4_t(smem_u32(cV + chunk_at<DH, KT>(kw * WK + u * 16 + (lane & 15), dw * (DC / 16) + c2 * 2 + (lane >> 4))),
                   r[0], r[1], r[2], r[3]);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -542,6 +540,9 @@ static long long q8_range(int maxT, int n, int mode, int window) {
   return mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1) : (long long)maxT * n;
 }
 
+// Positions of a tile.
+static int q8_tile(int Dh, int rg, bool tc) { return tc || Dh == 64 || (Dh == 128 && rg > 16) ? 128 : 64; }
+
 // Splits of a step on the tensor cores (`tc`) or not: the fewest waves times (tiles of a CTA + about two tiles' time to
 // start and end it), a combine kernel of about three tiles' time beside more than one split.  At most four waves of
 // CTAs, which bounds the workspace: `bound` gives the most that any smaller maxT or window takes.
@@ -551,14 +552,15 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
   p.M = n * p.G;
   p.ngroups = (p.M + decq8::kMaxRows - 1) / decq8::kMaxRows;
   p.rg = ((p.M + p.ngroups - 1) / p.ngroups + 15) / 16 * 16;
-  const int KT = !tc && Dh == 256 ? decq8::ktile<256>() : decq8::ktile<128>();
+  const int KT = q8_tile(Dh, p.rg, tc);
   const long long tiles = (q8_range(maxT, n, mode, window) + KT - 1) / KT, ctas = (long long)B * Hkv * p.ngroups;
-  int per_sm = tc ? decode_q8_tc_per_sm(p.rg, Dh) : p.rg > (Dh == 256 ? 16 : 32) ? 1 : Dh == 64 && p.rg == 16 ? 4 : 2;
+  int per_sm = tc ? decode_q8_tc_per_sm(p.rg, Dh) : p.rg > (Dh == 256 ? 16 : 32) ? 1 : Dh <= 128 && p.rg == 16 ? 4 : 2;
   // few tiles: fewer splits, which the combine kernel merges faster (1 x 8192 tokens, 4 streams, 32 over 8 heads of 128, 13
   // tiles an SM: two CTAs an SM 21.2 us, three 23.1; 8 x 2048, 27 tiles: 29.1 and 28.0; both before starts were shortened)
   if (tc && ctas * tiles < 20 * kSmCount) per_sm = std::min(per_sm, 2);
   const long long resident = (long long)kSmCount * per_sm;
   const long long most = std::min({tiles, (long long)dec::kMaxSplit, std::max(1LL, 4 * resident / ctas)});
+  const int small = Dh * KT < 128 * 128 ? 2 : 1;  // tiles of half the bytes: twice as many in the time of a start
   long long best = 1, best_cost = -1;
   if (bound) {
     best = most;
@@ -566,7 +568,7 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
     for (long long ns = 1; ns <= most; ++ns) {
       const long long per = (tiles + ns - 1) / ns, used = (tiles + per - 1) / per;
       if (used != ns) continue;  // another ns gives the same chunks
-      const long long cost = ((ctas * ns + resident - 1) / resident) * (per + 2) + (ns > 1 ? 3 : 0);
+      const long long cost = ((ctas * ns + resident - 1) / resident) * (per + 2 * small) + (ns > 1 ? 3 * small : 0);
       if (best_cost < 0 || cost < best_cost) {
         best = ns;
         best_cost = cost;
@@ -590,16 +592,18 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
 
 // Whether the tcgen05 kernel takes a step.  It reads tiles by TMA alone, in pieces of at least kTmaRows rows of a page that
 // start on 128 bytes of shared memory, and takes longer to start and end, so up to 16 query rows leave it short ranges.
-// Measured (replayed from a graph, us, tcgen05 / mma.sync, 4 streams but where said):
-//   32 over 8 heads of 128   33 x 12 tokens 12.2 / 10.0, 4 x 50 10.3 / 10.1, 4 x 150 10.6 / 11.8, 4 x 1000 16.3 / 17.4, 16 x 1000
-//                            26.7 / 41.0; one stream, 7 of up to 20000 40.4 / 67.2
-//   16 over 4 of 64          3 streams, 4 x 400 11.7 / 9.1, 4 x 3000 17.0 / 18.2
-//   24 over 2 of 256         4 x 50 12.9 / 23.8;  96 over 8 of 128: 16 x 50 11.8 / 15.1, 16 x 400 23.3 / 46.9
+// Measured (replayed from a graph, us, tcgen05 / mma.sync; sequences x tokens x streams):
+//   16 over 4 of 64     4 x 400 x 3 10.7 / 9.2, 33 x 700 x 3 22.8 / 19.5, 2 x 8192 x 1 13.2 / 9.3, 4 x 6000 x 3 21.2 / 20.5,
+//                       33 x 3000 x 3 43.8 / 46.7, 8 x 8192 x 3 33.0 / 33.3
+//   32 over 8 of 128    33 x 12 x 4 11.3 / 9.0, 4 x 25 x 4 7.5 / 8.6, 33 x 25 x 4 10.9 / 10.1, 4 x 50 x 4 9.1 / 10.5, 4 x 1000 x 4
+//                       16.3 / 18.6, 16 x 1000 x 4 26.9 / 39.2
+//   24 over 2 of 256    33 x 20 x 1 9.8 / 8.6, 4 x 400 x 1 12.9 / 9.5, 4 x 1000 x 1 9.8 / 9.8, 33 x 1000 x 1 15.1 / 18.2
+//   more than 16 rows   24 over 2 of 256, 4 x 50 x 4 12.9 / 23.8; 96 over 8 of 128, 16 x 50 x 4 11.8 / 15.1
 constexpr int kTmaRows = 8;
 static bool q8_tc(int Dh, int prow, int rows, long long range) {
   const int piece = paged_piece(prow, 128);
   if (piece < kTmaRows || (Dh == 64 && piece % 2 != 0)) return false;
-  return rows > 16 || range > (Dh == 64 ? 2048 : Dh == 128 ? 256 : 0);
+  return rows > 16 || range > (Dh == 64 ? 8192 : Dh == 128 ? 64 : 512);
 }
 
 size_t decode_paged_q8_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {
@@ -608,19 +612,20 @@ size_t decode_paged_q8_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh,
   return std::max(x, q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, true, true).bytes());
 }
 
-template <int DH, bool WIDE>
+template <int DH, int MT>
 static cudaError_t launch_q8_t(const decq8::Args& a, cudaStream_t st) {
   using namespace decq8;
-  const int smem = (int)sizeof(Smem<DH, WIDE>) + 1024;
-  static_assert(sizeof(Smem<DH, WIDE>) + 1024 <= (WIDE ? 227 : 113) * 1024, "an SM's CTAs fit");
-  cudaError_t e = cudaFuncSetAttribute(decode_q8_kernel<DH, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const int smem = (int)sizeof(Smem<DH, MT>) + 1024;
+  static_assert(Cfg<DH, MT>::kPerSm * (sizeof(Smem<DH, MT>) + 2048) <= 228 * 1024, "an SM's CTAs fit");
+  cudaError_t e = cudaFuncSetAttribute(decode_q8_kernel<DH, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(true, decode_q8_kernel<DH, WIDE>, dim3((unsigned)a.nsplit * a.B * a.Hkv * a.ngroups),
+  return launch_kernel(true, decode_q8_kernel<DH, MT>, dim3((unsigned)a.nsplit * a.B * a.Hkv * a.ngroups),
                        (unsigned)a.rg / 16 * 128, smem, st, a);
 }
-template <int DH>
-static cudaError_t launch_q8_d(const decq8::Args& a, cudaStream_t st) {
-  return a.rg > 16 * decq8::Cfg<DH, false>::MT ? launch_q8_t<DH, true>(a, st) : launch_q8_t<DH, false>(a, st);
+static cudaError_t launch_q8(const decq8::Args& a, int Dh, cudaStream_t st) {
+  if (Dh == 64) return a.rg <= 32 ? launch_q8_t<64, 2>(a, st) : launch_q8_t<64, 4>(a, st);
+  if (Dh == 256) return a.rg <= 16 ? launch_q8_t<256, 1>(a, st) : launch_q8_t<256, 4>(a, st);
+  return a.rg <= 16 ? launch_q8_t<128, 1>(a, st) : a.rg <= 32 ? launch_q8_t<128, 2>(a, st) : launch_q8_t<128, 4>(a, st);
 }
 
 static cudaError_t launch_combine_q8(const decq8::Args& a, int Dh, cudaStream_t st) {
@@ -677,7 +682,7 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   a.d_G = make_fast_div((uint32_t)plan.G);
   a.d_n = make_fast_div((uint32_t)n);
   a.d_heads = make_fast_div((uint32_t)(Hkv * plan.ngroups));
-  const int KT = !tc && Dh == 256 ? decq8::ktile<256>() : decq8::ktile<128>();
+  const int KT = q8_tile(Dh, plan.rg, tc);
   a.piece = paged_piece(a.pg.prow, KT);
   a.tile = tc ? KT / a.piece * a.piece : n <= KT ? KT / n * n : KT;  // whole pieces; whole tokens where a tile holds one
   a.d_tile = make_fast_div((uint32_t)a.tile);
@@ -686,10 +691,7 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
   if (tc && (!make_q8_tmap(&p.tm_k, kc, num_pages, Hkv, a.pg.prow, Dh, a.piece) ||
              !make_q8_tmap(&p.tm_v, vc, num_pages, Hkv, a.pg.prow, Dh, a.piece)))
     return cudaErrorInvalidValue;
-  const cudaError_t e = tc          ? launch_decode_q8_tc(p, Dh, st)
-                        : Dh == 64  ? launch_q8_d<64>(a, st)
-                        : Dh == 128 ? launch_q8_d<128>(a, st)
-                                    : launch_q8_d<256>(a, st);
+  const cudaError_t e = tc ? launch_decode_q8_tc(p, Dh, st) : launch_q8(a, Dh, st);
   return e != cudaSuccess || (a.nsplit == 1 && !a.balanced) ? e : launch_combine_q8(a, Dh, st);
 }
 
