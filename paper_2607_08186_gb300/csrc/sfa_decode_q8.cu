@@ -39,7 +39,7 @@ constexpr int kMaxRows = 64;         // query rows of a CTA at most (four row ti
 // CTAs an SM while the queries leave room for three stages each: up to two row tiles, one at head dim 256; with four row
 // tiles one.  At head dim 128 a single row tile leaves eight warps an SM so, so its warps take 16 positions of a tile and not
 // 32, and four CTAs fit (pages of one token, 4 x 4000 tokens, 32 over 8 heads: 48.6 us
-// for 41.3); at 64 four fit as it is.
+// for 41.3); at 64 three fit as it is.
 template <int DH, int MT_>
 struct Cfg {
   static constexpr int MT = MT_, WK = DH == 128 && MT == 1 ? 16 : 32;             // positions of a tile that a warp takes
@@ -554,7 +554,7 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
   p.rg = ((p.M + p.ngroups - 1) / p.ngroups + 15) / 16 * 16;
   const int KT = q8_tile(Dh, p.rg, tc);
   const long long tiles = (q8_range(maxT, n, mode, window) + KT - 1) / KT, ctas = (long long)B * Hkv * p.ngroups;
-  int per_sm = tc ? decode_q8_tc_per_sm(p.rg, Dh) : p.rg > (Dh == 256 ? 16 : 32) ? 1 : Dh <= 128 && p.rg == 16 ? 4 : 2;
+  int per_sm = tc ? decode_q8_tc_per_sm(p.rg, Dh) : p.rg > (Dh == 256 ? 16 : 32) ? 1 : p.rg > 16 || Dh == 256 ? 2 : Dh == 64 ? 3 : 4;
   // few tiles: fewer splits, which the combine kernel merges faster (1 x 8192 tokens, 4 streams, 32 over 8 heads of 128, 13
   // tiles an SM: two CTAs an SM 21.2 us, three 23.1; 8 x 2048, 27 tiles: 29.1 and 28.0; both before starts were shortened)
   if (tc && ctas * tiles < 20 * kSmCount) per_sm = std::min(per_sm, 2);
@@ -591,19 +591,20 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
 }
 
 // Whether the tcgen05 kernel takes a step.  It reads tiles by TMA alone, in pieces of at least kTmaRows rows of a page that
-// start on 128 bytes of shared memory, and takes longer to start and end, so up to 16 query rows leave it short ranges.
+// start on 128 bytes of shared memory, and takes longer to start and end, so up to 16 query rows leave it short ranges; at
+// head dim 64, where a tile has half the bytes for the same softmax, all but a million positions over the heads.
 // Measured (replayed from a graph, us, tcgen05 / mma.sync; sequences x tokens x streams):
-//   16 over 4 of 64     4 x 400 x 3 10.7 / 9.2, 33 x 700 x 3 22.8 / 19.5, 2 x 8192 x 1 13.2 / 9.3, 4 x 6000 x 3 21.2 / 20.5,
-//                       33 x 3000 x 3 43.8 / 46.7, 8 x 8192 x 3 33.0 / 33.3
+//   16 over 4 of 64     4 x 400 x 3 10.8 / 9.2, 33 x 700 x 3 22.6 / 16.3, 2 x 8192 x 1 13.2 / 10.1, 4 x 6000 x 3 21.4 / 16.9, 8 x
+//                       8192 x 3 32.8 / 30.9, 33 x 3000 x 3 (1.2 M positions of a head) 43.7 / 44.2, 100 x 3000 x 3 93 / 119
 //   32 over 8 of 128    33 x 12 x 4 11.3 / 9.0, 4 x 25 x 4 7.5 / 8.6, 33 x 25 x 4 10.9 / 10.1, 4 x 50 x 4 9.1 / 10.5, 4 x 1000 x 4
 //                       16.3 / 18.6, 16 x 1000 x 4 26.9 / 39.2
 //   24 over 2 of 256    33 x 20 x 1 9.8 / 8.6, 4 x 400 x 1 12.9 / 9.5, 4 x 1000 x 1 9.8 / 9.8, 33 x 1000 x 1 15.1 / 18.2
 //   more than 16 rows   24 over 2 of 256, 4 x 50 x 4 12.9 / 23.8; 96 over 8 of 128, 16 x 50 x 4 11.8 / 15.1
 constexpr int kTmaRows = 8;
-static bool q8_tc(int Dh, int prow, int rows, long long range) {
+static bool q8_tc(int Dh, int prow, int rows, long long range, long long heads) {
   const int piece = paged_piece(prow, 128);
   if (piece < kTmaRows || (Dh == 64 && piece % 2 != 0)) return false;
-  return rows > 16 || range > (Dh == 64 ? 8192 : Dh == 128 ? 64 : 512);
+  return rows > 16 || (Dh == 64 ? range * heads > 1 << 20 : range > (Dh == 128 ? 64 : 512));
 }
 
 size_t decode_paged_q8_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {
@@ -643,7 +644,7 @@ cudaError_t launch_sfa_decode_paged_q8(const void* q, const void* kc, const void
                                        float scale, int mode, int window, void* ws, size_t ws_bytes, int32_t* status,
                                        cudaStream_t st) {
   const long long range = q8_range(maxT, n, mode, window);
-  const bool tc = q8_tc(Dh, P * n, n * (Hq / Hkv), range);
+  const bool tc = q8_tc(Dh, P * n, n * (Hq / Hkv), range, (long long)B * Hkv);
   const Q8Plan plan = q8_plan(B, maxT, n, Hq, Hkv, Dh, mode, window, tc, false);
   if (plan.bytes() > ws_bytes) return cudaErrorInvalidValue;  // the bound says that it is not
   decq8::Params p = {};

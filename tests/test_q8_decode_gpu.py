@@ -147,7 +147,8 @@ def test_scores_that_change(shape, B, n, Hq, Hkv, Dh, P, T, L):
 @pytest.mark.parametrize("B,n,Hq,Hkv,Dh,P,T", [(132, 1, 8, 4, 64, 48, 1), (132, 1, 8, 4, 64, 16, 16), (100, 4, 12, 3, 128, 12, 1),
                                                (60, 1, 9, 9, 128, 24, 1), (12, 4, 32, 8, 128, 16, 16), (24, 2, 48, 8, 128, 15, 1),
                                                (128, 1, 12, 3, 256, 9, 9), (20, 4, 48, 1, 256, 10, 5), (9, 8, 72, 3, 128, 11, 11),
-                                               (20, 8, 8, 4, 64, 6, 1), (40, 8, 4, 2, 64, 2, 2)])
+                                               (20, 8, 8, 4, 64, 6, 1), (100, 8, 8, 4, 64, 6, 1),
+                                               (132, 8, 4, 2, 64, 2, 2)])
 def test_long_sequences_in_numbers(B, n, Hq, Hkv, Dh, P, T):
     L = 1500
     q, kc, vc = _case(2, L, n, Hq, Hkv, Dh, B + P)
