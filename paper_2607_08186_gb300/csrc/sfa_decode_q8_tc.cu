@@ -24,8 +24,8 @@
 // brings the scales 384 blocks ahead, since a load behind a saturated memory's queue takes thousands of cycles.
 //
 // A batch of long sequences is one wave of CTAs, each with an equal share of all tiles (Work), because a CTA takes about
-// 12000 cycles to start and 4000 to end, six tiles' time: 8 x 8192 tokens, 96 over 8 heads of 128, 122 us with three waves
-// of splits and 101 so.
+// 12000 cycles to start and 4000 to end, six to eight tiles' time: 8 x 8192 tokens, 96 over 8 heads of 128, 122 us with
+// three waves of splits and 101 so.
 //
 // Bound by memory at 16 query rows, of 8 heads of 128: 16 sequences of 32768 tokens, 32 over 8 heads, 390 to 397 us (6.9
 // TB/s of codes and scales; 400 at the copy rate), 8 of up to 16384 112 for 103.  With more rows by the softmax warps'
@@ -430,7 +430,8 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ the products
-    constexpr uint32_t idS = C::kPair ? idesc_f8(128, 2 * R, 0, 0, 0, 0) : idesc_f8(128, R, 0, 1, 0, 0), idO = idesc_f8(RB, 3 * R, 0, 1, 1, 1);
+    constexpr uint32_t idS = C::kPair ? idesc_f8(128, 2 * R, 0, 0, 0, 0) : idesc_f8(128, R, 0, 1, 0, 0);
+    constexpr uint32_t idO = idesc_f8(RB, 3 * R, 0, 1, 1, 1);
     const uint64_t kd = sdesc_rows<RB>(smem_u32(sm.ring[0])), qd = sdesc_rows<RB>(smem_u32(sm.q[0][0]));
     const uint64_t pd = sdesc_plain_mn(smem_u32(sm.p[0][0]), 128, KT * 16);
     int slot = 0, lap = 0, done = 0, seq = 0;  // done: tiles of the sequences before
