@@ -11,6 +11,27 @@ using dec::kBadPage;
 
 constexpr uint32_t kNoRow = 0xffffffffu;
 
+// The softmax's sum counts P 2^-ev, and P is 2^(s + ev - m).  Where ev lies far below the largest that m has met, P leaves
+// fp32's range before 2^-ev would bring it back (a block of zeros has ev = -64 whatever its neighbours hold), although
+// the weight 2^s may count.  So from kFarSum binary orders on the partial's rows are computed again by exact_row.  (Up to
+// there, what is flushed to 0, P < 2^-126, is a weight of less than 2^-35 of the row's largest.)
+constexpr int kFarSum = 96;
+
+// The exponent of a partial's sum l, by which the partial is divided: l is a sum of P 2^-ev and P is relative to m, which
+// counts ev, so between partials whose ev lie far apart the factors 2^(m - m') would leave fp32's range where the weights'
+// do not.  Divided so, m is the logarithm of the partial's weight, to a binary order, and l lies in [1, 2).
+HD_DEVINLINE int sum_exponent(float l) {
+  const int e = (__float_as_int(l) >> 23) - 127;
+  return l >= 1.17549435e-38f && e < 127 ? e : 0;  // (0, NaN and infinity as they are)
+}
+HD_DEVINLINE float two_to_minus(int e) { return __int_as_float((127 - e) << 23); }
+// sum += x, the rounding error of the sum so far in `err` (Kahan).
+HD_DEVINLINE void add_exactly(float& sum, float& err, float x) {
+  const float y = x - err, t = sum + y;
+  err = (t - sum) - y;
+  sum = t;
+}
+
 struct Args : DecodeArgs {
   const uint8_t *kcodes, *vcodes, *kscale, *vscale;
   int blocks;       // blocks of a page
@@ -36,10 +57,11 @@ HD_DEVINLINE uint32_t row_at(const Args& a, const int32_t* table, int g, int p, 
 }
 
 // A row's partial over the visible positions of [k0, k1), by one warp on the fp32 units: lane i holds DH/32 columns.
-// Only visible rows are read: what a hidden NaN has made of the products' row is not.
+// Only visible rows are read: what a hidden NaN has made of the products' row is not.  The sums lose nothing of many small
+// weights beside a large one; four positions' loads are in flight.
 template <int DH>
 __device__ __noinline__ void exact_row(const Args& a, int b, int g, int r, int T, int k0, int k1, float* po, float2* pml) {
-  constexpr int C = DH / 32;
+  constexpr int C = DH / 32, NP = 4;
   const int lane = threadIdx.x & 31, s = r / a.G, h = g * a.G + r % a.G, pq = (T - 1) * a.n + s;
   const int32_t* table = a.table + (long long)b * a.pg.max_pages;
   int p = a.mode == SFA_LOCAL ? max(k0, pq - a.window + 1) : k0, step = 1;
@@ -49,31 +71,48 @@ __device__ __noinline__ void exact_row(const Args& a, int b, int g, int r, int T
   }
   const int end = min(k1, pq + 1);
   const bf16* q = a.q + (((long long)b * a.n + s) * a.Hq + h) * DH + lane * C;
-  float qf[C], o[C], m = -INFINITY, l = 0.f;
+  float qf[C], o[C], oe[C], m = -INFINITY, l = 0.f, le = 0.f;
 #pragma unroll
-  for (int c = 0; c < C; ++c) qf[c] = __bfloat162float(q[c]), o[c] = 0.f;
-  for (; p < end; p += step) {
-    size_t sc = 0;
-    const uint32_t row = row_at(a, table, g, p, &sc);
-    if (row == kNoRow) continue;
-    const size_t at = (size_t)row * DH;
-    float x = 0.f, v[C];
+  for (int c = 0; c < C; ++c) qf[c] = __bfloat162float(q[c]), o[c] = oe[c] = 0.f;
+  for (; p < end; p += NP * step) {
+    float x[NP], v[NP][C];
+    bool in[NP];
 #pragma unroll
-    for (int c = 0; c < C; c += 2) {
-      const float2 kv = q8::values2(*reinterpret_cast<const uint16_t*>(a.kcodes + at + lane * C + c));
-      const float2 vv = q8::values2(*reinterpret_cast<const uint16_t*>(a.vcodes + at + lane * C + c));
-      x += qf[c] * kv.x + qf[c + 1] * kv.y;
-      v[c] = vv.x, v[c + 1] = vv.y;
+    for (int e = 0; e < NP; ++e) {
+      const int at_p = p + e * step;
+      size_t sc = 0;
+      const uint32_t row = at_p < end ? row_at(a, table, g, at_p, &sc) : kNoRow;
+      in[e] = row != kNoRow;
+      x[e] = 0.f;
+      if (!in[e]) continue;
+      const size_t at = (size_t)row * DH;
+      const float fk = q8::scale_of(q8::clamp_byte(a.kscale[sc])), fv = q8::scale_of(q8::clamp_byte(a.vscale[sc]));
+#pragma unroll
+      for (int c = 0; c < C; c += 2) {
+        const float2 kv = q8::values2(*reinterpret_cast<const uint16_t*>(a.kcodes + at + lane * C + c));
+        const float2 vv = q8::values2(*reinterpret_cast<const uint16_t*>(a.vcodes + at + lane * C + c));
+        x[e] += qf[c] * kv.x + qf[c + 1] * kv.y;
+        v[e][c] = vv.x * fv, v[e][c + 1] = vv.y * fv;
+      }
+      x[e] *= a.scale_log2 * fk;
     }
 #pragma unroll
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    x *= a.scale_log2 * q8::scale_of(q8::clamp_byte(a.kscale[sc]));
-    const float fv = q8::scale_of(q8::clamp_byte(a.vscale[sc]));
-    const float mn = fmaxf(m, x), mu = mn == -INFINITY ? 0.f : mn, corr = exp2f(m - mu), w = exp2f(x - mu);
-    m = mn;
-    l = l * corr + w;
+    for (int d = 16; d; d >>= 1)
 #pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = o[c] * corr + w * (v[c] * fv);
+      for (int e = 0; e < NP; ++e) x[e] += __shfl_xor_sync(0xffffffffu, x[e], d);
+#pragma unroll
+    for (int e = 0; e < NP; ++e) {
+      if (!in[e]) continue;
+      const float mn = fmaxf(m, x[e]), mu = mn == -INFINITY ? 0.f : mn, corr = exp2f(m - mu), w = exp2f(x[e] - mu);
+      m = mn;
+      l *= corr, le *= corr;
+      add_exactly(l, le, w);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        o[c] *= corr, oe[c] *= corr;
+        add_exactly(o[c], oe[c], w * v[e][c]);
+      }
+    }
   }
   if (l != l) m = INFINITY;
 #pragma unroll

@@ -7,7 +7,8 @@
 // exponent: with x_p = s_p + ev_p and m the running maximum of x (not of s), P_p = 2^(x_p - m + 15) is at most 2^15, f16
 // holds it to 2^-12 down to 2^-29 of the largest contribution (2^-40 as a subnormal), and
 //   o = sum P_p cv_p / sum P_p 2^(-ev_p):
-// the sum's terms are one fused multiply-add each.  As e lies in [-64, 50], no term that counts leaves fp32's range.  The
+// the sum's terms are one fused multiply-add each.  Where V's scales lie so far apart that a term leaves fp32's range although
+// its weight counts (kFarSum), the rows are computed again, a position at a time (exact_row).  The
 // queries are scaled by a power of two for each row, so that f16 holds them as bf16 did (a row's largest to 2^15; values
 // 2^-39 below it lose bits).
 //
@@ -59,7 +60,8 @@ struct Smem {
   float4 scale[C::kWarps][C::WK];   // a warp's keys: 2^ek, ev, 2^-ev
   float qscale[C::MT * 16];
   uint32_t row[4][C::KT];               // rows of the pool (kNoRow: none) of four tiles
-  unsigned not_finite[2];               // a bit for each row of the merged partial
+  unsigned again[2];                    // rows of the merged partial (bits) that are not finite, which exact_row computes,
+  int far;                              // and whether it computes all of them: V's scales lie far apart
   int bad_page;
 };
 
@@ -111,7 +113,8 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
   const int tile = a.tile;
   if (tid == 0) {
     sm.bad_page = 0;
-    sm.not_finite[0] = sm.not_finite[1] = 0;
+    sm.again[0] = sm.again[1] = 0;
+    sm.far = 0;
   }
   // this thread's query rows g4 and g4 + 8 of the row tile: their streams (-1: padding).  Where n divides a tile, which
   // of this thread's keys are of a row's stream is the same in every tile.
@@ -183,7 +186,8 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
     at_row += step_rows;
     if (at_row >= a.pg.prow) at_row -= a.pg.prow, ++at_page;
   };
-  int kb = 127, vb = 127;
+  int kb = 127, vb = -1;
+  unsigned ends = 0;  // V's largest so far << 16, and 255 less its smallest
   auto scale_bytes = [&] {
     if ((unsigned)next_entry < (unsigned)a.pg.num_pages) {
       const size_t at = ((size_t)next_entry * a.Hkv + g) * a.blocks + fast_div(next_row_in, a.d_brow);
@@ -242,12 +246,17 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
 #pragma unroll
   for (int i = 0; i < DC / 8; ++i) oacc[i][0] = oacc[i][1] = oacc[i][2] = oacc[i][3] = 0.f;
 
+  {  // a lane without a key holds another's byte, so that it does not count as one of its own
+    const int some = __reduce_max_sync(0xffffffffu, vb);
+    if (vb < 0) vb = some < 0 ? 127 : some;
+  }
   for (int it = 0, st = 0; it < nsub; ++it) {
     const int base = k0 + it * tile;
     // this tile's scales into shared memory, the next ones' loads on their way
     {
       kb = q8::clamp_byte(kb);
       vb = q8::clamp_byte(vb);
+      ends = __vmaxu2(ends, (unsigned)vb << 16 | (unsigned)(255 - vb));
       if (lane < WK) sm.scale[warp][lane] = make_float4(q8::scale_of(kb), (float)(vb - 127), q8::inverse_of(vb), 0.f);
       scale_bytes();
       scale_entry();
@@ -315,10 +324,22 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
       tmax[hf] = fmaxf(tmax[hf], __shfl_xor_sync(0xffffffffu, tmax[hf], 1));
       tmax[hf] = fmaxf(tmax[hf], __shfl_xor_sync(0xffffffffu, tmax[hf], 2));
       const float mnew = fmaxf(mx[hf], tmax[hf]), mu = mnew == -INFINITY ? 0.f : mnew;
-      corr[hf] = ex2_approx(mx[hf] - mu);
+      corr[hf] = ex2_approx(0.5f * (mx[hf] - mu));  // (the root: the sum's range is wider than a power's)
       msub[hf] = mu - kShift;
       mx[hf] = mnew;
-      ls[hf] *= corr[hf];
+    }
+    if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+      ls[0] = ls[0] * corr[0] * corr[0];
+      ls[1] = ls[1] * corr[1] * corr[1];
+      corr[0] *= corr[0];
+      corr[1] *= corr[1];
+#pragma unroll
+      for (int i = 0; i < DC / 8; ++i) {
+        oacc[i][0] *= corr[0];
+        oacc[i][1] *= corr[0];
+        oacc[i][2] *= corr[1];
+        oacc[i][3] *= corr[1];
+      }
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
@@ -332,15 +353,6 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
           ls[hf] = fmaf(p, inv, ls[hf]);
         }
       }
-    if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
-#pragma unroll
-      for (int i = 0; i < DC / 8; ++i) {
-        oacc[i][0] *= corr[0];
-        oacc[i][1] *= corr[0];
-        oacc[i][2] *= corr[1];
-        oacc[i][3] *= corr[1];
-      }
-    }
     // O += P cv over this warp's keys, 16 at a time
 #pragma unroll
     for (int u = 0; u < NJ / 2; ++u) {
@@ -367,10 +379,14 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
     if (++st == STAGES) st = 0;
   }
   cp_async_wait<0>();
+  {
+    const int most = (int)__reduce_max_sync(0xffffffffu, ends >> 16), least = 255 - (int)__reduce_max_sync(0xffffffffu, ends & 0xffff);
+    if (most > least + kFarSum) sm.far = 1;
+  }
   __syncthreads();
 
-  // merge the key groups' partials in shared memory (the ring is free now): [KW][R][DH], then the running maxima (in
-  // the partials' units, where P is at most 2^15) and sums
+  // merge the key groups' partials in shared memory (the ring is free now): [KW][R][DH], then what the sums count
+  // from, and the sums, each partial divided by its sum's power of two
   static_assert((KW * C::kMergeRows * DH + 2 * KW * C::kMergeRows) * 4 <= 2 * STAGES * KT * DH, "merge fits the ring");
   static_assert(kMaxRows <= 128, "one thread per row");
   float* sO = reinterpret_cast<float*>(sm.k[0]);
@@ -380,15 +396,16 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
   for (int hf = 0; hf < 2; ++hf) {
     ls[hf] += __shfl_xor_sync(0xffffffffu, ls[hf], 1);
     ls[hf] += __shfl_xor_sync(0xffffffffu, ls[hf], 2);
-    const int row = kw * R + mt * 16 + g4 + 8 * hf;
+    const int row = kw * R + mt * 16 + g4 + 8 * hf, k = sum_exponent(ls[hf]);
+    const float f = two_to_minus(k);
     if (t4 == 0 && dw == 0) {
-      sM[row] = mx[hf] - kShift;
-      sL[row] = ls[hf];
+      sM[row] = mx[hf] - kShift + (float)k;
+      sL[row] = ls[hf] * f;
     }
 #pragma unroll
     for (int c = 0; c < DC / 16; ++c)
-      *reinterpret_cast<float4*>(sO + row * DH + dw * DC + c * 16 + 4 * t4) =
-          make_float4(oacc[2 * c][2 * hf], oacc[2 * c + 1][2 * hf], oacc[2 * c][2 * hf + 1], oacc[2 * c + 1][2 * hf + 1]);
+      *reinterpret_cast<float4*>(sO + row * DH + dw * DC + c * 16 + 4 * t4) = make_float4(
+          oacc[2 * c][2 * hf] * f, oacc[2 * c + 1][2 * hf] * f, oacc[2 * c][2 * hf + 1] * f, oacc[2 * c + 1][2 * hf + 1] * f);
   }
   __syncthreads();
   const bool bad = sm.bad_page != 0;
@@ -420,15 +437,15 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
       o.w += f * v.w;
     }
     *reinterpret_cast<float4*>(po + row * DH + c4 * 4) = o;
-    if (!(fabsf(o.x) + fabsf(o.y) + fabsf(o.z) + fabsf(o.w) <= FLT_MAX)) atomicOr(&sm.not_finite[row >> 5], 1u << (row & 31));
+    if (!(fabsf(o.x) + fabsf(o.y) + fabsf(o.z) + fabsf(o.w) <= FLT_MAX)) atomicOr(&sm.again[row >> 5], 1u << (row & 31));
   }
   __syncthreads();
   if (!bad)
 #pragma unroll
     for (int half = 0; half < 2; ++half)
-      for (unsigned rows = sm.not_finite[half]; rows; rows &= rows - 1) {
+      for (unsigned rows = sm.far ? 0xffffffffu : sm.again[half]; rows; rows &= rows - 1) {
         const int row = half * 32 + __ffs(rows) - 1;
-        if (row % W == warp && rg * R + row < a.M)
+        if (row % W == warp && row < R && rg * R + row < a.M)
           exact_row<DH>(a, b, g, rg * R + row, T, k0, k1, po + row * DH, pml + row);
       }
   if (a.nsplit > 1) return;

@@ -86,13 +86,13 @@ struct Smem {
   int entry[4][128];                         // its page entry
   uint16_t scale[8 * 128];                   // blocks' scale bytes, K's and V's above it
   float rowf[C::R];                          // a row's factor of q
-  float nref[4][C::R];                       // its reference, negated: a copy for each warp of the group
-  float most[4][C::R];                       // a warp's maxima, or sums
+  float nref[4][C::R];                       // its reference, negated: a copy for each warp of the group; its sums at last
+  float most[4][C::R];                       // a warp's maxima
   uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], sc_full[8], q_full, drain;
-  unsigned raise[4 * WG];                    // a warp's rows whose references go up; kGaveUp
+  unsigned raise[4 * WG];                    // a warp's rows whose references go up, its largest scale byte << 16; kGaveUp
   uint32_t tmem_base;
-  unsigned not_finite[2];                    // rows of O; whether a row is kRedo
-  int redo;
+  unsigned again[2];                         // rows of O that exact_row computes (kRedo): not finite, or a group's, with
+  int redo;                                  // V's scales far apart; whether there are any
   int abort, bad_page[16];                   // of the sequence with this number, mod 16 (the ring holds fewer)
 };
 
@@ -128,7 +128,7 @@ HD_DEVINLINE void mma_f8_ss_w(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, u
       " @e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accum));
 }
-// This warp's 32 lanes of N columns of tensor memory, STEP apart, times f.
+// This warp's 32 lanes of N columns of tensor memory, STEP apart, times f twice.
 template <int N, int STEP>
 HD_DEVINLINE void tmem_scale(uint32_t taddr, float f) {
   float x[N];
@@ -138,7 +138,7 @@ HD_DEVINLINE void tmem_scale(uint32_t taddr, float f) {
   tmem_ld_wait();
 #pragma unroll
   for (int i = 0; i < N; ++i)
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};\n" ::"r"(taddr + i * STEP), "f"(x[i] * f) : "memory");
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};\n" ::"r"(taddr + i * STEP), "f"(x[i] * f * f) : "memory");
 }
 // Whether `v` holds for a thread of the 128 on hardware barrier `id`.
 HD_DEVINLINE bool group_any(int id, bool v) {
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
     mbar_init(&sm.q_full, 4 * WG);
     mbar_init(&sm.drain, 1);
     sm.abort = 0;
-    sm.not_finite[0] = sm.not_finite[1] = sm.redo = 0;
+    sm.again[0] = sm.again[1] = sm.redo = 0;
     fence_mbar_init();
   }
   if (warp == 0) {
@@ -627,6 +627,7 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
 #pragma unroll
       for (int r = 0; r < RW / 2; ++r) l[r] = 0;
       uint32_t set = 0;  // rows whose reference is set
+      int top_vb = 0;    // V's largest scale byte in the tiles that set references: no row's sum is below 2^kSet 2^-ev of it
       const int brow = a.pg.prow / a.blocks;
       int waited = 0;                               // chunks that this warp has waited for
       long long scales_end = (long long)b0 * brow;  // the first position behind them
@@ -705,25 +706,34 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
             if (lane == r) m = from_ordered(x);
           }
           mask = __reduce_or_sync(0xffffffffu, mask | (ok ? 0 : kGaveUp));
+          const unsigned top = __reduce_max_sync(0xffffffffu, vis != 0 ? (unsigned)vb : 0u);
           if (lane < RW) sm.most[q4][r0 + lane] = m;
-          if (lane == 0) sm.raise[wg * 4 + q4] = mask;
+          if (lane == 0) sm.raise[wg * 4 + q4] = mask | top << 16;
           named_bar_sync(bar, 128);  // (the next vote lies before these are written again)
-          mask = (sm.raise[wg * 4] | sm.raise[wg * 4 + 1]) | (sm.raise[wg * 4 + 2] | sm.raise[wg * 4 + 3]);
+          mask = 0;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const unsigned x = sm.raise[wg * 4 + w];
+            mask |= x & (0xffffu | kGaveUp);
+            top_vb = max(top_vb, (int)(x >> 16 & 255));
+          }
           if (mask & kGaveUp) {
             ok = false;
             break;
           }
-          float down = 0.f, fac = 1.f;  // lane r: what row r's reference goes up by, negated; 2^ that
+          float down = 0.f, fac = 1.f;  // lane r: what row r's reference goes up by, negated; the root of 2^ that (a sum's
+                                        // range is wider than a power's)
           if (lane < RW && (mask >> lane & 1u)) {
             const int r = r0 + lane;
             down = kSet - fmaxf(fmaxf(sm.most[0][r], sm.most[1][r]), fmaxf(sm.most[2][r], sm.most[3][r]));
             sm.nref[q4][r] += down;
-            if (set >> lane & 1u) fac = ex2_approx(down);
+            if (set >> lane & 1u) fac = ex2_approx(0.5f * down);
           }
           __syncwarp();
 #pragma unroll
           for (int r = 0; r < RW; r += 2) {
-            l[r / 2] = fmul2(l[r / 2], f2pack(__shfl_sync(0xffffffffu, fac, r), __shfl_sync(0xffffffffu, fac, r + 1)));
+            const uint64_t root = f2pack(__shfl_sync(0xffffffffu, fac, r), __shfl_sync(0xffffffffu, fac, r + 1));
+            l[r / 2] = fmul2(fmul2(l[r / 2], root), root);
             y[r] += __shfl_sync(0xffffffffu, down, r);
             y[r + 1] += __shfl_sync(0xffffffffu, down, r + 1);
           }
@@ -740,6 +750,8 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
           set |= mask;
         }
         if (!ok) continue;
+        if (vis != 0 && vb + decq8::kFarSum < top_vb) atomicOr(&sm.again[r0 >> 5], 0xffffu << (r0 & 31));
+        __syncwarp();
         // S of this tile was issued behind the products of the tile before the last, so these are done: P's buffer is free
         const uint64_t inv2 = f2pack(inv, inv);
         {
@@ -797,10 +809,19 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
         for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
         if (lane == r) sum = x;
       }
+      // (this warp's references are its own to write over)
+      const float ref = lane < RW ? sm.nref[q4][r0 + lane] : 0.f;
+      if (lane < RW) sm.nref[q4][r0 + lane] = sum;
       ok = ok && __all_sync(0xffffffffu, mbar_wait(&sm.pv_done[(done + nt - 1) & 1], ((done + nt - 1) >> 1) & 1, abort, a.status));
-      if (group_any(bar, !ok)) ok = false;  // (also: every warp has read the last maxima)
+      if (group_any(bar, !ok)) ok = false;  // (also: every warp's sums are written)
       if (ok) {
-        if (lane < RW) sm.most[q4][r0 + lane] = sum;
+        int k = 0;  // lane r: the exponent of row r's sum, by which its partial is divided
+        if (lane < RW) {
+          const int r = r0 + lane;
+          sum = (sm.nref[0][r] + sm.nref[1][r]) + (sm.nref[2][r] + sm.nref[3][r]);
+          k = decq8::sum_exponent(sum);
+        }
+        const float part = decq8::two_to_minus(k);
         tc_fence_after();
         const bool bad = *(volatile int*)&sm.bad_page[seq & 15] != 0;
         // this lane's row of O^T: all 128, or (a product of 64 rows) 16 of each 32
@@ -814,23 +835,24 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
           uint32_t wrong = 0;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float x = fmaf(__uint_as_float(o[2][e]), 1.f / kLow, __uint_as_float(o[0][e]) + __uint_as_float(o[1][e]));
+            const float x = fmaf(__uint_as_float(o[2][e]), 1.f / kLow, __uint_as_float(o[0][e]) + __uint_as_float(o[1][e])) *
+                            __shfl_sync(0xffffffffu, part, e);
             if (column < 0) continue;
             po[(size_t)(r0 + e) * DH + hf * RB + column] = x;
             if (!(fabsf(x) <= FLT_MAX)) wrong |= 1u << e;
           }
           wrong = __reduce_or_sync(0xffffffffu, wrong);
-          if (wrong != 0 && lane == 0) atomicOr(&sm.not_finite[r0 >> 5], wrong << (r0 & 31));
+          if (wrong != 0 && lane == 0) atomicOr(&sm.again[r0 >> 5], wrong << (r0 & 31));
         }
         named_bar_sync(bar, 128);
         if (key < RW) {
           const int r = r0 + key;
-          sum = (sm.most[0][r] + sm.most[1][r]) + (sm.most[2][r] + sm.most[3][r]);
-          float m = (set >> key) & 1u ? -sm.nref[0][r] : -INFINITY;
+          sum *= part;
+          float m = (set >> key) & 1u ? (float)k - ref : -INFINITY;
           if (sum != sum) m = INFINITY;  // a visible score that is not finite: the combined row is NaN
           if (bad) {
             m = -INFINITY, sum = decq8::kBadPage;
-          } else if (r < rows && sm.not_finite[r >> 5] >> (r & 31) & 1u) {
+          } else if (r < rows && sm.again[r >> 5] >> (r & 31) & 1u) {
             sum = kRedo;
             sm.redo = 1;
           }
@@ -838,7 +860,7 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
           if (!SHARED && a.nsplit == 1 && bad && key == 0) set_status(a.status, HD_DEVBIT_INDEX);
         }
         named_bar_sync(bar, 128);
-        if (key == 0) atomicAnd(&sm.not_finite[r0 >> 5], ~(0xffffu << (r0 & 31)));
+        if (key == 0) atomicAnd(&sm.again[r0 >> 5], ~(0xffffu << (r0 & 31)));
       }
       done += nt;
       chunks += waited;

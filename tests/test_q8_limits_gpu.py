@@ -1,0 +1,108 @@
+"""Decoding over the 8-bit paged cache where values lie far apart: V's scales, a row's weights, the queries' values.
+Against the 64-bit oracle on the values that the codes stand for.
+
+Caches here are a few kinds of pages, which a table names over and over, so that many positions stay small.  Tolerance:
+test_q8_decode_gpu's."""
+import pytest
+import torch
+
+import oracle
+import q8
+from paper_2607_08186_gb300 import binding, build, inputs
+from test_q8_decode_gpu import _assert_rows, _decode, _i32
+
+pytestmark = pytest.mark.gpu
+
+WITHIN, CROSS, LOCAL = inputs.WITHIN, inputs.CROSS, inputs.LOCAL
+F8, BF = torch.float8_e4m3fn, torch.bfloat16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build.build()
+
+
+def _codes(x):
+    """Values to the nearest codes, as values."""
+    return q8.nearest(x.clamp(-448, 448))
+
+
+def _cache(kinds, order, n, P):
+    """Pages of the kinds [(K codes' values [Hkv][P*n][Dh], its exponent, V's, its exponent)], a scale a page, and the
+    table row that names them in this order: (k, v, ks, vs, table [1][pages], K's values, V's)."""
+    table = torch.tensor([order], dtype=torch.int32)
+    out = []
+    for i in (0, 2):
+        codes = torch.stack([_codes(k[i]) for k in kinds])
+        scales = torch.tensor([k[i + 1] + q8.BIAS for k in kinds], dtype=torch.uint8)[:, None, None]
+        scales = scales.expand(-1, codes.shape[1], 1).contiguous()
+        codes = codes.float().to(F8)
+        pages, Hkv, _, Dh = codes.shape
+        values = q8.Cache(pages, P, n, Hkv, Dh, P, codes, scales).rows(order, len(order) * P).to(BF)[None]
+        out.append((codes, scales, values))
+    return out[0][0], out[1][0], out[0][1], out[1][1], table, out[0][2], out[1][2]
+
+
+def _normal(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+
+
+def _order(where, one, other, pages):
+    """Page kind `one` once among `pages` of `other`: first, last or in the middle."""
+    order = [other] * pages
+    order[{"first": 0, "last": -1, "middle": pages // 2}[where]] = one
+    return order
+
+
+def _signs(Dh):
+    return torch.where(_normal(1, Dh) > 0, 1.0, -1.0).double()
+
+
+def _key(rows, d):
+    """K of a page whose first key scores d binary orders above zero against a query of signs (codes of exponent -6); its
+    others 0.  Some columns have the code below what every one should have, the others the code above it."""
+    Dh = rows[2]
+    grid = q8.nearest(torch.arange(16, 449).double()).unique()
+    total = d / 1.4426950408889634 * Dh**0.5 * 64
+    i = int((grid <= total / Dh).sum()) - 1
+    many = round((total - Dh * float(grid[i])) / float(grid[i + 1] - grid[i]))
+    k = torch.zeros(rows, dtype=torch.float64)
+    k[:, 0] = _signs(Dh) * torch.where(torch.arange(Dh) < many, grid[i + 1], grid[i])
+    return k
+
+
+# The largest V first, last or among many keys of far smaller ones whose scores lie d binary orders lower and which
+# together weigh about as much as it does.  B = 1: many splits; some: shared by one wave; many: a CTA each.  Pages of 4
+# rows: the mma.sync kernel, of 16 positions or more the tcgen05 one.
+@pytest.mark.parametrize("where", ["first", "last", "middle"])
+@pytest.mark.parametrize("B,n,Hq,Hkv,Dh,P,pages,d", [
+    (1, 4, 4, 1, 128, 16, 512, 18), (400, 4, 4, 2, 128, 16, 512, 18), (24, 4, 4, 1, 128, 16, 512, 18), (40, 4, 12, 1, 256, 16, 256, 18),
+    (24, 4, 8, 1, 64, 16, 512, 18), (1, 1, 4, 1, 128, 4, 4096, 14), (200, 1, 4, 1, 64, 4, 4096, 14), (120, 2, 4, 1, 256, 2, 4096, 13)])
+def test_sums_over_scales_far_apart(where, B, n, Hq, Hkv, Dh, P, pages, d):
+    rows = (Hkv, P * n, Dh)
+    q = _signs(Dh).to(BF).expand(B, n, Hq, Dh).contiguous()
+    lens = _i32([pages * P] * B)
+    big = (_key(rows, d), -6, _normal(2, *rows) * 100, q8.E_MAX)
+    for ev in (q8.E_MIN, q8.E_MIN + 9):
+        small = (_normal(3, *rows) * 32, -12, _normal(4, *rows) * 100 * (ev > q8.E_MIN), ev)
+        k, v, ks, vs, table, kv, vv = _cache([big, small], _order(where, 0, 1, pages), n, P)
+        for mode in (CROSS, WITHIN):
+            o, lse, st = _decode(q, k, v, ks, vs, table.expand(B, -1).contiguous(), lens, n, mode)
+            assert st == 0
+            for b in {0, B - 1}:
+                _assert_rows(o[b:b + 1], lse[b:b + 1], q[:1], kv, vv, pages * P, 0, n, mode, 0)
+
+
+def test_sums_of_many_light_keys():
+    """The same on the mma.sync kernel where the largest V comes first, and a CTA has a sequence and head whole: 27
+    orders lower, a key's weight times its V's scale is below fp32's smallest beside that one's.  (Pages of a prime
+    number of rows, which TMA would bring one at a time.)"""
+    n, Hq, Hkv, Dh, P, pages, d, B = 1, 2, 1, 64, 131, 6400, 27.2, 960
+    rows = (Hkv, P * n, Dh)
+    big = (_key(rows, d), -6, _normal(2, *rows) * 100, q8.E_MAX)
+    small = (_normal(3, *rows) * 4, -12, torch.zeros(rows, dtype=torch.float64), q8.E_MIN)
+    k, v, ks, vs, table, kv, vv = _cache([big, small], _order("first", 0, 1, pages), n, P)
+    q = _signs(Dh).to(BF).expand(B, n, Hq, Dh).contiguous()
+    o, lse, st = _decode(q, k, v, ks, vs, table.expand(B, -1).contiguous(), _i32([pages * P] + [P] * (B - 1)), n, CROSS)
+    assert st == 0
+    _assert_rows(o[:1], lse[:1], q[:1], kv, vv, pages * P, 0, n, CROSS, 0)
