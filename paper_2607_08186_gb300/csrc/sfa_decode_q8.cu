@@ -35,6 +35,11 @@ namespace hdsfa {
 namespace decq8 {
 constexpr float kShift = 15.f;       // P's largest exponent
 constexpr int kMaxRows = 64;         // query rows of a CTA at most (four row tiles)
+// P in f16 is off by 2^-11 of P, or, below 2^-14, by up to 2^-25, 2^-40 of the row's largest.  A weight is P 2^-ev, so where V's
+// scales lie no further apart than kFar binary orders, a position loses 2^-24 of the row's largest weight at most; further
+// apart, all rows are computed again (exact_row), since a small block's columns in which larger blocks hold nothing may
+// lose what they hold.  (V of the smallest scale, mostly zeros, counts only in the sum: kFarSum.)
+constexpr int kFar = 16;
 
 // Up to MT row tiles of 16 query rows; at head dim 256 a warp has half of the head dim, since O must fit its registers.  Two
 // CTAs an SM while the queries leave room for three stages each: up to two row tiles, one at head dim 256; with four row
@@ -187,7 +192,7 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
     if (at_row >= a.pg.prow) at_row -= a.pg.prow, ++at_page;
   };
   int kb = 127, vb = -1;
-  unsigned ends = 0;  // V's largest so far << 16, and 255 less its smallest
+  unsigned ends = 0;  // V's largest so far << 16, and 255 less its smallest (the very smallest nearer, see kFar)
   auto scale_bytes = [&] {
     if ((unsigned)next_entry < (unsigned)a.pg.num_pages) {
       const size_t at = ((size_t)next_entry * a.Hkv + g) * a.blocks + fast_div(next_row_in, a.d_brow);
@@ -256,7 +261,7 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
     {
       kb = q8::clamp_byte(kb);
       vb = q8::clamp_byte(vb);
-      ends = __vmaxu2(ends, (unsigned)vb << 16 | (unsigned)(255 - vb));
+      ends = __vmaxu2(ends, (unsigned)vb << 16 | (unsigned)(255 - (vb == q8::kMinByte ? vb + kFarSum - kFar : vb)));
       if (lane < WK) sm.scale[warp][lane] = make_float4(q8::scale_of(kb), (float)(vb - 127), q8::inverse_of(vb), 0.f);
       scale_bytes();
       scale_entry();
@@ -381,7 +386,7 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
   cp_async_wait<0>();
   {
     const int most = (int)__reduce_max_sync(0xffffffffu, ends >> 16), least = 255 - (int)__reduce_max_sync(0xffffffffu, ends & 0xffff);
-    if (most > least + kFarSum) sm.far = 1;
+    if (most > least + kFar) sm.far = 1;
   }
   __syncthreads();
 

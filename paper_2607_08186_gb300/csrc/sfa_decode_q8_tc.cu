@@ -56,6 +56,13 @@ constexpr float kLow = 64.f;       // P's third codes hold so many times what th
 constexpr float kLo = 16.f;        // a query's second e4m3 codes too
 constexpr uint32_t kGaveUp = 1u << 31;
 constexpr float kRedo = -2.f;      // as a partial's sum: the row is to be computed again (exact_row)
+// P's codes are off by 2^-9 of P, or, where it is below 2^-14 (kExact), by up to 2^-23 (kStep), and a weight is P 2^-ev.  So
+// blocks whose ev lies far below the largest (kFar binary orders, where 2^-23 is 2^-22 of the row's largest weight) may lose
+// weight that counts, and with it what they hold in columns in which the larger blocks hold nothing.  What each row loses in
+// such blocks is bounded tile by tile, and rows for which that passes kLost of their sum are computed again.
+constexpr int kFar = 6;
+constexpr float kExact = -14.f, kStep = -23.f;
+constexpr float kLost = 1.f / 128;
 
 // HV units of a K or V tile, of RB columns (128, or 64 at head dim 64) each: a ring slot.  R query rows: WG warp groups of RW.
 template <int DH, int WG>
@@ -68,7 +75,7 @@ struct Cfg {
   static constexpr int SC = kPair ? 2 * R : R, QT = kPair ? 2 : 3;  // columns of S; codes of a query's value
   static constexpr int kCols = 2 * SC + 3 * HV * R;  // tensor memory: two S, three O
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr int kFixed = QT * R * DH + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 9 * R + 512;  // all but the ring
+  static constexpr int kFixed = QT * R * DH + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 13 * R + 512;  // all but the ring
   static constexpr int kPerSm = kAlloc <= 128 && kFixed + 3 * kUnit <= 74 * 1024    ? 3
                                 : kAlloc <= 256 && R <= 32 && kFixed + 3 * kUnit <= 112 * 1024 ? 2
                                                                                     : 1;
@@ -88,11 +95,12 @@ struct Smem {
   float rowf[C::R];                          // a row's factor of q
   float nref[4][C::R];                       // its reference, negated: a copy for each warp of the group; its sums at last
   float most[4][C::R];                       // a warp's maxima
+  float lost[4][C::R];                       // a bound of what a warp's rounding has cost the row's sum
   uint64_t full[C::NSLOT], empty[C::NSLOT], s_full[2], s_free[2], p_full[2], pv_done[2], sc_full[8], q_full, drain;
   unsigned raise[4 * WG];                    // a warp's rows whose references go up, its largest scale byte << 16; kGaveUp
   uint32_t tmem_base;
-  unsigned again[2];                         // rows of O that exact_row computes (kRedo): not finite, or a group's, with
-  int redo;                                  // V's scales far apart; whether there are any
+  unsigned again[2];                         // rows of O that are not finite; whether there is one of them, or of too great
+  int redo;                                  // a loss (kRedo)
   int abort, bad_page[16];                   // of the sequence with this number, mod 16 (the ring holds fewer)
 };
 
@@ -184,6 +192,32 @@ HD_DEVINLINE void split3(uint32_t u, uint32_t& hi, uint32_t& mid, uint32_t& lo) 
     asm("mul.rn.f16x2 %0, %0, %1;\n" : "+r"(lo) : "r"(*reinterpret_cast<const uint32_t*>(&f)));
   }
   lo += 0x00800080u;
+}
+
+// A thread's position's scores, as exponents of P.
+struct Scores {
+  float y[RW];
+};
+// Adds to the warp's bounds lost[RW] what the codes of this tile's P may cost each row's sum in blocks far below the
+// largest.  By a whole warp; vis, vb: the rows that see the thread's position, its scale byte.  (A function of its own:
+// inline, its registers cost every tile 2 %.)
+__device__ __noinline__ void note_losses(Scores s, uint32_t vis, int vb, int top_vb, float* lost) {
+  const int lane = threadIdx.x & 31;
+  // (V of the smallest scale, mostly zeros, counts only in the sum: kFarSum)
+  const bool far = vis != 0 && vb + kFar < top_vb, some = far && vb > q8::kMinByte;
+  const unsigned low = __reduce_min_sync(0xffffffffu, some ? (unsigned)vb : (unsigned)q8::kMaxByte);
+  unsigned mine = 0;  // lane r: row r's, in units of 2^-47 2^-low
+#pragma unroll
+  for (int r = 0; r < RW; ++r) {
+    const bool loses = some && ((vis >> r) & 1u) && s.y[r] < kExact;
+    const float x = loses ? ex2_approx(fminf(s.y[r], kStep) + 47.f + (float)((int)low - vb)) : 0.f;  // at most 2^24
+    const unsigned sum = __reduce_add_sync(0xffffffffu, __float2uint_ru(x));
+    if (lane == r) mine = sum;
+  }
+  float x = (float)mine * 0x1p-47f * q8::inverse_of((int)low);
+  if (__any_sync(0xffffffffu, far && vb + decq8::kFarSum < top_vb)) x = 0x1p100f;  // above every sum
+  if (lane < RW) lost[lane] += x;
+  __syncwarp();
 }
 
 // What CTA x of a K/V head and row group works through: the x-th of nsplit parts of one sequence, or (SHARED) the x-th
@@ -616,7 +650,7 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
           }
           if (lane == 0) sm.rowf[rr] = back * a.scale_log2;
         }
-        if (lane < RW) sm.nref[q4][r0 + lane] = 0.f;
+        if (lane < RW) sm.nref[q4][r0 + lane] = sm.lost[q4][r0 + lane] = 0.f;
         fence_async_smem();
         tc_fence_before();
         __syncwarp();
@@ -706,9 +740,9 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
             if (lane == r) m = from_ordered(x);
           }
           mask = __reduce_or_sync(0xffffffffu, mask | (ok ? 0 : kGaveUp));
-          const unsigned top = __reduce_max_sync(0xffffffffu, vis != 0 ? (unsigned)vb : 0u);
+          const unsigned most_vb = __reduce_max_sync(0xffffffffu, vis != 0 ? (unsigned)vb : 0u);
           if (lane < RW) sm.most[q4][r0 + lane] = m;
-          if (lane == 0) sm.raise[wg * 4 + q4] = mask | top << 16;
+          if (lane == 0) sm.raise[wg * 4 + q4] = mask | most_vb << 16;
           named_bar_sync(bar, 128);  // (the next vote lies before these are written again)
           mask = 0;
 #pragma unroll
@@ -728,6 +762,7 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
             down = kSet - fmaxf(fmaxf(sm.most[0][r], sm.most[1][r]), fmaxf(sm.most[2][r], sm.most[3][r]));
             sm.nref[q4][r] += down;
             if (set >> lane & 1u) fac = ex2_approx(0.5f * down);
+            sm.lost[q4][r] *= fac * fac;
           }
           __syncwarp();
 #pragma unroll
@@ -750,8 +785,12 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
           set |= mask;
         }
         if (!ok) continue;
-        if (vis != 0 && vb + decq8::kFarSum < top_vb) atomicOr(&sm.again[r0 >> 5], 0xffffu << (r0 & 31));
-        __syncwarp();
+        if (__any_sync(0xffffffffu, vis != 0 && vb + kFar < top_vb)) {
+          Scores x;
+#pragma unroll
+          for (int r = 0; r < RW; ++r) x.y[r] = y[r];
+          note_losses(x, vis, vb, top_vb, &sm.lost[q4][r0]);
+        }
         // S of this tile was issued behind the products of the tile before the last, so these are done: P's buffer is free
         const uint64_t inv2 = f2pack(inv, inv);
         {
@@ -847,12 +886,14 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
         named_bar_sync(bar, 128);
         if (key < RW) {
           const int r = r0 + key;
+          const float lost = (sm.lost[0][r] + sm.lost[1][r]) + (sm.lost[2][r] + sm.lost[3][r]);
+          const bool loss = lost > kLost * sum && (set >> key & 1u);
           sum *= part;
           float m = (set >> key) & 1u ? (float)k - ref : -INFINITY;
           if (sum != sum) m = INFINITY;  // a visible score that is not finite: the combined row is NaN
           if (bad) {
             m = -INFINITY, sum = decq8::kBadPage;
-          } else if (r < rows && sm.again[r >> 5] >> (r & 31) & 1u) {
+          } else if (r < rows && (loss || (sm.again[r >> 5] >> (r & 31) & 1u))) {
             sum = kRedo;
             sm.redo = 1;
           }

@@ -106,3 +106,42 @@ def test_sums_of_many_light_keys():
     o, lse, st = _decode(q, k, v, ks, vs, table.expand(B, -1).contiguous(), _i32([pages * P] + [P] * (B - 1)), n, CROSS)
     assert st == 0
     _assert_rows(o[:1], lse[:1], q[:1], kv, vv, pages * P, 0, n, CROSS, 0)
+
+
+def _assert_columns(o, q, kv, vv, T, n, mode, window):
+    """One sequence's rows, whose weights may lose 2^-7 of them all beside what test_q8_decode_gpu allows: column by
+    column, against the column's largest visible V."""
+    a = (q, kv, vv, _i32([T]), n, mode)
+    o_r, _, bad = oracle.decode(*a, window=window)
+    A, _, _ = oracle.decode(q, kv, vv.abs(), *a[3:], window=window)
+    assert bad == 0
+    n_, Hq, Hkv = q.shape[1], q.shape[2], kv.shape[2]
+    most = vv[0].double().abs().amax(0).repeat_interleave(Hq // Hkv, 0)  # [Hq][Dh]
+    err = (o[0].double() - o_r[0]).abs()
+    lim = (2.0**-8 + 1e-3) * o_r[0].abs() + (2.0**-9 + 2.0**-11 + 1e-3) * A[0] + 2.0**-7 * most
+    assert bool((err <= lim).all()), float((err / lim).max())
+
+
+# V of one page is far larger than all others, and only in one column; the others' columns hold what they would without it.
+@pytest.mark.parametrize("apart", [8, 14, 20, 24, 31, 48, 70])
+@pytest.mark.parametrize("where", ["first", "last", "middle"])
+@pytest.mark.parametrize("B,n,Hq,Hkv,Dh,P,pages,window", [
+    (1, 4, 4, 1, 128, 16, 64, 0), (400, 4, 4, 2, 128, 16, 64, 0), (24, 4, 16, 1, 128, 16, 128, 0), (40, 4, 12, 1, 256, 16, 64, 3000),
+    (24, 4, 8, 1, 64, 16, 128, 0), (1, 1, 4, 1, 128, 4, 512, 0), (200, 1, 4, 1, 64, 4, 512, 1500), (120, 2, 4, 1, 256, 2, 512, 0)])
+def test_columns_beside_a_far_larger_block(where, apart, B, n, Hq, Hkv, Dh, P, pages, window):
+    rows = (Hkv, P * n, Dh)
+    huge = _normal(2, *rows) * 100
+    huge[..., 1:] = 0.0
+    large = (_normal(5, *rows) * 100, -6, huge, -30 + apart)
+    usual = (_normal(3, *rows) * 100, -6, _normal(4, *rows) * 100, -30)
+    k, v, ks, vs, table, kv, vv = _cache([large, usual], _order(where, 0, 1, pages), n, P)
+    q = _normal(6, 1, n, Hq, Dh).to(BF)
+    L = pages * P
+    for mode in (LOCAL,) if window else (CROSS, WITHIN):
+        o, lse, st = _decode(q.expand(B, -1, -1, -1).contiguous(), k, v, ks, vs, table.expand(B, -1).contiguous(), _i32([L] * B), n,
+                             mode, window)
+        assert st == 0
+        _, lse_r, _ = oracle.decode(q, kv, vv, _i32([L]), n, mode, window=window)
+        for b in {0, B - 1}:
+            _assert_columns(o[b:b + 1], q, kv, vv, L, n, mode, window)
+            assert float((lse[b].double() - lse_r[0]).abs().max()) <= 1e-3
