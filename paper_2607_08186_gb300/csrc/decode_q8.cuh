@@ -17,6 +17,12 @@ constexpr uint32_t kNoRow = 0xffffffffu;
 // there, what is flushed to 0, P < 2^-126, is a weight of less than 2^-35 of the row's largest.)
 constexpr int kFarSum = 96;
 
+// A query's codes (or its f16 form) miss its values far below its row's largest, which count where K's are as much larger.
+// The row's sum of what they miss times K's largest value, 448 2^ek of its largest scale, bounds how far a score is off;
+// rows whose bound passes kMissed (in log2 units) are computed again.  (Ordinary rows miss 2^-21 of their largest value
+// in a column or none: 2^-14 of a score's unit where K's largest is 200 times a query's.)
+constexpr float kMissed = 1.f / 256;
+
 // The exponent of a partial's sum l, by which the partial is divided: l is a sum of P 2^-ev and P is relative to m, which
 // counts ev, so between partials whose ev lie far apart the factors 2^(m - m') would leave fp32's range where the weights'
 // do not.  Divided so, m is the logarithm of the partial's weight, to a binary order, and l lies in [1, 2).

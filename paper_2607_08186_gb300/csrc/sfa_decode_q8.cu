@@ -64,9 +64,10 @@ struct Smem {
   __half q[C::MT * 16 * DH];
   float4 scale[C::kWarps][C::WK];   // a warp's keys: 2^ek, ev, 2^-ev
   float qscale[C::MT * 16];
+  unsigned missed;                      // the most that a row's f16 query misses (kMissed), as bits
   uint32_t row[4][C::KT];               // rows of the pool (kNoRow: none) of four tiles
   unsigned again[2];                    // rows of the merged partial (bits) that are not finite, which exact_row computes,
-  int far;                              // and whether it computes all of them: V's scales lie far apart
+  int far;                              // and whether it computes all of them: V's scales lie far apart, or queries miss too much
   int bad_page;
 };
 
@@ -88,6 +89,17 @@ HD_DEVINLINE void mma_f16_16816(float* d, const uint32_t* a, uint32_t b0, uint32
 HD_DEVINLINE uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Whether a query that misses `missed` 2^-ek is too far off at a position p, p + blockDim.x, ... < k1.  (Hardly ever called:
+// f16 misses values 2^-31 of a row's largest and below.)
+__device__ __noinline__ bool misses_keys(const Args& a, const int32_t* table, int g, int p, int k1, float missed) {
+  bool r = false;
+  for (; p < k1; p += blockDim.x) {
+    size_t at = 0;
+    if (row_at(a, table, g, p, &at) != kNoRow) r |= missed * q8::scale_of(q8::clamp_byte(a.kscale[at])) > kMissed;
+  }
+  return r;
 }
 
 template <int DH, int MT>
@@ -120,6 +132,7 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
     sm.bad_page = 0;
     sm.again[0] = sm.again[1] = 0;
     sm.far = 0;
+    sm.missed = 0;
   }
   // this thread's query rows g4 and g4 + 8 of the row tile: their streams (-1: padding).  Where n divides a tile, which
   // of this thread's keys are of a row's stream is the same in every tile.
@@ -235,13 +248,18 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
     const int e = min(max((int)(most >> 23), 20), 254);
     const float to = __int_as_float(min(127 + 14 + 127 - e, 254) << 23);  // 2^(14 - (e - 127)), at most 2^127
     const float back = __int_as_float(max(e - 14, 1) << 23);              // 2^(e - 127 - 14)
+    float miss = 0.f;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int p = lane * NP + i, kk = p >> 3, t = (p >> 1) & 3, hi = p & 1;
-      *reinterpret_cast<uint32_t*>(sm.q + swz<DH>(rr, kk * 16 + hi * 8 + 2 * t)) =
-          pack_f16(__uint_as_float(w[i] << 16) * to, __uint_as_float(w[i] & 0xffff0000u) * to);
+      const float x0 = __uint_as_float(w[i] << 16) * to, x1 = __uint_as_float(w[i] & 0xffff0000u) * to;
+      const __half2 u = __floats2half2_rn(x0, x1);
+      const float2 y = __half22float2(u);
+      miss += fabsf(x0 - y.x) + fabsf(x1 - y.y);
+      *reinterpret_cast<__half2*>(sm.q + swz<DH>(rr, kk * 16 + hi * 8 + 2 * t)) = u;
     }
     if (lane == 0) sm.qscale[rr] = back * a.scale_log2;
+    if (miss > 0.f) atomicMax(&sm.missed, __float_as_uint(miss * (32.f * 448.f) * fabsf(back * a.scale_log2)));  // (32 lanes')
   }
   __syncthreads();
 
@@ -388,6 +406,7 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
     const int most = (int)__reduce_max_sync(0xffffffffu, ends >> 16), least = 255 - (int)__reduce_max_sync(0xffffffffu, ends & 0xffff);
     if (most > least + kFar) sm.far = 1;
   }
+  if (sm.missed != 0 && misses_keys(a, table, g, max(k0, seen) + tid, k1, __uint_as_float(sm.missed))) sm.far = 1;
   __syncthreads();
 
   // merge the key groups' partials in shared memory (the ring is free now): [KW][R][DH], then what the sums count

@@ -75,7 +75,7 @@ struct Cfg {
   static constexpr int SC = kPair ? 2 * R : R, QT = kPair ? 2 : 3;  // columns of S; codes of a query's value
   static constexpr int kCols = 2 * SC + 3 * HV * R;  // tensor memory: two S, three O
   static constexpr int kAlloc = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-  static constexpr int kFixed = QT * R * DH + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 13 * R + 512;  // all but the ring
+  static constexpr int kFixed = QT * R * DH + 6 * R * KT + 128 * (4 * 12 + 8 * 2) + 4 * 14 * R + 512;  // all but the ring
   static constexpr int kPerSm = kAlloc <= 128 && kFixed + 3 * kUnit <= 74 * 1024    ? 3
                                 : kAlloc <= 256 && R <= 32 && kFixed + 3 * kUnit <= 112 * 1024 ? 2
                                                                                     : 1;
@@ -93,6 +93,7 @@ struct Smem {
   int entry[4][128];                         // its page entry
   uint16_t scale[8 * 128];                   // blocks' scale bytes, K's and V's above it
   float rowf[C::R];                          // a row's factor of q
+  float missed[C::R];                        // what its codes miss (decq8::kMissed)
   float nref[4][C::R];                       // its reference, negated: a copy for each warp of the group; its sums at last
   float most[4][C::R];                       // a warp's maxima
   float lost[4][C::R];                       // a bound of what a warp's rounding has cost the row's sum
@@ -101,6 +102,7 @@ struct Smem {
   uint32_t tmem_base;
   unsigned again[2];                         // rows of O that are not finite; whether there is one of them, or of too great
   int redo;                                  // a loss (kRedo)
+  int most_kb[2][4];                         // K's largest scale byte of this sequence and the one before, by the first group's warps
   int abort, bad_page[16];                   // of the sequence with this number, mod 16 (the ring holds fewer)
 };
 
@@ -577,7 +579,10 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
         const int c = handed++;
         const uint2 x = sm.words[c & 3][key];
         const int sh = (places >> (c & 3) * 2 & 3) * 8;
-        sm.scale[((chunks + c) & 7) * 128 + key] = (uint16_t)(q8::clamp_byte(x.x >> sh & 255) | q8::clamp_byte(x.y >> sh & 255) << 8);
+        const int kb = q8::clamp_byte(x.x >> sh & 255), block = c * 128 + key;
+        sm.scale[((chunks + c) & 7) * 128 + key] = (uint16_t)(kb | q8::clamp_byte(x.y >> sh & 255) << 8);
+        const int most = (int)__reduce_max_sync(0xffffffffu, block >= b_seen && block < nblocks ? (unsigned)kb : 0u);
+        if (lane == 0) sm.most_kb[seq & 1][q4] = max(c > 0 ? sm.most_kb[seq & 1][q4] : 0, most);
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.sc_full[(chunks + c) & 7]);
         chunk_words(c + 3, sm.entry[(c + 3) & 3][key]);
@@ -628,19 +633,29 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
           constexpr int kUp = C::kPair ? 7 : 14;  // the largest to [2^kUp, 2^(kUp + 1))
           const float to = __int_as_float(min(127 + kUp + 127 - e, 254) << 23);  // 2^(kUp - (e - 127)), at most 2^127
           const float back = __int_as_float(max(e - kUp, 1) << 23);              // 2^(e - 127 - kUp)
+          float miss = 0.f;  // at most 2^-14 a value (2^-17 where kUp is 14)
 #pragma unroll
           for (int i = 0; i < NP; ++i) {
             const float x0 = __uint_as_float(w[x][i] << 16) * to, x1 = __uint_as_float(w[x][i] & 0xffff0000u) * to;
+            [[maybe_unused]] float2 left = make_float2(x0, x1);
             uint32_t t[3];
             if (C::kPair) {
               t[0] = q8::code2(x0, x1);
               const float2 y = q8::values2((uint16_t)t[0]);
               t[1] = q8::code2((x0 - y.x) * kLo, (x1 - y.y) * kLo);
+              const float2 z = q8::values2((uint16_t)t[1]);
+              miss += fabsf(x0 - y.x - z.x / kLo) + fabsf(x1 - y.y - z.y / kLo);
             } else {
               const __half2 u = __floats2half2_rn(x0, x1);
               split3<false>(*reinterpret_cast<const uint32_t*>(&u), t[0], t[1], t[2]);
 #pragma unroll
-              for (int y = 0; y < 3; ++y) t[y] = __byte_perm(t[y], 0, 0x31);
+              for (int y = 0; y < 3; ++y) {
+                const uint32_t code = t[y] & 0xff00ff00u;
+                const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&code));
+                left.x -= z.x, left.y -= z.y;
+                t[y] = __byte_perm(t[y], 0, 0x31);
+              }
+              miss += fabsf(left.x) + fabsf(left.y);
             }
             const int c = (lane * NP + i) * 2, at = (c % RB) >> 4, off = c & 15;  // column; its 16-byte chunk
             const int swizzled = RB == 64 ? at ^ (rr >> 1 & 3) : at ^ (rr & 7);
@@ -648,7 +663,12 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
             for (int y = 0; y < C::QT; ++y)
               *reinterpret_cast<uint16_t*>(sm.q[c / RB][y] + rr * RB + swizzled * 16 + off) = (uint16_t)t[y];
           }
-          if (lane == 0) sm.rowf[rr] = back * a.scale_log2;
+          constexpr float kUnit24 = C::kPair ? 0x1p36f : 0x1p39f;
+          const unsigned missed = __reduce_add_sync(0xffffffffu, __float2uint_ru(miss * kUnit24));
+          if (lane == 0) {
+            sm.rowf[rr] = back * a.scale_log2;
+            sm.missed[rr] = (float)missed / kUnit24 * 448.f * fabsf(back * a.scale_log2);
+          }
         }
         if (lane < RW) sm.nref[q4][r0 + lane] = sm.lost[q4][r0 + lane] = 0.f;
         fence_async_smem();
@@ -887,7 +907,9 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
         if (key < RW) {
           const int r = r0 + key;
           const float lost = (sm.lost[0][r] + sm.lost[1][r]) + (sm.lost[2][r] + sm.lost[3][r]);
-          const bool loss = lost > kLost * sum && (set >> key & 1u);
+          const int* kb = sm.most_kb[seq & 1];
+          const float missed = sm.missed[r] * q8::scale_of(max(max(kb[0], kb[1]), max(kb[2], kb[3])));
+          const bool loss = (lost > kLost * sum || missed > decq8::kMissed) && (set >> key & 1u);
           sum *= part;
           float m = (set >> key) & 1u ? (float)k - ref : -INFINITY;
           if (sum != sum) m = INFINITY;  // a visible score that is not finite: the combined row is NaN

@@ -145,3 +145,28 @@ def test_columns_beside_a_far_larger_block(where, apart, B, n, Hq, Hkv, Dh, P, p
         for b in {0, B - 1}:
             _assert_columns(o[b:b + 1], q, kv, vv, L, n, mode, window)
             assert float((lse[b].double() - lse_r[0]).abs().max()) <= 1e-3
+
+
+# Queries whose largest value meets zeros of K, and whose others, 2^small times as large, make the scores; every other head
+# has ordinary queries beside a smaller K.  The second shape's K is small in one half of the sequence.
+@pytest.mark.parametrize("small", [-8, -12, -16, -22, -28, -36, -48])
+@pytest.mark.parametrize("B,n,Hq,Hkv,Dh,P,pages", [
+    (1, 4, 4, 1, 128, 16, 64), (24, 4, 16, 1, 128, 16, 64), (400, 1, 24, 2, 128, 16, 64), (40, 4, 12, 1, 256, 16, 32),
+    (3, 1, 16, 2, 256, 64, 32), (6, 4, 8, 1, 256, 16, 32), (2, 4, 16, 1, 256, 16, 32), (24, 4, 8, 1, 64, 16, 64), (1, 1, 4, 1, 128, 4, 256), (200, 1, 4, 1, 64, 4, 256), (12, 4, 24, 2, 256, 1, 256)])
+def test_small_values_of_queries(small, B, n, Hq, Hkv, Dh, P, pages):
+    rows = (Hkv, P * n, Dh)
+    k_large, k_small = _normal(2, *rows) * 100, _normal(3, *rows) * 100
+    k_large[..., 0] = 0.0
+    large = (k_large, -7 - small, _normal(4, *rows) * 100, -6)
+    little = (k_small, -9, _normal(5, *rows) * 100, -6)
+    k, v, ks, vs, table, kv, vv = _cache([large, little], [0] * (pages // 2) + [1] * (pages - pages // 2), n, P)
+    q = _normal(6, 1, n, Hq, Dh)
+    q[..., 1:] *= 2.0**small
+    q[:, :, ::2, 0] = 1.5
+    q = q.to(BF)
+    L = pages * P
+    for mode in (CROSS, WITHIN):
+        o, lse, st = _decode(q.expand(B, -1, -1, -1).contiguous(), k, v, ks, vs, table.expand(B, -1).contiguous(), _i32([L] * B), n, mode)
+        assert st == 0
+        for b in {0, B - 1}:
+            _assert_rows(o[b:b + 1], lse[b:b + 1], q, kv, vv, L, 0, n, mode, 0)
