@@ -97,10 +97,10 @@ __device__ __noinline__ void exact_row(const Args& a, int b, int g, int r, int T
       for (int c = 0; c < C; c += 2) {
         const float2 kv = q8::values2(*reinterpret_cast<const uint16_t*>(a.kcodes + at + lane * C + c));
         const float2 vv = q8::values2(*reinterpret_cast<const uint16_t*>(a.vcodes + at + lane * C + c));
-        x[e] += qf[c] * kv.x + qf[c + 1] * kv.y;
+        x[e] += qf[c] * (kv.x * fk) + qf[c + 1] * (kv.y * fk);  // (codes alone may pass fp32's range)
         v[e][c] = vv.x * fv, v[e][c + 1] = vv.y * fv;
       }
-      x[e] *= a.scale_log2 * fk;
+      x[e] *= a.scale_log2;
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1)

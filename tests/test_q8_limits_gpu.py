@@ -170,3 +170,20 @@ def test_small_values_of_queries(small, B, n, Hq, Hkv, Dh, P, pages):
         assert st == 0
         for b in {0, B - 1}:
             _assert_rows(o[b:b + 1], lse[b:b + 1], q, kv, vv, L, 0, n, mode, 0)
+
+
+# Queries near bf16's largest values over K's smallest scale: scores of 2^60 and more, whose products in codes pass fp32's
+# range before the scale brings them back.  The largest score takes the row; LSE relative to it.
+@pytest.mark.parametrize("B,n,Hq,Hkv,Dh,P,pages", [(1, 4, 4, 1, 128, 16, 8), (5, 4, 12, 1, 256, 16, 6), (3, 4, 8, 1, 64, 16, 8), (2, 1, 4, 1, 128, 4, 16)])
+def test_large_queries_over_small_keys(B, n, Hq, Hkv, Dh, P, pages):
+    rows = (Hkv, P * n, Dh)
+    page = (_normal(2, *rows) * 100, q8.E_MIN, _normal(4, *rows) * 100, -6)
+    k, v, ks, vs, table, kv, vv = _cache([page], [0] * pages, n, P)
+    q = (_normal(6, 1, n, Hq, Dh) * 2.0**124).to(BF)
+    L = P  # (pages past the first would repeat its scores)
+    o, lse, st = _decode(q.expand(B, -1, -1, -1).contiguous(), k, v, ks, vs, table.expand(B, -1).contiguous(), _i32([L] * B), n, CROSS)
+    assert st == 0
+    o_r, lse_r, _ = oracle.decode(q, kv, vv, _i32([L]), n, CROSS)
+    for b in {0, B - 1}:
+        assert float((lse[b].double() / lse_r[0] - 1).abs().max()) <= 1e-3
+        assert float((o[b].double() - o_r[0]).abs().max()) <= 2.0**-8 * float(o_r.abs().max())
