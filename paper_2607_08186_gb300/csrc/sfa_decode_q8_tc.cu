@@ -881,6 +881,7 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
           k = decq8::sum_exponent(sum);
         }
         const float part = decq8::two_to_minus(k);
+        __syncwarp();  // (lanes' branches lie behind the accesses to tensor memory, here and below)
         tc_fence_after();
         const bool bad = *(volatile int*)&sm.bad_page[seq & 15] != 0;
         // this lane's row of O^T: all 128, or (a product of 64 rows) 16 of each 32
@@ -902,6 +903,7 @@ __global__ void __launch_bounds__(Cfg<DH, WG>::kThreads, Cfg<DH, WG>::kPerSm)
           }
           wrong = __reduce_or_sync(0xffffffffu, wrong);
           if (wrong != 0 && lane == 0) atomicOr(&sm.again[r0 >> 5], wrong << (r0 & 31));
+          __syncwarp();
         }
         named_bar_sync(bar, 128);
         if (key < RW) {
