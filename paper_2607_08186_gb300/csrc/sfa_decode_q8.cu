@@ -576,11 +576,6 @@ struct Q8Plan {
 };
 }  // namespace
 
-// Positions that a step of maxT tokens reads at most.
-static long long q8_range(int maxT, int n, int mode, int window) {
-  return mode == SFA_LOCAL ? std::min<long long>((long long)maxT * n, (long long)window + n - 1) : (long long)maxT * n;
-}
-
 // Positions of a tile.
 static int q8_tile(int Dh, int rg, bool tc) { return tc || Dh == 64 || (Dh == 128 && rg > 16) ? 128 : 64; }
 
@@ -629,23 +624,6 @@ static Q8Plan q8_plan(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode,
   p.part_o_bytes = parts * p.rg * Dh * sizeof(float);
   p.part_ml_bytes = parts * p.rg * sizeof(float2);
   return p;
-}
-
-// Whether the tcgen05 kernel takes a step.  It reads tiles by TMA alone, in pieces of at least kTmaRows rows of a page that
-// start on 128 bytes of shared memory, and takes longer to start and end, so up to 16 query rows leave it short ranges; at
-// head dim 64, where a tile has half the bytes for the same softmax, all but a million positions over the heads.
-// Measured (replayed from a graph, us, tcgen05 / mma.sync; sequences x tokens x streams):
-//   16 over 4 of 64     4 x 400 x 3 10.8 / 9.2, 33 x 700 x 3 22.6 / 16.3, 2 x 8192 x 1 13.2 / 10.1, 4 x 6000 x 3 21.4 / 16.9, 8 x
-//                       8192 x 3 32.8 / 30.9, 33 x 3000 x 3 (1.2 M positions of a head) 43.7 / 44.2, 100 x 3000 x 3 93 / 119
-//   32 over 8 of 128    33 x 12 x 4 11.3 / 9.0, 4 x 25 x 4 7.5 / 8.6, 33 x 25 x 4 10.9 / 10.1, 4 x 50 x 4 9.1 / 10.5, 4 x 1000 x 4
-//                       16.3 / 18.6, 16 x 1000 x 4 26.9 / 39.2
-//   24 over 2 of 256    33 x 20 x 1 9.8 / 8.6, 4 x 400 x 1 12.9 / 9.5, 4 x 1000 x 1 9.8 / 9.8, 33 x 1000 x 1 15.1 / 18.2
-//   more than 16 rows   24 over 2 of 256, 4 x 50 x 4 12.9 / 23.8; 96 over 8 of 128, 16 x 50 x 4 11.8 / 15.1
-constexpr int kTmaRows = 8;
-static bool q8_tc(int Dh, int prow, int rows, long long range, long long heads) {
-  const int piece = paged_piece(prow, 128);
-  if (piece < kTmaRows || (Dh == 64 && piece % 2 != 0)) return false;
-  return rows > 16 || (Dh == 64 ? range * heads > 1 << 20 : range > (Dh == 128 ? 64 : 512));
 }
 
 size_t decode_paged_q8_ws_bytes(int B, int maxT, int n, int Hq, int Hkv, int Dh, int mode, int window) {

@@ -1,0 +1,9 @@
+"""Decoding cases over the 8-bit cache and the kernel that each is for (test infrastructure)."""
+TC, MMA = True, False
+
+# (B, n, Hq, Hkv, Dh, P, T, L): scores that climb, fall or jump on the tcgen05 kernel at head dim 64, whose O has 64 rows:
+# 32, 48 and 64 query rows of a K/V head, groups of them, and few rows of many positions
+CHANGE = [(2, 4, 16, 2, 64, 16, 16, 700), (3, 4, 48, 4, 64, 32, 8, 500), (2, 8, 16, 2, 64, 8, 2, 300), (2, 4, 96, 4, 64, 20, 5, 400),
+          (90, 4, 4, 4, 64, 32, 1, 760)]
+# (B, n, Hq, Hkv, Dh, P, T, L): one wave shared by uneven sequences there
+WAVE = [(2, 4, 32, 4, 64, 32, 8, 16000)]
