@@ -7,3 +7,6 @@ CHANGE = [(2, 4, 16, 2, 64, 16, 16, 700), (3, 4, 48, 4, 64, 32, 8, 500), (2, 8, 
           (90, 4, 4, 4, 64, 32, 1, 760)]
 # (B, n, Hq, Hkv, Dh, P, T, L): one wave shared by uneven sequences there
 WAVE = [(2, 4, 32, 4, 64, 32, 8, 16000)]
+# (kernel, n, Hq, Hkv, Dh, P, T, L): queries far from 1, explicit scales
+SIZES = [(TC, 2, 8, 2, 128, 8, 2, 80), (TC, 4, 12, 1, 256, 16, 4, 80), (TC, 4, 8, 1, 256, 16, 16, 80), (TC, 4, 12, 2, 64, 16, 16, 80),
+         (MMA, 2, 8, 2, 128, 3, 1, 80), (MMA, 1, 8, 2, 64, 16, 16, 200), (MMA, 4, 24, 2, 256, 1, 1, 60), (MMA, 4, 12, 1, 128, 1, 1, 60)]

@@ -14,6 +14,12 @@ def test_cases_for_the_tensor_cores(c):
         assert q8_rule.tensor_cores(B, n, Hq, Hkv, Dh, P, L, mode, w)
 
 
+@pytest.mark.parametrize("c", q8_kernels.SIZES)
+def test_cases_of_sizes(c):
+    kernel, n, Hq, Hkv, Dh, P, T, L = c
+    assert q8_rule.tensor_cores(1, n, Hq, Hkv, Dh, P, L) == kernel
+
+
 def test_borders():
     tc = q8_rule.tensor_cores
     # pieces that TMA cannot bring are never for the tensor cores

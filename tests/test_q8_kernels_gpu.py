@@ -29,3 +29,35 @@ def test_scores_that_change(shape, c):
 @pytest.mark.parametrize("c", q8_kernels.WAVE)
 def test_a_wave_shared_by_uneven_sequences(c):
     decode.test_a_wave_shared_by_uneven_sequences(*c)
+
+
+@pytest.mark.parametrize("size", [1e-16, 1e-10, 1e-4, 30.0, 3e4, 1e12])
+@pytest.mark.parametrize("c", q8_kernels.SIZES)
+def test_sizes_of_queries_and_keys(c, size):
+    """Queries far from 1 with keys as far on the other side, so that scores stay of order 1; a row of zeros, one of very
+    different magnitudes."""
+    _, n, Hq, Hkv, Dh, P, T, L = c
+    q, kc, vc = _case(1, L, n, Hq, Hkv, Dh, 6)
+    q, kc = (q.float() * size).to(BF), (kc.float() / size).to(BF)
+    q[0, 0, 0] = 0.0
+    q[0, n - 1, 3, ::2] *= 2.0**-9
+    lens = _i32([L])
+    kq, ks, table, kv = q8.quantised(kc, lens, P, T, n, 0)
+    vq, vs, _, vv = q8.quantised(vc, lens, P, T, n, 0)
+    o, lse, st = _decode(q, kq, vq, ks, vs, table, lens, n, CROSS)
+    assert st == 0
+    _assert_rows(o, lse, q, kv, vv, L, 0, n, CROSS, 0)
+
+
+@pytest.mark.parametrize("scale", [1e-3, 0.02, 0.3])
+@pytest.mark.parametrize("c", q8_kernels.SIZES)
+def test_explicit_scales(c, scale):
+    _, n, Hq, Hkv, Dh, P, T, L = c
+    q, kc, vc = _case(1, L, n, Hq, Hkv, Dh, 7)
+    lens = _i32([L])
+    kq, ks, table, kv = q8.quantised(kc, lens, P, T, n, 0)
+    vq, vs, _, vv = q8.quantised(vc, lens, P, T, n, 0)
+    for with_lse in (True, False):
+        o, lse, st = _decode(q, kq, vq, ks, vs, table, lens, n, CROSS, scale=scale, with_lse=with_lse)
+        assert st == 0
+        _assert_rows(o, lse, q, kv, vv, L, 0, n, CROSS, 0, scale=scale)
