@@ -10,3 +10,7 @@ WAVE = [(2, 4, 32, 4, 64, 32, 8, 16000)]
 # (kernel, n, Hq, Hkv, Dh, P, T, L): queries far from 1, explicit scales
 SIZES = [(TC, 2, 8, 2, 128, 8, 2, 80), (TC, 4, 12, 1, 256, 16, 4, 80), (TC, 4, 8, 1, 256, 16, 16, 80), (TC, 4, 12, 2, 64, 16, 16, 80),
          (MMA, 2, 8, 2, 128, 3, 1, 80), (MMA, 1, 8, 2, 64, 16, 16, 200), (MMA, 4, 24, 2, 256, 1, 1, 60), (MMA, 4, 12, 1, 128, 1, 1, 60)]
+# (kernel, n, Hq, Hkv, Dh, P, T, L, window): pages given up behind the window, which starts inside a page, a tile, a piece
+GIVEN_UP = [(k, n, Hq, Hkv, Dh, P, T, L, w) for k, n, Hq, Hkv, Dh, P, T, L in
+            [(TC, 2, 16, 2, 128, 16, 16, 300), (TC, 4, 12, 1, 128, 20, 5, 200), (TC, 4, 24, 2, 256, 16, 4, 200), (TC, 4, 16, 2, 64, 32, 8, 200),
+             (MMA, 2, 8, 2, 128, 3, 3, 200), (MMA, 1, 8, 2, 64, 16, 4, 400), (MMA, 4, 24, 2, 256, 1, 1, 150)] for w in (97, 131, 256, 300)]

@@ -20,6 +20,12 @@ def test_cases_of_sizes(c):
     assert q8_rule.tensor_cores(1, n, Hq, Hkv, Dh, P, L) == kernel
 
 
+@pytest.mark.parametrize("c", q8_kernels.GIVEN_UP)
+def test_cases_of_given_up_pages(c):
+    kernel, n, Hq, Hkv, Dh, P, T, L, w = c
+    assert q8_rule.tensor_cores(3, n, Hq, Hkv, Dh, P, L, inputs.LOCAL, w) == kernel
+
+
 def test_borders():
     tc = q8_rule.tensor_cores
     # pieces that TMA cannot bring are never for the tensor cores

@@ -61,3 +61,31 @@ def test_explicit_scales(c, scale):
         o, lse, st = _decode(q, kq, vq, ks, vs, table, lens, n, CROSS, scale=scale, with_lse=with_lse)
         assert st == 0
         _assert_rows(o, lse, q, kv, vv, L, 0, n, CROSS, 0, scale=scale)
+
+
+@pytest.mark.parametrize("c", q8_kernels.GIVEN_UP)
+def test_pages_given_up_behind_a_window(c):
+    """A sequence whose pages before its window are given back (entries -1, or pages of other sequences) has the rows that
+    it would have with them."""
+    _, n, Hq, Hkv, Dh, P, T, L, w = c
+    q, kc, vc = _case(3, L, n, Hq, Hkv, Dh, 11)
+    lens = [L, L - 37, L // 2 + 1]
+    kq, ks, table, kv = q8.quantised(kc, lens, P, T, n, 1)
+    vq, vs, _, vv = q8.quantised(vc, lens, P, T, n, 1)
+    given = 0
+    for b, x in enumerate(lens):
+        first = max(0, (x - 1) * n - w + 1)  # the first position that a row sees
+        keep = first // n // P
+        table[b, :keep] = _i32([-1, -7, kq.shape[0], 2**31 - 1])[torch.arange(keep) % 4]
+        given += keep
+    assert given > 0
+    o, lse, st = _decode(q, kq, vq, ks, vs, table, _i32(lens), n, LOCAL, window=w)
+    assert st == 0
+    for b, x in enumerate(lens):
+        _assert_rows(o, lse, q, kv, vv, x, b, n, LOCAL, w)
+    # one entry more, which a row sees, empties the sequence
+    last = max(0, (lens[0] - 1) * n - w + 1) // n // P
+    table[0, last] = -1
+    o, lse, st = _decode(q, kq, vq, ks, vs, table, _i32(lens), n, LOCAL, window=w)
+    assert st == binding.HD_DEVBIT_INDEX and torch.count_nonzero(o[0]) == 0
+    _assert_rows(o, lse, q, kv, vv, lens[1], 1, n, LOCAL, w)
