@@ -80,4 +80,21 @@ inline bool q8_tc(int Dh, int prow, int rows, long long range, long long heads) 
   return rows > 16 || (Dh == 64 ? range * heads > 1 << 20 : range > (Dh == 128 ? 64 : 512));
 }
 
+// The parts that one wave of CTAs makes of a batch's `all` units (tiles and starts), the longest sequence of `most` units:
+// at most `total` parts, none empty, and no sequence in more than max_split of them.  Part x begins at unit x * all / S.
+struct WaveParts {
+  unsigned all, S;
+  __host__ __device__ WaveParts(unsigned all_, unsigned most, unsigned total, unsigned max_split) : all(all_) {
+    S = total < all ? total : all;
+    if (S < 1) S = 1;
+    if ((unsigned long long)most * S > (max_split - 2ull) * all) S = (unsigned)((max_split - 2ull) * all / most);
+  }
+  // (S and x are hundreds at most)
+  __host__ __device__ unsigned begin(unsigned x) const {
+    const unsigned per = all / S;
+    return x * per + x * (all - per * S) / S;
+  }
+  __host__ __device__ int of(unsigned u) const { return (int)(((u + 1ull) * S - 1) / all); }  // the part that holds unit u
+};
+
 }  // namespace hdsfa

@@ -41,6 +41,7 @@
 
 #include <algorithm>
 
+#include "decode_plan.cuh"
 #include "decode_q8.cuh"
 
 namespace hdsfa {
@@ -238,11 +239,9 @@ struct Work {
       T = a.lens[b];
       dec::split_range<true>(a, T, x - b * a.nsplit, a.tile, k0, k1);
     } else {
-      const uint2 whole = parts(a);
-      const unsigned all = whole.x, S = whole.y, per = all / S, rest = all - per * S;
-      // part x begins at x * all / S; S and x are hundreds at most
-      const unsigned u0 = x * per + x * rest / S, u1 = (x + 1) * per + (x + 1) * rest / S;
-      if (x >= (int)S || u0 >= u1) return;
+      const WaveParts whole = parts(a);
+      const unsigned u0 = whole.begin(x), u1 = whole.begin(x + 1);
+      if (x >= (int)whole.S || u0 >= u1) return;
       each(a, [&](int q, int len, unsigned first, unsigned size) {
         const unsigned hit = __ballot_sync(0xffffffffu, first <= u0 && u0 < first + size);
         if (hit == 0) return false;
@@ -268,12 +267,11 @@ struct Work {
   }
   // For the combine kernel, by one warp: each sequence's first partial, and their number.
   static HD_DEVINLINE void report(const Args& a) {
-    const uint2 whole = parts(a);
+    const WaveParts whole = parts(a);
     each(a, [&](int q, int, unsigned first, unsigned size) {
-      auto part_of = [&](unsigned u) { return (int)((((unsigned long long)u + 1) * whole.y - 1) / whole.x); };  // that holds tile u
       if (q < a.B) {
-        const int x0 = size > 0 ? part_of(first + kStart) : 0;
-        a.share[q] = size > 0 ? make_int2(x0 + q, part_of(first + size - 1) - x0 + 1) : make_int2(0, 0);
+        const int x0 = size > 0 ? whole.of(first + kStart) : 0;
+        a.share[q] = size > 0 ? make_int2(x0 + q, whole.of(first + size - 1) - x0 + 1) : make_int2(0, 0);
       }
       return false;
     });
@@ -286,8 +284,7 @@ struct Work {
     return fast_div(hi - fast_div(lo, a.d_tile) * a.tile + a.tile - 1, a.d_tile);
   }
   static HD_DEVINLINE unsigned size_of(const Args& a, int len) { return len >= 1 && len <= a.maxT ? tiles_of(a, len) + kStart : 0; }
-  // All sequences' tiles, starts among them, and the number of parts: none empty, and no sequence in more than kMaxSplit.
-  static HD_DEVINLINE uint2 parts(const Args& a) {
+  static HD_DEVINLINE WaveParts parts(const Args& a) {
     unsigned all = 0, most = 0;
 #pragma unroll 1
     for (int q = threadIdx.x & 31; q < a.B; q += 32) {
@@ -298,9 +295,7 @@ struct Work {
     __syncwarp();
     all = __reduce_add_sync(0xffffffffu, all);
     most = __reduce_max_sync(0xffffffffu, most);
-    unsigned S = max(1u, min((unsigned)a.total, all));
-    if ((unsigned long long)most * S > (dec::kMaxSplit - 2ull) * all) S = (unsigned)((dec::kMaxSplit - 2ull) * all / most);
-    return make_uint2(all, S);
+    return WaveParts(all, most, (unsigned)a.total, dec::kMaxSplit);
   }
   // f(sequence, its tokens, the tiles before its start, its own and its start's) for each lane's, until one returns true.
   template <class F>
