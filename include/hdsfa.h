@@ -442,6 +442,13 @@ hd_status_t hd_pages_copy(void* k_pages, void* v_pages, const int32_t* copies, i
  *
  * sfa_decode_paged_q8 -- sfa_decode_paged over such a cache: the same masks, outputs, errors and workspace rules (with
  *   its own workspace size).  The result is that of the values that the codes stand for.  Dh 64, 128 or 256.
+ *   To what: o is rounded to bf16.  Sums are in 32 bits.  A position's weight is held to 2^-9 of itself, or, where the
+ *   weight times its block's 2^e (of V) lies below 2^-19 of the row's largest such product, to 2^-28 of that: 2^-22 of the
+ *   row's largest weight at most where its block's e lies no more than 6 below the largest, and else, for all such
+ *   positions of a row together, 2^-7 of the sum of its weights.  A score is off by at most 2^-8 (in log2 units) for what
+ *   is held of a query's values below 2^-13 of its row's largest.  Rows for which these bounds do not hold (blocks of V
+ *   some 2^10 and more apart, or query values as far apart that meet K as much larger) are computed in 32 bits, position
+ *   by position: as exact, but a step with many such rows takes 40 to 200 times as long.
  *
  * hd_pages_copy_q8 -- hd_pages_copy for codes (page_bytes = Hkv*P*n*Dh, a multiple of 16) and scales (page_scales =
  *   Hkv*P/block_tokens bytes a page).

@@ -597,7 +597,8 @@ def sfa_decode_paged_q8_workspace_bytes(B, max_tokens, n, Hq, Hkv, Dh, mode, win
 def sfa_decode_paged_q8(q, k_pages, v_pages, k_scales, v_scales, page_table, lens, o, n, mode, workspace,
                         max_tokens=None, lse=None, softmax_scale=0.0, window=0, dev_status=None, stream=None):
     """sfa_decode_paged over an 8-bit cache: q, o [B][n][Hq][Dh] bf16, lse [B][Hq][n] float32 or None; the result is that
-    of the values that the codes stand for."""
+    of the values that the codes stand for, to bounds that hdsfa.h gives (rows with blocks of V, or query values, too far
+    apart for them are computed in 32 bits, far slower)."""
     (pages, P, Hkv, Dh, T, B, width), pools = _q8_pools(k_pages, v_pages, k_scales, v_scales, page_table, n)
     if q.dim() != 4:
         raise ValueError("q must be [B][n][Hq][Dh]")

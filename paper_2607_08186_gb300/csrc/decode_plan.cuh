@@ -67,12 +67,12 @@ inline long long q8_range(int maxT, int n, int mode, int window) {
 // rows leave it short ranges; at head dim 64, where a tile has half the bytes for the same softmax, all but a million
 // positions over the heads.
 // Measured (replayed from a graph, us, tcgen05 / mma.sync; sequences x tokens x streams):
-//   16 over 4 of 64     4 x 400 x 3 10.8 / 9.2, 33 x 700 x 3 22.6 / 16.3, 2 x 8192 x 1 13.2 / 10.1, 4 x 6000 x 3 21.4 / 16.9, 8 x
-//                       8192 x 3 32.8 / 30.9, 33 x 3000 x 3 (1.2 M positions over the heads) 43.7 / 44.2, 100 x 3000 x 3 93 / 119
-//   32 over 8 of 128    33 x 12 x 4 11.3 / 9.0, 4 x 25 x 4 7.5 / 8.6, 33 x 25 x 4 10.9 / 10.1, 4 x 50 x 4 9.1 / 10.5, 4 x 1000 x 4
-//                       16.3 / 18.6, 16 x 1000 x 4 26.9 / 39.2
-//   24 over 2 of 256    33 x 20 x 1 9.8 / 8.6, 4 x 400 x 1 12.9 / 9.5, 4 x 1000 x 1 9.8 / 9.8, 33 x 1000 x 1 15.1 / 18.2
-//   more than 16 rows   24 over 2 of 256, 4 x 50 x 4 12.9 / 23.8; 96 over 8 of 128, 16 x 50 x 4 11.8 / 15.1
+//   16 over 4 of 64     4 x 400 x 3 11.2 / 9.3, 33 x 700 x 3 24.4 / 16.9, 2 x 8192 x 1 14.2 / 10.8, 4 x 6000 x 3 22.4 / 18.0, 8 x
+//                       8192 x 3 34.5 / 32.4, 33 x 3000 x 3 (1.2 M positions over the heads) 45.6 / 46.3, 100 x 3000 x 3 98 / 122
+//   32 over 8 of 128    33 x 12 x 4 11.6 / 9.4, 4 x 25 x 4 8.0 / 8.9, 33 x 25 x 4 11.3 / 10.6, 4 x 50 x 4 9.2 / 10.6, 4 x 1000 x 4
+//                       17.0 / 18.4, 16 x 1000 x 4 28.0 / 40.4
+//   24 over 2 of 256    33 x 20 x 1 10.0 / 8.9, 4 x 400 x 1 12.7 / 9.6, 4 x 1000 x 1 10.3 / 10.3, 33 x 1000 x 1 15.3 / 18.1
+//   more than 16 rows   24 over 2 of 256, 4 x 50 x 4 13.8 / 22.0; 96 over 8 of 128, 16 x 50 x 4 12.5 / 14.2
 constexpr int kQ8TmaRows = 8;
 inline bool q8_tc(int Dh, int prow, int rows, long long range, long long heads) {
   const int piece = paged_piece(prow, 128);

@@ -98,7 +98,8 @@ constexpr int kHeld = 4;  // chunks that a thread holds from the maximum to the 
 // A unit is what a call appends to one block of tokens.  For each head and tensor (a pair, of which there are 2 Hkv) a team
 // of threads finds the new rows' largest magnitude, which gives the scale, and codes the rows; they are read once where
 // they fit kHeld chunks a thread.  A block that held tokens before keeps at least its scale, and where that grows the older
-// rows are coded again.  A team is the CTA (a unit and pair each), or as many lanes of a warp as the rows need: then a warp
+// rows are coded again, by the new rows' team (one token of 64 sequences, 8 heads of 128, 4 streams: 2.9 us where no block
+// grows, 14 to 16 where some or all do with 16 tokens a block, 43 to 58 with 64).  A team is the CTA (a unit and pair each), or as many lanes of a warp as the rows need: then a warp
 // takes a unit and finds its place once for all its pairs, or for one in gridDim.y of them where units are few.  (A warp
 // for each unit and pair: 24 prompts of up to 701 tokens, 3 streams, 4 heads of 64, a scale a token 35.7 us.)
 // With offsets, sequence b's units have the numbers from offsets[b] / T + 2 b on: x tokens touch at most x / T + 2
@@ -235,9 +236,9 @@ struct ReadArgs {
 constexpr int kPiece = 128;
 
 // Packed tokens out of the cache: a warp per token and piece (of its n * Hkv * Dh values, K's and V's), a lane's loads of 16
-// codes ahead of its stores.  Bound by the bytes, two thirds of them written (6 prompts of up to 4000 tokens, 4 streams, 8
-// heads of 128: 47.5 us, 5.2 TB/s; a warp that takes all of a token's pieces 53, pieces twice as large 57, stores of 32
-// bytes 50).
+// codes ahead of its stores.  Bound by the latency of a warp's chain (search, page, loads, stores), with DRAM at 47 % and issue
+// at 41 % under ncu (6 prompts of up to 4000 tokens, 4 streams, 8 heads of 128: 47.3 us, 5.2 TB/s; a warp that takes all of a
+// token's pieces 53, pieces twice as large 57, stores of 32 bytes 50).
 __global__ void __launch_bounds__(256) read_q8_kernel(ReadArgs a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const bool report = blockIdx.y == 0;

@@ -5,25 +5,26 @@
 //   o = sum_p 2^(s_p) 2^(ev_p) cv_p / sum_p 2^(s_p),   s_p = c (q . ck_p) 2^(ek_p)   (c: scale * log2 e).
 // The codes go into the products as they are (e4m3 -> f16 is exact), ek multiplies a score, and ev is added to its
 // exponent: with x_p = s_p + ev_p and m the running maximum of x (not of s), P_p = 2^(x_p - m + 15) is at most 2^15, f16
-// holds it to 2^-12 down to 2^-29 of the largest contribution (2^-40 as a subnormal), and
+// holds it to 2^-11 of itself, below 2^-29 of the largest contribution to 2^-40 of that, and
 //   o = sum P_p cv_p / sum P_p 2^(-ev_p):
-// the sum's terms are one fused multiply-add each.  Where V's scales lie so far apart that a term leaves fp32's range although
-// its weight counts (kFarSum), the rows are computed again, a position at a time (exact_row).  The
-// queries are scaled by a power of two for each row, so that f16 holds them as bf16 did (a row's largest to 2^15; values
-// 2^-39 below it lose bits).
+// the sum's terms are one fused multiply-add each.  The queries are scaled by a power of two for each row, so that f16 holds
+// them as bf16 did (a row's largest to 2^15; values from 2^-31 of it down lose bits, and vanish from 2^-39).  Where
+// V's scales lie so far apart that weights that count lose bits (kFar) or leave fp32's range (kFarSum), or K is large where a
+// query lost bits (kMissed), the rows are computed again in fp32, a position at a time (exact_row): right, and 40 to 200
+// times as slow.
 //
 // This kernel takes what the tcgen05 kernel (sfa_decode_q8_tc.cu) does not: pages too small for TMA, and short ranges of few
-// query rows, where it starts and ends sooner.  A warp takes 16 query rows and 32 of a tile's positions; the warps of the
-// row tiles share the tile in shared memory, so up to 64 rows of a K/V head's group read the cache once.  Tiles stream
+// query rows, where it starts and ends sooner.  A warp takes 16 query rows and 32 of a tile's positions (16 with a single row
+// tile at head dim 128); the warps of the row tiles share the tile in shared memory, so up to 64 rows of a K/V head's group read the cache once.  Tiles stream
 // through a ring by 16-byte cp.async, whose rows the threads look up three tiles ahead.  mma.sync m16n8k16 (f16): a
 // thread's four bytes of an ldmatrix row are k = 2t, 2t + 1, 2t + 8, 2t + 9 of the product, so q lies in that order; V's
 // transposed loads bring pairs of head-dim columns for two keys, so even and odd columns are products of their own.
 //
 // Bound by the latency of a tile's chain (table entry, rows, scales, products, softmax) and by the instructions that
 // turn codes into f16: 32 over 8 heads of 128, 4 streams, 4 sequences of 4000 tokens on pages of one token with a scale each
-// take 41.3 us, 14.7 of them the bytes at the copy rate (64 over 8 58, 96 over 8 92).  Bringing larger pieces by TMA here with
-// two sets of warps on alternate tiles gained nothing where this kernel runs (4 x 50 tokens 9.3 us and 10.1 without, 33 x
-// 12 10.9 and 10.0, two sequences of 64 over heads of 64 6.5 and 6.1).
+// take 42.2 us, 14.7 of them the bytes at the copy rate (64 over 8 58, 96 over 8 91.5).  Bringing larger pieces by TMA here
+// with two sets of warps on alternate tiles gained nothing where this kernel runs (33 x 12 tokens 10.9 us and 10.0
+// without, two sequences of 64 over heads of 64 6.5 and 6.1).
 #include <float.h>
 
 #include <algorithm>
@@ -487,7 +488,7 @@ __global__ void __launch_bounds__(Cfg<DH, MT>::kThreads, Cfg<DH, MT>::kPerSm) de
 // a step of 4 streams, CTA a row / warp a row, in us
 //   128 rows   1 x 8192 tokens, 32 over 8 heads of 128 19.0 / 28.0;  384   4 x 8192, 24 over 2 of 256 30.2 / 40.3
 //   512        4 x 4000, 32 over 8 28.9 / 33.3;  1024   8 x 16384 113.6 / 114.5;  2048   16 x 400 22.9 / 19.8
-//   2560       20 x 2000 49.7 / 45.3;  3072   8 x 8192, 96 over 8 101.5 / 96.0;  7680   20 x 2000, 96 over 8 87.0 / 73.1
+//   2560       20 x 2000 49.7 / 45.3;  8 x 8192, 96 over 8 101.5 / 96.0;  7680   20 x 2000, 96 over 8 87.0 / 73.1
 template <int DH>
 __global__ void __launch_bounds__(256) combine_rows_kernel(Args a) {
   constexpr int C = DH / 32, NB = DH == 256 ? 4 : 8, NW = dec::kMaxSplit / 32;  // columns, splits in flight, weights of a lane

@@ -5,13 +5,13 @@
 // have the cached positions or the head dim as their rows, and the few query rows as columns, so that no row of a
 // tile is empty and a thread has one position:
 //   S^T [128 positions x 2 R] = K (e4m3) * [q_hi | q_lo]^T (e4m3): a row's bf16 values, scaled by a power of two to [2^7,
-//     2^8), are hi + lo / 16 in two codes, exact for values down to 2^-14 of the row's largest and to 2^-22 of it below.  K is
-//     read from shared memory once.  Where tensor memory has no room for two columns a row (R = 32 and 64 at head dim
+//     2^8), are hi + lo / 16 in two codes, exact for values down to 2^-13 of the row's largest and to 2^-21 of it below (see
+//     kMissed).  K is read from shared memory once.  Where tensor memory has no room for two columns a row (R = 32 and 64 at head dim
 //     256), three e5m2 codes of the query's f16 form one after another instead, which read K three times.
 //   O^T [Dh x 3 R] += V^T (e4m3) * [P_hi | P_mid | P_lo] (e5m2): three codes of three bits, so P is rounded to nine bits (of
 //     its f16 form), half a step 2^-9 of it.  A row's largest P is 2^5 when its reference is set, and at most 2^15 before
-//     it goes up; the third codes hold 64 times what they stand for, so steps end at 2^-22, 2^-27 of the row's largest.
-//     The three columns are added at the end.
+//     it goes up; the third codes hold 64 times what they stand for, so steps end at 2^-22, 2^-27 of the row's largest
+//     (see kFar).  The three columns are added at the end.
 // A thread of a softmax warp takes its position's scores for its group's 16 rows: scales by 2^ek, adds ev, masks (what
 // a position is visible to is a range of rows), and subtracts the row's reference.  References are the group's (a copy
 // for each warp), and go up only when some P would pass 2^15 (a vote for each tile; every tile after the first few has
@@ -28,10 +28,10 @@
 // three waves of splits and 101 so.
 //
 // Bound by memory at 16 query rows, of 8 heads of 128: 16 sequences of 32768 tokens, 32 over 8 heads, 390 to 397 us (6.9
-// TB/s of codes and scales; 400 at the copy rate), 8 of up to 16384 112 for 103.  With more rows by the softmax warps'
+// TB/s of codes and scales; 400 at the copy rate), 8 of up to 16384 113 for 103.  With more rows by the softmax warps'
 // chain, about 350 instructions for 16 rows of a warp's 32 positions, 2000 cycles a tile for each group at once (clock64,
 // 48 rows: masks and scales 450, waiting for S 240, scores 430, vote 340, codes of P 380, fence 130): these
-// lengths reach 0.88 of the copy rate at 32 rows (117 us), 0.61 at 48, 0.49 at 64; 48 of heads of 256 0.78 (66 for 52); more
+// lengths reach 0.86 of the copy rate at 32 rows (120 us), 0.61 at 48, 0.49 at 64; 48 of heads of 256 0.77 (67.5 for 52); more
 // than 64 rows read the cache once for each group of 64 (8 x 8192, 96 rows, 340 for 104).  Three
 // CTAs an SM at 16 rows (up to head dim 128) hide a tile's chain of barriers: 133 us with two, 114 with three.  Tried and
 // dropped: warps of 24 to 48 rows (registers: fewer warps to hide the latency), two tiles in turn with an O each, two tiles for
