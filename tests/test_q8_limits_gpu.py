@@ -187,3 +187,41 @@ def test_large_queries_over_small_keys(B, n, Hq, Hkv, Dh, P, pages):
     for b in {0, B - 1}:
         assert float((lse[b].double() / lse_r[0] - 1).abs().max()) <= 1e-3
         assert float((o[b].double() - o_r[0]).abs().max()) <= 2.0**-8 * float(o_r.abs().max())
+
+
+# Batches in which some sequences have a page far larger, or queries far apart over large K, and the others do not, of uneven
+# lengths, some empty or on bad pages: CTAs that go on from one to another keep their bounds apart.
+@pytest.mark.parametrize("B,n,Hq,Hkv,Dh,P,pages", [(24, 4, 16, 1, 128, 16, 96), (40, 4, 12, 1, 256, 16, 48), (128, 2, 16, 1, 64, 16, 60), (33, 4, 96, 4, 128, 16, 40),
+                                                   (60, 1, 4, 1, 128, 4, 200), (4, 4, 4, 1, 128, 16, 96)])
+def test_sequences_far_apart_beside_ordinary_ones(B, n, Hq, Hkv, Dh, P, pages):
+    rows = (Hkv, P * n, Dh)
+    huge = _normal(2, *rows) * 100
+    huge[..., 1:] = 0.0
+    k_large = _normal(3, *rows) * 100
+    k_large[..., 0] = 0.0
+    usual = (_normal(4, *rows) * 100, -6, _normal(5, *rows) * 100, -30)
+    kinds = [usual, (_normal(6, *rows) * 100, -6, huge, 10), (k_large, 13, _normal(7, *rows) * 100, -30), (_normal(8, *rows) * 100, -6, _normal(9, *rows), q8.E_MAX)]
+    orders = [[0] * pages, [0] * pages, [2] * pages, [0] * pages]
+    orders[1][pages // 3], orders[3][1] = 1, 3
+    caches = [_cache(kinds, o, n, P) for o in orders]
+    k, v, ks, vs = caches[0][:4]
+    which = [(b * 7 // 3) % 4 for b in range(B)]
+    lens = [pages * P - (b * 53) % (pages * P - P) for b in range(B)]
+    lens[1] = 0
+    table = torch.cat([caches[w][4] for w in which]).clone()
+    table[2, 0] = -1
+    small = _normal(10, 1, n, Hq, Dh)
+    apart = small.clone()
+    apart[..., 1:] *= 2.0**-20
+    apart[..., 0] = 1.5
+    q = torch.cat([apart if w == 2 else small for w in which]).to(BF)
+    for mode, window in ((CROSS, 0), (LOCAL, 30 * n), (WITHIN, 0)):
+        o, lse, st = _decode(q, k, v, ks, vs, table, _i32(lens), n, mode, window)
+        assert st == (binding.HD_DEVBIT_INDEX if mode != LOCAL else st)
+        for b in (1, 2) if mode != LOCAL else (1,):
+            assert torch.count_nonzero(o[b]) == 0 and bool((lse[b] == -float("inf")).all())
+        for b in ({0, B - 1} | set(range(3, min(B, 12)))) - {1, 2}:
+            kv, vv = caches[which[b]][5:]
+            _assert_columns(o[b:b + 1], q[b:b + 1], kv, vv, lens[b], n, mode, window)
+            _, lse_r, _ = oracle.decode(q[b:b + 1], kv, vv, _i32([lens[b]]), n, mode, window=window)
+            assert float((lse[b].double() - lse_r[0]).abs().max()) <= 1e-3
